@@ -49,7 +49,8 @@ typedef enum gnmr_status {
 
 typedef enum gnmr_dtype {
     GNMR_DTYPE_F32 = 0,       /* IEEE binary32 gradients */
-    GNMR_DTYPE_BF16 = 1       /* bfloat16 gradients */
+    GNMR_DTYPE_BF16 = 1,      /* bfloat16 gradients */
+    GNMR_DTYPE_F16 = 2        /* IEEE binary16: the expert products and the 8-bit codes only */
 } gnmr_dtype;
 
 /* Controller configuration (Sec. 3.3-3.4).  gnmr_config_defaults fills it
@@ -390,6 +391,109 @@ gnmr_status gnmr_actuator_destroy(gnmr_actuator *a);
 gnmr_status gnmr_unit_norms_static(const void *d_arena, int64_t arena_elems, int32_t dtype,
                                    int32_t num_units, const int64_t *offsets,
                                    const int64_t *lengths, double *d_norms, void *stream);
+
+/* ---- Expert products: the two paths of a linear unit --------------------
+ * The mask decides, per unit, which path its linear takes; these calls are the
+ * products of both.  The recovery path multiplies in 16 bits, the low-cost path
+ * on 8-bit integer codes with one scale per token and one per channel (the
+ * paper's INT8 recipe, App. E.3).  Both are grouped: an expert (group) g has
+ * the rows d_offsets[g] up to d_offsets[g + 1] of the activations and a weight
+ * W_g of its own, [n_out x n_in]; a dense linear is one group.  With x the
+ * inputs [rows x n_in] and dy the outputs' gradients [rows x n_out]:
+ *
+ *   GNMR_PRODUCT_FORWARD      out[r] = W_g x[r]            (r in group g)
+ *   GNMR_PRODUCT_INPUT_GRAD   out[r] = W_g^T dy[r]
+ *   GNMR_PRODUCT_WEIGHT_GRAD  out_g  = sum over g's rows of dy[r] x[r]^T,
+ *                             or that added to out_g (a group without rows
+ *                             gives zeros, or is left as it is)
+ *   GNMR_PRODUCT_FORWARD_I8   out[r] = x_scale[r] * w_scale_g * (W_g x[r]),
+ *                             W and x being 8-bit codes
+ *
+ * The backward pass of the 8-bit path is GNMR_PRODUCT_FORWARD_I8 on the codes
+ * of dy and of W_g^T (gnmr_quantize_columns), n_out and n_in exchanged.
+ *
+ * Sums are held in 32 bits: fp32 for 16-bit operands, exact integers for codes
+ * (n_in up to 131,071), and rounded once to the output's type.  Infinities and
+ * NaNs reach the outputs that they belong to and no others.  A call repeated on
+ * the same operands gives the same bits. */
+typedef enum gnmr_product_op {
+    GNMR_PRODUCT_FORWARD = 0,
+    GNMR_PRODUCT_INPUT_GRAD = 1,
+    GNMR_PRODUCT_WEIGHT_GRAD = 2,
+    GNMR_PRODUCT_FORWARD_I8 = 3
+} gnmr_product_op;
+
+/* One product.  Strides are in elements; every matrix is row-major with
+ * contiguous rows.  A row stride that is a multiple of 16 bytes, with base and
+ * group strides alike, is read in place; other operands are first copied to
+ * d_scratch (gnmr_products_scratch_bytes). */
+typedef struct gnmr_product {
+    int32_t op;                /* gnmr_product_op */
+    int32_t groups;            /* 1 .. 2048 */
+    int64_t rows;              /* rows of x / dy, 0 .. 2^31 - 1 */
+    int32_t n_out, n_in;       /* W_g is [n_out x n_in], each >= 1 */
+    int32_t dtype;             /* 16-bit operands: GNMR_DTYPE_BF16 or _F16; ignored for codes */
+    int32_t out_dtype;         /* BF16, F16 or F32; 16-bit products: dtype or F32 */
+    const int64_t *d_offsets;  /* device [groups + 1], not decreasing, within [0, rows]; values outside
+                                * are taken as the nearest allowed.  NULL (groups = 1): all rows */
+    const uint8_t *d_mask;     /* device, a byte every mask_stride bytes for each group, as written by
+                                * gnmr_step; the 16-bit products compute the groups whose byte is not 0,
+                                * the 8-bit product those whose byte is 0; NULL: all groups.  The other
+                                * groups' outputs are left as they are */
+    int64_t mask_stride;
+    const void *d_x;           /* FORWARD, WEIGHT_GRAD, FORWARD_I8 */
+    int64_t x_stride;          /* >= n_in */
+    const void *d_dy;          /* INPUT_GRAD, WEIGHT_GRAD */
+    int64_t dy_stride;         /* >= n_out */
+    const void *d_w;           /* FORWARD, INPUT_GRAD, FORWARD_I8 */
+    int64_t w_stride;          /* >= n_in */
+    int64_t w_group_stride;    /* >= 0; groups may share a weight (0) */
+    const float *d_x_scale;    /* FORWARD_I8: [rows] */
+    const float *d_w_scale;    /* FORWARD_I8: [groups x n_out] */
+    void *d_out;               /* [rows x n_out], [rows x n_in], or per group [n_out x n_in]; no operand */
+    int64_t out_stride;
+    int64_t out_group_stride;  /* WEIGHT_GRAD: groups must not overlap */
+    int32_t add;               /* WEIGHT_GRAD: add to d_out instead of writing it */
+    void *d_scratch;           /* 256-byte aligned, used during the call only; NULL if none is needed */
+    int64_t scratch_bytes;
+} gnmr_product;
+
+/* A handle holds what the products need beside their operands: one device
+ * allocation made here, of about 39 MiB, for sums that several SMs
+ * share.  It is not tied to any size; one serves every layer of a model.  As
+ * with the monitor: one host thread and one stream at a time. */
+typedef struct gnmr_products gnmr_products;
+gnmr_status gnmr_products_create(int32_t device, gnmr_products **out);
+
+/* Enqueues one product on `stream`.  Errors: GNMR_ERR_INVALID_ARG,
+ * GNMR_ERR_LAYOUT (strides, alignment, or scratch too small), GNMR_ERR_CUDA,
+ * GNMR_ERR_STATE (an earlier product of this handle gave up waiting inside the
+ * GPU; its output is not valid); detail via gnmr_last_error(NULL). */
+gnmr_status gnmr_products_run(gnmr_products *h, const gnmr_product *p, void *stream);
+
+/* Scratch that gnmr_products_run needs for *p (d_scratch and scratch_bytes are
+ * not read).  Makes no CUDA call.  Errors: GNMR_ERR_INVALID_ARG, GNMR_ERR_LAYOUT. */
+gnmr_status gnmr_products_scratch_bytes(const gnmr_product *p, int64_t *bytes);
+
+/* Waits for the handle's device and frees the handle.  NULL is accepted. */
+gnmr_status gnmr_products_destroy(gnmr_products *h);
+
+/* 8-bit codes of `groups` [rows x cols] matrices (BF16, F16 or F32; strides in
+ * elements), one scale for every row: amax = max |x|, q = round(x * (127 * (1 / amax))),
+ * halves to even, scale = amax / 127, each operation rounded to fp32.  A row whose amax is 0, or so
+ * small that 127 / amax overflows, has codes and scale 0; one that holds a NaN or
+ * an infinity has codes 0 and scale NaN.  Runs on the calling thread's current
+ * device and allocates nothing.  d_scale: [groups x rows].  Errors:
+ * GNMR_ERR_INVALID_ARG, GNMR_ERR_LAYOUT, GNMR_ERR_CUDA. */
+gnmr_status gnmr_quantize_rows(const void *d_x, int32_t dtype, int32_t groups, int64_t rows, int64_t cols,
+                               int64_t x_stride, int64_t x_group_stride, int8_t *d_q, int64_t q_stride,
+                               int64_t q_group_stride, float *d_scale, void *stream);
+
+/* The same with one scale for every column, and the codes transposed: d_q is
+ * [cols x rows] per group, d_scale [groups x cols]. */
+gnmr_status gnmr_quantize_columns(const void *d_x, int32_t dtype, int32_t groups, int64_t rows, int64_t cols,
+                                  int64_t x_stride, int64_t x_group_stride, int8_t *d_q, int64_t q_stride,
+                                  int64_t q_group_stride, float *d_scale, void *stream);
 
 #ifdef __cplusplus
 }

@@ -7,9 +7,12 @@ kernel launch per training step, behind the C ABI in ``include/gnmr.h``.
 
 * :mod:`._native` -- ctypes binding with the C entry points' names.
 * :class:`Monitor` -- torch-facing wrapper (torch supplies memory and streams).
+* :class:`ExpertProducts`, :func:`expert_linear` -- the products of the units that the
+  mask chooses a path for: 16-bit and 8-bit, grouped by expert, with their gradients.
 * :mod:`.build` -- compiles ``libgnmr.so`` for sm_103a.
 """
 from ._native import GnmrError, load  # noqa: F401
 from .monitor import Monitor  # noqa: F401
+from .products import ExpertProducts, expert_linear  # noqa: F401
 
-__all__ = ["Monitor", "GnmrError", "load"]
+__all__ = ["Monitor", "ExpertProducts", "expert_linear", "GnmrError", "load"]

@@ -20,10 +20,14 @@ GNMR_ERR_STATE = 5
 
 GNMR_DTYPE_F32 = 0
 GNMR_DTYPE_BF16 = 1
+GNMR_DTYPE_F16 = 2
 
 GNMR_FQ_NONE, GNMR_FQ_E2M1, GNMR_FQ_E3M2, GNMR_FQ_E4M3, GNMR_FQ_E5M2 = 0, 1, 2, 3, 4
 
 GNMR_POLICY_ACTIVE_CAP, GNMR_POLICY_ADMISSION_CAP, GNMR_POLICY_STATIC_TOP = 0, 1, 2
+GNMR_PRODUCT_FORWARD, GNMR_PRODUCT_INPUT_GRAD = 0, 1
+GNMR_PRODUCT_WEIGHT_GRAD, GNMR_PRODUCT_FORWARD_I8 = 2, 3
+
 GNMR_LOOP_AUTO, GNMR_LOOP_SMALL_UNITS, GNMR_LOOP_LARGE_UNITS = 0, 1, 2
 
 _P = ctypes.c_void_p
@@ -86,6 +90,36 @@ class gnmr_info(ctypes.Structure):
     ]
 
 
+class gnmr_product(ctypes.Structure):
+    _fields_ = [
+        ("op", ctypes.c_int32),
+        ("groups", ctypes.c_int32),
+        ("rows", ctypes.c_int64),
+        ("n_out", ctypes.c_int32),
+        ("n_in", ctypes.c_int32),
+        ("dtype", ctypes.c_int32),
+        ("out_dtype", ctypes.c_int32),
+        ("d_offsets", _P),
+        ("d_mask", _P),
+        ("mask_stride", ctypes.c_int64),
+        ("d_x", _P),
+        ("x_stride", ctypes.c_int64),
+        ("d_dy", _P),
+        ("dy_stride", ctypes.c_int64),
+        ("d_w", _P),
+        ("w_stride", ctypes.c_int64),
+        ("w_group_stride", ctypes.c_int64),
+        ("d_x_scale", _P),
+        ("d_w_scale", _P),
+        ("d_out", _P),
+        ("out_stride", ctypes.c_int64),
+        ("out_group_stride", ctypes.c_int64),
+        ("add", ctypes.c_int32),
+        ("d_scratch", _P),
+        ("scratch_bytes", ctypes.c_int64),
+    ]
+
+
 class GnmrError(RuntimeError):
     def __init__(self, status: int, detail: str):
         super().__init__(f"{status_string(status)} ({detail})" if detail else status_string(status))
@@ -116,6 +150,16 @@ PROTOTYPES = {
     "gnmr_finish": (ctypes.c_int, [_P, _P, _P, _P, ctypes.POINTER(gnmr_stats)]),
     "gnmr_get_state": (ctypes.c_int, [_P, _P, _P, ctypes.c_int64, ctypes.POINTER(ctypes.c_int64)]),
     "gnmr_set_state": (ctypes.c_int, [_P, _P, _P, ctypes.c_int64]),
+    "gnmr_products_create": (ctypes.c_int, [ctypes.c_int32, ctypes.POINTER(_P)]),
+    "gnmr_products_run": (ctypes.c_int, [_P, _P, _P]),
+    "gnmr_products_scratch_bytes": (ctypes.c_int, [_P, _P]),
+    "gnmr_products_destroy": (ctypes.c_int, [_P]),
+    "gnmr_quantize_rows": (ctypes.c_int, [_P, ctypes.c_int32, ctypes.c_int32, ctypes.c_int64, ctypes.c_int64,
+                                          ctypes.c_int64, ctypes.c_int64, _P, ctypes.c_int64,
+                                          ctypes.c_int64, _P, _P]),
+    "gnmr_quantize_columns": (ctypes.c_int, [_P, ctypes.c_int32, ctypes.c_int32, ctypes.c_int64, ctypes.c_int64,
+                                             ctypes.c_int64, ctypes.c_int64, _P, ctypes.c_int64,
+                                             ctypes.c_int64, _P, _P]),
 }
 
 _lib = None
@@ -255,3 +299,37 @@ def gnmr_actuator_apply(handle: int, d_in: int, d_out: int, arena_elems: int, d_
 
 def gnmr_actuator_destroy(handle: int) -> None:
     _check(load().gnmr_actuator_destroy(handle), None)
+
+
+def gnmr_products_create(device: int = 0) -> int:
+    h = _P()
+    _check(load().gnmr_products_create(int(device), ctypes.byref(h)), None)
+    return h.value
+
+
+def gnmr_products_run(handle: int, p: gnmr_product, stream: int = 0) -> None:
+    _check(load().gnmr_products_run(handle, ctypes.addressof(p), stream), None)
+
+
+def gnmr_products_scratch_bytes(p: gnmr_product) -> int:
+    n = ctypes.c_int64(0)
+    _check(load().gnmr_products_scratch_bytes(ctypes.addressof(p), ctypes.addressof(n)), None)
+    return n.value
+
+
+def gnmr_products_destroy(handle: int) -> None:
+    _check(load().gnmr_products_destroy(handle), None)
+
+
+def gnmr_quantize_rows(d_x: int, dtype: int, groups: int, rows: int, cols: int, x_stride: int,
+                       x_group_stride: int, d_q: int, q_stride: int, q_group_stride: int, d_scale: int,
+                       stream: int = 0) -> None:
+    _check(load().gnmr_quantize_rows(d_x, dtype, groups, rows, cols, x_stride, x_group_stride, d_q, q_stride,
+                                     q_group_stride, d_scale, stream), None)
+
+
+def gnmr_quantize_columns(d_x: int, dtype: int, groups: int, rows: int, cols: int, x_stride: int,
+                          x_group_stride: int, d_q: int, q_stride: int, q_group_stride: int, d_scale: int,
+                          stream: int = 0) -> None:
+    _check(load().gnmr_quantize_columns(d_x, dtype, groups, rows, cols, x_stride, x_group_stride, d_q, q_stride,
+                                        q_group_stride, d_scale, stream), None)

@@ -18,7 +18,8 @@ BUILD_DIR = os.path.join(PKG, "_build")
 LIB_PATH = os.path.join(PKG, "libgnmr.so")
 
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
-CUDA_SOURCES = ["gnmr_kernels.cu", "gnmr_static.cu", "gnmr_actuator.cu"]
+CUDA_SOURCES = ["gnmr_kernels.cu", "gnmr_static.cu", "gnmr_actuator.cu", "gnmr_products.cu",
+                "gnmr_quantize.cu"]
 CXX_SOURCES = ["gnmr_api.cpp", "gnmr_plan.cpp"]
 HEADERS = ["gnmr_internal.h", "gnmr_stream.cuh"]
 

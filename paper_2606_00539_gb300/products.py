@@ -1,0 +1,331 @@
+"""torch-facing wrapper of the expert products: the linear units that the recovery mask
+chooses a path for, in 16 bits (recovery path) and on 8-bit integer codes (low-cost
+path), grouped by expert over ragged rows.  PyTorch supplies device memory and the
+stream; every product and every code is computed by libgnmr's kernels."""
+from __future__ import annotations
+
+import ctypes
+
+from . import _native as N
+
+
+def _torch():
+    import torch
+    return torch
+
+
+def _codes_of():
+    torch = _torch()
+    return {torch.bfloat16: N.GNMR_DTYPE_BF16, torch.float16: N.GNMR_DTYPE_F16, torch.float32: N.GNMR_DTYPE_F32}
+
+
+_DTYPES: dict = {}
+
+
+def _dtype_code(dtype):
+    if not _DTYPES:
+        _DTYPES.update(_codes_of())
+    return _DTYPES.get(dtype)
+
+
+def _named_dtype(name):
+    torch = _torch()
+    named = {"bf16": torch.bfloat16, "bfloat16": torch.bfloat16, "f16": torch.float16, "float16": torch.float16,
+             "f32": torch.float32, "float32": torch.float32}
+    if name in named:
+        return named[name]
+    if name in named.values():
+        return name
+    raise ValueError(f"out_dtype must be one of {sorted(named)} or the torch type, got {name!r}")
+
+
+class ExpertProducts:
+    """Products of linear units grouped by expert, on one device.
+
+    Rows lie group by group: group g has the rows offsets[g] up to offsets[g + 1] of the
+    activations (offsets: int64 tensor [groups + 1] on the device, as a router's cumulative
+    counts give it; None for one group of all rows).  Weights are [groups, n_out, n_in], or
+    [n_out, n_in] for one group, with contiguous rows and any strides between rows and
+    groups, so views of a flat arena will do.
+
+    mask: uint8 tensor [groups] on the device (any stride), as Monitor.step returns it for
+    the experts' units: the 16-bit products compute the groups whose entry is not 0, forward_i8 those
+    whose entry is 0, and both leave the other groups' outputs as they are.
+
+    Rows of `out` that belong to no group are left as they are.  stream: a torch stream, default the
+    current one; as with any torch call, tensors that were made on another stream are the
+    caller's to order.  One instance serves any sizes; use it from one stream at a time."""
+
+    def __init__(self, device=0):
+        self._h = None
+        self.device_index = int(device.index if hasattr(device, "index") else device)
+        self._h = N.gnmr_products_create(self.device_index)
+        self._run = N.load().gnmr_products_run
+
+    # -- lifetime -----------------------------------------------------------
+    def close(self) -> None:
+        if self._h:
+            N.gnmr_products_destroy(self._h)
+            self._h = None
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.close()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    # -- argument checks ------------------------------------------------------
+    def _tensor(self, t, name, dims, dtypes):
+        torch = _torch()
+        if not isinstance(t, torch.Tensor) or not t.is_cuda or t.device.index != self.device_index:
+            raise ValueError(f"{name} must be a CUDA tensor on device {self.device_index}")
+        if t.dtype not in dtypes:
+            raise ValueError(f"{name} must be {' or '.join(str(d) for d in dtypes)}, got {t.dtype}")
+        if t.dim() not in dims:
+            raise ValueError(f"{name} must have {' or '.join(str(d) for d in dims)} dimensions, got {t.dim()}")
+        if t.dim() > 1 and t.shape[-1] > 1 and t.stride(-1) != 1:
+            raise ValueError(f"{name} must have contiguous rows")
+        return t
+
+    @staticmethod
+    def _row_stride(t):
+        # a single row has no stride of its own, and torch may give it any
+        return t.stride(-2) if t.shape[-2] > 1 else max(t.stride(-2), t.shape[-1])
+
+    def _weight(self, w, name, dtypes):
+        self._tensor(w, name, (2, 3), dtypes)
+        groups = w.shape[0] if w.dim() == 3 else 1
+        return groups, w.shape[-2], w.shape[-1], self._row_stride(w), w.stride(0) if groups > 1 else 0
+
+    def _grouping(self, p, groups, rows, offsets, mask):
+        torch = _torch()
+        p.groups, p.rows = groups, rows
+        if offsets is not None:
+            self._tensor(offsets, "offsets", (1,), (torch.int64,))
+            if offsets.numel() != groups + 1 or not offsets.is_contiguous():
+                raise ValueError(f"offsets must hold groups + 1 = {groups + 1} contiguous entries")
+            p.d_offsets = offsets.data_ptr()
+        elif groups != 1:
+            raise ValueError("offsets may be None for one group only")
+        if mask is not None:
+            self._tensor(mask, "mask", (1,), (torch.uint8,))
+            if mask.numel() != groups:
+                raise ValueError(f"mask must have one entry per group ({groups})")
+            p.d_mask, p.mask_stride = mask.data_ptr(), mask.stride(0) if groups > 1 else 1
+
+    def _enqueue(self, p, stream, names):
+        torch = _torch()
+        if not self._h:
+            raise ValueError("the products were closed")
+        if stream is None:
+            stream = torch.cuda.current_stream(self.device_index)
+        status = self._run(self._h, ctypes.addressof(p), stream.cuda_stream)
+        if status == N.GNMR_ERR_LAYOUT and not p.d_scratch:
+            # operands that cannot be read in place: room for their copies, on the same stream
+            need = N.gnmr_products_scratch_bytes(p)
+            if need:
+                with torch.cuda.stream(stream):
+                    scratch = torch.empty(need, dtype=torch.uint8, device=torch.device("cuda", self.device_index))
+                p.d_scratch, p.scratch_bytes = scratch.data_ptr(), need
+                status = self._run(self._h, ctypes.addressof(p), stream.cuda_stream)
+        if status:
+            N._check(status, None)
+
+    def _out(self, out, rows, width, dtype, stream):
+        torch = _torch()
+        if out is None:
+            dev = torch.device("cuda", self.device_index)
+            if stream is None:
+                return torch.empty(rows, width, dtype=dtype, device=dev)
+            with torch.cuda.stream(stream):
+                return torch.empty(rows, width, dtype=dtype, device=dev)
+        self._tensor(out, "out", (2,), (dtype,))
+        if tuple(out.shape) != (rows, width):
+            raise ValueError(f"out must be [{rows}, {width}], got {list(out.shape)}")
+        return out
+
+    def _rows(self, t, name, width, dtypes):
+        self._tensor(t, name, (2,), dtypes)
+        if t.shape[1] != width:
+            raise ValueError(f"{name} must have {width} columns, got {t.shape[1]}")
+        return t.shape[0]
+
+    # -- 16-bit products ------------------------------------------------------
+    def _sixteen(self):
+        torch = _torch()
+        return torch.bfloat16, torch.float16
+
+    def _by_rows(self, op, a, name, w, offsets, out, mask, stream):
+        p = N.gnmr_product()
+        groups, p.n_out, p.n_in, p.w_stride, p.w_group_stride = self._weight(w, "w", self._sixteen())
+        across, to = (p.n_in, p.n_out) if op == N.GNMR_PRODUCT_FORWARD else (p.n_out, p.n_in)
+        rows = self._rows(a, name, across, (w.dtype,))
+        self._grouping(p, groups, rows, offsets, mask)
+        out = self._out(out, rows, to, w.dtype, stream)
+        p.op = op
+        p.dtype = p.out_dtype = _dtype_code(w.dtype)
+        p.d_w = w.data_ptr()
+        if op == N.GNMR_PRODUCT_FORWARD:
+            p.d_x, p.x_stride = a.data_ptr(), self._row_stride(a)
+        else:
+            p.d_dy, p.dy_stride = a.data_ptr(), self._row_stride(a)
+        p.d_out, p.out_stride = out.data_ptr(), self._row_stride(out)
+        self._enqueue(p, stream, (name, "w", "out"))
+        return out
+
+    def forward(self, x, w, offsets=None, *, out=None, mask=None, stream=None):
+        """y[r] = W_g x[r] for the rows r of every group g: x [rows, n_in] -> [rows, n_out]."""
+        return self._by_rows(N.GNMR_PRODUCT_FORWARD, x, "x", w, offsets, out, mask, stream)
+
+    def input_grad(self, dy, w, offsets=None, *, out=None, mask=None, stream=None):
+        """dx[r] = W_g^T dy[r]: dy [rows, n_out] -> [rows, n_in]."""
+        return self._by_rows(N.GNMR_PRODUCT_INPUT_GRAD, dy, "dy", w, offsets, out, mask, stream)
+
+    def weight_grad(self, dy, x, offsets=None, *, out, add=False, mask=None, stream=None):
+        """out_g = sum over the group's rows of dy[r] x[r]^T, or that added to out_g.
+
+        out: [groups, n_out, n_in] (or [n_out, n_in]) of dy's type or fp32, e.g. a view of
+        the gradient arena that the monitor reads.  A group without rows gets zeros
+        (nothing is added)."""
+        torch = _torch()
+        p = N.gnmr_product()
+        self._tensor(dy, "dy", (2,), self._sixteen())
+        groups, p.n_out, p.n_in, p.out_stride, p.out_group_stride = self._weight(out, "out", (dy.dtype, torch.float32))
+        rows = self._rows(dy, "dy", p.n_out, (dy.dtype,))
+        if self._rows(x, "x", p.n_in, (dy.dtype,)) != rows:
+            raise ValueError("dy and x must have the same number of rows")
+        self._grouping(p, groups, rows, offsets, mask)
+        p.op, p.add = N.GNMR_PRODUCT_WEIGHT_GRAD, int(bool(add))
+        p.dtype, p.out_dtype = _dtype_code(dy.dtype), _dtype_code(out.dtype)
+        p.d_dy, p.dy_stride = dy.data_ptr(), self._row_stride(dy)
+        p.d_x, p.x_stride = x.data_ptr(), self._row_stride(x)
+        p.d_out = out.data_ptr()
+        self._enqueue(p, stream, ("dy", "x", "out"))
+        return out
+
+    # -- 8-bit products -------------------------------------------------------
+    def _quantize(self, x, columns, stream):
+        torch = _torch()
+        self._tensor(x, "x", (2, 3), (torch.bfloat16, torch.float16, torch.float32))
+        groups, rows, cols = x.shape[0] if x.dim() == 3 else 1, x.shape[-2], x.shape[-1]
+        high, wide = (cols, rows) if columns else (rows, cols)
+        held = (wide + 15) // 16 * 16              # rows of codes start at multiples of 16 bytes
+        dev = torch.device("cuda", self.device_index)
+        if stream is None:
+            stream = torch.cuda.current_stream(self.device_index)
+        with torch.cuda.stream(stream):
+            q = torch.empty(*x.shape[:-2], high, held, dtype=torch.int8, device=dev)
+            scale = torch.empty(*x.shape[:-2], high, dtype=torch.float32, device=dev)
+            fn = N.gnmr_quantize_columns if columns else N.gnmr_quantize_rows
+            fn(x.data_ptr(), _dtype_code(x.dtype), groups, rows, cols, self._row_stride(x),
+               x.stride(0) if groups > 1 else 0, q.data_ptr(), held, high * held, scale.data_ptr(),
+               stream.cuda_stream)
+        return q[..., :wide], scale
+
+    def quantize_rows(self, x, *, stream=None):
+        """8-bit codes of every row of x ([rows, cols] or [groups, rows, cols]; bf16, f16 or
+        fp32) and its scale: (int8 codes of x's shape, fp32 scales).  round(x * (127 * (1 / amax))),
+        halves to even; x is about codes * scale.  Activations by token, weights by output channel."""
+        return self._quantize(x, False, stream)
+
+    def quantize_columns(self, w, *, stream=None):
+        """8-bit codes of every column of w, transposed, and its scale: ([..., cols, rows],
+        [..., cols]).  Weights by input channel, for the backward product of the 8-bit path:
+        dx = forward_i8(codes of dy, ..., codes of w's columns, ...)."""
+        return self._quantize(w, True, stream)
+
+    def forward_i8(self, xq, x_scale, wq, w_scale, offsets=None, *, out=None, out_dtype="bf16", mask=None,
+                   stream=None):
+        """y[r] = x_scale[r] * w_scale_g * (Wq_g xq[r]) on 8-bit codes; the sum is an exact
+        integer (n_in up to 131,071), rounded once to out's type."""
+        torch = _torch()
+        p = N.gnmr_product()
+        groups, p.n_out, p.n_in, p.w_stride, p.w_group_stride = self._weight(wq, "wq", (torch.int8,))
+        rows = self._rows(xq, "xq", p.n_in, (torch.int8,))
+        self._grouping(p, groups, rows, offsets, mask)
+        for t, name, n in ((x_scale, "x_scale", rows), (w_scale, "w_scale", groups * p.n_out)):
+            self._tensor(t, name, (1, 2), (torch.float32,))
+            if t.numel() != n or not t.is_contiguous():
+                raise ValueError(f"{name} must hold {n} contiguous entries")
+        if out is not None:
+            self._tensor(out, "out", (2,), (torch.bfloat16, torch.float16, torch.float32))
+            out = self._out(out, rows, p.n_out, out.dtype, stream)
+        else:
+            out = self._out(None, rows, p.n_out, _named_dtype(out_dtype), stream)
+        p.op, p.out_dtype = N.GNMR_PRODUCT_FORWARD_I8, _dtype_code(out.dtype)
+        p.d_x, p.x_stride, p.d_x_scale = xq.data_ptr(), self._row_stride(xq), x_scale.data_ptr()
+        p.d_w, p.d_w_scale = wq.data_ptr(), w_scale.data_ptr()
+        p.d_out, p.out_stride = out.data_ptr(), self._row_stride(out)
+        self._enqueue(p, stream, ("xq", "wq", "out"))
+        return out
+
+
+def _expert_linear_function():
+    torch = _torch()
+
+    class ExpertLinear(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, w, products, offsets, mask, grad, codes):
+            x, w = x.detach(), w.detach()
+            y = torch.empty(x.shape[0], w.shape[-2], dtype=x.dtype, device=x.device)
+            products.forward(x, w, offsets, out=y, mask=mask)
+            if mask is not None:
+                xq, xs = products.quantize_rows(x)
+                wq, ws = codes[:2] if codes is not None else products.quantize_rows(w)
+                products.forward_i8(xq, xs, wq, ws, offsets, out=y, mask=mask)
+            ctx.products, ctx.grad, ctx.codes = products, grad, codes
+            ctx.save_for_backward(x, w, *(t for t in (offsets, mask) if t is not None))
+            ctx.has = (offsets is not None, mask is not None)
+            return y
+
+        @staticmethod
+        def backward(ctx, dy):
+            x, w, *rest = ctx.saved_tensors
+            offsets = rest.pop(0) if ctx.has[0] else None
+            mask = rest.pop(0) if ctx.has[1] else None
+            products, dx, dw = ctx.products, None, None
+            dy = dy.contiguous()
+            if ctx.needs_input_grad[0]:
+                dx = torch.empty_like(x, memory_format=torch.contiguous_format)
+                products.input_grad(dy, w, offsets, out=dx, mask=mask)
+                if mask is not None:
+                    dq, ds = products.quantize_rows(dy)
+                    vq, vs = ctx.codes[2:] if ctx.codes is not None else products.quantize_columns(w)
+                    products.forward_i8(dq, ds, vq, vs, offsets, out=dx, mask=mask)
+            if ctx.grad is not None:
+                products.weight_grad(dy, x, offsets, out=ctx.grad)
+            elif ctx.needs_input_grad[1]:
+                dw = torch.empty_like(w, memory_format=torch.contiguous_format)
+                products.weight_grad(dy, x, offsets, out=dw)
+            return dx, dw, None, None, None, None, None
+
+    return ExpertLinear
+
+
+_ExpertLinear = None
+
+
+def expert_linear(products, x, w, offsets=None, mask=None, grad=None, *, codes=None):
+    """A linear layer of experts with a backward pass, each expert on the path that the
+    mask gives it: 16 bits where its entry is not 0, 8-bit codes where it is 0 (16 bits
+    everywhere without a mask).
+
+    x: [rows, n_in], every row in some group; w: [groups, n_out, n_in]; offsets and mask as in
+    :class:`ExpertProducts`; the mask is read again in the backward pass, which follows the
+    same paths.  Gradients pass through the codes as if they were the values they stand for
+    (straight through); the weights' gradient is the 16-bit product for every expert.
+
+    grad: where the weights' gradient is written, e.g. the experts' part of the arena that
+    the monitor reads; the backward pass then writes all of it, and w gets no gradient
+    from autograd.  codes: (wq, ws, vq, vs) of quantize_rows(w) and quantize_columns(w), for
+    weights that do not change; by default both are made anew in each pass."""
+    global _ExpertLinear
+    if _ExpertLinear is None:
+        _ExpertLinear = _expert_linear_function()
+    return _ExpertLinear.apply(x, w, products, offsets, mask, grad, codes)
