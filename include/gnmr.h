@@ -430,8 +430,8 @@ typedef enum gnmr_product_op {
 typedef struct gnmr_product {
     int32_t op;                /* gnmr_product_op */
     int32_t groups;            /* 1 .. 2048 */
-    int64_t rows;              /* rows of x / dy, 0 .. 2^31 - 1 */
-    int32_t n_out, n_in;       /* W_g is [n_out x n_in], each >= 1 */
+    int64_t rows;              /* rows of x / dy, 0 .. 2^30 - 1 */
+    int32_t n_out, n_in;       /* W_g is [n_out x n_in], each 1 .. 2^30 - 1 */
     int32_t dtype;             /* 16-bit operands: GNMR_DTYPE_BF16 or _F16; ignored for codes */
     int32_t out_dtype;         /* BF16, F16 or F32; 16-bit products: dtype or F32 */
     const int64_t *d_offsets;  /* device [groups + 1], not decreasing, within [0, rows]; values outside
@@ -459,7 +459,7 @@ typedef struct gnmr_product {
 } gnmr_product;
 
 /* A handle holds what the products need beside their operands: one device
- * allocation made here, of about 39 MiB, for sums that several SMs
+ * allocation made here, of about 40 MiB, for sums that several SMs
  * share.  It is not tied to any size; one serves every layer of a model.  As
  * with the monitor: one host thread and one stream at a time. */
 typedef struct gnmr_products gnmr_products;

@@ -21,7 +21,7 @@ ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 CUDA_SOURCES = ["gnmr_kernels.cu", "gnmr_static.cu", "gnmr_actuator.cu", "gnmr_products.cu",
                 "gnmr_quantize.cu"]
 CXX_SOURCES = ["gnmr_api.cpp", "gnmr_plan.cpp"]
-HEADERS = ["gnmr_internal.h", "gnmr_stream.cuh"]
+HEADERS = ["gnmr_internal.h", "gnmr_stream.cuh", "gnmr_mma.cuh"]
 
 
 def _cuda_home() -> str:

@@ -1,0 +1,179 @@
+// sm_103a building blocks of the expert products: barriers in shared memory with
+// bounded waits, tile loads by the TMA unit, and the fifth-generation tensor cores
+// (tcgen05) used by pairs of CTAs.
+#pragma once
+
+#include <cuda.h>
+#include <cuda_runtime.h>
+
+#include <cstdint>
+
+namespace gnmr_mma {
+
+__device__ __forceinline__ uint32_t smem_addr(const void *p)
+{
+    return static_cast<uint32_t>(__cvta_generic_to_shared(p));
+}
+
+__device__ __forceinline__ uint32_t cta_rank()
+{
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+
+// The same shared-memory address in CTA `rank` of the cluster.
+__device__ __forceinline__ uint32_t in_cta(uint32_t addr, uint32_t rank)
+{
+    uint32_t a;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(addr), "r"(rank));
+    return a;
+}
+
+__device__ __forceinline__ void cluster_sync()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+// ---- barriers ---------------------------------------------------------------
+
+__device__ __forceinline__ void barrier_init(uint32_t bar, uint32_t count)
+{
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+
+__device__ __forceinline__ void barrier_init_fence()
+{
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+}
+
+// Arrives on a barrier of any CTA of the cluster (an address from in_cta).
+__device__ __forceinline__ void arrive(uint32_t bar)
+{
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+
+__device__ __forceinline__ void arrive_expect(uint32_t bar, uint32_t bytes)
+{
+    asm volatile("mbarrier.arrive.expect_tx.release.cluster.shared::cluster.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes)
+                 : "memory");
+}
+
+// Every wait ends: after kWaits tries (tens of milliseconds at the least, where a
+// wait of a running kernel takes microseconds) it returns false, and its caller
+// leaves its loop.
+constexpr int kWaits = 1 << 20;
+
+__device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity)
+{
+    for (int i = 0; i < kWaits; ++i) {
+        uint32_t done;
+        asm volatile("{\n.reg .pred p;\n"
+                     "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n"
+                     "selp.u32 %0, 1, 0, p;\n}"
+                     : "=r"(done)
+                     : "r"(bar), "r"(parity)
+                     : "memory");
+        if (done)
+            return true;
+    }
+    return false;
+}
+
+// ---- tile loads ---------------------------------------------------------------
+// The barrier may be the other CTA's of the pair.
+
+__device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap *map, int x, int y, int z, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
+                 "[%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+                 "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+                 : "memory");
+}
+
+__device__ __forceinline__ void prefetch_map(const CUtensorMap *map)
+{
+    asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
+}
+
+// What generic stores wrote to shared memory, for the tensor cores to read.
+__device__ __forceinline__ void fence_async_proxy()
+{
+    asm volatile("fence.proxy.async;" ::: "memory");
+}
+
+// ---- tensor memory and tensor cores, by pairs of CTAs --------------------------
+
+__device__ __forceinline__ void tmem_alloc(uint32_t smem_result, uint32_t columns)
+{
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_result), "r"(columns)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+}
+
+__device__ __forceinline__ void tmem_free(uint32_t tmem, uint32_t columns)
+{
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(columns) : "memory");
+}
+
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+
+// Shared-memory operand in 128-byte swizzled rows.
+//   rows along the contraction (K-major): 8 rows of 64 elements are 1,024 bytes,
+//     `stride` the bytes to the next 8 rows; `lead` is not used;
+//   rows along the lanes or columns (MN-major): each 128-byte row is 64 of them at
+//     one place of the contraction, `stride` the bytes to the next 8 places,
+//     `lead` those to the next 64 lanes or columns.
+__device__ __forceinline__ uint64_t operand(uint32_t addr, uint32_t lead, uint32_t stride)
+{
+    return static_cast<uint64_t>((addr >> 4) & 0x3fff) | static_cast<uint64_t>((lead >> 4) & 0x3fff) << 16 |
+           static_cast<uint64_t>((stride >> 4) & 0x3fff) << 32 | uint64_t(1) << 46 | uint64_t(2) << 61;
+}
+
+// 256 lanes (128 in each CTA) by `columns`, 16-bit operands of one type, fp32 sums.
+__device__ __forceinline__ uint32_t shape(bool bf16, bool a_along_lanes, bool b_along_columns, uint32_t columns)
+{
+    const uint32_t type = bf16 ? 1 : 0;
+    return 1u << 4 | type << 7 | type << 10 | (a_along_lanes ? 1u << 15 : 0) | (b_along_columns ? 1u << 16 : 0) |
+           (columns >> 3) << 17 | (256u >> 4) << 24;
+}
+
+// One step of 16 along the contraction, by one thread for both CTAs.
+__device__ __forceinline__ void multiply(uint32_t tmem, uint64_t a, uint64_t b, uint32_t shape, bool add)
+{
+    asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\n"
+                 "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(tmem),
+                 "l"(a), "l"(b), "r"(shape), "r"(static_cast<uint32_t>(add))
+                 : "memory");
+}
+
+// Arrives on `bar` in both CTAs once every multiply issued so far is done.
+__device__ __forceinline__ void commit(uint32_t bar)
+{
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
+                 "h"(static_cast<uint16_t>(3))
+                 : "memory");
+}
+
+// 16 columns of this warp's 32 lanes; complete after load_wait.
+__device__ __forceinline__ void load16(uint32_t tmem, uint32_t (&v)[16])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+                 "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
+                   "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+                 : "r"(tmem));
+}
+
+// Until the last load16 of this thread is in; v is named so that nothing reads it earlier.
+__device__ __forceinline__ void load_wait(uint32_t (&v)[16])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(v[0]), "+r"(v[1]), "+r"(v[2]), "+r"(v[3]), "+r"(v[4]), "+r"(v[5]), "+r"(v[6]), "+r"(v[7]),
+                   "+r"(v[8]), "+r"(v[9]), "+r"(v[10]), "+r"(v[11]), "+r"(v[12]), "+r"(v[13]), "+r"(v[14]), "+r"(v[15])
+                 :
+                 : "memory");
+}
+
+}  // namespace gnmr_mma

@@ -51,13 +51,22 @@ def test_operands_read_in_place_need_no_scratch():
     assert N.gnmr_products_scratch_bytes(product(op=N.GNMR_PRODUCT_WEIGHT_GRAD)) == 0
 
 
+def test_other_operands_are_copied_to_scratch():
+    """An odd start, row stride or group stride, and 8-bit codes: rows of 16-bit
+    elements in multiples of eight, each operand's copy in whole 256 bytes."""
+    assert N.gnmr_products_scratch_bytes(product(d_x=4098)) == 256            # 10 x 8
+    assert N.gnmr_products_scratch_bytes(product(n_in=9, x_stride=9, w_stride=16)) == 512          # 10 x 16
+    assert N.gnmr_products_scratch_bytes(product(w_group_stride=129)) == 512  # 2 x 16 x 8
+    assert N.gnmr_products_scratch_bytes(product(w_group_stride=0, d_w=4098)) == 256
+
+
 INVALID, LAYOUT = N.GNMR_ERR_INVALID_ARG, N.GNMR_ERR_LAYOUT
 WG, I8 = N.GNMR_PRODUCT_WEIGHT_GRAD, N.GNMR_PRODUCT_FORWARD_I8
 
 
 @pytest.mark.parametrize("status,over", [
     (INVALID, dict(op=-1)), (INVALID, dict(op=4)), (INVALID, dict(groups=0)), (INVALID, dict(groups=2049)),
-    (INVALID, dict(rows=-1)), (INVALID, dict(rows=1 << 31)), (INVALID, dict(n_out=0)), (INVALID, dict(n_in=0)),
+    (INVALID, dict(rows=-1)), (INVALID, dict(rows=1 << 30)), (INVALID, dict(n_out=0)), (INVALID, dict(n_in=0)),
     (INVALID, dict(dtype=N.GNMR_DTYPE_F32)), (INVALID, dict(dtype=7)), (INVALID, dict(out_dtype=N.GNMR_DTYPE_F16)),
     (INVALID, dict(op=I8, out_dtype=7)), (INVALID, dict(op=I8, n_in=131072, x_stride=131072, w_stride=131072)),
     (INVALID, dict(d_offsets=None)), (INVALID, dict(d_x=None)), (INVALID, dict(d_w=None)), (INVALID, dict(d_out=None)),
