@@ -35,6 +35,14 @@ __device__ __forceinline__ void cluster_sync()
     asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
+// One lane of a converged warp, the same one each time.
+__device__ __forceinline__ bool elected()
+{
+    uint32_t yes;
+    asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(yes));
+    return yes != 0;
+}
+
 // ---- barriers ---------------------------------------------------------------
 
 __device__ __forceinline__ void barrier_init(uint32_t bar, uint32_t count)
@@ -47,21 +55,29 @@ __device__ __forceinline__ void barrier_init_fence()
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
 }
 
-// Arrives on a barrier of any CTA of the cluster (an address from in_cta).
+// Arrivals on a barrier of any CTA of the cluster (an address from in_cta).  The
+// plain ones order nothing but what the tensor cores' and the TMA unit's own rules do: a
+// release would wait for the outputs' stores too (49152 x 2048 -> 1408 over 64 experts
+// 558 us with releases, 290 without).
 __device__ __forceinline__ void arrive(uint32_t bar)
+{
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+
+__device__ __forceinline__ void arrive_release(uint32_t bar)
 {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
 __device__ __forceinline__ void arrive_expect(uint32_t bar, uint32_t bytes)
 {
-    asm volatile("mbarrier.arrive.expect_tx.release.cluster.shared::cluster.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes)
+    asm volatile("mbarrier.arrive.expect_tx.relaxed.cluster.shared::cluster.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes)
                  : "memory");
 }
 
 // Every wait ends: after kWaits tries (tens of milliseconds at the least, where a
 // wait of a running kernel takes microseconds) it returns false, and its caller
-// leaves its loop.
+// leaves its loop.  By a whole warp, which goes on or gives up as one.
 constexpr int kWaits = 1 << 20;
 
 __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity)
@@ -69,15 +85,26 @@ __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity)
     for (int i = 0; i < kWaits; ++i) {
         uint32_t done;
         asm volatile("{\n.reg .pred p;\n"
-                     "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n"
+                     "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n"
                      "selp.u32 %0, 1, 0, p;\n}"
                      : "=r"(done)
                      : "r"(bar), "r"(parity)
                      : "memory");
-        if (done)
+        if (__all_sync(~0u, done))
             return true;
     }
     return false;
+}
+
+// Registers a thread of this warpgroup may use from here on.
+template <int kRegisters> __device__ __forceinline__ void more_registers()
+{
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRegisters));
+}
+
+template <int kRegisters> __device__ __forceinline__ void fewer_registers()
+{
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kRegisters));
 }
 
 // ---- tile loads ---------------------------------------------------------------

@@ -66,8 +66,12 @@ using namespace gnmr_mma;
 constexpr int kLanes = 256;                            // of a pair's tile
 constexpr int kStep = 64;                              // contraction steps of a stage: 128-byte rows of 16 bits
 constexpr int kEpilogueWarps = 8;
-constexpr int kProducerWarp = 0, kMultiplyWarp = 1, kFirstEpilogueWarp = 2, kTailWarp = kFirstEpilogueWarp + kEpilogueWarps;
-constexpr int kThreads = 32 * (kTailWarp + 1);
+constexpr int kProducerWarp = 0, kMultiplyWarp = 1, kTailWarp = 2, kTablesWarp = 3, kFirstEpilogueWarp = 4;
+constexpr int kThreads = 32 * (kFirstEpilogueWarp + kEpilogueWarps);
+// The epilogue's warpgroups hold 128 sums a thread: 216 registers there and 72 in the
+// others' warpgroup, together the 168 a thread that the block is launched with.
+constexpr int kControlRegisters = 72, kEpilogueRegisters = 216;
+static_assert(128 * kControlRegisters + 256 * kEpilogueRegisters <= kThreads * 168, "registers of the launch");
 constexpr int kAStage = 128 * 128;                     // bytes of A's tile in one CTA
 constexpr int kBlock = 64 * 128;                       // bytes of a tile of 64 lanes or columns lying along rows
 
@@ -88,7 +92,6 @@ struct Product {
     const uint8_t *mask;
     int64_t mask_stride;
     int want;                          // groups computed: mask byte != 0 (1), == 0 (0)
-    int a_along_lanes, b_along_columns;
     int a_by_group;                    // A's third coordinate is the group
     int bf16;
     int chunk;                         // stages of a piece
@@ -221,6 +224,14 @@ __device__ __forceinline__ unsigned pack(float lo, float hi, int type)
     return reinterpret_cast<const unsigned &>(v);
 }
 
+// Two columns of this thread's lane become one column of two lanes, the even lane's
+// column j and the odd lane's column j + 1.
+__device__ __forceinline__ unsigned exchange(float vj, float vj1, int type, unsigned which)
+{
+    const unsigned w = pack(vj, vj1, type);
+    return __byte_perm(w, __shfl_xor_sync(~0u, w, 1), which);
+}
+
 __device__ __forceinline__ float load_out(const void *at, int type)
 {
     return type == GNMR_DTYPE_F32    ? *static_cast<const float *>(at)
@@ -234,32 +245,48 @@ __device__ __forceinline__ void store16(const Product &p, const Item &it, int la
 {
     const int64_t base = p.cols ? it.g * p.out_group + int64_t(it.col0 + col) * p.out_col
                                 : int64_t(it.row0 + it.col0 + col) * p.out_col;
-    const int left = it.cols - col;
-    const bool mine = lane < p.lanes;
+    const int left = it.cols - col, odd = lane & 1;
+    const bool whole = left >= 16 && (lane | 31) < p.lanes, mine = lane < p.lanes;
+    const unsigned which = odd ? 0x3276 : 0x5410;
     if (p.out_type == GNMR_DTYPE_F32) {
         float *out = static_cast<float *>(p.out) + base + lane;
-        if (p.add)
+        if (whole) {
+            if (p.add) {
+                float old[16];
+#pragma unroll
+                for (int j = 0; j < 16; ++j)
+                    old[j] = out[j * p.out_col];
+#pragma unroll
+                for (int j = 0; j < 16; ++j)
+                    v[j] += old[j];
+            }
+#pragma unroll
+            for (int j = 0; j < 16; ++j, out += p.out_col)
+                *out = v[j];
+        } else {
 #pragma unroll
             for (int j = 0; j < 16; ++j)
                 if (mine && j < left)
-                    v[j] += out[j * p.out_col];
-#pragma unroll
-        for (int j = 0; j < 16; ++j)
-            if (mine && j < left)
-                out[j * p.out_col] = v[j];
+                    out[j * p.out_col] = p.add ? v[j] + out[j * p.out_col] : v[j];
+        }
         return;
     }
     uint16_t *out = static_cast<uint16_t *>(p.out) + base + lane;
+    if (whole && p.pairs_aligned && !p.add) {
+        out += odd ? p.out_col - 1 : 0;
+#pragma unroll
+        for (int j = 0; j < 16; j += 2, out += 2 * p.out_col)
+            *reinterpret_cast<unsigned *>(out) = exchange(v[j], v[j + 1], p.out_type, which);
+        return;
+    }
     if (p.add)
 #pragma unroll
         for (int j = 0; j < 16; ++j)
             if (mine && j < left)
                 v[j] += load_out(out + j * p.out_col, p.out_type);
-    const int odd = lane & 1;
 #pragma unroll
     for (int j = 0; j < 16; j += 2) {
-        const float other = __shfl_xor_sync(~0u, odd ? v[j] : v[j + 1], 1);
-        const unsigned w = odd ? pack(other, v[j + 1], p.out_type) : pack(v[j], other, p.out_type);
+        const unsigned w = exchange(v[j], v[j + 1], p.out_type, which);
         const int k = j + odd;                       // the column that this thread writes, lanes lane & ~1 and the next
         uint16_t *to = out - odd + k * p.out_col;
         if (k < left) {
@@ -294,18 +321,23 @@ __device__ __forceinline__ void finish16(const Product &p, const Item &it, int l
     store16(p, it, lane, col, v);
 }
 
+// The first piece's sums, or another's added to them.
 template <bool kCodes>
-__device__ __forceinline__ void add_piece(uint32_t (&acc)[16], const uint32_t (&v)[16], bool first)
+__device__ __forceinline__ void begin_sum(uint32_t (&acc)[16])
+{
+    if (kCodes)
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+            acc[j] = __float2int_rn(__uint_as_float(acc[j]));
+}
+
+template <bool kCodes>
+__device__ __forceinline__ void add_to_sum(uint32_t (&acc)[16], const uint32_t (&v)[16])
 {
 #pragma unroll
-    for (int j = 0; j < 16; ++j) {
-        if (kCodes) {
-            const int whole = __float2int_rn(__uint_as_float(v[j]));
-            acc[j] = first ? whole : static_cast<int>(acc[j]) + whole;
-        } else {
-            acc[j] = first ? v[j] : __float_as_uint(__uint_as_float(acc[j]) + __uint_as_float(v[j]));
-        }
-    }
+    for (int j = 0; j < 16; ++j)
+        acc[j] = kCodes ? acc[j] + __float2int_rn(__uint_as_float(v[j]))
+                        : __float_as_uint(__uint_as_float(acc[j]) + __uint_as_float(v[j]));
 }
 
 // ---- the kernel -------------------------------------------------------------------
@@ -319,21 +351,298 @@ struct Barriers {
     unsigned last;                     // whether this CTA is a split tile's last
 };
 
+// What the roles of a CTA share.
+struct Cta {
+    uint8_t *stages;
+    const Tables *tables;
+    Barriers *bars;
+    uint32_t rank, tmem;
+    int pair, pairs, lane_tiles, items;
+};
+
+// The contraction is a group's rows; lanes, or columns, lie along an operand's rows.
+__host__ __device__ constexpr bool rows_deep(int op) { return op == GNMR_PRODUCT_WEIGHT_GRAD; }
+__host__ __device__ constexpr bool a_along_lanes(int op)
+{
+    return op == GNMR_PRODUCT_WEIGHT_GRAD || op == GNMR_PRODUCT_INPUT_GRAD;
+}
+__host__ __device__ constexpr bool b_along_columns(int op) { return op == GNMR_PRODUCT_WEIGHT_GRAD; }
+
+// The roles below are loops of whole warps, of which one lane issues: values that
+// the compiler knows to be the same in all lanes stay in uniform registers, which
+// these instructions take their operands from.
+
+template <int kColumns, int kOp>
+__device__ __forceinline__ bool load_stages(const CUtensorMap &map_a, const CUtensorMap &map_b, const Product &p, const Cta &c)
+{
+    using S = Shape<kColumns>;
+    constexpr int kBoxB = b_along_columns(kOp) ? 64 : S::kBox;
+    const uint32_t full = in_cta(smem_addr(&c.bars->full[0]), 0), empty = smem_addr(&c.bars->empty[0]);
+    const uint32_t tail = smem_addr(&c.bars->tail[0]), base = smem_addr(c.stages);
+    int stage = 0;
+    uint32_t phase = 1;
+    for (int i = c.pair; i < c.items; i += c.pairs) {
+        const Item it = item_of<kColumns>(p, *c.tables, c.lane_tiles, i);
+        const int half = (it.cols + 31) / 32 * 16;                         // B's columns in this CTA
+        const int a_lane = it.lane0 + c.rank * 128, b_col = it.col0 + c.rank * half + (rows_deep(kOp) ? 0 : it.row0);
+        const int boxes = parts_of(half, kBoxB), za = p.a_by_group ? it.g : 0;
+        const uint32_t bytes = kAStage + boxes * kBoxB * 128;
+        int at = it.k0 * kStep + (rows_deep(kOp) ? it.row0 : 0);
+        const int cut = rows_deep(kOp) && it.depth % kStep ? it.depth / kStep : INT32_MAX;   // the stage with a tail
+        for (int k = it.k0; k < it.k1; ++k, at += kStep) {
+            if (!wait(empty + stage * 8, phase))
+                return false;
+            if (elected()) {
+                const uint32_t bar = rows_deep(kOp) && k == cut ? tail + stage * 8 : full + stage * 8;
+                const uint32_t a = base + stage * S::kStage, b = a + kAStage;
+                arrive_expect(rows_deep(kOp) && k == cut ? in_cta(bar, c.rank) : bar, bytes);
+                if (a_along_lanes(kOp)) {
+                    load_tile(a, &map_a, a_lane, at, za, bar);
+                    load_tile(a + kBlock, &map_a, a_lane + 64, at, za, bar);
+                } else {
+                    load_tile(a, &map_a, at, a_lane, za, bar);
+                }
+#pragma unroll
+                for (int q = 0; q < S::kBStage / (kBoxB * 128) || q == 0; ++q)
+                    if (q < boxes) {
+                        if (b_along_columns(kOp))
+                            load_tile(b + q * kBlock, &map_b, b_col + q * 64, at, 0, bar);
+                        else
+                            load_tile(b + q * S::kBox * 128, &map_b, at, b_col + q * S::kBox, 0, bar);
+                    }
+            }
+            __syncwarp();
+            if (++stage == S::kStages)
+                stage = 0, phase ^= 1;
+        }
+    }
+    return true;
+}
+
+template <int kColumns, int kOp>
+__device__ __forceinline__ bool multiply_stages(const Product &p, const Cta &c)
+{
+    using S = Shape<kColumns>;
+    constexpr uint32_t kALead = a_along_lanes(kOp) ? kBlock : 16, kANext = (a_along_lanes(kOp) ? 16 * 128 : 32) >> 4;
+    constexpr uint32_t kBLead = b_along_columns(kOp) ? kBlock : 16, kBNext = (b_along_columns(kOp) ? 16 * 128 : 32) >> 4;
+    const uint32_t full = smem_addr(&c.bars->full[0]), empty = smem_addr(&c.bars->empty[0]);
+    const uint32_t done = smem_addr(&c.bars->done[0]), drained = smem_addr(&c.bars->drained[0]);
+    const uint64_t first_a = operand(smem_addr(c.stages), kALead, 1024);
+    const uint64_t first_b = operand(smem_addr(c.stages) + kAStage, kBLead, 1024);
+    int stage = 0, half = 0;
+    uint32_t phase = 0, free_phase = 1;                  // free_phase: of both halves, while half is 0
+    for (int i = c.pair; i < c.items; i += c.pairs) {
+        const Item it = item_of<kColumns>(p, *c.tables, c.lane_tiles, i);
+        const uint32_t idesc = shape(p.bf16, a_along_lanes(kOp), b_along_columns(kOp), (it.cols + 31) / 32 * 32);
+        for (int k = it.k0; k < it.k1;) {
+            if (!wait(drained + half * 8, free_phase))
+                return false;
+            fence_after();
+            const int stop = min(it.k1, k + p.chunk);
+            const uint32_t sums = c.tmem + half * kColumns;
+            for (bool add = false; k < stop; ++k, add = true) {
+                if (!wait(full + stage * 8, phase))
+                    return false;
+                fence_after();
+                if (elected()) {
+                    const uint64_t a = first_a + stage * (S::kStage >> 4), b = first_b + stage * (S::kStage >> 4);
+                    const int left = it.depth - k * kStep;               // steps of 16 wholly past the end are left out
+                    multiply(sums, a, b, idesc, add);
+                    if (left > 16)
+                        multiply(sums, a + kANext, b + kBNext, idesc, true);
+                    if (left > 32)
+                        multiply(sums, a + 2 * kANext, b + 2 * kBNext, idesc, true);
+                    if (left > 48)
+                        multiply(sums, a + 3 * kANext, b + 3 * kBNext, idesc, true);
+                    commit(empty + stage * 8);
+                    if (k + 1 == stop)
+                        commit(done + half * 8);
+                }
+                __syncwarp();
+                if (++stage == S::kStages)
+                    stage = 0, phase ^= 1;
+            }
+            if (half ^= 1; half == 0)
+                free_phase ^= 1;
+        }
+    }
+    return true;
+}
+
+// The last stage of a group's rows holds rows of the next group: cleared up to the
+// next multiple of 16, beyond which nothing is multiplied.
+template <int kColumns>
+__device__ __forceinline__ bool clear_tails(const Product &p, const Cta &c)
+{
+    using S = Shape<kColumns>;
+    const int lane = threadIdx.x & 31;
+    const uint32_t full = in_cta(smem_addr(&c.bars->full[0]), 0);
+    int stage = 0;
+    uint32_t phase = 0;                                  // a bit for each stage
+    for (int i = c.pair; i < c.items; i += c.pairs) {
+        const Item it = item_of<kColumns>(p, *c.tables, c.lane_tiles, i);
+        const int left = it.depth % kStep, count = it.k1 - it.k0;
+        if (left && count > 0 && it.k1 * kStep > it.depth) {
+            const int at = (stage + count - 1) % S::kStages;
+            if (!wait(smem_addr(&c.bars->tail[at]), (phase >> at) & 1))
+                return false;
+            phase ^= 1u << at;
+            const int blocks = 2 + parts_of((it.cols + 31) / 32 * 16, 64), stop = (left + 15) / 16 * 16;
+            uint4 *to = reinterpret_cast<uint4 *>(c.stages + at * S::kStage);
+            for (int q = 0; q < blocks; ++q)
+                for (int v = left * 8 + lane; v < stop * 8; v += 32)
+                    to[q * (kBlock / 16) + v] = make_uint4(0, 0, 0, 0);
+            fence_async_proxy();
+            __syncwarp();
+            if (lane == 0)
+                arrive_release(full + at * 8);
+        }
+        stage = (stage + count) % S::kStages;
+    }
+    return true;
+}
+
+// A split tile: this part goes to memory, and the last CTA of its rank to get here
+// takes the sum of all parts, in their order.  1: it has; 0: another will; -1: gave up.
 template <int kColumns, bool kCodes>
+__device__ __forceinline__ int join_parts(const Product &p, const Cta &c, const Item &it, uint32_t (&acc)[Shape<kColumns>::kPieces][16],
+                                          int span, int col, int warp, uint32_t turn)
+{
+    using S = Shape<kColumns>;
+    const int lane = threadIdx.x & 31, split = c.tables->split;
+    uint32_t *part = reinterpret_cast<uint32_t *>(p.parts) + int64_t(it.tile) * split * kPartFloats +
+                     c.rank * (kPartFloats / 2) + (warp & 3) * 32 + lane;
+#pragma unroll
+    for (int q = 0; q < S::kPieces; ++q)
+        if (q * 16 < span)
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+                part[it.part * kPartFloats + (col + q * 16 + j) * 128] = acc[q][j];
+    __threadfence();
+    __syncwarp();
+    if (lane == 0)
+        arrive_release(in_cta(smem_addr(&c.bars->written), c.rank));
+    if (warp == kFirstEpilogueWarp) {
+        if (!wait(smem_addr(&c.bars->written), turn))
+            return -1;
+        if (lane == 0) {
+            __threadfence();
+            unsigned *ticket = p.tickets + 2 * it.tile + c.rank;
+            c.bars->last = atomicAdd(ticket, 1u) + 1 == static_cast<unsigned>(split);
+            if (c.bars->last)
+                *ticket = 0;
+            __threadfence();
+            arrive_release(in_cta(smem_addr(&c.bars->counted), c.rank));
+        }
+        __syncwarp();
+    }
+    if (!wait(smem_addr(&c.bars->counted), turn))
+        return -1;
+    if (!c.bars->last)
+        return 0;
+#pragma unroll
+    for (int q = 0; q < S::kPieces; ++q)
+        if (q * 16 < span) {
+            for (int s = 0; s < split; ++s)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    const uint32_t v = __ldcg(part + s * kPartFloats + (col + q * 16 + j) * 128);
+                    if (s == 0)
+                        acc[q][j] = v;
+                    else
+                        acc[q][j] = kCodes ? acc[q][j] + v : __float_as_uint(__uint_as_float(acc[q][j]) + __uint_as_float(v));
+                }
+        }
+    return 1;
+}
+
+template <int kColumns, bool kCodes>
+__device__ __forceinline__ bool write_outputs(const Product &p, const Cta &c)
+{
+    using S = Shape<kColumns>;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int quarter = warp & 3, side = (warp - kFirstEpilogueWarp) >> 2;
+    const uint32_t done = smem_addr(&c.bars->done[0]), drained = in_cta(smem_addr(&c.bars->drained[0]), 0);
+    int half = 0;
+    uint32_t phase = 0, joins = 0;
+    for (int i = c.pair; i < c.items; i += c.pairs) {
+        const Item it = item_of<kColumns>(p, *c.tables, c.lane_tiles, i);
+        const int span = (it.cols + 31) / 32 * 16;                          // columns of this warp
+        const int at = it.lane0 + c.rank * 128 + quarter * 32 + lane, col = side * span;
+        uint32_t acc[S::kPieces][16];
+        if (it.k0 == it.k1)
+#pragma unroll
+            for (int q = 0; q < S::kPieces; ++q)
+#pragma unroll
+                for (int j = 0; j < 16; ++j)
+                    acc[q][j] = 0;
+        for (int k = it.k0; k < it.k1; k += p.chunk) {
+            if (!wait(done + half * 8, phase))
+                return false;
+            fence_after();
+            const uint32_t from = c.tmem + half * kColumns + (uint32_t(quarter * 32) << 16) + col;
+            if (k == it.k0) {
+#pragma unroll
+                for (int q = 0; q < S::kPieces; ++q)
+                    if (q * 16 < span)
+                        load16(from + q * 16, acc[q]);
+#pragma unroll
+                for (int q = 0; q < S::kPieces; ++q) {
+                    load_wait(acc[q]);
+                    begin_sum<kCodes>(acc[q]);
+                }
+            } else {
+#pragma unroll
+                for (int q = 0; q < S::kPieces; ++q)
+                    if (q * 16 < span) {
+                        uint32_t v[16];
+                        load16(from + q * 16, v);
+                        load_wait(v);
+                        add_to_sum<kCodes>(acc[q], v);
+                    }
+            }
+            fence_before();
+            __syncwarp();
+            if (lane == 0)
+                arrive(drained + half * 8);
+            if (half ^= 1; half == 0)
+                phase ^= 1;
+        }
+        if (c.tables->split > 1) {
+            const int mine = join_parts<kColumns, kCodes>(p, c, it, acc, span, col, warp, joins++ & 1);
+            if (mine < 0)
+                return false;
+            if (mine == 0)
+                continue;
+        }
+        if (p.add && it.depth == 0)
+            continue;                                    // nothing to add
+#pragma unroll
+        for (int q = 0; q < S::kPieces; ++q)
+            if (q * 16 < span && col + q * 16 < it.cols)
+                finish16<kCodes>(p, it, at, col + q * 16, acc[q]);
+    }
+    return true;
+}
+
+template <int kColumns, int kOp>
 __global__ void __launch_bounds__(kThreads, 1)
-product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const Product p)
+product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ Product p)
 {
     using S = Shape<kColumns>;
     extern __shared__ uint8_t dynamic[];
-    uint8_t *stages = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(dynamic) + 1023) & ~uintptr_t(1023));
-    Tables &tables = *reinterpret_cast<Tables *>(stages + S::kStages * S::kStage);
     __shared__ Barriers bars;
+    Cta c;
+    c.stages = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(dynamic) + 1023) & ~uintptr_t(1023));
+    Tables *tables = reinterpret_cast<Tables *>(c.stages + S::kStages * S::kStage);
+    c.tables = tables;
+    c.bars = &bars;
+    c.rank = cta_rank();
+    c.pair = blockIdx.x >> 1;
+    c.pairs = gridDim.x >> 1;
+    c.lane_tiles = parts_of(p.lanes, kLanes);
 
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t rank = cta_rank();
-    const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
-    const int lane_tiles = parts_of(p.lanes, kLanes);
-
+    const int warp = __shfl_sync(~0u, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     if (warp == kProducerWarp && lane == 0) {
         prefetch_map(&map_a);
         prefetch_map(&map_b);
@@ -352,205 +661,27 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     }
     if (warp == kMultiplyWarp)
         tmem_alloc(smem_addr(&bars.tmem), S::kTmem);
-    if (warp == kTailWarp)
-        fill_tables(p, tables, kColumns, lane_tiles, pairs);
+    if (warp == kTablesWarp)
+        fill_tables(p, *tables, kColumns, c.lane_tiles, c.pairs);
     fence_before();
     __syncthreads();
     cluster_sync();
     fence_after();
-    const uint32_t tmem = bars.tmem;
-    const int items = tables.first[p.groups] * tables.split;
-    const bool rows_deep = p.depth == 0;               // the contraction is a group's rows
-    bool fine = true;
+    c.tmem = bars.tmem;
+    c.items = tables->first[p.groups] * tables->split;
 
-    if (warp == kProducerWarp) {
-        if (lane == 0) {
-            const uint32_t first = in_cta(smem_addr(&bars.full[0]), 0);
-            int stage = 0;
-            uint32_t phase = 0;
-            for (int i = pair; fine && i < items; i += pairs) {
-                const Item it = item_of<kColumns>(p, tables, lane_tiles, i);
-                const int half = (it.cols + 31) / 32 * 16;                 // B's columns in this CTA
-                const int a_lane = it.lane0 + rank * 128, b_col = it.col0 + rank * half;
-                const int box_b = p.b_along_columns ? 64 : S::kBox, boxes = parts_of(half, box_b);
-                const uint32_t bytes = kAStage + boxes * box_b * 128;
-                for (int k = it.k0; k < it.k1; ++k) {
-                    if (!(fine = wait(smem_addr(&bars.empty[stage]), phase ^ 1)))
-                        break;
-                    const bool tail = rows_deep && (k + 1) * kStep > it.depth;
-                    const uint32_t bar = tail ? smem_addr(&bars.tail[stage]) : first + stage * 8;
-                    arrive_expect(tail ? in_cta(bar, rank) : bar, bytes);
-                    const uint32_t a = smem_addr(stages + stage * S::kStage), b = a + kAStage;
-                    const int c = k * kStep + (rows_deep ? it.row0 : 0);
-                    const int za = p.a_by_group ? it.g : 0;
-                    if (p.a_along_lanes) {
-                        load_tile(a, &map_a, a_lane, c, za, bar);
-                        load_tile(a + kBlock, &map_a, a_lane + 64, c, za, bar);
-                    } else {
-                        load_tile(a, &map_a, c, a_lane, za, bar);
-                    }
-                    for (int q = 0; q < boxes; ++q)
-                        if (p.b_along_columns)
-                            load_tile(b + q * kBlock, &map_b, b_col + q * 64, c, 0, bar);
-                        else
-                            load_tile(b + q * S::kBox * 128, &map_b, c, it.row0 + b_col + q * S::kBox, 0, bar);
-                    if (++stage == S::kStages)
-                        stage = 0, phase ^= 1;
-                }
-            }
-        }
-    } else if (warp == kMultiplyWarp) {
-        if (lane == 0 && rank == 0) {
-            int stage = 0, half = 0;
-            uint32_t phase = 0, drained = 0;
-            const uint32_t a_lead = p.a_along_lanes ? kBlock : 16, b_lead = p.b_along_columns ? kBlock : 16;
-            const uint32_t a_next = (p.a_along_lanes ? 16 * 128 : 32) >> 4, b_next = (p.b_along_columns ? 16 * 128 : 32) >> 4;
-            for (int i = pair; fine && i < items; i += pairs) {
-                const Item it = item_of<kColumns>(p, tables, lane_tiles, i);
-                const uint32_t idesc = shape(p.bf16, p.a_along_lanes, p.b_along_columns, (it.cols + 31) / 32 * 32);
-                for (int k = it.k0; fine && k < it.k1;) {
-                    if (!(fine = wait(smem_addr(&bars.drained[half]), ((drained >> half) & 1) ^ 1)))
-                        break;
-                    drained ^= 1u << half;
-                    fence_after();
-                    const int stop = min(it.k1, k + p.chunk);
-                    for (bool add = false; k < stop; ++k) {
-                        if (!(fine = wait(smem_addr(&bars.full[stage]), phase)))
-                            break;
-                        fence_after();
-                        const uint32_t a = smem_addr(stages + stage * S::kStage), b = a + kAStage;
-                        const uint64_t da = operand(a, a_lead, 1024), db = operand(b, b_lead, 1024);
-                        const int steps = parts_of(min(kStep, it.depth - k * kStep), 16);
-                        for (int q = 0; q < steps; ++q, add = true)
-                            multiply(tmem + half * kColumns, da + q * a_next, db + q * b_next, idesc, add);
-                        commit(smem_addr(&bars.empty[stage]));
-                        if (++stage == S::kStages)
-                            stage = 0, phase ^= 1;
-                    }
-                    commit(smem_addr(&bars.done[half]));
-                    half ^= 1;
-                }
-            }
-        }
-    } else if (warp == kTailWarp) {
-        // The last stage of a group's rows holds rows of the next group: cleared up to
-        // the next multiple of 16, beyond which nothing is multiplied.
-        if (rows_deep) {
-            const uint32_t full = in_cta(smem_addr(&bars.full[0]), 0);
-            int stage = 0;
-            uint32_t phase = 0;
-            for (int i = pair; fine && i < items; i += pairs) {
-                const Item it = item_of<kColumns>(p, tables, lane_tiles, i);
-                const int left = it.depth % kStep, stages_of = it.k1 - it.k0;
-                if (left && it.k1 * kStep > it.depth && stages_of > 0) {
-                    const int at = (stage + stages_of - 1) % S::kStages;
-                    if (!(fine = __all_sync(~0u, wait(smem_addr(&bars.tail[at]), (phase >> at) & 1))))
-                        break;
-                    phase ^= 1u << at;
-                    const int blocks = 2 + parts_of((it.cols + 31) / 32 * 16, 64), stop = (left + 15) / 16 * 16;
-                    uint4 *to = reinterpret_cast<uint4 *>(stages + at * S::kStage);
-                    for (int q = 0; q < blocks; ++q)
-                        for (int v = left * 8 + lane; v < stop * 8; v += 32)
-                            to[q * (kBlock / 16) + v] = make_uint4(0, 0, 0, 0);
-                    fence_async_proxy();
-                    __syncwarp();
-                    if (lane == 0)
-                        arrive(full + at * 8);
-                }
-                stage = (stage + stages_of) % S::kStages;
-            }
-        }
+    bool fine = true;
+    if (warp < kFirstEpilogueWarp) {
+        fewer_registers<kControlRegisters>();
+        if (warp == kProducerWarp)
+            fine = load_stages<kColumns, kOp>(map_a, map_b, p, c);
+        else if (warp == kMultiplyWarp && c.rank == 0)
+            fine = multiply_stages<kColumns, kOp>(p, c);
+        else if (warp == kTailWarp && rows_deep(kOp))
+            fine = clear_tails<kColumns>(p, c);
     } else {
-        const int quarter = warp & 3, side = (warp - kFirstEpilogueWarp) >> 2;
-        const uint32_t drained = in_cta(smem_addr(&bars.drained[0]), 0);
-        int half = 0;
-        uint32_t phase = 0, joins = 0;
-        for (int i = pair; fine && i < items; i += pairs) {
-            const Item it = item_of<kColumns>(p, tables, lane_tiles, i);
-            const int span = (it.cols + 31) / 32 * 16;                      // columns of this warp
-            const int at = it.lane0 + rank * 128 + quarter * 32 + lane, col = side * span;
-            uint32_t acc[S::kPieces][16];
-#pragma unroll
-            for (int q = 0; q < S::kPieces; ++q)
-#pragma unroll
-                for (int j = 0; j < 16; ++j)
-                    acc[q][j] = 0;
-            for (int k = it.k0; k < it.k1; k += p.chunk) {
-                if (!(fine = __all_sync(~0u, wait(smem_addr(&bars.done[half]), (phase >> half) & 1))))
-                    break;
-                phase ^= 1u << half;
-                fence_after();
-                const uint32_t from = tmem + half * kColumns + (uint32_t(quarter * 32) << 16) + col;
-#pragma unroll
-                for (int q = 0; q < S::kPieces; ++q)
-                    if (q * 16 < span) {
-                        uint32_t v[16];
-                        load16(from + q * 16, v);
-                        load_wait(v);
-                        add_piece<kCodes>(acc[q], v, k == it.k0);
-                    }
-                fence_before();
-                __syncwarp();
-                if (lane == 0)
-                    arrive(drained + half * 8);
-                half ^= 1;
-            }
-            if (!fine)
-                break;
-            if (tables.split > 1) {
-                // this part to memory; the last CTA of its rank to get here adds them all
-                uint32_t *part = reinterpret_cast<uint32_t *>(p.parts) +
-                                 (int64_t(it.tile) * tables.split) * kPartFloats + rank * (kPartFloats / 2) + quarter * 32 + lane;
-#pragma unroll
-                for (int q = 0; q < S::kPieces; ++q)
-                    if (q * 16 < span)
-#pragma unroll
-                        for (int j = 0; j < 16; ++j)
-                            part[it.part * kPartFloats + (col + q * 16 + j) * 128] = acc[q][j];
-                __threadfence();
-                __syncwarp();
-                if (lane == 0)
-                    arrive(in_cta(smem_addr(&bars.written), rank));
-                if (warp == kFirstEpilogueWarp) {
-                    if (!(fine = __all_sync(~0u, wait(smem_addr(&bars.written), joins & 1))))
-                        break;
-                    if (lane == 0) {
-                        const unsigned n = atomicAdd(&p.tickets[2 * it.tile + rank], 1u);
-                        bars.last = n + 1 == static_cast<unsigned>(tables.split);
-                        if (bars.last)
-                            p.tickets[2 * it.tile + rank] = 0;
-                        __threadfence();
-                        arrive(in_cta(smem_addr(&bars.counted), rank));
-                    }
-                    __syncwarp();
-                }
-                if (!(fine = __all_sync(~0u, wait(smem_addr(&bars.counted), joins & 1))))
-                    break;
-                ++joins;
-                const bool last = bars.last;
-                if (!last)
-                    continue;
-#pragma unroll
-                for (int q = 0; q < S::kPieces; ++q)
-                    if (q * 16 < span) {
-                        for (int s = 0; s < tables.split; ++s)
-#pragma unroll
-                            for (int j = 0; j < 16; ++j) {
-                                const uint32_t v = __ldcg(part + s * kPartFloats + (col + q * 16 + j) * 128);
-                                if (kCodes)
-                                    acc[q][j] = s ? acc[q][j] + v : v;
-                                else
-                                    acc[q][j] = s ? __float_as_uint(__uint_as_float(acc[q][j]) + __uint_as_float(v)) : v;
-                            }
-                    }
-            }
-            if (p.add && it.depth == 0)
-                continue;                              // nothing to add
-#pragma unroll
-            for (int q = 0; q < S::kPieces; ++q)
-                if (q * 16 < span && col + q * 16 < it.cols)
-                    finish16<kCodes>(p, it, at, col + q * 16, acc[q]);
-        }
+        more_registers<kEpilogueRegisters>();
+        fine = write_outputs<kColumns, kOp == GNMR_PRODUCT_FORWARD_I8>(p, c);
     }
     __syncwarp();
     if (!fine) {
@@ -565,7 +696,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     cluster_sync();
     fence_after();
     if (warp == kMultiplyWarp)
-        tmem_free(tmem, S::kTmem);
+        tmem_free(c.tmem, S::kTmem);
 }
 
 // ---- operands that the TMA unit cannot read, and codes as 16-bit numbers ------------
@@ -729,12 +860,12 @@ template <int kColumns> constexpr int shared_bytes()
     return Shape<kColumns>::kStages * Shape<kColumns>::kStage + static_cast<int>(sizeof(Tables)) + 1024;
 }
 
-template <int kColumns, bool kCodes>
+template <int kColumns, int kOp>
 cudaError_t launch(const gnmr_products *h, const Operands &o, const Product &p, cudaStream_t st, bool *mapped)
 {
     CUtensorMap a, b;
-    *mapped = tile_map(h, &a, o.a, p.bf16, p.a_along_lanes ? 64 : 128) &&
-              tile_map(h, &b, o.b, p.bf16, p.b_along_columns ? 64 : Shape<kColumns>::kBox);
+    *mapped = tile_map(h, &a, o.a, p.bf16, a_along_lanes(kOp) ? 64 : 128) &&
+              tile_map(h, &b, o.b, p.bf16, b_along_columns(kOp) ? 64 : Shape<kColumns>::kBox);
     if (!*mapped)
         return cudaSuccess;
     cudaLaunchConfig_t cfg = {};
@@ -748,13 +879,33 @@ cudaError_t launch(const gnmr_products *h, const Operands &o, const Product &p, 
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, product_kernel<kColumns, kCodes>, a, b, p);
+    return cudaLaunchKernelEx(&cfg, product_kernel<kColumns, kOp>, a, b, p);
 }
 
-template <int kColumns, bool kCodes> cudaError_t allow_shared()
+template <int kColumns, int kOp> cudaError_t allow_shared()
 {
-    return cudaFuncSetAttribute(product_kernel<kColumns, kCodes>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+    return cudaFuncSetAttribute(product_kernel<kColumns, kOp>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                 shared_bytes<kColumns>());
+}
+
+// The kernels, by op and whether a group has few rows.
+using Launch = cudaError_t (*)(const gnmr_products *, const Operands &, const Product &, cudaStream_t, bool *);
+constexpr Launch kLaunch[4][2] = {
+    {launch<256, GNMR_PRODUCT_FORWARD>, launch<64, GNMR_PRODUCT_FORWARD>},
+    {launch<256, GNMR_PRODUCT_INPUT_GRAD>, launch<64, GNMR_PRODUCT_INPUT_GRAD>},
+    {launch<256, GNMR_PRODUCT_WEIGHT_GRAD>, launch<256, GNMR_PRODUCT_WEIGHT_GRAD>},
+    {launch<256, GNMR_PRODUCT_FORWARD_I8>, launch<64, GNMR_PRODUCT_FORWARD_I8>},
+};
+
+cudaError_t allow_all_shared()
+{
+    cudaError_t e = cudaSuccess;
+    for (const cudaError_t r : {allow_shared<256, GNMR_PRODUCT_FORWARD>(), allow_shared<64, GNMR_PRODUCT_FORWARD>(),
+                                allow_shared<256, GNMR_PRODUCT_INPUT_GRAD>(), allow_shared<64, GNMR_PRODUCT_INPUT_GRAD>(),
+                                allow_shared<256, GNMR_PRODUCT_WEIGHT_GRAD>(), allow_shared<256, GNMR_PRODUCT_FORWARD_I8>(),
+                                allow_shared<64, GNMR_PRODUCT_FORWARD_I8>()})
+        e = e == cudaSuccess ? r : e;
+    return e;
 }
 
 }  // namespace
@@ -803,13 +954,7 @@ gnmr_status gnmr_products_create(int32_t device, gnmr_products **out)
         e = cudaErrorNotSupported;
     h->encode = reinterpret_cast<decltype(h->encode)>(encode);
     if (e == cudaSuccess)
-        e = allow_shared<256, false>();
-    if (e == cudaSuccess)
-        e = allow_shared<256, true>();
-    if (e == cudaSuccess)
-        e = allow_shared<64, false>();
-    if (e == cudaSuccess)
-        e = allow_shared<64, true>();
+        e = allow_all_shared();
     cudaSetDevice(prev);
     if (e != cudaSuccess) {
         cudaGetLastError();
@@ -859,8 +1004,6 @@ gnmr_status gnmr_products_run(gnmr_products *h, const gnmr_product *p, void *str
     q.mask = p->d_mask;
     q.mask_stride = p->mask_stride;
     q.want = codes ? 0 : 1;
-    q.a_along_lanes = wgrad || back;
-    q.b_along_columns = wgrad;
     q.a_by_group = o.a.groups > 1;
     q.bf16 = !codes && p->dtype == GNMR_DTYPE_BF16;
     q.chunk = !codes && p->out_dtype == GNMR_DTYPE_F32 ? 8 : 16;
@@ -893,8 +1036,7 @@ gnmr_status gnmr_products_run(gnmr_products *h, const gnmr_product *p, void *str
     const bool few = !wgrad && p->rows <= 32 * int64_t(p->groups);
     bool mapped = true;
     if (e == cudaSuccess)
-        e = codes ? (few ? launch<64, true>(h, o, q, st, &mapped) : launch<256, true>(h, o, q, st, &mapped))
-                  : (few ? launch<64, false>(h, o, q, st, &mapped) : launch<256, false>(h, o, q, st, &mapped));
+        e = kLaunch[p->op][few](h, o, q, st, &mapped);
     if (e != cudaSuccess)
         cudaGetLastError();                              // reported here, not by the caller's next call
     if (prev != h->device)
