@@ -126,7 +126,7 @@ __device__ __forceinline__ void prefetch_map(const CUtensorMap *map)
 // What generic stores wrote to shared memory, for the tensor cores to read.
 __device__ __forceinline__ void fence_async_proxy()
 {
-    asm volatile("fence.proxy.async;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
 }
 
 // ---- tensor memory and tensor cores, by pairs of CTAs --------------------------

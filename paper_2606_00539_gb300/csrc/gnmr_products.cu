@@ -92,6 +92,7 @@ struct Product {
     const uint8_t *mask;
     int64_t mask_stride;
     int want;                          // groups computed: mask byte != 0 (1), == 0 (0)
+    unsigned lane_tiles_inverse;       // ceil(2^32 / tiles of 256 lanes)
     int a_by_group;                    // A's third coordinate is the group
     int bf16;
     int chunk;                         // stages of a piece
@@ -111,6 +112,7 @@ struct Product {
 struct Tables {
     int first[kMaxGroups + 1];         // tiles before group g; in the end all of them
     int row[kMaxGroups + 1];           // first row of group g; in the end the last group's end
+    uint16_t each[kMaxGroups];         // columns of group g's tiles
     int split;                         // parts of every tile's contraction
 };
 
@@ -119,7 +121,13 @@ struct Item {
     int row0;                          // the group's first row
     int depth, k0, k1;                 // the whole contraction; the stages of this part
     int tile, part;
+    bool tail;                         // the last stage holds rows past the group's end
 };
+
+// The stage with the tail is loaded first and multiplied fourth (or last): clearing it
+// takes as long as multiplying a few others.  kTailTurn + 2 stages at least are in
+// the ring, so that it is never waited for by a stage that waits for its place.
+constexpr int kTailTurn = 3;
 
 __device__ __forceinline__ int parts_of(int n, int each) { return (n + each - 1) / each; }
 
@@ -151,7 +159,10 @@ __device__ __forceinline__ void fill_tables(const Product &p, Tables &t, int mos
         int n = 0;
         if (g < p.groups && (!p.mask || (p.mask[g * p.mask_stride] != 0) == (p.want != 0))) {
             const int rows = t.row[g + 1] - t.row[g];
-            n = lane_tiles * parts_of(p.cols ? p.cols : rows, most);
+            const int cols = p.cols ? p.cols : rows, across = parts_of(cols, most);
+            n = lane_tiles * across;
+            // a group's columns are shared out evenly, in multiples of 32
+            t.each[g] = static_cast<uint16_t>(across ? parts_of(parts_of(cols, across), 32) * 32 : 0);
             deepest = max(deepest, p.depth ? p.depth : rows);
         }
         int sum = n;
@@ -181,42 +192,50 @@ __device__ __forceinline__ void fill_tables(const Product &p, Tables &t, int mos
     }
 }
 
-template <int kColumns>
-__device__ __forceinline__ Item item_of(const Product &p, const Tables &t, int lane_tiles, int i)
+// Item i of the call, by a whole warp that comes with growing i.  g: the group of the one
+// before, 0 at first.
+__device__ __forceinline__ Item item_of(const Product &p, const Tables &t, int lane_tiles, int i, int &g)
 {
     Item it;
-    it.tile = i / t.split;
+    it.tile = t.split == 1 ? i : i / t.split;
     it.part = i - it.tile * t.split;
-    int lo = 0, hi = p.groups;                       // the last group that begins at or before the tile
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) / 2;
-        if (t.first[mid] <= it.tile)
-            lo = mid;
-        else
-            hi = mid;
+    for (;;) {                                       // the last group that begins at or before the tile
+        const int next = g + 1 + (threadIdx.x & 31);
+        const unsigned past = __ballot_sync(~0u, next >= p.groups || t.first[next] > it.tile);
+        if (past) {
+            g += __ffs(past) - 1;
+            break;
+        }
+        g += 32;
     }
-    it.g = lo;
-    it.row0 = t.row[lo];
-    const int rows = t.row[lo + 1] - it.row0, at = it.tile - t.first[lo];
-    const int cols = p.cols ? p.cols : rows;
-    // a group's columns are shared out evenly, in multiples of 32
-    const int each = (parts_of(cols, parts_of(cols, kColumns)) + 31) / 32 * 32;
-    const int c = at / lane_tiles;
+    it.g = g;
+    it.row0 = t.row[g];
+    const int rows = t.row[g + 1] - it.row0, at = it.tile - t.first[g], each = t.each[g];
+    int c = at;                                      // at / lane_tiles
+    if (lane_tiles > 1) {
+        c = __umulhi(at, p.lane_tiles_inverse);      // that, or one more
+        c -= c * lane_tiles > at;
+    }
     it.lane0 = (at - c * lane_tiles) * kLanes;
     it.col0 = c * each;
-    it.cols = min(each, cols - it.col0);
+    it.cols = min(each, (p.cols ? p.cols : rows) - it.col0);
     it.depth = p.depth ? p.depth : rows;
     const int stages = parts_of(it.depth, kStep);
-    it.k0 = static_cast<int>(int64_t(stages) * it.part / t.split);
-    it.k1 = static_cast<int>(int64_t(stages) * (it.part + 1) / t.split);
+    it.k0 = 0;
+    it.k1 = stages;
+    if (t.split > 1) {
+        it.k0 = stages * it.part / t.split;
+        it.k1 = stages * (it.part + 1) / t.split;
+    }
+    it.tail = !p.depth && it.depth % kStep && it.k0 < it.k1 && it.k1 == stages;
     return it;
 }
 
 // ---- outputs --------------------------------------------------------------------
 
-__device__ __forceinline__ unsigned pack(float lo, float hi, int type)
+template <int kOut> __device__ __forceinline__ unsigned pack(float lo, float hi)
 {
-    if (type == GNMR_DTYPE_BF16) {
+    if (kOut == GNMR_DTYPE_BF16) {
         const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
         return reinterpret_cast<const unsigned &>(v);
     }
@@ -224,101 +243,109 @@ __device__ __forceinline__ unsigned pack(float lo, float hi, int type)
     return reinterpret_cast<const unsigned &>(v);
 }
 
-// Two columns of this thread's lane become one column of two lanes, the even lane's
-// column j and the odd lane's column j + 1.
-__device__ __forceinline__ unsigned exchange(float vj, float vj1, int type, unsigned which)
+template <int kOut> __device__ __forceinline__ float load_out(const char *at)
 {
-    const unsigned w = pack(vj, vj1, type);
+    return kOut == GNMR_DTYPE_F32    ? *reinterpret_cast<const float *>(at)
+           : kOut == GNMR_DTYPE_BF16 ? __bfloat162float(*reinterpret_cast<const __nv_bfloat16 *>(at))
+                                     : __half2float(*reinterpret_cast<const __half *>(at));
+}
+
+// Two columns of this thread's lane become one column of two lanes: the even lane gets
+// the first column's, the odd lane the second's.
+template <int kOut> __device__ __forceinline__ unsigned exchange(float first, float second, unsigned which)
+{
+    const unsigned w = pack<kOut>(first, second);
     return __byte_perm(w, __shfl_xor_sync(~0u, w, 1), which);
 }
 
-__device__ __forceinline__ float load_out(const void *at, int type)
+// This warp's sums to the outputs: lane `lane` of columns col .. col + span - 1 of the
+// tile.  Two lanes' 16-bit values of a column go out as one where they can: 64
+// contiguous bytes a column from a warp.
+template <int kPieces, bool kCodes, int kOut>
+__device__ __forceinline__ void finish(const Product &p, const Item &it, uint32_t (&acc)[kPieces][16], int lane, int col, int span)
 {
-    return type == GNMR_DTYPE_F32    ? *static_cast<const float *>(at)
-           : type == GNMR_DTYPE_BF16 ? __bfloat162float(*static_cast<const __nv_bfloat16 *>(at))
-                                     : __half2float(*static_cast<const __half *>(at));
-}
-
-// 16 columns of this thread's lane.  Two lanes' values of a column go out as one
-// where they can: 64 contiguous bytes a column from a warp.
-__device__ __forceinline__ void store16(const Product &p, const Item &it, int lane, int col, float (&v)[16])
-{
-    const int64_t base = p.cols ? it.g * p.out_group + int64_t(it.col0 + col) * p.out_col
-                                : int64_t(it.row0 + it.col0 + col) * p.out_col;
+    constexpr int kBytes = kOut == GNMR_DTYPE_F32 ? 4 : 2;
+    const int64_t step = p.out_col * kBytes;
+    const int64_t row = p.cols ? it.col0 + col : int64_t(it.row0) + it.col0 + col;
+    char *out = static_cast<char *>(p.out) + (p.cols ? it.g * p.out_group * kBytes : 0) + row * step + int64_t(lane) * kBytes;
     const int left = it.cols - col, odd = lane & 1;
-    const bool whole = left >= 16 && (lane | 31) < p.lanes, mine = lane < p.lanes;
+    const bool mine = lane < p.lanes;
+    const bool whole = (lane | 31) < p.lanes && (kBytes == 4 || (p.pairs_aligned && !p.add));
     const unsigned which = odd ? 0x3276 : 0x5410;
-    if (p.out_type == GNMR_DTYPE_F32) {
-        float *out = static_cast<float *>(p.out) + base + lane;
-        if (whole) {
-            if (p.add) {
-                float old[16];
+    float by_lane = 0.0f;
+    const float *by_col = nullptr;
+    if (kCodes) {
+        by_lane = mine ? p.lane_scale[int64_t(it.g) * p.lanes + lane] : 0.0f;
+        by_col = p.col_scale + it.row0 + it.col0 + col;
+    }
+    if (whole && kBytes == 2)
+        out += odd ? step - 2 : 0;
 #pragma unroll
-                for (int j = 0; j < 16; ++j)
-                    old[j] = out[j * p.out_col];
+    for (int q = 0; q < kPieces; ++q) {
+        const int n = min(span, left) - q * 16;          // columns of this piece that there are
+        if (n <= 0)
+            break;
+        float v[16];
 #pragma unroll
-                for (int j = 0; j < 16; ++j)
-                    v[j] += old[j];
-            }
-#pragma unroll
-            for (int j = 0; j < 16; ++j, out += p.out_col)
-                *out = v[j];
-        } else {
+        for (int j = 0; j < 16; ++j)
+            v[j] = kCodes ? (j < n ? by_col[q * 16 + j] : 0.0f) : __uint_as_float(acc[q][j]);
+        if (kCodes)
 #pragma unroll
             for (int j = 0; j < 16; ++j)
-                if (mine && j < left)
-                    out[j * p.out_col] = p.add ? v[j] + out[j * p.out_col] : v[j];
-        }
-        return;
-    }
-    uint16_t *out = static_cast<uint16_t *>(p.out) + base + lane;
-    if (whole && p.pairs_aligned && !p.add) {
-        out += odd ? p.out_col - 1 : 0;
+                v[j] = static_cast<float>(static_cast<int>(acc[q][j])) * v[j] * by_lane;
+        if (whole && n >= 16) {
+            if (kBytes == 4) {
+                if (p.add) {
+                    float old[16];
+                    const char *from = out;
 #pragma unroll
-        for (int j = 0; j < 16; j += 2, out += 2 * p.out_col)
-            *reinterpret_cast<unsigned *>(out) = exchange(v[j], v[j + 1], p.out_type, which);
-        return;
-    }
-    if (p.add)
+                    for (int j = 0; j < 16; ++j, from += step)
+                        old[j] = *reinterpret_cast<const float *>(from);
 #pragma unroll
-        for (int j = 0; j < 16; ++j)
-            if (mine && j < left)
-                v[j] += load_out(out + j * p.out_col, p.out_type);
+                    for (int j = 0; j < 16; ++j)
+                        v[j] += old[j];
+                }
 #pragma unroll
-    for (int j = 0; j < 16; j += 2) {
-        const unsigned w = exchange(v[j], v[j + 1], p.out_type, which);
-        const int k = j + odd;                       // the column that this thread writes, lanes lane & ~1 and the next
-        uint16_t *to = out - odd + k * p.out_col;
-        if (k < left) {
-            if (p.pairs_aligned && (lane | 1) < p.lanes) {
-                *reinterpret_cast<unsigned *>(to) = w;
+                for (int j = 0; j < 16; ++j, out += step)
+                    *reinterpret_cast<float *>(out) = v[j];
             } else {
-                if ((lane & ~1) < p.lanes)
-                    to[0] = static_cast<uint16_t>(w);
-                if ((lane | 1) < p.lanes)
-                    to[1] = static_cast<uint16_t>(w >> 16);
+#pragma unroll
+                for (int j = 0; j < 16; j += 2, out += 2 * step)
+                    *reinterpret_cast<unsigned *>(out) = exchange<kOut>(v[j], v[j + 1], which);
+            }
+            continue;
+        }
+        if (whole && kBytes == 2)                        // back to this lane's own place in the first column
+            out -= odd ? step - 2 : 0;
+        if (p.add)
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+                if (mine && j < n)
+                    v[j] += load_out<kOut>(out + j * step);
+        if (kBytes == 4) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+                if (mine && j < n)
+                    *reinterpret_cast<float *>(out + j * step) = v[j];
+        } else {
+#pragma unroll
+            for (int j = 0; j < 16; j += 2) {
+                const unsigned w = exchange<kOut>(v[j], v[j + 1], which);
+                char *to = out - 2 * odd + (j + odd) * step;     // the column that this thread writes, two lanes of it
+                if (j + odd < n) {
+                    if (p.pairs_aligned && (lane | 1) < p.lanes) {
+                        *reinterpret_cast<unsigned *>(to) = w;
+                    } else {
+                        if ((lane & ~1) < p.lanes)
+                            *reinterpret_cast<uint16_t *>(to) = static_cast<uint16_t>(w);
+                        if ((lane | 1) < p.lanes)
+                            *reinterpret_cast<uint16_t *>(to + 2) = static_cast<uint16_t>(w >> 16);
+                    }
+                }
             }
         }
+        out += 16 * step;
     }
-}
-
-template <bool kCodes>
-__device__ __forceinline__ void finish16(const Product &p, const Item &it, int lane, int col, uint32_t (&acc)[16])
-{
-    float v[16];
-    if (kCodes) {
-        const float by_lane = lane < p.lanes ? p.lane_scale[int64_t(it.g) * p.lanes + lane] : 0.0f;
-#pragma unroll
-        for (int j = 0; j < 16; ++j) {
-            const float by_col = col + j < it.cols ? p.col_scale[it.row0 + it.col0 + col + j] : 0.0f;
-            v[j] = static_cast<float>(static_cast<int>(acc[j])) * by_col * by_lane;
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < 16; ++j)
-            v[j] = __uint_as_float(acc[j]);
-    }
-    store16(p, it, lane, col, v);
 }
 
 // The first piece's sums, or another's added to them.
@@ -381,21 +408,25 @@ __device__ __forceinline__ bool load_stages(const CUtensorMap &map_a, const CUte
     const uint32_t tail = smem_addr(&c.bars->tail[0]), base = smem_addr(c.stages);
     int stage = 0;
     uint32_t phase = 1;
-    for (int i = c.pair; i < c.items; i += c.pairs) {
-        const Item it = item_of<kColumns>(p, *c.tables, c.lane_tiles, i);
+    for (int i = c.pair, g = 0; i < c.items; i += c.pairs) {
+        const Item it = item_of(p, *c.tables, c.lane_tiles, i, g);
         const int half = (it.cols + 31) / 32 * 16;                         // B's columns in this CTA
         const int a_lane = it.lane0 + c.rank * 128, b_col = it.col0 + c.rank * half + (rows_deep(kOp) ? 0 : it.row0);
         const int boxes = parts_of(half, kBoxB), za = p.a_by_group ? it.g : 0;
         const uint32_t bytes = kAStage + boxes * kBoxB * 128;
-        int at = it.k0 * kStep + (rows_deep(kOp) ? it.row0 : 0);
-        const int cut = rows_deep(kOp) && it.depth % kStep ? it.depth / kStep : INT32_MAX;   // the stage with a tail
-        for (int k = it.k0; k < it.k1; ++k, at += kStep) {
+        for (int k = it.k0; k < it.k1; ++k) {
             if (!wait(empty + stage * 8, phase))
                 return false;
             if (elected()) {
-                const uint32_t bar = rows_deep(kOp) && k == cut ? tail + stage * 8 : full + stage * 8;
+                int at = k * kStep;
+                bool first_tail = false;
+                if (rows_deep(kOp)) {
+                    first_tail = it.tail && k == it.k0;
+                    at = it.row0 + (!it.tail ? k : first_tail ? it.k1 - 1 : k - 1) * kStep;
+                }
+                const uint32_t bar = first_tail ? tail + stage * 8 : full + stage * 8;
                 const uint32_t a = base + stage * S::kStage, b = a + kAStage;
-                arrive_expect(rows_deep(kOp) && k == cut ? in_cta(bar, c.rank) : bar, bytes);
+                arrive_expect(first_tail ? in_cta(bar, c.rank) : bar, bytes);
                 if (a_along_lanes(kOp)) {
                     load_tile(a, &map_a, a_lane, at, za, bar);
                     load_tile(a + kBlock, &map_a, a_lane + 64, at, za, bar);
@@ -431,30 +462,44 @@ __device__ __forceinline__ bool multiply_stages(const Product &p, const Cta &c)
     const uint64_t first_b = operand(smem_addr(c.stages) + kAStage, kBLead, 1024);
     int stage = 0, half = 0;
     uint32_t phase = 0, free_phase = 1;                  // free_phase: of both halves, while half is 0
-    for (int i = c.pair; i < c.items; i += c.pairs) {
-        const Item it = item_of<kColumns>(p, *c.tables, c.lane_tiles, i);
+    for (int i = c.pair, g = 0; i < c.items; i += c.pairs) {
+        const Item it = item_of(p, *c.tables, c.lane_tiles, i, g);
         const uint32_t idesc = shape(p.bf16, a_along_lanes(kOp), b_along_columns(kOp), (it.cols + 31) / 32 * 32);
-        for (int k = it.k0; k < it.k1;) {
+        const int count = it.k1 - it.k0, turn = it.tail ? min(kTailTurn, count - 1) : -1;
+        const int first = stage;
+        const uint32_t first_phase = phase;
+        for (int k = 0; k < count;) {
             if (!wait(drained + half * 8, free_phase))
                 return false;
             fence_after();
-            const int stop = min(it.k1, k + p.chunk);
+            const int stop = min(count, k + p.chunk);
             const uint32_t sums = c.tmem + half * kColumns;
             for (bool add = false; k < stop; ++k, add = true) {
-                if (!wait(full + stage * 8, phase))
+                int at = stage, left = it.depth - (it.k0 + k) * kStep;
+                uint32_t its = phase;
+                if (rows_deep(kOp)) {
+                    left = kStep;
+                    if (k < turn) {                      // the one after: the tail was loaded before all
+                        if (++at == S::kStages)
+                            at = 0, its ^= 1;
+                    } else if (k == turn) {
+                        at = first, its = first_phase;
+                        left = it.depth % kStep;
+                    }
+                }
+                if (!wait(full + at * 8, its))
                     return false;
                 fence_after();
                 if (elected()) {
-                    const uint64_t a = first_a + stage * (S::kStage >> 4), b = first_b + stage * (S::kStage >> 4);
-                    const int left = it.depth - k * kStep;               // steps of 16 wholly past the end are left out
-                    multiply(sums, a, b, idesc, add);
+                    const uint64_t a = first_a + at * (S::kStage >> 4), b = first_b + at * (S::kStage >> 4);
+                    multiply(sums, a, b, idesc, add);                    // steps of 16 wholly past the end are left out
                     if (left > 16)
                         multiply(sums, a + kANext, b + kBNext, idesc, true);
                     if (left > 32)
                         multiply(sums, a + 2 * kANext, b + 2 * kBNext, idesc, true);
                     if (left > 48)
                         multiply(sums, a + 3 * kANext, b + 3 * kBNext, idesc, true);
-                    commit(empty + stage * 8);
+                    commit(empty + at * 8);
                     if (k + 1 == stop)
                         commit(done + half * 8);
                 }
@@ -469,7 +514,7 @@ __device__ __forceinline__ bool multiply_stages(const Product &p, const Cta &c)
     return true;
 }
 
-// The last stage of a group's rows holds rows of the next group: cleared up to the
+// A group's last stage holds rows of the next group: cleared up to the
 // next multiple of 16, beyond which nothing is multiplied.
 template <int kColumns>
 __device__ __forceinline__ bool clear_tails(const Product &p, const Cta &c)
@@ -479,11 +524,10 @@ __device__ __forceinline__ bool clear_tails(const Product &p, const Cta &c)
     const uint32_t full = in_cta(smem_addr(&c.bars->full[0]), 0);
     int stage = 0;
     uint32_t phase = 0;                                  // a bit for each stage
-    for (int i = c.pair; i < c.items; i += c.pairs) {
-        const Item it = item_of<kColumns>(p, *c.tables, c.lane_tiles, i);
-        const int left = it.depth % kStep, count = it.k1 - it.k0;
-        if (left && count > 0 && it.k1 * kStep > it.depth) {
-            const int at = (stage + count - 1) % S::kStages;
+    for (int i = c.pair, g = 0; i < c.items; i += c.pairs) {
+        const Item it = item_of(p, *c.tables, c.lane_tiles, i, g);
+        if (it.tail) {
+            const int left = it.depth % kStep, at = stage;
             if (!wait(smem_addr(&c.bars->tail[at]), (phase >> at) & 1))
                 return false;
             phase ^= 1u << at;
@@ -497,7 +541,7 @@ __device__ __forceinline__ bool clear_tails(const Product &p, const Cta &c)
             if (lane == 0)
                 arrive_release(full + at * 8);
         }
-        stage = (stage + count) % S::kStages;
+        stage = (stage + it.k1 - it.k0) % S::kStages;
     }
     return true;
 }
@@ -565,8 +609,8 @@ __device__ __forceinline__ bool write_outputs(const Product &p, const Cta &c)
     const uint32_t done = smem_addr(&c.bars->done[0]), drained = in_cta(smem_addr(&c.bars->drained[0]), 0);
     int half = 0;
     uint32_t phase = 0, joins = 0;
-    for (int i = c.pair; i < c.items; i += c.pairs) {
-        const Item it = item_of<kColumns>(p, *c.tables, c.lane_tiles, i);
+    for (int i = c.pair, g = 0; i < c.items; i += c.pairs) {
+        const Item it = item_of(p, *c.tables, c.lane_tiles, i, g);
         const int span = (it.cols + 31) / 32 * 16;                          // columns of this warp
         const int at = it.lane0 + c.rank * 128 + quarter * 32 + lane, col = side * span;
         uint32_t acc[S::kPieces][16];
@@ -617,10 +661,12 @@ __device__ __forceinline__ bool write_outputs(const Product &p, const Cta &c)
         }
         if (p.add && it.depth == 0)
             continue;                                    // nothing to add
-#pragma unroll
-        for (int q = 0; q < S::kPieces; ++q)
-            if (q * 16 < span && col + q * 16 < it.cols)
-                finish16<kCodes>(p, it, at, col + q * 16, acc[q]);
+        if (p.out_type == GNMR_DTYPE_F32)
+            finish<S::kPieces, kCodes, GNMR_DTYPE_F32>(p, it, acc, at, col, span);
+        else if (p.out_type == GNMR_DTYPE_BF16)
+            finish<S::kPieces, kCodes, GNMR_DTYPE_BF16>(p, it, acc, at, col, span);
+        else
+            finish<S::kPieces, kCodes, GNMR_DTYPE_F16>(p, it, acc, at, col, span);
     }
     return true;
 }
@@ -661,6 +707,9 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     }
     if (warp == kMultiplyWarp)
         tmem_alloc(smem_addr(&bars.tmem), S::kTmem);
+    // Nothing above depends on the kernels before this one on the stream.
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if (warp == kTablesWarp)
         fill_tables(p, *tables, kColumns, c.lane_tiles, c.pairs);
     fence_before();
@@ -873,12 +922,14 @@ cudaError_t launch(const gnmr_products *h, const Operands &o, const Product &p, 
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = shared_bytes<kColumns>();
     cfg.stream = st;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = 2;
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = 2;
     return cudaLaunchKernelEx(&cfg, product_kernel<kColumns, kOp>, a, b, p);
 }
 
@@ -998,6 +1049,8 @@ gnmr_status gnmr_products_run(gnmr_products *h, const gnmr_product *p, void *str
     q.lanes = wgrad || back ? p->n_in : p->n_out;
     q.depth = wgrad ? 0 : back ? p->n_out : p->n_in;
     q.cols = wgrad ? p->n_out : 0;
+    const int64_t lane_tiles = (int64_t(q.lanes) + kLanes - 1) / kLanes;
+    q.lane_tiles_inverse = static_cast<unsigned>(((int64_t(1) << 32) + lane_tiles - 1) / lane_tiles);
     q.rows = static_cast<int>(p->rows);
     q.groups = p->groups;
     q.offsets = p->d_offsets;

@@ -12,6 +12,7 @@
 
 #include <algorithm>
 #include <cstdint>
+#include <type_traits>
 
 #include "gnmr.h"
 #include "gnmr_internal.h"
@@ -32,35 +33,101 @@ __device__ __forceinline__ unsigned magnitude(float v) { return __float_as_uint(
 
 struct Scale {
     float up, down;
+    unsigned keep;                                   // 0 where the codes are 0 whatever the values
 };
 
 __device__ __forceinline__ Scale scale_of(unsigned amax_bits)
 {
     if (amax_bits >= kInfBits)
-        return {0.0f, __uint_as_float(0x7fc00000u)};
+        return {0.0f, __uint_as_float(0x7fc00000u), 0u};
     const float amax = __uint_as_float(amax_bits);
     const float up = __fmul_rn(127.0f, __frcp_rn(amax));
     if (!(magnitude(up) < kInfBits))                 // amax is 0, or 127 / amax is past fp32
-        return {0.0f, 0.0f};
-    return {up, __fdiv_rn(amax, 127.0f)};
+        return {0.0f, 0.0f, 0u};
+    return {up, __fdiv_rn(amax, 127.0f), ~0u};
 }
 
-// A row that holds a NaN or an infinity has up = 0: its codes are 0, not NaN * 0.
-__device__ __forceinline__ int code_of(float v, const Scale &s)
+// v * up, rounded, plus 1.5 * 2^23, rounded: halves to even at whole numbers, which are
+// then the low bits of the sum.  (Conversions to integers run at an eighth of the rate.
+// Products two at a time; sums are left single: a packed product and a packed sum came out
+// of the assembler as one operation with one rounding, and 63.5 - 2^-18 as 63 for 64.)
+constexpr float kWhole = 12582912.0f;
+
+__device__ __forceinline__ unsigned whole(float v) { return __float_as_uint(__fadd_rn(v, kWhole)); }
+
+__device__ __forceinline__ void whole2(float a, float b, float up_a, float up_b, unsigned &wa, unsigned &wb)
 {
-    return s.up == 0.0f ? 0 : __float2int_rn(__fmul_rn(v, s.up));
+    float pa, pb;
+    asm("{\n.reg .b64 v, u;\nmov.b64 v, {%2, %3};\nmov.b64 u, {%4, %5};\n"
+        "mul.rn.f32x2 v, v, u;\nmov.b64 {%0, %1}, v;\n}"
+        : "=f"(pa), "=f"(pb)
+        : "f"(a), "f"(b), "f"(up_a), "f"(up_b));
+    wa = whole(pa);
+    wb = whole(pb);
 }
 
-__device__ __forceinline__ unsigned pack4(int a, int b, int c, int d)
+__device__ __forceinline__ unsigned low_bytes(unsigned a, unsigned b, unsigned c, unsigned d)
 {
-    return (a & 255u) | (b & 255u) << 8 | (c & 255u) << 16 | static_cast<unsigned>(d) << 24;
+    return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
+}
+
+__device__ __forceinline__ int8_t code_of(float v, const Scale &s)
+{
+    return static_cast<int8_t>(whole(__fmul_rn(v, s.up)) & s.keep);
 }
 
 // 16 bytes of a row, and how many elements they are.
 template <typename T> struct Vec {
     static constexpr int kN = 16 / sizeof(T);
-    alignas(16) T v[kN];
+    uint4 w;
 };
+
+template <typename T> __device__ __forceinline__ void widen(const Vec<T> &v, float (&f)[Vec<T>::kN])
+{
+    const unsigned w[4] = {v.w.x, v.w.y, v.w.z, v.w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(T) == 4) {
+            f[i] = __uint_as_float(w[i]);
+        } else if constexpr (std::is_same_v<T, __nv_bfloat16>) {
+            f[2 * i] = __uint_as_float(w[i] << 16);
+            f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        } else {
+            const float2 p = __half22float2(reinterpret_cast<const __half2 &>(w[i]));
+            f[2 * i] = p.x;
+            f[2 * i + 1] = p.y;
+        }
+    }
+}
+
+// The running maximum of magnitudes in the inputs' own bits, 16-bit types two at a time.
+template <typename T> __device__ __forceinline__ void add_max(unsigned &m, const Vec<T> &v)
+{
+    if constexpr (sizeof(T) == 4) {
+        m = __vimax3_u32(m, v.w.x & 0x7fffffffu, v.w.y & 0x7fffffffu);
+        m = __vimax3_u32(m, v.w.z & 0x7fffffffu, v.w.w & 0x7fffffffu);
+    } else {
+        m = __vimax3_u16x2(m, v.w.x & 0x7fff7fffu, v.w.y & 0x7fff7fffu);
+        m = __vimax3_u16x2(m, v.w.z & 0x7fff7fffu, v.w.w & 0x7fff7fffu);
+    }
+}
+
+// The same as fp32 bits; of the larger half.
+template <typename T> __device__ __forceinline__ unsigned half_bits(unsigned half)
+{
+    if constexpr (std::is_same_v<T, __nv_bfloat16>)
+        return half << 16;
+    else
+        return __float_as_uint(__half2float(__ushort_as_half(static_cast<unsigned short>(half))));
+}
+
+template <typename T> __device__ __forceinline__ unsigned max_bits(unsigned m)
+{
+    if constexpr (sizeof(T) == 4)
+        return m;
+    else
+        return half_bits<T>(max(m & 0xffffu, m >> 16));
+}
 
 struct Matrix {
     const void *x;
@@ -73,21 +140,19 @@ struct Matrix {
 
 // ---- by row ---------------------------------------------------------------
 // kTeam threads hold a row in registers, kHeld 16-byte vectors each, so that it
-// is read once.  A row that they cannot hold is read twice, the second time
-// mostly from L2.
+// is read once, and load the next one while they work on it.  A row that they cannot hold
+// is read twice, the second time mostly from L2.
 template <int kTeam>
 __device__ __forceinline__ unsigned team_max(unsigned m, unsigned *shared)
 {
-#pragma unroll
-    for (int d = 16; d; d >>= 1)
-        m = max(m, __shfl_xor_sync(~0u, m, d));
+    m = __reduce_max_sync(~0u, m);
     if (kTeam > 32) {
         __syncthreads();                             // the last row's maxima have been read
         if ((threadIdx.x & 31) == 0)
             shared[threadIdx.x >> 5] = m;
         __syncthreads();
 #pragma unroll
-        for (int w = 0; w < kThreads / 32; ++w)
+        for (int w = 0; w < kTeam / 32; ++w)
             m = max(m, shared[w]);
     }
     return m;
@@ -97,65 +162,78 @@ template <typename T>
 __device__ __forceinline__ void store_codes(int8_t *to, const Vec<T> &v, const Scale &s)
 {
     constexpr int kN = Vec<T>::kN;
-    unsigned w[kN / 4];
+    float f[kN];
+    widen<T>(v, f);
+    unsigned w[kN];
 #pragma unroll
-    for (int i = 0; i < kN; i += 4)
-        w[i / 4] = pack4(code_of(to_f32(v.v[i]), s), code_of(to_f32(v.v[i + 1]), s), code_of(to_f32(v.v[i + 2]), s),
-                         code_of(to_f32(v.v[i + 3]), s));
-    if (kN == 8)
-        *reinterpret_cast<uint2 *>(to) = make_uint2(w[0], w[kN / 4 - 1]);
+    for (int i = 0; i < kN; i += 2)
+        whole2(f[i], f[i + 1], s.up, s.up, w[i], w[i + 1]);
+    if constexpr (kN == 8)
+        *reinterpret_cast<uint2 *>(to) =
+            make_uint2(low_bytes(w[0], w[1], w[2], w[3]) & s.keep, low_bytes(w[4], w[5], w[6], w[7]) & s.keep);
     else
-        *reinterpret_cast<unsigned *>(to) = w[0];
+        *reinterpret_cast<unsigned *>(to) = low_bytes(w[0], w[1], w[2], w[3]) & s.keep;
 }
 
+// Blocks of kTeam threads, or of 256 where a team is a warp.
+template <int kTeam> constexpr int kBlockOf = kTeam == 32 ? 256 : kTeam;
+
 template <typename T, int kTeam, int kHeld>
-__global__ void __launch_bounds__(kThreads) rows_kernel(Matrix m)
+__global__ void __launch_bounds__(kBlockOf<kTeam>) rows_kernel(Matrix m)
 {
-    constexpr int kN = Vec<T>::kN;
-    __shared__ unsigned s_max[kThreads / 32];
+    constexpr int kN = Vec<T>::kN, kTeams = kBlockOf<kTeam> / kTeam;
+    __shared__ unsigned s_max[kTeam / 32];
     const int lane = threadIdx.x % kTeam;
-    const int64_t total = m.rows * m.groups, step = int64_t(gridDim.x) * (kThreads / kTeam);
+    const int64_t total = m.rows * m.groups, step = int64_t(gridDim.x) * kTeams;
     const int64_t vecs = m.cols / kN;                // whole vectors; the rest one by one
-    for (int64_t r = int64_t(blockIdx.x) * (kThreads / kTeam) + threadIdx.x / kTeam; r < total; r += step) {
-        const int64_t g = r / m.rows, i = r - g * m.rows;
-        const T *x = static_cast<const T *>(m.x) + g * m.group_stride + i * m.stride;
-        int8_t *q = m.q + g * m.q_group_stride + i * m.q_stride;
-        Vec<T> held[kHeld];
-        unsigned amax = 0;
+    const auto row_of = [&](int64_t r) {
+        const int64_t g = m.groups == 1 ? 0 : r / m.rows;
+        return static_cast<const T *>(m.x) + g * m.group_stride + (r - g * m.rows) * m.stride;
+    };
+    const auto load = [&](Vec<T> (&v)[kHeld], const T *x) {
 #pragma unroll
         for (int k = 0; k < kHeld; ++k)
             if (lane + k * kTeam < vecs)
-                *reinterpret_cast<uint4 *>(held[k].v) =
-                    __ldcs(reinterpret_cast<const uint4 *>(x) + lane + k * kTeam);
+                v[k].w = __ldcs(reinterpret_cast<const uint4 *>(x) + lane + k * kTeam);
+    };
+    int64_t r = int64_t(blockIdx.x) * kTeams + threadIdx.x / kTeam;
+    if (r >= total)
+        return;
+    Vec<T> held[kHeld], next[kHeld];
+    load(held, row_of(r));
+    for (;;) {
+        const T *x = row_of(r);
+        if (r + step < total)
+            load(next, row_of(r + step));
+        unsigned own = 0;
 #pragma unroll
         for (int k = 0; k < kHeld; ++k)
             if (lane + k * kTeam < vecs)
-#pragma unroll
-                for (int e = 0; e < kN; ++e)
-                    amax = max(amax, magnitude(to_f32(held[k].v[e])));
-        for (int64_t at = lane + int64_t(kHeld) * kTeam; at < vecs; at += kTeam) {
-            Vec<T> v;
-            *reinterpret_cast<uint4 *>(v.v) = *(reinterpret_cast<const uint4 *>(x) + at);
-#pragma unroll
-            for (int e = 0; e < kN; ++e)
-                amax = max(amax, magnitude(to_f32(v.v[e])));
-        }
+                add_max<T>(own, held[k]);
+        for (int64_t at = lane + int64_t(kHeld) * kTeam; at < vecs; at += kTeam)
+            add_max<T>(own, Vec<T>{*(reinterpret_cast<const uint4 *>(x) + at)});
+        unsigned amax = max_bits<T>(own);
         for (int64_t c = vecs * kN + lane; c < m.cols; c += kTeam)
             amax = max(amax, magnitude(to_f32(x[c])));
         const Scale s = scale_of(team_max<kTeam>(amax, s_max));
         if (lane == 0)
             m.scale[r] = s.down;
+        const int64_t g = m.groups == 1 ? 0 : r / m.rows;
+        int8_t *q = m.q + g * m.q_group_stride + (r - g * m.rows) * m.q_stride;
 #pragma unroll
         for (int k = 0; k < kHeld; ++k)
             if (lane + k * kTeam < vecs)
-                store_codes(q + int64_t(lane + k * kTeam) * kN, held[k], s);
-        for (int64_t at = lane + int64_t(kHeld) * kTeam; at < vecs; at += kTeam) {
-            Vec<T> v;
-            *reinterpret_cast<uint4 *>(v.v) = *(reinterpret_cast<const uint4 *>(x) + at);
-            store_codes(q + at * kN, v, s);
-        }
+                store_codes<T>(q + int64_t(lane + k * kTeam) * kN, held[k], s);
+        for (int64_t at = lane + int64_t(kHeld) * kTeam; at < vecs; at += kTeam)
+            store_codes<T>(q + at * kN, Vec<T>{*(reinterpret_cast<const uint4 *>(x) + at)}, s);
         for (int64_t c = vecs * kN + lane; c < m.cols; c += kTeam)
-            q[c] = static_cast<int8_t>(code_of(to_f32(x[c]), s));
+            q[c] = code_of(to_f32(x[c]), s);
+        r += step;
+        if (r >= total)
+            return;
+#pragma unroll
+        for (int k = 0; k < kHeld; ++k)
+            held[k] = next[k];
     }
 }
 
@@ -178,72 +256,116 @@ __global__ void __launch_bounds__(kThreads) rows_by_element_kernel(Matrix m)
             m.scale[r] = s.down;
 #pragma unroll 8
         for (int64_t c = lane; c < m.cols; c += 32)
-            q[c] = static_cast<int8_t>(code_of(to_f32(x[c]), s));
+            q[c] = code_of(to_f32(x[c]), s);
     }
 }
 
 // ---- by column --------------------------------------------------------------
-// A cluster takes a strip of 64 columns, its CTAs an equal part of the rows
-// each: maxima first, joined over the cluster through distributed shared
-// memory, then the same rows again (from L2) as codes, transposed by shared
-// memory in tiles of 64 columns and 128 rows, 128-byte lines of codes going out.
+// A cluster takes a strip of 64 columns, its CTAs an equal part of the rows each.
+// Parts of up to 32 KiB go to shared memory whole, all of their loads in flight at once;
+// larger ones are read a second time, from L2.  Maxima are joined over the
+// cluster through distributed shared memory; then the part goes out as codes,
+// transposed in tiles of 64 columns and 128 rows, 128-byte lines of codes.
 constexpr int kStrip = 64;
 constexpr int kTileRows = 128;
 constexpr int kPitch = kTileRows / 4 + 1;            // words a column: lanes that read along rows meet no conflict
+constexpr int64_t kHoldBytes = 32 << 10;
 
+template <typename T> constexpr int kStripVecs = 8 / Vec<T>::kN;      // vectors of a thread's 8 columns
+
+// 8 columns of a row, zeros past the last.
 template <typename T, bool kVector>
-__device__ __forceinline__ void load8(const T *x, int64_t cols_left, float (&v)[8])
+__device__ __forceinline__ void load8(const T *x, int64_t cols_left, Vec<T> (&v)[kStripVecs<T>])
 {
     if (kVector && cols_left >= 8) {
 #pragma unroll
-        for (int h = 0; h < 8 / Vec<T>::kN; ++h) {
-            Vec<T> t;
-            *reinterpret_cast<uint4 *>(t.v) = *(reinterpret_cast<const uint4 *>(x) + h);
-#pragma unroll
-            for (int e = 0; e < Vec<T>::kN; ++e)
-                v[h * Vec<T>::kN + e] = to_f32(t.v[e]);
-        }
+        for (int h = 0; h < kStripVecs<T>; ++h)
+            v[h].w = *(reinterpret_cast<const uint4 *>(x) + h);
         return;
     }
+    union {
+        T e[8];
+        Vec<T> v[kStripVecs<T>];
+    } u;
+#pragma unroll
+    for (int h = 0; h < kStripVecs<T>; ++h)
+        u.v[h].w = make_uint4(0, 0, 0, 0);
 #pragma unroll
     for (int e = 0; e < 8; ++e)
-        v[e] = e < cols_left ? to_f32(x[e]) : 0.0f;
+        if (e < cols_left)
+            u.e[e] = x[e];
+#pragma unroll
+    for (int h = 0; h < kStripVecs<T>; ++h)
+        v[h] = u.v[h];
 }
 
-template <typename T, bool kVector>
-__global__ void __launch_bounds__(kThreads) columns_kernel(Matrix m, int parts)
+__device__ __forceinline__ void copy16(void *to, const void *from)
 {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(static_cast<unsigned>(__cvta_generic_to_shared(to))),
+                 "l"(from)
+                 : "memory");
+}
+
+// kHold: parts in shared memory, of whole strips in 16-byte vectors.
+template <typename T, bool kVector, bool kHold>
+__global__ void __launch_bounds__(kThreads) columns_kernel(Matrix m, int parts, int64_t each)
+{
+    constexpr int kVecs = kStripVecs<T>, kN = Vec<T>::kN;
+    extern __shared__ uint4 s_held[];
     __shared__ unsigned s_max[kStrip];
     __shared__ unsigned s_tile[kStrip * kPitch];
     const int tx = threadIdx.x & 7, ty = threadIdx.x >> 3;       // 8 columns; a row of 32
     const int64_t strips = (m.cols + kStrip - 1) / kStrip;
     const int64_t at = blockIdx.x / parts, part = blockIdx.x % parts;
     const int64_t g = at / strips, c0 = (at - g * strips) * kStrip;
-    const int64_t each = (m.rows + int64_t(parts) * kTileRows - 1) / (int64_t(parts) * kTileRows) * kTileRows;
     const int64_t r0 = min(m.rows, part * each), r1 = min(m.rows, r0 + each);
     const int64_t left = m.cols - c0 - 8 * tx;
     const T *x = static_cast<const T *>(m.x) + g * m.group_stride + c0 + 8 * tx;
+    uint4 *held = s_held + kVecs * tx;                           // a row of the strip is 8 kVecs vectors
+    const bool hold = kHold && left >= 8;                        // a ragged strip's last columns come from memory
+    const auto load_row = [&](int64_t r, Vec<T> (&v)[kVecs]) {
+        if (hold)
+            load8<T, true>(reinterpret_cast<const T *>(held + (r - r0) * (8 * kVecs)), 8, v);
+        else
+            load8<T, kVector>(x + r * m.stride, left, v);
+    };
 
     if (threadIdx.x < kStrip)
         s_max[threadIdx.x] = 0;
+    if (hold) {
+        for (int64_t r = r0 + ty; r < r1; r += kThreads / 8)
+#pragma unroll
+            for (int h = 0; h < kVecs; ++h)
+                copy16(held + (r - r0) * (8 * kVecs) + h, x + r * m.stride + h * kN);
+        asm volatile("cp.async.wait_all;" ::: "memory");         // a thread reads what it copied itself
+    }
     __syncthreads();
-    unsigned amax[8] = {};
     if (left > 0) {
+        // of 8 columns: fp32 bits, or pairs of 16-bit magnitudes
+        unsigned own[4 * kVecs] = {};
 #pragma unroll 4
         for (int64_t r = r0 + ty; r < r1; r += kThreads / 8) {
-            float v[8];
-            load8<T, kVector>(x + r * m.stride, left, v);
+            Vec<T> v[kVecs];
+            load_row(r, v);
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-                amax[e] = max(amax[e], magnitude(v[e]));
+            for (int h = 0; h < kVecs; ++h) {
+                const unsigned w[4] = {v[h].w.x, v[h].w.y, v[h].w.z, v[h].w.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    own[4 * h + i] = sizeof(T) == 4 ? max(own[4 * h + i], w[i] & 0x7fffffffu)
+                                                    : __vmaxu2(own[4 * h + i], w[i] & 0x7fff7fffu);
+            }
         }
-    }
+        // maxima: order does not matter
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        amax[e] = max(amax[e], __shfl_xor_sync(~0u, amax[e], 8));
-        amax[e] = max(amax[e], __shfl_xor_sync(~0u, amax[e], 16));
-        if ((threadIdx.x & 31) < 8)
-            atomicMax(&s_max[8 * tx + e], amax[e]);              // a maximum: order does not matter
+        for (int i = 0; i < 4 * kVecs; ++i) {
+            if constexpr (sizeof(T) == 4) {
+                atomicMax(&s_max[8 * tx + i], own[i]);
+            } else {
+                atomicMax(&s_max[8 * tx + 2 * i], half_bits<T>(own[i] & 0xffffu));
+                atomicMax(&s_max[8 * tx + 2 * i + 1], half_bits<T>(own[i] >> 16));
+            }
+        }
     }
     cg::cluster_group cluster = cg::this_cluster();
     cluster.sync();
@@ -258,42 +380,61 @@ __global__ void __launch_bounds__(kThreads) columns_kernel(Matrix m, int parts)
             m.scale[g * m.cols + c0 + threadIdx.x] = scale_of(mine).down;
     }
     __syncthreads();
-    Scale s[8];
+    float up[8];
+    unsigned keep[8];
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-        s[e] = scale_of(s_max[8 * tx + e]);
+    for (int e = 0; e < 8; ++e) {
+        const Scale s = scale_of(s_max[8 * tx + e]);
+        up[e] = s.up;
+        keep[e] = s.keep;
+    }
 
     int8_t *q = m.q + g * m.q_group_stride + c0 * m.q_stride;
     const bool words = ((reinterpret_cast<uintptr_t>(m.q) | m.q_stride | m.q_group_stride) & 3) == 0;
+    const int lane = threadIdx.x & 31;
     for (int64_t t0 = r0; t0 < r1; t0 += kTileRows) {
         if (left > 0) {
-            float v[4][8];
+            unsigned w[4][8];                                    // a row's 8 codes, each a word's low byte
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int64_t r = t0 + 4 * ty + i;
+                Vec<T> v[kVecs] = {};
                 if (r < r1)
-                    load8<T, kVector>(x + r * m.stride, left, v[i]);
-                else
+                    load_row(r, v);
+                float f[8];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        v[i][e] = 0.0f;
+                for (int h = 0; h < kVecs; ++h) {
+                    float part8[kN];
+                    widen<T>(v[h], part8);
+#pragma unroll
+                    for (int e = 0; e < kN; ++e)
+                        f[h * kN + e] = part8[e];
+                }
+#pragma unroll
+                for (int e = 0; e < 8; e += 2)
+                    whole2(f[e], f[e + 1], up[e], up[e + 1], w[i][e], w[i][e + 1]);
             }
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-                s_tile[(8 * tx + e) * kPitch + ty] = pack4(code_of(v[0][e], s[e]), code_of(v[1][e], s[e]),
-                                                           code_of(v[2][e], s[e]), code_of(v[3][e], s[e]));
+                s_tile[(8 * tx + e) * kPitch + ty] = low_bytes(w[0][e], w[1][e], w[2][e], w[3][e]) & keep[e];
         }
         __syncthreads();
-        const int lane = threadIdx.x & 31;
         const int64_t r = t0 + 4 * lane;
-        for (int c = threadIdx.x >> 5; c < kStrip && c0 + c < m.cols; c += kThreads / 32) {
-            const unsigned w = s_tile[c * kPitch + lane];
-            int8_t *to = q + c * m.q_stride + r;
-            if (words && r + 4 <= r1)
-                *reinterpret_cast<unsigned *>(to) = w;
-            else
-                for (int i = 0; i < 4 && r + i < r1; ++i)
-                    to[i] = static_cast<int8_t>(w >> (8 * i));
+        if (words && t0 + kTileRows <= r1 && c0 + kStrip <= m.cols) {
+            int8_t *to = q + (threadIdx.x >> 5) * m.q_stride + r;
+#pragma unroll
+            for (int i = 0; i < kStrip / (kThreads / 32); ++i, to += kThreads / 32 * m.q_stride)
+                *reinterpret_cast<unsigned *>(to) = s_tile[((threadIdx.x >> 5) + i * (kThreads / 32)) * kPitch + lane];
+        } else {
+            for (int c = threadIdx.x >> 5; c < kStrip && c0 + c < m.cols; c += kThreads / 32) {
+                const unsigned w = s_tile[c * kPitch + lane];
+                int8_t *to = q + c * m.q_stride + r;
+                if (words && r + 4 <= r1)
+                    *reinterpret_cast<unsigned *>(to) = w;
+                else
+                    for (int i = 0; i < 4 && r + i < r1; ++i)
+                        to[i] = static_cast<int8_t>(w >> (8 * i));
+            }
         }
         __syncthreads();
     }
@@ -323,18 +464,22 @@ cudaError_t launch_rows(const Matrix &m, int sms, cudaStream_t st)
     const bool vector = ((reinterpret_cast<uintptr_t>(m.x) | (m.stride * sizeof(T)) | (m.group_stride * sizeof(T))) & 15) == 0 &&
                         ((reinterpret_cast<uintptr_t>(m.q) | m.q_stride | m.q_group_stride) % kN) == 0;
     const int64_t total = m.rows * m.groups;
-    const auto grid = [&](int64_t per, int ctas) {
-        return static_cast<unsigned>(std::min<int64_t>((total + per - 1) / per, int64_t(sms) * ctas));
+    const auto launch = [&](auto kernel, int threads, int rows, int ctas) {
+        kernel<<<static_cast<unsigned>(std::min((total + rows - 1) / rows, int64_t(sms) * ctas)), threads, 0, st>>>(m);
+        return cudaGetLastError();
     };
+    const int64_t vecs = m.cols / kN;
     if (!vector)
-        rows_by_element_kernel<T><<<grid(kThreads / 32, 8), kThreads, 0, st>>>(m);
-    else if (m.cols <= 32 * kN * 4)
-        rows_kernel<T, 32, 4><<<grid(kThreads / 32, 8), kThreads, 0, st>>>(m);
-    else if (m.cols <= kThreads * kN * 4)
-        rows_kernel<T, kThreads, 4><<<grid(1, 8), kThreads, 0, st>>>(m);
-    else
-        rows_kernel<T, kThreads, 8><<<grid(1, 5), kThreads, 0, st>>>(m);
-    return cudaGetLastError();
+        return launch(rows_by_element_kernel<T>, kThreads, kThreads / 32, 8);
+    if (vecs <= 32 * 4)
+        return launch(rows_kernel<T, 32, 4>, 256, 8, 4);
+    if (vecs <= 32 * 8)
+        return launch(rows_kernel<T, 32, 8>, 256, 8, 2);
+    if (vecs <= 128 * 4)
+        return launch(rows_kernel<T, 128, 4>, 128, 1, 6);
+    if (vecs <= 128 * 8)
+        return launch(rows_kernel<T, 128, 8>, 128, 1, 4);
+    return launch(rows_kernel<T, 256, 8>, 256, 1, 2);
 }
 
 template <typename T>
@@ -342,14 +487,21 @@ cudaError_t launch_columns(const Matrix &m, int sms, cudaStream_t st)
 {
     const bool vector = ((reinterpret_cast<uintptr_t>(m.x) | (m.stride * sizeof(T)) | (m.group_stride * sizeof(T))) & 15) == 0;
     const int64_t strips = (m.cols + kStrip - 1) / kStrip * m.groups;
-    int parts = 1;
-    while (parts < 8 && m.rows > int64_t(parts) * kTileRows && strips * parts < 8 * int64_t(sms))
-        parts *= 2;
+    constexpr int64_t kRowBytes = kStrip * sizeof(T);
+    const int64_t tiles = std::max<int64_t>((m.rows + kTileRows - 1) / kTileRows, 1);
+    int64_t per = std::max<int64_t>(kHoldBytes / (kRowBytes * kTileRows), (tiles + 7) / 8);      // tiles of a part
+    if (strips * 2 < sms)
+        per = (tiles + 7) / 8;                       // few strips: as many parts as a cluster has
+    const int parts = static_cast<int>((tiles + per - 1) / per);
     if (strips * parts > INT32_MAX)
         return cudaErrorInvalidValue;
+    const int64_t each = per * kTileRows;
+    const bool hold = vector && each * kRowBytes <= kHoldBytes;
+    const auto kernel = hold ? columns_kernel<T, true, true> : vector ? columns_kernel<T, true, false> : columns_kernel<T, false, false>;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(strips * parts));
     cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = hold ? each * kRowBytes : 0;
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -357,8 +509,7 @@ cudaError_t launch_columns(const Matrix &m, int sms, cudaStream_t st)
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return vector ? cudaLaunchKernelEx(&cfg, columns_kernel<T, true>, m, parts)
-                  : cudaLaunchKernelEx(&cfg, columns_kernel<T, false>, m, parts);
+    return cudaLaunchKernelEx(&cfg, kernel, m, parts, each);
 }
 
 gnmr_status fail(gnmr_status s, const char *why)

@@ -14,18 +14,13 @@ def _torch():
     return torch
 
 
-def _codes_of():
+_DTYPES: dict = {}                                 # torch type -> gnmr_dtype
+
+
+def _dtypes():
     torch = _torch()
-    return {torch.bfloat16: N.GNMR_DTYPE_BF16, torch.float16: N.GNMR_DTYPE_F16, torch.float32: N.GNMR_DTYPE_F32}
-
-
-_DTYPES: dict = {}
-
-
-def _dtype_code(dtype):
-    if not _DTYPES:
-        _DTYPES.update(_codes_of())
-    return _DTYPES.get(dtype)
+    _DTYPES.update({torch.bfloat16: N.GNMR_DTYPE_BF16, torch.float16: N.GNMR_DTYPE_F16,
+                    torch.float32: N.GNMR_DTYPE_F32})
 
 
 def _named_dtype(name):
@@ -61,6 +56,10 @@ class ExpertProducts:
         self.device_index = int(device.index if hasattr(device, "index") else device)
         self._h = N.gnmr_products_create(self.device_index)
         self._run = N.load().gnmr_products_run
+        torch = _torch()
+        self._device = torch.device("cuda", self.device_index)
+        self._sixteen = (torch.bfloat16, torch.float16)
+        _dtypes()
 
     # -- lifetime -----------------------------------------------------------
     def close(self) -> None:
@@ -83,109 +82,108 @@ class ExpertProducts:
     # -- argument checks ------------------------------------------------------
     def _tensor(self, t, name, dims, dtypes):
         torch = _torch()
-        if not isinstance(t, torch.Tensor) or not t.is_cuda or t.device.index != self.device_index:
+        if not isinstance(t, torch.Tensor) or t.get_device() != self.device_index:
             raise ValueError(f"{name} must be a CUDA tensor on device {self.device_index}")
         if t.dtype not in dtypes:
             raise ValueError(f"{name} must be {' or '.join(str(d) for d in dtypes)}, got {t.dtype}")
         if t.dim() not in dims:
             raise ValueError(f"{name} must have {' or '.join(str(d) for d in dims)} dimensions, got {t.dim()}")
-        if t.dim() > 1 and t.shape[-1] > 1 and t.stride(-1) != 1:
+
+    def _matrix(self, t, name, dims, dtypes):
+        """(groups, rows, columns, row stride, group stride) of a tensor of contiguous rows."""
+        self._tensor(t, name, dims, dtypes)
+        shape, stride = t.shape, t.stride()
+        rows, cols = shape[-2], shape[-1]
+        if cols > 1 and stride[-1] != 1:
             raise ValueError(f"{name} must have contiguous rows")
-        return t
+        # a single row, or group, has no stride of its own, and torch may give it any
+        row = stride[-2] if rows > 1 else max(stride[-2], cols)
+        if len(shape) == 2:
+            return 1, rows, cols, row, 0
+        return shape[0], rows, cols, row, stride[0] if shape[0] > 1 else 0
 
-    @staticmethod
-    def _row_stride(t):
-        # a single row has no stride of its own, and torch may give it any
-        return t.stride(-2) if t.shape[-2] > 1 else max(t.stride(-2), t.shape[-1])
-
-    def _weight(self, w, name, dtypes):
-        self._tensor(w, name, (2, 3), dtypes)
-        groups = w.shape[0] if w.dim() == 3 else 1
-        return groups, w.shape[-2], w.shape[-1], self._row_stride(w), w.stride(0) if groups > 1 else 0
-
-    def _grouping(self, p, groups, rows, offsets, mask):
+    def _grouping(self, groups, offsets, mask):
+        """Device pointers of offsets and mask, and the mask's stride."""
         torch = _torch()
-        p.groups, p.rows = groups, rows
+        at, bits, step = None, None, 1
         if offsets is not None:
             self._tensor(offsets, "offsets", (1,), (torch.int64,))
             if offsets.numel() != groups + 1 or not offsets.is_contiguous():
                 raise ValueError(f"offsets must hold groups + 1 = {groups + 1} contiguous entries")
-            p.d_offsets = offsets.data_ptr()
+            at = offsets.data_ptr()
         elif groups != 1:
             raise ValueError("offsets may be None for one group only")
         if mask is not None:
             self._tensor(mask, "mask", (1,), (torch.uint8,))
             if mask.numel() != groups:
                 raise ValueError(f"mask must have one entry per group ({groups})")
-            p.d_mask, p.mask_stride = mask.data_ptr(), mask.stride(0) if groups > 1 else 1
+            bits, step = mask.data_ptr(), mask.stride(0) if groups > 1 else 1
+        return at, bits, step
 
-    def _enqueue(self, p, stream, names):
+    def _new(self, shape, dtype, stream):
         torch = _torch()
+        if stream is None:
+            return torch.empty(shape, dtype=dtype, device=self._device)
+        with torch.cuda.stream(stream):
+            return torch.empty(shape, dtype=dtype, device=self._device)
+
+    def _stream(self, stream):
+        return (_torch().cuda.current_stream(self.device_index) if stream is None else stream).cuda_stream
+
+    def _out(self, out, rows, width, dtypes, stream):
+        """(out, its row stride): the tensor given, checked, or a new one of the first type."""
+        if out is None:
+            return self._new((rows, width), dtypes[0], stream), width
+        _, r, c, step, _ = self._matrix(out, "out", (2,), dtypes)
+        if (r, c) != (rows, width):
+            raise ValueError(f"out must be [{rows}, {width}], got [{r}, {c}]")
+        return out, step
+
+    def _enqueue(self, p, stream):
         if not self._h:
             raise ValueError("the products were closed")
-        if stream is None:
-            stream = torch.cuda.current_stream(self.device_index)
-        status = self._run(self._h, ctypes.addressof(p), stream.cuda_stream)
-        if status == N.GNMR_ERR_LAYOUT and not p.d_scratch:
+        handle = self._stream(stream)
+        status = self._run(self._h, ctypes.addressof(p), handle)
+        if status == N.GNMR_ERR_LAYOUT:
             # operands that cannot be read in place: room for their copies, on the same stream
             need = N.gnmr_products_scratch_bytes(p)
-            if need:
-                with torch.cuda.stream(stream):
-                    scratch = torch.empty(need, dtype=torch.uint8, device=torch.device("cuda", self.device_index))
+            if need > p.scratch_bytes:
+                scratch = self._new(need, _torch().uint8, stream)
                 p.d_scratch, p.scratch_bytes = scratch.data_ptr(), need
-                status = self._run(self._h, ctypes.addressof(p), stream.cuda_stream)
+                status = self._run(self._h, ctypes.addressof(p), handle)
         if status:
             N._check(status, None)
 
-    def _out(self, out, rows, width, dtype, stream):
-        torch = _torch()
-        if out is None:
-            dev = torch.device("cuda", self.device_index)
-            if stream is None:
-                return torch.empty(rows, width, dtype=dtype, device=dev)
-            with torch.cuda.stream(stream):
-                return torch.empty(rows, width, dtype=dtype, device=dev)
-        self._tensor(out, "out", (2,), (dtype,))
-        if tuple(out.shape) != (rows, width):
-            raise ValueError(f"out must be [{rows}, {width}], got {list(out.shape)}")
-        return out
-
-    def _rows(self, t, name, width, dtypes):
-        self._tensor(t, name, (2,), dtypes)
-        if t.shape[1] != width:
-            raise ValueError(f"{name} must have {width} columns, got {t.shape[1]}")
-        return t.shape[0]
-
     # -- 16-bit products ------------------------------------------------------
-    def _sixteen(self):
-        torch = _torch()
-        return torch.bfloat16, torch.float16
-
-    def _by_rows(self, op, a, name, w, offsets, out, mask, stream):
-        p = N.gnmr_product()
-        groups, p.n_out, p.n_in, p.w_stride, p.w_group_stride = self._weight(w, "w", self._sixteen())
-        across, to = (p.n_in, p.n_out) if op == N.GNMR_PRODUCT_FORWARD else (p.n_out, p.n_in)
-        rows = self._rows(a, name, across, (w.dtype,))
-        self._grouping(p, groups, rows, offsets, mask)
-        out = self._out(out, rows, to, w.dtype, stream)
-        p.op = op
-        p.dtype = p.out_dtype = _dtype_code(w.dtype)
-        p.d_w = w.data_ptr()
-        if op == N.GNMR_PRODUCT_FORWARD:
-            p.d_x, p.x_stride = a.data_ptr(), self._row_stride(a)
-        else:
-            p.d_dy, p.dy_stride = a.data_ptr(), self._row_stride(a)
-        p.d_out, p.out_stride = out.data_ptr(), self._row_stride(out)
-        self._enqueue(p, stream, (name, "w", "out"))
-        return out
-
     def forward(self, x, w, offsets=None, *, out=None, mask=None, stream=None):
         """y[r] = W_g x[r] for the rows r of every group g: x [rows, n_in] -> [rows, n_out]."""
-        return self._by_rows(N.GNMR_PRODUCT_FORWARD, x, "x", w, offsets, out, mask, stream)
+        groups, n_out, n_in, row, group = self._matrix(w, "w", (2, 3), self._sixteen)
+        dtype = w.dtype
+        _, rows, cols, step, _ = self._matrix(x, "x", (2,), (dtype,))
+        if cols != n_in:
+            raise ValueError(f"x must have {n_in} columns, got {cols}")
+        at, bits, each = self._grouping(groups, offsets, mask)
+        out, across = self._out(out, rows, n_out, (dtype,), stream)
+        code = _DTYPES[dtype]
+        self._enqueue(N.gnmr_product(N.GNMR_PRODUCT_FORWARD, groups, rows, n_out, n_in, code, code, at, bits, each,
+                                     x.data_ptr(), step, None, 0, w.data_ptr(), row, group, None, None,
+                                     out.data_ptr(), across), stream)
+        return out
 
     def input_grad(self, dy, w, offsets=None, *, out=None, mask=None, stream=None):
         """dx[r] = W_g^T dy[r]: dy [rows, n_out] -> [rows, n_in]."""
-        return self._by_rows(N.GNMR_PRODUCT_INPUT_GRAD, dy, "dy", w, offsets, out, mask, stream)
+        groups, n_out, n_in, row, group = self._matrix(w, "w", (2, 3), self._sixteen)
+        dtype = w.dtype
+        _, rows, cols, step, _ = self._matrix(dy, "dy", (2,), (dtype,))
+        if cols != n_out:
+            raise ValueError(f"dy must have {n_out} columns, got {cols}")
+        at, bits, each = self._grouping(groups, offsets, mask)
+        out, across = self._out(out, rows, n_in, (dtype,), stream)
+        code = _DTYPES[dtype]
+        self._enqueue(N.gnmr_product(N.GNMR_PRODUCT_INPUT_GRAD, groups, rows, n_out, n_in, code, code, at, bits, each,
+                                     None, 0, dy.data_ptr(), step, w.data_ptr(), row, group, None, None,
+                                     out.data_ptr(), across), stream)
+        return out
 
     def weight_grad(self, dy, x, offsets=None, *, out, add=False, mask=None, stream=None):
         """out_g = sum over the group's rows of dy[r] x[r]^T, or that added to out_g.
@@ -193,40 +191,38 @@ class ExpertProducts:
         out: [groups, n_out, n_in] (or [n_out, n_in]) of dy's type or fp32, e.g. a view of
         the gradient arena that the monitor reads.  A group without rows gets zeros
         (nothing is added)."""
-        torch = _torch()
-        p = N.gnmr_product()
-        self._tensor(dy, "dy", (2,), self._sixteen())
-        groups, p.n_out, p.n_in, p.out_stride, p.out_group_stride = self._weight(out, "out", (dy.dtype, torch.float32))
-        rows = self._rows(dy, "dy", p.n_out, (dy.dtype,))
-        if self._rows(x, "x", p.n_in, (dy.dtype,)) != rows:
+        _, rows, n_out, dy_step, _ = self._matrix(dy, "dy", (2,), self._sixteen)
+        dtype = dy.dtype
+        _, x_rows, n_in, x_step, _ = self._matrix(x, "x", (2,), (dtype,))
+        if x_rows != rows:
             raise ValueError("dy and x must have the same number of rows")
-        self._grouping(p, groups, rows, offsets, mask)
-        p.op, p.add = N.GNMR_PRODUCT_WEIGHT_GRAD, int(bool(add))
-        p.dtype, p.out_dtype = _dtype_code(dy.dtype), _dtype_code(out.dtype)
-        p.d_dy, p.dy_stride = dy.data_ptr(), self._row_stride(dy)
-        p.d_x, p.x_stride = x.data_ptr(), self._row_stride(x)
-        p.d_out = out.data_ptr()
-        self._enqueue(p, stream, ("dy", "x", "out"))
+        groups, high, wide, row, group = self._matrix(out, "out", (2, 3), (dtype, _torch().float32))
+        if (high, wide) != (n_out, n_in):
+            raise ValueError(f"out must be [{n_out}, {n_in}] for each group, got [{high}, {wide}]")
+        at, bits, each = self._grouping(groups, offsets, mask)
+        self._enqueue(N.gnmr_product(N.GNMR_PRODUCT_WEIGHT_GRAD, groups, rows, n_out, n_in, _DTYPES[dtype],
+                                     _DTYPES[out.dtype], at, bits, each, x.data_ptr(), x_step, dy.data_ptr(), dy_step,
+                                     None, 0, 0, None, None, out.data_ptr(), row, group, bool(add)), stream)
         return out
 
     # -- 8-bit products -------------------------------------------------------
     def _quantize(self, x, columns, stream):
         torch = _torch()
-        self._tensor(x, "x", (2, 3), (torch.bfloat16, torch.float16, torch.float32))
-        groups, rows, cols = x.shape[0] if x.dim() == 3 else 1, x.shape[-2], x.shape[-1]
+        groups, rows, cols, row, group = self._matrix(x, "x", (2, 3), tuple(_DTYPES))
         high, wide = (cols, rows) if columns else (rows, cols)
         held = (wide + 15) // 16 * 16              # rows of codes start at multiples of 16 bytes
-        dev = torch.device("cuda", self.device_index)
-        if stream is None:
-            stream = torch.cuda.current_stream(self.device_index)
-        with torch.cuda.stream(stream):
-            q = torch.empty(*x.shape[:-2], high, held, dtype=torch.int8, device=dev)
-            scale = torch.empty(*x.shape[:-2], high, dtype=torch.float32, device=dev)
-            fn = N.gnmr_quantize_columns if columns else N.gnmr_quantize_rows
-            fn(x.data_ptr(), _dtype_code(x.dtype), groups, rows, cols, self._row_stride(x),
-               x.stride(0) if groups > 1 else 0, q.data_ptr(), held, high * held, scale.data_ptr(),
-               stream.cuda_stream)
-        return q[..., :wide], scale
+        lead = x.shape[:-2]
+        q = self._new((*lead, high, held), torch.int8, stream)
+        scale = self._new((*lead, high), torch.float32, stream)
+        fn = N.gnmr_quantize_columns if columns else N.gnmr_quantize_rows
+        args = (x.data_ptr(), _DTYPES[x.dtype], groups, rows, cols, row, group, q.data_ptr(), held, high * held,
+                scale.data_ptr(), self._stream(stream))
+        if torch.cuda.current_device() == self.device_index:
+            fn(*args)
+        else:
+            with torch.cuda.device(self.device_index):
+                fn(*args)
+        return q if held == wide else q[..., :wide], scale
 
     def quantize_rows(self, x, *, stream=None):
         """8-bit codes of every row of x ([rows, cols] or [groups, rows, cols]; bf16, f16 or
@@ -245,24 +241,19 @@ class ExpertProducts:
         """y[r] = x_scale[r] * w_scale_g * (Wq_g xq[r]) on 8-bit codes; the sum is an exact
         integer (n_in up to 131,071), rounded once to out's type."""
         torch = _torch()
-        p = N.gnmr_product()
-        groups, p.n_out, p.n_in, p.w_stride, p.w_group_stride = self._weight(wq, "wq", (torch.int8,))
-        rows = self._rows(xq, "xq", p.n_in, (torch.int8,))
-        self._grouping(p, groups, rows, offsets, mask)
-        for t, name, n in ((x_scale, "x_scale", rows), (w_scale, "w_scale", groups * p.n_out)):
+        groups, n_out, n_in, row, group = self._matrix(wq, "wq", (2, 3), (torch.int8,))
+        _, rows, cols, step, _ = self._matrix(xq, "xq", (2,), (torch.int8,))
+        if cols != n_in:
+            raise ValueError(f"xq must have {n_in} columns, got {cols}")
+        for t, name, n in ((x_scale, "x_scale", rows), (w_scale, "w_scale", groups * n_out)):
             self._tensor(t, name, (1, 2), (torch.float32,))
             if t.numel() != n or not t.is_contiguous():
                 raise ValueError(f"{name} must hold {n} contiguous entries")
-        if out is not None:
-            self._tensor(out, "out", (2,), (torch.bfloat16, torch.float16, torch.float32))
-            out = self._out(out, rows, p.n_out, out.dtype, stream)
-        else:
-            out = self._out(None, rows, p.n_out, _named_dtype(out_dtype), stream)
-        p.op, p.out_dtype = N.GNMR_PRODUCT_FORWARD_I8, _dtype_code(out.dtype)
-        p.d_x, p.x_stride, p.d_x_scale = xq.data_ptr(), self._row_stride(xq), x_scale.data_ptr()
-        p.d_w, p.d_w_scale = wq.data_ptr(), w_scale.data_ptr()
-        p.d_out, p.out_stride = out.data_ptr(), self._row_stride(out)
-        self._enqueue(p, stream, ("xq", "wq", "out"))
+        at, bits, each = self._grouping(groups, offsets, mask)
+        out, across = self._out(out, rows, n_out, (_named_dtype(out_dtype),) if out is None else tuple(_DTYPES), stream)
+        self._enqueue(N.gnmr_product(N.GNMR_PRODUCT_FORWARD_I8, groups, rows, n_out, n_in, 0, _DTYPES[out.dtype], at,
+                                     bits, each, xq.data_ptr(), step, None, 0, wq.data_ptr(), row, group,
+                                     x_scale.data_ptr(), w_scale.data_ptr(), out.data_ptr(), across), stream)
         return out
 
 
