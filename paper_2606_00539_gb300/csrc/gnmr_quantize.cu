@@ -13,6 +13,7 @@
 #include <algorithm>
 #include <cstdint>
 #include <type_traits>
+#include <utility>
 
 #include "gnmr.h"
 #include "gnmr_internal.h"
@@ -50,7 +51,7 @@ __device__ __forceinline__ Scale scale_of(unsigned amax_bits)
 // v * up, rounded, plus 1.5 * 2^23, rounded: halves to even at whole numbers, which are
 // then the low bits of the sum.  (Conversions to integers run at an eighth of the rate.
 // Products two at a time; sums are left single: a packed product and a packed sum came out
-// of the assembler as one operation with one rounding, and 63.5 - 2^-18 as 63 for 64.)
+// of the assembler as one operation with one rounding: values just below 63.5 as 63 for 64.)
 constexpr float kWhole = 12582912.0f;
 
 __device__ __forceinline__ unsigned whole(float v) { return __float_as_uint(__fadd_rn(v, kWhole)); }
@@ -312,9 +313,11 @@ __global__ void __launch_bounds__(kThreads) columns_kernel(Matrix m, int parts, 
 {
     constexpr int kVecs = kStripVecs<T>, kN = Vec<T>::kN;
     extern __shared__ uint4 s_held[];
-    __shared__ unsigned s_max[kStrip];
+    __shared__ unsigned s_max[kStrip], s_keep[kStrip];
+    __shared__ float s_up[kStrip];
     __shared__ unsigned s_tile[kStrip * kPitch];
     const int tx = threadIdx.x & 7, ty = threadIdx.x >> 3;       // 8 columns; a row of 32
+    const int lane = threadIdx.x & 31;
     const int64_t strips = (m.cols + kStrip - 1) / kStrip;
     const int64_t at = blockIdx.x / parts, part = blockIdx.x % parts;
     const int64_t g = at / strips, c0 = (at - g * strips) * kStrip;
@@ -340,58 +343,67 @@ __global__ void __launch_bounds__(kThreads) columns_kernel(Matrix m, int parts, 
         asm volatile("cp.async.wait_all;" ::: "memory");         // a thread reads what it copied itself
     }
     __syncthreads();
-    if (left > 0) {
-        // of 8 columns: fp32 bits, or pairs of 16-bit magnitudes
-        unsigned own[4 * kVecs] = {};
-#pragma unroll 4
-        for (int64_t r = r0 + ty; r < r1; r += kThreads / 8) {
-            Vec<T> v[kVecs];
-            load_row(r, v);
+    // of 8 columns: fp32 bits, or pairs of 16-bit magnitudes
+    unsigned own[4 * kVecs] = {};
+    const auto take = [&](const Vec<T> (&v)[kVecs], const Vec<T> (&w)[kVecs]) {
 #pragma unroll
-            for (int h = 0; h < kVecs; ++h) {
-                const unsigned w[4] = {v[h].w.x, v[h].w.y, v[h].w.z, v[h].w.w};
+        for (int h = 0; h < kVecs; ++h) {
+            const unsigned a[4] = {v[h].w.x, v[h].w.y, v[h].w.z, v[h].w.w}, b[4] = {w[h].w.x, w[h].w.y, w[h].w.z, w[h].w.w};
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    own[4 * h + i] = sizeof(T) == 4 ? max(own[4 * h + i], w[i] & 0x7fffffffu)
-                                                    : __vmaxu2(own[4 * h + i], w[i] & 0x7fff7fffu);
-            }
+            for (int i = 0; i < 4; ++i)
+                own[4 * h + i] = sizeof(T) == 4 ? __vimax3_u32(own[4 * h + i], a[i] & 0x7fffffffu, b[i] & 0x7fffffffu)
+                                                : __vimax3_u16x2(own[4 * h + i], a[i] & 0x7fff7fffu, b[i] & 0x7fff7fffu);
         }
-        // maxima: order does not matter
+    };
+    if (left > 0) {
+#pragma unroll 2
+        for (int64_t r = r0 + ty; r < r1; r += kThreads / 4) {
+            Vec<T> v[kVecs], w[kVecs];
+            load_row(r, v);
+            load_row(min(r + kThreads / 8, r1 - 1), w);          // past the end: some row again
+            take(v, w);
+        }
+    }
 #pragma unroll
-        for (int i = 0; i < 4 * kVecs; ++i) {
-            if constexpr (sizeof(T) == 4) {
-                atomicMax(&s_max[8 * tx + i], own[i]);
-            } else {
-                atomicMax(&s_max[8 * tx + 2 * i], half_bits<T>(own[i] & 0xffffu));
-                atomicMax(&s_max[8 * tx + 2 * i + 1], half_bits<T>(own[i] >> 16));
-            }
+    for (int i = 0; i < 4 * kVecs; ++i) {
+#pragma unroll
+        for (int d = 8; d < 32; d *= 2) {
+            const unsigned other = __shfl_xor_sync(~0u, own[i], d);
+            own[i] = sizeof(T) == 4 ? max(own[i], other) : __vimax3_u16x2(own[i], other, 0);
+        }
+        if (lane >= 8)
+            continue;
+        if constexpr (sizeof(T) == 4) {                          // maxima: order does not matter
+            atomicMax(&s_max[8 * tx + i], own[i]);
+        } else {
+            atomicMax(&s_max[8 * tx + 2 * i], half_bits<T>(own[i] & 0xffffu));
+            atomicMax(&s_max[8 * tx + 2 * i + 1], half_bits<T>(own[i] >> 16));
         }
     }
     cg::cluster_group cluster = cg::this_cluster();
     cluster.sync();
-    unsigned mine = 0;
-    if (threadIdx.x < kStrip)
-        for (int k = 0; k < parts; ++k)
-            mine = max(mine, cluster.map_shared_rank(s_max, k)[threadIdx.x]);
-    cluster.sync();                                              // every CTA has read every other's
     if (threadIdx.x < kStrip) {
-        s_max[threadIdx.x] = mine;
+        unsigned all = 0;
+        for (int k = 0; k < parts; ++k)
+            all = max(all, cluster.map_shared_rank(s_max, k)[threadIdx.x]);
+        const Scale s = scale_of(all);
+        s_up[threadIdx.x] = s.up;
+        s_keep[threadIdx.x] = s.keep;
         if (part == 0 && c0 + threadIdx.x < m.cols)
-            m.scale[g * m.cols + c0 + threadIdx.x] = scale_of(mine).down;
+            m.scale[g * m.cols + c0 + threadIdx.x] = s.down;
     }
     __syncthreads();
+    auto others = cluster.barrier_arrive();                      // no CTA ends before every other has read its maxima
     float up[8];
     unsigned keep[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        const Scale s = scale_of(s_max[8 * tx + e]);
-        up[e] = s.up;
-        keep[e] = s.keep;
+        up[e] = s_up[8 * tx + e];
+        keep[e] = s_keep[8 * tx + e];
     }
 
     int8_t *q = m.q + g * m.q_group_stride + c0 * m.q_stride;
     const bool words = ((reinterpret_cast<uintptr_t>(m.q) | m.q_stride | m.q_group_stride) & 3) == 0;
-    const int lane = threadIdx.x & 31;
     for (int64_t t0 = r0; t0 < r1; t0 += kTileRows) {
         if (left > 0) {
             unsigned w[4][8];                                    // a row's 8 codes, each a word's low byte
@@ -438,6 +450,7 @@ __global__ void __launch_bounds__(kThreads) columns_kernel(Matrix m, int parts, 
         }
         __syncthreads();
     }
+    cluster.barrier_wait(std::move(others));
 }
 
 // ---- launches -----------------------------------------------------------------
