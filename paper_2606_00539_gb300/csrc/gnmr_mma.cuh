@@ -18,7 +18,7 @@ __device__ __forceinline__ uint32_t smem_addr(const void *p)
 __device__ __forceinline__ uint32_t cta_rank()
 {
     uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    asm volatile("mov.u32 %0, %cluster_ctarank;" : "=r"(r));
     return r;
 }
 
@@ -175,6 +175,15 @@ __device__ __forceinline__ void multiply(uint32_t tmem, uint64_t a, uint64_t b, 
                  : "memory");
 }
 
+// The same with A's 16 elements of each lane in tensor memory, two to a column.
+__device__ __forceinline__ void multiply(uint32_t tmem, uint32_t a, uint64_t b, uint32_t shape, bool add)
+{
+    asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\n"
+                 "tcgen05.mma.cta_group::2.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(tmem),
+                 "r"(a), "l"(b), "r"(shape), "r"(static_cast<uint32_t>(add))
+                 : "memory");
+}
+
 // Arrives on `bar` in both CTAs once every multiply issued so far is done.
 __device__ __forceinline__ void commit(uint32_t bar)
 {
@@ -202,5 +211,17 @@ __device__ __forceinline__ void load_wait(uint32_t (&v)[16])
                  :
                  : "memory");
 }
+
+// 32 columns of this warp's 32 lanes; complete after store_wait.
+__device__ __forceinline__ void store32(uint32_t tmem, const uint32_t (&v)[32])
+{
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+                 "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+                 :
+                 : "r"(tmem), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]), "r"(v[22]), "r"(v[23]), "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31])
+                 : "memory");
+}
+
+__device__ __forceinline__ void store_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 }  // namespace gnmr_mma

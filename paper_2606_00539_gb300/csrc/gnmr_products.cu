@@ -36,37 +36,17 @@
 
 #include "gnmr.h"
 #include "gnmr_internal.h"
-#include "gnmr_mma.cuh"
+#include "gnmr_products.h"
+#include "gnmr_tiles.cuh"
 
 namespace {
 
-constexpr int kMaxGroups = 2048;
-constexpr int kMaxPairs = 80;
-constexpr int kMaxParts = 2 * kMaxPairs;               // split tiles' parts in one call
-constexpr int64_t kPartFloats = 256 * 256;             // one part: both CTAs' lanes by the columns
+using namespace gnmr_tiles;
+using gnmr::Operand;
+using gnmr::Operands;
 
-}  // namespace
-
-struct gnmr_products {
-    int device = 0;
-    int pairs = 1;
-    float *parts = nullptr;            // [kMaxParts][kPartFloats]
-    unsigned *tickets = nullptr;       // [kMaxParts][2], 0 between calls
-    int *gave_up = nullptr;            // host memory that the kernels can write
-    void *dmem = nullptr;
-    CUresult (*encode)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
-                       const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
-                       CUtensorMapL2promotion, CUtensorMapFloatOOBfill) = nullptr;
-};
-
-namespace {
-
-using namespace gnmr_mma;
-
-constexpr int kLanes = 256;                            // of a pair's tile
 constexpr int kStep = 64;                              // contraction steps of a stage: 128-byte rows of 16 bits
-constexpr int kEpilogueWarps = 8;
-constexpr int kProducerWarp = 0, kMultiplyWarp = 1, kTailWarp = 2, kTablesWarp = 3, kFirstEpilogueWarp = 4;
+constexpr int kProducerWarp = 0, kMultiplyWarp = 1, kTailWarp = 2, kTablesWarp = 3;
 constexpr int kThreads = 32 * (kFirstEpilogueWarp + kEpilogueWarps);
 // The epilogue's warpgroups hold 128 sums a thread: 216 registers there and 72 in the
 // others' warpgroup, together the 168 a thread that the block is launched with.
@@ -82,46 +62,6 @@ template <int kColumns> struct Shape {
     static constexpr int kStages = kColumns == 256 ? 6 : 8;
     static constexpr int kBox = kColumns == 256 ? 64 : 16;
     static constexpr int kTmem = 2 * kColumns;
-    static constexpr int kPieces = kColumns / 2 / 16;  // 16-column pieces of an epilogue warp
-};
-
-struct Product {
-    int lanes, depth, cols;            // depth, or cols, is 0 where it is a group's rows
-    int rows, groups;
-    const int64_t *offsets;
-    const uint8_t *mask;
-    int64_t mask_stride;
-    int want;                          // groups computed: mask byte != 0 (1), == 0 (0)
-    unsigned lane_tiles_inverse;       // ceil(2^32 / tiles of 256 lanes)
-    int a_by_group;                    // A's third coordinate is the group
-    int bf16;
-    int chunk;                         // stages of a piece
-    void *out;
-    int out_type;
-    int pairs_aligned;                 // two outputs of a row may be stored as one
-    int add;
-    int64_t out_col, out_group;
-    const float *lane_scale, *col_scale;
-    float *parts;
-    unsigned *tickets;
-    int *gave_up;
-};
-
-// ---- work: tiles of every group, and their parts --------------------------------
-
-struct Tables {
-    int first[kMaxGroups + 1];         // tiles before group g; in the end all of them
-    int row[kMaxGroups + 1];           // first row of group g; in the end the last group's end
-    uint16_t each[kMaxGroups];         // columns of group g's tiles
-    int split;                         // parts of every tile's contraction
-};
-
-struct Item {
-    int g, lane0, col0, cols;          // the tile: the pair's lanes, and its columns
-    int row0;                          // the group's first row
-    int depth, k0, k1;                 // the whole contraction; the stages of this part
-    int tile, part;
-    bool tail;                         // the last stage holds rows past the group's end
 };
 
 // The stage with the tail is loaded first and multiplied fourth (or last): clearing it
@@ -129,263 +69,7 @@ struct Item {
 // the ring, so that it is never waited for by a stage that waits for its place.
 constexpr int kTailTurn = 3;
 
-__device__ __forceinline__ int parts_of(int n, int each) { return (n + each - 1) / each; }
-
-// Filled by one warp.  Offsets are clamped to [0, rows] and made not decreasing.
-__device__ __forceinline__ void fill_tables(const Product &p, Tables &t, int most, int lane_tiles, int pairs)
-{
-    const int lane = threadIdx.x & 31;
-    int carry = 0;
-    for (int j0 = 0; j0 <= p.groups; j0 += 32) {
-        const int j = j0 + lane;
-        int at = j == 0 ? 0 : p.rows;
-        if (p.offsets && j <= p.groups)
-            at = static_cast<int>(min(max(p.offsets[j], int64_t(0)), int64_t(p.rows)));
-        at = max(at, carry);
-#pragma unroll
-        for (int d = 1; d < 32; d *= 2) {
-            const int v = __shfl_up_sync(~0u, at, d);
-            if (lane >= d)
-                at = max(at, v);
-        }
-        if (j <= p.groups)
-            t.row[j] = at;
-        carry = __shfl_sync(~0u, at, 31);
-    }
-    __syncwarp();
-    int tiles = 0, deepest = 0;
-    for (int g0 = 0; g0 < p.groups; g0 += 32) {
-        const int g = g0 + lane;
-        int n = 0;
-        if (g < p.groups && (!p.mask || (p.mask[g * p.mask_stride] != 0) == (p.want != 0))) {
-            const int rows = t.row[g + 1] - t.row[g];
-            const int cols = p.cols ? p.cols : rows, across = parts_of(cols, most);
-            n = lane_tiles * across;
-            // a group's columns are shared out evenly, in multiples of 32
-            t.each[g] = static_cast<uint16_t>(across ? parts_of(parts_of(cols, across), 32) * 32 : 0);
-            deepest = max(deepest, p.depth ? p.depth : rows);
-        }
-        int sum = n;
-#pragma unroll
-        for (int d = 1; d < 32; d *= 2) {
-            const int v = __shfl_up_sync(~0u, sum, d);
-            if (lane >= d)
-                sum += v;
-        }
-        if (g < p.groups)
-            t.first[g] = tiles + sum - n;
-        tiles += __shfl_sync(~0u, sum, 31);
-    }
-    // Few tiles: the number of parts that takes the fewest rounds of stages, a
-    // part costing about six stages more for its beginning and its joining.
-    int best = 1;
-    if (tiles > 0 && tiles < pairs) {
-        const int stages = parts_of(__reduce_max_sync(~0u, deepest), kStep), parts = lane + 1;
-        const bool fits = parts == 1 || (tiles * parts <= min(2 * pairs, kMaxParts) && 2 * parts <= stages);
-        const int cost = fits ? parts_of(tiles * parts, pairs) * (parts_of(stages, parts) + (parts > 1 ? 6 : 0)) : INT32_MAX;
-        const int least = __reduce_min_sync(~0u, cost);
-        best = __ffs(__ballot_sync(~0u, cost == least));
-    }
-    if (lane == 0) {
-        t.first[p.groups] = tiles;
-        t.split = best;
-    }
-}
-
-// Item i of the call, by a whole warp that comes with growing i.  g: the group of the one
-// before, 0 at first.
-__device__ __forceinline__ Item item_of(const Product &p, const Tables &t, int lane_tiles, int i, int &g)
-{
-    Item it;
-    it.tile = t.split == 1 ? i : i / t.split;
-    it.part = i - it.tile * t.split;
-    for (;;) {                                       // the last group that begins at or before the tile
-        const int next = g + 1 + (threadIdx.x & 31);
-        const unsigned past = __ballot_sync(~0u, next >= p.groups || t.first[next] > it.tile);
-        if (past) {
-            g += __ffs(past) - 1;
-            break;
-        }
-        g += 32;
-    }
-    it.g = g;
-    it.row0 = t.row[g];
-    const int rows = t.row[g + 1] - it.row0, at = it.tile - t.first[g], each = t.each[g];
-    int c = at;                                      // at / lane_tiles
-    if (lane_tiles > 1) {
-        c = __umulhi(at, p.lane_tiles_inverse);      // that, or one more
-        c -= c * lane_tiles > at;
-    }
-    it.lane0 = (at - c * lane_tiles) * kLanes;
-    it.col0 = c * each;
-    it.cols = min(each, (p.cols ? p.cols : rows) - it.col0);
-    it.depth = p.depth ? p.depth : rows;
-    const int stages = parts_of(it.depth, kStep);
-    it.k0 = 0;
-    it.k1 = stages;
-    if (t.split > 1) {
-        it.k0 = stages * it.part / t.split;
-        it.k1 = stages * (it.part + 1) / t.split;
-    }
-    it.tail = !p.depth && it.depth % kStep && it.k0 < it.k1 && it.k1 == stages;
-    return it;
-}
-
-// ---- outputs --------------------------------------------------------------------
-
-template <int kOut> __device__ __forceinline__ unsigned pack(float lo, float hi)
-{
-    if (kOut == GNMR_DTYPE_BF16) {
-        const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
-        return reinterpret_cast<const unsigned &>(v);
-    }
-    const __half2 v = __floats2half2_rn(lo, hi);
-    return reinterpret_cast<const unsigned &>(v);
-}
-
-template <int kOut> __device__ __forceinline__ float load_out(const char *at)
-{
-    return kOut == GNMR_DTYPE_F32    ? *reinterpret_cast<const float *>(at)
-           : kOut == GNMR_DTYPE_BF16 ? __bfloat162float(*reinterpret_cast<const __nv_bfloat16 *>(at))
-                                     : __half2float(*reinterpret_cast<const __half *>(at));
-}
-
-// Two columns of this thread's lane become one column of two lanes: the even lane gets
-// the first column's, the odd lane the second's.
-template <int kOut> __device__ __forceinline__ unsigned exchange(float first, float second, unsigned which)
-{
-    const unsigned w = pack<kOut>(first, second);
-    return __byte_perm(w, __shfl_xor_sync(~0u, w, 1), which);
-}
-
-// This warp's sums to the outputs: lane `lane` of columns col .. col + span - 1 of the
-// tile.  Two lanes' 16-bit values of a column go out as one where they can: 64
-// contiguous bytes a column from a warp.
-template <int kPieces, bool kCodes, int kOut>
-__device__ __forceinline__ void finish(const Product &p, const Item &it, uint32_t (&acc)[kPieces][16], int lane, int col, int span)
-{
-    constexpr int kBytes = kOut == GNMR_DTYPE_F32 ? 4 : 2;
-    const int64_t step = p.out_col * kBytes;
-    const int64_t row = p.cols ? it.col0 + col : int64_t(it.row0) + it.col0 + col;
-    char *out = static_cast<char *>(p.out) + (p.cols ? it.g * p.out_group * kBytes : 0) + row * step + int64_t(lane) * kBytes;
-    const int left = it.cols - col, odd = lane & 1;
-    const bool mine = lane < p.lanes;
-    const bool whole = (lane | 31) < p.lanes && (kBytes == 4 || (p.pairs_aligned && !p.add));
-    const unsigned which = odd ? 0x3276 : 0x5410;
-    float by_lane = 0.0f;
-    const float *by_col = nullptr;
-    if (kCodes) {
-        by_lane = mine ? p.lane_scale[int64_t(it.g) * p.lanes + lane] : 0.0f;
-        by_col = p.col_scale + it.row0 + it.col0 + col;
-    }
-    if (whole && kBytes == 2)
-        out += odd ? step - 2 : 0;
-#pragma unroll
-    for (int q = 0; q < kPieces; ++q) {
-        const int n = min(span, left) - q * 16;          // columns of this piece that there are
-        if (n <= 0)
-            break;
-        float v[16];
-#pragma unroll
-        for (int j = 0; j < 16; ++j)
-            v[j] = kCodes ? (j < n ? by_col[q * 16 + j] : 0.0f) : __uint_as_float(acc[q][j]);
-        if (kCodes)
-#pragma unroll
-            for (int j = 0; j < 16; ++j)
-                v[j] = static_cast<float>(static_cast<int>(acc[q][j])) * v[j] * by_lane;
-        if (whole && n >= 16) {
-            if (kBytes == 4) {
-                if (p.add) {
-                    float old[16];
-                    const char *from = out;
-#pragma unroll
-                    for (int j = 0; j < 16; ++j, from += step)
-                        old[j] = *reinterpret_cast<const float *>(from);
-#pragma unroll
-                    for (int j = 0; j < 16; ++j)
-                        v[j] += old[j];
-                }
-#pragma unroll
-                for (int j = 0; j < 16; ++j, out += step)
-                    *reinterpret_cast<float *>(out) = v[j];
-            } else {
-#pragma unroll
-                for (int j = 0; j < 16; j += 2, out += 2 * step)
-                    *reinterpret_cast<unsigned *>(out) = exchange<kOut>(v[j], v[j + 1], which);
-            }
-            continue;
-        }
-        if (whole && kBytes == 2)                        // back to this lane's own place in the first column
-            out -= odd ? step - 2 : 0;
-        if (p.add)
-#pragma unroll
-            for (int j = 0; j < 16; ++j)
-                if (mine && j < n)
-                    v[j] += load_out<kOut>(out + j * step);
-        if (kBytes == 4) {
-#pragma unroll
-            for (int j = 0; j < 16; ++j)
-                if (mine && j < n)
-                    *reinterpret_cast<float *>(out + j * step) = v[j];
-        } else {
-#pragma unroll
-            for (int j = 0; j < 16; j += 2) {
-                const unsigned w = exchange<kOut>(v[j], v[j + 1], which);
-                char *to = out - 2 * odd + (j + odd) * step;     // the column that this thread writes, two lanes of it
-                if (j + odd < n) {
-                    if (p.pairs_aligned && (lane | 1) < p.lanes) {
-                        *reinterpret_cast<unsigned *>(to) = w;
-                    } else {
-                        if ((lane & ~1) < p.lanes)
-                            *reinterpret_cast<uint16_t *>(to) = static_cast<uint16_t>(w);
-                        if ((lane | 1) < p.lanes)
-                            *reinterpret_cast<uint16_t *>(to + 2) = static_cast<uint16_t>(w >> 16);
-                    }
-                }
-            }
-        }
-        out += 16 * step;
-    }
-}
-
-// The first piece's sums, or another's added to them.
-template <bool kCodes>
-__device__ __forceinline__ void begin_sum(uint32_t (&acc)[16])
-{
-    if (kCodes)
-#pragma unroll
-        for (int j = 0; j < 16; ++j)
-            acc[j] = __float2int_rn(__uint_as_float(acc[j]));
-}
-
-template <bool kCodes>
-__device__ __forceinline__ void add_to_sum(uint32_t (&acc)[16], const uint32_t (&v)[16])
-{
-#pragma unroll
-    for (int j = 0; j < 16; ++j)
-        acc[j] = kCodes ? acc[j] + __float2int_rn(__uint_as_float(v[j]))
-                        : __float_as_uint(__uint_as_float(acc[j]) + __uint_as_float(v[j]));
-}
-
 // ---- the kernel -------------------------------------------------------------------
-
-struct Barriers {
-    uint64_t full[8], empty[8];        // stages; `full` counts in the first CTA of the pair
-    uint64_t tail[8];                  // a stage that the tail warp looks at first
-    uint64_t done[2], drained[2];      // halves of tensor memory; `drained` counts in the first CTA
-    uint64_t written, counted;         // of a split tile's part: by its warps, and its ticket
-    uint32_t tmem;
-    unsigned last;                     // whether this CTA is a split tile's last
-};
-
-// What the roles of a CTA share.
-struct Cta {
-    uint8_t *stages;
-    const Tables *tables;
-    Barriers *bars;
-    uint32_t rank, tmem;
-    int pair, pairs, lane_tiles, items;
-};
 
 // The contraction is a group's rows; lanes, or columns, lie along an operand's rows.
 __host__ __device__ constexpr bool rows_deep(int op) { return op == GNMR_PRODUCT_WEIGHT_GRAD; }
@@ -409,7 +93,7 @@ __device__ __forceinline__ bool load_stages(const CUtensorMap &map_a, const CUte
     int stage = 0;
     uint32_t phase = 1;
     for (int i = c.pair, g = 0; i < c.items; i += c.pairs) {
-        const Item it = item_of(p, *c.tables, c.lane_tiles, i, g);
+        const Item it = item_of<kStep>(p, *c.tables, c.lane_tiles, i, g);
         const int half = (it.cols + 31) / 32 * 16;                         // B's columns in this CTA
         const int a_lane = it.lane0 + c.rank * 128, b_col = it.col0 + c.rank * half + (rows_deep(kOp) ? 0 : it.row0);
         const int boxes = parts_of(half, kBoxB), za = p.a_by_group ? it.g : 0;
@@ -463,7 +147,7 @@ __device__ __forceinline__ bool multiply_stages(const Product &p, const Cta &c)
     int stage = 0, half = 0;
     uint32_t phase = 0, free_phase = 1;                  // free_phase: of both halves, while half is 0
     for (int i = c.pair, g = 0; i < c.items; i += c.pairs) {
-        const Item it = item_of(p, *c.tables, c.lane_tiles, i, g);
+        const Item it = item_of<kStep>(p, *c.tables, c.lane_tiles, i, g);
         const uint32_t idesc = shape(p.bf16, a_along_lanes(kOp), b_along_columns(kOp), (it.cols + 31) / 32 * 32);
         const int count = it.k1 - it.k0, turn = it.tail ? min(kTailTurn, count - 1) : -1;
         const int first = stage;
@@ -472,7 +156,7 @@ __device__ __forceinline__ bool multiply_stages(const Product &p, const Cta &c)
             if (!wait(drained + half * 8, free_phase))
                 return false;
             fence_after();
-            const int stop = min(count, k + p.chunk);
+            const int stop = min(count, k + p.piece / kStep);
             const uint32_t sums = c.tmem + half * kColumns;
             for (bool add = false; k < stop; ++k, add = true) {
                 int at = stage, left = it.depth - (it.k0 + k) * kStep;
@@ -525,7 +209,7 @@ __device__ __forceinline__ bool clear_tails(const Product &p, const Cta &c)
     int stage = 0;
     uint32_t phase = 0;                                  // a bit for each stage
     for (int i = c.pair, g = 0; i < c.items; i += c.pairs) {
-        const Item it = item_of(p, *c.tables, c.lane_tiles, i, g);
+        const Item it = item_of<kStep>(p, *c.tables, c.lane_tiles, i, g);
         if (it.tail) {
             const int left = it.depth % kStep, at = stage;
             if (!wait(smem_addr(&c.bars->tail[at]), (phase >> at) & 1))
@@ -542,131 +226,6 @@ __device__ __forceinline__ bool clear_tails(const Product &p, const Cta &c)
                 arrive_release(full + at * 8);
         }
         stage = (stage + it.k1 - it.k0) % S::kStages;
-    }
-    return true;
-}
-
-// A split tile: this part goes to memory, and the last CTA of its rank to get here
-// takes the sum of all parts, in their order.  1: it has; 0: another will; -1: gave up.
-template <int kColumns, bool kCodes>
-__device__ __forceinline__ int join_parts(const Product &p, const Cta &c, const Item &it, uint32_t (&acc)[Shape<kColumns>::kPieces][16],
-                                          int span, int col, int warp, uint32_t turn)
-{
-    using S = Shape<kColumns>;
-    const int lane = threadIdx.x & 31, split = c.tables->split;
-    uint32_t *part = reinterpret_cast<uint32_t *>(p.parts) + int64_t(it.tile) * split * kPartFloats +
-                     c.rank * (kPartFloats / 2) + (warp & 3) * 32 + lane;
-#pragma unroll
-    for (int q = 0; q < S::kPieces; ++q)
-        if (q * 16 < span)
-#pragma unroll
-            for (int j = 0; j < 16; ++j)
-                part[it.part * kPartFloats + (col + q * 16 + j) * 128] = acc[q][j];
-    __threadfence();
-    __syncwarp();
-    if (lane == 0)
-        arrive_release(in_cta(smem_addr(&c.bars->written), c.rank));
-    if (warp == kFirstEpilogueWarp) {
-        if (!wait(smem_addr(&c.bars->written), turn))
-            return -1;
-        if (lane == 0) {
-            __threadfence();
-            unsigned *ticket = p.tickets + 2 * it.tile + c.rank;
-            c.bars->last = atomicAdd(ticket, 1u) + 1 == static_cast<unsigned>(split);
-            if (c.bars->last)
-                *ticket = 0;
-            __threadfence();
-            arrive_release(in_cta(smem_addr(&c.bars->counted), c.rank));
-        }
-        __syncwarp();
-    }
-    if (!wait(smem_addr(&c.bars->counted), turn))
-        return -1;
-    if (!c.bars->last)
-        return 0;
-#pragma unroll
-    for (int q = 0; q < S::kPieces; ++q)
-        if (q * 16 < span) {
-            for (int s = 0; s < split; ++s)
-#pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                    const uint32_t v = __ldcg(part + s * kPartFloats + (col + q * 16 + j) * 128);
-                    if (s == 0)
-                        acc[q][j] = v;
-                    else
-                        acc[q][j] = kCodes ? acc[q][j] + v : __float_as_uint(__uint_as_float(acc[q][j]) + __uint_as_float(v));
-                }
-        }
-    return 1;
-}
-
-template <int kColumns, bool kCodes>
-__device__ __forceinline__ bool write_outputs(const Product &p, const Cta &c)
-{
-    using S = Shape<kColumns>;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int quarter = warp & 3, side = (warp - kFirstEpilogueWarp) >> 2;
-    const uint32_t done = smem_addr(&c.bars->done[0]), drained = in_cta(smem_addr(&c.bars->drained[0]), 0);
-    int half = 0;
-    uint32_t phase = 0, joins = 0;
-    for (int i = c.pair, g = 0; i < c.items; i += c.pairs) {
-        const Item it = item_of(p, *c.tables, c.lane_tiles, i, g);
-        const int span = (it.cols + 31) / 32 * 16;                          // columns of this warp
-        const int at = it.lane0 + c.rank * 128 + quarter * 32 + lane, col = side * span;
-        uint32_t acc[S::kPieces][16];
-        if (it.k0 == it.k1)
-#pragma unroll
-            for (int q = 0; q < S::kPieces; ++q)
-#pragma unroll
-                for (int j = 0; j < 16; ++j)
-                    acc[q][j] = 0;
-        for (int k = it.k0; k < it.k1; k += p.chunk) {
-            if (!wait(done + half * 8, phase))
-                return false;
-            fence_after();
-            const uint32_t from = c.tmem + half * kColumns + (uint32_t(quarter * 32) << 16) + col;
-            if (k == it.k0) {
-#pragma unroll
-                for (int q = 0; q < S::kPieces; ++q)
-                    if (q * 16 < span)
-                        load16(from + q * 16, acc[q]);
-#pragma unroll
-                for (int q = 0; q < S::kPieces; ++q) {
-                    load_wait(acc[q]);
-                    begin_sum<kCodes>(acc[q]);
-                }
-            } else {
-#pragma unroll
-                for (int q = 0; q < S::kPieces; ++q)
-                    if (q * 16 < span) {
-                        uint32_t v[16];
-                        load16(from + q * 16, v);
-                        load_wait(v);
-                        add_to_sum<kCodes>(acc[q], v);
-                    }
-            }
-            fence_before();
-            __syncwarp();
-            if (lane == 0)
-                arrive(drained + half * 8);
-            if (half ^= 1; half == 0)
-                phase ^= 1;
-        }
-        if (c.tables->split > 1) {
-            const int mine = join_parts<kColumns, kCodes>(p, c, it, acc, span, col, warp, joins++ & 1);
-            if (mine < 0)
-                return false;
-            if (mine == 0)
-                continue;
-        }
-        if (p.add && it.depth == 0)
-            continue;                                    // nothing to add
-        if (p.out_type == GNMR_DTYPE_F32)
-            finish<S::kPieces, kCodes, GNMR_DTYPE_F32>(p, it, acc, at, col, span);
-        else if (p.out_type == GNMR_DTYPE_BF16)
-            finish<S::kPieces, kCodes, GNMR_DTYPE_BF16>(p, it, acc, at, col, span);
-        else
-            finish<S::kPieces, kCodes, GNMR_DTYPE_F16>(p, it, acc, at, col, span);
     }
     return true;
 }
@@ -693,16 +252,11 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         prefetch_map(&map_a);
         prefetch_map(&map_b);
         for (int s = 0; s < S::kStages; ++s) {
-            barrier_init(smem_addr(&bars.full[s]), 2);
+            barrier_init(smem_addr(&bars.full[s]), 2);               // counts in the first CTA, from both
             barrier_init(smem_addr(&bars.empty[s]), 1);
             barrier_init(smem_addr(&bars.tail[s]), 1);
         }
-        for (int h = 0; h < 2; ++h) {
-            barrier_init(smem_addr(&bars.done[h]), 1);
-            barrier_init(smem_addr(&bars.drained[h]), 2 * kEpilogueWarps);
-        }
-        barrier_init(smem_addr(&bars.written), kEpilogueWarps);
-        barrier_init(smem_addr(&bars.counted), 1);
+        init_epilogue_barriers(bars);
         barrier_init_fence();
     }
     if (warp == kMultiplyWarp)
@@ -711,7 +265,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if (warp == kTablesWarp)
-        fill_tables(p, *tables, kColumns, c.lane_tiles, c.pairs);
+        fill_tables<kStep>(p, *tables, kColumns, c.lane_tiles, c.pairs);
     fence_before();
     __syncthreads();
     cluster_sync();
@@ -730,55 +284,11 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             fine = clear_tails<kColumns>(p, c);
     } else {
         more_registers<kEpilogueRegisters>();
-        fine = write_outputs<kColumns, kOp == GNMR_PRODUCT_FORWARD_I8>(p, c);
+        fine = write_outputs<kColumns, kOp == GNMR_PRODUCT_FORWARD_I8, kStep>(p, c);
     }
-    __syncwarp();
-    if (!fine) {
-        // Loads that a role left behind are in long before this ends.
-        if (lane == 0)
-            *p.gave_up = 1;
-        for (int i = 0; i < 1000; ++i)
-            __nanosleep(1000);
-    }
-    fence_before();
-    __syncthreads();
-    cluster_sync();
-    fence_after();
+    finish_pair(fine, p.gave_up);
     if (warp == kMultiplyWarp)
         tmem_free(c.tmem, S::kTmem);
-}
-
-// ---- operands that the TMA unit cannot read, and codes as 16-bit numbers ------------
-// [groups][rows][cols] with any strides to rows of `held` 16-bit elements (a multiple of
-// eight), the rest of each row 0.  Bound by memory.
-struct Copy {
-    const void *from;
-    uint16_t *to;
-    int64_t rows, cols, stride, group_stride, held, total;   // total: vectors of 8
-};
-
-template <typename T>
-__global__ void __launch_bounds__(256) copy_kernel(Copy c)
-{
-    const int64_t across = c.held / 8;
-    for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < c.total; i += int64_t(gridDim.x) * 256) {
-        const int64_t r = i / across, at = (i - r * across) * 8, g = r / c.rows;
-        const T *from = static_cast<const T *>(c.from) + g * c.group_stride + (r - g * c.rows) * c.stride + at;
-        uint16_t v[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            v[j] = 0;
-            if (at + j < c.cols) {
-                if (sizeof(T) == 1)
-                    v[j] = __half_as_ushort(__int2half_rn(static_cast<int>(from[j])));
-                else
-                    v[j] = static_cast<uint16_t>(from[j]);
-            }
-        }
-        uint4 w;
-        memcpy(&w, v, 16);
-        *reinterpret_cast<uint4 *>(c.to + i * 8) = w;
-    }
 }
 
 // ---- host -----------------------------------------------------------------------
@@ -835,73 +345,22 @@ gnmr_status check(const gnmr_product *p)
     return GNMR_OK;
 }
 
-// A matrix operand, and whether (and how large) a copy of it has to be made.
-struct Operand {
-    const void *at;
-    int64_t rows, cols, stride, group_stride;
-    int groups;
-    bool codes;
-    int64_t held() const { return (cols + 7) / 8 * 8; }
-    bool in_place() const
-    {
-        return !codes && !misaligned(at, 16) && stride % 8 == 0 && (groups == 1 || group_stride % 8 == 0);
-    }
-    int64_t copy_bytes() const
-    {
-        return in_place() || rows == 0 ? 0 : (groups * rows * held() * 2 + 255) / 256 * 256;
-    }
-};
-
-struct Operands {
-    Operand a, b;
-};
+// Codes, up to this many rows to a group, are multiplied from 8 bits; from more, they
+// are widened in memory first.
+constexpr int64_t kFewCodes = 64;
+constexpr int64_t kFewRows = 32;
 
 Operands operands(const gnmr_product *p)
 {
     const bool codes = p->op == GNMR_PRODUCT_FORWARD_I8;
-    const Operand x{p->d_x, p->rows, p->n_in, p->x_stride, 0, 1, codes};
-    const Operand dy{p->d_dy, p->rows, p->n_out, p->dy_stride, 0, 1, false};
+    const int bytes = codes ? 1 : 2, read = codes && p->rows <= kFewCodes * p->groups ? 1 : 2;
+    const Operand x{p->d_x, p->rows, p->n_in, p->x_stride, 0, 1, bytes, read};
+    const Operand dy{p->d_dy, p->rows, p->n_out, p->dy_stride, 0, 1, bytes, read};
     const bool shared = p->w_group_stride == 0;          // one weight for all groups
-    const Operand w{p->d_w, p->n_out, p->n_in, p->w_stride, p->w_group_stride, shared ? 1 : p->groups, codes};
+    const Operand w{p->d_w, p->n_out, p->n_in, p->w_stride, p->w_group_stride, shared ? 1 : p->groups, bytes, read};
     if (p->op == GNMR_PRODUCT_WEIGHT_GRAD)
         return {x, dy};
     return {w, p->op == GNMR_PRODUCT_INPUT_GRAD ? dy : x};
-}
-
-cudaError_t copy(const Operand &o, uint16_t *to, int sms, cudaStream_t st)
-{
-    const Copy c{o.at, to, o.rows, o.cols, o.stride, o.group_stride, o.held(), o.groups * o.rows * (o.held() / 8)};
-    const unsigned grid = static_cast<unsigned>(std::min<int64_t>((c.total + 255) / 256, int64_t(sms) * 8));
-    if (o.codes)
-        copy_kernel<int8_t><<<grid, 256, 0, st>>>(c);
-    else
-        copy_kernel<uint16_t><<<grid, 256, 0, st>>>(c);
-    return cudaGetLastError();
-}
-
-// Tiles of `high` rows by 64 columns of an operand.
-bool tile_map(const gnmr_products *h, CUtensorMap *map, const Operand &o, bool bf16, int high)
-{
-    if (o.rows == 0) {                                   // nothing will be loaded
-        memset(map, 0, sizeof(*map));
-        return true;
-    }
-    const cuuint64_t dims[3] = {static_cast<cuuint64_t>(o.cols), static_cast<cuuint64_t>(o.rows), static_cast<cuuint64_t>(o.groups)};
-    const cuuint64_t row = static_cast<cuuint64_t>(o.stride) * 2;
-    const cuuint64_t strides[2] = {row, o.groups > 1 ? static_cast<cuuint64_t>(o.group_stride) * 2 : row};
-    const cuuint32_t box[3] = {64, static_cast<cuuint32_t>(high), 1}, one[3] = {1, 1, 1};
-    const auto encode = [&] {
-        return h->encode(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3,
-                         const_cast<void *>(o.at), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                         CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    };
-    CUresult r = encode();
-    if (r == CUDA_ERROR_INVALID_CONTEXT || r == CUDA_ERROR_NOT_INITIALIZED) {
-        cudaSetDevice(h->device);                        // a host thread's first CUDA call: it has no context yet
-        r = encode();
-    }
-    return r == CUDA_SUCCESS;
 }
 
 template <int kColumns> constexpr int shared_bytes()
@@ -913,8 +372,9 @@ template <int kColumns, int kOp>
 cudaError_t launch(const gnmr_products *h, const Operands &o, const Product &p, cudaStream_t st, bool *mapped)
 {
     CUtensorMap a, b;
-    *mapped = tile_map(h, &a, o.a, p.bf16, a_along_lanes(kOp) ? 64 : 128) &&
-              tile_map(h, &b, o.b, p.bf16, b_along_columns(kOp) ? 64 : Shape<kColumns>::kBox);
+    const CUtensorMapDataType type = p.bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+    *mapped = gnmr::tile_map(h, &a, o.a, type, a_along_lanes(kOp) ? 64 : 128) &&
+              gnmr::tile_map(h, &b, o.b, type, b_along_columns(kOp) ? 64 : Shape<kColumns>::kBox);
     if (!*mapped)
         return cudaSuccess;
     cudaLaunchConfig_t cfg = {};
@@ -945,7 +405,7 @@ constexpr Launch kLaunch[4][2] = {
     {launch<256, GNMR_PRODUCT_FORWARD>, launch<64, GNMR_PRODUCT_FORWARD>},
     {launch<256, GNMR_PRODUCT_INPUT_GRAD>, launch<64, GNMR_PRODUCT_INPUT_GRAD>},
     {launch<256, GNMR_PRODUCT_WEIGHT_GRAD>, launch<256, GNMR_PRODUCT_WEIGHT_GRAD>},
-    {launch<256, GNMR_PRODUCT_FORWARD_I8>, launch<64, GNMR_PRODUCT_FORWARD_I8>},
+    {launch<256, GNMR_PRODUCT_FORWARD_I8>, gnmr::launch_codes},
 };
 
 cudaError_t allow_all_shared()
@@ -954,12 +414,39 @@ cudaError_t allow_all_shared()
     for (const cudaError_t r : {allow_shared<256, GNMR_PRODUCT_FORWARD>(), allow_shared<64, GNMR_PRODUCT_FORWARD>(),
                                 allow_shared<256, GNMR_PRODUCT_INPUT_GRAD>(), allow_shared<64, GNMR_PRODUCT_INPUT_GRAD>(),
                                 allow_shared<256, GNMR_PRODUCT_WEIGHT_GRAD>(), allow_shared<256, GNMR_PRODUCT_FORWARD_I8>(),
-                                allow_shared<64, GNMR_PRODUCT_FORWARD_I8>()})
+                                gnmr::allow_codes_shared()})
         e = e == cudaSuccess ? r : e;
     return e;
 }
 
 }  // namespace
+
+namespace gnmr {
+
+bool tile_map(const gnmr_products *h, CUtensorMap *map, const Operand &o, CUtensorMapDataType type, int high)
+{
+    if (o.rows == 0) {                                   // nothing will be loaded
+        memset(map, 0, sizeof(*map));
+        return true;
+    }
+    const cuuint64_t dims[3] = {static_cast<cuuint64_t>(o.cols), static_cast<cuuint64_t>(o.rows), static_cast<cuuint64_t>(o.groups)};
+    const cuuint64_t row = static_cast<cuuint64_t>(o.stride) * o.read_bytes;
+    const cuuint64_t strides[2] = {row, o.groups > 1 ? static_cast<cuuint64_t>(o.group_stride) * o.read_bytes : row};
+    const cuuint32_t box[3] = {static_cast<cuuint32_t>(128 / o.read_bytes), static_cast<cuuint32_t>(high), 1}, one[3] = {1, 1, 1};
+    const auto encode = [&] {
+        return h->encode(map, type, 3, const_cast<void *>(o.at), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                         CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    };
+    CUresult r = encode();
+    if (r == CUDA_ERROR_INVALID_CONTEXT || r == CUDA_ERROR_NOT_INITIALIZED) {
+        cudaSetDevice(h->device);                        // a host thread's first CUDA call: it has no context yet
+        r = encode();
+    }
+    return r == CUDA_SUCCESS;
+}
+
+}  // namespace gnmr
 
 extern "C" {
 
@@ -1059,7 +546,7 @@ gnmr_status gnmr_products_run(gnmr_products *h, const gnmr_product *p, void *str
     q.want = codes ? 0 : 1;
     q.a_by_group = o.a.groups > 1;
     q.bf16 = !codes && p->dtype == GNMR_DTYPE_BF16;
-    q.chunk = !codes && p->out_dtype == GNMR_DTYPE_F32 ? 8 : 16;
+    q.piece = !codes && p->out_dtype == GNMR_DTYPE_F32 ? 512 : 1024;
     q.out = p->d_out;
     q.out_type = p->out_dtype;
     q.add = wgrad && p->add;
@@ -1081,12 +568,12 @@ gnmr_status gnmr_products_run(gnmr_products *h, const gnmr_product *p, void *str
     char *scratch = static_cast<char *>(p->d_scratch);
     for (Operand *m : {&o.a, &o.b})
         if (const int64_t n = m->copy_bytes(); n && e == cudaSuccess) {
-            e = copy(*m, reinterpret_cast<uint16_t *>(scratch), 2 * h->pairs, st);
-            *m = Operand{scratch, m->rows, m->cols, m->held(), m->rows * m->held(), m->groups, false};
+            e = gnmr::copy_operand(*m, scratch, q, !wgrad && m == &o.a && m->groups == p->groups, 2 * h->pairs, st);
+            *m = Operand{scratch, m->rows, m->cols, m->held(), m->rows * m->held(), m->groups, m->read_bytes, m->read_bytes};
             scratch += n;
         }
     // few rows to a group: smaller tiles, more of them in flight
-    const bool few = !wgrad && p->rows <= 32 * int64_t(p->groups);
+    const bool few = !wgrad && (codes ? o.a.read_bytes == 1 : p->rows <= kFewRows * p->groups);
     bool mapped = true;
     if (e == cudaSuccess)
         e = kLaunch[p->op][few](h, o, q, st, &mapped);

@@ -1,0 +1,60 @@
+// The expert products' handle and operands, and what their translation units
+// call of each other.  Not part of the public ABI.
+#pragma once
+
+#include <cuda.h>
+#include <cuda_runtime_api.h>
+
+#include <cstdint>
+
+#include "gnmr_tiles.cuh"
+
+struct gnmr_products {
+    int device = 0;
+    int pairs = 1;
+    float *parts = nullptr;            // [kMaxParts][kPartFloats]
+    unsigned *tickets = nullptr;       // [kMaxParts][2], 0 between calls
+    int *gave_up = nullptr;            // host memory that the kernels can write
+    void *dmem = nullptr;
+    CUresult (*encode)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                       const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                       CUtensorMapL2promotion, CUtensorMapFloatOOBfill) = nullptr;
+};
+
+namespace gnmr {
+
+// A matrix operand of 1- or 2-byte elements, and the element size that its kernel
+// reads; operands that are not read in place are copied to rows of `held` elements.
+struct Operand {
+    const void *at;
+    int64_t rows, cols, stride, group_stride;
+    int groups;
+    int bytes, read_bytes;
+    int64_t held() const { return (cols * read_bytes + 15) / 16 * 16 / read_bytes; }
+    bool in_place() const
+    {
+        const int64_t steps = stride * bytes | (groups > 1 ? group_stride * bytes : 0);
+        return bytes == read_bytes && ((reinterpret_cast<uintptr_t>(at) | static_cast<uintptr_t>(steps)) & 15) == 0;
+    }
+    int64_t copy_bytes() const
+    {
+        return in_place() || rows == 0 ? 0 : (groups * rows * held() * read_bytes + 255) / 256 * 256;
+    }
+};
+
+struct Operands {
+    Operand a, b;
+};
+
+// Tiles of `high` rows by 128 bytes of an operand.
+bool tile_map(const gnmr_products *h, CUtensorMap *map, const Operand &o, CUtensorMapDataType type, int high);
+
+// The copy of an operand in `to`.  by_group: groups that p does not compute, or that have no
+// rows, are left out.
+cudaError_t copy_operand(const Operand &o, void *to, const gnmr_tiles::Product &p, bool by_group, int sms, cudaStream_t st);
+
+// The 8-bit product on operands in 8 bits, for few rows to a group.
+cudaError_t launch_codes(const gnmr_products *h, const Operands &o, const gnmr_tiles::Product &p, cudaStream_t st, bool *mapped);
+cudaError_t allow_codes_shared();
+
+}  // namespace gnmr

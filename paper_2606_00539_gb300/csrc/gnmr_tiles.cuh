@@ -1,0 +1,480 @@
+// What the kernels of the expert products share: the work of a call as tiles of every
+// group, sums that several pairs of CTAs share, and the epilogue.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+
+#include <cstdint>
+
+#include "gnmr.h"
+#include "gnmr_mma.cuh"
+
+namespace gnmr_tiles {
+
+using namespace gnmr_mma;
+
+constexpr int kMaxGroups = 2048;
+constexpr int kMaxPairs = 80;
+constexpr int kMaxParts = 2 * kMaxPairs;               // split tiles' parts in one call
+constexpr int64_t kPartFloats = 256 * 256;             // one part: both CTAs' lanes by the columns
+constexpr int kLanes = 256;                            // of a pair's tile
+constexpr int kEpilogueWarps = 8;
+constexpr int kFirstEpilogueWarp = 4;
+
+struct Product {
+    int lanes, depth, cols;            // depth, or cols, is 0 where it is a group's rows
+    int rows, groups;
+    const int64_t *offsets;
+    const uint8_t *mask;
+    int64_t mask_stride;
+    int want;                          // groups computed: mask byte != 0 (1), == 0 (0)
+    unsigned lane_tiles_inverse;       // ceil(2^32 / tiles of 256 lanes)
+    int a_by_group;                    // A's third coordinate is the group
+    int bf16;
+    int piece;                         // contraction steps of a piece
+    void *out;
+    int out_type;
+    int pairs_aligned;                 // two outputs of a row may be stored as one
+    int add;
+    int64_t out_col, out_group;
+    const float *lane_scale, *col_scale;
+    float *parts;
+    unsigned *tickets;
+    int *gave_up;
+};
+
+// ---- work: tiles of every group, and their parts --------------------------------
+
+struct Tables {
+    int first[kMaxGroups + 1];         // tiles before group g; in the end all of them
+    int row[kMaxGroups + 1];           // first row of group g; in the end the last group's end
+    uint16_t each[kMaxGroups];         // columns of group g's tiles
+    int split;                         // parts of every tile's contraction
+};
+
+struct Item {
+    int g, lane0, col0, cols;          // the tile: the pair's lanes, and its columns
+    int row0;                          // the group's first row
+    int depth, k0, k1;                 // the whole contraction; the stages of this part
+    int tile, part;
+    bool tail;                         // the last stage holds rows past the group's end
+};
+
+__device__ __forceinline__ int parts_of(int n, int each) { return (n + each - 1) / each; }
+
+// Filled by one warp; kStep: contraction steps of a stage.  Offsets are clamped to [0, rows] and made not decreasing.
+template <int kStep>
+__device__ __forceinline__ void fill_tables(const Product &p, Tables &t, int most, int lane_tiles, int pairs)
+{
+    const int lane = threadIdx.x & 31;
+    int carry = 0;
+    for (int j0 = 0; j0 <= p.groups; j0 += 32) {
+        const int j = j0 + lane;
+        int at = j == 0 ? 0 : p.rows;
+        if (p.offsets && j <= p.groups)
+            at = static_cast<int>(min(max(p.offsets[j], int64_t(0)), int64_t(p.rows)));
+        at = max(at, carry);
+#pragma unroll
+        for (int d = 1; d < 32; d *= 2) {
+            const int v = __shfl_up_sync(~0u, at, d);
+            if (lane >= d)
+                at = max(at, v);
+        }
+        if (j <= p.groups)
+            t.row[j] = at;
+        carry = __shfl_sync(~0u, at, 31);
+    }
+    __syncwarp();
+    int tiles = 0, deepest = 0;
+    for (int g0 = 0; g0 < p.groups; g0 += 32) {
+        const int g = g0 + lane;
+        int n = 0;
+        if (g < p.groups && (!p.mask || (p.mask[g * p.mask_stride] != 0) == (p.want != 0))) {
+            const int rows = t.row[g + 1] - t.row[g];
+            const int cols = p.cols ? p.cols : rows, across = parts_of(cols, most);
+            n = lane_tiles * across;
+            // a group's columns are shared out evenly, in multiples of 32
+            t.each[g] = static_cast<uint16_t>(across ? parts_of(parts_of(cols, across), 32) * 32 : 0);
+            deepest = max(deepest, p.depth ? p.depth : rows);
+        }
+        int sum = n;
+#pragma unroll
+        for (int d = 1; d < 32; d *= 2) {
+            const int v = __shfl_up_sync(~0u, sum, d);
+            if (lane >= d)
+                sum += v;
+        }
+        if (g < p.groups)
+            t.first[g] = tiles + sum - n;
+        tiles += __shfl_sync(~0u, sum, 31);
+    }
+    // Few tiles: the number of parts that takes the fewest rounds of stages, a
+    // part costing about six stages more for its beginning and its joining.
+    int best = 1;
+    if (tiles > 0 && tiles < pairs) {
+        const int stages = parts_of(__reduce_max_sync(~0u, deepest), kStep), parts = lane + 1;
+        const bool fits = parts == 1 || (tiles * parts <= min(2 * pairs, kMaxParts) && 2 * parts <= stages);
+        const int cost = fits ? parts_of(tiles * parts, pairs) * (parts_of(stages, parts) + (parts > 1 ? 6 : 0)) : INT32_MAX;
+        const int least = __reduce_min_sync(~0u, cost);
+        best = __ffs(__ballot_sync(~0u, cost == least));
+    }
+    if (lane == 0) {
+        t.first[p.groups] = tiles;
+        t.split = best;
+    }
+}
+
+// Item i of the call, by a whole warp that comes with growing i.  g: the group of the one
+// before, 0 at first.
+template <int kStep>
+__device__ __forceinline__ Item item_of(const Product &p, const Tables &t, int lane_tiles, int i, int &g)
+{
+    Item it;
+    it.tile = t.split == 1 ? i : i / t.split;
+    it.part = i - it.tile * t.split;
+    for (;;) {                                       // the last group that begins at or before the tile
+        const int next = g + 1 + (threadIdx.x & 31);
+        const unsigned past = __ballot_sync(~0u, next >= p.groups || t.first[next] > it.tile);
+        if (past) {
+            g += __ffs(past) - 1;
+            break;
+        }
+        g += 32;
+    }
+    it.g = g;
+    it.row0 = t.row[g];
+    const int rows = t.row[g + 1] - it.row0, at = it.tile - t.first[g], each = t.each[g];
+    int c = at;                                      // at / lane_tiles
+    if (lane_tiles > 1) {
+        c = __umulhi(at, p.lane_tiles_inverse);      // that, or one more
+        c -= c * lane_tiles > at;
+    }
+    it.lane0 = (at - c * lane_tiles) * kLanes;
+    it.col0 = c * each;
+    it.cols = min(each, (p.cols ? p.cols : rows) - it.col0);
+    it.depth = p.depth ? p.depth : rows;
+    const int stages = parts_of(it.depth, kStep);
+    it.k0 = 0;
+    it.k1 = stages;
+    if (t.split > 1) {
+        it.k0 = stages * it.part / t.split;
+        it.k1 = stages * (it.part + 1) / t.split;
+    }
+    it.tail = !p.depth && it.depth % kStep && it.k0 < it.k1 && it.k1 == stages;
+    return it;
+}
+
+// ---- outputs --------------------------------------------------------------------
+
+template <int kOut> __device__ __forceinline__ unsigned pack(float lo, float hi)
+{
+    if (kOut == GNMR_DTYPE_BF16) {
+        const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+        return reinterpret_cast<const unsigned &>(v);
+    }
+    const __half2 v = __floats2half2_rn(lo, hi);
+    return reinterpret_cast<const unsigned &>(v);
+}
+
+template <int kOut> __device__ __forceinline__ float load_out(const char *at)
+{
+    return kOut == GNMR_DTYPE_F32    ? *reinterpret_cast<const float *>(at)
+           : kOut == GNMR_DTYPE_BF16 ? __bfloat162float(*reinterpret_cast<const __nv_bfloat16 *>(at))
+                                     : __half2float(*reinterpret_cast<const __half *>(at));
+}
+
+// Two columns of this thread's lane become one column of two lanes: the even lane gets
+// the first column's, the odd lane the second's.
+template <int kOut> __device__ __forceinline__ unsigned exchange(float first, float second, unsigned which)
+{
+    const unsigned w = pack<kOut>(first, second);
+    return __byte_perm(w, __shfl_xor_sync(~0u, w, 1), which);
+}
+
+// This warp's sums to the outputs: lane `lane` of columns col .. col + span - 1 of the
+// tile.  Two lanes' 16-bit values of a column go out as one where they can: 64
+// contiguous bytes a column from a warp.
+template <int kPieces, bool kCodes, int kOut>
+__device__ __forceinline__ void finish(const Product &p, const Item &it, uint32_t (&acc)[kPieces][16], int lane, int col, int span)
+{
+    constexpr int kBytes = kOut == GNMR_DTYPE_F32 ? 4 : 2;
+    const int64_t step = p.out_col * kBytes;
+    const int64_t row = p.cols ? it.col0 + col : int64_t(it.row0) + it.col0 + col;
+    char *out = static_cast<char *>(p.out) + (p.cols ? it.g * p.out_group * kBytes : 0) + row * step + int64_t(lane) * kBytes;
+    const int left = it.cols - col, odd = lane & 1;
+    const bool mine = lane < p.lanes;
+    const bool whole = (lane | 31) < p.lanes && (kBytes == 4 || (p.pairs_aligned && !p.add));
+    const unsigned which = odd ? 0x3276 : 0x5410;
+    float by_lane = 0.0f;
+    const float *by_col = nullptr;
+    if (kCodes) {
+        by_lane = mine ? p.lane_scale[int64_t(it.g) * p.lanes + lane] : 0.0f;
+        by_col = p.col_scale + it.row0 + it.col0 + col;
+    }
+    if (whole && kBytes == 2)
+        out += odd ? step - 2 : 0;
+#pragma unroll
+    for (int q = 0; q < kPieces; ++q) {
+        const int n = min(span, left) - q * 16;          // columns of this piece that there are
+        if (n <= 0)
+            break;
+        float v[16];
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+            v[j] = kCodes ? (j < n ? by_col[q * 16 + j] : 0.0f) : __uint_as_float(acc[q][j]);
+        if (kCodes)
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+                v[j] = static_cast<float>(static_cast<int>(acc[q][j])) * v[j] * by_lane;
+        if (whole && n >= 16) {
+            if (kBytes == 4) {
+                if (p.add) {
+                    float old[16];
+                    const char *from = out;
+#pragma unroll
+                    for (int j = 0; j < 16; ++j, from += step)
+                        old[j] = *reinterpret_cast<const float *>(from);
+#pragma unroll
+                    for (int j = 0; j < 16; ++j)
+                        v[j] += old[j];
+                }
+#pragma unroll
+                for (int j = 0; j < 16; ++j, out += step)
+                    *reinterpret_cast<float *>(out) = v[j];
+            } else {
+#pragma unroll
+                for (int j = 0; j < 16; j += 2, out += 2 * step)
+                    *reinterpret_cast<unsigned *>(out) = exchange<kOut>(v[j], v[j + 1], which);
+            }
+            continue;
+        }
+        if (whole && kBytes == 2)                        // back to this lane's own place in the first column
+            out -= odd ? step - 2 : 0;
+        if (p.add)
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+                if (mine && j < n)
+                    v[j] += load_out<kOut>(out + j * step);
+        if (kBytes == 4) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+                if (mine && j < n)
+                    *reinterpret_cast<float *>(out + j * step) = v[j];
+        } else {
+#pragma unroll
+            for (int j = 0; j < 16; j += 2) {
+                const unsigned w = exchange<kOut>(v[j], v[j + 1], which);
+                char *to = out - 2 * odd + (j + odd) * step;     // the column that this thread writes, two lanes of it
+                if (j + odd < n) {
+                    if (p.pairs_aligned && (lane | 1) < p.lanes) {
+                        *reinterpret_cast<unsigned *>(to) = w;
+                    } else {
+                        if ((lane & ~1) < p.lanes)
+                            *reinterpret_cast<uint16_t *>(to) = static_cast<uint16_t>(w);
+                        if ((lane | 1) < p.lanes)
+                            *reinterpret_cast<uint16_t *>(to + 2) = static_cast<uint16_t>(w >> 16);
+                    }
+                }
+            }
+        }
+        out += 16 * step;
+    }
+}
+
+// The first piece's sums, or another's added to them.
+template <bool kCodes>
+__device__ __forceinline__ void begin_sum(uint32_t (&acc)[16])
+{
+    if (kCodes)
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+            acc[j] = __float2int_rn(__uint_as_float(acc[j]));
+}
+
+template <bool kCodes>
+__device__ __forceinline__ void add_to_sum(uint32_t (&acc)[16], const uint32_t (&v)[16])
+{
+#pragma unroll
+    for (int j = 0; j < 16; ++j)
+        acc[j] = kCodes ? acc[j] + __float2int_rn(__uint_as_float(v[j]))
+                        : __float_as_uint(__uint_as_float(acc[j]) + __uint_as_float(v[j]));
+}
+
+// ---- a CTA ------------------------------------------------------------------------
+
+struct Barriers {
+    uint64_t full[8], empty[8];        // stages of operands
+    uint64_t tail[8];                  // a stage that the tail warp looks at first
+    uint64_t ready[4], used[4];        // operands widened from 8 bits
+    uint64_t done[2], drained[2];      // halves of tensor memory; `drained` counts in the first CTA
+    uint64_t written, counted;         // of a split tile's part: by its warps, and its ticket
+    uint32_t tmem;
+    unsigned last;                     // whether this CTA is a split tile's last
+};
+
+// What the roles of a CTA share.
+struct Cta {
+    uint8_t *stages;                   // dynamic shared memory, from a multiple of 1,024
+    const Tables *tables;
+    Barriers *bars;
+    uint32_t rank, tmem;
+    int pair, pairs, lane_tiles, items;
+};
+
+// The barriers that the epilogue counts on.
+__device__ __forceinline__ void init_epilogue_barriers(Barriers &b)
+{
+    for (int h = 0; h < 2; ++h) {
+        barrier_init(smem_addr(&b.done[h]), 1);
+        barrier_init(smem_addr(&b.drained[h]), 2 * kEpilogueWarps);
+    }
+    barrier_init(smem_addr(&b.written), kEpilogueWarps);
+    barrier_init(smem_addr(&b.counted), 1);
+}
+
+// The end of every kernel: both CTAs of a pair are through, and a role that gave up has
+// said so.  Loads that it left behind are in long before the wait is over.
+__device__ __forceinline__ void finish_pair(bool fine, int *gave_up)
+{
+    __syncwarp();
+    if (!fine) {
+        if ((threadIdx.x & 31) == 0)
+            *gave_up = 1;
+        for (int i = 0; i < 1000; ++i)
+            __nanosleep(1000);
+    }
+    fence_before();
+    __syncthreads();
+    cluster_sync();
+    fence_after();
+}
+
+// A split tile: this part goes to memory, and the last CTA of its rank to get here
+// takes the sum of all parts, in their order.  1: it has; 0: another will; -1: gave up.
+template <int kColumns, bool kCodes>
+__device__ __forceinline__ int join_parts(const Product &p, const Cta &c, const Item &it, uint32_t (&acc)[kColumns / 32][16],
+                                          int span, int col, int warp, uint32_t turn)
+{
+    constexpr int kPieces = kColumns / 32;               // of 16 columns
+    const int lane = threadIdx.x & 31, split = c.tables->split;
+    uint32_t *part = reinterpret_cast<uint32_t *>(p.parts) + int64_t(it.tile) * split * kPartFloats +
+                     c.rank * (kPartFloats / 2) + (warp & 3) * 32 + lane;
+#pragma unroll
+    for (int q = 0; q < kPieces; ++q)
+        if (q * 16 < span)
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+                part[it.part * kPartFloats + (col + q * 16 + j) * 128] = acc[q][j];
+    __threadfence();
+    __syncwarp();
+    if (lane == 0)
+        arrive_release(in_cta(smem_addr(&c.bars->written), c.rank));
+    if (warp == kFirstEpilogueWarp) {
+        if (!wait(smem_addr(&c.bars->written), turn))
+            return -1;
+        if (lane == 0) {
+            __threadfence();
+            unsigned *ticket = p.tickets + 2 * it.tile + c.rank;
+            c.bars->last = atomicAdd(ticket, 1u) + 1 == static_cast<unsigned>(split);
+            if (c.bars->last)
+                *ticket = 0;
+            __threadfence();
+            arrive_release(in_cta(smem_addr(&c.bars->counted), c.rank));
+        }
+        __syncwarp();
+    }
+    if (!wait(smem_addr(&c.bars->counted), turn))
+        return -1;
+    if (!c.bars->last)
+        return 0;
+#pragma unroll
+    for (int q = 0; q < kPieces; ++q)
+        if (q * 16 < span) {
+            for (int s = 0; s < split; ++s)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    const uint32_t v = __ldcg(part + s * kPartFloats + (col + q * 16 + j) * 128);
+                    if (s == 0)
+                        acc[q][j] = v;
+                    else
+                        acc[q][j] = kCodes ? acc[q][j] + v : __float_as_uint(__uint_as_float(acc[q][j]) + __uint_as_float(v));
+                }
+        }
+    return 1;
+}
+
+// The epilogue's warps: a tile's pieces added up and written.
+template <int kColumns, bool kCodes, int kStep>
+__device__ __forceinline__ bool write_outputs(const Product &p, const Cta &c)
+{
+    constexpr int kPieces = kColumns / 32;               // of 16 columns
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int quarter = warp & 3, side = (warp - kFirstEpilogueWarp) >> 2;
+    const uint32_t done = smem_addr(&c.bars->done[0]), drained = in_cta(smem_addr(&c.bars->drained[0]), 0);
+    int half = 0;
+    uint32_t phase = 0, joins = 0;
+    for (int i = c.pair, g = 0; i < c.items; i += c.pairs) {
+        const Item it = item_of<kStep>(p, *c.tables, c.lane_tiles, i, g);
+        const int span = (it.cols + 31) / 32 * 16;                          // columns of this warp
+        const int at = it.lane0 + c.rank * 128 + quarter * 32 + lane, col = side * span;
+        uint32_t acc[kPieces][16];
+        if (it.k0 == it.k1)
+#pragma unroll
+            for (int q = 0; q < kPieces; ++q)
+#pragma unroll
+                for (int j = 0; j < 16; ++j)
+                    acc[q][j] = 0;
+        for (int k = it.k0; k < it.k1; k += p.piece / kStep) {
+            if (!wait(done + half * 8, phase))
+                return false;
+            fence_after();
+            const uint32_t from = c.tmem + half * kColumns + (uint32_t(quarter * 32) << 16) + col;
+            if (k == it.k0) {
+#pragma unroll
+                for (int q = 0; q < kPieces; ++q)
+                    if (q * 16 < span)
+                        load16(from + q * 16, acc[q]);
+#pragma unroll
+                for (int q = 0; q < kPieces; ++q) {
+                    load_wait(acc[q]);
+                    begin_sum<kCodes>(acc[q]);
+                }
+            } else {
+#pragma unroll
+                for (int q = 0; q < kPieces; ++q)
+                    if (q * 16 < span) {
+                        uint32_t v[16];
+                        load16(from + q * 16, v);
+                        load_wait(v);
+                        add_to_sum<kCodes>(acc[q], v);
+                    }
+            }
+            fence_before();
+            __syncwarp();
+            if (lane == 0)
+                arrive(drained + half * 8);
+            if (half ^= 1; half == 0)
+                phase ^= 1;
+        }
+        if (c.tables->split > 1) {
+            const int mine = join_parts<kColumns, kCodes>(p, c, it, acc, span, col, warp, joins++ & 1);
+            if (mine < 0)
+                return false;
+            if (mine == 0)
+                continue;
+        }
+        if (p.add && it.depth == 0)
+            continue;                                    // nothing to add
+        if (p.out_type == GNMR_DTYPE_F32)
+            finish<kPieces, kCodes, GNMR_DTYPE_F32>(p, it, acc, at, col, span);
+        else if (p.out_type == GNMR_DTYPE_BF16)
+            finish<kPieces, kCodes, GNMR_DTYPE_BF16>(p, it, acc, at, col, span);
+        else
+            finish<kPieces, kCodes, GNMR_DTYPE_F16>(p, it, acc, at, col, span);
+    }
+    return true;
+}
+
+}  // namespace gnmr_tiles
