@@ -5,8 +5,8 @@
 // 1,024 of them sums to at most 2^24, exact in fp32; pieces are added as integers.
 //
 // Few rows to a group are bound by reading the weights, so these stay 8 bits wide up
-// to the SM: eight warps widen A's tile into tensor memory (from where the tensor cores
-// take an operand as well, at no cost in shared-memory bandwidth) and B's, a
+// to the SM: eight warps widen A's tiles into tensor memory (from where the tensor cores
+// take an operand as well, at no cost in shared-memory bandwidth), two more B's, a
 // few columns, into shared memory.  Many rows are bound by the multiplies, and widening a
 // tile again for every 256 columns would take the shared memory that the
 // tensor cores read from: there both operands are widened in memory once, and the 16-bit
@@ -40,7 +40,7 @@ __device__ __forceinline__ uint2 widen4(uint32_t codes)
 
 constexpr int kColumns = 64;                           // of a tile, at most
 constexpr int kStep = 128;                             // contraction steps of a stage: 128-byte rows of codes
-constexpr int kProducerWarp = 0, kMultiplyWarp = 1, kTablesWarp = 3;
+constexpr int kProducerWarp = 0, kMultiplyWarp = 1, kFirstBWarp = 2, kTablesWarp = 3;
 constexpr int kFirstWidenWarp = kFirstEpilogueWarp + kEpilogueWarps, kWidenWarps = 8;
 constexpr int kThreads = 32 * (kFirstWidenWarp + kWidenWarps);
 constexpr int kAStage = 128 * kStep, kStage = kAStage + kColumns / 2 * kStep, kStages = 8;
@@ -77,60 +77,85 @@ __device__ __forceinline__ bool load_stages(const CUtensorMap &map_a, const CUte
     return true;
 }
 
-__device__ __forceinline__ bool widen_stages(const Product &p, const Cta &c)
+// A's tiles into tensor memory, by two teams of four warps that take the stages in turn.
+__device__ __forceinline__ bool widen_a(const Product &p, const Cta &c)
 {
-    const int warp = threadIdx.x / 32 - kFirstWidenWarp, lane = threadIdx.x & 31, quarter = warp & 3, side = warp >> 2;
+    const int warp = threadIdx.x / 32 - kFirstWidenWarp, lane = threadIdx.x & 31, quarter = warp & 3, team = warp >> 2;
     const uint32_t full = smem_addr(&c.bars->full[0]), empty = in_cta(smem_addr(&c.bars->empty[0]), c.rank);
     const uint32_t used = smem_addr(&c.bars->used[0]), ready = in_cta(smem_addr(&c.bars->ready[0]), 0);
-    const int row = quarter * 32 + lane;               // of A: 64 steps of it
-    const int b_row = threadIdx.x / 8 - kFirstWidenWarp * 4, b_chunk = threadIdx.x & 7;        // of B: 16 steps
-    uint8_t *slots = c.stages + kStages * kStage;
-    int stage = 0, slot = 0;
-    uint32_t phase = 0, slot_phase = 1;
+    const int row = quarter * 32 + lane;
+    const uint8_t *raw = c.stages + row * 128;
+    int n = 0;                                         // stages so far
     for (int i = c.pair, g = 0; i < c.items; i += c.pairs) {
         const Item it = item_of<kStep>(p, *c.tables, c.lane_tiles, i, g);
-        for (int k = it.k0; k < it.k1; ++k) {
-            if (!wait(full + stage * 8, phase))
-                return false;
-            const uint8_t *raw = c.stages + stage * kStage;
-            uint4 codes[5];
-#pragma unroll
-            for (int q = 0; q < 4; ++q)
-                codes[q] = *reinterpret_cast<const uint4 *>(raw + row * 128 + (((side * 4 + q) ^ (row & 7)) << 4));
-            codes[4] = *reinterpret_cast<const uint4 *>(raw + kAStage + b_row * 128 + ((b_chunk ^ (b_row & 7)) << 4));
-            uint32_t a[32];
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const uint32_t w[4] = {codes[q].x, codes[q].y, codes[q].z, codes[q].w};
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const uint2 v = widen4(w[j]);
-                    a[8 * q + 2 * j] = v.x;
-                    a[8 * q + 2 * j + 1] = v.y;
-                }
-            }
-            if (!wait(used + slot * 8, slot_phase))
+        const int end = n + it.k1 - it.k0;
+        for (n += (n ^ team) & 1; n < end; n += 2) {
+            const int stage = n % kStages, slot = n % kSlots;
+            if (!wait(full + stage * 8, (n / kStages) & 1) || !wait(used + slot * 8, (n / kSlots + 1) & 1))
                 return false;
             fence_after();
-            store32(c.tmem + kFirstA + slot * (kStep / 2) + side * 32 + (uint32_t(quarter * 32) << 16), a);
-            uint8_t *b = slots + slot * kSlot + (b_chunk >> 2) * kBTile + b_row * 128;
-            const int at = (b_chunk & 3) * 2, turn = b_row & 7;
-            const uint2 v0 = widen4(codes[4].x), v1 = widen4(codes[4].y), v2 = widen4(codes[4].z), v3 = widen4(codes[4].w);
-            *reinterpret_cast<uint4 *>(b + ((at ^ turn) << 4)) = make_uint4(v0.x, v0.y, v1.x, v1.y);
-            *reinterpret_cast<uint4 *>(b + (((at + 1) ^ turn) << 4)) = make_uint4(v2.x, v2.y, v3.x, v3.y);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                uint32_t a[32];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const uint4 codes = *reinterpret_cast<const uint4 *>(raw + stage * kStage + (((h * 4 + q) ^ (row & 7)) << 4));
+                    const uint32_t w[4] = {codes.x, codes.y, codes.z, codes.w};
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const uint2 v = widen4(w[j]);
+                        a[8 * q + 2 * j] = v.x;
+                        a[8 * q + 2 * j + 1] = v.y;
+                    }
+                }
+                store32(c.tmem + kFirstA + slot * (kStep / 2) + h * 32 + (uint32_t(quarter * 32) << 16), a);
+            }
+            __syncwarp();
+            if (lane == 0)
+                arrive(empty + stage * 8);
             store_wait();
-            fence_async_proxy();
             fence_before();
+            __syncwarp();
+            if (lane == 0)
+                arrive(ready + slot * 8);
+        }
+        n = end;
+    }
+    return true;
+}
+
+// B's tiles to shared memory, by two warps in turn.
+__device__ __forceinline__ bool widen_b(const Product &p, const Cta &c)
+{
+    const int lane = threadIdx.x & 31, turn = threadIdx.x / 32 - kFirstBWarp, chunk = lane & 7;
+    const uint32_t full = smem_addr(&c.bars->full[0]), empty = in_cta(smem_addr(&c.bars->empty[0]), c.rank);
+    const uint32_t used = smem_addr(&c.bars->used[0]), ready = in_cta(smem_addr(&c.bars->ready[0]), 0);
+    int n = 0;
+    for (int i = c.pair, g = 0; i < c.items; i += c.pairs) {
+        const Item it = item_of<kStep>(p, *c.tables, c.lane_tiles, i, g);
+        const int end = n + it.k1 - it.k0, half = (it.cols + 31) / 32 * 16;
+        for (n += (n ^ turn) & 1; n < end; n += 2) {
+            const int stage = n % kStages, slot = n % kSlots;
+            if (!wait(full + stage * 8, (n / kStages) & 1) || !wait(used + slot * 8, (n / kSlots + 1) & 1))
+                return false;
+            const uint8_t *raw = c.stages + stage * kStage + kAStage;
+            uint8_t *to = c.stages + kStages * kStage + slot * kSlot + (chunk >> 2) * kBTile;
+#pragma unroll 4
+            for (int r = lane >> 3; r < half; r += 4) {
+                const uint4 codes = *reinterpret_cast<const uint4 *>(raw + r * 128 + ((chunk ^ (r & 7)) << 4));
+                const uint2 v0 = widen4(codes.x), v1 = widen4(codes.y), v2 = widen4(codes.z), v3 = widen4(codes.w);
+                const int at = (chunk & 3) * 2, x = r & 7;
+                *reinterpret_cast<uint4 *>(to + r * 128 + ((at ^ x) << 4)) = make_uint4(v0.x, v0.y, v1.x, v1.y);
+                *reinterpret_cast<uint4 *>(to + r * 128 + (((at + 1) ^ x) << 4)) = make_uint4(v2.x, v2.y, v3.x, v3.y);
+            }
+            fence_async_proxy();
             __syncwarp();
             if (lane == 0) {
                 arrive(empty + stage * 8);
                 arrive_release(ready + slot * 8);
             }
-            if (++stage == kStages)
-                stage = 0, phase ^= 1;
-            if (++slot == kSlots)
-                slot = 0, slot_phase ^= 1;
         }
+        n = end;
     }
     return true;
 }
@@ -197,10 +222,10 @@ codes_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
         prefetch_map(&map_b);
         for (int s = 0; s < kStages; ++s) {
             barrier_init(smem_addr(&bars.full[s]), 1);
-            barrier_init(smem_addr(&bars.empty[s]), kWidenWarps);
+            barrier_init(smem_addr(&bars.empty[s]), kWidenWarps / 2 + 1);
         }
         for (int s = 0; s < kSlots; ++s) {
-            barrier_init(smem_addr(&bars.ready[s]), 2 * kWidenWarps);          // counts in the first CTA
+            barrier_init(smem_addr(&bars.ready[s]), 2 * (kWidenWarps / 2 + 1));    // counts in the first CTA, from both
             barrier_init(smem_addr(&bars.used[s]), 1);
         }
         init_epilogue_barriers(bars);
@@ -226,7 +251,9 @@ codes_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
     else if (warp == kMultiplyWarp && c.rank == 0)
         fine = multiply_slots(p, c);
     else if (warp >= kFirstWidenWarp)
-        fine = widen_stages(p, c);
+        fine = widen_a(p, c);
+    else if (warp == kFirstBWarp || warp == kFirstBWarp + 1)
+        fine = widen_b(p, c);
     else if (warp >= kFirstEpilogueWarp)
         fine = write_outputs<kColumns, true, kStep>(p, c);
     finish_pair(fine, p.gave_up);
