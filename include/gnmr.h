@@ -424,9 +424,10 @@ typedef enum gnmr_product_op {
 } gnmr_product_op;
 
 /* One product.  Strides are in elements; every matrix is row-major with
- * contiguous rows.  A row stride that is a multiple of 16 bytes, with base and
- * group strides alike, is read in place; other operands are first copied to
- * d_scratch (gnmr_products_scratch_bytes). */
+ * contiguous rows.  Operands whose start, row stride and group stride are multiples
+ * of 16 bytes are read in place; others are first copied to d_scratch, and so, as
+ * 16-bit numbers, are the x of an 8-bit product of many rows
+ * (gnmr_products_scratch_bytes). */
 typedef struct gnmr_product {
     int32_t op;                /* gnmr_product_op */
     int32_t groups;            /* 1 .. 2048 */

@@ -1,4 +1,5 @@
-// Expert products: the linear units of both paths, grouped by expert.
+// Expert products: the linear units of both paths, grouped by expert.  The 16-bit kernel
+// and the calls; 8-bit codes have a file of their own.
 //
 // Every product is out[col][lane] = sum over c of A[lane][c] B[col][c]:
 //   forward      A = W_g      [n_out lanes], c along its rows     B = x's rows    c < n_in
@@ -17,9 +18,7 @@
 // A piece is at most 1,024 steps (512 for fp32 outputs).  The tensor cores cut
 // sums that they hold rather than rounding them: 2,047 steps in one piece were
 // 1.5e-6 of the result off, in fp32 arithmetic 3.9e-7.  Pieces are added in registers,
-// rounded, while the next one is multiplied into the other half of tensor memory.  For
-// 8-bit codes a piece's sum is below 2^24, an exact integer in fp32, and pieces
-// are added as integers.
+// rounded, while the next one is multiplied into the other half of tensor memory.
 //
 // Where there are fewer tiles than pairs, a tile's contraction is split over
 // several pairs; each writes its part, and the last one to finish adds them up
@@ -284,7 +283,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             fine = clear_tails<kColumns>(p, c);
     } else {
         more_registers<kEpilogueRegisters>();
-        fine = write_outputs<kColumns, kOp == GNMR_PRODUCT_FORWARD_I8, kStep>(p, c);
+        fine = write_outputs<kColumns, false, kStep>(p, c);
     }
     finish_pair(fine, p.gave_up);
     if (warp == kMultiplyWarp)
@@ -345,19 +344,21 @@ gnmr_status check(const gnmr_product *p)
     return GNMR_OK;
 }
 
-// Codes, up to this many rows to a group, are multiplied from 8 bits; from more, they
-// are widened in memory first.
-constexpr int64_t kFewCodes = 64;
+// 8-bit codes: up to this many rows to a group the rows are read in 8 bits too; more are
+// widened in memory first.  5120 -> 13824, 16 rows: 22 us in 8 bits, 28 widened; 64: 28 and 29; 64
+// experts of 2048 -> 1408, 31 rows each: 53 and 51, 64 each: 73 and 55.
+constexpr int64_t kFewCodes = 32;
+// 16-bit operands: up to this many rows to a group, tiles of 64 columns.
 constexpr int64_t kFewRows = 32;
 
 Operands operands(const gnmr_product *p)
 {
     const bool codes = p->op == GNMR_PRODUCT_FORWARD_I8;
-    const int bytes = codes ? 1 : 2, read = codes && p->rows <= kFewCodes * p->groups ? 1 : 2;
-    const Operand x{p->d_x, p->rows, p->n_in, p->x_stride, 0, 1, bytes, read};
-    const Operand dy{p->d_dy, p->rows, p->n_out, p->dy_stride, 0, 1, bytes, read};
+    const int bytes = codes ? 1 : 2;
+    const Operand x{p->d_x, p->rows, p->n_in, p->x_stride, 0, 1, bytes, codes && p->rows <= kFewCodes * p->groups ? 1 : 2};
+    const Operand dy{p->d_dy, p->rows, p->n_out, p->dy_stride, 0, 1, 2, 2};
     const bool shared = p->w_group_stride == 0;          // one weight for all groups
-    const Operand w{p->d_w, p->n_out, p->n_in, p->w_stride, p->w_group_stride, shared ? 1 : p->groups, bytes, read};
+    const Operand w{p->d_w, p->n_out, p->n_in, p->w_stride, p->w_group_stride, shared ? 1 : p->groups, bytes, bytes};
     if (p->op == GNMR_PRODUCT_WEIGHT_GRAD)
         return {x, dy};
     return {w, p->op == GNMR_PRODUCT_INPUT_GRAD ? dy : x};
@@ -405,7 +406,7 @@ constexpr Launch kLaunch[4][2] = {
     {launch<256, GNMR_PRODUCT_FORWARD>, launch<64, GNMR_PRODUCT_FORWARD>},
     {launch<256, GNMR_PRODUCT_INPUT_GRAD>, launch<64, GNMR_PRODUCT_INPUT_GRAD>},
     {launch<256, GNMR_PRODUCT_WEIGHT_GRAD>, launch<256, GNMR_PRODUCT_WEIGHT_GRAD>},
-    {launch<256, GNMR_PRODUCT_FORWARD_I8>, gnmr::launch_codes},
+    {gnmr::launch_codes, gnmr::launch_codes},
 };
 
 cudaError_t allow_all_shared()
@@ -413,8 +414,7 @@ cudaError_t allow_all_shared()
     cudaError_t e = cudaSuccess;
     for (const cudaError_t r : {allow_shared<256, GNMR_PRODUCT_FORWARD>(), allow_shared<64, GNMR_PRODUCT_FORWARD>(),
                                 allow_shared<256, GNMR_PRODUCT_INPUT_GRAD>(), allow_shared<64, GNMR_PRODUCT_INPUT_GRAD>(),
-                                allow_shared<256, GNMR_PRODUCT_WEIGHT_GRAD>(), allow_shared<256, GNMR_PRODUCT_FORWARD_I8>(),
-                                gnmr::allow_codes_shared()})
+                                allow_shared<256, GNMR_PRODUCT_WEIGHT_GRAD>(), gnmr::allow_codes_shared()})
         e = e == cudaSuccess ? r : e;
     return e;
 }
@@ -568,12 +568,12 @@ gnmr_status gnmr_products_run(gnmr_products *h, const gnmr_product *p, void *str
     char *scratch = static_cast<char *>(p->d_scratch);
     for (Operand *m : {&o.a, &o.b})
         if (const int64_t n = m->copy_bytes(); n && e == cudaSuccess) {
-            e = gnmr::copy_operand(*m, scratch, q, !wgrad && m == &o.a && m->groups == p->groups, 2 * h->pairs, st);
+            e = gnmr::copy_operand(*m, scratch, 2 * h->pairs, st);
             *m = Operand{scratch, m->rows, m->cols, m->held(), m->rows * m->held(), m->groups, m->read_bytes, m->read_bytes};
             scratch += n;
         }
     // few rows to a group: smaller tiles, more of them in flight
-    const bool few = !wgrad && (codes ? o.a.read_bytes == 1 : p->rows <= kFewRows * p->groups);
+    const bool few = !wgrad && p->rows <= kFewRows * p->groups;
     bool mapped = true;
     if (e == cudaSuccess)
         e = kLaunch[p->op][few](h, o, q, st, &mapped);

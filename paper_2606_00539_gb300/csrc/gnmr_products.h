@@ -49,11 +49,10 @@ struct Operands {
 // Tiles of `high` rows by 128 bytes of an operand.
 bool tile_map(const gnmr_products *h, CUtensorMap *map, const Operand &o, CUtensorMapDataType type, int high);
 
-// The copy of an operand in `to`.  by_group: groups that p does not compute, or that have no
-// rows, are left out.
-cudaError_t copy_operand(const Operand &o, void *to, const gnmr_tiles::Product &p, bool by_group, int sms, cudaStream_t st);
+// The copy of an operand in `to`.
+cudaError_t copy_operand(const Operand &o, void *to, int sms, cudaStream_t st);
 
-// The 8-bit product on operands in 8 bits, for few rows to a group.
+// The 8-bit product; b may be widened.
 cudaError_t launch_codes(const gnmr_products *h, const Operands &o, const gnmr_tiles::Product &p, cudaStream_t st, bool *mapped);
 cudaError_t allow_codes_shared();
 

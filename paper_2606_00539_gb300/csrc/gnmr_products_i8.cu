@@ -4,13 +4,13 @@
 // multiplied as fp16, which holds them exactly: products are below 2^14 and a piece of
 // 1,024 of them sums to at most 2^24, exact in fp32; pieces are added as integers.
 //
-// Few rows to a group are bound by reading the weights, so these stay 8 bits wide up
-// to the SM: eight warps widen A's tiles into tensor memory (from where the tensor cores
-// take an operand as well, at no cost in shared-memory bandwidth), two more B's, a
-// few columns, into shared memory.  Many rows are bound by the multiplies, and widening a
-// tile again for every 256 columns would take the shared memory that the
-// tensor cores read from: there both operands are widened in memory once, and the 16-bit
-// kernel multiplies them.
+// The weights stay 8 bits wide up to the SM: eight warps widen A's tiles into tensor
+// memory, from where the tensor cores take an operand as well, at no cost in
+// shared-memory bandwidth (tiles of fp16 in shared memory, written and read again for each
+// tile of columns, would take more of it than there is beside the multiplies).  B, the
+// rows, are widened by two more warps where they are few, else in memory by a
+// kernel before this one.  Widening the weights in memory too, for the 16-bit kernel, was
+// slower up to 4,001 rows to a group (5120 -> 13824: 380 us, this way 355).
 #include <algorithm>
 #include <cstring>
 
@@ -36,41 +36,65 @@ __device__ __forceinline__ uint2 widen4(uint32_t codes)
     return v;
 }
 
-// ---- few rows to a group ------------------------------------------------------------
+// ---- weights in 8 bits --------------------------------------------------------------
 
-constexpr int kColumns = 64;                           // of a tile, at most
 constexpr int kStep = 128;                             // contraction steps of a stage: 128-byte rows of codes
 constexpr int kProducerWarp = 0, kMultiplyWarp = 1, kFirstBWarp = 2, kTablesWarp = 3;
 constexpr int kFirstWidenWarp = kFirstEpilogueWarp + kEpilogueWarps, kWidenWarps = 8;
 constexpr int kThreads = 32 * (kFirstWidenWarp + kWidenWarps);
-constexpr int kAStage = 128 * kStep, kStage = kAStage + kColumns / 2 * kStep, kStages = 8;
-// Widened: B in shared memory, as two tiles of 64 steps; A behind the sums in tensor
-// memory, 64 columns of two steps each.
-constexpr int kSlots = 4, kBTile = kColumns / 2 * 128, kSlot = 2 * kBTile;
-constexpr int kFirstA = 256, kTmem = 512;
-static_assert(2 * kColumns <= kFirstA && kFirstA + kSlots * kStep / 2 <= kTmem, "columns of tensor memory");
-constexpr int kShared = kStages * kStage + kSlots * kSlot + static_cast<int>(sizeof(Tables)) + 1024;
+// 96 registers a thread at launch, shared out anew: the epilogue holds the sums.
+constexpr int kControlRegisters = 56, kEpilogueRegisters = 136, kWidenRegisters = 72;
+static_assert(128 * kControlRegisters + 256 * kEpilogueRegisters + 256 * kWidenRegisters <= kThreads * 96, "registers of the launch");
+constexpr int kAStage = 128 * kStep, kSlots = 4, kFirstA = 256, kTmem = 512;
 
+// kWide: B comes in 16 bits, and a tile has up to 128 columns; else up to 64, widened
+// here.  Widened: A behind the sums in tensor memory, 64 columns of two steps each; B in
+// shared memory, as two tiles of 64 steps.
+template <bool kWide> struct Shape {
+    static constexpr int kColumns = kWide ? 128 : 64;
+    static constexpr int kBRows = kColumns / 2, kBTile = kBRows * 128;
+    static constexpr int kBox = 32;                    // rows of B's loads
+    static constexpr int kStage = kAStage + (kWide ? 2 : 1) * kBTile, kStages = kWide ? 6 : 8;
+    static constexpr int kSlot = 2 * kBTile;           // B widened
+    static constexpr int kShared = kStages * kStage + (kWide ? 0 : kSlots * kSlot) + static_cast<int>(sizeof(Tables)) + 1024;
+    static_assert(2 * kColumns <= kFirstA && kFirstA + kSlots * kStep / 2 <= kTmem, "columns of tensor memory");
+};
+
+template <bool kWide>
 __device__ __forceinline__ bool load_stages(const CUtensorMap &map_a, const CUtensorMap &map_b, const Product &p, const Cta &c)
 {
+    using S = Shape<kWide>;
     const uint32_t full = smem_addr(&c.bars->full[0]), empty = smem_addr(&c.bars->empty[0]), base = smem_addr(c.stages);
+    const uint32_t own = in_cta(full, c.rank), full_b = in_cta(smem_addr(&c.bars->tail[0]), 0);
     int stage = 0;
     uint32_t phase = 1;
     for (int i = c.pair, g = 0; i < c.items; i += c.pairs) {
         const Item it = item_of<kStep>(p, *c.tables, c.lane_tiles, i, g);
-        const int half = (it.cols + 31) / 32 * 16;
+        const int half = (it.cols + 31) / 32 * 16, boxes = parts_of(half, S::kBox);
         const int a_lane = it.lane0 + c.rank * 128, b_col = it.row0 + it.col0 + c.rank * half, za = p.a_by_group ? it.g : 0;
         for (int k = it.k0; k < it.k1; ++k) {
             if (!wait(empty + stage * 8, phase))
                 return false;
             if (elected()) {
-                const uint32_t bar = full + stage * 8, a = base + stage * kStage;
-                arrive_expect(in_cta(bar, c.rank), kStage);
-                load_tile(a, &map_a, k * kStep, a_lane, za, bar);
-                load_tile(a + kAStage, &map_b, k * kStep, b_col, 0, bar);
+                const uint32_t bar = full + stage * 8, a = base + stage * S::kStage, b = a + kAStage;
+                if (kWide) {
+                    arrive_expect(own + stage * 8, kAStage);
+                    arrive_expect(full_b + stage * 8, 2 * boxes * S::kBox * 128);
+                    load_tile(a, &map_a, k * kStep, a_lane, za, bar);
+#pragma unroll
+                    for (int q = 0; q < S::kBRows / S::kBox; ++q)
+                        if (q < boxes) {
+                            load_tile(b + q * S::kBox * 128, &map_b, k * kStep, b_col + q * S::kBox, 0, full_b + stage * 8);
+                            load_tile(b + S::kBTile + q * S::kBox * 128, &map_b, k * kStep + 64, b_col + q * S::kBox, 0, full_b + stage * 8);
+                        }
+                } else {
+                    arrive_expect(own + stage * 8, S::kStage);
+                    load_tile(a, &map_a, k * kStep, a_lane, za, bar);
+                    load_tile(b, &map_b, k * kStep, b_col, 0, bar);
+                }
             }
             __syncwarp();
-            if (++stage == kStages)
+            if (++stage == S::kStages)
                 stage = 0, phase ^= 1;
         }
     }
@@ -78,8 +102,10 @@ __device__ __forceinline__ bool load_stages(const CUtensorMap &map_a, const CUte
 }
 
 // A's tiles into tensor memory, by two teams of four warps that take the stages in turn.
+template <bool kWide>
 __device__ __forceinline__ bool widen_a(const Product &p, const Cta &c)
 {
+    constexpr int kStage = Shape<kWide>::kStage, kStages = Shape<kWide>::kStages;
     const int warp = threadIdx.x / 32 - kFirstWidenWarp, lane = threadIdx.x & 31, quarter = warp & 3, team = warp >> 2;
     const uint32_t full = smem_addr(&c.bars->full[0]), empty = in_cta(smem_addr(&c.bars->empty[0]), c.rank);
     const uint32_t used = smem_addr(&c.bars->used[0]), ready = in_cta(smem_addr(&c.bars->ready[0]), 0);
@@ -127,6 +153,8 @@ __device__ __forceinline__ bool widen_a(const Product &p, const Cta &c)
 // B's tiles to shared memory, by two warps in turn.
 __device__ __forceinline__ bool widen_b(const Product &p, const Cta &c)
 {
+    using S = Shape<false>;
+    constexpr int kStage = S::kStage, kStages = S::kStages, kSlot = S::kSlot, kBTile = S::kBTile;
     const int lane = threadIdx.x & 31, turn = threadIdx.x / 32 - kFirstBWarp, chunk = lane & 7;
     const uint32_t full = smem_addr(&c.bars->full[0]), empty = in_cta(smem_addr(&c.bars->empty[0]), c.rank);
     const uint32_t used = smem_addr(&c.bars->used[0]), ready = in_cta(smem_addr(&c.bars->ready[0]), 0);
@@ -160,13 +188,16 @@ __device__ __forceinline__ bool widen_b(const Product &p, const Cta &c)
     return true;
 }
 
+template <bool kWide>
 __device__ __forceinline__ bool multiply_slots(const Product &p, const Cta &c)
 {
+    using S = Shape<kWide>;
     const uint32_t ready = smem_addr(&c.bars->ready[0]), used = smem_addr(&c.bars->used[0]);
+    const uint32_t full_b = smem_addr(&c.bars->tail[0]), empty = smem_addr(&c.bars->empty[0]);
     const uint32_t done = smem_addr(&c.bars->done[0]), drained = smem_addr(&c.bars->drained[0]);
-    const uint64_t first_b = operand(smem_addr(c.stages) + kStages * kStage, 16, 1024);
-    int slot = 0, half = 0;
-    uint32_t phase = 0, free_phase = 1;
+    const uint64_t first_b = operand(smem_addr(c.stages) + (kWide ? kAStage : S::kStages * S::kStage), 16, 1024);
+    int slot = 0, stage = 0, half = 0;
+    uint32_t phase = 0, stage_phase = 0, free_phase = 1;
     for (int i = c.pair, g = 0; i < c.items; i += c.pairs) {
         const Item it = item_of<kStep>(p, *c.tables, c.lane_tiles, i, g);
         const uint32_t idesc = shape(false, false, false, (it.cols + 31) / 32 * 32);
@@ -175,24 +206,28 @@ __device__ __forceinline__ bool multiply_slots(const Product &p, const Cta &c)
                 return false;
             fence_after();
             const int stop = min(it.k1, k + p.piece / kStep);
-            const uint32_t sums = c.tmem + half * kColumns;
+            const uint32_t sums = c.tmem + half * S::kColumns;
             for (bool add = false; k < stop; ++k, add = true) {
-                if (!wait(ready + slot * 8, phase))
+                if ((kWide && !wait(full_b + stage * 8, stage_phase)) || !wait(ready + slot * 8, phase))
                     return false;
                 fence_after();
                 if (elected()) {
                     const uint32_t a = c.tmem + kFirstA + slot * (kStep / 2);
-                    const uint64_t b = first_b + slot * (kSlot >> 4);
+                    const uint64_t b = first_b + (kWide ? stage * (S::kStage >> 4) : slot * (S::kSlot >> 4));
 #pragma unroll
                     for (int q = 0; q < kStep / 16; ++q)
-                        multiply(sums, a + q * 8, b + (q >> 2) * (kBTile >> 4) + (q & 3) * 2, idesc, q > 0 || add);
+                        multiply(sums, a + q * 8, b + (q >> 2) * (S::kBTile >> 4) + (q & 3) * 2, idesc, q > 0 || add);
                     commit(used + slot * 8);
+                    if (kWide)
+                        commit(empty + stage * 8);
                     if (k + 1 == stop)
                         commit(done + half * 8);
                 }
                 __syncwarp();
                 if (++slot == kSlots)
                     slot = 0, phase ^= 1;
+                if (++stage == S::kStages)
+                    stage = 0, stage_phase ^= 1;
             }
             if (half ^= 1; half == 0)
                 free_phase ^= 1;
@@ -201,14 +236,16 @@ __device__ __forceinline__ bool multiply_slots(const Product &p, const Cta &c)
     return true;
 }
 
+template <bool kWide>
 __global__ void __launch_bounds__(kThreads, 1)
 codes_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ Product p)
 {
+    using S = Shape<kWide>;
     extern __shared__ uint8_t dynamic[];
     __shared__ Barriers bars;
     Cta c;
     c.stages = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(dynamic) + 1023) & ~uintptr_t(1023));
-    Tables *tables = reinterpret_cast<Tables *>(c.stages + kStages * kStage + kSlots * kSlot);
+    Tables *tables = reinterpret_cast<Tables *>(c.stages + S::kStages * S::kStage + (kWide ? 0 : kSlots * S::kSlot));
     c.tables = tables;
     c.bars = &bars;
     c.rank = cta_rank();
@@ -220,12 +257,13 @@ codes_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
     if (warp == kProducerWarp && lane == 0) {
         prefetch_map(&map_a);
         prefetch_map(&map_b);
-        for (int s = 0; s < kStages; ++s) {
+        for (int s = 0; s < S::kStages; ++s) {
             barrier_init(smem_addr(&bars.full[s]), 1);
-            barrier_init(smem_addr(&bars.empty[s]), kWidenWarps / 2 + 1);
+            barrier_init(smem_addr(&bars.empty[s]), kWidenWarps / 2 + 1);        // a team, and B's warp or multiplies
+            barrier_init(smem_addr(&bars.tail[s]), 2);                           // B in 16 bits: in the first CTA, from both
         }
         for (int s = 0; s < kSlots; ++s) {
-            barrier_init(smem_addr(&bars.ready[s]), 2 * (kWidenWarps / 2 + 1));    // counts in the first CTA, from both
+            barrier_init(smem_addr(&bars.ready[s]), 2 * (kWidenWarps / 2 + (kWide ? 0 : 1)));    // likewise
             barrier_init(smem_addr(&bars.used[s]), 1);
         }
         init_epilogue_barriers(bars);
@@ -237,7 +275,7 @@ codes_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if (warp == kTablesWarp)
-        fill_tables<kStep>(p, *tables, kColumns, c.lane_tiles, c.pairs);
+        fill_tables<kStep>(p, *tables, S::kColumns, c.lane_tiles, c.pairs);
     fence_before();
     __syncthreads();
     cluster_sync();
@@ -246,19 +284,48 @@ codes_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
     c.items = tables->first[p.groups] * tables->split;
 
     bool fine = true;
-    if (warp == kProducerWarp)
-        fine = load_stages(map_a, map_b, p, c);
-    else if (warp == kMultiplyWarp && c.rank == 0)
-        fine = multiply_slots(p, c);
-    else if (warp >= kFirstWidenWarp)
-        fine = widen_a(p, c);
-    else if (warp == kFirstBWarp || warp == kFirstBWarp + 1)
-        fine = widen_b(p, c);
-    else if (warp >= kFirstEpilogueWarp)
-        fine = write_outputs<kColumns, true, kStep>(p, c);
+    if (warp < kFirstEpilogueWarp) {
+        fewer_registers<kControlRegisters>();
+        if (warp == kProducerWarp)
+            fine = load_stages<kWide>(map_a, map_b, p, c);
+        else if (warp == kMultiplyWarp && c.rank == 0)
+            fine = multiply_slots<kWide>(p, c);
+        else if (!kWide && warp >= kFirstBWarp)
+            fine = widen_b(p, c);
+    } else if (warp < kFirstWidenWarp) {
+        more_registers<kEpilogueRegisters>();
+        fine = write_outputs<S::kColumns, true, kStep>(p, c);
+    } else {
+        fewer_registers<kWidenRegisters>();
+        fine = widen_a<kWide>(p, c);
+    }
     finish_pair(fine, p.gave_up);
     if (warp == kMultiplyWarp)
         tmem_free(c.tmem, kTmem);
+}
+
+template <bool kWide>
+cudaError_t launch(const gnmr_products *h, const Operands &o, const Product &p, cudaStream_t st, bool *mapped)
+{
+    CUtensorMap a, b;
+    *mapped = gnmr::tile_map(h, &a, o.a, CU_TENSOR_MAP_DATA_TYPE_UINT8, 128) &&
+              gnmr::tile_map(h, &b, o.b, kWide ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8, Shape<kWide>::kBox);
+    if (!*mapped)
+        return cudaSuccess;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(2 * h->pairs);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = Shape<kWide>::kShared;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 2;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, codes_kernel<kWide>, a, b, p);
 }
 
 // ---- copies of operands -------------------------------------------------------------
@@ -268,10 +335,6 @@ struct Copy {
     const void *from;
     void *to;
     int64_t rows, cols, stride, group_stride, held;
-    const int64_t *offsets;                            // not NULL: groups without rows are left out
-    const uint8_t *mask;                               // not NULL: and those that are not computed
-    int64_t mask_stride;
-    int want;
 };
 
 constexpr int kCopyThreads = 256;
@@ -284,8 +347,6 @@ __global__ void __launch_bounds__(kCopyThreads) copy_kernel(Copy c)
     const int g = blockIdx.y;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    if ((c.offsets && c.offsets[g + 1] <= c.offsets[g]) || (c.mask && (c.mask[g * c.mask_stride] != 0) != (c.want != 0)))
-        return;
     const char *from = static_cast<const char *>(c.from) + g * c.group_stride * kFrom;
     char *to = static_cast<char *>(c.to) + g * c.rows * c.held * kTo;
     const int64_t across = (c.held + kN - 1) / kN, total = c.rows * across;
@@ -346,15 +407,9 @@ cudaError_t launch_copy(const Copy &c, int groups, bool whole, int sms, cudaStre
 
 namespace gnmr {
 
-cudaError_t copy_operand(const Operand &o, void *to, const Product &p, bool by_group, int sms, cudaStream_t st)
+cudaError_t copy_operand(const Operand &o, void *to, int sms, cudaStream_t st)
 {
-    Copy c{o.at, to, o.rows, o.cols, o.stride, o.group_stride, o.held(), nullptr, nullptr, 0, 0};
-    if (by_group) {
-        c.offsets = p.offsets;
-        c.mask = p.mask;
-        c.mask_stride = p.mask_stride;
-        c.want = p.want;
-    }
+    const Copy c{o.at, to, o.rows, o.cols, o.stride, o.group_stride, o.held()};
     const int64_t steps = o.stride * o.bytes | (o.groups > 1 ? o.group_stride * o.bytes : 0);
     const bool whole = ((reinterpret_cast<uintptr_t>(o.at) | static_cast<uintptr_t>(steps)) & 15) == 0;
     if (o.bytes == 2)
@@ -364,30 +419,13 @@ cudaError_t copy_operand(const Operand &o, void *to, const Product &p, bool by_g
 
 cudaError_t allow_codes_shared()
 {
-    return cudaFuncSetAttribute(codes_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kShared);
+    const cudaError_t e = cudaFuncSetAttribute(codes_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<false>::kShared);
+    return e != cudaSuccess ? e : cudaFuncSetAttribute(codes_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<true>::kShared);
 }
 
 cudaError_t launch_codes(const gnmr_products *h, const Operands &o, const Product &p, cudaStream_t st, bool *mapped)
 {
-    CUtensorMap a, b;
-    *mapped = tile_map(h, &a, o.a, CU_TENSOR_MAP_DATA_TYPE_UINT8, 128) &&
-              tile_map(h, &b, o.b, CU_TENSOR_MAP_DATA_TYPE_UINT8, kColumns / 2);
-    if (!*mapped)
-        return cudaSuccess;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(2 * h->pairs);
-    cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = kShared;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = 2;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[1].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, codes_kernel, a, b, p);
+    return o.b.read_bytes == 2 ? launch<true>(h, o, p, st, mapped) : launch<false>(h, o, p, st, mapped);
 }
 
 }  // namespace gnmr

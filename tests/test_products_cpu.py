@@ -58,6 +58,11 @@ def test_other_operands_are_copied_to_scratch():
     assert N.gnmr_products_scratch_bytes(product(n_in=9, x_stride=9, w_stride=16)) == 512          # 10 x 16
     assert N.gnmr_products_scratch_bytes(product(w_group_stride=129)) == 512  # 2 x 16 x 8
     assert N.gnmr_products_scratch_bytes(product(w_group_stride=0, d_w=4098)) == 256
+    i8 = dict(op=N.GNMR_PRODUCT_FORWARD_I8, n_in=32, x_stride=32, w_stride=32, w_group_stride=512)
+    assert N.gnmr_products_scratch_bytes(product(**i8)) == 0
+    assert N.gnmr_products_scratch_bytes(product(**i8, rows=64)) == 0
+    assert N.gnmr_products_scratch_bytes(product(**i8, rows=65)) == 65 * 64 + 192     # widened
+    assert N.gnmr_products_scratch_bytes(product(**{**i8, "w_stride": 33, "w_group_stride": 528})) == 2 * 16 * 32
 
 
 INVALID, LAYOUT = N.GNMR_ERR_INVALID_ARG, N.GNMR_ERR_LAYOUT
