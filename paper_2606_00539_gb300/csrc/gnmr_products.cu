@@ -260,15 +260,14 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     }
     if (warp == kMultiplyWarp)
         tmem_alloc(smem_addr(&bars.tmem), S::kTmem);
+    __syncwarp();
+    greet_pair();
     // Nothing above depends on the kernels before this one on the stream.
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if (warp == kTablesWarp)
         fill_tables<kStep>(p, *tables, kColumns, c.lane_tiles, c.pairs);
-    fence_before();
-    __syncthreads();
-    cluster_sync();
-    fence_after();
+    join_pair();
     c.tmem = bars.tmem;
     c.items = tables->first[p.groups] * tables->split;
 
@@ -468,7 +467,7 @@ gnmr_status gnmr_products_create(int32_t device, gnmr_products **out)
     cudaGetDevice(&prev);
     cudaSetDevice(device);
     h->device = device;
-    const size_t parts = size_t(kMaxParts) * kPartFloats * 4, tickets = size_t(kMaxParts) * 2 * 4;
+    const size_t parts = size_t(kMaxParts) * kPartFloats * 4, tickets = size_t(kMaxParts) * 2 * kEpilogueWarps * 4;
     cudaError_t e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
     h->pairs = std::min(std::max(sms / 2, 1), kMaxPairs);
     if (e == cudaSuccess)

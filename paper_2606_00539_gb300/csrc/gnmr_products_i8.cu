@@ -271,15 +271,14 @@ codes_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
     }
     if (warp == kMultiplyWarp)
         tmem_alloc(smem_addr(&bars.tmem), kTmem);
+    __syncwarp();
+    greet_pair();
     // Nothing above depends on the kernels before this one on the stream.
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if (warp == kTablesWarp)
         fill_tables<kStep>(p, *tables, S::kColumns, c.lane_tiles, c.pairs);
-    fence_before();
-    __syncthreads();
-    cluster_sync();
-    fence_after();
+    join_pair();
     c.tmem = bars.tmem;
     c.items = tables->first[p.groups] * tables->split;
 

@@ -166,6 +166,25 @@ __device__ __forceinline__ Item item_of(const Product &p, const Tables &t, int l
     return it;
 }
 
+// ---- a CTA ------------------------------------------------------------------------
+
+struct Barriers {
+    uint64_t full[8], empty[8];        // stages of operands
+    uint64_t tail[8];                  // a stage that the tail warp looks at first
+    uint64_t ready[4], used[4];        // operands widened from 8 bits
+    uint64_t done[2], drained[2];      // halves of tensor memory; `drained` counts in the first CTA
+    uint32_t tmem;
+};
+
+// What the roles of a CTA share.
+struct Cta {
+    uint8_t *stages;                   // dynamic shared memory, from a multiple of 1,024
+    const Tables *tables;
+    Barriers *bars;
+    uint32_t rank, tmem;
+    int pair, pairs, lane_tiles, items;
+};
+
 // ---- outputs --------------------------------------------------------------------
 
 template <int kOut> __device__ __forceinline__ unsigned pack(float lo, float hi)
@@ -191,6 +210,21 @@ template <int kOut> __device__ __forceinline__ unsigned exchange(float first, fl
 {
     const unsigned w = pack<kOut>(first, second);
     return __byte_perm(w, __shfl_xor_sync(~0u, w, 1), which);
+}
+
+// The outputs that a tile will be added to, to L2 while it is multiplied: read as they are
+// needed, 16 at a time, they took longer than the multiplies.
+__device__ __forceinline__ void fetch_outputs(const Product &p, const Cta &c, const Item &it, int warp)
+{
+    const int bytes = p.out_type == GNMR_DTYPE_F32 ? 4 : 2, lines = 128 * bytes / 128;     // of a column, a CTA's lanes
+    const int lane = threadIdx.x & 31, first = it.lane0 + c.rank * 128;
+    const int64_t row = p.cols ? it.col0 : int64_t(it.row0) + it.col0;
+    const char *out = static_cast<const char *>(p.out) + ((p.cols ? it.g * p.out_group : 0) + row * p.out_col + first) * bytes;
+    for (int i = warp * 32 + lane; i < it.cols * lines; i += kEpilogueWarps * 32) {
+        const int col = i / lines, line = i - col * lines;
+        if (first + line * (128 / bytes) < p.lanes)
+            asm volatile("prefetch.global.L2 [%0];" ::"l"(out + col * p.out_col * bytes + line * 128));
+    }
 }
 
 // This warp's sums to the outputs: lane `lane` of columns col .. col + span - 1 of the
@@ -302,27 +336,6 @@ __device__ __forceinline__ void add_to_sum(uint32_t (&acc)[16], const uint32_t (
                         : __float_as_uint(__uint_as_float(acc[j]) + __uint_as_float(v[j]));
 }
 
-// ---- a CTA ------------------------------------------------------------------------
-
-struct Barriers {
-    uint64_t full[8], empty[8];        // stages of operands
-    uint64_t tail[8];                  // a stage that the tail warp looks at first
-    uint64_t ready[4], used[4];        // operands widened from 8 bits
-    uint64_t done[2], drained[2];      // halves of tensor memory; `drained` counts in the first CTA
-    uint64_t written, counted;         // of a split tile's part: by its warps, and its ticket
-    uint32_t tmem;
-    unsigned last;                     // whether this CTA is a split tile's last
-};
-
-// What the roles of a CTA share.
-struct Cta {
-    uint8_t *stages;                   // dynamic shared memory, from a multiple of 1,024
-    const Tables *tables;
-    Barriers *bars;
-    uint32_t rank, tmem;
-    int pair, pairs, lane_tiles, items;
-};
-
 // The barriers that the epilogue counts on.
 __device__ __forceinline__ void init_epilogue_barriers(Barriers &b)
 {
@@ -330,8 +343,21 @@ __device__ __forceinline__ void init_epilogue_barriers(Barriers &b)
         barrier_init(smem_addr(&b.done[h]), 1);
         barrier_init(smem_addr(&b.drained[h]), 2 * kEpilogueWarps);
     }
-    barrier_init(smem_addr(&b.written), kEpilogueWarps);
-    barrier_init(smem_addr(&b.counted), 1);
+}
+
+// The beginning of every kernel, after the barriers' initialisation: the other CTA's
+// are initialised too by the time that join_pair returns.
+__device__ __forceinline__ void greet_pair()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+}
+
+__device__ __forceinline__ void join_pair()
+{
+    fence_before();
+    __syncthreads();
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    fence_after();
 }
 
 // The end of every kernel: both CTAs of a pair are through, and a role that gave up has
@@ -351,11 +377,12 @@ __device__ __forceinline__ void finish_pair(bool fine, int *gave_up)
     fence_after();
 }
 
-// A split tile: this part goes to memory, and the last CTA of its rank to get here
-// takes the sum of all parts, in their order.  1: it has; 0: another will; -1: gave up.
+// A split tile: this warp's lanes and columns of this part go to memory, and the warp that
+// gets here last takes the sum of all parts, in their order.  Warps do not wait for one
+// another: whether this one has the sum.
 template <int kColumns, bool kCodes>
-__device__ __forceinline__ int join_parts(const Product &p, const Cta &c, const Item &it, uint32_t (&acc)[kColumns / 32][16],
-                                          int span, int col, int warp, uint32_t turn)
+__device__ __forceinline__ bool join_parts(const Product &p, const Cta &c, const Item &it, uint32_t (&acc)[kColumns / 32][16],
+                                           int cols, int col, int warp)
 {
     constexpr int kPieces = kColumns / 32;               // of 16 columns
     const int lane = threadIdx.x & 31, split = c.tables->split;
@@ -363,46 +390,37 @@ __device__ __forceinline__ int join_parts(const Product &p, const Cta &c, const 
                      c.rank * (kPartFloats / 2) + (warp & 3) * 32 + lane;
 #pragma unroll
     for (int q = 0; q < kPieces; ++q)
-        if (q * 16 < span)
 #pragma unroll
-            for (int j = 0; j < 16; ++j)
+        for (int j = 0; j < 16; ++j)
+            if (q * 16 + j < cols)
                 part[it.part * kPartFloats + (col + q * 16 + j) * 128] = acc[q][j];
     __threadfence();
     __syncwarp();
-    if (lane == 0)
-        arrive_release(in_cta(smem_addr(&c.bars->written), c.rank));
-    if (warp == kFirstEpilogueWarp) {
-        if (!wait(smem_addr(&c.bars->written), turn))
-            return -1;
-        if (lane == 0) {
-            __threadfence();
-            unsigned *ticket = p.tickets + 2 * it.tile + c.rank;
-            c.bars->last = atomicAdd(ticket, 1u) + 1 == static_cast<unsigned>(split);
-            if (c.bars->last)
-                *ticket = 0;
-            __threadfence();
-            arrive_release(in_cta(smem_addr(&c.bars->counted), c.rank));
-        }
-        __syncwarp();
+    unsigned before = 0;
+    if (lane == 0) {
+        unsigned *ticket = p.tickets + (2 * it.tile + c.rank) * kEpilogueWarps + warp - kFirstEpilogueWarp;
+        before = atomicAdd(ticket, 1u);
+        if (before + 1 == static_cast<unsigned>(split))
+            *ticket = 0;                                 // for the next call
+        __threadfence();
     }
-    if (!wait(smem_addr(&c.bars->counted), turn))
-        return -1;
-    if (!c.bars->last)
-        return 0;
+    if (__shfl_sync(~0u, before, 0) + 1 != static_cast<unsigned>(split))
+        return false;
 #pragma unroll
     for (int q = 0; q < kPieces; ++q)
-        if (q * 16 < span) {
+        if (q * 16 < cols) {
+#pragma unroll 2
             for (int s = 0; s < split; ++s)
 #pragma unroll
                 for (int j = 0; j < 16; ++j) {
-                    const uint32_t v = __ldcg(part + s * kPartFloats + (col + q * 16 + j) * 128);
+                    const uint32_t v = q * 16 + j < cols ? __ldcg(part + s * kPartFloats + (col + q * 16 + j) * 128) : 0;
                     if (s == 0)
                         acc[q][j] = v;
                     else
                         acc[q][j] = kCodes ? acc[q][j] + v : __float_as_uint(__uint_as_float(acc[q][j]) + __uint_as_float(v));
                 }
         }
-    return 1;
+    return true;
 }
 
 // The epilogue's warps: a tile's pieces added up and written.
@@ -414,11 +432,13 @@ __device__ __forceinline__ bool write_outputs(const Product &p, const Cta &c)
     const int quarter = warp & 3, side = (warp - kFirstEpilogueWarp) >> 2;
     const uint32_t done = smem_addr(&c.bars->done[0]), drained = in_cta(smem_addr(&c.bars->drained[0]), 0);
     int half = 0;
-    uint32_t phase = 0, joins = 0;
+    uint32_t phase = 0;
     for (int i = c.pair, g = 0; i < c.items; i += c.pairs) {
         const Item it = item_of<kStep>(p, *c.tables, c.lane_tiles, i, g);
         const int span = (it.cols + 31) / 32 * 16;                          // columns of this warp
         const int at = it.lane0 + c.rank * 128 + quarter * 32 + lane, col = side * span;
+        if (p.add)
+            fetch_outputs(p, c, it, warp - kFirstEpilogueWarp);
         uint32_t acc[kPieces][16];
         if (it.k0 == it.k1)
 #pragma unroll
@@ -458,13 +478,8 @@ __device__ __forceinline__ bool write_outputs(const Product &p, const Cta &c)
             if (half ^= 1; half == 0)
                 phase ^= 1;
         }
-        if (c.tables->split > 1) {
-            const int mine = join_parts<kColumns, kCodes>(p, c, it, acc, span, col, warp, joins++ & 1);
-            if (mine < 0)
-                return false;
-            if (mine == 0)
-                continue;
-        }
+        if (c.tables->split > 1 && !join_parts<kColumns, kCodes>(p, c, it, acc, min(span, it.cols - col), col, warp))
+            continue;
         if (p.add && it.depth == 0)
             continue;                                    // nothing to add
         if (p.out_type == GNMR_DTYPE_F32)
