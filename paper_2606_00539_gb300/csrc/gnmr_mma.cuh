@@ -112,11 +112,11 @@ template <int kRegisters> __device__ __forceinline__ void fewer_registers()
 // ---- tile loads ---------------------------------------------------------------
 // The barrier may be the other CTA's of the pair.
 
-__device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap *map, int x, int y, int z, uint32_t bar)
+__device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap *map, int x, int y, int block, int z, uint32_t bar)
 {
-    asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
-                 "[%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
-                 "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+    asm volatile("cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
+                 "[%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
+                 "l"(map), "r"(x), "r"(y), "r"(block), "r"(z), "r"(bar)
                  : "memory");
 }
 

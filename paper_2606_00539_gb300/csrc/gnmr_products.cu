@@ -54,12 +54,13 @@ static_assert(128 * kControlRegisters + 256 * kEpilogueRegisters <= kThreads * 1
 constexpr int kAStage = 128 * 128;                     // bytes of A's tile in one CTA
 constexpr int kBlock = 64 * 128;                       // bytes of a tile of 64 lanes or columns lying along rows
 
-// kColumns columns at most; a CTA loads half of B's tile, in boxes of kBox rows.
+// kColumns columns at most; a CTA loads half of B's tile, as kBox rows in one load whatever
+// there are (each load costs its issuing thread about 100 of the 512 cycles that a stage's
+// multiplies take: with two for B, 8192^3 took 621 us).
 template <int kColumns> struct Shape {
-    static constexpr int kBStage = kColumns / 2 * 128;
-    static constexpr int kStage = kAStage + (kBStage < kBlock ? kBlock : kBStage);
-    static constexpr int kStages = kColumns == 256 ? 6 : 8;
-    static constexpr int kBox = kColumns == 256 ? 64 : 16;
+    static constexpr int kBox = kColumns / 2;
+    static constexpr int kStage = kAStage + kBox * 128;
+    static constexpr int kStages = kColumns == 256 ? 6 : 10;
     static constexpr int kTmem = 2 * kColumns;
 };
 
@@ -86,17 +87,17 @@ template <int kColumns, int kOp>
 __device__ __forceinline__ bool load_stages(const CUtensorMap &map_a, const CUtensorMap &map_b, const Product &p, const Cta &c)
 {
     using S = Shape<kColumns>;
-    constexpr int kBoxB = b_along_columns(kOp) ? 64 : S::kBox;
     const uint32_t full = in_cta(smem_addr(&c.bars->full[0]), 0), empty = smem_addr(&c.bars->empty[0]);
     const uint32_t tail = smem_addr(&c.bars->tail[0]), base = smem_addr(c.stages);
     int stage = 0;
     uint32_t phase = 1;
     for (int i = c.pair, g = 0; i < c.items; i += c.pairs) {
         const Item it = item_of<kStep>(p, *c.tables, c.lane_tiles, i, g);
-        const int half = (it.cols + 31) / 32 * 16;                         // B's columns in this CTA
+        const int half = it.wide / 2;                         // B's columns in this CTA
         const int a_lane = it.lane0 + c.rank * 128, b_col = it.col0 + c.rank * half + (rows_deep(kOp) ? 0 : it.row0);
-        const int boxes = parts_of(half, kBoxB), za = p.a_by_group ? it.g : 0;
-        const uint32_t bytes = kAStage + boxes * kBoxB * 128;
+        const int za = p.a_by_group ? it.g : 0;
+        const bool two = b_along_columns(kOp) && (p.b_blocks || half > 64);        // blocks of B
+        const uint32_t bytes = kAStage + (!b_along_columns(kOp) ? S::kBox * 128 : two ? 2 * kBlock : kBlock);
         for (int k = it.k0; k < it.k1; ++k) {
             if (!wait(empty + stage * 8, phase))
                 return false;
@@ -110,20 +111,23 @@ __device__ __forceinline__ bool load_stages(const CUtensorMap &map_a, const CUte
                 const uint32_t bar = first_tail ? tail + stage * 8 : full + stage * 8;
                 const uint32_t a = base + stage * S::kStage, b = a + kAStage;
                 arrive_expect(first_tail ? in_cta(bar, c.rank) : bar, bytes);
-                if (a_along_lanes(kOp)) {
-                    load_tile(a, &map_a, a_lane, at, za, bar);
-                    load_tile(a + kBlock, &map_a, a_lane + 64, at, za, bar);
+                if (!a_along_lanes(kOp)) {
+                    load_tile(a, &map_a, at, a_lane, 0, za, bar);
+                } else if (p.a_blocks) {
+                    load_tile(a, &map_a, 0, at, a_lane >> 6, za, bar);
                 } else {
-                    load_tile(a, &map_a, at, a_lane, za, bar);
+                    load_tile(a, &map_a, a_lane, at, 0, za, bar);
+                    load_tile(a + kBlock, &map_a, a_lane + 64, at, 0, za, bar);
                 }
-#pragma unroll
-                for (int q = 0; q < S::kBStage / (kBoxB * 128) || q == 0; ++q)
-                    if (q < boxes) {
-                        if (b_along_columns(kOp))
-                            load_tile(b + q * kBlock, &map_b, b_col + q * 64, at, 0, bar);
-                        else
-                            load_tile(b + q * S::kBox * 128, &map_b, at, b_col + q * S::kBox, 0, bar);
-                    }
+                if (!b_along_columns(kOp)) {
+                    load_tile(b, &map_b, at, b_col, 0, 0, bar);
+                } else if (p.b_blocks) {
+                    load_tile(b, &map_b, 0, at, b_col >> 6, 0, bar);
+                } else {
+                    load_tile(b, &map_b, b_col, at, 0, 0, bar);
+                    if (two)
+                        load_tile(b + kBlock, &map_b, b_col + 64, at, 0, 0, bar);
+                }
             }
             __syncwarp();
             if (++stage == S::kStages)
@@ -147,7 +151,7 @@ __device__ __forceinline__ bool multiply_stages(const Product &p, const Cta &c)
     uint32_t phase = 0, free_phase = 1;                  // free_phase: of both halves, while half is 0
     for (int i = c.pair, g = 0; i < c.items; i += c.pairs) {
         const Item it = item_of<kStep>(p, *c.tables, c.lane_tiles, i, g);
-        const uint32_t idesc = shape(p.bf16, a_along_lanes(kOp), b_along_columns(kOp), (it.cols + 31) / 32 * 32);
+        const uint32_t idesc = shape(p.bf16, a_along_lanes(kOp), b_along_columns(kOp), it.wide);
         const int count = it.k1 - it.k0, turn = it.tail ? min(kTailTurn, count - 1) : -1;
         const int first = stage;
         const uint32_t first_phase = phase;
@@ -214,7 +218,7 @@ __device__ __forceinline__ bool clear_tails(const Product &p, const Cta &c)
             if (!wait(smem_addr(&c.bars->tail[at]), (phase >> at) & 1))
                 return false;
             phase ^= 1u << at;
-            const int blocks = 2 + parts_of((it.cols + 31) / 32 * 16, 64), stop = (left + 15) / 16 * 16;
+            const int blocks = 2 + parts_of(it.wide / 2, 64), stop = (left + 15) / 16 * 16;
             uint4 *to = reinterpret_cast<uint4 *>(c.stages + at * S::kStage);
             for (int q = 0; q < blocks; ++q)
                 for (int v = left * 8 + lane; v < stop * 8; v += 32)
@@ -373,8 +377,8 @@ cudaError_t launch(const gnmr_products *h, const Operands &o, const Product &p, 
 {
     CUtensorMap a, b;
     const CUtensorMapDataType type = p.bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
-    *mapped = gnmr::tile_map(h, &a, o.a, type, a_along_lanes(kOp) ? 64 : 128) &&
-              gnmr::tile_map(h, &b, o.b, type, b_along_columns(kOp) ? 64 : Shape<kColumns>::kBox);
+    *mapped = gnmr::tile_map(h, &a, o.a, type, a_along_lanes(kOp) ? kStep : 128, p.a_blocks ? 2 : 1) &&
+              gnmr::tile_map(h, &b, o.b, type, b_along_columns(kOp) ? kStep : Shape<kColumns>::kBox, p.b_blocks ? 2 : 1);
     if (!*mapped)
         return cudaSuccess;
     cudaLaunchConfig_t cfg = {};
@@ -422,18 +426,21 @@ cudaError_t allow_all_shared()
 
 namespace gnmr {
 
-bool tile_map(const gnmr_products *h, CUtensorMap *map, const Operand &o, CUtensorMapDataType type, int high)
+bool tile_map(const gnmr_products *h, CUtensorMap *map, const Operand &o, CUtensorMapDataType type, int high, int blocks)
 {
     if (o.rows == 0) {                                   // nothing will be loaded
         memset(map, 0, sizeof(*map));
         return true;
     }
-    const cuuint64_t dims[3] = {static_cast<cuuint64_t>(o.cols), static_cast<cuuint64_t>(o.rows), static_cast<cuuint64_t>(o.groups)};
+    const int wide = 128 / o.read_bytes;
     const cuuint64_t row = static_cast<cuuint64_t>(o.stride) * o.read_bytes;
-    const cuuint64_t strides[2] = {row, o.groups > 1 ? static_cast<cuuint64_t>(o.group_stride) * o.read_bytes : row};
-    const cuuint32_t box[3] = {static_cast<cuuint32_t>(128 / o.read_bytes), static_cast<cuuint32_t>(high), 1}, one[3] = {1, 1, 1};
+    const cuuint64_t dims[4] = {static_cast<cuuint64_t>(blocks > 1 ? wide : o.cols), static_cast<cuuint64_t>(o.rows),
+                                static_cast<cuuint64_t>(blocks > 1 ? o.cols / wide : 1), static_cast<cuuint64_t>(o.groups)};
+    const cuuint64_t strides[3] = {row, 128, o.groups > 1 ? static_cast<cuuint64_t>(o.group_stride) * o.read_bytes : row};
+    const cuuint32_t box[4] = {static_cast<cuuint32_t>(wide), static_cast<cuuint32_t>(high), static_cast<cuuint32_t>(blocks), 1};
+    const cuuint32_t one[4] = {1, 1, 1, 1};
     const auto encode = [&] {
-        return h->encode(map, type, 3, const_cast<void *>(o.at), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+        return h->encode(map, type, 4, const_cast<void *>(o.at), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
                          CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     };
@@ -544,6 +551,9 @@ gnmr_status gnmr_products_run(gnmr_products *h, const gnmr_product *p, void *str
     q.mask_stride = p->mask_stride;
     q.want = codes ? 0 : 1;
     q.a_by_group = o.a.groups > 1;
+    q.a_blocks = (wgrad || back) && q.lanes % 64 == 0;
+    q.b_blocks = wgrad && q.cols % 64 == 0;
+    q.granule = q.b_blocks ? 128 : 32;
     q.bf16 = !codes && p->dtype == GNMR_DTYPE_BF16;
     q.piece = !codes && p->out_dtype == GNMR_DTYPE_F32 ? 512 : 1024;
     q.out = p->d_out;
@@ -568,7 +578,9 @@ gnmr_status gnmr_products_run(gnmr_products *h, const gnmr_product *p, void *str
     for (Operand *m : {&o.a, &o.b})
         if (const int64_t n = m->copy_bytes(); n && e == cudaSuccess) {
             e = gnmr::copy_operand(*m, scratch, 2 * h->pairs, st);
-            *m = Operand{scratch, m->rows, m->cols, m->held(), m->rows * m->held(), m->groups, m->read_bytes, m->read_bytes};
+            const bool widened = m->bytes != m->read_bytes;      // then the zeros after the last column count as columns
+            *m = Operand{scratch, m->rows, widened ? m->held() : m->cols, m->held(), m->rows * m->held(), m->groups, m->read_bytes,
+                         m->read_bytes};
             scratch += n;
         }
     // few rows to a group: smaller tiles, more of them in flight

@@ -24,13 +24,18 @@ struct gnmr_products {
 namespace gnmr {
 
 // A matrix operand of 1- or 2-byte elements, and the element size that its kernel
-// reads; operands that are not read in place are copied to rows of `held` elements.
+// reads; operands that are not read in place are copied to rows of `held` elements, zeros
+// after the last column: whole 16 bytes, or whole blocks of 128 where they are widened.
 struct Operand {
     const void *at;
     int64_t rows, cols, stride, group_stride;
     int groups;
     int bytes, read_bytes;
-    int64_t held() const { return (cols * read_bytes + 15) / 16 * 16 / read_bytes; }
+    int64_t held() const
+    {
+        const int64_t unit = (bytes == read_bytes ? 16 : 128) / read_bytes;
+        return (cols + unit - 1) / unit * unit;
+    }
     bool in_place() const
     {
         const int64_t steps = stride * bytes | (groups > 1 ? group_stride * bytes : 0);
@@ -46,8 +51,10 @@ struct Operands {
     Operand a, b;
 };
 
-// Tiles of `high` rows by 128 bytes of an operand.
-bool tile_map(const gnmr_products *h, CUtensorMap *map, const Operand &o, CUtensorMapDataType type, int high);
+// Tiles of `high` rows by `blocks` blocks of 128 bytes of an operand, a block after the other.
+// Several blocks: the operand's columns are whole blocks.  Coordinates of a tile: its
+// first column, or 0 where there are several blocks; row; block, or 0 where there is one; group.
+bool tile_map(const gnmr_products *h, CUtensorMap *map, const Operand &o, CUtensorMapDataType type, int high, int blocks);
 
 // The copy of an operand in `to`.
 cudaError_t copy_operand(const Operand &o, void *to, int sms, cudaStream_t st);

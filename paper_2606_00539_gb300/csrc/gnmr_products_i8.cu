@@ -53,7 +53,6 @@ constexpr int kAStage = 128 * kStep, kSlots = 4, kFirstA = 256, kTmem = 512;
 template <bool kWide> struct Shape {
     static constexpr int kColumns = kWide ? 128 : 64;
     static constexpr int kBRows = kColumns / 2, kBTile = kBRows * 128;
-    static constexpr int kBox = 32;                    // rows of B's loads
     static constexpr int kStage = kAStage + (kWide ? 2 : 1) * kBTile, kStages = kWide ? 6 : 8;
     static constexpr int kSlot = 2 * kBTile;           // B widened
     static constexpr int kShared = kStages * kStage + (kWide ? 0 : kSlots * kSlot) + static_cast<int>(sizeof(Tables)) + 1024;
@@ -70,7 +69,7 @@ __device__ __forceinline__ bool load_stages(const CUtensorMap &map_a, const CUte
     uint32_t phase = 1;
     for (int i = c.pair, g = 0; i < c.items; i += c.pairs) {
         const Item it = item_of<kStep>(p, *c.tables, c.lane_tiles, i, g);
-        const int half = (it.cols + 31) / 32 * 16, boxes = parts_of(half, S::kBox);
+        const int half = it.wide / 2;
         const int a_lane = it.lane0 + c.rank * 128, b_col = it.row0 + it.col0 + c.rank * half, za = p.a_by_group ? it.g : 0;
         for (int k = it.k0; k < it.k1; ++k) {
             if (!wait(empty + stage * 8, phase))
@@ -79,18 +78,13 @@ __device__ __forceinline__ bool load_stages(const CUtensorMap &map_a, const CUte
                 const uint32_t bar = full + stage * 8, a = base + stage * S::kStage, b = a + kAStage;
                 if (kWide) {
                     arrive_expect(own + stage * 8, kAStage);
-                    arrive_expect(full_b + stage * 8, 2 * boxes * S::kBox * 128);
-                    load_tile(a, &map_a, k * kStep, a_lane, za, bar);
-#pragma unroll
-                    for (int q = 0; q < S::kBRows / S::kBox; ++q)
-                        if (q < boxes) {
-                            load_tile(b + q * S::kBox * 128, &map_b, k * kStep, b_col + q * S::kBox, 0, full_b + stage * 8);
-                            load_tile(b + S::kBTile + q * S::kBox * 128, &map_b, k * kStep + 64, b_col + q * S::kBox, 0, full_b + stage * 8);
-                        }
+                    arrive_expect(full_b + stage * 8, 2 * S::kBTile);
+                    load_tile(a, &map_a, k * kStep, a_lane, 0, za, bar);
+                    load_tile(b, &map_b, 0, b_col, 2 * k, 0, full_b + stage * 8);
                 } else {
                     arrive_expect(own + stage * 8, S::kStage);
-                    load_tile(a, &map_a, k * kStep, a_lane, za, bar);
-                    load_tile(b, &map_b, k * kStep, b_col, 0, bar);
+                    load_tile(a, &map_a, k * kStep, a_lane, 0, za, bar);
+                    load_tile(b, &map_b, k * kStep, b_col, 0, 0, bar);
                 }
             }
             __syncwarp();
@@ -161,7 +155,7 @@ __device__ __forceinline__ bool widen_b(const Product &p, const Cta &c)
     int n = 0;
     for (int i = c.pair, g = 0; i < c.items; i += c.pairs) {
         const Item it = item_of<kStep>(p, *c.tables, c.lane_tiles, i, g);
-        const int end = n + it.k1 - it.k0, half = (it.cols + 31) / 32 * 16;
+        const int end = n + it.k1 - it.k0, half = it.wide / 2;
         for (n += (n ^ turn) & 1; n < end; n += 2) {
             const int stage = n % kStages, slot = n % kSlots;
             if (!wait(full + stage * 8, (n / kStages) & 1) || !wait(used + slot * 8, (n / kSlots + 1) & 1))
@@ -200,7 +194,7 @@ __device__ __forceinline__ bool multiply_slots(const Product &p, const Cta &c)
     uint32_t phase = 0, stage_phase = 0, free_phase = 1;
     for (int i = c.pair, g = 0; i < c.items; i += c.pairs) {
         const Item it = item_of<kStep>(p, *c.tables, c.lane_tiles, i, g);
-        const uint32_t idesc = shape(false, false, false, (it.cols + 31) / 32 * 32);
+        const uint32_t idesc = shape(false, false, false, it.wide);
         for (int k = it.k0; k < it.k1;) {
             if (!wait(drained + half * 8, free_phase))
                 return false;
@@ -307,8 +301,9 @@ template <bool kWide>
 cudaError_t launch(const gnmr_products *h, const Operands &o, const Product &p, cudaStream_t st, bool *mapped)
 {
     CUtensorMap a, b;
-    *mapped = gnmr::tile_map(h, &a, o.a, CU_TENSOR_MAP_DATA_TYPE_UINT8, 128) &&
-              gnmr::tile_map(h, &b, o.b, kWide ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8, Shape<kWide>::kBox);
+    *mapped = gnmr::tile_map(h, &a, o.a, CU_TENSOR_MAP_DATA_TYPE_UINT8, 128, 1) &&
+              (kWide ? gnmr::tile_map(h, &b, o.b, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, Shape<kWide>::kBRows, 2)
+                     : gnmr::tile_map(h, &b, o.b, CU_TENSOR_MAP_DATA_TYPE_UINT8, Shape<kWide>::kBRows, 1));
     if (!*mapped)
         return cudaSuccess;
     cudaLaunchConfig_t cfg = {};

@@ -31,7 +31,9 @@ struct Product {
     int64_t mask_stride;
     int want;                          // groups computed: mask byte != 0 (1), == 0 (0)
     unsigned lane_tiles_inverse;       // ceil(2^32 / tiles of 256 lanes)
-    int a_by_group;                    // A's third coordinate is the group
+    int a_by_group;                    // A's tiles are those of the group
+    int a_blocks, b_blocks;            // two blocks of 64 lanes or columns in one load
+    int granule;                       // a tile's columns are multiples of it: 32 or 128
     int bf16;
     int piece;                         // contraction steps of a piece
     void *out;
@@ -56,6 +58,7 @@ struct Tables {
 
 struct Item {
     int g, lane0, col0, cols;          // the tile: the pair's lanes, and its columns
+    int wide;                          // the columns multiplied, half of them from each CTA's B
     int row0;                          // the group's first row
     int depth, k0, k1;                 // the whole contraction; the stages of this part
     int tile, part;
@@ -95,8 +98,8 @@ __device__ __forceinline__ void fill_tables(const Product &p, Tables &t, int mos
             const int rows = t.row[g + 1] - t.row[g];
             const int cols = p.cols ? p.cols : rows, across = parts_of(cols, most);
             n = lane_tiles * across;
-            // a group's columns are shared out evenly, in multiples of 32
-            t.each[g] = static_cast<uint16_t>(across ? parts_of(parts_of(cols, across), 32) * 32 : 0);
+            // a group's columns are shared out evenly, in multiples of the granule
+            t.each[g] = static_cast<uint16_t>(across ? parts_of(parts_of(cols, across), p.granule) * p.granule : 0);
             deepest = max(deepest, p.depth ? p.depth : rows);
         }
         int sum = n;
@@ -154,6 +157,7 @@ __device__ __forceinline__ Item item_of(const Product &p, const Tables &t, int l
     it.lane0 = (at - c * lane_tiles) * kLanes;
     it.col0 = c * each;
     it.cols = min(each, (p.cols ? p.cols : rows) - it.col0);
+    it.wide = (it.cols + p.granule - 1) & -p.granule;
     it.depth = p.depth ? p.depth : rows;
     const int stages = parts_of(it.depth, kStep);
     it.k0 = 0;
@@ -169,8 +173,8 @@ __device__ __forceinline__ Item item_of(const Product &p, const Tables &t, int l
 // ---- a CTA ------------------------------------------------------------------------
 
 struct Barriers {
-    uint64_t full[8], empty[8];        // stages of operands
-    uint64_t tail[8];                  // a stage that the tail warp looks at first
+    uint64_t full[10], empty[10];      // stages of operands
+    uint64_t tail[10];                 // a stage that the tail warp looks at first
     uint64_t ready[4], used[4];        // operands widened from 8 bits
     uint64_t done[2], drained[2];      // halves of tensor memory; `drained` counts in the first CTA
     uint32_t tmem;
@@ -435,7 +439,7 @@ __device__ __forceinline__ bool write_outputs(const Product &p, const Cta &c)
     uint32_t phase = 0;
     for (int i = c.pair, g = 0; i < c.items; i += c.pairs) {
         const Item it = item_of<kStep>(p, *c.tables, c.lane_tiles, i, g);
-        const int span = (it.cols + 31) / 32 * 16;                          // columns of this warp
+        const int span = it.wide / 2;                          // columns of this warp
         const int at = it.lane0 + c.rank * 128 + quarter * 32 + lane, col = side * span;
         if (p.add)
             fetch_outputs(p, c, it, warp - kFirstEpilogueWarp);

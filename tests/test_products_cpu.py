@@ -61,7 +61,7 @@ def test_other_operands_are_copied_to_scratch():
     i8 = dict(op=N.GNMR_PRODUCT_FORWARD_I8, n_in=32, x_stride=32, w_stride=32, w_group_stride=512)
     assert N.gnmr_products_scratch_bytes(product(**i8)) == 0
     assert N.gnmr_products_scratch_bytes(product(**i8, rows=64)) == 0
-    assert N.gnmr_products_scratch_bytes(product(**i8, rows=65)) == 65 * 64 + 192     # widened
+    assert N.gnmr_products_scratch_bytes(product(**i8, rows=65)) == 65 * 128 + 128    # widened, to whole 128 bytes
     assert N.gnmr_products_scratch_bytes(product(**{**i8, "w_stride": 33, "w_group_stride": 528})) == 2 * 16 * 32
 
 
