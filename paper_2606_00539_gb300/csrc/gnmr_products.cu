@@ -60,7 +60,6 @@ constexpr int kBlock = 64 * 128;                       // bytes of a tile of 64 
 template <int kColumns> struct Shape {
     static constexpr int kBox = kColumns / 2;
     static constexpr int kStage = kAStage + kBox * 128;
-    static constexpr int kStages = kColumns == 256 ? 6 : 10;
     static constexpr int kTmem = 2 * kColumns;
 };
 
@@ -92,7 +91,7 @@ __device__ __forceinline__ bool load_stages(const CUtensorMap &map_a, const CUte
     int stage = 0;
     uint32_t phase = 1;
     for (int i = c.pair, g = 0; i < c.items; i += c.pairs) {
-        const Item it = item_of<kStep>(p, *c.tables, c.lane_tiles, i, g);
+        const Item it = item_of<kStep>(p, c.tables, c.split, c.lane_tiles, i, g);
         const int half = it.wide / 2;                         // B's columns in this CTA
         const int a_lane = it.lane0 + c.rank * 128, b_col = it.col0 + c.rank * half + (rows_deep(kOp) ? 0 : it.row0);
         const int za = p.a_by_group ? it.g : 0;
@@ -130,7 +129,7 @@ __device__ __forceinline__ bool load_stages(const CUtensorMap &map_a, const CUte
                 }
             }
             __syncwarp();
-            if (++stage == S::kStages)
+            if (++stage == c.ring)
                 stage = 0, phase ^= 1;
         }
     }
@@ -150,7 +149,7 @@ __device__ __forceinline__ bool multiply_stages(const Product &p, const Cta &c)
     int stage = 0, half = 0;
     uint32_t phase = 0, free_phase = 1;                  // free_phase: of both halves, while half is 0
     for (int i = c.pair, g = 0; i < c.items; i += c.pairs) {
-        const Item it = item_of<kStep>(p, *c.tables, c.lane_tiles, i, g);
+        const Item it = item_of<kStep>(p, c.tables, c.split, c.lane_tiles, i, g);
         const uint32_t idesc = shape(p.bf16, a_along_lanes(kOp), b_along_columns(kOp), it.wide);
         const int count = it.k1 - it.k0, turn = it.tail ? min(kTailTurn, count - 1) : -1;
         const int first = stage;
@@ -167,7 +166,7 @@ __device__ __forceinline__ bool multiply_stages(const Product &p, const Cta &c)
                 if (rows_deep(kOp)) {
                     left = kStep;
                     if (k < turn) {                      // the one after: the tail was loaded before all
-                        if (++at == S::kStages)
+                        if (++at == c.ring)
                             at = 0, its ^= 1;
                     } else if (k == turn) {
                         at = first, its = first_phase;
@@ -191,7 +190,7 @@ __device__ __forceinline__ bool multiply_stages(const Product &p, const Cta &c)
                         commit(done + half * 8);
                 }
                 __syncwarp();
-                if (++stage == S::kStages)
+                if (++stage == c.ring)
                     stage = 0, phase ^= 1;
             }
             if (half ^= 1; half == 0)
@@ -212,7 +211,7 @@ __device__ __forceinline__ bool clear_tails(const Product &p, const Cta &c)
     int stage = 0;
     uint32_t phase = 0;                                  // a bit for each stage
     for (int i = c.pair, g = 0; i < c.items; i += c.pairs) {
-        const Item it = item_of<kStep>(p, *c.tables, c.lane_tiles, i, g);
+        const Item it = item_of<kStep>(p, c.tables, c.split, c.lane_tiles, i, g);
         if (it.tail) {
             const int left = it.depth % kStep, at = stage;
             if (!wait(smem_addr(&c.bars->tail[at]), (phase >> at) & 1))
@@ -228,7 +227,7 @@ __device__ __forceinline__ bool clear_tails(const Product &p, const Cta &c)
             if (lane == 0)
                 arrive_release(full + at * 8);
         }
-        stage = (stage + it.k1 - it.k0) % S::kStages;
+        stage = (stage + it.k1 - it.k0) % c.ring;
     }
     return true;
 }
@@ -238,23 +237,15 @@ __global__ void __launch_bounds__(kThreads, 1)
 product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ Product p)
 {
     using S = Shape<kColumns>;
-    extern __shared__ uint8_t dynamic[];
-    __shared__ Barriers bars;
-    Cta c;
-    c.stages = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(dynamic) + 1023) & ~uintptr_t(1023));
-    Tables *tables = reinterpret_cast<Tables *>(c.stages + S::kStages * S::kStage);
-    c.tables = tables;
-    c.bars = &bars;
-    c.rank = cta_rank();
-    c.pair = blockIdx.x >> 1;
-    c.pairs = gridDim.x >> 1;
-    c.lane_tiles = parts_of(p.lanes, kLanes);
+    extern __shared__ __align__(1024) uint8_t dynamic[];
+    Cta c = cta_of(p, dynamic, p.ring * S::kStage);
+    Barriers &bars = *c.bars;
 
     const int warp = __shfl_sync(~0u, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     if (warp == kProducerWarp && lane == 0) {
         prefetch_map(&map_a);
         prefetch_map(&map_b);
-        for (int s = 0; s < S::kStages; ++s) {
+        for (int s = 0; s < c.ring; ++s) {
             barrier_init(smem_addr(&bars.full[s]), 2);               // counts in the first CTA, from both
             barrier_init(smem_addr(&bars.empty[s]), 1);
             barrier_init(smem_addr(&bars.tail[s]), 1);
@@ -270,10 +261,11 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if (warp == kTablesWarp)
-        fill_tables<kStep>(p, *tables, kColumns, c.lane_tiles, c.pairs);
+        fill_tables<kStep>(p, c.tables, kColumns, c.lane_tiles, c.pairs);
     join_pair();
     c.tmem = bars.tmem;
-    c.items = tables->first[p.groups] * tables->split;
+    c.split = c.tables.each[p.groups];
+    c.items = c.tables.first[p.groups] * c.split;
 
     bool fine = true;
     if (warp < kFirstEpilogueWarp) {
@@ -367,14 +359,10 @@ Operands operands(const gnmr_product *p)
     return {w, p->op == GNMR_PRODUCT_INPUT_GRAD ? dy : x};
 }
 
-template <int kColumns> constexpr int shared_bytes()
-{
-    return Shape<kColumns>::kStages * Shape<kColumns>::kStage + static_cast<int>(sizeof(Tables)) + 1024;
-}
-
 template <int kColumns, int kOp>
-cudaError_t launch(const gnmr_products *h, const Operands &o, const Product &p, cudaStream_t st, bool *mapped)
+cudaError_t launch(const gnmr_products *h, const Operands &o, Product p, cudaStream_t st, bool *mapped)
 {
+    p.ring = ring_of(p.groups, Shape<kColumns>::kStage, 0);
     CUtensorMap a, b;
     const CUtensorMapDataType type = p.bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
     *mapped = gnmr::tile_map(h, &a, o.a, type, a_along_lanes(kOp) ? kStep : 128, p.a_blocks ? 2 : 1) &&
@@ -384,7 +372,7 @@ cudaError_t launch(const gnmr_products *h, const Operands &o, const Product &p, 
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(2 * h->pairs);
     cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = shared_bytes<kColumns>();
+    cfg.dynamicSmemBytes = shared_bytes(p.groups, Shape<kColumns>::kStage, 0);
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -399,12 +387,11 @@ cudaError_t launch(const gnmr_products *h, const Operands &o, const Product &p, 
 
 template <int kColumns, int kOp> cudaError_t allow_shared()
 {
-    return cudaFuncSetAttribute(product_kernel<kColumns, kOp>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                shared_bytes<kColumns>());
+    return cudaFuncSetAttribute(product_kernel<kColumns, kOp>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSharedMost);
 }
 
 // The kernels, by op and whether a group has few rows.
-using Launch = cudaError_t (*)(const gnmr_products *, const Operands &, const Product &, cudaStream_t, bool *);
+using Launch = cudaError_t (*)(const gnmr_products *, const Operands &, Product, cudaStream_t, bool *);
 constexpr Launch kLaunch[4][2] = {
     {launch<256, GNMR_PRODUCT_FORWARD>, launch<64, GNMR_PRODUCT_FORWARD>},
     {launch<256, GNMR_PRODUCT_INPUT_GRAD>, launch<64, GNMR_PRODUCT_INPUT_GRAD>},

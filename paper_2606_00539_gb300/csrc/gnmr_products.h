@@ -60,7 +60,7 @@ bool tile_map(const gnmr_products *h, CUtensorMap *map, const Operand &o, CUtens
 cudaError_t copy_operand(const Operand &o, void *to, int sms, cudaStream_t st);
 
 // The 8-bit product; b may be widened.
-cudaError_t launch_codes(const gnmr_products *h, const Operands &o, const gnmr_tiles::Product &p, cudaStream_t st, bool *mapped);
+cudaError_t launch_codes(const gnmr_products *h, const Operands &o, gnmr_tiles::Product p, cudaStream_t st, bool *mapped);
 cudaError_t allow_codes_shared();
 
 }  // namespace gnmr

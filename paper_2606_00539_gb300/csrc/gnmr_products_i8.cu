@@ -53,9 +53,9 @@ constexpr int kAStage = 128 * kStep, kSlots = 4, kFirstA = 256, kTmem = 512;
 template <bool kWide> struct Shape {
     static constexpr int kColumns = kWide ? 128 : 64;
     static constexpr int kBRows = kColumns / 2, kBTile = kBRows * 128;
-    static constexpr int kStage = kAStage + (kWide ? 2 : 1) * kBTile, kStages = kWide ? 6 : 8;
-    static constexpr int kSlot = 2 * kBTile;           // B widened
-    static constexpr int kShared = kStages * kStage + (kWide ? 0 : kSlots * kSlot) + static_cast<int>(sizeof(Tables)) + 1024;
+    static constexpr int kStage = kAStage + (kWide ? 2 : 1) * kBTile;
+    static constexpr int kSlot = 2 * kBTile;           // B widened, before the stages
+    static constexpr int kWidened = kWide ? 0 : kSlots * kSlot;
     static_assert(2 * kColumns <= kFirstA && kFirstA + kSlots * kStep / 2 <= kTmem, "columns of tensor memory");
 };
 
@@ -63,12 +63,12 @@ template <bool kWide>
 __device__ __forceinline__ bool load_stages(const CUtensorMap &map_a, const CUtensorMap &map_b, const Product &p, const Cta &c)
 {
     using S = Shape<kWide>;
-    const uint32_t full = smem_addr(&c.bars->full[0]), empty = smem_addr(&c.bars->empty[0]), base = smem_addr(c.stages);
+    const uint32_t full = smem_addr(&c.bars->full[0]), empty = smem_addr(&c.bars->empty[0]), base = smem_addr(c.stages) + S::kWidened;
     const uint32_t own = in_cta(full, c.rank), full_b = in_cta(smem_addr(&c.bars->tail[0]), 0);
     int stage = 0;
     uint32_t phase = 1;
     for (int i = c.pair, g = 0; i < c.items; i += c.pairs) {
-        const Item it = item_of<kStep>(p, *c.tables, c.lane_tiles, i, g);
+        const Item it = item_of<kStep>(p, c.tables, c.split, c.lane_tiles, i, g);
         const int half = it.wide / 2;
         const int a_lane = it.lane0 + c.rank * 128, b_col = it.row0 + it.col0 + c.rank * half, za = p.a_by_group ? it.g : 0;
         for (int k = it.k0; k < it.k1; ++k) {
@@ -88,30 +88,38 @@ __device__ __forceinline__ bool load_stages(const CUtensorMap &map_a, const CUte
                 }
             }
             __syncwarp();
-            if (++stage == S::kStages)
+            if (++stage == c.ring)
                 stage = 0, phase ^= 1;
         }
     }
     return true;
 }
 
+// Two places on in a ring of n.
+__device__ __forceinline__ void two_on(int &at, uint32_t &phase, int n)
+{
+    if ((at += 2) >= n)
+        at -= n, phase ^= 1;
+}
+
 // A's tiles into tensor memory, by two teams of four warps that take the stages in turn.
 template <bool kWide>
 __device__ __forceinline__ bool widen_a(const Product &p, const Cta &c)
 {
-    constexpr int kStage = Shape<kWide>::kStage, kStages = Shape<kWide>::kStages;
+    constexpr int kStage = Shape<kWide>::kStage;
     const int warp = threadIdx.x / 32 - kFirstWidenWarp, lane = threadIdx.x & 31, quarter = warp & 3, team = warp >> 2;
     const uint32_t full = smem_addr(&c.bars->full[0]), empty = in_cta(smem_addr(&c.bars->empty[0]), c.rank);
     const uint32_t used = smem_addr(&c.bars->used[0]), ready = in_cta(smem_addr(&c.bars->ready[0]), 0);
     const int row = quarter * 32 + lane;
-    const uint8_t *raw = c.stages + row * 128;
-    int n = 0;                                         // stages so far
+    const uint8_t *raw = c.stages + Shape<kWide>::kWidened + row * 128;
+    int stage = team, slot = team;                     // every other stage, from the team's first
+    uint32_t phase = 0, slot_phase = 1;
+    int skip = team;                                   // stages until then
     for (int i = c.pair, g = 0; i < c.items; i += c.pairs) {
-        const Item it = item_of<kStep>(p, *c.tables, c.lane_tiles, i, g);
-        const int end = n + it.k1 - it.k0;
-        for (n += (n ^ team) & 1; n < end; n += 2) {
-            const int stage = n % kStages, slot = n % kSlots;
-            if (!wait(full + stage * 8, (n / kStages) & 1) || !wait(used + slot * 8, (n / kSlots + 1) & 1))
+        const Item it = item_of<kStep>(p, c.tables, c.split, c.lane_tiles, i, g);
+        int k = it.k0 + skip;
+        for (; k < it.k1; k += 2) {
+            if (!wait(full + stage * 8, phase) || !wait(used + slot * 8, slot_phase))
                 return false;
             fence_after();
 #pragma unroll
@@ -138,8 +146,10 @@ __device__ __forceinline__ bool widen_a(const Product &p, const Cta &c)
             __syncwarp();
             if (lane == 0)
                 arrive(ready + slot * 8);
+            two_on(stage, phase, c.ring);
+            two_on(slot, slot_phase, kSlots);
         }
-        n = end;
+        skip = k - it.k1;
     }
     return true;
 }
@@ -148,20 +158,21 @@ __device__ __forceinline__ bool widen_a(const Product &p, const Cta &c)
 __device__ __forceinline__ bool widen_b(const Product &p, const Cta &c)
 {
     using S = Shape<false>;
-    constexpr int kStage = S::kStage, kStages = S::kStages, kSlot = S::kSlot, kBTile = S::kBTile;
+    constexpr int kStage = S::kStage, kSlot = S::kSlot, kBTile = S::kBTile;
     const int lane = threadIdx.x & 31, turn = threadIdx.x / 32 - kFirstBWarp, chunk = lane & 7;
     const uint32_t full = smem_addr(&c.bars->full[0]), empty = in_cta(smem_addr(&c.bars->empty[0]), c.rank);
     const uint32_t used = smem_addr(&c.bars->used[0]), ready = in_cta(smem_addr(&c.bars->ready[0]), 0);
-    int n = 0;
+    int stage = turn, slot = turn, skip = turn;
+    uint32_t phase = 0, slot_phase = 1;
     for (int i = c.pair, g = 0; i < c.items; i += c.pairs) {
-        const Item it = item_of<kStep>(p, *c.tables, c.lane_tiles, i, g);
-        const int end = n + it.k1 - it.k0, half = it.wide / 2;
-        for (n += (n ^ turn) & 1; n < end; n += 2) {
-            const int stage = n % kStages, slot = n % kSlots;
-            if (!wait(full + stage * 8, (n / kStages) & 1) || !wait(used + slot * 8, (n / kSlots + 1) & 1))
+        const Item it = item_of<kStep>(p, c.tables, c.split, c.lane_tiles, i, g);
+        const int half = it.wide / 2;
+        int k = it.k0 + skip;
+        for (; k < it.k1; k += 2) {
+            if (!wait(full + stage * 8, phase) || !wait(used + slot * 8, slot_phase))
                 return false;
-            const uint8_t *raw = c.stages + stage * kStage + kAStage;
-            uint8_t *to = c.stages + kStages * kStage + slot * kSlot + (chunk >> 2) * kBTile;
+            const uint8_t *raw = c.stages + S::kWidened + stage * kStage + kAStage;
+            uint8_t *to = c.stages + slot * kSlot + (chunk >> 2) * kBTile;
 #pragma unroll 4
             for (int r = lane >> 3; r < half; r += 4) {
                 const uint4 codes = *reinterpret_cast<const uint4 *>(raw + r * 128 + ((chunk ^ (r & 7)) << 4));
@@ -176,8 +187,10 @@ __device__ __forceinline__ bool widen_b(const Product &p, const Cta &c)
                 arrive(empty + stage * 8);
                 arrive_release(ready + slot * 8);
             }
+            two_on(stage, phase, c.ring);
+            two_on(slot, slot_phase, kSlots);
         }
-        n = end;
+        skip = k - it.k1;
     }
     return true;
 }
@@ -189,11 +202,11 @@ __device__ __forceinline__ bool multiply_slots(const Product &p, const Cta &c)
     const uint32_t ready = smem_addr(&c.bars->ready[0]), used = smem_addr(&c.bars->used[0]);
     const uint32_t full_b = smem_addr(&c.bars->tail[0]), empty = smem_addr(&c.bars->empty[0]);
     const uint32_t done = smem_addr(&c.bars->done[0]), drained = smem_addr(&c.bars->drained[0]);
-    const uint64_t first_b = operand(smem_addr(c.stages) + (kWide ? kAStage : S::kStages * S::kStage), 16, 1024);
+    const uint64_t first_b = operand(smem_addr(c.stages) + (kWide ? kAStage : 0), 16, 1024);
     int slot = 0, stage = 0, half = 0;
     uint32_t phase = 0, stage_phase = 0, free_phase = 1;
     for (int i = c.pair, g = 0; i < c.items; i += c.pairs) {
-        const Item it = item_of<kStep>(p, *c.tables, c.lane_tiles, i, g);
+        const Item it = item_of<kStep>(p, c.tables, c.split, c.lane_tiles, i, g);
         const uint32_t idesc = shape(false, false, false, it.wide);
         for (int k = it.k0; k < it.k1;) {
             if (!wait(drained + half * 8, free_phase))
@@ -220,7 +233,7 @@ __device__ __forceinline__ bool multiply_slots(const Product &p, const Cta &c)
                 __syncwarp();
                 if (++slot == kSlots)
                     slot = 0, phase ^= 1;
-                if (++stage == S::kStages)
+                if (++stage == c.ring)
                     stage = 0, stage_phase ^= 1;
             }
             if (half ^= 1; half == 0)
@@ -235,23 +248,15 @@ __global__ void __launch_bounds__(kThreads, 1)
 codes_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ Product p)
 {
     using S = Shape<kWide>;
-    extern __shared__ uint8_t dynamic[];
-    __shared__ Barriers bars;
-    Cta c;
-    c.stages = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(dynamic) + 1023) & ~uintptr_t(1023));
-    Tables *tables = reinterpret_cast<Tables *>(c.stages + S::kStages * S::kStage + (kWide ? 0 : kSlots * S::kSlot));
-    c.tables = tables;
-    c.bars = &bars;
-    c.rank = cta_rank();
-    c.pair = blockIdx.x >> 1;
-    c.pairs = gridDim.x >> 1;
-    c.lane_tiles = parts_of(p.lanes, kLanes);
+    extern __shared__ __align__(1024) uint8_t dynamic[];
+    Cta c = cta_of(p, dynamic, p.ring * S::kStage + S::kWidened);
+    Barriers &bars = *c.bars;
 
     const int warp = __shfl_sync(~0u, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
     if (warp == kProducerWarp && lane == 0) {
         prefetch_map(&map_a);
         prefetch_map(&map_b);
-        for (int s = 0; s < S::kStages; ++s) {
+        for (int s = 0; s < c.ring; ++s) {
             barrier_init(smem_addr(&bars.full[s]), 1);
             barrier_init(smem_addr(&bars.empty[s]), kWidenWarps / 2 + 1);        // a team, and B's warp or multiplies
             barrier_init(smem_addr(&bars.tail[s]), 2);                           // B in 16 bits: in the first CTA, from both
@@ -271,10 +276,11 @@ codes_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if (warp == kTablesWarp)
-        fill_tables<kStep>(p, *tables, S::kColumns, c.lane_tiles, c.pairs);
+        fill_tables<kStep>(p, c.tables, S::kColumns, c.lane_tiles, c.pairs);
     join_pair();
     c.tmem = bars.tmem;
-    c.items = tables->first[p.groups] * tables->split;
+    c.split = c.tables.each[p.groups];
+    c.items = c.tables.first[p.groups] * c.split;
 
     bool fine = true;
     if (warp < kFirstEpilogueWarp) {
@@ -298,18 +304,20 @@ codes_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
 }
 
 template <bool kWide>
-cudaError_t launch(const gnmr_products *h, const Operands &o, const Product &p, cudaStream_t st, bool *mapped)
+cudaError_t launch(const gnmr_products *h, const Operands &o, Product p, cudaStream_t st, bool *mapped)
 {
+    using S = Shape<kWide>;
+    p.ring = ring_of(p.groups, S::kStage, S::kWidened);
     CUtensorMap a, b;
     *mapped = gnmr::tile_map(h, &a, o.a, CU_TENSOR_MAP_DATA_TYPE_UINT8, 128, 1) &&
-              (kWide ? gnmr::tile_map(h, &b, o.b, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, Shape<kWide>::kBRows, 2)
-                     : gnmr::tile_map(h, &b, o.b, CU_TENSOR_MAP_DATA_TYPE_UINT8, Shape<kWide>::kBRows, 1));
+              (kWide ? gnmr::tile_map(h, &b, o.b, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, S::kBRows, 2)
+                     : gnmr::tile_map(h, &b, o.b, CU_TENSOR_MAP_DATA_TYPE_UINT8, S::kBRows, 1));
     if (!*mapped)
         return cudaSuccess;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(2 * h->pairs);
     cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = Shape<kWide>::kShared;
+    cfg.dynamicSmemBytes = shared_bytes(p.groups, S::kStage, S::kWidened);
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeClusterDimension;
@@ -413,11 +421,11 @@ cudaError_t copy_operand(const Operand &o, void *to, int sms, cudaStream_t st)
 
 cudaError_t allow_codes_shared()
 {
-    const cudaError_t e = cudaFuncSetAttribute(codes_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<false>::kShared);
-    return e != cudaSuccess ? e : cudaFuncSetAttribute(codes_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<true>::kShared);
+    const cudaError_t e = cudaFuncSetAttribute(codes_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSharedMost);
+    return e != cudaSuccess ? e : cudaFuncSetAttribute(codes_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSharedMost);
 }
 
-cudaError_t launch_codes(const gnmr_products *h, const Operands &o, const Product &p, cudaStream_t st, bool *mapped)
+cudaError_t launch_codes(const gnmr_products *h, const Operands &o, Product p, cudaStream_t st, bool *mapped)
 {
     return o.b.read_bytes == 2 ? launch<true>(h, o, p, st, mapped) : launch<false>(h, o, p, st, mapped);
 }

@@ -36,6 +36,7 @@ struct Product {
     int granule;                       // a tile's columns are multiples of it: 32 or 128
     int bf16;
     int piece;                         // contraction steps of a piece
+    int ring;                          // stages of operands in shared memory
     void *out;
     int out_type;
     int pairs_aligned;                 // two outputs of a row may be stored as one
@@ -49,12 +50,14 @@ struct Product {
 
 // ---- work: tiles of every group, and their parts --------------------------------
 
+// In shared memory, [groups + 1] each, after the barriers.
 struct Tables {
-    int first[kMaxGroups + 1];         // tiles before group g; in the end all of them
-    int row[kMaxGroups + 1];           // first row of group g; in the end the last group's end
-    uint16_t each[kMaxGroups];         // columns of group g's tiles
-    int split;                         // parts of every tile's contraction
+    int *first;                        // tiles before group g; in the end all of them
+    int *row;                          // first row of group g; in the end the last group's end
+    uint16_t *each;                    // columns of group g's tiles; in the end the parts of every tile's contraction
 };
+
+__host__ __device__ constexpr int table_bytes(int groups) { return (groups + 1) * (4 + 4 + 2); }
 
 struct Item {
     int g, lane0, col0, cols;          // the tile: the pair's lanes, and its columns
@@ -69,7 +72,7 @@ __device__ __forceinline__ int parts_of(int n, int each) { return (n + each - 1)
 
 // Filled by one warp; kStep: contraction steps of a stage.  Offsets are clamped to [0, rows] and made not decreasing.
 template <int kStep>
-__device__ __forceinline__ void fill_tables(const Product &p, Tables &t, int most, int lane_tiles, int pairs)
+__device__ __forceinline__ void fill_tables(const Product &p, const Tables &t, int most, int lane_tiles, int pairs)
 {
     const int lane = threadIdx.x & 31;
     int carry = 0;
@@ -125,18 +128,18 @@ __device__ __forceinline__ void fill_tables(const Product &p, Tables &t, int mos
     }
     if (lane == 0) {
         t.first[p.groups] = tiles;
-        t.split = best;
+        t.each[p.groups] = static_cast<uint16_t>(best);
     }
 }
 
 // Item i of the call, by a whole warp that comes with growing i.  g: the group of the one
 // before, 0 at first.
 template <int kStep>
-__device__ __forceinline__ Item item_of(const Product &p, const Tables &t, int lane_tiles, int i, int &g)
+__device__ __forceinline__ Item item_of(const Product &p, const Tables &t, int split, int lane_tiles, int i, int &g)
 {
     Item it;
-    it.tile = t.split == 1 ? i : i / t.split;
-    it.part = i - it.tile * t.split;
+    it.tile = split == 1 ? i : i / split;
+    it.part = i - it.tile * split;
     for (;;) {                                       // the last group that begins at or before the tile
         const int next = g + 1 + (threadIdx.x & 31);
         const unsigned past = __ballot_sync(~0u, next >= p.groups || t.first[next] > it.tile);
@@ -162,9 +165,9 @@ __device__ __forceinline__ Item item_of(const Product &p, const Tables &t, int l
     const int stages = parts_of(it.depth, kStep);
     it.k0 = 0;
     it.k1 = stages;
-    if (t.split > 1) {
-        it.k0 = stages * it.part / t.split;
-        it.k1 = stages * (it.part + 1) / t.split;
+    if (split > 1) {
+        it.k0 = stages * it.part / split;
+        it.k1 = stages * (it.part + 1) / split;
     }
     it.tail = !p.depth && it.depth % kStep && it.k0 < it.k1 && it.k1 == stages;
     return it;
@@ -172,9 +175,11 @@ __device__ __forceinline__ Item item_of(const Product &p, const Tables &t, int l
 
 // ---- a CTA ------------------------------------------------------------------------
 
+constexpr int kMostStages = 11;
+
 struct Barriers {
-    uint64_t full[10], empty[10];      // stages of operands
-    uint64_t tail[10];                 // a stage that the tail warp looks at first
+    uint64_t full[kMostStages], empty[kMostStages];      // stages of operands
+    uint64_t tail[kMostStages];        // a stage that the tail warp looks at first
     uint64_t ready[4], used[4];        // operands widened from 8 bits
     uint64_t done[2], drained[2];      // halves of tensor memory; `drained` counts in the first CTA
     uint32_t tmem;
@@ -182,12 +187,45 @@ struct Barriers {
 
 // What the roles of a CTA share.
 struct Cta {
-    uint8_t *stages;                   // dynamic shared memory, from a multiple of 1,024
-    const Tables *tables;
+    uint8_t *stages;                   // operands, in dynamic shared memory
+    int ring;                          // how many stages there are
     Barriers *bars;
+    Tables tables;
     uint32_t rank, tmem;
-    int pair, pairs, lane_tiles, items;
+    int pair, pairs, lane_tiles, items, split;
 };
+
+// Dynamic shared memory: `bytes` of operands, whole kilobytes, then barriers and tables.
+// None is static, so that it begins at a multiple of 1,024, as swizzled tiles have to.
+__device__ __forceinline__ Cta cta_of(const Product &p, uint8_t *shared, int bytes)
+{
+    Cta c;
+    c.stages = shared;
+    c.ring = p.ring;
+    c.bars = reinterpret_cast<Barriers *>(shared + bytes);
+    c.tables.first = reinterpret_cast<int *>(c.bars + 1);
+    c.tables.row = c.tables.first + p.groups + 1;
+    c.tables.each = reinterpret_cast<uint16_t *>(c.tables.row + p.groups + 1);
+    c.rank = cta_rank();
+    c.pair = blockIdx.x >> 1;
+    c.pairs = gridDim.x >> 1;
+    c.lane_tiles = parts_of(p.lanes, kLanes);
+    return c;
+}
+
+// As many stages as fit beside `more` bytes of operands, barriers and tables.
+constexpr int kSharedMost = 227 << 10;
+
+constexpr int ring_of(int groups, int stage, int more)
+{
+    const int n = (kSharedMost - more - static_cast<int>(sizeof(Barriers)) - table_bytes(groups)) / stage;
+    return n < kMostStages ? n : kMostStages;
+}
+
+constexpr int shared_bytes(int groups, int stage, int more)
+{
+    return ring_of(groups, stage, more) * stage + more + static_cast<int>(sizeof(Barriers)) + table_bytes(groups);
+}
 
 // ---- outputs --------------------------------------------------------------------
 
@@ -389,7 +427,7 @@ __device__ __forceinline__ bool join_parts(const Product &p, const Cta &c, const
                                            int cols, int col, int warp)
 {
     constexpr int kPieces = kColumns / 32;               // of 16 columns
-    const int lane = threadIdx.x & 31, split = c.tables->split;
+    const int lane = threadIdx.x & 31, split = c.split;
     uint32_t *part = reinterpret_cast<uint32_t *>(p.parts) + int64_t(it.tile) * split * kPartFloats +
                      c.rank * (kPartFloats / 2) + (warp & 3) * 32 + lane;
 #pragma unroll
@@ -438,7 +476,7 @@ __device__ __forceinline__ bool write_outputs(const Product &p, const Cta &c)
     int half = 0;
     uint32_t phase = 0;
     for (int i = c.pair, g = 0; i < c.items; i += c.pairs) {
-        const Item it = item_of<kStep>(p, *c.tables, c.lane_tiles, i, g);
+        const Item it = item_of<kStep>(p, c.tables, c.split, c.lane_tiles, i, g);
         const int span = it.wide / 2;                          // columns of this warp
         const int at = it.lane0 + c.rank * 128 + quarter * 32 + lane, col = side * span;
         if (p.add)
@@ -482,7 +520,7 @@ __device__ __forceinline__ bool write_outputs(const Product &p, const Cta &c)
             if (half ^= 1; half == 0)
                 phase ^= 1;
         }
-        if (c.tables->split > 1 && !join_parts<kColumns, kCodes>(p, c, it, acc, min(span, it.cols - col), col, warp))
+        if (c.split > 1 && !join_parts<kColumns, kCodes>(p, c, it, acc, min(span, it.cols - col), col, warp))
             continue;
         if (p.add && it.depth == 0)
             continue;                                    // nothing to add
