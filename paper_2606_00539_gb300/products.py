@@ -9,29 +9,27 @@ import ctypes
 from . import _native as N
 
 
-def _torch():
-    import torch
-    return torch
-
-
+torch = None                                       # loaded with the first ExpertProducts, as the monitor does
 _DTYPES: dict = {}                                 # torch type -> gnmr_dtype
+_NAMED: dict = {}                                  # name -> torch type
 
 
-def _dtypes():
-    torch = _torch()
+def _load_torch():
+    global torch
+    import torch as module
+    torch = module
     _DTYPES.update({torch.bfloat16: N.GNMR_DTYPE_BF16, torch.float16: N.GNMR_DTYPE_F16,
                     torch.float32: N.GNMR_DTYPE_F32})
+    _NAMED.update({"bf16": torch.bfloat16, "bfloat16": torch.bfloat16, "f16": torch.float16,
+                   "float16": torch.float16, "f32": torch.float32, "float32": torch.float32})
 
 
 def _named_dtype(name):
-    torch = _torch()
-    named = {"bf16": torch.bfloat16, "bfloat16": torch.bfloat16, "f16": torch.float16, "float16": torch.float16,
-             "f32": torch.float32, "float32": torch.float32}
-    if name in named:
-        return named[name]
-    if name in named.values():
+    if name in _NAMED:
+        return _NAMED[name]
+    if name in _DTYPES:
         return name
-    raise ValueError(f"out_dtype must be one of {sorted(named)} or the torch type, got {name!r}")
+    raise ValueError(f"out_dtype must be one of {sorted(_NAMED)} or the torch type, got {name!r}")
 
 
 class ExpertProducts:
@@ -54,12 +52,14 @@ class ExpertProducts:
     def __init__(self, device=0):
         self._h = None
         self.device_index = int(device.index if hasattr(device, "index") else device)
+        if torch is None:
+            _load_torch()
         self._h = N.gnmr_products_create(self.device_index)
         self._run = N.load().gnmr_products_run
-        torch = _torch()
         self._device = torch.device("cuda", self.device_index)
         self._sixteen = (torch.bfloat16, torch.float16)
-        _dtypes()
+        self._any = tuple(_DTYPES)
+        self._raw_stream = torch._C._cuda_getCurrentRawStream
 
     # -- lifetime -----------------------------------------------------------
     def close(self) -> None:
@@ -80,31 +80,38 @@ class ExpertProducts:
             pass
 
     # -- argument checks ------------------------------------------------------
-    def _tensor(self, t, name, dims, dtypes):
-        torch = _torch()
+    # A small product takes the GPU under 10 us: these checks are written to cost the host
+    # no more than that.
+    def _refuse(self, t, name, dims, dtypes):
         if not isinstance(t, torch.Tensor) or t.get_device() != self.device_index:
             raise ValueError(f"{name} must be a CUDA tensor on device {self.device_index}")
         if t.dtype not in dtypes:
             raise ValueError(f"{name} must be {' or '.join(str(d) for d in dtypes)}, got {t.dtype}")
-        if t.dim() not in dims:
-            raise ValueError(f"{name} must have {' or '.join(str(d) for d in dims)} dimensions, got {t.dim()}")
+        raise ValueError(f"{name} must have {' or '.join(str(d) for d in dims)} dimensions, got {t.dim()}")
+
+    def _tensor(self, t, name, dims, dtypes):
+        if not isinstance(t, torch.Tensor) or t.get_device() != self.device_index or t.dtype not in dtypes or \
+                t.dim() not in dims:
+            self._refuse(t, name, dims, dtypes)
 
     def _matrix(self, t, name, dims, dtypes):
         """(groups, rows, columns, row stride, group stride) of a tensor of contiguous rows."""
-        self._tensor(t, name, dims, dtypes)
+        if not isinstance(t, torch.Tensor) or t.get_device() != self.device_index or t.dtype not in dtypes:
+            self._refuse(t, name, dims, dtypes)
         shape, stride = t.shape, t.stride()
-        rows, cols = shape[-2], shape[-1]
-        if cols > 1 and stride[-1] != 1:
+        if len(shape) not in dims:
+            self._refuse(t, name, dims, dtypes)
+        *lead, rows, cols = shape
+        if stride[-1] != 1 and cols > 1:
             raise ValueError(f"{name} must have contiguous rows")
         # a single row, or group, has no stride of its own, and torch may give it any
         row = stride[-2] if rows > 1 else max(stride[-2], cols)
-        if len(shape) == 2:
+        if not lead:
             return 1, rows, cols, row, 0
-        return shape[0], rows, cols, row, stride[0] if shape[0] > 1 else 0
+        return lead[0], rows, cols, row, stride[0] if lead[0] > 1 else 0
 
     def _grouping(self, groups, offsets, mask):
         """Device pointers of offsets and mask, and the mask's stride."""
-        torch = _torch()
         at, bits, step = None, None, 1
         if offsets is not None:
             self._tensor(offsets, "offsets", (1,), (torch.int64,))
@@ -121,14 +128,13 @@ class ExpertProducts:
         return at, bits, step
 
     def _new(self, shape, dtype, stream):
-        torch = _torch()
         if stream is None:
             return torch.empty(shape, dtype=dtype, device=self._device)
         with torch.cuda.stream(stream):
             return torch.empty(shape, dtype=dtype, device=self._device)
 
     def _stream(self, stream):
-        return (_torch().cuda.current_stream(self.device_index) if stream is None else stream).cuda_stream
+        return self._raw_stream(self.device_index) if stream is None else stream.cuda_stream
 
     def _out(self, out, rows, width, dtypes, stream):
         """(out, its row stride): the tensor given, checked, or a new one of the first type."""
@@ -148,7 +154,7 @@ class ExpertProducts:
             # operands that cannot be read in place: room for their copies, on the same stream
             need = N.gnmr_products_scratch_bytes(p)
             if need > p.scratch_bytes:
-                scratch = self._new(need, _torch().uint8, stream)
+                scratch = self._new(need, torch.uint8, stream)
                 p.d_scratch, p.scratch_bytes = scratch.data_ptr(), need
                 status = self._run(self._h, ctypes.addressof(p), handle)
         if status:
@@ -196,7 +202,7 @@ class ExpertProducts:
         _, x_rows, n_in, x_step, _ = self._matrix(x, "x", (2,), (dtype,))
         if x_rows != rows:
             raise ValueError("dy and x must have the same number of rows")
-        groups, high, wide, row, group = self._matrix(out, "out", (2, 3), (dtype, _torch().float32))
+        groups, high, wide, row, group = self._matrix(out, "out", (2, 3), (dtype, torch.float32))
         if (high, wide) != (n_out, n_in):
             raise ValueError(f"out must be [{n_out}, {n_in}] for each group, got [{high}, {wide}]")
         at, bits, each = self._grouping(groups, offsets, mask)
@@ -207,8 +213,7 @@ class ExpertProducts:
 
     # -- 8-bit products -------------------------------------------------------
     def _quantize(self, x, columns, stream):
-        torch = _torch()
-        groups, rows, cols, row, group = self._matrix(x, "x", (2, 3), tuple(_DTYPES))
+        groups, rows, cols, row, group = self._matrix(x, "x", (2, 3), self._any)
         high, wide = (cols, rows) if columns else (rows, cols)
         held = (wide + 15) // 16 * 16              # rows of codes start at multiples of 16 bytes
         lead = x.shape[:-2]
@@ -240,7 +245,6 @@ class ExpertProducts:
                    stream=None):
         """y[r] = x_scale[r] * w_scale_g * (Wq_g xq[r]) on 8-bit codes; the sum is an exact
         integer (n_in up to 131,071), rounded once to out's type."""
-        torch = _torch()
         groups, n_out, n_in, row, group = self._matrix(wq, "wq", (2, 3), (torch.int8,))
         _, rows, cols, step, _ = self._matrix(xq, "xq", (2,), (torch.int8,))
         if cols != n_in:
@@ -250,7 +254,7 @@ class ExpertProducts:
             if t.numel() != n or not t.is_contiguous():
                 raise ValueError(f"{name} must hold {n} contiguous entries")
         at, bits, each = self._grouping(groups, offsets, mask)
-        out, across = self._out(out, rows, n_out, (_named_dtype(out_dtype),) if out is None else tuple(_DTYPES), stream)
+        out, across = self._out(out, rows, n_out, (_named_dtype(out_dtype),) if out is None else self._any, stream)
         self._enqueue(N.gnmr_product(N.GNMR_PRODUCT_FORWARD_I8, groups, rows, n_out, n_in, 0, _DTYPES[out.dtype], at,
                                      bits, each, xq.data_ptr(), step, None, 0, wq.data_ptr(), row, group,
                                      x_scale.data_ptr(), w_scale.data_ptr(), out.data_ptr(), across), stream)
@@ -258,8 +262,6 @@ class ExpertProducts:
 
 
 def _expert_linear_function():
-    torch = _torch()
-
     class ExpertLinear(torch.autograd.Function):
         @staticmethod
         def forward(ctx, x, w, products, offsets, mask, grad, codes):

@@ -142,6 +142,29 @@ def test_strides_and_views(products):
             check(dw[e], D.T @ X, D.abs().T @ X.abs(), counts[e], "f32")
 
 
+@pytest.mark.parametrize("groups", [270, 2048])
+def test_many_groups(products, groups):
+    """Tables that leave room for fewer stages, and most groups without rows."""
+    g, t = gen(groups), torch.bfloat16
+    counts = [0] * groups
+    for e, c in ((0, 3), (7, 70), (groups // 2, 1), (groups - 2, 300), (groups - 1, 33)):
+        counts[e] = c
+    R, n, k = sum(counts), 40, 72
+    off = offsets_of(counts)
+    x, dy, w = normal(g, R, k, dtype=t), normal(g, R, n, dtype=t), normal(g, groups, n, k, dtype=t)
+    y, dx = products.forward(x, w, off), products.input_grad(dy, w, off)
+    dw = products.weight_grad(dy, x, off, out=torch.full((groups, n, k), 7.0, device="cuda"))
+    (xq, xs), (wq, ws) = products.quantize_rows(x), products.quantize_rows(w)
+    low = products.forward_i8(xq, xs, wq, ws, off, out_dtype="f32")
+    for e, at in spans(counts):
+        X, D, W = x[at].double(), dy[at].double(), w[e].double()
+        check(y[at], X @ W.T, X.abs() @ W.abs().T, k, "bf16")
+        check(dx[at], D @ W, D.abs() @ W.abs(), n, "bf16")
+        check(dw[e], D.T @ X, D.abs().T @ X.abs(), counts[e], "f32")
+        want = (xq[at].double() @ wq[e].double().T) * xs[at].double()[:, None] * ws[e].double()
+        assert ((low[at].double() - want).abs() <= want.abs() * 2.0 ** -21).all()
+
+
 def test_groups_may_share_a_weight(products):
     g = gen(6)
     x, w = normal(g, 90, 64, dtype=torch.float16), normal(g, 72, 64, dtype=torch.float16)
