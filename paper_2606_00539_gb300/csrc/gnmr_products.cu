@@ -323,14 +323,18 @@ gnmr_status check(const gnmr_product *p)
         return fail(GNMR_ERR_INVALID_ARG, "products: NULL operand");
     const int64_t wide_out = p->op == GNMR_PRODUCT_FORWARD || codes ? p->n_out : p->n_in;
     const int64_t far = int64_t(1) << 36;                // strides stay within what a tensor map takes
-    if ((x && p->x_stride < p->n_in) || (dy && p->dy_stride < p->n_out) ||
-        (w && (p->w_stride < p->n_in || p->w_group_stride < 0)) || p->out_stride < wide_out ||
-        (wgrad && p->groups > 1 && p->out_group_stride < (p->n_out - 1) * p->out_stride + p->n_in) ||
-        (p->d_mask && p->groups > 1 && p->mask_stride < 1))
-        return fail(GNMR_ERR_LAYOUT, "products: a stride below what it strides over");
     if ((x && p->x_stride > far) || (dy && p->dy_stride > far) || (w && (p->w_stride > far || p->w_group_stride > far)) ||
         p->out_stride > far || (wgrad && p->out_group_stride > far))
         return fail(GNMR_ERR_LAYOUT, "products: a stride above 2^36 elements");
+    const __int128 group = static_cast<__int128>(p->n_out - 1) * p->out_stride + p->n_in;
+    if ((x && p->x_stride < p->n_in) || (dy && p->dy_stride < p->n_out) ||
+        (w && (p->w_stride < p->n_in || p->w_group_stride < 0)) || p->out_stride < wide_out ||
+        (wgrad && p->groups > 1 && p->out_group_stride < group) || (p->d_mask && p->groups > 1 && p->mask_stride < 1))
+        return fail(GNMR_ERR_LAYOUT, "products: a stride below what it strides over");
+    // operands that could not be copied, whatever memory there is
+    const __int128 most_rows = std::max<int64_t>(p->rows, w ? int64_t(p->groups) * p->n_out : 0);
+    if (most_rows * std::max(p->n_out, p->n_in) > (int64_t(1) << 56))
+        return fail(GNMR_ERR_LAYOUT, "products: operands too large");
     const size_t eb = codes ? 1 : 2, ob = p->out_dtype == GNMR_DTYPE_F32 ? 4 : 2;
     if ((x && misaligned(p->d_x, eb)) || (dy && misaligned(p->d_dy, eb)) || (w && misaligned(p->d_w, eb)) ||
         misaligned(p->d_out, ob) || misaligned(p->d_offsets, 8) ||

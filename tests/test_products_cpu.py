@@ -81,6 +81,9 @@ WG, I8 = N.GNMR_PRODUCT_WEIGHT_GRAD, N.GNMR_PRODUCT_FORWARD_I8
     (LAYOUT, dict(out_stride=15)), (LAYOUT, dict(op=N.GNMR_PRODUCT_INPUT_GRAD, dy_stride=15)),
     (LAYOUT, dict(op=WG, out_group_stride=16 * 15 + 7)), (LAYOUT, dict(d_x=4097)), (LAYOUT, dict(d_out=4097)),
     (LAYOUT, dict(d_offsets=4100)), (LAYOUT, dict(out_dtype=N.GNMR_DTYPE_F32, d_out=4098)),
+    (LAYOUT, dict(x_stride=(1 << 36) + 1)), (LAYOUT, dict(op=WG, out_stride=(1 << 62), out_group_stride=(1 << 62))),
+    (LAYOUT, dict(op=WG, n_out=1 << 29, dy_stride=1 << 29, out_stride=1 << 36, out_group_stride=1 << 36)),
+    (LAYOUT, dict(n_out=1 << 29, n_in=1 << 29, groups=2048, x_stride=1 << 29, w_stride=1 << 29, out_stride=1 << 29)),
     (LAYOUT, dict(d_mask=4096, mask_stride=0)), (LAYOUT, dict(op=I8, d_x_scale=4098)),
 ])
 def test_refusals(status, over):
