@@ -61,6 +61,7 @@ template <int kColumns> struct Shape {
     static constexpr int kBox = kColumns / 2;
     static constexpr int kStage = kAStage + kBox * 128;
     static constexpr int kTmem = 2 * kColumns;
+    static constexpr int kJoin = kColumns / 64;
 };
 
 // The stage with the tail is loaded first and multiplied fourth (or last): clearing it
@@ -261,7 +262,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if (warp == kTablesWarp)
-        fill_tables<kStep>(p, c.tables, kColumns, c.lane_tiles, c.pairs);
+        fill_tables<kStep, S::kJoin>(p, c.tables, kColumns, c.lane_tiles, c.pairs);
     join_pair();
     c.tmem = bars.tmem;
     c.split = c.tables.each[p.groups];

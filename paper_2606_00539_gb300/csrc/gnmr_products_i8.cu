@@ -276,7 +276,7 @@ codes_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if (warp == kTablesWarp)
-        fill_tables<kStep>(p, c.tables, S::kColumns, c.lane_tiles, c.pairs);
+        fill_tables<kStep, kWide ? 2 : 1>(p, c.tables, S::kColumns, c.lane_tiles, c.pairs);
     join_pair();
     c.tmem = bars.tmem;
     c.split = c.tables.each[p.groups];

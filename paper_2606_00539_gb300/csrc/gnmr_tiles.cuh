@@ -70,8 +70,9 @@ struct Item {
 
 __device__ __forceinline__ int parts_of(int n, int each) { return (n + each - 1) / each; }
 
-// Filled by one warp; kStep: contraction steps of a stage.  Offsets are clamped to [0, rows] and made not decreasing.
-template <int kStep>
+// Filled by one warp; kStep: contraction steps of a stage; kJoin: stages that reading one
+// part of a tile back takes as long as.  Offsets are clamped to [0, rows] and made not decreasing.
+template <int kStep, int kJoin>
 __device__ __forceinline__ void fill_tables(const Product &p, const Tables &t, int most, int lane_tiles, int pairs)
 {
     const int lane = threadIdx.x & 31;
@@ -130,13 +131,14 @@ __device__ __forceinline__ void fill_tables(const Product &p, const Tables &t, i
             t.first[g] = tiles + sum - n;
         tiles += __shfl_sync(~0u, sum, 31);
     }
-    // Few tiles: the number of parts that takes the fewest rounds of stages, a
-    // part costing about six stages more for its beginning and its joining.
+    // Few tiles: the number of parts that takes the fewest stages, those included that
+    // beginning parts (six) and reading them back (kJoin each) take as long as.  With reading
+    // left out, 50,000 rows into a gradient of 136 x 200 took 32 parts and 70 us.
     int best = 1;
     if (tiles > 0 && tiles < pairs) {
         const int stages = parts_of(__reduce_max_sync(~0u, deepest), kStep), parts = lane + 1;
         const bool fits = parts == 1 || (tiles * parts <= min(2 * pairs, kMaxParts) && 2 * parts <= stages);
-        const int cost = fits ? parts_of(tiles * parts, pairs) * (parts_of(stages, parts) + (parts > 1 ? 6 : 0)) : INT32_MAX;
+        const int cost = fits ? parts_of(tiles * parts, pairs) * parts_of(stages, parts) + (parts > 1 ? 6 + kJoin * parts : 0) : INT32_MAX;
         const int least = __reduce_min_sync(~0u, cost);
         best = __ffs(__ballot_sync(~0u, cost == least));
     }
