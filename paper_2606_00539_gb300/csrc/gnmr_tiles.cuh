@@ -297,7 +297,10 @@ __device__ __forceinline__ void finish(const Product &p, const Item &it, uint32_
     char *out = static_cast<char *>(p.out) + (p.cols ? it.g * p.out_group * kBytes : 0) + row * step + int64_t(lane) * kBytes;
     const int left = it.cols - col, odd = lane & 1;
     const bool mine = lane < p.lanes;
-    const bool whole = (lane | 31) < p.lanes && (kBytes == 4 || (p.pairs_aligned && !p.add));
+    // every lane there, and 16 columns' offsets that one multiplication each gives (a chain of
+    // additions held up stores)
+    const bool whole = (lane | 31) < p.lanes && (kBytes == 4 || (p.pairs_aligned && !p.add)) && step < (int64_t(1) << 28);
+    const unsigned near = static_cast<unsigned>(step);
     const unsigned which = odd ? 0x3276 : 0x5410;
     float by_lane = 0.0f;
     const float *by_col = nullptr;
@@ -324,22 +327,26 @@ __device__ __forceinline__ void finish(const Product &p, const Item &it, uint32_
             if (kBytes == 4) {
                 if (p.add) {
                     float old[16];
-                    const char *from = out;
 #pragma unroll
-                    for (int j = 0; j < 16; ++j, from += step)
-                        old[j] = *reinterpret_cast<const float *>(from);
+                    for (int j = 0; j < 16; ++j)
+                        old[j] = *reinterpret_cast<const float *>(out + j * near);
 #pragma unroll
                     for (int j = 0; j < 16; ++j)
                         v[j] += old[j];
                 }
 #pragma unroll
-                for (int j = 0; j < 16; ++j, out += step)
-                    *reinterpret_cast<float *>(out) = v[j];
+                for (int j = 0; j < 16; ++j)
+                    *reinterpret_cast<float *>(out + j * near) = v[j];
             } else {
+                unsigned w[8];
 #pragma unroll
-                for (int j = 0; j < 16; j += 2, out += 2 * step)
-                    *reinterpret_cast<unsigned *>(out) = exchange<kOut>(v[j], v[j + 1], which);
+                for (int j = 0; j < 8; ++j)
+                    w[j] = exchange<kOut>(v[2 * j], v[2 * j + 1], which);
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    *reinterpret_cast<unsigned *>(out + 2 * j * near) = w[j];
             }
+            out += 16 * step;
             continue;
         }
         if (whole && kBytes == 2)                        // back to this lane's own place in the first column
