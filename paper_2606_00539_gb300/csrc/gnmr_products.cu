@@ -46,13 +46,21 @@ using gnmr::Operands;
 
 constexpr int kStep = 64;                              // contraction steps of a stage: 128-byte rows of 16 bits
 constexpr int kProducerWarp = 0, kMultiplyWarp = 1, kTailWarp = 2, kTablesWarp = 3;
-constexpr int kThreads = 32 * (kFirstEpilogueWarp + kEpilogueWarps);
-// The epilogue's warpgroups hold 128 sums a thread: 216 registers there and 72 in the
-// others' warpgroup, together the 168 a thread that the block is launched with.
-constexpr int kControlRegisters = 72, kEpilogueRegisters = 216;
-static_assert(128 * kControlRegisters + 256 * kEpilogueRegisters <= kThreads * 168, "registers of the launch");
 constexpr int kAStage = 128 * 128;                     // bytes of A's tile in one CTA
 constexpr int kBlock = 64 * 128;                       // bytes of a tile of 64 lanes or columns lying along rows
+
+// The epilogue's warps and the registers that the warpgroups share out between them, out of what the
+// block is launched with.  A weight gradient's contraction is short, so that it is bound by its
+// epilogue: 16 warps of 64 columns each (12288 rows, 64 fp32 gradients of 1408 x 2048: 8 warps 156 us,
+// 16 141); the others 8 of 128, with which 16 made no difference.
+template <int kOp> struct Roles {
+    static constexpr int kSides = kOp == GNMR_PRODUCT_WEIGHT_GRAD ? 4 : 2;
+    static constexpr int kThreads = 32 * (kFirstEpilogueWarp + 4 * kSides);
+    static constexpr int kLaunchRegisters = kSides == 4 ? 96 : 168;
+    static constexpr int kControlRegisters = kSides == 4 ? 64 : 72, kEpilogueRegisters = kSides == 4 ? 104 : 216;
+    static_assert(128 * kControlRegisters + 128 * kSides * kEpilogueRegisters <= kThreads * kLaunchRegisters &&
+                      kThreads * kLaunchRegisters <= 65536, "registers of the launch");
+};
 
 // kColumns columns at most; a CTA loads half of B's tile, as kBox rows in one load whatever
 // there are (each load costs its issuing thread about 100 of the 512 cycles that a stage's
@@ -234,7 +242,7 @@ __device__ __forceinline__ bool clear_tails(const Product &p, const Cta &c)
 }
 
 template <int kColumns, int kOp>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(Roles<kOp>::kThreads, 1)
 product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ Product p)
 {
     using S = Shape<kColumns>;
@@ -251,7 +259,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             barrier_init(smem_addr(&bars.empty[s]), 1);
             barrier_init(smem_addr(&bars.tail[s]), 1);
         }
-        init_epilogue_barriers(bars);
+        init_epilogue_barriers(bars, 4 * Roles<kOp>::kSides);
         barrier_init_fence();
     }
     if (warp == kMultiplyWarp)
@@ -270,7 +278,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
 
     bool fine = true;
     if (warp < kFirstEpilogueWarp) {
-        fewer_registers<kControlRegisters>();
+        fewer_registers<Roles<kOp>::kControlRegisters>();
         if (warp == kProducerWarp)
             fine = load_stages<kColumns, kOp>(map_a, map_b, p, c);
         else if (warp == kMultiplyWarp && c.rank == 0)
@@ -278,8 +286,8 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
         else if (warp == kTailWarp && rows_deep(kOp))
             fine = clear_tails<kColumns>(p, c);
     } else {
-        more_registers<kEpilogueRegisters>();
-        fine = write_outputs<kColumns, false, kStep>(p, c);
+        more_registers<Roles<kOp>::kEpilogueRegisters>();
+        fine = write_outputs<kColumns, Roles<kOp>::kSides, false, kStep>(p, c);
     }
     finish_pair(fine, p.gave_up);
     if (warp == kMultiplyWarp)
@@ -376,7 +384,7 @@ cudaError_t launch(const gnmr_products *h, const Operands &o, Product p, cudaStr
         return cudaSuccess;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(2 * h->pairs);
-    cfg.blockDim = dim3(kThreads);
+    cfg.blockDim = dim3(Roles<kOp>::kThreads);
     cfg.dynamicSmemBytes = shared_bytes(p.groups, Shape<kColumns>::kStage, 0);
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
@@ -466,7 +474,7 @@ gnmr_status gnmr_products_create(int32_t device, gnmr_products **out)
     cudaGetDevice(&prev);
     cudaSetDevice(device);
     h->device = device;
-    const size_t parts = size_t(kMaxParts) * kPartFloats * 4, tickets = size_t(kMaxParts) * 2 * kEpilogueWarps * 4;
+    const size_t parts = size_t(kMaxParts) * kPartFloats * 4, tickets = size_t(kMaxParts) * 2 * kMostEpilogueWarps * 4;
     cudaError_t e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
     h->pairs = std::min(std::max(sms / 2, 1), kMaxPairs);
     if (e == cudaSuccess)

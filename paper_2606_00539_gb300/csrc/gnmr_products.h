@@ -13,7 +13,7 @@ struct gnmr_products {
     int device = 0;
     int pairs = 1;
     float *parts = nullptr;            // [kMaxParts][kPartFloats]
-    unsigned *tickets = nullptr;       // [kMaxParts][2][kEpilogueWarps], 0 between calls
+    unsigned *tickets = nullptr;       // [kMaxParts][2][kMostEpilogueWarps], 0 between calls
     int *gave_up = nullptr;            // host memory that the kernels can write
     void *dmem = nullptr;
     CUresult (*encode)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,

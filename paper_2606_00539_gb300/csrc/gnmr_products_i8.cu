@@ -40,7 +40,7 @@ __device__ __forceinline__ uint2 widen4(uint32_t codes)
 
 constexpr int kStep = 128;                             // contraction steps of a stage: 128-byte rows of codes
 constexpr int kProducerWarp = 0, kMultiplyWarp = 1, kFirstBWarp = 2, kTablesWarp = 3;
-constexpr int kFirstWidenWarp = kFirstEpilogueWarp + kEpilogueWarps, kWidenWarps = 8;
+constexpr int kSides = 2, kFirstWidenWarp = kFirstEpilogueWarp + 4 * kSides, kWidenWarps = 8;
 constexpr int kThreads = 32 * (kFirstWidenWarp + kWidenWarps);
 // 96 registers a thread at launch, shared out anew: the epilogue holds the sums.
 constexpr int kControlRegisters = 56, kEpilogueRegisters = 136, kWidenRegisters = 72;
@@ -265,7 +265,7 @@ codes_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
             barrier_init(smem_addr(&bars.ready[s]), 2 * (kWidenWarps / 2 + (kWide ? 0 : 1)));    // likewise
             barrier_init(smem_addr(&bars.used[s]), 1);
         }
-        init_epilogue_barriers(bars);
+        init_epilogue_barriers(bars, 4 * kSides);
         barrier_init_fence();
     }
     if (warp == kMultiplyWarp)
@@ -293,7 +293,7 @@ codes_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
             fine = widen_b(p, c);
     } else if (warp < kFirstWidenWarp) {
         more_registers<kEpilogueRegisters>();
-        fine = write_outputs<S::kColumns, true, kStep>(p, c);
+        fine = write_outputs<S::kColumns, kSides, true, kStep>(p, c);
     } else {
         fewer_registers<kWidenRegisters>();
         fine = widen_a<kWide>(p, c);

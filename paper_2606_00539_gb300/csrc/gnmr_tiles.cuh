@@ -20,7 +20,7 @@ constexpr int kMaxPairs = 80;
 constexpr int kMaxParts = 2 * kMaxPairs;               // split tiles' parts in one call
 constexpr int64_t kPartFloats = 256 * 256;             // one part: both CTAs' lanes by the columns
 constexpr int kLanes = 256;                            // of a pair's tile
-constexpr int kEpilogueWarps = 8;
+constexpr int kMostEpilogueWarps = 16;
 constexpr int kFirstEpilogueWarp = 4;
 
 struct Product {
@@ -272,13 +272,13 @@ template <int kOut> __device__ __forceinline__ unsigned exchange(float first, fl
 
 // The outputs that a tile will be added to, to L2 while it is multiplied: read as they are
 // needed, 16 at a time, they took longer than the multiplies.
-__device__ __forceinline__ void fetch_outputs(const Product &p, const Cta &c, const Item &it, int warp)
+__device__ __forceinline__ void fetch_outputs(const Product &p, const Cta &c, const Item &it, int warp, int warps)
 {
     const int bytes = p.out_type == GNMR_DTYPE_F32 ? 4 : 2, lines = 128 * bytes / 128;     // of a column, a CTA's lanes
     const int lane = threadIdx.x & 31, first = it.lane0 + c.rank * 128;
     const int64_t row = p.cols ? it.col0 : int64_t(it.row0) + it.col0;
     const char *out = static_cast<const char *>(p.out) + ((p.cols ? it.g * p.out_group : 0) + row * p.out_col + first) * bytes;
-    for (int i = warp * 32 + lane; i < it.cols * lines; i += kEpilogueWarps * 32) {
+    for (int i = warp * 32 + lane; i < it.cols * lines; i += warps * 32) {
         const int col = i / lines, line = i - col * lines;
         if (first + line * (128 / bytes) < p.lanes)
             asm volatile("prefetch.global.L2 [%0];" ::"l"(out + col * p.out_col * bytes + line * 128));
@@ -338,13 +338,16 @@ __device__ __forceinline__ void finish(const Product &p, const Item &it, uint32_
                 for (int j = 0; j < 16; ++j)
                     *reinterpret_cast<float *>(out + j * near) = v[j];
             } else {
-                unsigned w[8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    w[j] = exchange<kOut>(v[2 * j], v[2 * j + 1], which);
+                for (int h = 0; h < 16; h += 8) {
+                    unsigned w[4];
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    *reinterpret_cast<unsigned *>(out + 2 * j * near) = w[j];
+                    for (int j = 0; j < 4; ++j)
+                        w[j] = exchange<kOut>(v[h + 2 * j], v[h + 2 * j + 1], which);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        *reinterpret_cast<unsigned *>(out + (h + 2 * j) * near) = w[j];
+                }
             }
             out += 16 * step;
             continue;
@@ -402,11 +405,11 @@ __device__ __forceinline__ void add_to_sum(uint32_t (&acc)[16], const uint32_t (
 }
 
 // The barriers that the epilogue counts on.
-__device__ __forceinline__ void init_epilogue_barriers(Barriers &b)
+__device__ __forceinline__ void init_epilogue_barriers(Barriers &b, int warps)
 {
     for (int h = 0; h < 2; ++h) {
         barrier_init(smem_addr(&b.done[h]), 1);
-        barrier_init(smem_addr(&b.drained[h]), 2 * kEpilogueWarps);
+        barrier_init(smem_addr(&b.drained[h]), 2 * warps);
     }
 }
 
@@ -445,11 +448,10 @@ __device__ __forceinline__ void finish_pair(bool fine, int *gave_up)
 // A split tile: this warp's lanes and columns of this part go to memory, and the warp that
 // gets here last takes the sum of all parts, in their order.  Warps do not wait for one
 // another: whether this one has the sum.
-template <int kColumns, bool kCodes>
-__device__ __forceinline__ bool join_parts(const Product &p, const Cta &c, const Item &it, uint32_t (&acc)[kColumns / 32][16],
+template <int kPieces, bool kCodes>
+__device__ __forceinline__ bool join_parts(const Product &p, const Cta &c, const Item &it, uint32_t (&acc)[kPieces][16],
                                            int cols, int col, int warp)
 {
-    constexpr int kPieces = kColumns / 32;               // of 16 columns
     const int lane = threadIdx.x & 31, split = c.split;
     uint32_t *part = reinterpret_cast<uint32_t *>(p.parts) + int64_t(it.tile) * split * kPartFloats +
                      c.rank * (kPartFloats / 2) + (warp & 3) * 32 + lane;
@@ -463,7 +465,7 @@ __device__ __forceinline__ bool join_parts(const Product &p, const Cta &c, const
     __syncwarp();
     unsigned before = 0;
     if (lane == 0) {
-        unsigned *ticket = p.tickets + (2 * it.tile + c.rank) * kEpilogueWarps + warp - kFirstEpilogueWarp;
+        unsigned *ticket = p.tickets + (2 * it.tile + c.rank) * kMostEpilogueWarps + warp - kFirstEpilogueWarp;
         before = atomicAdd(ticket, 1u);
         if (before + 1 == static_cast<unsigned>(split))
             *ticket = 0;                                 // for the next call
@@ -488,11 +490,12 @@ __device__ __forceinline__ bool join_parts(const Product &p, const Cta &c, const
     return true;
 }
 
-// The epilogue's warps: a tile's pieces added up and written.
-template <int kColumns, bool kCodes, int kStep>
+// The epilogue's warps, four (one to 32 lanes) for each of kSides shares of a tile's columns: its
+// pieces added up and written.
+template <int kColumns, int kSides, bool kCodes, int kStep>
 __device__ __forceinline__ bool write_outputs(const Product &p, const Cta &c)
 {
-    constexpr int kPieces = kColumns / 32;               // of 16 columns
+    constexpr int kPieces = kColumns / 16 / kSides;      // of 16 columns
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int quarter = warp & 3, side = (warp - kFirstEpilogueWarp) >> 2;
     const uint32_t done = smem_addr(&c.bars->done[0]), drained = in_cta(smem_addr(&c.bars->drained[0]), 0);
@@ -500,10 +503,10 @@ __device__ __forceinline__ bool write_outputs(const Product &p, const Cta &c)
     uint32_t phase = 0;
     for (int i = c.pair, g = 0; i < c.items; i += c.pairs) {
         const Item it = item_of<kStep>(p, c.tables, c.split, c.lane_tiles, i, g);
-        const int span = it.wide / 2;                          // columns of this warp
+        const int span = parts_of(it.wide, 16 * kSides) * 16;               // columns of this warp, or fewer
         const int at = it.lane0 + c.rank * 128 + quarter * 32 + lane, col = side * span;
         if (p.add)
-            fetch_outputs(p, c, it, warp - kFirstEpilogueWarp);
+            fetch_outputs(p, c, it, warp - kFirstEpilogueWarp, 4 * kSides);
         uint32_t acc[kPieces][16];
         if (it.k0 == it.k1)
 #pragma unroll
@@ -543,7 +546,7 @@ __device__ __forceinline__ bool write_outputs(const Product &p, const Cta &c)
             if (half ^= 1; half == 0)
                 phase ^= 1;
         }
-        if (c.split > 1 && !join_parts<kColumns, kCodes>(p, c, it, acc, min(span, it.cols - col), col, warp))
+        if (c.split > 1 && !join_parts<kPieces, kCodes>(p, c, it, acc, min(span, it.cols - col), col, warp))
             continue;
         if (p.add && it.depth == 0)
             continue;                                    // nothing to add
