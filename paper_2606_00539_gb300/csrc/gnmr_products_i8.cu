@@ -1,7 +1,7 @@
 // Expert products on 8-bit codes.
 //
-// sm_103a's tensor cores take no 8-bit integers at their full rate, so codes are
-// multiplied as fp16, which holds them exactly: products are below 2^14 and a piece of
+// sm_103a's tensor cores (tcgen05) take no 8-bit integers, so codes are multiplied as
+// fp16, which holds them exactly: products are below 2^14 and a piece of
 // 1,024 of them sums to at most 2^24, exact in fp32; pieces are added as integers.
 //
 // The weights stay 8 bits wide up to the SM: eight warps widen A's tiles into tensor
@@ -10,7 +10,7 @@
 // tile of columns, would take more of it than there is beside the multiplies).  B, the
 // rows, are widened by two more warps where they are few, else in memory by a
 // kernel before this one.  Widening the weights in memory too, for the 16-bit kernel, was
-// slower up to 4,001 rows to a group (5120 -> 13824: 380 us, this way 355).
+// slower at 4,001 rows to a group (5120 -> 13824: 380 us, this way 321).
 #include <algorithm>
 #include <cstring>
 
