@@ -483,18 +483,22 @@ gnmr_status gnmr_products_destroy(gnmr_products *h);
  * elements), one scale for every row: amax = max |x|, q = round(x * (127 * (1 / amax))),
  * halves to even, scale = amax / 127, each operation rounded to fp32.  A row whose amax is 0, or so
  * small that 127 / amax overflows, has codes and scale 0; one that holds a NaN or
- * an infinity has codes 0 and scale NaN.  Runs on the calling thread's current
+ * an infinity has codes 0 and scale NaN.  d_mask: as in gnmr_product, NULL for
+ * all groups; groups whose byte is not 0, which the 8-bit product leaves out, have
+ * their codes and scales left as they are.  Runs on the calling thread's current
  * device and allocates nothing.  d_scale: [groups x rows].  Errors:
  * GNMR_ERR_INVALID_ARG, GNMR_ERR_LAYOUT, GNMR_ERR_CUDA. */
 gnmr_status gnmr_quantize_rows(const void *d_x, int32_t dtype, int32_t groups, int64_t rows, int64_t cols,
-                               int64_t x_stride, int64_t x_group_stride, int8_t *d_q, int64_t q_stride,
-                               int64_t q_group_stride, float *d_scale, void *stream);
+                               int64_t x_stride, int64_t x_group_stride, const uint8_t *d_mask,
+                               int64_t mask_stride, int8_t *d_q, int64_t q_stride, int64_t q_group_stride,
+                               float *d_scale, void *stream);
 
 /* The same with one scale for every column, and the codes transposed: d_q is
  * [cols x rows] per group, d_scale [groups x cols]. */
 gnmr_status gnmr_quantize_columns(const void *d_x, int32_t dtype, int32_t groups, int64_t rows, int64_t cols,
-                                  int64_t x_stride, int64_t x_group_stride, int8_t *d_q, int64_t q_stride,
-                                  int64_t q_group_stride, float *d_scale, void *stream);
+                                  int64_t x_stride, int64_t x_group_stride, const uint8_t *d_mask,
+                                  int64_t mask_stride, int8_t *d_q, int64_t q_stride, int64_t q_group_stride,
+                                  float *d_scale, void *stream);
 
 #ifdef __cplusplus
 }

@@ -155,11 +155,11 @@ PROTOTYPES = {
     "gnmr_products_scratch_bytes": (ctypes.c_int, [_P, _P]),
     "gnmr_products_destroy": (ctypes.c_int, [_P]),
     "gnmr_quantize_rows": (ctypes.c_int, [_P, ctypes.c_int32, ctypes.c_int32, ctypes.c_int64, ctypes.c_int64,
-                                          ctypes.c_int64, ctypes.c_int64, _P, ctypes.c_int64,
-                                          ctypes.c_int64, _P, _P]),
+                                          ctypes.c_int64, ctypes.c_int64, _P, ctypes.c_int64, _P,
+                                          ctypes.c_int64, ctypes.c_int64, _P, _P]),
     "gnmr_quantize_columns": (ctypes.c_int, [_P, ctypes.c_int32, ctypes.c_int32, ctypes.c_int64, ctypes.c_int64,
-                                             ctypes.c_int64, ctypes.c_int64, _P, ctypes.c_int64,
-                                             ctypes.c_int64, _P, _P]),
+                                             ctypes.c_int64, ctypes.c_int64, _P, ctypes.c_int64, _P,
+                                             ctypes.c_int64, ctypes.c_int64, _P, _P]),
 }
 
 _lib = None
@@ -322,14 +322,14 @@ def gnmr_products_destroy(handle: int) -> None:
 
 
 def gnmr_quantize_rows(d_x: int, dtype: int, groups: int, rows: int, cols: int, x_stride: int,
-                       x_group_stride: int, d_q: int, q_stride: int, q_group_stride: int, d_scale: int,
-                       stream: int = 0) -> None:
-    _check(load().gnmr_quantize_rows(d_x, dtype, groups, rows, cols, x_stride, x_group_stride, d_q, q_stride,
-                                     q_group_stride, d_scale, stream), None)
+                       x_group_stride: int, d_mask, mask_stride: int, d_q: int, q_stride: int,
+                       q_group_stride: int, d_scale: int, stream: int = 0) -> None:
+    _check(load().gnmr_quantize_rows(d_x, dtype, groups, rows, cols, x_stride, x_group_stride, d_mask, mask_stride,
+                                d_q, q_stride, q_group_stride, d_scale, stream), None)
 
 
 def gnmr_quantize_columns(d_x: int, dtype: int, groups: int, rows: int, cols: int, x_stride: int,
-                          x_group_stride: int, d_q: int, q_stride: int, q_group_stride: int, d_scale: int,
-                          stream: int = 0) -> None:
-    _check(load().gnmr_quantize_columns(d_x, dtype, groups, rows, cols, x_stride, x_group_stride, d_q, q_stride,
-                                        q_group_stride, d_scale, stream), None)
+                          x_group_stride: int, d_mask, mask_stride: int, d_q: int, q_stride: int,
+                          q_group_stride: int, d_scale: int, stream: int = 0) -> None:
+    _check(load().gnmr_quantize_columns(d_x, dtype, groups, rows, cols, x_stride, x_group_stride, d_mask, mask_stride,
+                                   d_q, q_stride, q_group_stride, d_scale, stream), None)

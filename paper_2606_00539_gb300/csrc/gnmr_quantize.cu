@@ -136,7 +136,11 @@ struct Matrix {
     int64_t q_stride, q_group_stride;
     float *scale;
     int groups;
+    const uint8_t *mask;                             // groups whose byte is not 0 are left out; NULL: none
+    int64_t mask_stride;
 };
+
+__device__ __forceinline__ bool left_out(const Matrix &m, int64_t g) { return m.mask && m.mask[g * m.mask_stride] != 0; }
 
 // ---- by row ---------------------------------------------------------------
 // kTeam threads hold a row in registers, kHeld 16-byte vectors each, so that it
@@ -196,15 +200,22 @@ __global__ void __launch_bounds__(kBlockOf<kTeam>) rows_kernel(Matrix m)
             if (lane + k * kTeam < vecs)
                 v[k].w = __ldcs(reinterpret_cast<const uint4 *>(x) + lane + k * kTeam);
     };
-    int64_t r = int64_t(blockIdx.x) * kTeams + threadIdx.x / kTeam;
+    // the team's next row that is wanted, r itself or one after it
+    const auto wanted = [&](int64_t r) {
+        while (m.mask && r < total && left_out(m, r / m.rows))
+            r += step;
+        return r;
+    };
+    int64_t r = wanted(int64_t(blockIdx.x) * kTeams + threadIdx.x / kTeam);
     if (r >= total)
         return;
     Vec<T> held[kHeld], next[kHeld];
     load(held, row_of(r));
     for (;;) {
         const T *x = row_of(r);
-        if (r + step < total)
-            load(next, row_of(r + step));
+        const int64_t after = wanted(r + step);
+        if (after < total)
+            load(next, row_of(after));
         unsigned own = 0;
 #pragma unroll
         for (int k = 0; k < kHeld; ++k)
@@ -228,7 +239,7 @@ __global__ void __launch_bounds__(kBlockOf<kTeam>) rows_kernel(Matrix m)
             store_codes<T>(q + at * kN, Vec<T>{*(reinterpret_cast<const uint4 *>(x) + at)}, s);
         for (int64_t c = vecs * kN + lane; c < m.cols; c += kTeam)
             q[c] = code_of(to_f32(x[c]), s);
-        r += step;
+        r = after;
         if (r >= total)
             return;
 #pragma unroll
@@ -245,6 +256,8 @@ __global__ void __launch_bounds__(kThreads) rows_by_element_kernel(Matrix m)
     const int64_t total = m.rows * m.groups, step = int64_t(gridDim.x) * (kThreads / 32);
     for (int64_t r = int64_t(blockIdx.x) * (kThreads / 32) + threadIdx.x / 32; r < total; r += step) {
         const int64_t g = r / m.rows, i = r - g * m.rows;
+        if (left_out(m, g))
+            continue;
         const T *x = static_cast<const T *>(m.x) + g * m.group_stride + i * m.stride;
         int8_t *q = m.q + g * m.q_group_stride + i * m.q_stride;
         unsigned amax = 0;
@@ -339,6 +352,8 @@ __global__ void __launch_bounds__(kThreads) columns_kernel(Matrix m, unsigned pa
     // fewer CTAs than 2^31, so strips too
     const unsigned strips = static_cast<unsigned>((m.cols + kStrip - 1) / kStrip);
     const unsigned at = blockIdx.x / parts, part = blockIdx.x - at * parts, g = at / strips;
+    if (left_out(m, g))
+        return;                                                  // and so do the cluster's other CTAs
     const int64_t c0 = int64_t(at - g * strips) * kStrip;
     const int64_t r0 = min(m.rows, part * each), r1 = min(m.rows, r0 + each);
     const int chunks = static_cast<int>((r1 - r0 + kChunkRows - 1) / kChunkRows);
@@ -552,15 +567,15 @@ int64_t span(int64_t groups, int64_t rows, int64_t stride, int64_t group_stride)
 }
 
 gnmr_status quantize(bool columns, const void *d_x, int32_t dtype, int32_t groups, int64_t rows, int64_t cols,
-                     int64_t x_stride, int64_t x_group_stride, int8_t *d_q, int64_t q_stride, int64_t q_group_stride,
-                     float *d_scale, void *stream)
+                     int64_t x_stride, int64_t x_group_stride, const uint8_t *d_mask, int64_t mask_stride, int8_t *d_q,
+                     int64_t q_stride, int64_t q_group_stride, float *d_scale, void *stream)
 {
     if (dtype != GNMR_DTYPE_F32 && dtype != GNMR_DTYPE_BF16 && dtype != GNMR_DTYPE_F16)
         return fail(GNMR_ERR_INVALID_ARG, "quantize: unknown dtype");
     if (groups < 1 || rows < 0 || cols < 0)
         return fail(GNMR_ERR_INVALID_ARG, "quantize: groups < 1, or a negative size");
     const int64_t high = columns ? cols : rows, wide = columns ? rows : cols;    // of the codes
-    if (x_stride < cols || q_stride < wide || x_group_stride < 0 || q_group_stride < 0)
+    if (x_stride < cols || q_stride < wide || x_group_stride < 0 || q_group_stride < 0 || (d_mask && groups > 1 && mask_stride < 1))
         return fail(GNMR_ERR_LAYOUT, "quantize: a row stride below the row's length, or a negative stride");
     if (rows > INT32_MAX || cols > INT32_MAX || span(groups, rows, x_stride, x_group_stride) < 0 || span(groups, high, q_stride, q_group_stride) < 0)
         return fail(GNMR_ERR_LAYOUT, "quantize: matrices too large");
@@ -576,7 +591,7 @@ gnmr_status quantize(bool columns, const void *d_x, int32_t dtype, int32_t group
         cudaGetLastError();
         return fail(GNMR_ERR_CUDA, "quantize: no current device");
     }
-    const Matrix m{d_x, rows, cols, x_stride, x_group_stride, d_q, q_stride, q_group_stride, d_scale, groups};
+    const Matrix m{d_x, rows, cols, x_stride, x_group_stride, d_q, q_stride, q_group_stride, d_scale, groups, d_mask, mask_stride};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     cudaError_t e;
     if (columns)
@@ -599,19 +614,19 @@ gnmr_status quantize(bool columns, const void *d_x, int32_t dtype, int32_t group
 extern "C" {
 
 gnmr_status gnmr_quantize_rows(const void *d_x, int32_t dtype, int32_t groups, int64_t rows, int64_t cols,
-                               int64_t x_stride, int64_t x_group_stride, int8_t *d_q, int64_t q_stride,
-                               int64_t q_group_stride, float *d_scale, void *stream)
+                               int64_t x_stride, int64_t x_group_stride, const uint8_t *d_mask, int64_t mask_stride,
+                               int8_t *d_q, int64_t q_stride, int64_t q_group_stride, float *d_scale, void *stream)
 {
-    return quantize(false, d_x, dtype, groups, rows, cols, x_stride, x_group_stride, d_q, q_stride, q_group_stride,
-                    d_scale, stream);
+    return quantize(false, d_x, dtype, groups, rows, cols, x_stride, x_group_stride, d_mask, mask_stride, d_q, q_stride,
+                    q_group_stride, d_scale, stream);
 }
 
 gnmr_status gnmr_quantize_columns(const void *d_x, int32_t dtype, int32_t groups, int64_t rows, int64_t cols,
-                                  int64_t x_stride, int64_t x_group_stride, int8_t *d_q, int64_t q_stride,
-                                  int64_t q_group_stride, float *d_scale, void *stream)
+                                  int64_t x_stride, int64_t x_group_stride, const uint8_t *d_mask, int64_t mask_stride,
+                                  int8_t *d_q, int64_t q_stride, int64_t q_group_stride, float *d_scale, void *stream)
 {
-    return quantize(true, d_x, dtype, groups, rows, cols, x_stride, x_group_stride, d_q, q_stride, q_group_stride,
-                    d_scale, stream);
+    return quantize(true, d_x, dtype, groups, rows, cols, x_stride, x_group_stride, d_mask, mask_stride, d_q, q_stride,
+                    q_group_stride, d_scale, stream);
 }
 
 }  // extern "C"

@@ -110,9 +110,18 @@ class ExpertProducts:
             return 1, rows, cols, row, 0
         return lead[0], rows, cols, row, stride[0] if lead[0] > 1 else 0
 
+    def _mask(self, mask, groups):
+        """Device pointer of the mask, and its stride."""
+        if mask is None:
+            return None, 1
+        self._tensor(mask, "mask", (1,), (torch.uint8,))
+        if mask.numel() != groups:
+            raise ValueError(f"mask must have one entry per group ({groups})")
+        return mask.data_ptr(), mask.stride(0) if groups > 1 else 1
+
     def _grouping(self, groups, offsets, mask):
         """Device pointers of offsets and mask, and the mask's stride."""
-        at, bits, step = None, None, 1
+        at = None
         if offsets is not None:
             self._tensor(offsets, "offsets", (1,), (torch.int64,))
             if offsets.numel() != groups + 1 or not offsets.is_contiguous():
@@ -120,12 +129,7 @@ class ExpertProducts:
             at = offsets.data_ptr()
         elif groups != 1:
             raise ValueError("offsets may be None for one group only")
-        if mask is not None:
-            self._tensor(mask, "mask", (1,), (torch.uint8,))
-            if mask.numel() != groups:
-                raise ValueError(f"mask must have one entry per group ({groups})")
-            bits, step = mask.data_ptr(), mask.stride(0) if groups > 1 else 1
-        return at, bits, step
+        return (at, *self._mask(mask, groups))
 
     def _new(self, shape, dtype, stream):
         if stream is None:
@@ -212,16 +216,17 @@ class ExpertProducts:
         return out
 
     # -- 8-bit products -------------------------------------------------------
-    def _quantize(self, x, columns, stream):
+    def _quantize(self, x, columns, mask, stream):
         groups, rows, cols, row, group = self._matrix(x, "x", (2, 3), self._any)
+        bits, step = self._mask(mask, groups)
         high, wide = (cols, rows) if columns else (rows, cols)
         held = (wide + 15) // 16 * 16              # rows of codes start at multiples of 16 bytes
         lead = x.shape[:-2]
         q = self._new((*lead, high, held), torch.int8, stream)
         scale = self._new((*lead, high), torch.float32, stream)
         fn = N.gnmr_quantize_columns if columns else N.gnmr_quantize_rows
-        args = (x.data_ptr(), _DTYPES[x.dtype], groups, rows, cols, row, group, q.data_ptr(), held, high * held,
-                scale.data_ptr(), self._stream(stream))
+        args = (x.data_ptr(), _DTYPES[x.dtype], groups, rows, cols, row, group, bits, step, q.data_ptr(), held,
+                high * held, scale.data_ptr(), self._stream(stream))
         if torch.cuda.current_device() == self.device_index:
             fn(*args)
         else:
@@ -229,17 +234,18 @@ class ExpertProducts:
                 fn(*args)
         return q if held == wide else q[..., :wide], scale
 
-    def quantize_rows(self, x, *, stream=None):
+    def quantize_rows(self, x, *, mask=None, stream=None):
         """8-bit codes of every row of x ([rows, cols] or [groups, rows, cols]; bf16, f16 or
         fp32) and its scale: (int8 codes of x's shape, fp32 scales).  round(x * (127 * (1 / amax))),
-        halves to even; x is about codes * scale.  Activations by token, weights by output channel."""
-        return self._quantize(x, False, stream)
+        halves to even; x is about codes * scale.  Activations by token, weights by output channel.
+        mask: groups whose entry is not 0, which forward_i8 leaves out, get no codes."""
+        return self._quantize(x, False, mask, stream)
 
-    def quantize_columns(self, w, *, stream=None):
+    def quantize_columns(self, w, *, mask=None, stream=None):
         """8-bit codes of every column of w, transposed, and its scale: ([..., cols, rows],
         [..., cols]).  Weights by input channel, for the backward product of the 8-bit path:
         dx = forward_i8(codes of dy, ..., codes of w's columns, ...)."""
-        return self._quantize(w, True, stream)
+        return self._quantize(w, True, mask, stream)
 
     def forward_i8(self, xq, x_scale, wq, w_scale, offsets=None, *, out=None, out_dtype="bf16", mask=None,
                    stream=None):
@@ -270,7 +276,7 @@ def _expert_linear_function():
             products.forward(x, w, offsets, out=y, mask=mask)
             if mask is not None:
                 xq, xs = products.quantize_rows(x)
-                wq, ws = codes[:2] if codes is not None else products.quantize_rows(w)
+                wq, ws = codes[:2] if codes is not None else products.quantize_rows(w, mask=mask)
                 products.forward_i8(xq, xs, wq, ws, offsets, out=y, mask=mask)
             ctx.products, ctx.grad, ctx.codes = products, grad, codes
             ctx.save_for_backward(x, w, *(t for t in (offsets, mask) if t is not None))
@@ -289,7 +295,7 @@ def _expert_linear_function():
                 products.input_grad(dy, w, offsets, out=dx, mask=mask)
                 if mask is not None:
                     dq, ds = products.quantize_rows(dy)
-                    vq, vs = ctx.codes[2:] if ctx.codes is not None else products.quantize_columns(w)
+                    vq, vs = ctx.codes[2:] if ctx.codes is not None else products.quantize_columns(w, mask=mask)
                     products.forward_i8(dq, ds, vq, vs, offsets, out=dx, mask=mask)
             if ctx.grad is not None:
                 products.weight_grad(dy, x, offsets, out=ctx.grad)

@@ -321,6 +321,27 @@ def test_codes_of_views(products):
             assert np.array_equal(q[0].cpu().numpy(), wq) and np.array_equal(q[1].cpu().numpy(), ws)
 
 
+@pytest.mark.parametrize("shape", [(5, 130, 72), (5, 9, 1032), (5, 7, 5), (5, 3, 9000)])
+def test_codes_of_masked_groups_are_left_as_they_are(products, shape):
+    x = normal(gen(15), *shape, dtype=torch.bfloat16)
+    mask = torch.tensor([0, 7, 1, 0, 9, 255, 0, 7, 0], dtype=torch.uint8, device="cuda")[::2]     # 0 1 9 0 0
+    for fn, want in ((products.quantize_rows, x), (products.quantize_columns, x.transpose(1, 2))):
+        q, s = fn(x, mask=mask)
+        wq, ws = codes_oracle(want)
+        for e in (0, 3, 4):
+            assert np.array_equal(q[e].cpu().numpy(), wq[e]) and np.array_equal(s[e].cpu().numpy(), ws[e])
+    held = torch.full((5, 130, 16), 77, dtype=torch.int8, device="cuda")
+    scale = torch.full((5, 130), 7.0, device="cuda")
+    from paper_2606_00539_gb300 import _native as N
+    y = normal(gen(16), 5, 130, 16, dtype=torch.float32)
+    every = torch.ones(5, dtype=torch.uint8, device="cuda")
+    N.gnmr_quantize_rows(y.data_ptr(), N.GNMR_DTYPE_F32, 5, 130, 16, 16, 130 * 16, every.data_ptr(), 1, held.data_ptr(),
+                         16, 130 * 16, scale.data_ptr(), torch.cuda.current_stream().cuda_stream)
+    N.gnmr_quantize_columns(y.data_ptr(), N.GNMR_DTYPE_F32, 5, 130, 16, 16, 130 * 16, every.data_ptr(), 1,
+                            held.data_ptr(), 130, 130 * 16, scale.data_ptr(), torch.cuda.current_stream().cuda_stream)
+    assert (held == 77).all() and (scale == 7).all()
+
+
 def codes(g, *shape, low=-127):
     return torch.randint(low, 128, shape, device="cuda", generator=g, dtype=torch.int8)
 

@@ -107,11 +107,11 @@ def test_refusals_without_arguments(lib):
     (INVALID, dict(dtype=3)), (INVALID, dict(groups=0)), (INVALID, dict(rows=-1)), (INVALID, dict(cols=-1)),
     (INVALID, dict(x=None)), (INVALID, dict(q=None)), (INVALID, dict(scale=None)), (LAYOUT, dict(x_stride=7)),
     (LAYOUT, dict(q_stride=6)), (LAYOUT, dict(x_group_stride=-1)), (LAYOUT, dict(x=4097)), (LAYOUT, dict(scale=4098)),
-    (LAYOUT, dict(rows=1 << 40, x_stride=1 << 40, q_stride=1 << 40)),
+    (LAYOUT, dict(rows=1 << 40, x_stride=1 << 40, q_stride=1 << 40)), (LAYOUT, dict(groups=2, mask=4096, mask_stride=0)),
 ])
 def test_quantize_refusals(columns, status, over):
-    kw = dict(x=4096, dtype=N.GNMR_DTYPE_BF16, groups=1, rows=8, cols=8, x_stride=8, x_group_stride=64, q=4096,
-              q_stride=8, q_group_stride=64, scale=4096)
+    kw = dict(x=4096, dtype=N.GNMR_DTYPE_BF16, groups=1, rows=8, cols=8, x_stride=8, x_group_stride=64, mask=None,
+              mask_stride=1, q=4096, q_stride=8, q_group_stride=64, scale=4096)
     kw.update(over)
     fn = N.gnmr_quantize_columns if columns else N.gnmr_quantize_rows
     with pytest.raises(GnmrError) as e:
@@ -120,5 +120,5 @@ def test_quantize_refusals(columns, status, over):
 
 
 def test_quantize_of_nothing_is_no_work():
-    N.gnmr_quantize_rows(None, N.GNMR_DTYPE_F32, 1, 0, 8, 8, 0, None, 8, 0, None)
-    N.gnmr_quantize_columns(None, N.GNMR_DTYPE_F32, 1, 8, 0, 8, 0, None, 8, 0, None)
+    N.gnmr_quantize_rows(None, N.GNMR_DTYPE_F32, 1, 0, 8, 8, 0, None, 1, None, 8, 0, None)
+    N.gnmr_quantize_columns(None, N.GNMR_DTYPE_F32, 1, 8, 0, 8, 0, None, 1, None, 8, 0, None)
