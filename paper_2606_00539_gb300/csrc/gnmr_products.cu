@@ -11,9 +11,14 @@
 // A pair of CTAs computes 256 lanes by up to 256 columns (two SMs share an operand
 // tile: 32 KB of operands an SM for 64 steps of the contraction, where one SM alone
 // would need 48).  Per CTA: one warp has the TMA unit load tiles of 64 steps into a
-// ring of stages, one (of the first CTA) issues the multiplies, eight add up the
-// finished pieces and write the outputs, and one clears what the last tile of a
+// ring of stages, one (of the first CTA) issues the multiplies, eight or sixteen add up
+// the finished pieces and write the outputs, and one clears what the last tile of a
 // group's rows holds past their end (weight gradient).
+//
+// Measured (one GB300, 64 experts of 1408 x 2048, bf16): forward of 49,152 rows 190 us, 1.5 PFLOP/s,
+// multiplies under way 79 % of the time at the 1.6 GHz that the power limit leaves; input gradient
+// of 24,571 rows 102 us, weight gradient 120 us (bound by its outputs); forward of 282 rows 59 us, 6.3
+// TB/s of weights.  Dense 4096^3 74 us, 1.85 PFLOP/s.
 //
 // A piece is at most 1,024 steps (512 for fp32 outputs).  The tensor cores cut
 // sums that they hold rather than rounding them: 2,047 steps in one piece were
@@ -356,8 +361,11 @@ gnmr_status check(const gnmr_product *p)
 // widened in memory first.  5120 -> 13824, 16 rows: 22 us in 8 bits, 28 widened; 64: 28 and 29; 64
 // experts of 2048 -> 1408, 31 rows each: 53 and 51, 64 each: 73 and 55.
 constexpr int64_t kFewCodes = 32;
-// 16-bit operands: up to this many rows to a group, tiles of 64 columns.
-constexpr int64_t kFewRows = 32;
+// 16-bit operands: tiles of 64 columns up to this many rows to a group, and for one group
+// while they make one round at most.  5120 -> 13824, 16 rows: 26 us so, 28 in tiles of 256; 64: 27 and 29;
+// 128: 39 and 30.  2048 -> 2048, 16 rows: 8 and 12; 200: 10 and 17.  64 experts of 1408 -> 2048, 1 row
+// each: 39 and 42, 64 each: 66 and 65.
+constexpr int64_t kFewRows = 64;
 
 Operands operands(const gnmr_product *p)
 {
@@ -583,8 +591,7 @@ gnmr_status gnmr_products_run(gnmr_products *h, const gnmr_product *p, void *str
                          m->read_bytes};
             scratch += n;
         }
-    // few rows to a group: smaller tiles, more of them in flight
-    const bool few = !wgrad && p->rows <= kFewRows * p->groups;
+    const bool few = !wgrad && (p->rows <= kFewRows * p->groups || (p->groups == 1 && lane_tiles * ((p->rows + 63) / 64) <= h->pairs));
     bool mapped = true;
     if (e == cudaSuccess)
         e = kLaunch[p->op][few](h, o, q, st, &mapped);

