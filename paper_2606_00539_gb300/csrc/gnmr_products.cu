@@ -357,10 +357,12 @@ gnmr_status check(const gnmr_product *p)
     return GNMR_OK;
 }
 
-// 8-bit codes: up to this many rows to a group the rows are read in 8 bits too; more are
-// widened in memory first.  5120 -> 13824, 16 rows: 22 us in 8 bits, 28 widened; 64: 28 and 29; 64
-// experts of 2048 -> 1408, 31 rows each: 53 and 51, 64 each: 73 and 55.
-constexpr int64_t kFewCodes = 32;
+// 8-bit codes: the rows are read in 8 bits too up to this many to a group, and for one group
+// while its tiles of 64 columns are few; otherwise they are widened in memory first.  5120 -> 13824, 16
+// rows: 22 us in 8 bits, 28 widened; 64 experts of 2048 -> 1408, 31 rows each: 53 and 51, 64 each: 73 and 55.
+// One group, 4096 -> 1024, 100 rows (8 tiles): 12 and 19; 2048 -> 2048, 200 (32): 12.5 and 14; 7296 -> 4352, 200
+// (68): 31 and 25.
+constexpr int64_t kFewCodes = 32, kFewCodeTiles = 48;
 // 16-bit operands: tiles of 64 columns up to this many rows to a group, and for one group
 // while they make one round at most.  5120 -> 13824, 16 rows: 26 us so, 28 in tiles of 256; 64: 27 and 29;
 // 128: 39 and 30.  2048 -> 2048, 16 rows: 8 and 12; 200: 10 and 17.  64 experts of 1408 -> 2048, 1 row
@@ -371,7 +373,9 @@ Operands operands(const gnmr_product *p)
 {
     const bool codes = p->op == GNMR_PRODUCT_FORWARD_I8;
     const int bytes = codes ? 1 : 2;
-    const Operand x{p->d_x, p->rows, p->n_in, p->x_stride, 0, 1, bytes, codes && p->rows <= kFewCodes * p->groups ? 1 : 2};
+    const int64_t narrow = (int64_t(p->n_out) + kLanes - 1) / kLanes * ((p->rows + 63) / 64);
+    const bool few = p->rows <= kFewCodes * p->groups || (p->groups == 1 && narrow <= kFewCodeTiles);
+    const Operand x{p->d_x, p->rows, p->n_in, p->x_stride, 0, 1, bytes, codes && few ? 1 : 2};
     const Operand dy{p->d_dy, p->rows, p->n_out, p->dy_stride, 0, 1, 2, 2};
     const bool shared = p->w_group_stride == 0;          // one weight for all groups
     const Operand w{p->d_w, p->n_out, p->n_in, p->w_stride, p->w_group_stride, shared ? 1 : p->groups, bytes, bytes};

@@ -62,6 +62,8 @@ def test_other_operands_are_copied_to_scratch():
     assert N.gnmr_products_scratch_bytes(product(**i8)) == 0
     assert N.gnmr_products_scratch_bytes(product(**i8, rows=64)) == 0
     assert N.gnmr_products_scratch_bytes(product(**i8, rows=65)) == 65 * 128 + 128    # widened, to whole 128 bytes
+    assert N.gnmr_products_scratch_bytes(product(**i8, rows=65, groups=1)) == 0       # few tiles
+    assert N.gnmr_products_scratch_bytes(product(**i8, rows=48 * 64 + 1, groups=1)) == 3073 * 128 + 128
     assert N.gnmr_products_scratch_bytes(product(**{**i8, "w_stride": 33, "w_group_stride": 528})) == 2 * 16 * 32
 
 
