@@ -142,6 +142,63 @@ def test_strides_and_views(products):
             check(dw[e], D.T @ X, D.abs().T @ X.abs(), counts[e], "f32")
 
 
+@pytest.mark.parametrize("n,k,held,lead", [(40, 65, 72, 0), (33, 130, 136, 8), (41, 67, 71, 1), (72, 63, 64, 3)])
+def test_what_lies_between_rows_has_no_influence(products, n, k, held, lead):
+    """NaN after the last column of every row, in operands read in place and in copied ones."""
+    counts, t, g = [50, 0, 21, 200], torch.bfloat16, gen(n)
+    off, R = offsets_of(counts), 271
+
+    def inside(*shape):
+        flat = torch.full((shape[0] * (shape[1] if len(shape) == 3 else 1) * (held + 16) + lead + 64,), float("nan"),
+                          dtype=t, device="cuda")
+        row = held if shape[-1] <= held else shape[-1]
+        strides = (row * shape[1] + 8, row, 1) if len(shape) == 3 else (row, 1)
+        v = torch.as_strided(flat, shape, strides, lead)
+        v.copy_(normal(g, *shape, dtype=t))
+        return v
+
+    x, w, dy = inside(R, k), inside(4, n, k), inside(R, n)
+    y, dx = products.forward(x, w, off), products.input_grad(dy, w, off)
+    dw = products.weight_grad(dy, x, off, out=torch.empty(4, n, k, device="cuda"))
+    for e, at in spans(counts):
+        X, D, W = x[at].double(), dy[at].double(), w[e].double()
+        check(y[at], X @ W.T, X.abs() @ W.abs().T, k, "bf16")
+        check(dx[at], D @ W, D.abs() @ W.abs(), n, "bf16")
+        check(dw[e], D.T @ X, D.abs().T @ X.abs(), counts[e], "f32")
+
+
+def test_offsets_past_32_bits(products):
+    """Rows, and an arena, of more than 2^31 elements: what lies at their ends."""
+    rows, k, n = 1_100_001, 2048, 24
+    if torch.cuda.mem_get_info()[0] < 24 << 30:
+        pytest.skip("needs 24 GB")
+    g, t = gen(17), torch.bfloat16
+    x = torch.empty(rows, k, dtype=t, device="cuda").normal_(generator=g)
+    w, dy = normal(g, 2, n, k, dtype=t), torch.zeros(rows, n, dtype=t, device="cuda")
+    dy[rows - 9:] = normal(g, 9, n, dtype=t)
+    off = torch.tensor([0, rows - 7, rows], dtype=torch.int64, device="cuda")
+    y = products.forward(x, w, off)
+    for at, e in ((slice(rows - 7, rows), 1), (slice(rows - 60, rows - 7), 0), (slice(0, 50), 0)):
+        X, W = x[at].double(), w[e].double()
+        check(y[at], X @ W.T, X.abs() @ W.abs().T, k, "bf16")
+    arena = torch.zeros(2 ** 31 + 2 * n * k, device="cuda")
+    out = torch.as_strided(arena, (2, n, k), (2 ** 31 + n * k, k, 1))
+    products.weight_grad(dy, x, off, out=out)
+    for e, at in ((0, slice(rows - 9, rows - 7)), (1, slice(rows - 7, rows))):
+        X, D = x[at].double(), dy[at].double()
+        check(out[e], D.T @ X, D.abs().T @ X.abs(), rows if e == 0 else 7, "f32")
+    assert int((arena != 0).sum()) == int((out != 0).sum())
+    del arena, out, y
+    q, s = products.quantize_rows(x)
+    wq, ws = codes_oracle(x[-5:])
+    assert np.array_equal(q[-5:].cpu().numpy(), wq) and np.array_equal(s[-5:].cpu().numpy(), ws)
+    (vq, vs) = products.quantize_rows(w)
+    low = products.forward_i8(q, s, vq, vs, off, out_dtype="f32")
+    at = slice(rows - 7, rows)
+    want = (q[at].double() @ vq[1].double().T) * s[at].double()[:, None] * vs[1].double()
+    assert ((low[at].double() - want).abs() <= want.abs() * 2.0 ** -21).all()
+
+
 @pytest.mark.parametrize("groups", [270, 2048])
 def test_many_groups(products, groups):
     """Tables that leave room for fewer stages, and most groups without rows."""
@@ -456,3 +513,25 @@ def test_expert_linear(products, bits):
                 assert (err <= np.abs(want) * (ROUND["bf16"] + 2.0 ** -21)).all()
         check(arena[e], D.T @ X, D.abs().T @ X.abs(), counts[e], "f32")
         check(dw2[e], D.T @ X, D.abs().T @ X.abs(), counts[e], "bf16")
+
+
+@pytest.mark.parametrize("bit", [0, 1])
+def test_expert_linear_of_one_dense_unit(products, bit):
+    g, t = gen(18), torch.bfloat16
+    x, w, dy = normal(g, 90, 136, dtype=t), normal(g, 72, 136, dtype=t, size=0.1), normal(g, 90, 72, dtype=t)
+    arena = torch.full((72, 136), 7.0, device="cuda")
+    mask = torch.tensor([bit], dtype=torch.uint8, device="cuda")
+    x.requires_grad_()
+    y = expert_linear(products, x, w, None, mask, arena)
+    dx, = torch.autograd.grad(y, x, dy.expand(90, 72))
+    X, D, W = x.detach().double(), dy.double(), w.double()
+    check(arena, D.T @ X, D.abs().T @ X.abs(), 90, "f32")
+    if bit:
+        check(y, X @ W.T, X.abs() @ W.abs().T, 136, "bf16")
+        check(dx, D @ W, D.abs() @ W.abs(), 72, "bf16")
+    else:
+        (xq, xs), (dq, ds), (wq, ws), (vq, vs) = (codes_oracle(a) for a in (x.detach(), dy, w, w.T))
+        for got, a, s, b, u in ((y, xq, xs, wq, ws), (dx, dq, ds, vq, vs)):
+            want = (a.astype(float) @ b.astype(float).T) * s.astype(float)[:, None] * u.astype(float)
+            err = np.abs(got.detach().double().cpu().numpy() - want)
+            assert (err <= np.abs(want) * (ROUND["bf16"] + 2.0 ** -21)).all()
