@@ -167,6 +167,8 @@ __device__ __forceinline__ bool widen_b(const Product &p, const Cta &c)
     for (int i = c.pair, g = 0; i < c.items; i += c.pairs) {
         const Item it = item_of<kStep>(p, c.tables, c.split, c.lane_tiles, i, g);
         const int half = it.wide / 2;
+        // rows beyond these are columns that nobody reads
+        const int rows = min(half, it.cols - static_cast<int>(c.rank) * half);
         int k = it.k0 + skip;
         for (; k < it.k1; k += 2) {
             if (!wait(full + stage * 8, phase) || !wait(used + slot * 8, slot_phase))
@@ -174,7 +176,7 @@ __device__ __forceinline__ bool widen_b(const Product &p, const Cta &c)
             const uint8_t *raw = c.stages + S::kWidened + stage * kStage + kAStage;
             uint8_t *to = c.stages + slot * kSlot + (chunk >> 2) * kBTile;
 #pragma unroll 4
-            for (int r = lane >> 3; r < half; r += 4) {
+            for (int r = lane >> 3; r < rows; r += 4) {
                 const uint4 codes = *reinterpret_cast<const uint4 *>(raw + r * 128 + ((chunk ^ (r & 7)) << 4));
                 const uint2 v0 = widen4(codes.x), v1 = widen4(codes.y), v2 = widen4(codes.z), v3 = widen4(codes.w);
                 const int at = (chunk & 3) * 2, x = r & 7;
