@@ -471,6 +471,7 @@ __device__ __forceinline__ bool join_parts(const Product &p, const Cta &c, const
             *ticket = 0;                                 // for the next call
         __threadfence();
     }
+    __syncwarp();                                        // the other lanes' loads come after that fence (a shuffle orders none)
     if (__shfl_sync(~0u, before, 0) + 1 != static_cast<unsigned>(split))
         return false;
 #pragma unroll
