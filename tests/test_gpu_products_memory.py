@@ -8,7 +8,7 @@ pytestmark = pytest.mark.gpu
 
 import torch  # noqa: E402
 
-from test_gpu_products import check, gen, normal, offsets_of, spans  # noqa: E402
+from .test_gpu_products import check, gen, normal, offsets_of, spans  # noqa: E402
 
 
 @pytest.fixture(scope="module")
