@@ -354,7 +354,9 @@ __global__ void __launch_bounds__(kCopyThreads) copy_kernel(Copy c)
     const char *from = static_cast<const char *>(c.from) + g * c.group_stride * kFrom;
     char *to = static_cast<char *>(c.to) + g * c.rows * c.held * kTo;
     const int64_t across = (c.held + kN - 1) / kN, total = c.rows * across;
-    const bool flat = c.stride == c.held;              // then a row's last vector is whole too
+    // then a row's last vector is whole too; with fewer columns than `held`, what follows the last
+    // row's need not be the caller's
+    const bool flat = c.stride == c.held && c.cols == c.held;
     for (int64_t i = int64_t(blockIdx.x) * kCopyThreads + threadIdx.x; i < total; i += int64_t(gridDim.x) * kCopyThreads) {
         int64_t at = i * kN, out = i * kN;
         int left = kN, room = kN;
