@@ -343,11 +343,13 @@ struct Copy {
 
 constexpr int kCopyThreads = 256;
 
-// kFrom bytes an element to kTo; 16 codes or 8 numbers a thread and turn.  kWhole: rows that 16-byte loads can take.
+// kFrom bytes an element to kTo; 16 codes or 8 numbers a thread and turn.  kWhole: rows that 16-byte loads can take,
+// of codes to be widened (others of that kind are read in place).
 template <int kFrom, int kTo, bool kWhole>
 __global__ void __launch_bounds__(kCopyThreads) copy_kernel(Copy c)
 {
     constexpr int kN = 16 / kFrom;
+    static_assert(!kWhole || kFrom < kTo, "aligned operands that are not widened are not copied");
     const int g = blockIdx.y;
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -359,13 +361,12 @@ __global__ void __launch_bounds__(kCopyThreads) copy_kernel(Copy c)
     const bool flat = c.stride == c.held && c.cols == c.held;
     for (int64_t i = int64_t(blockIdx.x) * kCopyThreads + threadIdx.x; i < total; i += int64_t(gridDim.x) * kCopyThreads) {
         int64_t at = i * kN, out = i * kN;
-        int left = kN, room = kN;
+        int left = kN;
         if (!flat || !kWhole) {
             const int64_t r = i / across, col = (i - r * across) * kN;
             at = r * c.stride + col;
             out = r * c.held + col;
             left = static_cast<int>(min(int64_t(kN), c.cols - col));
-            room = static_cast<int>(min(int64_t(kN), c.held - col));
         }
         uint4 v;
         if (kWhole && left == kN) {
@@ -386,14 +387,13 @@ __global__ void __launch_bounds__(kCopyThreads) copy_kernel(Copy c)
         } else {
             const uint2 a = widen4(v.x), b = widen4(v.y), d = widen4(v.z), e = widen4(v.w);
             w[0] = make_uint4(a.x, a.y, b.x, b.y);
-            if (room > 8)
-                w[1] = make_uint4(d.x, d.y, e.x, e.y);
+            w[1] = make_uint4(d.x, d.y, e.x, e.y);            // `held` is whole 128 bytes
         }
     }
 }
 
-template <int kFrom, int kTo>
-cudaError_t launch_copy(const Copy &c, int groups, bool whole, int sms, cudaStream_t st)
+template <int kFrom, int kTo, bool kWhole>
+cudaError_t launch_copy(const Copy &c, int groups, int sms, cudaStream_t st)
 {
     const int64_t vectors = c.rows * ((c.held * kFrom + 15) / 16);
     const int64_t most = std::max<int64_t>(int64_t(sms) * 32 / groups, 1);
@@ -406,7 +406,7 @@ cudaError_t launch_copy(const Copy &c, int groups, bool whole, int sms, cudaStre
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, whole ? copy_kernel<kFrom, kTo, true> : copy_kernel<kFrom, kTo, false>, c);
+    return cudaLaunchKernelEx(&cfg, copy_kernel<kFrom, kTo, kWhole>, c);
 }
 
 }  // namespace
@@ -419,8 +419,10 @@ cudaError_t copy_operand(const Operand &o, void *to, int sms, cudaStream_t st)
     const int64_t steps = o.stride * o.bytes | (o.groups > 1 ? o.group_stride * o.bytes : 0);
     const bool whole = ((reinterpret_cast<uintptr_t>(o.at) | static_cast<uintptr_t>(steps)) & 15) == 0;
     if (o.bytes == 2)
-        return launch_copy<2, 2>(c, o.groups, whole, sms, st);
-    return o.read_bytes == 2 ? launch_copy<1, 2>(c, o.groups, whole, sms, st) : launch_copy<1, 1>(c, o.groups, whole, sms, st);
+        return launch_copy<2, 2, false>(c, o.groups, sms, st);
+    if (o.read_bytes == 1)
+        return launch_copy<1, 1, false>(c, o.groups, sms, st);
+    return whole ? launch_copy<1, 2, true>(c, o.groups, sms, st) : launch_copy<1, 2, false>(c, o.groups, sms, st);
 }
 
 cudaError_t allow_codes_shared()
