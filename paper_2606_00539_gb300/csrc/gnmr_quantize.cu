@@ -412,9 +412,10 @@ __global__ void __launch_bounds__(kThreads) columns_kernel(Matrix m, unsigned pa
         if (lane < 8)
             for (unsigned k = 0; k < parts; ++k)
                 top = max(top, cluster.map_shared_rank(s_max, k)[col + lane]);
-        // no CTA ends before every other has read its maxima: waited for at the end
+        // no CTA ends before every other has read its maxima: waited for at the end.  The arrival is a
+        // release, which comes after the reads (a relaxed one may overtake them).
         __syncwarp();
-        asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     }
     const Scale mine = scale_of(top);
     if (part == 0 && lane < 8 && col + lane < cols)
@@ -476,7 +477,7 @@ __global__ void __launch_bounds__(kThreads) columns_kernel(Matrix m, unsigned pa
     }
     if (parts > 1) {
         __syncwarp();
-        asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
     }
 }
 

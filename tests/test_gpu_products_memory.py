@@ -1,5 +1,6 @@
 """Expert products: repeated calls, sums that several SMs share, and the memory that a call
 may touch.  Tolerances are those of test_gpu_products."""
+import numpy as np
 import pytest
 
 from paper_2606_00539_gb300 import ExpertProducts
@@ -9,7 +10,7 @@ pytestmark = pytest.mark.gpu
 
 import torch  # noqa: E402
 
-from .test_gpu_products import check, gen, normal, offsets_of, spans  # noqa: E402
+from .test_gpu_products import check, codes_oracle, gen, normal, offsets_of, spans  # noqa: E402
 
 
 @pytest.fixture(scope="module")
@@ -61,3 +62,16 @@ def test_widened_codes_hold_no_columns_but_the_rows_own(products, k, stride):
     assert torch.equal(held16[:, :k].char(), xq) and not held16[:, k:].any()
     for e, at in spans([90, 60]):
         assert torch.equal(out[at].double(), xq[at].double() @ wq[e].double().T)
+
+
+def test_column_codes_of_clusters_whose_ctas_end_at_different_times(products):
+    """Rows that leave a cluster's last CTA a single row, so that it is through while others still read
+    its maxima: codes and scales of every column, and the same ones in every one of many calls."""
+    for rows, cols in ((769, 200), (8 * 128 + 1, 64), (3 * 128 * 7 + 1, 136)):
+        x = normal(gen(rows), 3, rows, cols, dtype=torch.bfloat16, size=3.0)
+        x[:, rows - 1] *= 64                                     # the maxima lie in the last CTA's row
+        q, s = products.quantize_columns(x)
+        wq, ws = codes_oracle(x.transpose(1, 2))
+        assert np.array_equal(q.cpu().numpy(), wq) and np.array_equal(s.cpu().numpy(), ws)
+        for q2, s2 in [products.quantize_columns(x) for _ in range(50)]:
+            assert torch.equal(q, q2) and torch.equal(s, s2)
