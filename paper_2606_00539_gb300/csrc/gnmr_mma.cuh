@@ -1,6 +1,6 @@
 // sm_103a building blocks of the expert products: barriers in shared memory with
 // bounded waits, tile loads by the TMA unit, and the fifth-generation tensor cores
-// (tcgen05) used by pairs of CTAs.
+// (tcgen05) used by one CTA or by pairs (kCtas: 1 or 2).
 #pragma once
 
 #include <cuda.h>
@@ -56,18 +56,23 @@ __device__ __forceinline__ void barrier_init_fence()
 }
 
 // Arrivals on a barrier of any CTA of the cluster (an address from in_cta).  The
-// plain ones order nothing but what the tensor cores' and the TMA unit's own rules do: a
-// release would wait for the outputs' stores too (49152 x 2048 -> 1408 over 64 experts
-// 558 us with releases, 290 without).
+// plain one hands over tensor memory and nothing else, between tcgen05.wait and fence_before on this
+// side and fence_after on the other, which order it: a release would wait for the outputs' stores
+// too (49152 x 2048 -> 1408 over 64 experts 558 us with releases, 290 without).
 __device__ __forceinline__ void arrive(uint32_t bar)
 {
     asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
-// After shared memory was written that this CTA's warps, or, past fence_async_proxy, its tensor cores
-// will read.  (A release for the whole cluster took 2,000 cycles.)
-__device__ __forceinline__ void arrive_release(uint32_t bar)
+// After shared memory was read that will be written anew, or was written and, past fence_async_proxy, the
+// tensor cores will read: kPaired where the thread that waits is in the other CTA, which the narrower
+// scope says nothing about.  (It takes 2,000 cycles, so that a loop of every stage keeps to its own CTA.)
+template <bool kPaired = false> __device__ __forceinline__ void arrive_release(uint32_t bar)
 {
+    if (kPaired) {
+        asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+        return;
+    }
     asm volatile("mbarrier.arrive.release.cta.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
@@ -79,19 +84,28 @@ __device__ __forceinline__ void arrive_expect(uint32_t bar, uint32_t bytes)
 
 // Every wait ends: after kWaits tries (tens of milliseconds at the least, where a
 // wait of a running kernel takes microseconds) it returns false, and its caller
-// leaves its loop.  By a whole warp, which goes on or gives up as one.
+// leaves its loop.  By a whole warp, which goes on or gives up as one.  kPaired: for a barrier
+// on which the other CTA arrives too, or its multiplies.
 constexpr int kWaits = 1 << 20;
 
-__device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity)
+template <bool kPaired> __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity)
 {
     for (int i = 0; i < kWaits; ++i) {
         uint32_t done;
-        asm volatile("{\n.reg .pred p;\n"
-                     "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n"
-                     "selp.u32 %0, 1, 0, p;\n}"
-                     : "=r"(done)
-                     : "r"(bar), "r"(parity)
-                     : "memory");
+        if (kPaired)
+            asm volatile("{\n.reg .pred p;\n"
+                         "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n"
+                         "selp.u32 %0, 1, 0, p;\n}"
+                         : "=r"(done)
+                         : "r"(bar), "r"(parity)
+                         : "memory");
+        else
+            asm volatile("{\n.reg .pred p;\n"
+                         "mbarrier.try_wait.parity.acquire.cta.shared::cta.b64 p, [%1], %2;\n"
+                         "selp.u32 %0, 1, 0, p;\n}"
+                         : "=r"(done)
+                         : "r"(bar), "r"(parity)
+                         : "memory");
         if (__all_sync(~0u, done))
             return true;
     }
@@ -110,10 +124,18 @@ template <int kRegisters> __device__ __forceinline__ void fewer_registers()
 }
 
 // ---- tile loads ---------------------------------------------------------------
-// The barrier may be the other CTA's of the pair.
+// In a pair, the barrier may be the other CTA's.
 
+template <int kCtas>
 __device__ __forceinline__ void load_tile(uint32_t dst, const CUtensorMap *map, int x, int y, int block, int z, uint32_t bar)
 {
+    if (kCtas == 1) {
+        asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
+                     "[%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
+                     "l"(map), "r"(x), "r"(y), "r"(block), "r"(z), "r"(bar)
+                     : "memory");
+        return;
+    }
     asm volatile("cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes "
                  "[%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst),
                  "l"(map), "r"(x), "r"(y), "r"(block), "r"(z), "r"(bar)
@@ -131,17 +153,27 @@ __device__ __forceinline__ void fence_async_proxy()
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
 }
 
-// ---- tensor memory and tensor cores, by pairs of CTAs --------------------------
+// ---- tensor memory and tensor cores ----------------------------------------------
 
-__device__ __forceinline__ void tmem_alloc(uint32_t smem_result, uint32_t columns)
+template <int kCtas> __device__ __forceinline__ void tmem_alloc(uint32_t smem_result, uint32_t columns)
 {
+    if (kCtas == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_result), "r"(columns)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        return;
+    }
     asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_result), "r"(columns)
                  : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
 }
 
-__device__ __forceinline__ void tmem_free(uint32_t tmem, uint32_t columns)
+template <int kCtas> __device__ __forceinline__ void tmem_free(uint32_t tmem, uint32_t columns)
 {
+    if (kCtas == 1) {
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(columns) : "memory");
+        return;
+    }
     asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(columns) : "memory");
 }
 
@@ -160,15 +192,16 @@ __device__ __forceinline__ uint64_t operand(uint32_t addr, uint32_t lead, uint32
            static_cast<uint64_t>((stride >> 4) & 0x3fff) << 32 | uint64_t(1) << 46 | uint64_t(2) << 61;
 }
 
-// 256 lanes (128 in each CTA) by `columns`, 16-bit operands of one type, fp32 sums.
+// 128 lanes in each CTA by `columns`, 16-bit operands of one type, fp32 sums.
+template <int kCtas>
 __device__ __forceinline__ uint32_t shape(bool bf16, bool a_along_lanes, bool b_along_columns, uint32_t columns)
 {
     const uint32_t type = bf16 ? 1 : 0;
     return 1u << 4 | type << 7 | type << 10 | (a_along_lanes ? 1u << 15 : 0) | (b_along_columns ? 1u << 16 : 0) |
-           (columns >> 3) << 17 | (256u >> 4) << 24;
+           (columns >> 3) << 17 | (128u * kCtas >> 4) << 24;
 }
 
-// One step of 16 along the contraction, by one thread for both CTAs.
+// One step of 16 along the contraction, by one thread, of a pair's first CTA for both.
 __device__ __forceinline__ void multiply(uint32_t tmem, uint64_t a, uint64_t b, uint32_t shape, bool add)
 {
     asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\n"
@@ -178,17 +211,29 @@ __device__ __forceinline__ void multiply(uint32_t tmem, uint64_t a, uint64_t b, 
 }
 
 // The same with A's 16 elements of each lane in tensor memory, two to a column.
+template <int kCtas>
 __device__ __forceinline__ void multiply(uint32_t tmem, uint32_t a, uint64_t b, uint32_t shape, bool add)
 {
+    if (kCtas == 1) {
+        asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\n"
+                     "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(tmem),
+                     "r"(a), "l"(b), "r"(shape), "r"(static_cast<uint32_t>(add))
+                     : "memory");
+        return;
+    }
     asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\n"
                  "tcgen05.mma.cta_group::2.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(tmem),
                  "r"(a), "l"(b), "r"(shape), "r"(static_cast<uint32_t>(add))
                  : "memory");
 }
 
-// Arrives on `bar` in both CTAs once every multiply issued so far is done.
-__device__ __forceinline__ void commit(uint32_t bar)
+// Arrives on `bar`, in both CTAs of a pair, once every multiply issued so far is done.
+template <int kCtas> __device__ __forceinline__ void commit(uint32_t bar)
 {
+    if (kCtas == 1) {
+        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+        return;
+    }
     asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
                  "h"(static_cast<uint16_t>(3))
                  : "memory");

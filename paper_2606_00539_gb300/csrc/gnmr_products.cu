@@ -112,7 +112,7 @@ __device__ __forceinline__ bool load_stages(const CUtensorMap &map_a, const CUte
         const bool two = b_along_columns(kOp) && (p.b_blocks || half > 64);        // blocks of B
         const uint32_t bytes = kAStage + (!b_along_columns(kOp) ? S::kBox * 128 : two ? 2 * kBlock : kBlock);
         for (int k = it.k0; k < it.k1; ++k) {
-            if (!wait(empty + stage * 8, phase))
+            if (!wait<true>(empty + stage * 8, phase))
                 return false;
             if (elected()) {
                 int at = k * kStep;
@@ -125,21 +125,21 @@ __device__ __forceinline__ bool load_stages(const CUtensorMap &map_a, const CUte
                 const uint32_t a = base + stage * S::kStage, b = a + kAStage;
                 arrive_expect(first_tail ? in_cta(bar, c.rank) : bar, bytes);
                 if (!a_along_lanes(kOp)) {
-                    load_tile(a, &map_a, at, a_lane, 0, za, bar);
+                    load_tile<2>(a, &map_a, at, a_lane, 0, za, bar);
                 } else if (p.a_blocks) {
-                    load_tile(a, &map_a, 0, at, a_lane >> 6, za, bar);
+                    load_tile<2>(a, &map_a, 0, at, a_lane >> 6, za, bar);
                 } else {
-                    load_tile(a, &map_a, a_lane, at, 0, za, bar);
-                    load_tile(a + kBlock, &map_a, a_lane + 64, at, 0, za, bar);
+                    load_tile<2>(a, &map_a, a_lane, at, 0, za, bar);
+                    load_tile<2>(a + kBlock, &map_a, a_lane + 64, at, 0, za, bar);
                 }
                 if (!b_along_columns(kOp)) {
-                    load_tile(b, &map_b, at, b_col, 0, 0, bar);
+                    load_tile<2>(b, &map_b, at, b_col, 0, 0, bar);
                 } else if (p.b_blocks) {
-                    load_tile(b, &map_b, 0, at, b_col >> 6, 0, bar);
+                    load_tile<2>(b, &map_b, 0, at, b_col >> 6, 0, bar);
                 } else {
-                    load_tile(b, &map_b, b_col, at, 0, 0, bar);
+                    load_tile<2>(b, &map_b, b_col, at, 0, 0, bar);
                     if (two)
-                        load_tile(b + kBlock, &map_b, b_col + 64, at, 0, 0, bar);
+                        load_tile<2>(b + kBlock, &map_b, b_col + 64, at, 0, 0, bar);
                 }
             }
             __syncwarp();
@@ -164,12 +164,12 @@ __device__ __forceinline__ bool multiply_stages(const Product &p, const Cta &c)
     uint32_t phase = 0, free_phase = 1;                  // free_phase: of both halves, while half is 0
     for (int i = c.pair, g = 0; i < c.items; i += c.pairs) {
         const Item it = item_of<kStep>(p, c.tables, c.split, c.lane_tiles, i, g);
-        const uint32_t idesc = shape(p.bf16, a_along_lanes(kOp), b_along_columns(kOp), it.wide);
+        const uint32_t idesc = shape<2>(p.bf16, a_along_lanes(kOp), b_along_columns(kOp), it.wide);
         const int count = it.k1 - it.k0, turn = it.tail ? min(kTailTurn, count - 1) : -1;
         const int first = stage;
         const uint32_t first_phase = phase;
         for (int k = 0; k < count;) {
-            if (!wait(drained + half * 8, free_phase))
+            if (!wait<true>(drained + half * 8, free_phase))
                 return false;
             fence_after();
             const int stop = min(count, k + p.piece / kStep);
@@ -187,7 +187,7 @@ __device__ __forceinline__ bool multiply_stages(const Product &p, const Cta &c)
                         left = it.depth % kStep;
                     }
                 }
-                if (!wait(full + at * 8, its))
+                if (!wait<true>(full + at * 8, its))
                     return false;
                 fence_after();
                 if (elected()) {
@@ -199,9 +199,9 @@ __device__ __forceinline__ bool multiply_stages(const Product &p, const Cta &c)
                         multiply(sums, a + 2 * kANext, b + 2 * kBNext, idesc, true);
                     if (left > 48)
                         multiply(sums, a + 3 * kANext, b + 3 * kBNext, idesc, true);
-                    commit(empty + at * 8);
+                    commit<2>(empty + at * 8);
                     if (k + 1 == stop)
-                        commit(done + half * 8);
+                        commit<2>(done + half * 8);
                 }
                 __syncwarp();
                 if (++stage == c.ring)
@@ -228,7 +228,7 @@ __device__ __forceinline__ bool clear_tails(const Product &p, const Cta &c)
         const Item it = item_of<kStep>(p, c.tables, c.split, c.lane_tiles, i, g);
         if (it.tail) {
             const int left = it.depth % kStep, at = stage;
-            if (!wait(smem_addr(&c.bars->tail[at]), (phase >> at) & 1))
+            if (!wait<false>(smem_addr(&c.bars->tail[at]), (phase >> at) & 1))
                 return false;
             phase ^= 1u << at;
             const int blocks = 2 + parts_of(it.wide / 2, 64), stop = (left + 15) / 16 * 16;
@@ -239,7 +239,7 @@ __device__ __forceinline__ bool clear_tails(const Product &p, const Cta &c)
             fence_async_proxy();
             __syncwarp();
             if (lane == 0)
-                arrive_release(full + at * 8);
+                arrive_release<true>(full + at * 8);
         }
         stage = (stage + it.k1 - it.k0) % c.ring;
     }
@@ -264,11 +264,11 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             barrier_init(smem_addr(&bars.empty[s]), 1);
             barrier_init(smem_addr(&bars.tail[s]), 1);
         }
-        init_epilogue_barriers(bars, 4 * Roles<kOp>::kSides);
+        init_epilogue_barriers<2>(bars, 4 * Roles<kOp>::kSides);
         barrier_init_fence();
     }
     if (warp == kMultiplyWarp)
-        tmem_alloc(smem_addr(&bars.tmem), S::kTmem);
+        tmem_alloc<2>(smem_addr(&bars.tmem), S::kTmem);
     __syncwarp();
     greet_pair();
     // Nothing above depends on the kernels before this one on the stream.
@@ -292,11 +292,11 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             fine = clear_tails<kColumns>(p, c);
     } else {
         more_registers<Roles<kOp>::kEpilogueRegisters>();
-        fine = write_outputs<kColumns, Roles<kOp>::kSides, false, kStep>(p, c);
+        fine = write_outputs<kColumns, Roles<kOp>::kSides, false, kStep, 2>(p, c);
     }
     finish_pair(fine, p.gave_up);
     if (warp == kMultiplyWarp)
-        tmem_free(c.tmem, S::kTmem);
+        tmem_free<2>(c.tmem, S::kTmem);
 }
 
 // ---- host -----------------------------------------------------------------------
@@ -357,12 +357,13 @@ gnmr_status check(const gnmr_product *p)
     return GNMR_OK;
 }
 
-// 8-bit codes: the rows are read in 8 bits too up to this many to a group, and for one group
-// while its tiles of 64 columns are few; otherwise they are widened in memory first.  5120 -> 13824, 16
-// rows: 22 us in 8 bits, 28 widened; 64 experts of 2048 -> 1408, 31 rows each: 53 and 51, 64 each: 73 and 55.
-// One group, 4096 -> 1024, 100 rows (8 tiles): 12 and 19; 2048 -> 2048, 200 (32): 12.5 and 14; 7296 -> 4352, 200
-// (68): 31 and 25.
-constexpr int64_t kFewCodes = 32, kFewCodeTiles = 48;
+// 8-bit codes: the rows are read in 8 bits too up to kFewestCodes to a group, and up to kFewCodes to a
+// group, or any number of one group, while tiles are few; otherwise they are widened in memory first.
+// Measured in 8 bits and widened, us: 5120 -> 13824, 16 rows 19.9 and 21.0, 32 rows 24.5 and 21.3; 64 experts of
+// 2048 -> 1408, 282 rows 35 and 39, 1,024 rows 45 and 44, 31 rows each 57 and 45; one group, 4096 -> 1024, 100 rows
+// (8 tiles) 11.6 and 20; 2048 -> 2048, 200 (32) 12.4 and 14.8; 7296 -> 4352, 200 (68) 56 and 27; 24 experts of
+// 1371 -> 1003, 400 rows (28) 16 and 20.  Rows to a group are an average: the counts are on the device.
+constexpr int64_t kFewestCodes = 16, kFewCodes = 32, kFewCodeTiles = 48;
 // 16-bit operands: tiles of 64 columns up to this many rows to a group, and for one group
 // while they make one round at most.  5120 -> 13824, 16 rows: 26 us so, 28 in tiles of 256; 64: 27 and 29;
 // 128: 39 and 30.  2048 -> 2048, 16 rows: 8 and 12; 200: 10 and 17.  64 experts of 1408 -> 2048, 1 row
@@ -374,7 +375,8 @@ Operands operands(const gnmr_product *p)
     const bool codes = p->op == GNMR_PRODUCT_FORWARD_I8;
     const int bytes = codes ? 1 : 2;
     const int64_t narrow = (int64_t(p->n_out) + kLanes - 1) / kLanes * ((p->rows + 63) / 64);
-    const bool few = p->rows <= kFewCodes * p->groups || (p->groups == 1 && narrow <= kFewCodeTiles);
+    const bool few = p->rows <= kFewestCodes * p->groups ||
+                     ((p->groups == 1 || p->rows <= kFewCodes * p->groups) && narrow <= kFewCodeTiles);
     const Operand x{p->d_x, p->rows, p->n_in, p->x_stride, 0, 1, bytes, codes && few ? 1 : 2};
     const Operand dy{p->d_dy, p->rows, p->n_out, p->dy_stride, 0, 1, 2, 2};
     const bool shared = p->w_group_stride == 0;          // one weight for all groups

@@ -8,8 +8,9 @@
 // memory, from where the tensor cores take an operand as well, at no cost in
 // shared-memory bandwidth (tiles of fp16 in shared memory, written and read again for each
 // tile of columns, would take more of it than there is beside the multiplies).  B, the
-// rows, are widened by two more warps where they are few, else in memory by a
-// kernel before this one.  Widening the weights in memory too, for the 16-bit kernel, was
+// rows, are widened by two more warps where they are few, and each CTA multiplies alone: what is
+// widened in shared memory is then handed over within its CTA (between CTAs that takes 2,000 cycles a
+// stage).  Else rows are widened in memory by a kernel before this one, and CTAs multiply in pairs.  Widening the weights in memory too, for the 16-bit kernel, was
 // slower at 4,001 rows to a group (5120 -> 13824: 380 us, this way 321).
 #include <algorithm>
 #include <cstring>
@@ -47,12 +48,13 @@ constexpr int kControlRegisters = 56, kEpilogueRegisters = 136, kWidenRegisters 
 static_assert(128 * kControlRegisters + 256 * kEpilogueRegisters + 256 * kWidenRegisters <= kThreads * 96, "registers of the launch");
 constexpr int kAStage = 128 * kStep, kSlots = 4, kFirstA = 256, kTmem = 512;
 
-// kWide: B comes in 16 bits, and a tile has up to 128 columns; else up to 64, widened
-// here.  Widened: A behind the sums in tensor memory, 64 columns of two steps each; B in
+// kWide: B comes in 16 bits, and a tile has up to 128 columns; else up to 32, widened here
+// (up to 64 leave room for fewer stages: one token through 5120 -> 13824 23.9 us, 18.6 so).  Widened: A behind the sums in tensor memory, 64 columns of two steps each; B in
 // shared memory, as two tiles of 64 steps.
 template <bool kWide> struct Shape {
-    static constexpr int kColumns = kWide ? 128 : 64;
-    static constexpr int kBRows = kColumns / 2, kBTile = kBRows * 128;
+    static constexpr int kCtas = kWide ? 2 : 1;        // that multiply as one
+    static constexpr int kColumns = kWide ? 128 : 32;
+    static constexpr int kBRows = kColumns / kCtas, kBTile = kBRows * 128;
     static constexpr int kStage = kAStage + (kWide ? 2 : 1) * kBTile;
     static constexpr int kSlot = 2 * kBTile;           // B widened, before the stages
     static constexpr int kWidened = kWide ? 0 : kSlots * kSlot;
@@ -69,22 +71,22 @@ __device__ __forceinline__ bool load_stages(const CUtensorMap &map_a, const CUte
     uint32_t phase = 1;
     for (int i = c.pair, g = 0; i < c.items; i += c.pairs) {
         const Item it = item_of<kStep>(p, c.tables, c.split, c.lane_tiles, i, g);
-        const int half = it.wide / 2;
-        const int a_lane = it.lane0 + c.rank * 128, b_col = it.row0 + it.col0 + c.rank * half, za = p.a_by_group ? it.g : 0;
+        const int a_lane = it.lane0 + c.rank * 128, za = p.a_by_group ? it.g : 0;
+        const int b_col = it.row0 + it.col0 + (kWide ? c.rank * (it.wide / 2) : 0);
         for (int k = it.k0; k < it.k1; ++k) {
-            if (!wait(empty + stage * 8, phase))
+            if (!wait<kWide>(empty + stage * 8, phase))
                 return false;
             if (elected()) {
                 const uint32_t bar = full + stage * 8, a = base + stage * S::kStage, b = a + kAStage;
                 if (kWide) {
                     arrive_expect(own + stage * 8, kAStage);
                     arrive_expect(full_b + stage * 8, 2 * S::kBTile);
-                    load_tile(a, &map_a, k * kStep, a_lane, 0, za, bar);
-                    load_tile(b, &map_b, 0, b_col, 2 * k, 0, full_b + stage * 8);
+                    load_tile<S::kCtas>(a, &map_a, k * kStep, a_lane, 0, za, bar);
+                    load_tile<S::kCtas>(b, &map_b, 0, b_col, 2 * k, 0, full_b + stage * 8);
                 } else {
                     arrive_expect(own + stage * 8, S::kStage);
-                    load_tile(a, &map_a, k * kStep, a_lane, 0, za, bar);
-                    load_tile(b, &map_b, k * kStep, b_col, 0, 0, bar);
+                    load_tile<S::kCtas>(a, &map_a, k * kStep, a_lane, 0, za, bar);
+                    load_tile<S::kCtas>(b, &map_b, k * kStep, b_col, 0, 0, bar);
                 }
             }
             __syncwarp();
@@ -109,7 +111,7 @@ __device__ __forceinline__ bool widen_a(const Product &p, const Cta &c)
     constexpr int kStage = Shape<kWide>::kStage;
     const int warp = threadIdx.x / 32 - kFirstWidenWarp, lane = threadIdx.x & 31, quarter = warp & 3, team = warp >> 2;
     const uint32_t full = smem_addr(&c.bars->full[0]), empty = in_cta(smem_addr(&c.bars->empty[0]), c.rank);
-    const uint32_t used = smem_addr(&c.bars->used[0]), ready = in_cta(smem_addr(&c.bars->ready[0]), 0);
+    const uint32_t used = smem_addr(&c.bars->used[0]), ready = in_cta(smem_addr(&c.bars->ready[0]), kWide ? 0 : c.rank);
     const int row = quarter * 32 + lane;
     const uint8_t *raw = c.stages + Shape<kWide>::kWidened + row * 128;
     int stage = team, slot = team;                     // every other stage, from the team's first
@@ -119,7 +121,7 @@ __device__ __forceinline__ bool widen_a(const Product &p, const Cta &c)
         const Item it = item_of<kStep>(p, c.tables, c.split, c.lane_tiles, i, g);
         int k = it.k0 + skip;
         for (; k < it.k1; k += 2) {
-            if (!wait(full + stage * 8, phase) || !wait(used + slot * 8, slot_phase))
+            if (!wait<false>(full + stage * 8, phase) || !wait<kWide>(used + slot * 8, slot_phase))
                 return false;
             fence_after();
 #pragma unroll
@@ -140,7 +142,7 @@ __device__ __forceinline__ bool widen_a(const Product &p, const Cta &c)
             }
             __syncwarp();
             if (lane == 0)
-                arrive(empty + stage * 8);
+                arrive_release(empty + stage * 8);
             store_wait();
             fence_before();
             __syncwarp();
@@ -161,17 +163,15 @@ __device__ __forceinline__ bool widen_b(const Product &p, const Cta &c)
     constexpr int kStage = S::kStage, kSlot = S::kSlot, kBTile = S::kBTile;
     const int lane = threadIdx.x & 31, turn = threadIdx.x / 32 - kFirstBWarp, chunk = lane & 7;
     const uint32_t full = smem_addr(&c.bars->full[0]), empty = in_cta(smem_addr(&c.bars->empty[0]), c.rank);
-    const uint32_t used = smem_addr(&c.bars->used[0]), ready = in_cta(smem_addr(&c.bars->ready[0]), 0);
+    const uint32_t used = smem_addr(&c.bars->used[0]), ready = in_cta(smem_addr(&c.bars->ready[0]), c.rank);
     int stage = turn, slot = turn, skip = turn;
     uint32_t phase = 0, slot_phase = 1;
     for (int i = c.pair, g = 0; i < c.items; i += c.pairs) {
         const Item it = item_of<kStep>(p, c.tables, c.split, c.lane_tiles, i, g);
-        const int half = it.wide / 2;
-        // rows beyond these are columns that nobody reads
-        const int rows = min(half, it.cols - static_cast<int>(c.rank) * half);
+        const int rows = it.cols;                      // those beyond are columns that nobody reads
         int k = it.k0 + skip;
         for (; k < it.k1; k += 2) {
-            if (!wait(full + stage * 8, phase) || !wait(used + slot * 8, slot_phase))
+            if (!wait<false>(full + stage * 8, phase) || !wait<false>(used + slot * 8, slot_phase))
                 return false;
             const uint8_t *raw = c.stages + S::kWidened + stage * kStage + kAStage;
             uint8_t *to = c.stages + slot * kSlot + (chunk >> 2) * kBTile;
@@ -186,7 +186,7 @@ __device__ __forceinline__ bool widen_b(const Product &p, const Cta &c)
             fence_async_proxy();
             __syncwarp();
             if (lane == 0) {
-                arrive(empty + stage * 8);
+                arrive_release(empty + stage * 8);
                 arrive_release(ready + slot * 8);
             }
             two_on(stage, phase, c.ring);
@@ -209,15 +209,15 @@ __device__ __forceinline__ bool multiply_slots(const Product &p, const Cta &c)
     uint32_t phase = 0, stage_phase = 0, free_phase = 1;
     for (int i = c.pair, g = 0; i < c.items; i += c.pairs) {
         const Item it = item_of<kStep>(p, c.tables, c.split, c.lane_tiles, i, g);
-        const uint32_t idesc = shape(false, false, false, it.wide);
+        const uint32_t idesc = shape<S::kCtas>(false, false, false, it.wide);
         for (int k = it.k0; k < it.k1;) {
-            if (!wait(drained + half * 8, free_phase))
+            if (!wait<kWide>(drained + half * 8, free_phase))
                 return false;
             fence_after();
             const int stop = min(it.k1, k + p.piece / kStep);
             const uint32_t sums = c.tmem + half * S::kColumns;
             for (bool add = false; k < stop; ++k, add = true) {
-                if ((kWide && !wait(full_b + stage * 8, stage_phase)) || !wait(ready + slot * 8, phase))
+                if ((kWide && !wait<true>(full_b + stage * 8, stage_phase)) || !wait<kWide>(ready + slot * 8, phase))
                     return false;
                 fence_after();
                 if (elected()) {
@@ -225,12 +225,12 @@ __device__ __forceinline__ bool multiply_slots(const Product &p, const Cta &c)
                     const uint64_t b = first_b + (kWide ? stage * (S::kStage >> 4) : slot * (S::kSlot >> 4));
 #pragma unroll
                     for (int q = 0; q < kStep / 16; ++q)
-                        multiply(sums, a + q * 8, b + (q >> 2) * (S::kBTile >> 4) + (q & 3) * 2, idesc, q > 0 || add);
-                    commit(used + slot * 8);
+                        multiply<S::kCtas>(sums, a + q * 8, b + (q >> 2) * (S::kBTile >> 4) + (q & 3) * 2, idesc, q > 0 || add);
+                    commit<S::kCtas>(used + slot * 8);
                     if (kWide)
-                        commit(empty + stage * 8);
+                        commit<S::kCtas>(empty + stage * 8);
                     if (k + 1 == stop)
-                        commit(done + half * 8);
+                        commit<S::kCtas>(done + half * 8);
                 }
                 __syncwarp();
                 if (++slot == kSlots)
@@ -264,14 +264,14 @@ codes_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
             barrier_init(smem_addr(&bars.tail[s]), 2);                           // B in 16 bits: in the first CTA, from both
         }
         for (int s = 0; s < kSlots; ++s) {
-            barrier_init(smem_addr(&bars.ready[s]), 2 * (kWidenWarps / 2 + (kWide ? 0 : 1)));    // likewise
+            barrier_init(smem_addr(&bars.ready[s]), kWide ? 2 * (kWidenWarps / 2) : kWidenWarps / 2 + 1);      // likewise; this CTA's
             barrier_init(smem_addr(&bars.used[s]), 1);
         }
-        init_epilogue_barriers(bars, 4 * kSides);
+        init_epilogue_barriers<S::kCtas>(bars, 4 * kSides);
         barrier_init_fence();
     }
     if (warp == kMultiplyWarp)
-        tmem_alloc(smem_addr(&bars.tmem), kTmem);
+        tmem_alloc<S::kCtas>(smem_addr(&bars.tmem), kTmem);
     __syncwarp();
     greet_pair();
     // Nothing above depends on the kernels before this one on the stream.
@@ -289,20 +289,20 @@ codes_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
         fewer_registers<kControlRegisters>();
         if (warp == kProducerWarp)
             fine = load_stages<kWide>(map_a, map_b, p, c);
-        else if (warp == kMultiplyWarp && c.rank == 0)
+        else if (warp == kMultiplyWarp && (c.rank == 0 || !kWide))
             fine = multiply_slots<kWide>(p, c);
         else if (!kWide && warp >= kFirstBWarp)
             fine = widen_b(p, c);
     } else if (warp < kFirstWidenWarp) {
         more_registers<kEpilogueRegisters>();
-        fine = write_outputs<S::kColumns, kSides, true, kStep>(p, c);
+        fine = write_outputs<S::kColumns, kSides, true, kStep, S::kCtas>(p, c);
     } else {
         fewer_registers<kWidenRegisters>();
         fine = widen_a<kWide>(p, c);
     }
     finish_pair(fine, p.gave_up);
     if (warp == kMultiplyWarp)
-        tmem_free(c.tmem, kTmem);
+        tmem_free<S::kCtas>(c.tmem, kTmem);
 }
 
 template <bool kWide>

@@ -197,7 +197,7 @@ struct Barriers {
     uint64_t full[kMostStages], empty[kMostStages];      // stages of operands
     uint64_t tail[kMostStages];        // a stage that the tail warp looks at first
     uint64_t ready[4], used[4];        // operands widened from 8 bits
-    uint64_t done[2], drained[2];      // halves of tensor memory; `drained` counts in the first CTA
+    uint64_t done[2], drained[2];      // halves of tensor memory; in a pair `drained` counts in the first CTA
     uint32_t tmem;
 };
 
@@ -404,12 +404,13 @@ __device__ __forceinline__ void add_to_sum(uint32_t (&acc)[16], const uint32_t (
                         : __float_as_uint(__uint_as_float(acc[j]) + __uint_as_float(v[j]));
 }
 
-// The barriers that the epilogue counts on.
+// The barriers that the epilogue counts on, of `warps` warps a CTA.
+template <int kCtas>
 __device__ __forceinline__ void init_epilogue_barriers(Barriers &b, int warps)
 {
     for (int h = 0; h < 2; ++h) {
         barrier_init(smem_addr(&b.done[h]), 1);
-        barrier_init(smem_addr(&b.drained[h]), 2 * warps);
+        barrier_init(smem_addr(&b.drained[h]), kCtas * warps);
     }
 }
 
@@ -492,14 +493,14 @@ __device__ __forceinline__ bool join_parts(const Product &p, const Cta &c, const
 }
 
 // The epilogue's warps, four (one to 32 lanes) for each of kSides shares of a tile's columns: its
-// pieces added up and written.
-template <int kColumns, int kSides, bool kCodes, int kStep>
+// pieces added up and written.  kCtas: those that multiply as one.
+template <int kColumns, int kSides, bool kCodes, int kStep, int kCtas>
 __device__ __forceinline__ bool write_outputs(const Product &p, const Cta &c)
 {
     constexpr int kPieces = kColumns / 16 / kSides;      // of 16 columns
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int quarter = warp & 3, side = (warp - kFirstEpilogueWarp) >> 2;
-    const uint32_t done = smem_addr(&c.bars->done[0]), drained = in_cta(smem_addr(&c.bars->drained[0]), 0);
+    const uint32_t done = smem_addr(&c.bars->done[0]), drained = in_cta(smem_addr(&c.bars->drained[0]), kCtas == 2 ? 0 : c.rank);
     int half = 0;
     uint32_t phase = 0;
     for (int i = c.pair, g = 0; i < c.items; i += c.pairs) {
@@ -516,7 +517,7 @@ __device__ __forceinline__ bool write_outputs(const Product &p, const Cta &c)
                 for (int j = 0; j < 16; ++j)
                     acc[q][j] = 0;
         for (int k = it.k0; k < it.k1; k += p.piece / kStep) {
-            if (!wait(done + half * 8, phase))
+            if (!wait<kCtas == 2>(done + half * 8, phase))
                 return false;
             fence_after();
             const uint32_t from = c.tmem + half * kColumns + (uint32_t(quarter * 32) << 16) + col;

@@ -75,3 +75,40 @@ def test_column_codes_of_clusters_whose_ctas_end_at_different_times(products):
         assert np.array_equal(q.cpu().numpy(), wq) and np.array_equal(s.cpu().numpy(), ws)
         for q2, s2 in [products.quantize_columns(x) for _ in range(50)]:
             assert torch.equal(q, q2) and torch.equal(s, s2)
+
+
+def test_cleared_tails_of_both_ctas_reach_the_multiplies(products):
+    """Groups of rows that end inside a stage, infinities in the rows after them, over hundreds of tiles:
+    both CTAs of a pair clear their half of such a stage, and the first one's multiplies read both."""
+    counts = [70, 1, 131, 64, 193, 5, 0, 257, 63, 65, 130, 17]
+    g, t, G, R, n, k = gen(21), torch.bfloat16, 12, sum(counts), 1000, 1544
+    x, dy = normal(g, R, k, dtype=t), normal(g, R, n, dtype=t)
+    off = offsets_of(counts)
+    want = {e: (dy[at].double().T @ x[at].double(), dy[at].double().abs().T @ x[at].double().abs()) for e, at in spans(counts)}
+    for odd in (0, 1):                                           # every other group's rows, in turn, are infinities
+        x2, dy2 = x.clone(), dy.clone()
+        for e, at in spans(counts):
+            if e % 2 == odd:
+                x2[at], dy2[at] = float("inf"), float("-inf")
+        first = products.weight_grad(dy2, x2, off, out=torch.empty(G, n, k, device="cuda"))
+        for e, at in spans(counts):
+            if e % 2 != odd:
+                check(first[e], *want[e], counts[e], "f32")
+        for _ in range(20):
+            again = products.weight_grad(dy2, x2, off, out=torch.empty(G, n, k, device="cuda"))
+            assert torch.equal(torch.nan_to_num(again), torch.nan_to_num(first))
+
+
+@pytest.mark.parametrize("counts,n,k", [([3, 1, 40, 0, 7, 16, 2, 33, 1, 5, 12, 31, 9, 4, 1, 30], 2000, 1400),
+                                        ([1], 30000, 1500), ([90], 1100, 3000), ([1] * 700, 300, 136)])
+def test_few_rows_of_codes_over_many_tiles(products, counts, n, k):
+    """Rows that are widened on the SM, over more tiles than there are SMs: every output."""
+    g, G, R = gen(n), len(counts), sum(counts)
+    held = -(-k // 16) * 16
+    xq = torch.randint(-128, 128, (R, held), device="cuda", generator=g, dtype=torch.int8)[:, :k]
+    wq = torch.randint(-128, 128, (G, n, held), device="cuda", generator=g, dtype=torch.int8)[..., :k]
+    off, xs, ws = offsets_of(counts), torch.ones(R, device="cuda"), torch.ones(G, n, device="cuda")
+    for _ in range(5):
+        y = products.forward_i8(xq, xs, wq, ws, off, out_dtype="f32")
+        for e, at in spans(counts):
+            assert torch.equal(y[at], (xq[at].double() @ wq[e].double().T).float())
