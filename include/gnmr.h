@@ -468,15 +468,26 @@ gnmr_status gnmr_products_create(int32_t device, gnmr_products **out);
 
 /* Enqueues one product on `stream`.  Errors: GNMR_ERR_INVALID_ARG,
  * GNMR_ERR_LAYOUT (strides, alignment, or scratch too small), GNMR_ERR_CUDA,
- * GNMR_ERR_STATE (an earlier product of this handle gave up waiting inside the
- * GPU; its output is not valid); detail via gnmr_last_error(NULL). */
+ * GNMR_ERR_STATE (see gnmr_products_status); detail via gnmr_last_error(NULL). */
 gnmr_status gnmr_products_run(gnmr_products *h, const gnmr_product *p, void *stream);
 
 /* Scratch that gnmr_products_run needs for *p (d_scratch and scratch_bytes are
  * not read).  Makes no CUDA call.  Errors: GNMR_ERR_INVALID_ARG, GNMR_ERR_LAYOUT. */
 gnmr_status gnmr_products_scratch_bytes(const gnmr_product *p, int64_t *bytes);
 
-/* Waits for the handle's device and frees the handle.  NULL is accepted. */
+/* GNMR_ERR_STATE once a product of this handle has given up waiting inside the GPU, GNMR_OK
+ * before.  Its output is not valid, nor are those after it, and the handle takes no more products.
+ * Waits for nothing: for the products enqueued so far, synchronize with their stream first. */
+gnmr_status gnmr_products_status(gnmr_products *h);
+
+/* The longest that one wait inside a product's kernels may take, from the next product on.  Negative, as
+ * at first: many times what the product's sizes need, two seconds at the least.  No call that is
+ * otherwise right reaches that; with a limit below what a product takes it gives up, with 0 at the first
+ * wait. */
+gnmr_status gnmr_products_set_wait_limit(gnmr_products *h, int64_t nanoseconds);
+
+/* Waits for the handle's device and frees the handle.  NULL is accepted.  GNMR_ERR_STATE, the handle
+ * freed all the same, where gnmr_products_status says so. */
 gnmr_status gnmr_products_destroy(gnmr_products *h);
 
 /* 8-bit codes of `groups` [rows x cols] matrices (BF16, F16 or F32; strides in

@@ -153,6 +153,8 @@ PROTOTYPES = {
     "gnmr_products_create": (ctypes.c_int, [ctypes.c_int32, ctypes.POINTER(_P)]),
     "gnmr_products_run": (ctypes.c_int, [_P, _P, _P]),
     "gnmr_products_scratch_bytes": (ctypes.c_int, [_P, _P]),
+    "gnmr_products_status": (ctypes.c_int, [_P]),
+    "gnmr_products_set_wait_limit": (ctypes.c_int, [_P, ctypes.c_int64]),
     "gnmr_products_destroy": (ctypes.c_int, [_P]),
     "gnmr_quantize_rows": (ctypes.c_int, [_P, ctypes.c_int32, ctypes.c_int32, ctypes.c_int64, ctypes.c_int64,
                                           ctypes.c_int64, ctypes.c_int64, _P, ctypes.c_int64, _P,
@@ -315,6 +317,14 @@ def gnmr_products_scratch_bytes(p: gnmr_product) -> int:
     n = ctypes.c_int64(0)
     _check(load().gnmr_products_scratch_bytes(ctypes.addressof(p), ctypes.addressof(n)), None)
     return n.value
+
+
+def gnmr_products_status(handle: int) -> None:
+    _check(load().gnmr_products_status(handle), None)
+
+
+def gnmr_products_set_wait_limit(handle: int, nanoseconds: int) -> None:
+    _check(load().gnmr_products_set_wait_limit(handle, nanoseconds), None)
 
 
 def gnmr_products_destroy(handle: int) -> None:

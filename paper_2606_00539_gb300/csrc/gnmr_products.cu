@@ -112,7 +112,7 @@ __device__ __forceinline__ bool load_stages(const CUtensorMap &map_a, const CUte
         const bool two = b_along_columns(kOp) && (p.b_blocks || half > 64);        // blocks of B
         const uint32_t bytes = kAStage + (!b_along_columns(kOp) ? S::kBox * 128 : two ? 2 * kBlock : kBlock);
         for (int k = it.k0; k < it.k1; ++k) {
-            if (!wait<true>(empty + stage * 8, phase))
+            if (!wait<true>(empty + stage * 8, phase, p.most_ns))
                 return false;
             if (elected()) {
                 int at = k * kStep;
@@ -169,7 +169,7 @@ __device__ __forceinline__ bool multiply_stages(const Product &p, const Cta &c)
         const int first = stage;
         const uint32_t first_phase = phase;
         for (int k = 0; k < count;) {
-            if (!wait<true>(drained + half * 8, free_phase))
+            if (!wait<true>(drained + half * 8, free_phase, p.most_ns))
                 return false;
             fence_after();
             const int stop = min(count, k + p.piece / kStep);
@@ -187,7 +187,7 @@ __device__ __forceinline__ bool multiply_stages(const Product &p, const Cta &c)
                         left = it.depth % kStep;
                     }
                 }
-                if (!wait<true>(full + at * 8, its))
+                if (!wait<true>(full + at * 8, its, p.most_ns))
                     return false;
                 fence_after();
                 if (elected()) {
@@ -228,7 +228,7 @@ __device__ __forceinline__ bool clear_tails(const Product &p, const Cta &c)
         const Item it = item_of<kStep>(p, c.tables, c.split, c.lane_tiles, i, g);
         if (it.tail) {
             const int left = it.depth % kStep, at = stage;
-            if (!wait<false>(smem_addr(&c.bars->tail[at]), (phase >> at) & 1))
+            if (!wait<false>(smem_addr(&c.bars->tail[at]), (phase >> at) & 1, p.most_ns))
                 return false;
             phase ^= 1u << at;
             const int blocks = 2 + parts_of(it.wide / 2, 64), stop = (left + 15) / 16 * 16;
@@ -309,7 +309,26 @@ gnmr_status fail(gnmr_status s, const char *why)
 
 bool sixteen(int32_t dtype) { return dtype == GNMR_DTYPE_BF16 || dtype == GNMR_DTYPE_F16; }
 
+gnmr_status gave_up(const gnmr_products *h)
+{
+    if (*static_cast<volatile int *>(h->gave_up))
+        return fail(GNMR_ERR_STATE, "products: a product of this handle gave up waiting inside the GPU");
+    return GNMR_OK;
+}
+
 bool misaligned(const void *p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes != 0; }
+
+// How long a wait inside the kernel may take.  One warp's can span all the others' work (that for the
+// last stage that rows end in, or past tiles that are only written), so it is many times the whole
+// call's: padded multiplies at a ninth of the tensor cores' rate, padded outputs at a hundredth of memory's, and two
+// seconds, in which all that memory holds is read thirty times.
+int64_t most_ns(const gnmr_product *p, const Product &q, int64_t lane_tiles)
+{
+    const double lanes = double(lane_tiles) * kLanes, more = 256.0 * q.groups;
+    const double cols = q.cols ? q.cols + 256.0 : double(p->rows) + more, depth = q.depth ? q.depth : double(p->rows) + more;
+    const double outputs = lanes * cols * (q.cols ? q.groups : 1);
+    return static_cast<int64_t>(std::min(2e9 + lanes * cols * depth / 1e5 + outputs / 10, 9e18));
+}
 
 gnmr_status check(const gnmr_product *p)
 {
@@ -541,8 +560,8 @@ gnmr_status gnmr_products_run(gnmr_products *h, const gnmr_product *p, void *str
         return fail(GNMR_ERR_INVALID_ARG, "products: NULL handle");
     if (const gnmr_status s = check(p))
         return s;
-    if (*static_cast<volatile int *>(h->gave_up))
-        return fail(GNMR_ERR_STATE, "products: an earlier product gave up waiting inside the GPU");
+    if (const gnmr_status s = gave_up(h))
+        return s;
     const bool codes = p->op == GNMR_PRODUCT_FORWARD_I8, wgrad = p->op == GNMR_PRODUCT_WEIGHT_GRAD;
     if (p->rows == 0 && (!wgrad || p->add))
         return GNMR_OK;
@@ -581,6 +600,7 @@ gnmr_status gnmr_products_run(gnmr_products *h, const gnmr_product *p, void *str
     q.parts = h->parts;
     q.tickets = h->tickets;
     q.gave_up = h->gave_up;
+    q.most_ns = h->wait_ns < 0 ? most_ns(p, q, lane_tiles) : h->wait_ns;
 
     int prev = h->device;
     cudaGetDevice(&prev);
@@ -612,6 +632,21 @@ gnmr_status gnmr_products_run(gnmr_products *h, const gnmr_product *p, void *str
     return GNMR_OK;
 }
 
+gnmr_status gnmr_products_status(gnmr_products *h)
+{
+    if (!h)
+        return fail(GNMR_ERR_INVALID_ARG, "products: NULL handle");
+    return gave_up(h);
+}
+
+gnmr_status gnmr_products_set_wait_limit(gnmr_products *h, int64_t nanoseconds)
+{
+    if (!h)
+        return fail(GNMR_ERR_INVALID_ARG, "products: NULL handle");
+    h->wait_ns = nanoseconds;
+    return GNMR_OK;
+}
+
 gnmr_status gnmr_products_destroy(gnmr_products *h)
 {
     if (!h)
@@ -619,14 +654,16 @@ gnmr_status gnmr_products_destroy(gnmr_products *h)
     int prev = 0;
     cudaGetDevice(&prev);
     cudaSetDevice(h->device);
-    cudaError_t e = h->dmem ? cudaFree(h->dmem) : cudaSuccess;
+    cudaError_t e = h->dmem ? cudaFree(h->dmem) : cudaSuccess;      // waits for the device
+    gnmr_status status = GNMR_OK;
     if (h->gave_up) {
+        status = gave_up(h);
         const cudaError_t f = cudaFreeHost(h->gave_up);
         e = e == cudaSuccess ? f : e;
     }
     cudaSetDevice(prev);
     delete h;
-    return e == cudaSuccess ? GNMR_OK : GNMR_ERR_CUDA;
+    return e == cudaSuccess ? status : GNMR_ERR_CUDA;
 }
 
 }  // extern "C"

@@ -15,6 +15,7 @@ struct gnmr_products {
     float *parts = nullptr;            // [kMaxParts][kPartFloats]
     unsigned *tickets = nullptr;       // [kMaxParts][2][kMostEpilogueWarps], 0 between calls
     int *gave_up = nullptr;            // host memory that the kernels can write
+    int64_t wait_ns = -1;              // limit of a wait; negative: by the call's sizes
     void *dmem = nullptr;
     CUresult (*encode)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
                        const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,

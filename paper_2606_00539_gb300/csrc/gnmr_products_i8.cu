@@ -74,7 +74,7 @@ __device__ __forceinline__ bool load_stages(const CUtensorMap &map_a, const CUte
         const int a_lane = it.lane0 + c.rank * 128, za = p.a_by_group ? it.g : 0;
         const int b_col = it.row0 + it.col0 + (kWide ? c.rank * (it.wide / 2) : 0);
         for (int k = it.k0; k < it.k1; ++k) {
-            if (!wait<kWide>(empty + stage * 8, phase))
+            if (!wait<kWide>(empty + stage * 8, phase, p.most_ns))
                 return false;
             if (elected()) {
                 const uint32_t bar = full + stage * 8, a = base + stage * S::kStage, b = a + kAStage;
@@ -121,7 +121,7 @@ __device__ __forceinline__ bool widen_a(const Product &p, const Cta &c)
         const Item it = item_of<kStep>(p, c.tables, c.split, c.lane_tiles, i, g);
         int k = it.k0 + skip;
         for (; k < it.k1; k += 2) {
-            if (!wait<false>(full + stage * 8, phase) || !wait<kWide>(used + slot * 8, slot_phase))
+            if (!wait<false>(full + stage * 8, phase, p.most_ns) || !wait<kWide>(used + slot * 8, slot_phase, p.most_ns))
                 return false;
             fence_after();
 #pragma unroll
@@ -171,7 +171,7 @@ __device__ __forceinline__ bool widen_b(const Product &p, const Cta &c)
         const int rows = it.cols;                      // those beyond are columns that nobody reads
         int k = it.k0 + skip;
         for (; k < it.k1; k += 2) {
-            if (!wait<false>(full + stage * 8, phase) || !wait<false>(used + slot * 8, slot_phase))
+            if (!wait<false>(full + stage * 8, phase, p.most_ns) || !wait<false>(used + slot * 8, slot_phase, p.most_ns))
                 return false;
             const uint8_t *raw = c.stages + S::kWidened + stage * kStage + kAStage;
             uint8_t *to = c.stages + slot * kSlot + (chunk >> 2) * kBTile;
@@ -211,13 +211,13 @@ __device__ __forceinline__ bool multiply_slots(const Product &p, const Cta &c)
         const Item it = item_of<kStep>(p, c.tables, c.split, c.lane_tiles, i, g);
         const uint32_t idesc = shape<S::kCtas>(false, false, false, it.wide);
         for (int k = it.k0; k < it.k1;) {
-            if (!wait<kWide>(drained + half * 8, free_phase))
+            if (!wait<kWide>(drained + half * 8, free_phase, p.most_ns))
                 return false;
             fence_after();
             const int stop = min(it.k1, k + p.piece / kStep);
             const uint32_t sums = c.tmem + half * S::kColumns;
             for (bool add = false; k < stop; ++k, add = true) {
-                if ((kWide && !wait<true>(full_b + stage * 8, stage_phase)) || !wait<kWide>(ready + slot * 8, phase))
+                if ((kWide && !wait<true>(full_b + stage * 8, stage_phase, p.most_ns)) || !wait<kWide>(ready + slot * 8, phase, p.most_ns))
                     return false;
                 fence_after();
                 if (elected()) {

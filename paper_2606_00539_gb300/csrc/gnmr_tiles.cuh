@@ -46,6 +46,7 @@ struct Product {
     float *parts;
     unsigned *tickets;
     int *gave_up;
+    uint64_t most_ns;                  // of every wait
 };
 
 // ---- work: tiles of every group, and their parts --------------------------------
@@ -429,19 +430,17 @@ __device__ __forceinline__ void join_pair()
     fence_after();
 }
 
-// The end of every kernel: both CTAs of a pair are through, and a role that gave up has
-// said so.  Loads that it left behind are in long before the wait is over.
+// The end of every kernel: both CTAs of a pair are through, and one with a role that gave up
+// says so, and stays until the loads and multiplies that it left behind, microseconds' work, are over.
 __device__ __forceinline__ void finish_pair(bool fine, int *gave_up)
 {
-    __syncwarp();
-    if (!fine) {
-        if ((threadIdx.x & 31) == 0)
+    fence_before();
+    if (__syncthreads_or(!fine)) {
+        if (threadIdx.x == 0)
             *gave_up = 1;
-        for (int i = 0; i < 1000; ++i)
+        for (const uint64_t since = nanoseconds(); nanoseconds() - since < 1000000;)
             __nanosleep(1000);
     }
-    fence_before();
-    __syncthreads();
     cluster_sync();
     fence_after();
 }
@@ -517,7 +516,7 @@ __device__ __forceinline__ bool write_outputs(const Product &p, const Cta &c)
                 for (int j = 0; j < 16; ++j)
                     acc[q][j] = 0;
         for (int k = it.k0; k < it.k1; k += p.piece / kStep) {
-            if (!wait<kCtas == 2>(done + half * 8, phase))
+            if (!wait<kCtas == 2>(done + half * 8, phase, p.most_ns))
                 return false;
             fence_after();
             const uint32_t from = c.tmem + half * kColumns + (uint32_t(quarter * 32) << 16) + col;

@@ -63,9 +63,17 @@ class ExpertProducts:
 
     # -- lifetime -----------------------------------------------------------
     def close(self) -> None:
+        """Waits for the device and frees the handle; raises what :meth:`check` does."""
         if self._h:
-            N.gnmr_products_destroy(self._h)
-            self._h = None
+            h, self._h = self._h, None
+            N.gnmr_products_destroy(h)
+
+    def check(self) -> None:
+        """Raises GnmrError if a product gave up waiting inside the GPU (its output is not valid, and
+        no further product is taken).  Waits for nothing: synchronize first for the products enqueued so far."""
+        if not self._h:
+            raise ValueError("the products were closed")
+        N.gnmr_products_status(self._h)
 
     def __enter__(self):
         return self

@@ -3,7 +3,7 @@ may touch.  Tolerances are those of test_gpu_products."""
 import numpy as np
 import pytest
 
-from paper_2606_00539_gb300 import ExpertProducts
+from paper_2606_00539_gb300 import ExpertProducts, GnmrError
 from paper_2606_00539_gb300 import _native as N
 
 pytestmark = pytest.mark.gpu
@@ -112,3 +112,41 @@ def test_few_rows_of_codes_over_many_tiles(products, counts, n, k):
         y = products.forward_i8(xq, xs, wq, ws, off, out_dtype="f32")
         for e, at in spans(counts):
             assert torch.equal(y[at], (xq[at].double() @ wq[e].double().T).float())
+
+
+CALLS = {                                                        # each kernel; rows that end inside a stage among them
+    "few rows": lambda p, a: p.forward(a["x"][:9], a["w"], a["few"]),
+    "many rows": lambda p, a: p.forward(a["x"], a["w"], a["off"]),
+    "input gradient": lambda p, a: p.input_grad(a["dy"], a["w"], a["off"]),
+    "weight gradient": lambda p, a: p.weight_grad(a["dy"], a["x"], a["off"], out=torch.empty(4, 700, 1100, device="cuda")),
+    "few codes": lambda p, a: p.forward_i8(a["xq"][:9], a["xs"][:9], a["wq"], a["ws"], a["few"]),
+    "many codes": lambda p, a: p.forward_i8(a["xq"], a["xs"], a["wq"], a["ws"], a["off"]),
+}
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_a_wait_that_runs_out_ends_the_product_and_is_reported(name):
+    """With no time to wait for their first loads, all roles of the kernel give up.  The kernel ends, the
+    handle says so and takes no more products, and another handle, on the same context, is not affected."""
+    g, t = gen(31), torch.bfloat16
+    a = dict(x=normal(g, 900, 1100, dtype=t), dy=normal(g, 900, 700, dtype=t), w=normal(g, 4, 700, 1100, dtype=t),
+             off=offsets_of([300, 299, 1, 300]), few=offsets_of([3, 0, 5, 1]))
+    with ExpertProducts(device=0) as fine:
+        a["xq"], a["xs"] = fine.quantize_rows(a["x"])
+        a["wq"], a["ws"] = fine.quantize_rows(a["w"])
+        want = CALLS[name](fine, a)
+        fine.check()
+        p = ExpertProducts(device=0)
+        N.gnmr_products_set_wait_limit(p._h, 0)
+        CALLS[name](p, a)
+        torch.cuda.synchronize()
+        for call in (p.check, lambda: CALLS[name](p, a), p.close):
+            with pytest.raises(GnmrError) as e:
+                call()
+            assert e.value.status == N.GNMR_ERR_STATE and "gave up" in e.value.detail
+        p.close()
+        assert torch.equal(CALLS[name](fine, a), want)
+        N.gnmr_products_set_wait_limit(fine._h, 10 ** 9)
+        assert torch.equal(CALLS[name](fine, a), want)
+        torch.cuda.synchronize()
+        fine.check()
