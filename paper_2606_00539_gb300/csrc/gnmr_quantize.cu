@@ -280,11 +280,12 @@ __global__ void __launch_bounds__(kThreads) rows_by_element_kernel(Matrix m)
 // flight; a lane has 4 rows of a chunk, so that a warp's 4-byte words of codes are 128
 // contiguous bytes of a transposed row, with no exchange between warps (through tiles
 // that the CTA transposed together, with two barriers each, 64 x 1408 x 2048 took 132 us).
-// Maxima first, joined over the cluster through distributed shared memory, then
+// Maxima first, written to every CTA of the cluster through distributed shared memory (read there
+// instead, no CTA might end before all had read: a second barrier, 98 us for 95 below), then
 // the codes, last chunks first: parts of up to three chunks are still there, others are
 // read again, from L2.  16-byte vectors lie swizzled by their rows: lanes that read 4 rows
 // apart meet no conflict.
-constexpr int kStrip = 64, kChunkRows = 128, kChunks = 3;
+constexpr int kStrip = 64, kChunkRows = 128, kChunks = 3, kMostParts = 8;
 static_assert(kThreads / 32 * 8 == kStrip && 32 * 4 == kChunkRows, "a warp's columns, a lane's rows");
 
 template <typename T> constexpr int kVecs = 8 / Vec<T>::kN;              // vectors of 8 columns
@@ -348,13 +349,15 @@ __global__ void __launch_bounds__(kThreads) columns_kernel(Matrix m, unsigned pa
 {
     constexpr int kV = kVecs<T>, kN = Vec<T>::kN;
     extern __shared__ uint4 s_chunks[];
-    __shared__ unsigned s_max[kStrip];
+    __shared__ unsigned s_max[kMostParts][kStrip];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     // fewer CTAs than 2^31, so strips too
     const unsigned strips = static_cast<unsigned>((m.cols + kStrip - 1) / kStrip);
     const unsigned at = blockIdx.x / parts, part = blockIdx.x - at * parts, g = at / strips;
     if (left_out(m, g))
         return;                                                  // and so do the cluster's other CTAs
+    if (parts > 1)
+        asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");    // this CTA has begun
     const int64_t c0 = int64_t(at - g * strips) * kStrip;
     const int64_t r0 = min(m.rows, part * each), r1 = min(m.rows, r0 + each);
     const int chunks = static_cast<int>((r1 - r0 + kChunkRows - 1) / kChunkRows);
@@ -406,16 +409,14 @@ __global__ void __launch_bounds__(kThreads) columns_kernel(Matrix m, unsigned pa
     }
     if (parts > 1) {
         cg::cluster_group cluster = cg::this_cluster();
-        if (lane < 8)
-            s_max[col + lane] = top;
-        cluster.sync();
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");      // all have begun
         if (lane < 8)
             for (unsigned k = 0; k < parts; ++k)
-                top = max(top, cluster.map_shared_rank(s_max, k)[col + lane]);
-        // no CTA ends before every other has read its maxima: waited for at the end.  The arrival is a
-        // release, which comes after the reads (a relaxed one may overtake them).
-        __syncwarp();
-        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+                cluster.map_shared_rank(&s_max[part][col + lane], k)[0] = top;
+        cluster.sync();                                          // nothing of another CTA's is touched after this
+        if (lane < 8)
+            for (unsigned k = 0; k < parts; ++k)
+                top = max(top, s_max[k][col + lane]);
     }
     const Scale mine = scale_of(top);
     if (part == 0 && lane < 8 && col + lane < cols)
@@ -475,10 +476,6 @@ __global__ void __launch_bounds__(kThreads) columns_kernel(Matrix m, unsigned pa
             load(k - kChunks);
         }
     }
-    if (parts > 1) {
-        __syncwarp();
-        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-    }
 }
 
 // ---- launches -----------------------------------------------------------------
@@ -532,7 +529,7 @@ cudaError_t launch_columns(const Matrix &m, int sms, cudaStream_t st)
     // Parts of up to six chunks; fewer, to fill the SMs; more, where a cluster's eight CTAs have to
     // take all.  64 x 1408 x 2048: parts of three 122 us, of six 109, of all eleven 115.
     const int64_t fill = chunks * strips / (4 * int64_t(sms)) + 1;
-    const int64_t per = std::max(std::min<int64_t>(6, fill), (chunks + 7) / 8), each = per * kChunkRows;
+    const int64_t per = std::max(std::min<int64_t>(6, fill), (chunks + kMostParts - 1) / kMostParts), each = per * kChunkRows;
     const int parts = static_cast<int>((chunks + per - 1) / per);
     if (strips * parts > INT32_MAX)
         return cudaErrorInvalidValue;
