@@ -276,6 +276,17 @@ class ExpertProducts:
 
 
 def _expert_linear_function():
+    class Once(torch.autograd.Function):
+        """A gradient that has none of its own: passing one back through it is an error."""
+
+        @staticmethod
+        def forward(ctx, anchor, g):
+            return g.view_as(g)
+
+        @staticmethod
+        def backward(ctx, _):
+            raise RuntimeError("expert_linear has no second derivatives: its gradients cannot be differentiated")
+
     class ExpertLinear(torch.autograd.Function):
         @staticmethod
         def forward(ctx, x, w, products, offsets, mask, grad, codes):
@@ -293,6 +304,15 @@ def _expert_linear_function():
 
         @staticmethod
         def backward(ctx, dy):
+            with torch.no_grad():
+                dx, dw = ExpertLinear.gradients(ctx, dy)
+            if torch.is_grad_enabled():            # create_graph: the kernels above record nothing
+                anchor = torch.empty(0, requires_grad=True)
+                dx, dw = (g if g is None else Once.apply(anchor, g) for g in (dx, dw))
+            return dx, dw, None, None, None, None, None
+
+        @staticmethod
+        def gradients(ctx, dy):
             x, w, *rest = ctx.saved_tensors
             offsets = rest.pop(0) if ctx.has[0] else None
             mask = rest.pop(0) if ctx.has[1] else None
@@ -310,7 +330,7 @@ def _expert_linear_function():
             elif ctx.needs_input_grad[1]:
                 dw = torch.empty_like(w, memory_format=torch.contiguous_format)
                 products.weight_grad(dy, x, offsets, out=dw)
-            return dx, dw, None, None, None, None, None
+            return dx, dw
 
     return ExpertLinear
 
@@ -331,7 +351,9 @@ def expert_linear(products, x, w, offsets=None, mask=None, grad=None, *, codes=N
     grad: where the weights' gradient is written, e.g. the experts' part of the arena that
     the monitor reads; the backward pass then writes all of it, and w gets no gradient
     from autograd.  codes: (wq, ws, vq, vs) of quantize_rows(w) and quantize_columns(w), for
-    weights that do not change; by default both are made anew in each pass."""
+    weights that do not change; by default both are made anew in each pass.
+
+    The gradients have no gradients of their own: differentiating them raises RuntimeError."""
     global _ExpertLinear
     if _ExpertLinear is None:
         _ExpertLinear = _expert_linear_function()

@@ -1,0 +1,54 @@
+"""expert_linear's autograd without a GPU: the products are torch's, written into `out` as the
+kernels do, so that autograd sees nothing of them."""
+import pytest
+import torch
+
+from paper_2606_00539_gb300 import expert_linear, products as module
+
+
+class Products:
+    """One group, 64 bits."""
+
+    def forward(self, x, w, offsets=None, *, out, mask=None):
+        out.copy_(x.detach() @ w.detach().T)
+
+    def input_grad(self, dy, w, offsets=None, *, out, mask=None):
+        out.copy_(dy.detach() @ w.detach())
+
+    def weight_grad(self, dy, x, offsets=None, *, out, add=False, mask=None):
+        dw = dy.detach().T @ x.detach()
+        out.copy_(out + dw if add else dw)
+
+
+@pytest.fixture(autouse=True)
+def loaded():
+    if module.torch is None:
+        module._load_torch()
+
+
+def tensors(x_grad=True, w_grad=True):
+    g = torch.Generator().manual_seed(3)
+    x = torch.randn(7, 5, dtype=torch.float64, generator=g, requires_grad=x_grad)
+    w = torch.randn(4, 5, dtype=torch.float64, generator=g, requires_grad=w_grad)
+    return x, w
+
+
+def test_first_derivatives():
+    x, w = tensors()
+    got = torch.autograd.grad((expert_linear(Products(), x, w) ** 3).sum(), (x, w))
+    want = torch.autograd.grad(((x @ w.T) ** 3).sum(), (x, w))
+    assert all(torch.allclose(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("cube", [True, False])
+def test_second_derivatives_are_refused(cube):
+    """A loss that contains the gradient: of a cube, whose gradient depends on y, and of a sum, whose
+    gradient depends on the weights alone.  The values are right; passing them back is an error."""
+    x, w = tensors()
+    y = expert_linear(Products(), x, w)
+    g, = torch.autograd.grad((y ** 3 if cube else y).sum(), x, create_graph=True)
+    z = x @ w.T
+    want, = torch.autograd.grad((z ** 3 if cube else z).sum(), x)
+    assert torch.allclose(g, want)
+    with pytest.raises(RuntimeError, match="second derivatives"):
+        ((y ** 2).sum() + (g ** 2).sum()).backward()
