@@ -289,7 +289,7 @@ def _expert_linear_function():
 
     class ExpertLinear(torch.autograd.Function):
         @staticmethod
-        def forward(ctx, x, w, products, offsets, mask, grad, codes):
+        def forward(ctx, x, w, products, offsets, mask, grad, add, codes, anchor):
             x, w = x.detach(), w.detach()
             y = torch.empty(x.shape[0], w.shape[-2], dtype=x.dtype, device=x.device)
             products.forward(x, w, offsets, out=y, mask=mask)
@@ -297,7 +297,7 @@ def _expert_linear_function():
                 xq, xs = products.quantize_rows(x)
                 wq, ws = codes[:2] if codes is not None else products.quantize_rows(w, mask=mask)
                 products.forward_i8(xq, xs, wq, ws, offsets, out=y, mask=mask)
-            ctx.products, ctx.grad, ctx.codes = products, grad, codes
+            ctx.products, ctx.grad, ctx.add, ctx.codes = products, grad, add, codes
             ctx.save_for_backward(x, w, *(t for t in (offsets, mask) if t is not None))
             ctx.has = (offsets is not None, mask is not None)
             return y
@@ -309,7 +309,7 @@ def _expert_linear_function():
             if torch.is_grad_enabled():            # create_graph: the kernels above record nothing
                 anchor = torch.empty(0, requires_grad=True)
                 dx, dw = (g if g is None else Once.apply(anchor, g) for g in (dx, dw))
-            return dx, dw, None, None, None, None, None
+            return (dx, dw) + (None,) * 7
 
         @staticmethod
         def gradients(ctx, dy):
@@ -326,7 +326,7 @@ def _expert_linear_function():
                     vq, vs = ctx.codes[2:] if ctx.codes is not None else products.quantize_columns(w, mask=mask)
                     products.forward_i8(dq, ds, vq, vs, offsets, out=dx, mask=mask)
             if ctx.grad is not None:
-                products.weight_grad(dy, x, offsets, out=ctx.grad)
+                products.weight_grad(dy, x, offsets, out=ctx.grad, add=ctx.add)
             elif ctx.needs_input_grad[1]:
                 dw = torch.empty_like(w, memory_format=torch.contiguous_format)
                 products.weight_grad(dy, x, offsets, out=dw)
@@ -338,7 +338,7 @@ def _expert_linear_function():
 _ExpertLinear = None
 
 
-def expert_linear(products, x, w, offsets=None, mask=None, grad=None, *, codes=None):
+def expert_linear(products, x, w, offsets=None, mask=None, grad=None, *, add=False, codes=None):
     """A linear layer of experts with a backward pass, each expert on the path that the
     mask gives it: 16 bits where its entry is not 0, 8-bit codes where it is 0 (16 bits
     everywhere without a mask).
@@ -349,12 +349,17 @@ def expert_linear(products, x, w, offsets=None, mask=None, grad=None, *, codes=N
     (straight through); the weights' gradient is the 16-bit product for every expert.
 
     grad: where the weights' gradient is written, e.g. the experts' part of the arena that
-    the monitor reads; the backward pass then writes all of it, and w gets no gradient
-    from autograd.  codes: (wq, ws, vq, vs) of quantize_rows(w) and quantize_columns(w), for
+    the monitor reads; the backward pass then writes all of it, whether or not x or w
+    requires a gradient (so y does), and w gets no gradient from autograd.  It holds the one
+    backward pass that ran last: for a weight that is used several times, or several micro-batches, clear
+    it before the first and give add=True, which adds to what is there.  codes: (wq, ws, vq, vs) of quantize_rows(w) and quantize_columns(w), for
     weights that do not change; by default both are made anew in each pass.
 
     The gradients have no gradients of their own: differentiating them raises RuntimeError."""
     global _ExpertLinear
     if _ExpertLinear is None:
         _ExpertLinear = _expert_linear_function()
-    return _ExpertLinear.apply(x, w, products, offsets, mask, grad, codes)
+    anchor = None
+    if grad is not None and torch.is_grad_enabled() and not (x.requires_grad or w.requires_grad):
+        anchor = torch.empty(0, requires_grad=True)          # without one autograd would leave the backward pass out
+    return _ExpertLinear.apply(x, w, products, offsets, mask, grad, add, codes, anchor)

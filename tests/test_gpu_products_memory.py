@@ -3,7 +3,7 @@ may touch.  Tolerances are those of test_gpu_products."""
 import numpy as np
 import pytest
 
-from paper_2606_00539_gb300 import ExpertProducts, GnmrError
+from paper_2606_00539_gb300 import ExpertProducts, GnmrError, expert_linear
 from paper_2606_00539_gb300 import _native as N
 
 pytestmark = pytest.mark.gpu
@@ -150,3 +150,21 @@ def test_a_wait_that_runs_out_ends_the_product_and_is_reported(name):
         assert torch.equal(CALLS[name](fine, a), want)
         torch.cuda.synchronize()
         fine.check()
+
+
+def test_expert_linear_adds_micro_batches_to_the_arena(products):
+    """Two micro-batches and a weight used twice, into an fp32 arena, with nothing that requires a gradient."""
+    counts, n, k, g, t = [40, 0, 30], 72, 136, gen(33), torch.bfloat16
+    off, R = offsets_of(counts), 70
+    w = normal(g, 3, n, k, dtype=t, size=0.1)
+    arena = torch.zeros(3, n, k, device="cuda")
+    want, size = (torch.zeros(3, n, k, dtype=torch.float64, device="cuda") for _ in range(2))
+    for _ in range(2):
+        xs, dys = [normal(g, R, k, dtype=t) for _ in range(2)], [normal(g, R, n, dtype=t) for _ in range(2)]
+        ys = [expert_linear(products, x, w, off, None, arena, add=True) for x in xs]
+        torch.autograd.backward(ys, dys)
+        for x, dy in zip(xs, dys):
+            for e, at in spans(counts):
+                want[e] += dy[at].double().T @ x[at].double()
+                size[e] += dy[at].double().abs().T @ x[at].double().abs()
+    check(arena, want, 4 * size, 40, "f32")                      # four sums, each added with a rounding of its own

@@ -52,3 +52,28 @@ def test_second_derivatives_are_refused(cube):
     assert torch.allclose(g, want)
     with pytest.raises(RuntimeError, match="second derivatives"):
         ((y ** 2).sum() + (g ** 2).sum()).backward()
+
+
+def test_the_arena_is_written_when_nothing_else_requires_a_gradient():
+    x, w = tensors(x_grad=False, w_grad=False)
+    arena = torch.full((4, 5), 7.0, dtype=torch.float64)
+    (expert_linear(Products(), x, w, grad=arena) ** 2).sum().backward()
+    assert torch.allclose(arena, 2 * (x @ w.T).T @ x)
+    with torch.no_grad():
+        assert not expert_linear(Products(), x, w, grad=arena).requires_grad
+    assert not expert_linear(Products(), x, w).requires_grad
+
+
+def test_a_shared_weight_and_micro_batches_add_to_the_arena():
+    """Two uses of one weight in one graph, then another micro-batch: the sum, as autograd has it."""
+    x, w = tensors()
+    arena = torch.zeros(4, 5, dtype=torch.float64)
+    want = torch.zeros(4, 5, dtype=torch.float64)
+    for scale in (1.0, 3.0):
+        y = expert_linear(Products(), x, w, grad=arena, add=True)
+        ((y ** 2).sum() + (expert_linear(Products(), scale * x, w, grad=arena, add=True) ** 3).sum()).backward()
+        z = x @ w.T
+        want += torch.autograd.grad((z ** 2).sum() + ((scale * x @ w.T) ** 3).sum(), w)[0]
+    assert w.grad is None and torch.allclose(arena, want)
+    (expert_linear(Products(), x, w, grad=arena) ** 2).sum().backward()          # without add: written
+    assert torch.allclose(arena, torch.autograd.grad(((x @ w.T) ** 2).sum(), w)[0])
