@@ -47,7 +47,10 @@ class ExpertProducts:
 
     Rows of `out` that belong to no group are left as they are.  stream: a torch stream, default the
     current one; as with any torch call, tensors that were made on another stream are the
-    caller's to order.  One instance serves any sizes; use it from one stream at a time."""
+    caller's to order.  One instance serves any sizes; use it from one stream at a time.
+
+    Autograd records none of these calls (expert_linear is the layer that it knows), so the
+    16-bit products refuse operands that require a gradient while it records."""
 
     def __init__(self, device=0):
         self._h = None
@@ -173,6 +176,11 @@ class ExpertProducts:
             N._check(status, None)
 
     # -- 16-bit products ------------------------------------------------------
+    @staticmethod
+    def _no_graph(a, b):
+        if (a.requires_grad or b.requires_grad) and torch.is_grad_enabled():
+            raise ValueError("autograd records nothing of a product: use expert_linear, or detach() or torch.no_grad()")
+
     def forward(self, x, w, offsets=None, *, out=None, mask=None, stream=None):
         """y[r] = W_g x[r] for the rows r of every group g: x [rows, n_in] -> [rows, n_out]."""
         groups, n_out, n_in, row, group = self._matrix(w, "w", (2, 3), self._sixteen)
@@ -180,6 +188,7 @@ class ExpertProducts:
         _, rows, cols, step, _ = self._matrix(x, "x", (2,), (dtype,))
         if cols != n_in:
             raise ValueError(f"x must have {n_in} columns, got {cols}")
+        self._no_graph(x, w)
         at, bits, each = self._grouping(groups, offsets, mask)
         out, across = self._out(out, rows, n_out, (dtype,), stream)
         code = _DTYPES[dtype]
@@ -195,6 +204,7 @@ class ExpertProducts:
         _, rows, cols, step, _ = self._matrix(dy, "dy", (2,), (dtype,))
         if cols != n_out:
             raise ValueError(f"dy must have {n_out} columns, got {cols}")
+        self._no_graph(dy, w)
         at, bits, each = self._grouping(groups, offsets, mask)
         out, across = self._out(out, rows, n_in, (dtype,), stream)
         code = _DTYPES[dtype]
@@ -217,6 +227,7 @@ class ExpertProducts:
         groups, high, wide, row, group = self._matrix(out, "out", (2, 3), (dtype, torch.float32))
         if (high, wide) != (n_out, n_in):
             raise ValueError(f"out must be [{n_out}, {n_in}] for each group, got [{high}, {wide}]")
+        self._no_graph(dy, x)
         at, bits, each = self._grouping(groups, offsets, mask)
         self._enqueue(N.gnmr_product(N.GNMR_PRODUCT_WEIGHT_GRAD, groups, rows, n_out, n_in, _DTYPES[dtype],
                                      _DTYPES[out.dtype], at, bits, each, x.data_ptr(), x_step, dy.data_ptr(), dy_step,

@@ -77,3 +77,23 @@ def test_a_shared_weight_and_micro_batches_add_to_the_arena():
     assert w.grad is None and torch.allclose(arena, want)
     (expert_linear(Products(), x, w, grad=arena) ** 2).sum().backward()          # without add: written
     assert torch.allclose(arena, torch.autograd.grad(((x @ w.T) ** 2).sum(), w)[0])
+
+
+@pytest.mark.parametrize("which", [0, 1])
+def test_products_refuse_operands_whose_gradient_would_be_lost(which):
+    """Before anything is enqueued; not under no_grad, where nothing is lost."""
+    p = module.ExpertProducts.__new__(module.ExpertProducts)
+    p._h, p.device_index, p._sixteen = None, -1, (torch.bfloat16, torch.float16)      # -1: tensors in host memory
+    x, dy, w = (torch.zeros(s, dtype=torch.bfloat16) for s in ((6, 8), (6, 16), (16, 8)))
+    out = torch.zeros(16, 8)
+    calls = [(lambda: p.forward(x, w, out=dy), (x, w)), (lambda: p.input_grad(dy, w, out=x), (dy, w)),
+             (lambda: p.weight_grad(dy, x, out=out), (dy, x))]
+    for call, operands in calls:
+        operands[which].requires_grad_()
+        with pytest.raises(ValueError, match="expert_linear"):
+            call()
+        with torch.no_grad(), pytest.raises(ValueError, match="closed"):
+            call()
+        operands[which].requires_grad_(False)
+        with pytest.raises(ValueError, match="closed"):
+            call()
