@@ -453,7 +453,7 @@ typedef struct gnmr_product {
     const float *d_w_scale;    /* FORWARD_I8: [groups x n_out] */
     void *d_out;               /* [rows x n_out], [rows x n_in], or per group [n_out x n_in]; no operand */
     int64_t out_stride;
-    int64_t out_group_stride;  /* WEIGHT_GRAD: groups must not overlap */
+    int64_t out_group_stride;  /* WEIGHT_GRAD: groups one after the other, or rows of all groups side by side */
     int32_t add;               /* WEIGHT_GRAD: add to d_out instead of writing it */
     void *d_scratch;           /* 256-byte aligned, used during the call only; NULL if none is needed */
     int64_t scratch_bytes;

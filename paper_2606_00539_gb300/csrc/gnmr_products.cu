@@ -359,10 +359,13 @@ gnmr_status check(const gnmr_product *p)
     if ((x && p->x_stride > far) || (dy && p->dy_stride > far) || (w && (p->w_stride > far || p->w_group_stride > far)) ||
         p->out_stride > far || (wgrad && p->out_group_stride > far))
         return fail(GNMR_ERR_LAYOUT, "products: a stride above 2^36 elements");
+    // a gradient's groups lie one after the other, or row by row beside each other
     const __int128 group = static_cast<__int128>(p->n_out - 1) * p->out_stride + p->n_in;
+    const __int128 rows_of_all = static_cast<__int128>(p->groups - 1) * p->out_group_stride + p->n_in;
+    const bool apart = p->out_group_stride >= group || (p->out_group_stride >= p->n_in && p->out_stride >= rows_of_all);
     if ((x && p->x_stride < p->n_in) || (dy && p->dy_stride < p->n_out) ||
         (w && (p->w_stride < p->n_in || p->w_group_stride < 0)) || p->out_stride < wide_out ||
-        (wgrad && p->groups > 1 && p->out_group_stride < group) || (p->d_mask && p->groups > 1 && p->mask_stride < 1))
+        (wgrad && p->groups > 1 && !apart) || (p->d_mask && p->groups > 1 && p->mask_stride < 1))
         return fail(GNMR_ERR_LAYOUT, "products: a stride below what it strides over");
     // operands that could not be copied, whatever memory there is
     const __int128 most_rows = std::max<int64_t>(p->rows, w ? int64_t(p->groups) * p->n_out : 0);

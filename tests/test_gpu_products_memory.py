@@ -10,7 +10,7 @@ pytestmark = pytest.mark.gpu
 
 import torch  # noqa: E402
 
-from .test_gpu_products import check, codes_oracle, gen, normal, offsets_of, spans  # noqa: E402
+from .test_gpu_products import TYPES, check, codes_oracle, gen, normal, offsets_of, spans  # noqa: E402
 
 
 @pytest.fixture(scope="module")
@@ -168,3 +168,16 @@ def test_expert_linear_adds_micro_batches_to_the_arena(products):
                 want[e] += dy[at].double().T @ x[at].double()
                 size[e] += dy[at].double().abs().T @ x[at].double().abs()
     check(arena, want, 4 * size, 40, "f32")                      # four sums, each added with a rounding of its own
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_gradients_of_groups_side_by_side(products, kind):
+    """Row n of every group's gradient beside the others': [n_out, groups, n_in] in memory."""
+    counts, n, k, g, t = [70, 0, 33], 136, 72, gen(35), torch.bfloat16
+    x, dy, off = normal(g, 103, k, dtype=t), normal(g, 103, n, dtype=t), offsets_of(counts)
+    held = normal(g, n, 3, k, dtype=TYPES[kind])
+    old = held.clone()
+    products.weight_grad(dy, x, off, out=held.transpose(0, 1), add=True)
+    for e, at in spans(counts):
+        X, D, before = x[at].double(), dy[at].double(), old[:, e].double()
+        check(held[:, e], D.T @ X + before, D.abs().T @ X.abs() + before.abs(), counts[e], kind)

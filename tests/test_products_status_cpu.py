@@ -36,3 +36,17 @@ def test_a_handle_is_freed_once_whatever_its_destruction_reports(monkeypatch):
     assert freed == [4096]
     with pytest.raises(ValueError):
         p.check()
+
+
+def test_gradients_of_groups_side_by_side_are_allowed_and_overlapping_ones_are_not():
+    p = N.gnmr_product(op=N.GNMR_PRODUCT_WEIGHT_GRAD, groups=3, rows=10, n_out=16, n_in=8, dtype=N.GNMR_DTYPE_BF16,
+                       out_dtype=N.GNMR_DTYPE_F32, d_offsets=4096, d_x=4096, x_stride=8, d_dy=4096, dy_stride=16, d_out=4096)
+    for row, group, fine in ((24, 8, True), (40, 16, True), (23, 8, False), (24, 7, False), (8, 128, True), (8, 127, False),
+                             (25, 8, True), (24, 0, False), (24, -8, False)):
+        p.out_stride, p.out_group_stride = row, group
+        if fine:
+            assert N.gnmr_products_scratch_bytes(p) == 0
+        else:
+            with pytest.raises(GnmrError) as e:
+                N.gnmr_products_scratch_bytes(p)
+            assert e.value.status == N.GNMR_ERR_LAYOUT
