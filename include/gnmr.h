@@ -482,8 +482,8 @@ gnmr_status gnmr_products_status(gnmr_products *h);
 
 /* The longest that one wait inside a product's kernels may take, from the next product on.  Negative, as
  * at first: many times what the product's sizes need, two seconds at the least.  No call that is
- * otherwise right reaches that; with a limit below what a product takes it gives up, with 0 at the first
- * wait. */
+ * otherwise right reaches that; with a limit below what a product takes it may give up, with 0 it
+ * does, before its first load. */
 gnmr_status gnmr_products_set_wait_limit(gnmr_products *h, int64_t nanoseconds);
 
 /* Waits for the handle's device and frees the handle.  NULL is accepted.  GNMR_ERR_STATE, the handle

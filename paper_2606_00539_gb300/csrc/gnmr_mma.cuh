@@ -83,9 +83,8 @@ __device__ __forceinline__ void arrive_expect(uint32_t bar, uint32_t bytes)
 }
 
 // Every wait ends: after `most` nanoseconds it returns false, and its caller leaves its
-// loop.  By a whole warp, which goes on or gives up as one.  With `most` 0 it only looks: a try that
-// waits may sleep as long as the hardware likes.  kPaired: for a barrier on which the other CTA arrives
-// too, or its multiplies.
+// loop.  By a whole warp, which goes on or gives up as one.  kPaired: for a barrier on which the other
+// CTA arrives too, or its multiplies.
 __device__ __forceinline__ uint64_t nanoseconds()
 {
     uint64_t t;
@@ -95,18 +94,9 @@ __device__ __forceinline__ uint64_t nanoseconds()
 
 template <bool kPaired> __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, uint64_t most)
 {
-    uint32_t done;
-    if (most == 0) {
-        asm volatile("{\n.reg .pred p;\n"
-                     "mbarrier.test_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n"
-                     "selp.u32 %0, 1, 0, p;\n}"
-                     : "=r"(done)
-                     : "r"(bar), "r"(parity)
-                     : "memory");
-        return __all_sync(~0u, done);
-    }
     uint64_t since = 0;
     for (bool first = true;; first = false) {
+        uint32_t done;
         if (kPaired)
             asm volatile("{\n.reg .pred p;\n"
                          "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n"

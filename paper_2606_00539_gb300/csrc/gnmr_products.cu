@@ -104,6 +104,8 @@ __device__ __forceinline__ bool load_stages(const CUtensorMap &map_a, const CUte
     const uint32_t tail = smem_addr(&c.bars->tail[0]), base = smem_addr(c.stages);
     int stage = 0;
     uint32_t phase = 1;
+    if (p.most_ns == 0)
+        return false;                                    // no time at all: the others wait in vain
     for (int i = c.pair, g = 0; i < c.items; i += c.pairs) {
         const Item it = item_of<kStep>(p, c.tables, c.split, c.lane_tiles, i, g);
         const int half = it.wide / 2;                         // B's columns in this CTA

@@ -69,6 +69,8 @@ __device__ __forceinline__ bool load_stages(const CUtensorMap &map_a, const CUte
     const uint32_t own = in_cta(full, c.rank), full_b = in_cta(smem_addr(&c.bars->tail[0]), 0);
     int stage = 0;
     uint32_t phase = 1;
+    if (p.most_ns == 0)
+        return false;                                    // no time at all: the others wait in vain
     for (int i = c.pair, g = 0; i < c.items; i += c.pairs) {
         const Item it = item_of<kStep>(p, c.tables, c.split, c.lane_tiles, i, g);
         const int a_lane = it.lane0 + c.rank * 128, za = p.a_by_group ? it.g : 0;

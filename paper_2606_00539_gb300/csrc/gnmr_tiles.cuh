@@ -46,7 +46,7 @@ struct Product {
     float *parts;
     unsigned *tickets;
     int *gave_up;
-    uint64_t most_ns;                  // of every wait
+    uint64_t most_ns;                  // of every wait; 0: nothing is loaded, so that they run out
 };
 
 // ---- work: tiles of every group, and their parts --------------------------------

@@ -126,7 +126,7 @@ CALLS = {                                                        # each kernel; 
 
 @pytest.mark.parametrize("name", CALLS)
 def test_a_wait_that_runs_out_ends_the_product_and_is_reported(name):
-    """With no time to wait for their first loads, all roles of the kernel give up.  The kernel ends, the
+    """With no time at all nothing is loaded, so that every role waits for what never comes, and gives up.  The kernel ends, the
     handle says so and takes no more products, and another handle, on the same context, is not affected."""
     g, t = gen(31), torch.bfloat16
     a = dict(x=normal(g, 900, 1100, dtype=t), dy=normal(g, 900, 700, dtype=t), w=normal(g, 4, 700, 1100, dtype=t),
