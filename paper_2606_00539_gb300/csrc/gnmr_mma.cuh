@@ -65,15 +65,17 @@ __device__ __forceinline__ void arrive(uint32_t bar)
 }
 
 // After shared memory was read that will be written anew, or was written and, past fence_async_proxy, the
-// tensor cores will read: kPaired where the thread that waits is in the other CTA, which the narrower
-// scope says nothing about.  (It takes 2,000 cycles, so that a loop of every stage keeps to its own CTA.)
-template <bool kPaired = false> __device__ __forceinline__ void arrive_release(uint32_t bar)
+// tensor cores will read.  On a barrier of this CTA (its own address), for a thread of it that waits; or on one
+// of the pair's first CTA (from in_cta), where the thread that waits is: the narrower scope says nothing about
+// that one.  (The wider one takes 2,000 cycles, so that a loop of every stage keeps to its own CTA.)
+__device__ __forceinline__ void release(uint32_t bar)
 {
-    if (kPaired) {
-        asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
-        return;
-    }
-    asm volatile("mbarrier.arrive.release.cta.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+    asm volatile("mbarrier.arrive.release.cta.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+
+__device__ __forceinline__ void release_in_pair(uint32_t bar)
+{
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
 __device__ __forceinline__ void arrive_expect(uint32_t bar, uint32_t bytes)
@@ -82,9 +84,28 @@ __device__ __forceinline__ void arrive_expect(uint32_t bar, uint32_t bytes)
                  : "memory");
 }
 
-// Every wait ends: after `most` nanoseconds it returns false, and its caller leaves its
-// loop.  By a whole warp, which goes on or gives up as one.  kPaired: for a barrier on which the other
-// CTA arrives too, or its multiplies.
+// Whether a phase is complete, for a whole warp, after a nap of the hardware's choosing.  kPaired: a barrier
+// on which the other CTA arrives too, or its multiplies.
+template <bool kPaired> __device__ __forceinline__ bool complete(uint32_t bar, uint32_t parity)
+{
+    uint32_t done;
+    if (kPaired)
+        asm volatile("{\n.reg .pred p;\n"
+                     "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n"
+                     "selp.u32 %0, 1, 0, p;\n}"
+                     : "=r"(done)
+                     : "r"(bar), "r"(parity)
+                     : "memory");
+    else
+        asm volatile("{\n.reg .pred p;\n"
+                     "mbarrier.try_wait.parity.acquire.cta.shared::cta.b64 p, [%1], %2;\n"
+                     "selp.u32 %0, 1, 0, p;\n}"
+                     : "=r"(done)
+                     : "r"(bar), "r"(parity)
+                     : "memory");
+    return __all_sync(~0u, done);
+}
+
 __device__ __forceinline__ uint64_t nanoseconds()
 {
     uint64_t t;
@@ -92,33 +113,16 @@ __device__ __forceinline__ uint64_t nanoseconds()
     return t;
 }
 
+// Every wait ends: after `most` nanoseconds it returns false, and its caller leaves its
+// loop.  By a whole warp, which goes on or gives up as one.
 template <bool kPaired> __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, uint64_t most)
 {
-    uint64_t since = 0;
-    for (bool first = true;; first = false) {
-        uint32_t done;
-        if (kPaired)
-            asm volatile("{\n.reg .pred p;\n"
-                         "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n"
-                         "selp.u32 %0, 1, 0, p;\n}"
-                         : "=r"(done)
-                         : "r"(bar), "r"(parity)
-                         : "memory");
-        else
-            asm volatile("{\n.reg .pred p;\n"
-                         "mbarrier.try_wait.parity.acquire.cta.shared::cta.b64 p, [%1], %2;\n"
-                         "selp.u32 %0, 1, 0, p;\n}"
-                         : "=r"(done)
-                         : "r"(bar), "r"(parity)
-                         : "memory");
-        if (__all_sync(~0u, done))
-            return true;
-        const uint64_t now = nanoseconds();
-        if (first)
-            since = now;
-        else if (__any_sync(~0u, now - since >= most))
+    if (complete<kPaired>(bar, parity))
+        return true;
+    for (const uint64_t since = nanoseconds(); !complete<kPaired>(bar, parity);)
+        if (__any_sync(~0u, nanoseconds() - since >= most))
             return false;
-    }
+    return true;
 }
 
 // Registers a thread of this warpgroup may use from here on.

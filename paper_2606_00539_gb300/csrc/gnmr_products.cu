@@ -241,7 +241,7 @@ __device__ __forceinline__ bool clear_tails(const Product &p, const Cta &c)
             fence_async_proxy();
             __syncwarp();
             if (lane == 0)
-                arrive_release<true>(full + at * 8);
+                release_in_pair(full + at * 8);
         }
         stage = (stage + it.k1 - it.k0) % c.ring;
     }

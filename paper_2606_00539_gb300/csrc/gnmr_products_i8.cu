@@ -112,7 +112,7 @@ __device__ __forceinline__ bool widen_a(const Product &p, const Cta &c)
 {
     constexpr int kStage = Shape<kWide>::kStage;
     const int warp = threadIdx.x / 32 - kFirstWidenWarp, lane = threadIdx.x & 31, quarter = warp & 3, team = warp >> 2;
-    const uint32_t full = smem_addr(&c.bars->full[0]), empty = in_cta(smem_addr(&c.bars->empty[0]), c.rank);
+    const uint32_t full = smem_addr(&c.bars->full[0]), empty = smem_addr(&c.bars->empty[0]);
     const uint32_t used = smem_addr(&c.bars->used[0]), ready = in_cta(smem_addr(&c.bars->ready[0]), kWide ? 0 : c.rank);
     const int row = quarter * 32 + lane;
     const uint8_t *raw = c.stages + Shape<kWide>::kWidened + row * 128;
@@ -144,7 +144,7 @@ __device__ __forceinline__ bool widen_a(const Product &p, const Cta &c)
             }
             __syncwarp();
             if (lane == 0)
-                arrive_release(empty + stage * 8);
+                release(empty + stage * 8);
             store_wait();
             fence_before();
             __syncwarp();
@@ -164,8 +164,8 @@ __device__ __forceinline__ bool widen_b(const Product &p, const Cta &c)
     using S = Shape<false>;
     constexpr int kStage = S::kStage, kSlot = S::kSlot, kBTile = S::kBTile;
     const int lane = threadIdx.x & 31, turn = threadIdx.x / 32 - kFirstBWarp, chunk = lane & 7;
-    const uint32_t full = smem_addr(&c.bars->full[0]), empty = in_cta(smem_addr(&c.bars->empty[0]), c.rank);
-    const uint32_t used = smem_addr(&c.bars->used[0]), ready = in_cta(smem_addr(&c.bars->ready[0]), c.rank);
+    const uint32_t full = smem_addr(&c.bars->full[0]), empty = smem_addr(&c.bars->empty[0]);
+    const uint32_t used = smem_addr(&c.bars->used[0]), ready = smem_addr(&c.bars->ready[0]);
     int stage = turn, slot = turn, skip = turn;
     uint32_t phase = 0, slot_phase = 1;
     for (int i = c.pair, g = 0; i < c.items; i += c.pairs) {
@@ -188,8 +188,8 @@ __device__ __forceinline__ bool widen_b(const Product &p, const Cta &c)
             fence_async_proxy();
             __syncwarp();
             if (lane == 0) {
-                arrive_release(empty + stage * 8);
-                arrive_release(ready + slot * 8);
+                release(empty + stage * 8);
+                release(ready + slot * 8);
             }
             two_on(stage, phase, c.ring);
             two_on(slot, slot_phase, kSlots);
