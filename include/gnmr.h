@@ -44,7 +44,7 @@ typedef enum gnmr_status {
     GNMR_ERR_LAYOUT = 2,      /* unit layout does not fit the arena given */
     GNMR_ERR_CUDA = 3,        /* a CUDA call failed; the handle is then only good for destroy */
     GNMR_ERR_OOM = 4,         /* host or device allocation failed in gnmr_create */
-    GNMR_ERR_STATE = 5        /* handle unusable after an earlier GNMR_ERR_CUDA */
+    GNMR_ERR_STATE = 5        /* handle unusable after an earlier GNMR_ERR_CUDA, or a product that gave up */
 } gnmr_status;
 
 typedef enum gnmr_dtype {
@@ -412,8 +412,10 @@ gnmr_status gnmr_unit_norms_static(const void *d_arena, int64_t arena_elems, int
  * The backward pass of the 8-bit path is GNMR_PRODUCT_FORWARD_I8 on the codes
  * of dy and of W_g^T (gnmr_quantize_columns), n_out and n_in exchanged.
  *
- * Sums are held in 32 bits: fp32 for 16-bit operands, exact integers for codes
- * (n_in up to 131,071), and rounded once to the output's type.  Infinities and
+ * Sums are held in 32 bits: fp32 for 16-bit operands, rounded once to the output's type; exact
+ * integers for codes (n_in up to 131,071), converted to fp32, multiplied by x_scale and then by
+ * w_scale, each rounded to fp32 (so the sum times x_scale has to be within its range too), and
+ * rounded to the output's type.  Infinities and
  * NaNs reach the outputs that they belong to and no others.  A call repeated on
  * the same operands gives the same bits. */
 typedef enum gnmr_product_op {

@@ -15,9 +15,9 @@
 // the finished pieces and write the outputs, and one clears what the last tile of a
 // group's rows holds past their end (weight gradient).
 //
-// Measured (one GB300, 64 experts of 1408 x 2048, bf16): forward of 49,152 rows 190 us, 1.5 PFLOP/s,
+// Measured (one GB300, 64 experts of 1408 x 2048, bf16): forward of 49,152 rows 190 to 200 us, 1.4 to 1.5 PFLOP/s,
 // multiplies under way 79 % of the time at the 1.6 GHz that the power limit leaves; input gradient
-// of 24,571 rows 102 us, weight gradient 120 us (bound by its outputs); forward of 282 rows 59 us, 6.3
+// of 24,571 rows 102 us, weight gradient 123 us (bound by its outputs); forward of 282 rows 59 us, 6.3
 // TB/s of weights.  Dense 4096^3 74 us, 1.85 PFLOP/s.
 //
 // A piece is at most 1,024 steps (512 for fp32 outputs).  The tensor cores cut
@@ -57,7 +57,8 @@ constexpr int kBlock = 64 * 128;                       // bytes of a tile of 64 
 // The epilogue's warps and the registers that the warpgroups share out between them, out of what the
 // block is launched with.  A weight gradient's contraction is short, so that it is bound by its
 // epilogue: 16 warps of 64 columns each (12288 rows, 64 fp32 gradients of 1408 x 2048: 8 warps 156 us,
-// 16 141); the others 8 of 128, with which 16 made no difference.
+// 16 141); the others 8 of 128, with which 16 made no difference.  The 16 warps' 104 registers do not hold
+// the 64 sums beside what addresses them: about 300 bytes a thread are spilled.
 template <int kOp> struct Roles {
     static constexpr int kSides = kOp == GNMR_PRODUCT_WEIGHT_GRAD ? 4 : 2;
     static constexpr int kThreads = 32 * (kFirstEpilogueWarp + 4 * kSides);
@@ -386,12 +387,14 @@ gnmr_status check(const gnmr_product *p)
 // Measured in 8 bits and widened, us: 5120 -> 13824, 16 rows 19.9 and 21.0, 32 rows 24.5 and 21.3; 64 experts of
 // 2048 -> 1408, 282 rows 35 and 39, 1,024 rows 45 and 44, 31 rows each 57 and 45; one group, 4096 -> 1024, 100 rows
 // (8 tiles) 11.6 and 20; 2048 -> 2048, 200 (32) 12.4 and 14.8; 7296 -> 4352, 200 (68) 56 and 27; 24 experts of
-// 1371 -> 1003, 400 rows (28) 16 and 20.  Rows to a group are an average: the counts are on the device.
+// 1371 -> 1003, 400 rows (28) 16 and 20.  Rows to a group are an average, the counts being on the device: 1,024 rows of
+// one of 64 experts of 2048 -> 1408 27 and 19, 16 rows each 39 and 43.
 constexpr int64_t kFewestCodes = 16, kFewCodes = 32, kFewCodeTiles = 48;
 // 16-bit operands: tiles of 64 columns up to this many rows to a group, and for one group
 // while they make one round at most.  5120 -> 13824, 16 rows: 26 us so, 28 in tiles of 256; 64: 27 and 29;
 // 128: 39 and 30.  2048 -> 2048, 16 rows: 8 and 12; 200: 10 and 17.  64 experts of 1408 -> 2048, 1 row
-// each: 39 and 42, 64 each: 66 and 65.
+// each: 39 and 42, 64 each: 66 and 65.  An average here too: 4,096 rows of one of 64 experts of 2048 -> 1408 34
+// and 31, 2,796 of 4,056 rows one expert's 77 and 77.
 constexpr int64_t kFewRows = 64;
 
 Operands operands(const gnmr_product *p)

@@ -1,17 +1,19 @@
 // Expert products on 8-bit codes.
 //
 // sm_103a's tensor cores (tcgen05) take no 8-bit integers, so codes are multiplied as
-// fp16, which holds them exactly: products are below 2^14 and a piece of
+// fp16, which holds them exactly: products are at most 2^14 and a piece of
 // 1,024 of them sums to at most 2^24, exact in fp32; pieces are added as integers.
 //
 // The weights stay 8 bits wide up to the SM: eight warps widen A's tiles into tensor
 // memory, from where the tensor cores take an operand as well, at no cost in
 // shared-memory bandwidth (tiles of fp16 in shared memory, written and read again for each
-// tile of columns, would take more of it than there is beside the multiplies).  B, the
-// rows, are widened by two more warps where they are few, and each CTA multiplies alone: what is
-// widened in shared memory is then handed over within its CTA (between CTAs that takes 2,000 cycles a
-// stage).  Else rows are widened in memory by a kernel before this one, and CTAs multiply in pairs.  Widening the weights in memory too, for the 16-bit kernel, was
-// slower at 4,001 rows to a group (5120 -> 13824: 380 us, this way 321).
+// tile of columns, would take more of it than there is beside the multiplies).
+//
+// B, the rows, are widened by two more warps where they are few, and each CTA multiplies alone:
+// what is widened in shared memory is then handed over within its CTA (between CTAs that takes
+// 2,000 cycles a stage).  Else a kernel before this one widens them in memory, and CTAs multiply
+// in pairs.  Widening the weights in memory too, for the 16-bit kernel, was slower at 4,001 rows
+// to a group (5120 -> 13824: 380 us, this way 321 to 337).
 #include <algorithm>
 #include <cstring>
 

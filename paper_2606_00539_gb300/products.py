@@ -269,7 +269,8 @@ class ExpertProducts:
     def forward_i8(self, xq, x_scale, wq, w_scale, offsets=None, *, out=None, out_dtype="bf16", mask=None,
                    stream=None):
         """y[r] = x_scale[r] * w_scale_g * (Wq_g xq[r]) on 8-bit codes; the sum is an exact
-        integer (n_in up to 131,071), rounded once to out's type."""
+        integer (n_in up to 131,071), converted and scaled in fp32 (by x_scale first, a rounding
+        each), then rounded to out's type."""
         groups, n_out, n_in, row, group = self._matrix(wq, "wq", (2, 3), (torch.int8,))
         _, rows, cols, step, _ = self._matrix(xq, "xq", (2,), (torch.int8,))
         if cols != n_in:
