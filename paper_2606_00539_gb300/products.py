@@ -316,9 +316,11 @@ def _expert_linear_function():
 
         @staticmethod
         def backward(ctx, dy):
-            with torch.no_grad():
+            if not torch.is_grad_enabled():
                 dx, dw = ExpertLinear.gradients(ctx, dy)
-            if torch.is_grad_enabled():            # create_graph: the kernels above record nothing
+            else:                                  # create_graph: the products record nothing
+                with torch.no_grad():
+                    dx, dw = ExpertLinear.gradients(ctx, dy)
                 anchor = torch.empty(0, requires_grad=True)
                 dx, dw = (g if g is None else Once.apply(anchor, g) for g in (dx, dw))
             return (dx, dw) + (None,) * 7
