@@ -50,7 +50,7 @@ typedef enum gnmr_status {
 typedef enum gnmr_dtype {
     GNMR_DTYPE_F32 = 0,       /* IEEE binary32 gradients */
     GNMR_DTYPE_BF16 = 1,      /* bfloat16 gradients */
-    GNMR_DTYPE_F16 = 2        /* IEEE binary16: the expert products and the 8-bit codes only */
+    GNMR_DTYPE_F16 = 2        /* IEEE binary16: everything but the monitor and the actuator */
 } gnmr_dtype;
 
 /* Controller configuration (Sec. 3.3-3.4).  gnmr_config_defaults fills it
@@ -512,6 +512,139 @@ gnmr_status gnmr_quantize_columns(const void *d_x, int32_t dtype, int32_t groups
                                   int64_t x_stride, int64_t x_group_stride, const uint8_t *d_mask,
                                   int64_t mask_stride, int8_t *d_q, int64_t q_stride, int64_t q_group_stride,
                                   float *d_scale, void *stream);
+
+/* ---- Gated feed-forward blocks -------------------------------------------
+ * h[r] = act(a) * b with [a, b] = W_g x[r], for the rows r of every group g: the
+ * two projections of a gated feed-forward layer, its activation and the product in one
+ * kernel.  W_g is [2 n x n_in], the n rows of the activated projection (the gate) before those
+ * of the other, so that GNMR_PRODUCT_INPUT_GRAD and _WEIGHT_GRAD with n_out = 2 n are the rest of
+ * its backward pass, and the quantizing calls and GNMR_PRODUCT_FORWARD_I8 its low-cost path.
+ *
+ * Sums are held in 32 bits as in gnmr_products_run; h is formed from them in fp32 and rounded once.
+ * An a of -infinity gives NaN for GNMR_ACT_SILU and GNMR_ACT_GELU alike (0 times infinity). */
+typedef enum gnmr_activation {
+    GNMR_ACT_SILU = 0,         /* a / (1 + exp(-a)) */
+    GNMR_ACT_GELU = 1          /* a (1 + erf(a / sqrt 2)) / 2 */
+} gnmr_activation;
+
+/* Strides in elements, rows contiguous; operands that are not read in place (see
+ * gnmr_product) are first copied to d_scratch.  The mask: groups whose byte is not 0 are
+ * computed, the other groups' rows of d_out and d_keep left as they are, and so are rows of
+ * no group. */
+typedef struct gnmr_gated {
+    int32_t groups;            /* 1 .. 2048 */
+    int32_t activation;        /* gnmr_activation */
+    int64_t rows;              /* 0 .. 2^30 - 1 */
+    int32_t n, n_in;           /* W_g is [2 n x n_in]; 2 n and n_in 1 .. 2^30 - 1 */
+    int32_t dtype;             /* of everything: GNMR_DTYPE_BF16 or _F16 */
+    const int64_t *d_offsets;  /* as in gnmr_product */
+    const uint8_t *d_mask;
+    int64_t mask_stride;
+    const void *d_x;           /* [rows x n_in] */
+    int64_t x_stride;
+    const void *d_w;           /* per group [2 n x n_in] */
+    int64_t w_stride;
+    int64_t w_group_stride;    /* >= 0 */
+    void *d_out;               /* [rows x n]; no operand */
+    int64_t out_stride;
+    void *d_keep;              /* [rows x 2 n]: [a, b], rounded to dtype, for the backward pass; NULL: not kept */
+    int64_t keep_stride;
+    void *d_scratch;           /* 256-byte aligned, used during the call only; NULL if none is needed */
+    int64_t scratch_bytes;
+} gnmr_gated;
+
+/* Enqueues one on `stream`.  The handle, its limits and errors: as in gnmr_products_run. */
+gnmr_status gnmr_products_gated(gnmr_products *h, const gnmr_gated *p, void *stream);
+
+/* Scratch that gnmr_products_gated needs for *p.  Makes no CUDA call. */
+gnmr_status gnmr_gated_scratch_bytes(const gnmr_gated *p, int64_t *bytes);
+
+/* h[r] = act(a) * b from [a, b] = d_gu[r] ([rows x 2 n], the gate first), for the rows of the groups
+ * whose mask byte is 0, as GNMR_PRODUCT_FORWARD_I8 left them there; the other groups' rows of d_h, and rows of no group,
+ * stay as they are.  NULL d_mask: all groups; NULL d_offsets (groups = 1): all rows.  dtype: BF16 or F16.
+ * Computed in fp32 and rounded once.  Runs on the calling thread's current device, allocates
+ * nothing.  Errors: GNMR_ERR_INVALID_ARG, GNMR_ERR_LAYOUT, GNMR_ERR_CUDA. */
+gnmr_status gnmr_gate(const void *d_gu, int32_t dtype, int32_t activation, int32_t groups, int64_t rows, int32_t n,
+                      int64_t gu_stride, const int64_t *d_offsets, const uint8_t *d_mask, int64_t mask_stride, void *d_h,
+                      int64_t h_stride, void *stream);
+
+/* d_dgu[r] = [dh b act'(a), dh act(a)]: the gradient of [a, b] = d_gu[r] from that of h, for all rows.
+ * d_dgu may be d_gu, with the same stride.  Otherwise as gnmr_gate. */
+gnmr_status gnmr_gate_grad(const void *d_dh, int32_t dtype, int32_t activation, int64_t rows, int32_t n, int64_t dh_stride,
+                           const void *d_gu, int64_t gu_stride, void *d_dgu, int64_t dgu_stride, void *stream);
+
+/* ---- Layer norm -------------------------------------------------------------
+ * By row of x [rows x cols]: mean, rstd = 1 / sqrt(mean of (x - mean)^2 + eps),
+ * y = (x - mean) rstd weight + bias.  Backward, with xh = (x - mean) rstd and t = dy weight:
+ *
+ *   dx      = rstd (t - mean of t - xh (mean of t xh))
+ *   dweight = sum over the rows of dy xh,   dbias = sum over the rows of dy
+ *
+ * Statistics and sums are held in fp32; each output is rounded once.  A row with a NaN or an
+ * infinity has NaN outputs; no other row is touched by it, but the sums over the rows are.
+ * A call repeated on the same operands gives the same bits. */
+typedef struct gnmr_norm {
+    int64_t rows;              /* 0 .. 2^31 - 1 */
+    int64_t cols;              /* 1 .. 2^30 */
+    int32_t dtype;             /* of x, y, dy, dx: BF16, F16 or F32 */
+    int32_t param_dtype;       /* of weight and bias: dtype or F32 */
+    double eps;                /* forward: >= 0 */
+    const void *d_x;
+    int64_t x_stride;          /* >= cols, elements */
+    const void *d_weight;      /* [cols]; NULL: 1 */
+    const void *d_bias;        /* forward: [cols]; NULL: 0 */
+    float *d_mean, *d_rstd;    /* [rows]: forward writes them (either may be NULL), backward reads both */
+    void *d_y;                 /* forward: [rows x cols]; may be d_x, with the same stride */
+    int64_t y_stride;
+    const void *d_dy;          /* backward */
+    int64_t dy_stride;
+    void *d_dx;                /* backward: [rows x cols], NULL: not wanted; may be d_dy, with the same stride */
+    int64_t dx_stride;
+    void *d_dweight, *d_dbias; /* backward: [cols] of grad_dtype; either may be NULL: not wanted */
+    int32_t grad_dtype;        /* BF16, F16 or F32 */
+    int32_t add;               /* backward: add to d_dweight and d_dbias instead of writing them */
+    void *d_scratch;           /* backward: 256-byte aligned, used during the call only */
+    int64_t scratch_bytes;
+} gnmr_norm;
+
+/* Both run on the calling thread's current device and allocate nothing.  No rows: dweight and
+ * dbias are zeros, or left as they are with `add`.  Errors: GNMR_ERR_INVALID_ARG, GNMR_ERR_LAYOUT,
+ * GNMR_ERR_CUDA; detail via gnmr_last_error(NULL). */
+gnmr_status gnmr_layer_norm(const gnmr_norm *p, void *stream);
+gnmr_status gnmr_layer_norm_grad(const gnmr_norm *p, void *stream);
+
+/* Scratch that gnmr_layer_norm_grad needs for *p on any device.  Makes no CUDA call. */
+gnmr_status gnmr_layer_norm_scratch_bytes(const gnmr_norm *p, int64_t *bytes);
+
+/* ---- The norm over many gradients, and clipping --------------------------------
+ * norm = sqrt(sum of x^2 over all tensors); where it is above max_norm, every
+ * element is multiplied by max_norm / norm (rounded to fp32), and the product rounded to its type.
+ * A norm that is not finite scales nothing: the gradients are what they were, and the norm says so.
+ * Squares are summed as in the monitor (fp32 in short blocks, the blocks as float pairs and in
+ * fp64; tensors whose squares leave fp32's range in fp64), so the norm is right over the whole range of the types. */
+typedef struct gnmr_clip gnmr_clip;
+
+/* A plan for `num_tensors` tensors of the given lengths (elements, 0 included) and types (gnmr_dtype),
+ * host arrays that are copied.  It holds no gradient's address, and nothing that a call writes. */
+gnmr_status gnmr_clip_create(int32_t num_tensors, const int64_t *lengths, const int32_t *dtypes, int32_t device,
+                             gnmr_clip **out);
+
+/* Bytes of scratch that a call of gnmr_clip_run needs. */
+gnmr_status gnmr_clip_scratch_bytes(const gnmr_clip *c, int64_t *bytes);
+
+/* One pass on `stream`.  d_in, d_out: HOST arrays of num_tensors device pointers, each aligned to its element
+ * size (NULL for an empty tensor only), read before the call returns.  d_out NULL: the gradients are scaled
+ * where they lie, and written only if they are above the limit; otherwise all of d_out is written (no overlap but of a
+ * tensor with itself).  max_norm: >= 0, infinity to scale nothing.  d_unit_norms: device fp64 [num_norms], the norms of parts that make up the
+ * tensors, as gnmr_step writes them to stats->norm: the norm is formed from them and the gradients are not read for it; NULL: from
+ * the gradients.  d_norm: device fp32 [1], written.  d_scratch: device, 256-byte aligned, used during the call only.
+ * Errors: GNMR_ERR_INVALID_ARG, GNMR_ERR_LAYOUT, GNMR_ERR_CUDA; detail via gnmr_last_error(NULL). */
+gnmr_status gnmr_clip_run(const gnmr_clip *c, const void *const *d_in, void *const *d_out, double max_norm,
+                          const double *d_unit_norms, int64_t num_norms, float *d_norm, void *d_scratch,
+                          int64_t scratch_bytes, void *stream);
+
+/* Waits for the plan's device and frees it.  NULL is accepted. */
+gnmr_status gnmr_clip_destroy(gnmr_clip *c);
 
 #ifdef __cplusplus
 }

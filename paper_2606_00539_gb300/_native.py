@@ -28,6 +28,8 @@ GNMR_POLICY_ACTIVE_CAP, GNMR_POLICY_ADMISSION_CAP, GNMR_POLICY_STATIC_TOP = 0, 1
 GNMR_PRODUCT_FORWARD, GNMR_PRODUCT_INPUT_GRAD = 0, 1
 GNMR_PRODUCT_WEIGHT_GRAD, GNMR_PRODUCT_FORWARD_I8 = 2, 3
 
+GNMR_ACT_SILU, GNMR_ACT_GELU = 0, 1
+
 GNMR_LOOP_AUTO, GNMR_LOOP_SMALL_UNITS, GNMR_LOOP_LARGE_UNITS = 0, 1, 2
 
 _P = ctypes.c_void_p
@@ -120,6 +122,59 @@ class gnmr_product(ctypes.Structure):
     ]
 
 
+class gnmr_gated(ctypes.Structure):
+    _fields_ = [
+        ("groups", ctypes.c_int32),
+        ("activation", ctypes.c_int32),
+        ("rows", ctypes.c_int64),
+        ("n", ctypes.c_int32),
+        ("n_in", ctypes.c_int32),
+        ("dtype", ctypes.c_int32),
+        ("d_offsets", _P),
+        ("d_mask", _P),
+        ("mask_stride", ctypes.c_int64),
+        ("d_x", _P),
+        ("x_stride", ctypes.c_int64),
+        ("d_w", _P),
+        ("w_stride", ctypes.c_int64),
+        ("w_group_stride", ctypes.c_int64),
+        ("d_out", _P),
+        ("out_stride", ctypes.c_int64),
+        ("d_keep", _P),
+        ("keep_stride", ctypes.c_int64),
+        ("d_scratch", _P),
+        ("scratch_bytes", ctypes.c_int64),
+    ]
+
+
+class gnmr_norm(ctypes.Structure):
+    _fields_ = [
+        ("rows", ctypes.c_int64),
+        ("cols", ctypes.c_int64),
+        ("dtype", ctypes.c_int32),
+        ("param_dtype", ctypes.c_int32),
+        ("eps", ctypes.c_double),
+        ("d_x", _P),
+        ("x_stride", ctypes.c_int64),
+        ("d_weight", _P),
+        ("d_bias", _P),
+        ("d_mean", _P),
+        ("d_rstd", _P),
+        ("d_y", _P),
+        ("y_stride", ctypes.c_int64),
+        ("d_dy", _P),
+        ("dy_stride", ctypes.c_int64),
+        ("d_dx", _P),
+        ("dx_stride", ctypes.c_int64),
+        ("d_dweight", _P),
+        ("d_dbias", _P),
+        ("grad_dtype", ctypes.c_int32),
+        ("add", ctypes.c_int32),
+        ("d_scratch", _P),
+        ("scratch_bytes", ctypes.c_int64),
+    ]
+
+
 class GnmrError(RuntimeError):
     def __init__(self, status: int, detail: str):
         super().__init__(f"{status_string(status)} ({detail})" if detail else status_string(status))
@@ -162,6 +217,19 @@ PROTOTYPES = {
     "gnmr_quantize_columns": (ctypes.c_int, [_P, ctypes.c_int32, ctypes.c_int32, ctypes.c_int64, ctypes.c_int64,
                                              ctypes.c_int64, ctypes.c_int64, _P, ctypes.c_int64, _P,
                                              ctypes.c_int64, ctypes.c_int64, _P, _P]),
+    "gnmr_products_gated": (ctypes.c_int, [_P, _P, _P]),
+    "gnmr_gated_scratch_bytes": (ctypes.c_int, [_P, _P]),
+    "gnmr_gate": (ctypes.c_int, [_P, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, ctypes.c_int64, ctypes.c_int32,
+                                 ctypes.c_int64, _P, _P, ctypes.c_int64, _P, ctypes.c_int64, _P]),
+    "gnmr_gate_grad": (ctypes.c_int, [_P, ctypes.c_int32, ctypes.c_int32, ctypes.c_int64, ctypes.c_int32,
+                                      ctypes.c_int64, _P, ctypes.c_int64, _P, ctypes.c_int64, _P]),
+    "gnmr_layer_norm": (ctypes.c_int, [_P, _P]),
+    "gnmr_layer_norm_grad": (ctypes.c_int, [_P, _P]),
+    "gnmr_layer_norm_scratch_bytes": (ctypes.c_int, [_P, _P]),
+    "gnmr_clip_create": (ctypes.c_int, [ctypes.c_int32, _P, _P, ctypes.c_int32, ctypes.POINTER(_P)]),
+    "gnmr_clip_scratch_bytes": (ctypes.c_int, [_P, _P]),
+    "gnmr_clip_run": (ctypes.c_int, [_P, _P, _P, ctypes.c_double, _P, ctypes.c_int64, _P, _P, ctypes.c_int64, _P]),
+    "gnmr_clip_destroy": (ctypes.c_int, [_P]),
 }
 
 _lib = None
@@ -343,3 +411,34 @@ def gnmr_quantize_columns(d_x: int, dtype: int, groups: int, rows: int, cols: in
                           q_group_stride: int, d_scale: int, stream: int = 0) -> None:
     _check(load().gnmr_quantize_columns(d_x, dtype, groups, rows, cols, x_stride, x_group_stride, d_mask, mask_stride,
                                    d_q, q_stride, q_group_stride, d_scale, stream), None)
+
+
+def gnmr_gated_scratch_bytes(p: gnmr_gated) -> int:
+    n = ctypes.c_int64(0)
+    _check(load().gnmr_gated_scratch_bytes(ctypes.addressof(p), ctypes.addressof(n)), None)
+    return n.value
+
+
+def gnmr_layer_norm_scratch_bytes(p: gnmr_norm) -> int:
+    n = ctypes.c_int64(0)
+    _check(load().gnmr_layer_norm_scratch_bytes(ctypes.addressof(p), ctypes.addressof(n)), None)
+    return n.value
+
+
+def gnmr_clip_create(lengths, dtypes, device: int = 0) -> int:
+    import numpy as np
+    ln = np.ascontiguousarray(lengths, dtype=np.int64)
+    dt = np.ascontiguousarray(dtypes, dtype=np.int32)
+    h = _P()
+    _check(load().gnmr_clip_create(len(ln), ln.ctypes.data, dt.ctypes.data, int(device), ctypes.byref(h)), None)
+    return h.value
+
+
+def gnmr_clip_scratch_bytes(handle: int) -> int:
+    n = ctypes.c_int64(0)
+    _check(load().gnmr_clip_scratch_bytes(handle, ctypes.addressof(n)), None)
+    return n.value
+
+
+def gnmr_clip_destroy(handle: int) -> None:
+    _check(load().gnmr_clip_destroy(handle), None)

@@ -19,10 +19,10 @@ LIB_PATH = os.path.join(PKG, "libgnmr.so")
 
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 CUDA_SOURCES = ["gnmr_kernels.cu", "gnmr_static.cu", "gnmr_actuator.cu", "gnmr_products.cu", "gnmr_products_i8.cu",
-                "gnmr_quantize.cu"]
+                "gnmr_quantize.cu", "gnmr_gate.cu", "gnmr_norm.cu", "gnmr_clip.cu"]
 CXX_SOURCES = ["gnmr_api.cpp", "gnmr_plan.cpp"]
 HEADERS = ["gnmr_internal.h", "gnmr_stream.cuh", "gnmr_mma.cuh", "gnmr_tiles.cuh",
-           "gnmr_products.h"]
+           "gnmr_products.h", "gnmr_act.cuh", "gnmr_rows.cuh"]
 
 
 def _cuda_home() -> str:

@@ -5,6 +5,7 @@
 //   forward      A = W_g      [n_out lanes], c along its rows     B = x's rows    c < n_in
 //   input grad   A = W_g^T    [n_in lanes], lanes along its rows  B = dy's rows   c < n_out
 //   weight grad  A = x^T      [n_in lanes], lanes along its rows  B = dy^T        c < the group's rows
+//   gated block  A = W_g's two halves, row by row in turn         B = x's rows    c < n_in
 // so that the tensor cores' 128 lanes lie along the output's contiguous axis and a
 // group's ragged rows are columns, of which a tile has any multiple of 32 up to 256.
 //
@@ -49,6 +50,7 @@ using namespace gnmr_tiles;
 using gnmr::Operand;
 using gnmr::Operands;
 
+constexpr int kGated = 4;                              // an op of this file: two projections, the activation, the product
 constexpr int kStep = 64;                              // contraction steps of a stage: 128-byte rows of 16 bits
 constexpr int kProducerWarp = 0, kMultiplyWarp = 1, kTailWarp = 2, kTablesWarp = 3;
 constexpr int kAStage = 128 * 128;                     // bytes of A's tile in one CTA
@@ -127,7 +129,9 @@ __device__ __forceinline__ bool load_stages(const CUtensorMap &map_a, const CUte
                 const uint32_t bar = first_tail ? tail + stage * 8 : full + stage * 8;
                 const uint32_t a = base + stage * S::kStage, b = a + kAStage;
                 arrive_expect(first_tail ? in_cta(bar, c.rank) : bar, bytes);
-                if (!a_along_lanes(kOp)) {
+                if (kOp == kGated) {
+                    load_tile<2>(a, &map_a, at, 0, a_lane >> 1, za, bar);
+                } else if (!a_along_lanes(kOp)) {
                     load_tile<2>(a, &map_a, at, a_lane, 0, za, bar);
                 } else if (p.a_blocks) {
                     load_tile<2>(a, &map_a, 0, at, a_lane >> 6, za, bar);
@@ -295,7 +299,7 @@ product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant_
             fine = clear_tails<kColumns>(p, c);
     } else {
         more_registers<Roles<kOp>::kEpilogueRegisters>();
-        fine = write_outputs<kColumns, Roles<kOp>::kSides, false, kStep, 2>(p, c);
+        fine = write_outputs<kColumns, Roles<kOp>::kSides, false, kStep, 2, kOp == kGated>(p, c);
     }
     finish_pair(fine, p.gave_up);
     if (warp == kMultiplyWarp)
@@ -419,7 +423,8 @@ cudaError_t launch(const gnmr_products *h, const Operands &o, Product p, cudaStr
     p.ring = ring_of(p.groups, Shape<kColumns>::kStage, 0);
     CUtensorMap a, b;
     const CUtensorMapDataType type = p.bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
-    *mapped = gnmr::tile_map(h, &a, o.a, type, a_along_lanes(kOp) ? kStep : 128, p.a_blocks ? 2 : 1) &&
+    *mapped = (kOp == kGated ? gnmr::halves_map(h, &a, o.a, type, 128)
+                             : gnmr::tile_map(h, &a, o.a, type, a_along_lanes(kOp) ? kStep : 128, p.a_blocks ? 2 : 1)) &&
               gnmr::tile_map(h, &b, o.b, type, b_along_columns(kOp) ? kStep : Shape<kColumns>::kBox, p.b_blocks ? 2 : 1);
     if (!*mapped)
         return cudaSuccess;
@@ -446,11 +451,12 @@ template <int kColumns, int kOp> cudaError_t allow_shared()
 
 // The kernels, by op and whether a group has few rows.
 using Launch = cudaError_t (*)(const gnmr_products *, const Operands &, Product, cudaStream_t, bool *);
-constexpr Launch kLaunch[4][2] = {
+constexpr Launch kLaunch[5][2] = {
     {launch<256, GNMR_PRODUCT_FORWARD>, launch<64, GNMR_PRODUCT_FORWARD>},
     {launch<256, GNMR_PRODUCT_INPUT_GRAD>, launch<64, GNMR_PRODUCT_INPUT_GRAD>},
     {launch<256, GNMR_PRODUCT_WEIGHT_GRAD>, launch<256, GNMR_PRODUCT_WEIGHT_GRAD>},
     {gnmr::launch_codes, gnmr::launch_codes},
+    {launch<256, kGated>, launch<64, kGated>},
 };
 
 cudaError_t allow_all_shared()
@@ -458,7 +464,8 @@ cudaError_t allow_all_shared()
     cudaError_t e = cudaSuccess;
     for (const cudaError_t r : {allow_shared<256, GNMR_PRODUCT_FORWARD>(), allow_shared<64, GNMR_PRODUCT_FORWARD>(),
                                 allow_shared<256, GNMR_PRODUCT_INPUT_GRAD>(), allow_shared<64, GNMR_PRODUCT_INPUT_GRAD>(),
-                                allow_shared<256, GNMR_PRODUCT_WEIGHT_GRAD>(), gnmr::allow_codes_shared()})
+                                allow_shared<256, GNMR_PRODUCT_WEIGHT_GRAD>(), allow_shared<256, kGated>(), allow_shared<64, kGated>(),
+                                gnmr::allow_codes_shared()})
         e = e == cudaSuccess ? r : e;
     return e;
 }
@@ -466,6 +473,23 @@ cudaError_t allow_all_shared()
 }  // namespace
 
 namespace gnmr {
+
+static bool encode(const gnmr_products *h, CUtensorMap *map, CUtensorMapDataType type, const void *at, const cuuint64_t *dims,
+                   const cuuint64_t *strides, const cuuint32_t *box)
+{
+    const cuuint32_t one[4] = {1, 1, 1, 1};
+    const auto once = [&] {
+        return h->encode(map, type, 4, const_cast<void *>(at), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                         CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    };
+    CUresult r = once();
+    if (r == CUDA_ERROR_INVALID_CONTEXT || r == CUDA_ERROR_NOT_INITIALIZED) {
+        cudaSetDevice(h->device);                        // a host thread's first CUDA call: it has no context yet
+        r = once();
+    }
+    return r == CUDA_SUCCESS;
+}
 
 bool tile_map(const gnmr_products *h, CUtensorMap *map, const Operand &o, CUtensorMapDataType type, int high, int blocks)
 {
@@ -479,21 +503,144 @@ bool tile_map(const gnmr_products *h, CUtensorMap *map, const Operand &o, CUtens
                                 static_cast<cuuint64_t>(blocks > 1 ? o.cols / wide : 1), static_cast<cuuint64_t>(o.groups)};
     const cuuint64_t strides[3] = {row, 128, o.groups > 1 ? static_cast<cuuint64_t>(o.group_stride) * o.read_bytes : row};
     const cuuint32_t box[4] = {static_cast<cuuint32_t>(wide), static_cast<cuuint32_t>(high), static_cast<cuuint32_t>(blocks), 1};
-    const cuuint32_t one[4] = {1, 1, 1, 1};
-    const auto encode = [&] {
-        return h->encode(map, type, 4, const_cast<void *>(o.at), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                         CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    };
-    CUresult r = encode();
-    if (r == CUDA_ERROR_INVALID_CONTEXT || r == CUDA_ERROR_NOT_INITIALIZED) {
-        cudaSetDevice(h->device);                        // a host thread's first CUDA call: it has no context yet
-        r = encode();
-    }
-    return r == CUDA_SUCCESS;
+    return encode(h, map, type, o.at, dims, strides, box);
+}
+
+bool halves_map(const gnmr_products *h, CUtensorMap *map, const Operand &o, CUtensorMapDataType type, int high)
+{
+    const cuuint64_t row = static_cast<cuuint64_t>(o.stride) * o.read_bytes, half = static_cast<cuuint64_t>(o.rows / 2);
+    const cuuint64_t dims[4] = {static_cast<cuuint64_t>(o.cols), 2, half, static_cast<cuuint64_t>(o.groups)};
+    const cuuint64_t strides[3] = {half * row, row, o.groups > 1 ? static_cast<cuuint64_t>(o.group_stride) * o.read_bytes : row};
+    const cuuint32_t box[4] = {static_cast<cuuint32_t>(128 / o.read_bytes), 2, static_cast<cuuint32_t>(high / 2), 1};
+    return encode(h, map, type, o.at, dims, strides, box);
 }
 
 }  // namespace gnmr
+
+namespace {
+
+// A gated block as the forward product of both its projections.
+gnmr_status check(const gnmr_gated *p, gnmr_product *both)
+{
+    if (!p)
+        return fail(GNMR_ERR_INVALID_ARG, "products: NULL argument");
+    if (p->activation != GNMR_ACT_SILU && p->activation != GNMR_ACT_GELU)
+        return fail(GNMR_ERR_INVALID_ARG, "products: unknown activation");
+    if (p->n < 1 || p->n > INT32_MAX / 4)
+        return fail(GNMR_ERR_INVALID_ARG, "products: n out of range");
+    const int64_t wide = 2 * int64_t(p->n), far = int64_t(1) << 36;
+    if (p->out_stride < p->n || (p->d_keep && p->keep_stride < wide))
+        return fail(GNMR_ERR_LAYOUT, "products: a stride below what it strides over");
+    if (p->out_stride > far || (p->d_keep && p->keep_stride > far))
+        return fail(GNMR_ERR_LAYOUT, "products: a stride above 2^36 elements");
+    if (misaligned(p->d_keep, 2))
+        return fail(GNMR_ERR_LAYOUT, "products: an operand not aligned to its element size");
+    *both = {};
+    both->op = GNMR_PRODUCT_FORWARD;
+    both->groups = p->groups;
+    both->rows = p->rows;
+    both->n_out = static_cast<int32_t>(wide);
+    both->n_in = p->n_in;
+    both->dtype = both->out_dtype = p->dtype;
+    both->d_offsets = p->d_offsets;
+    both->d_mask = p->d_mask;
+    both->mask_stride = p->mask_stride;
+    both->d_x = p->d_x;
+    both->x_stride = p->x_stride;
+    both->d_w = p->d_w;
+    both->w_stride = p->w_stride;
+    both->w_group_stride = p->w_group_stride;
+    both->d_out = p->d_out;
+    both->out_stride = wide;
+    both->d_scratch = p->d_scratch;
+    both->scratch_bytes = p->scratch_bytes;
+    return check(both);
+}
+
+// One product, or, as the forward product of both projections, a gated block; checked.
+gnmr_status run(gnmr_products *h, const gnmr_product *p, const gnmr_gated *gated, void *stream)
+{
+    if (const gnmr_status s = gave_up(h))
+        return s;
+    const bool codes = p->op == GNMR_PRODUCT_FORWARD_I8, wgrad = p->op == GNMR_PRODUCT_WEIGHT_GRAD;
+    if (p->rows == 0 && (!wgrad || p->add))
+        return GNMR_OK;
+    Operands o = operands(p);
+    const int64_t need = o.a.copy_bytes() + o.b.copy_bytes();
+    if (need && (!p->d_scratch || p->scratch_bytes < need || misaligned(p->d_scratch, 256)))
+        return fail(GNMR_ERR_LAYOUT, "products: operands that cannot be read in place, and no scratch for them");
+
+    Product q = {};
+    const bool back = p->op == GNMR_PRODUCT_INPUT_GRAD;
+    q.lanes = wgrad || back ? p->n_in : p->n_out;
+    q.depth = wgrad ? 0 : back ? p->n_out : p->n_in;
+    q.cols = wgrad ? p->n_out : 0;
+    const int64_t lane_tiles = (int64_t(q.lanes) + kLanes - 1) / kLanes;
+    q.lane_tiles_inverse = static_cast<unsigned>(((int64_t(1) << 32) + lane_tiles - 1) / lane_tiles);
+    q.rows = static_cast<int>(p->rows);
+    q.groups = p->groups;
+    q.offsets = p->d_offsets;
+    q.mask = p->d_mask;
+    q.mask_stride = p->mask_stride;
+    q.want = codes ? 0 : 1;
+    q.a_by_group = o.a.groups > 1;
+    q.a_blocks = (wgrad || back) && q.lanes % 64 == 0;
+    q.b_blocks = wgrad && q.cols % 64 == 0;
+    q.granule = q.b_blocks ? 128 : 32;
+    q.bf16 = !codes && p->dtype == GNMR_DTYPE_BF16;
+    q.piece = !codes && p->out_dtype == GNMR_DTYPE_F32 ? 512 : 1024;
+    q.out = p->d_out;
+    q.out_type = p->out_dtype;
+    q.add = wgrad && p->add;
+    q.out_col = p->out_stride;
+    q.out_group = p->out_group_stride;
+    q.pairs_aligned = !misaligned(p->d_out, 4) && p->out_stride % 2 == 0 && (!wgrad || p->groups == 1 || p->out_group_stride % 2 == 0);
+    if (gated) {
+        q.out_col = gated->out_stride;
+        q.pairs_aligned = !misaligned(gated->d_out, 4) && gated->out_stride % 2 == 0;
+        q.act = gated->activation;
+        q.keep = gated->d_keep;
+        q.keep_col = gated->keep_stride;
+        q.keep_aligned = !misaligned(gated->d_keep, 4) && gated->keep_stride % 2 == 0 && gated->n % 2 == 0;
+    }
+    if (codes)
+        q.lane_scale = p->d_w_scale, q.col_scale = p->d_x_scale;
+    q.parts = h->parts;
+    q.tickets = h->tickets;
+    q.gave_up = h->gave_up;
+    q.most_ns = h->wait_ns < 0 ? most_ns(p, q, lane_tiles) : h->wait_ns;
+
+    int prev = h->device;
+    cudaGetDevice(&prev);
+    if (prev != h->device)
+        cudaSetDevice(h->device);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    cudaError_t e = cudaSuccess;
+    char *scratch = static_cast<char *>(p->d_scratch);
+    for (Operand *m : {&o.a, &o.b})
+        if (const int64_t n = m->copy_bytes(); n && e == cudaSuccess) {
+            e = gnmr::copy_operand(*m, scratch, 2 * h->pairs, st);
+            const bool widened = m->bytes != m->read_bytes;      // then the zeros after the last column count as columns
+            *m = Operand{scratch, m->rows, widened ? m->held() : m->cols, m->held(), m->rows * m->held(), m->groups, m->read_bytes,
+                         m->read_bytes};
+            scratch += n;
+        }
+    const bool few = !wgrad && (p->rows <= kFewRows * p->groups || (p->groups == 1 && lane_tiles * ((p->rows + 63) / 64) <= h->pairs));
+    bool mapped = true;
+    if (e == cudaSuccess)
+        e = kLaunch[gated ? kGated : p->op][few](h, o, q, st, &mapped);
+    if (e != cudaSuccess)
+        cudaGetLastError();                              // reported here, not by the caller's next call
+    if (prev != h->device)
+        cudaSetDevice(prev);
+    if (!mapped)
+        return fail(GNMR_ERR_LAYOUT, "products: the strides of an operand have no tensor map");
+    if (e != cudaSuccess)
+        return fail(GNMR_ERR_CUDA, cudaGetErrorString(e));
+    return GNMR_OK;
+}
+
+}  // namespace
 
 extern "C" {
 
@@ -568,76 +715,30 @@ gnmr_status gnmr_products_run(gnmr_products *h, const gnmr_product *p, void *str
         return fail(GNMR_ERR_INVALID_ARG, "products: NULL handle");
     if (const gnmr_status s = check(p))
         return s;
-    if (const gnmr_status s = gave_up(h))
+    return run(h, p, nullptr, stream);
+}
+
+gnmr_status gnmr_gated_scratch_bytes(const gnmr_gated *p, int64_t *bytes)
+{
+    if (!bytes)
+        return fail(GNMR_ERR_INVALID_ARG, "products: NULL argument");
+    *bytes = 0;
+    gnmr_product both;
+    if (const gnmr_status s = check(p, &both))
         return s;
-    const bool codes = p->op == GNMR_PRODUCT_FORWARD_I8, wgrad = p->op == GNMR_PRODUCT_WEIGHT_GRAD;
-    if (p->rows == 0 && (!wgrad || p->add))
-        return GNMR_OK;
-    Operands o = operands(p);
-    const int64_t need = o.a.copy_bytes() + o.b.copy_bytes();
-    if (need && (!p->d_scratch || p->scratch_bytes < need || misaligned(p->d_scratch, 256)))
-        return fail(GNMR_ERR_LAYOUT, "products: operands that cannot be read in place, and no scratch for them");
-
-    Product q = {};
-    const bool back = p->op == GNMR_PRODUCT_INPUT_GRAD;
-    q.lanes = wgrad || back ? p->n_in : p->n_out;
-    q.depth = wgrad ? 0 : back ? p->n_out : p->n_in;
-    q.cols = wgrad ? p->n_out : 0;
-    const int64_t lane_tiles = (int64_t(q.lanes) + kLanes - 1) / kLanes;
-    q.lane_tiles_inverse = static_cast<unsigned>(((int64_t(1) << 32) + lane_tiles - 1) / lane_tiles);
-    q.rows = static_cast<int>(p->rows);
-    q.groups = p->groups;
-    q.offsets = p->d_offsets;
-    q.mask = p->d_mask;
-    q.mask_stride = p->mask_stride;
-    q.want = codes ? 0 : 1;
-    q.a_by_group = o.a.groups > 1;
-    q.a_blocks = (wgrad || back) && q.lanes % 64 == 0;
-    q.b_blocks = wgrad && q.cols % 64 == 0;
-    q.granule = q.b_blocks ? 128 : 32;
-    q.bf16 = !codes && p->dtype == GNMR_DTYPE_BF16;
-    q.piece = !codes && p->out_dtype == GNMR_DTYPE_F32 ? 512 : 1024;
-    q.out = p->d_out;
-    q.out_type = p->out_dtype;
-    q.add = wgrad && p->add;
-    q.out_col = p->out_stride;
-    q.out_group = p->out_group_stride;
-    q.pairs_aligned = !misaligned(p->d_out, 4) && p->out_stride % 2 == 0 && (!wgrad || p->groups == 1 || p->out_group_stride % 2 == 0);
-    if (codes)
-        q.lane_scale = p->d_w_scale, q.col_scale = p->d_x_scale;
-    q.parts = h->parts;
-    q.tickets = h->tickets;
-    q.gave_up = h->gave_up;
-    q.most_ns = h->wait_ns < 0 ? most_ns(p, q, lane_tiles) : h->wait_ns;
-
-    int prev = h->device;
-    cudaGetDevice(&prev);
-    if (prev != h->device)
-        cudaSetDevice(h->device);
-    cudaStream_t st = static_cast<cudaStream_t>(stream);
-    cudaError_t e = cudaSuccess;
-    char *scratch = static_cast<char *>(p->d_scratch);
-    for (Operand *m : {&o.a, &o.b})
-        if (const int64_t n = m->copy_bytes(); n && e == cudaSuccess) {
-            e = gnmr::copy_operand(*m, scratch, 2 * h->pairs, st);
-            const bool widened = m->bytes != m->read_bytes;      // then the zeros after the last column count as columns
-            *m = Operand{scratch, m->rows, widened ? m->held() : m->cols, m->held(), m->rows * m->held(), m->groups, m->read_bytes,
-                         m->read_bytes};
-            scratch += n;
-        }
-    const bool few = !wgrad && (p->rows <= kFewRows * p->groups || (p->groups == 1 && lane_tiles * ((p->rows + 63) / 64) <= h->pairs));
-    bool mapped = true;
-    if (e == cudaSuccess)
-        e = kLaunch[p->op][few](h, o, q, st, &mapped);
-    if (e != cudaSuccess)
-        cudaGetLastError();                              // reported here, not by the caller's next call
-    if (prev != h->device)
-        cudaSetDevice(prev);
-    if (!mapped)
-        return fail(GNMR_ERR_LAYOUT, "products: the strides of an operand have no tensor map");
-    if (e != cudaSuccess)
-        return fail(GNMR_ERR_CUDA, cudaGetErrorString(e));
+    const Operands o = operands(&both);
+    *bytes = o.a.copy_bytes() + o.b.copy_bytes();
     return GNMR_OK;
+}
+
+gnmr_status gnmr_products_gated(gnmr_products *h, const gnmr_gated *p, void *stream)
+{
+    if (!h)
+        return fail(GNMR_ERR_INVALID_ARG, "products: NULL handle");
+    gnmr_product both;
+    if (const gnmr_status s = check(p, &both))
+        return s;
+    return run(h, &both, p, stream);
 }
 
 gnmr_status gnmr_products_status(gnmr_products *h)

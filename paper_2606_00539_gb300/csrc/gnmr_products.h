@@ -57,6 +57,10 @@ struct Operands {
 // first column, or 0 where there are several blocks; row; block, or 0 where there is one; group.
 bool tile_map(const gnmr_products *h, CUtensorMap *map, const Operand &o, CUtensorMapDataType type, int high, int blocks);
 
+// Tiles of `high` rows by 128 bytes whose rows come from the operand's two halves in turn: row 2 i is row i, row
+// 2 i + 1 is row rows / 2 + i.  Coordinates: first column; 0; row of a half; group.
+bool halves_map(const gnmr_products *h, CUtensorMap *map, const Operand &o, CUtensorMapDataType type, int high);
+
 // The copy of an operand in `to`.
 cudaError_t copy_operand(const Operand &o, void *to, int sms, cudaStream_t st);
 

@@ -1,0 +1,116 @@
+// 16 bytes of a row at a time, widened to fp32 and rounded back: what the row kernels of the
+// gated blocks, the layer norm and the clipping share.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+
+#include <cstdint>
+#include <type_traits>
+
+#include "gnmr.h"
+
+namespace gnmr_rows {
+
+template <typename T> __device__ __forceinline__ float to_f32(T v) { return static_cast<float>(v); }
+template <> __device__ __forceinline__ float to_f32(__nv_bfloat16 v) { return __bfloat162float(v); }
+template <> __device__ __forceinline__ float to_f32(__half v) { return __half2float(v); }
+
+template <typename T> __device__ __forceinline__ T from_f32(float v) { return static_cast<T>(v); }
+template <> __device__ __forceinline__ __nv_bfloat16 from_f32(float v) { return __float2bfloat16_rn(v); }
+template <> __device__ __forceinline__ __half from_f32(float v) { return __float2half_rn(v); }
+
+// Elements of 16 bytes.
+template <typename T> constexpr int kIn16 = 16 / static_cast<int>(sizeof(T));
+
+template <typename T> __device__ __forceinline__ void widen(const uint4 &v, float (&f)[kIn16<T>])
+{
+    const unsigned w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(T) == 4) {
+            f[i] = __uint_as_float(w[i]);
+        } else if constexpr (std::is_same_v<T, __nv_bfloat16>) {
+            f[2 * i] = __uint_as_float(w[i] << 16);
+            f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        } else {
+            const float2 p = __half22float2(reinterpret_cast<const __half2 &>(w[i]));
+            f[2 * i] = p.x;
+            f[2 * i + 1] = p.y;
+        }
+    }
+}
+
+template <typename T> __device__ __forceinline__ uint4 narrow(const float (&f)[kIn16<T>])
+{
+    unsigned w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(T) == 4) {
+            w[i] = __float_as_uint(f[i]);
+        } else if constexpr (std::is_same_v<T, __nv_bfloat16>) {
+            const __nv_bfloat162 p = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+            w[i] = reinterpret_cast<const unsigned &>(p);
+        } else {
+            const __half2 p = __floats2half2_rn(f[2 * i], f[2 * i + 1]);
+            w[i] = reinterpret_cast<const unsigned &>(p);
+        }
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// Loads and stores of what is used once.  Volatile: none moves up over griddepcontrol.wait.
+__device__ __forceinline__ uint4 load_once(const void *p)
+{
+    uint4 v;
+    asm volatile("ld.global.L1::no_allocate.L2::256B.v4.u32 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+                 : "l"(p));
+    return v;
+}
+
+__device__ __forceinline__ void store_once(void *p, const uint4 &v)
+{
+    asm volatile("st.global.L1::no_allocate.v4.u32 [%0], {%1, %2, %3, %4};" ::"l"(p), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w)
+                 : "memory");
+}
+
+// ---- host ---------------------------------------------------------------------
+
+inline bool misaligned(const void *p, size_t bytes) { return reinterpret_cast<uintptr_t>(p) % bytes != 0; }
+
+inline size_t element_bytes(int32_t dtype) { return dtype == GNMR_DTYPE_F32 ? 4 : 2; }
+
+inline bool known(int32_t dtype) { return dtype == GNMR_DTYPE_F32 || dtype == GNMR_DTYPE_BF16 || dtype == GNMR_DTYPE_F16; }
+
+// Whether rows of `stride` elements from p on all start at multiples of 16 bytes.
+inline bool rows_of_16(const void *p, int64_t rows, int64_t stride, size_t bytes)
+{
+    return !misaligned(p, 16) && (rows <= 1 || stride * bytes % 16 == 0);
+}
+
+// The current device's SMs, or what hides them.
+inline cudaError_t current_sms(int *sms)
+{
+    int dev = 0;
+    const cudaError_t e = cudaGetDevice(&dev);
+    return e == cudaSuccess ? cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev) : e;
+}
+
+// Calls f with a value of the type that `dtype` names.
+template <typename F> cudaError_t by_type(int32_t dtype, F f)
+{
+    if (dtype == GNMR_DTYPE_F32)
+        return f(0.0f);
+    if (dtype == GNMR_DTYPE_BF16)
+        return f(__nv_bfloat16());
+    return f(__half());
+}
+
+template <typename F> cudaError_t by_16_bit_type(int32_t dtype, F f)
+{
+    return dtype == GNMR_DTYPE_BF16 ? f(__nv_bfloat16()) : f(__half());
+}
+
+}  // namespace gnmr_rows

@@ -49,6 +49,11 @@ template <> struct Elem<1> {             // bf16, two per 32-bit word
     static constexpr uint32_t kMagnitude = 0x7fff7fffu;
 };
 
+template <> struct Elem<2> {             // f16, two per 32-bit word
+    static constexpr int kBytes = 2;
+    static constexpr uint32_t kMagnitude = 0x7fff7fffu;
+};
+
 // 16-byte streaming load: no L1 allocation, 256-byte L2 prefetch granularity.
 // A coherent load, and volatile like the element loads below: a kernel that
 // was started early (griddepcontrol) knows its addresses before the data is
@@ -99,6 +104,12 @@ template <> __device__ __forceinline__ uint32_t ld_elem_bits<1>(const char *p)
     asm volatile("ld.global.u16 %0, [%1];" : "=h"(v) : "l"(p));
     return static_cast<uint32_t>(v) << 16;
 }
+template <> __device__ __forceinline__ uint32_t ld_elem_bits<2>(const char *p)
+{
+    float v;
+    asm volatile("{\n.reg .b16 h;\nld.global.b16 h, [%1];\ncvt.f32.f16 %0, h;\n}" : "=f"(v) : "l"(p));
+    return __float_as_uint(v);
+}
 
 // Sum of squares of the elements packed in one vector, in fp32 (two
 // independent chains per vector).
@@ -121,6 +132,19 @@ template <> __device__ __forceinline__ float vec_sumsq<1>(const Vec &v)
     for (int i = 0; i < kVecWords; ++i) {
         const float lo = __uint_as_float(v.w[i] << 16);
         const float hi = __uint_as_float(v.w[i] & 0xffff0000u);
+        s0 = fmaf(lo, lo, s0);
+        s1 = fmaf(hi, hi, s1);
+    }
+    return s0 + s1;
+}
+
+template <> __device__ __forceinline__ float vec_sumsq<2>(const Vec &v)
+{
+    float s0 = 0.f, s1 = 0.f;
+#pragma unroll
+    for (int i = 0; i < kVecWords; ++i) {
+        float lo, hi;
+        asm("{\n.reg .b16 a, b;\nmov.b32 {a, b}, %2;\ncvt.f32.f16 %0, a;\ncvt.f32.f16 %1, b;\n}" : "=f"(lo), "=f"(hi) : "r"(v.w[i]));
         s0 = fmaf(lo, lo, s0);
         s1 = fmaf(hi, hi, s1);
     }

@@ -9,6 +9,7 @@
 #include <cstdint>
 
 #include "gnmr.h"
+#include "gnmr_act.cuh"
 #include "gnmr_mma.cuh"
 
 namespace gnmr_tiles {
@@ -43,6 +44,10 @@ struct Product {
     int add;
     int64_t out_col, out_group;
     const float *lane_scale, *col_scale;
+    int act;                           // gated: lanes are the two projections' in turn
+    void *keep;
+    int64_t keep_col;
+    int keep_aligned;
     float *parts;
     unsigned *tickets;
     int *gave_up;
@@ -386,6 +391,73 @@ __device__ __forceinline__ void finish(const Product &p, const Item &it, uint32_
     }
 }
 
+// The same for a gated block: lanes 2 i and 2 i + 1 are output i's two projections.  Two
+// columns of a lane pair are exchanged, so that the even lane forms the first column's h and the odd
+// lane the second's; then two lane pairs exchange h's of four columns, so that each thread stores
+// two outputs of one column.  A warp's outputs of a column are 32 contiguous bytes.
+template <int kPieces, int kType, int kAct>
+__device__ __forceinline__ void finish_gated(const Product &p, const Item &it, uint32_t (&acc)[kPieces][16], int lane, int col, int span)
+{
+    const int odd = lane & 1, second = (lane >> 1) & 1, half = p.lanes >> 1;
+    const int at = lane >> 1, first = at & ~1;           // this lane's output, and the first of the two that it stores
+    const int64_t row = int64_t(it.row0) + it.col0 + col;
+    uint16_t *out = static_cast<uint16_t *>(p.out) + row * p.out_col + first;
+    uint16_t *keep = static_cast<uint16_t *>(p.keep) + row * p.keep_col + (odd ? half : 0) + first;
+    const int left = it.cols - col;
+    const int there = min(half - first, 2);              // of the two outputs: 0 or less, 1, 2
+    const unsigned which = second ? 0x3276 : 0x5410;
+#pragma unroll
+    for (int q = 0; q < kPieces; ++q) {
+        const int n = min(span, left) - q * 16;          // columns of this piece that there are
+        if (n <= 0)
+            break;
+        if (p.keep) {
+#pragma unroll
+            for (int j = 0; j < 16; j += 2) {
+                const unsigned w = pack<kType>(__uint_as_float(acc[q][j]), __uint_as_float(acc[q][j + 1]));
+                const unsigned two = __byte_perm(w, __shfl_xor_sync(~0u, w, 2), which);
+                uint16_t *to = keep + (j + second) * p.keep_col;
+                if (j + second < n) {
+                    if (p.keep_aligned && there == 2) {
+                        *reinterpret_cast<unsigned *>(to) = two;
+                    } else {
+                        if (there > 0)
+                            to[0] = static_cast<uint16_t>(two);
+                        if (there > 1)
+                            to[1] = static_cast<uint16_t>(two >> 16);
+                    }
+                }
+            }
+            keep += 16 * p.keep_col;
+        }
+        float h[8];                                      // of columns 2 i + odd
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float mine = __uint_as_float(odd ? acc[q][2 * i + 1] : acc[q][2 * i]);
+            const float other = __shfl_xor_sync(~0u, __uint_as_float(odd ? acc[q][2 * i] : acc[q][2 * i + 1]), 1);
+            h[i] = gnmr_act::activated<kAct>(odd ? other : mine) * (odd ? mine : other);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) {
+            const unsigned w = pack<kType>(h[i], h[i + 1]);
+            const unsigned two = __byte_perm(w, __shfl_xor_sync(~0u, w, 2), which);
+            const int c = 2 * (i + second) + odd;
+            uint16_t *to = out + c * p.out_col;
+            if (c < n) {
+                if (p.pairs_aligned && there == 2) {
+                    *reinterpret_cast<unsigned *>(to) = two;
+                } else {
+                    if (there > 0)
+                        to[0] = static_cast<uint16_t>(two);
+                    if (there > 1)
+                        to[1] = static_cast<uint16_t>(two >> 16);
+                }
+            }
+        }
+        out += 16 * p.out_col;
+    }
+}
+
 // The first piece's sums, or another's added to them.
 template <bool kCodes>
 __device__ __forceinline__ void begin_sum(uint32_t (&acc)[16])
@@ -493,7 +565,7 @@ __device__ __forceinline__ bool join_parts(const Product &p, const Cta &c, const
 
 // The epilogue's warps, four (one to 32 lanes) for each of kSides shares of a tile's columns: its
 // pieces added up and written.  kCtas: those that multiply as one.
-template <int kColumns, int kSides, bool kCodes, int kStep, int kCtas>
+template <int kColumns, int kSides, bool kCodes, int kStep, int kCtas, bool kGated = false>
 __device__ __forceinline__ bool write_outputs(const Product &p, const Cta &c)
 {
     constexpr int kPieces = kColumns / 16 / kSides;      // of 16 columns
@@ -551,7 +623,16 @@ __device__ __forceinline__ bool write_outputs(const Product &p, const Cta &c)
             continue;
         if (p.add && it.depth == 0)
             continue;                                    // nothing to add
-        if (p.out_type == GNMR_DTYPE_F32)
+        if (kGated) {
+            if (p.bf16 && p.act == GNMR_ACT_SILU)
+                finish_gated<kPieces, GNMR_DTYPE_BF16, GNMR_ACT_SILU>(p, it, acc, at, col, span);
+            else if (p.bf16)
+                finish_gated<kPieces, GNMR_DTYPE_BF16, GNMR_ACT_GELU>(p, it, acc, at, col, span);
+            else if (p.act == GNMR_ACT_SILU)
+                finish_gated<kPieces, GNMR_DTYPE_F16, GNMR_ACT_SILU>(p, it, acc, at, col, span);
+            else
+                finish_gated<kPieces, GNMR_DTYPE_F16, GNMR_ACT_GELU>(p, it, acc, at, col, span);
+        } else if (p.out_type == GNMR_DTYPE_F32)
             finish<kPieces, kCodes, GNMR_DTYPE_F32>(p, it, acc, at, col, span);
         else if (p.out_type == GNMR_DTYPE_BF16)
             finish<kPieces, kCodes, GNMR_DTYPE_BF16>(p, it, acc, at, col, span);

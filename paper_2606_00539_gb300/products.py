@@ -12,6 +12,7 @@ from . import _native as N
 torch = None                                       # loaded with the first ExpertProducts, as the monitor does
 _DTYPES: dict = {}                                 # torch type -> gnmr_dtype
 _NAMED: dict = {}                                  # name -> torch type
+_ACTIVATIONS = {"silu": N.GNMR_ACT_SILU, "gelu": N.GNMR_ACT_GELU}
 
 
 def _load_torch():
@@ -30,6 +31,12 @@ def _named_dtype(name):
     if name in _DTYPES:
         return name
     raise ValueError(f"out_dtype must be one of {sorted(_NAMED)} or the torch type, got {name!r}")
+
+
+def _activation(name):
+    if name not in _ACTIVATIONS:
+        raise ValueError(f"activation must be one of {sorted(_ACTIVATIONS)}, got {name!r}")
+    return _ACTIVATIONS[name]
 
 
 class ExpertProducts:
@@ -59,6 +66,7 @@ class ExpertProducts:
             _load_torch()
         self._h = N.gnmr_products_create(self.device_index)
         self._run = N.load().gnmr_products_run
+        self._run_gated = N.load().gnmr_products_gated
         self._device = torch.device("cuda", self.device_index)
         self._sixteen = (torch.bfloat16, torch.float16)
         self._any = tuple(_DTYPES)
@@ -160,26 +168,27 @@ class ExpertProducts:
             raise ValueError(f"out must be [{rows}, {width}], got [{r}, {c}]")
         return out, step
 
-    def _enqueue(self, p, stream):
+    def _enqueue(self, p, stream, run=None, scratch_bytes=N.gnmr_products_scratch_bytes):
         if not self._h:
             raise ValueError("the products were closed")
         handle = self._stream(stream)
-        status = self._run(self._h, ctypes.addressof(p), handle)
+        run = run or self._run
+        status = run(self._h, ctypes.addressof(p), handle)
         if status == N.GNMR_ERR_LAYOUT:
             # operands that cannot be read in place: room for their copies, on the same stream
-            need = N.gnmr_products_scratch_bytes(p)
+            need = scratch_bytes(p)
             if need > p.scratch_bytes:
                 scratch = self._new(need, torch.uint8, stream)
                 p.d_scratch, p.scratch_bytes = scratch.data_ptr(), need
-                status = self._run(self._h, ctypes.addressof(p), handle)
+                status = run(self._h, ctypes.addressof(p), handle)
         if status:
             N._check(status, None)
 
     # -- 16-bit products ------------------------------------------------------
     @staticmethod
-    def _no_graph(a, b):
-        if (a.requires_grad or b.requires_grad) and torch.is_grad_enabled():
-            raise ValueError("autograd records nothing of a product: use expert_linear, or detach() or torch.no_grad()")
+    def _no_graph(*operands):
+        if any(t.requires_grad for t in operands) and torch.is_grad_enabled():
+            raise ValueError("autograd records nothing of a product: use expert_linear or expert_gated, or detach() or torch.no_grad()")
 
     def forward(self, x, w, offsets=None, *, out=None, mask=None, stream=None):
         """y[r] = W_g x[r] for the rows r of every group g: x [rows, n_in] -> [rows, n_out]."""
@@ -234,7 +243,80 @@ class ExpertProducts:
                                      None, 0, 0, None, None, out.data_ptr(), row, group, bool(add)), stream)
         return out
 
+    # -- gated blocks -----------------------------------------------------------
+    def gated(self, x, w, offsets=None, *, out=None, keep=None, mask=None, activation="silu", stream=None):
+        """h[r] = act(a) * b with [a, b] = W_g x[r]: both projections of a gated block, the activation
+        ("silu" or "gelu", the one with erf) and the product in one kernel.  w: [groups, 2 n, n_in] (or
+        [2 n, n_in]), the n rows of the gate a before those of b; -> [rows, n].
+
+        keep: a [rows, 2 n] tensor of x's type that gets [a, b] as well, for gate_grad.  The rest of the
+        backward pass are products on w as it lies: dx = input_grad(dab, w, ...), dw = weight_grad(dab, x, ...)."""
+        act = _activation(activation)
+        groups, both, n_in, row, group = self._matrix(w, "w", (2, 3), self._sixteen)
+        dtype = w.dtype
+        _, rows, cols, step, _ = self._matrix(x, "x", (2,), (dtype,))
+        if cols != n_in:
+            raise ValueError(f"x must have {n_in} columns, got {cols}")
+        if both % 2:
+            raise ValueError(f"w must have the rows of two projections, got {both}")
+        self._no_graph(x, w)
+        at, bits, each = self._grouping(groups, offsets, mask)
+        out, across = self._out(out, rows, both // 2, (dtype,), stream)
+        kept, apart = None, 0
+        if keep is not None:
+            _, r, c, apart, _ = self._matrix(keep, "keep", (2,), (dtype,))
+            if (r, c) != (rows, both):
+                raise ValueError(f"keep must be [{rows}, {both}], got [{r}, {c}]")
+            kept = keep.data_ptr()
+        p = N.gnmr_gated(groups, act, rows, both // 2, n_in, _DTYPES[dtype], at, bits, each, x.data_ptr(), step,
+                         w.data_ptr(), row, group, out.data_ptr(), across, kept, apart)
+        self._enqueue(p, stream, self._run_gated, N.gnmr_gated_scratch_bytes)
+        return out
+
+    def gate(self, ab, offsets=None, *, out=None, mask=None, activation="silu", stream=None):
+        """h = act(a) * b from [a, b] = ab ([rows, 2 n]), for the groups whose mask entry is 0: those whose
+        projections forward_i8 computes."""
+        act = _activation(activation)
+        _, rows, both, step, _ = self._matrix(ab, "ab", (2,), self._sixteen)
+        if both % 2:
+            raise ValueError(f"ab must have the columns of two projections, got {both}")
+        if offsets is None and mask is not None and mask.numel() != 1:
+            raise ValueError("offsets may be None for one group only")
+        groups = 1 if offsets is None else offsets.numel() - 1
+        at, bits, each = self._grouping(groups, offsets, mask)
+        self._no_graph(ab)
+        out, across = self._out(out, rows, both // 2, (ab.dtype,), stream)
+        self._on_device(N.load().gnmr_gate, ab.data_ptr(), _DTYPES[ab.dtype], act, groups, rows, both // 2, step, at, bits,
+                        each, out.data_ptr(), across, self._stream(stream))
+        return out
+
+    def gate_grad(self, dh, ab, *, out=None, activation="silu", stream=None):
+        """The gradient of [a, b] = ab ([rows, 2 n], as gated keeps it) from that of h, dh: [rows, n], for
+        all rows.  out may be ab, which is then overwritten."""
+        act = _activation(activation)
+        _, rows, both, step, _ = self._matrix(ab, "ab", (2,), self._sixteen)
+        _, r, n, apart, _ = self._matrix(dh, "dh", (2,), (ab.dtype,))
+        if (r, 2 * n) != (rows, both):
+            raise ValueError(f"ab must be [{r}, {2 * n}] for this dh, got [{rows}, {both}]")
+        self._no_graph(dh, ab)
+        out, across = self._out(out, rows, both, (ab.dtype,), stream)
+        self._on_device(N.load().gnmr_gate_grad, dh.data_ptr(), _DTYPES[ab.dtype], act, rows, n, apart, ab.data_ptr(), step,
+                        out.data_ptr(), across, self._stream(stream))
+        return out
+
     # -- 8-bit products -------------------------------------------------------
+    def _on_device(self, fn, *args):
+        """A call that runs on the current device, on this one."""
+        if not self._h:
+            raise ValueError("the products were closed")
+        if torch.cuda.current_device() == self.device_index:
+            status = fn(*args)
+        else:
+            with torch.cuda.device(self.device_index):
+                status = fn(*args)
+        if status:
+            N._check(status, None)
+
     def _quantize(self, x, columns, mask, stream):
         groups, rows, cols, row, group = self._matrix(x, "x", (2, 3), self._any)
         bits, step = self._mask(mask, groups)
@@ -287,7 +369,7 @@ class ExpertProducts:
         return out
 
 
-def _expert_linear_function():
+def _once_function(name):
     class Once(torch.autograd.Function):
         """A gradient that has none of its own: passing one back through it is an error."""
 
@@ -297,7 +379,31 @@ def _expert_linear_function():
 
         @staticmethod
         def backward(ctx, _):
-            raise RuntimeError("expert_linear has no second derivatives: its gradients cannot be differentiated")
+            raise RuntimeError(f"{name} has no second derivatives: its gradients cannot be differentiated")
+
+    return Once
+
+
+def _first_gradients(once, gradients, ctx, *dy):
+    """gradients(ctx, *dy), of which autograd records nothing, and no gradients of these."""
+    if not torch.is_grad_enabled():
+        return gradients(ctx, *dy)
+    with torch.no_grad():                          # create_graph
+        got = gradients(ctx, *dy)
+    anchor = torch.empty(0, requires_grad=True)
+    return tuple(g if g is None else once.apply(anchor, g) for g in got)
+
+
+def _anchor(grad, *operands):
+    """A tensor that requires a gradient, where a gradient is to be written and no operand requires
+    one: without it autograd would leave the backward pass out."""
+    if grad is not None and torch.is_grad_enabled() and not any(t is not None and t.requires_grad for t in operands):
+        return torch.empty(0, requires_grad=True)
+    return None
+
+
+def _expert_linear_function():
+    Once = _once_function("expert_linear")
 
     class ExpertLinear(torch.autograd.Function):
         @staticmethod
@@ -316,14 +422,7 @@ def _expert_linear_function():
 
         @staticmethod
         def backward(ctx, dy):
-            if not torch.is_grad_enabled():
-                dx, dw = ExpertLinear.gradients(ctx, dy)
-            else:                                  # create_graph: the products record nothing
-                with torch.no_grad():
-                    dx, dw = ExpertLinear.gradients(ctx, dy)
-                anchor = torch.empty(0, requires_grad=True)
-                dx, dw = (g if g is None else Once.apply(anchor, g) for g in (dx, dw))
-            return (dx, dw) + (None,) * 7
+            return _first_gradients(Once, ExpertLinear.gradients, ctx, dy) + (None,) * 7
 
         @staticmethod
         def gradients(ctx, dy):
@@ -373,7 +472,75 @@ def expert_linear(products, x, w, offsets=None, mask=None, grad=None, *, add=Fal
     global _ExpertLinear
     if _ExpertLinear is None:
         _ExpertLinear = _expert_linear_function()
-    anchor = None
-    if grad is not None and torch.is_grad_enabled() and not (x.requires_grad or w.requires_grad):
-        anchor = torch.empty(0, requires_grad=True)          # without one autograd would leave the backward pass out
-    return _ExpertLinear.apply(x, w, products, offsets, mask, grad, add, codes, anchor)
+    return _ExpertLinear.apply(x, w, products, offsets, mask, grad, add, codes, _anchor(grad, x, w))
+
+
+def _expert_gated_function():
+    Once = _once_function("expert_gated")
+
+    class ExpertGated(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, w, products, offsets, mask, grad, add, codes, activation, keeps, anchor):
+            x, w = x.detach(), w.detach()
+            rows, both = x.shape[0], w.shape[-2]
+            h = torch.empty(rows, both // 2, dtype=x.dtype, device=x.device)
+            ab = torch.empty(rows, both, dtype=x.dtype, device=x.device) if keeps or mask is not None else None
+            products.gated(x, w, offsets, out=h, keep=ab if keeps else None, mask=mask, activation=activation)
+            if mask is not None:
+                xq, xs = products.quantize_rows(x)
+                wq, ws = codes[:2] if codes is not None else products.quantize_rows(w, mask=mask)
+                products.forward_i8(xq, xs, wq, ws, offsets, out=ab, mask=mask)
+                products.gate(ab, offsets, out=h, mask=mask, activation=activation)
+            ctx.products, ctx.grad, ctx.add, ctx.codes, ctx.activation = products, grad, add, codes, activation
+            ctx.has = (offsets is not None, mask is not None)
+            if keeps:
+                ctx.save_for_backward(x, w, ab, *(t for t in (offsets, mask) if t is not None))
+            return h
+
+        @staticmethod
+        def backward(ctx, dh):
+            return _first_gradients(Once, ExpertGated.gradients, ctx, dh) + (None,) * 9
+
+        @staticmethod
+        def gradients(ctx, dh):
+            x, w, ab, *rest = ctx.saved_tensors
+            offsets = rest.pop(0) if ctx.has[0] else None
+            mask = rest.pop(0) if ctx.has[1] else None
+            products, dx, dw = ctx.products, None, None
+            dab = products.gate_grad(dh.contiguous(), ab, activation=ctx.activation)
+            if ctx.needs_input_grad[0]:
+                dx = torch.empty_like(x, memory_format=torch.contiguous_format)
+                products.input_grad(dab, w, offsets, out=dx, mask=mask)
+                if mask is not None:
+                    dq, ds = products.quantize_rows(dab)
+                    vq, vs = ctx.codes[2:] if ctx.codes is not None else products.quantize_columns(w, mask=mask)
+                    products.forward_i8(dq, ds, vq, vs, offsets, out=dx, mask=mask)
+            if ctx.grad is not None:
+                products.weight_grad(dab, x, offsets, out=ctx.grad, add=ctx.add)
+            elif ctx.needs_input_grad[1]:
+                dw = torch.empty_like(w, memory_format=torch.contiguous_format)
+                products.weight_grad(dab, x, offsets, out=dw)
+            return dx, dw
+
+    return ExpertGated
+
+
+_ExpertGated = None
+
+
+def expert_gated(products, x, w, offsets=None, mask=None, grad=None, *, add=False, codes=None, activation="silu"):
+    """The first half of a gated feed-forward layer of experts with a backward pass: h = act(a) * b,
+    [a, b] = W_g x, each expert on the path that the mask gives it (expert_linear is the second half).
+
+    w: [groups, 2 n, n_in], the gate's rows first, as in :meth:`ExpertProducts.gated`; everything
+    else as in :func:`expert_linear`, codes of w as it lies.  On the low-cost path [a, b] is the 8-bit
+    product rounded to x's type, and h is formed from that; the backward pass takes [a, b] in x's type
+    on both paths, and their gradient's 8-bit codes by row for the low-cost one.
+
+    The gradients have no gradients of their own: differentiating them raises RuntimeError."""
+    global _ExpertGated
+    if _ExpertGated is None:
+        _ExpertGated = _expert_gated_function()
+    anchor = _anchor(grad, x, w)
+    keeps = torch.is_grad_enabled() and (anchor is not None or x.requires_grad or w.requires_grad)
+    return _ExpertGated.apply(x, w, products, offsets, mask, grad, add, codes, activation, keeps, anchor)

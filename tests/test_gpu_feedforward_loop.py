@@ -1,0 +1,79 @@
+"""The feed-forward half of a transformer layer, trained under the monitor with what this package has for it: layer
+norm, gated experts and their down projection on the paths that the mask gives, all gradients in one arena, the monitor's
+step on it, clipping by the monitor's own norms, and an update.
+
+Every step: the monitor's norms, the clipped arena and the limit against the gradients that autograd gets in 64 bits
+for the same path."""
+import numpy as np
+import pytest
+
+from paper_2606_00539_gb300 import ExpertProducts, GradientClip, LayerNorm, Monitor, expert_gated, expert_linear, layer_norm
+
+pytestmark = pytest.mark.gpu
+
+EXPERTS, HIDDEN, FFN, TOKENS, STEPS, LIMIT = 6, 136, 72, 160, 6, 0.05
+
+
+def test_monitored_layer(cuda_device):
+    import torch
+    torch.manual_seed(1)
+    dev, t = cuda_device, torch.bfloat16
+    up = (torch.randn(EXPERTS, 2 * FFN, HIDDEN, device=dev) * HIDDEN ** -0.5).to(t)
+    down = (torch.randn(EXPERTS, HIDDEN, FFN, device=dev) * FFN ** -0.5).to(t)
+    weight, bias = torch.ones(HIDDEN, device=dev), torch.zeros(HIDDEN, device=dev)
+    # the arena: the norm's two gradients, then each expert's two matrices
+    size, first = 3 * FFN * HIDDEN, 2 * HIDDEN
+    arena = torch.full((first + EXPERTS * size,), 7.0, device=dev)
+    g_norm = arena[:HIDDEN], arena[HIDDEN:first]
+    g_up = torch.as_strided(arena, (EXPERTS, 2 * FFN, HIDDEN), (size, HIDDEN, 1), first)
+    g_down = torch.as_strided(arena, (EXPERTS, HIDDEN, FFN), (size, FFN, 1), first + 2 * FFN * HIDDEN)
+    starts = [0] + [first + e * size + i * 2 * FFN * HIDDEN for e in range(EXPERTS) for i in range(2)]
+    lengths = [first] + [2 * FFN * HIDDEN, FFN * HIDDEN] * EXPERTS
+    mon = Monitor(starts, lengths, dtype="f32", segment_unit=[0] + list(np.repeat(np.arange(1, EXPERTS + 1), 2)), num_units=EXPERTS + 1,
+                  recoverable=[0] + [1] * EXPERTS, window=2, max_o=2, lock_len=2, alpha=0.9, beta=1.5)
+    stats, norms, clip = mon.new_stats(), LayerNorm(device=0), GradientClip([arena])
+    scaled = torch.empty_like(arena)
+    step_mask = torch.zeros(EXPERTS + 1, dtype=torch.uint8, device=dev)
+    recovered = 0
+    with ExpertProducts(device=0) as products:
+        for step in range(STEPS):
+            counts = np.random.default_rng(step).multinomial(TOKENS, np.ones(EXPERTS) / EXPERTS)
+            counts[step % EXPERTS] = 0
+            rows = int(counts.sum())
+            off = torch.tensor(np.concatenate([[0], np.cumsum(counts)]), device=dev)
+            mask = step_mask[1:]
+            x = torch.randn(rows, HIDDEN, device=dev).to(t)
+            y = layer_norm(norms, x, weight, bias, g_norm)
+            h = expert_gated(products, y, up, off, mask, g_up)
+            z = x + expert_linear(products, h, down, off, mask, g_down)
+            ((z.float() - 1).square().sum() / TOKENS).backward()
+            # 64 bits, every expert in 16-bit weights: the recovery path's values; on the other the 8-bit codes are off by 1 %
+            W, B, U, D = (v.double().requires_grad_() for v in (weight, bias, up, down))
+            Y = torch.nn.functional.layer_norm(x.double(), (HIDDEN,), W, B, 1e-5)
+            Z = []
+            for e in range(EXPERTS):
+                a, b = (Y[off[e]:off[e + 1]] @ U[e].T).chunk(2, 1)
+                Z.append((torch.nn.functional.silu(a) * b) @ D[e].T)
+            ((x.double() + torch.cat(Z) - 1).square().sum() / TOKENS).backward()
+            high = mask.bool()
+            for got, want in ((g_up, U.grad), (g_down, D.grad)):
+                for e in range(EXPERTS):
+                    assert (got[e] - want[e]).norm() <= (0.02 if high[e] else 0.06) * want[e].norm() + 1e-12
+            for got, want in zip(g_norm, (W.grad, B.grad)):
+                assert (got - want).norm() <= 0.06 * want.norm()
+            step_mask = mon.step(arena, stats=stats)
+            total = arena.double().norm().item()
+            norm = clip.clip([arena], LIMIT, out=[scaled], unit_norms=stats["norm"])
+            assert abs(norm.item() - total) <= 1e-5 * total
+            assert total > LIMIT and abs(scaled.double().norm().item() - LIMIT) <= 1e-5 * LIMIT
+            assert torch.allclose(scaled, arena * (LIMIT / total), rtol=1e-5, atol=0)
+            weight -= scaled[:HIDDEN]
+            bias -= scaled[HIDDEN:first]
+            up -= torch.as_strided(scaled, g_up.shape, g_up.stride(), first).to(t)
+            down -= torch.as_strided(scaled, g_down.shape, g_down.stride(), first + 2 * FFN * HIDDEN).to(t)
+            recovered += int(step_mask.sum())
+            assert step_mask[0] == 0
+        products.check()
+    mon.close()
+    clip.close()
+    assert recovered > 0                                         # both paths ran
