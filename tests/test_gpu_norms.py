@@ -148,12 +148,13 @@ def test_strides_and_arenas(norms, cols, pad, lead, dtype):
             assert (out[:, :lead] == 7).all() and (out[:, lead + cols:] == 7).all()
             for a, z in ((0, lead), (lead + cols, wide + lead), (wide + lead + cols, 2 * wide)):
                 assert torch.equal(arena[a:z], old[a:z])
-    want_y, want_dx = y, dx
-    want_y = norms.forward(x, w, b)[0]
-    own = dy.clone(memory_format=torch.contiguous_format)
-    assert torch.equal(norms.backward(own, x, w, mean, rstd, out=own, weight_grad=torch.empty_like(w)), want_dx)
-    own = x.clone(memory_format=torch.contiguous_format)
-    assert torch.equal(norms.forward(own, w, b, out=own)[0], want_y)
+    # in place, against other memory: the same operands, so the same bits
+    for a, b_ in ((dy, x), (dy.contiguous(), x.contiguous())):
+        own = a.clone(memory_format=torch.preserve_format) if a.is_contiguous() else a
+        want = norms.backward(own, b_, w, mean, rstd, weight_grad=torch.empty_like(w))
+        assert torch.equal(norms.backward(own, b_, w, mean, rstd, out=own, weight_grad=torch.empty_like(w)), want)
+        want = norms.forward(b_, w, b)[0]
+        assert torch.equal(norms.forward(b_, w, b, out=b_)[0], want)
 
 
 def test_no_rows(norms):
