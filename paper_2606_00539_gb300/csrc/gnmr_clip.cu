@@ -6,7 +6,7 @@
 // partial sums up in the same order, which takes it a microsecond, and scales its share.  Both are bound by
 // memory: the gradients are read twice (once where nothing is written: in place, below the limit) and
 // written once.  Where the tensors lie comes with each call, as kernel parameters, so that a captured
-// call keeps its own; how they are cut into chunks is in the plan.
+// call keeps its own; who takes what is in the plan: every warp an equal share of all tensors, laid end to end.
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
@@ -18,16 +18,36 @@
 #include "gnmr_rows.cuh"
 #include "gnmr_stream.cuh"
 
+namespace {
+
+// A tensor of a plan: its length, and where its share of the tensors laid end to end begins.
+struct alignas(16) Entry {
+    int64_t length, first;                             // elements; units
+    int32_t dtype;
+};
+
+// A kernel's CTAs, and where the table of its warps' first tensors begins ([warps + 1] of them).
+struct Grid {
+    int ctas;
+    size_t start;
+};
+
+// The tensors of one launch.
+struct Launch {
+    int from, tensors;
+    int64_t unit0, units;
+    Grid squares, both, in_place;                      // both: outputs in other memory
+};
+
+}  // namespace
+
 struct gnmr_clip {
-    int device = 0, sms = 1;
-    int tensors = 0;
-    int64_t chunks = 0;
-    std::vector<int64_t> lengths, first;               // first[i]: chunks before tensor i
-    std::vector<int32_t> dtypes;
-    int64_t chunk = 0;                                 // bytes
+    int device = 0;
+    std::vector<Entry> entries;                        // and one behind the last
+    std::vector<Launch> launches;
+    const Entry *d_entries = nullptr;
+    const int32_t *d_start = nullptr;
     void *dmem = nullptr;
-    const int64_t *d_lengths = nullptr, *d_first = nullptr;
-    const int32_t *d_dtypes = nullptr;
 };
 
 namespace {
@@ -36,52 +56,48 @@ using namespace gnmr_rows;
 
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
-constexpr int kUnroll = 8;
-constexpr int kCtas = 4;                               // an SM
-constexpr int kMostCtas = 1024;                        // of the first kernel: the partial sums
+// Few warps with many loads each on their way: 2.4 GB of bf16 took the first kernel 347 us so (7.0 TB/s), with 8
+// loads a lane and four CTAs an SM 377, with two 569.
+constexpr int kUnroll = 16, kSquaresCtas = 2;          // 16-byte loads a lane; CTAs an SM
+// The second kernel, of the same: 64 CTAs an SM, as they come, 733 us (6.6 TB/s moved), 8 763, 4 774; in place most calls end
+// with the limit not reached, and then a CTA costs its launch alone: 64 an SM 85 us, 4 less than one.  With 16 loads a lane
+// in place of 8, 4 an SM take 757.
+constexpr int kBothCtas = 64, kInPlaceCtas = 4;
+constexpr int kMostSquares = 512;                      // the first kernel's CTAs, each with a partial sum
 
+// Shares are counted in units of 512 bytes, and four for beginning a tensor: a microsecond's latency,
+// in which a warp's part of the memory's rate is 1.4 KB.
+constexpr int64_t kUnit = 512, kBegin = 4;
+// A warp takes 4 KB at least.
+constexpr int64_t kLeastUnits = 8;
 
-// Tensors first .. first + count - 1 of the plan, those that one launch takes.
 struct Plan {
-    const int64_t *lengths, *first;                    // [tensors], [tensors + 1]
-    const int32_t *dtypes;
-    int64_t chunk;
-    int tensor0, tensors;
-    int64_t chunk0, chunks;
+    const Entry *entries;                              // [tensors + 1], those of the launch
+    const int32_t *start;                              // [warps + 1] each warp's first tensor
+    int tensors;
+    int64_t unit0, units;
 };
 
 template <int kN> struct Places {
     const char *in[kN];
-    char *out[kN];
 };
 
-struct Part {
-    int tensor;                                        // among the launch's
-    int64_t at, n;                                     // elements
+template <int kN, bool kBoth> struct Outs {
+    char *out[kBoth ? kN : 1];
 };
 
-__device__ __forceinline__ int bytes_of(int dtype) { return dtype == GNMR_DTYPE_F32 ? 4 : 2; }
+struct Share {
+    int64_t u0, u1;                                    // units
+};
 
-// Chunk c: the last tensor that begins at or before it.  t: that of an earlier chunk.
-__device__ __forceinline__ Part part_of(const Plan &p, int64_t c, int &t)
+__device__ __forceinline__ Share share_of(const Plan &p, int64_t w, int64_t all) { return {p.unit0 + p.units * w / all, p.unit0 + p.units * (w + 1) / all}; }
+
+// The elements of an entry that lie in a share.
+__device__ __forceinline__ void part_of(const Entry &e, const Share &s, int64_t &from, int64_t &to)
 {
-    int hi = p.tensors;
-    if (t + 1 < hi && __ldg(p.first + p.tensor0 + t + 1) > c)
-        hi = t + 1;
-    for (; hi - t > 1;) {
-        const int mid = (t + hi) / 2;
-        if (__ldg(p.first + p.tensor0 + mid) <= c)
-            t = mid;
-        else
-            hi = mid;
-    }
-    const int i = p.tensor0 + t;
-    const int64_t each = p.chunk / bytes_of(__ldg(p.dtypes + i));
-    Part part;
-    part.tensor = t;
-    part.at = (c - __ldg(p.first + i)) * each;
-    part.n = min(each, __ldg(p.lengths + i) - part.at);
-    return part;
+    const int64_t each = e.dtype == GNMR_DTYPE_F32 ? kUnit / 4 : kUnit / 2;
+    from = min(max(s.u0 - e.first - kBegin, int64_t(0)) * each, e.length);
+    to = min(max(s.u1 - e.first - kBegin, int64_t(0)) * each, e.length);
 }
 
 template <int DT> __device__ __forceinline__ double squares(const char *at, int64_t n, int lane)
@@ -91,96 +107,122 @@ template <int DT> __device__ __forceinline__ double squares(const char *at, int6
     return suspect ? gnmr::warp_segment_sumsq_f64<DT>(at, n, lane) : s;
 }
 
+// A CTA's sum from its warps', in their order; in thread 0.
+__device__ __forceinline__ double cta_total(double sum, double *shared)
+{
+    if ((threadIdx.x & 31) == 0)
+        shared[threadIdx.x >> 5] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0)
+        for (int i = 1; i < kWarps; ++i)
+            sum += shared[i];
+    return sum;
+}
+
 // This CTA's partial sum.
 template <int kN>
-__global__ void __launch_bounds__(kThreads) squares_kernel(const __grid_constant__ Plan p, const __grid_constant__ Places<kN> places, double *partial)
+__global__ void __launch_bounds__(kThreads, kSquaresCtas) squares_kernel(const __grid_constant__ Plan p, const __grid_constant__ Places<kN> places, double *partial)
 {
     __shared__ double sums[kWarps];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int64_t w = int64_t(blockIdx.x) * kWarps + warp, all = int64_t(gridDim.x) * kWarps;
-    const int64_t c0 = p.chunk0 + p.chunks * w / all, c1 = p.chunk0 + p.chunks * (w + 1) / all;
+    const int lane = threadIdx.x & 31;
+    const int64_t w = int64_t(blockIdx.x) * kWarps + (threadIdx.x >> 5);
+    const Share share = share_of(p, w, int64_t(gridDim.x) * kWarps);
     double sum = 0.0;
-    int t = 0;
-    for (int64_t c = c0; c < c1; ++c) {
-        const Part part = part_of(p, c, t);
-        const int dtype = __ldg(p.dtypes + p.tensor0 + part.tensor);
-        const char *at = places.in[part.tensor] + part.at * bytes_of(dtype);
+    int t = __ldg(p.start + w);
+    Entry e = p.entries[t];
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    while (t < p.tensors && e.first < share.u1) {
+        int64_t from, to;
+        part_of(e, share, from, to);
+        const int dtype = e.dtype;
+        const char *const at = places.in[t] + from * (dtype == GNMR_DTYPE_F32 ? 4 : 2);
+        e = p.entries[++t];
+        if (from >= to)
+            continue;
         if (dtype == GNMR_DTYPE_F32)
-            sum += squares<GNMR_DTYPE_F32>(at, part.n, lane);
+            sum += squares<GNMR_DTYPE_F32>(at, to - from, lane);
         else if (dtype == GNMR_DTYPE_BF16)
-            sum += squares<GNMR_DTYPE_BF16>(at, part.n, lane);
+            sum += squares<GNMR_DTYPE_BF16>(at, to - from, lane);
         else
-            sum += squares<GNMR_DTYPE_F16>(at, part.n, lane);
+            sum += squares<GNMR_DTYPE_F16>(at, to - from, lane);
     }
-    if (lane == 0)
-        sums[warp] = sum;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int i = 1; i < kWarps; ++i)
-            sum += sums[i];
+    sum = cta_total(sum, sums);
+    if (threadIdx.x == 0)
         partial[blockIdx.x] = sum;
-    }
 }
 
 // The same from norms.
 __global__ void __launch_bounds__(kThreads) norms_kernel(const double *norms, int64_t n, double *partial)
 {
     __shared__ double sums[kWarps];
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     double sum = 0.0;
     for (int64_t i = int64_t(blockIdx.x) * kThreads + threadIdx.x; i < n; i += int64_t(gridDim.x) * kThreads)
         sum = fma(norms[i], norms[i], sum);
-    sum = gnmr::warp_allreduce_sum(sum);
-    if ((threadIdx.x & 31) == 0)
-        sums[threadIdx.x >> 5] = sum;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int i = 1; i < kWarps; ++i)
-            sum += sums[i];
+    sum = cta_total(gnmr::warp_allreduce_sum(sum), sums);
+    if (threadIdx.x == 0)
         partial[blockIdx.x] = sum;
-    }
 }
 
-// n elements scaled, by a warp.
-template <typename T> __device__ __forceinline__ void scale_part(const T *in, T *out, int64_t n, float scale, int lane)
+// n elements scaled, by a warp, the last ones first: those that the first kernel read last are still in L2.
+template <typename T, int kBatch> __device__ __forceinline__ void scale_part(const T *in, T *out, int64_t n, float scale, int lane)
 {
     constexpr int kV = kIn16<T>;
     const int64_t head = min(n, int64_t((16 - (reinterpret_cast<uintptr_t>(in) & 15)) & 15) / int64_t(sizeof(T)));
     const bool alike = ((reinterpret_cast<uintptr_t>(in) ^ reinterpret_cast<uintptr_t>(out)) & 15) == 0;
     const int64_t vecs = alike ? (n - head) / kV : 0;
-    for (int64_t i = lane; i < vecs; i += 32) {
-        float f[kV];
-        widen<T>(load_once(in + head + i * kV), f);
-#pragma unroll
-        for (int j = 0; j < kV; ++j)
-            f[j] *= scale;
-        store_once(out + head + i * kV, narrow<T>(f));
-    }
     // what lies around the vectors
     const int64_t rest = n - vecs * kV;
     for (int64_t i = lane; i < rest; i += 32) {
         const int64_t at = i < head ? i : i + vecs * kV;
         out[at] = from_f32<T>(to_f32(in[at]) * scale);
     }
+    in += head;
+    out += head;
+    for (int64_t end = vecs; end > 0; end -= 32 * kBatch) {
+        uint4 v[kBatch];
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+            const int64_t i = end - 32 * (j + 1) + lane;
+            if (i >= 0)
+                v[j] = load_once(in + i * kV);
+        }
+#pragma unroll
+        for (int j = 0; j < kBatch; ++j) {
+            const int64_t i = end - 32 * (j + 1) + lane;
+            float f[kV];
+            widen<T>(v[j], f);
+#pragma unroll
+            for (int k = 0; k < kV; ++k)
+                f[k] *= scale;
+            if (i >= 0)
+                store_once(out + i * kV, narrow<T>(f));
+        }
+    }
 }
 
-template <int kN>
+template <int kN, bool kBoth>
 __global__ void __launch_bounds__(kThreads)
-scale_kernel(const __grid_constant__ Plan p, const __grid_constant__ Places<kN> places, const double *partial, int partials, double max_norm,
-             float *norm_out, int in_place)
+scale_kernel(const __grid_constant__ Plan p, const __grid_constant__ Places<kN> places, const __grid_constant__ Outs<kN, kBoth> outs,
+             const double *partial, int partials, double max_norm, float *norm_out)
 {
     __shared__ double sums[kWarps];
     __shared__ float scale_of_all;
+    constexpr int kBatch = kBoth ? 8 : 16;             // loads a lane
+    const int lane = threadIdx.x & 31;
+    const int64_t w = int64_t(blockIdx.x) * kWarps + (threadIdx.x >> 5);
+    const Share share = share_of(p, w, int64_t(gridDim.x) * kWarps);
+    int t = __ldg(p.start + w + 1);                    // at or behind the last one
+    Entry e = p.entries[t];
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     double sum = 0.0;
     for (int i = threadIdx.x; i < partials; i += kThreads)
-        sum += partial[i];
-    sum = gnmr::warp_allreduce_sum(sum);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    if (lane == 0)
-        sums[warp] = sum;
-    __syncthreads();
+        sum += __ldcg(partial + i);
+    sum = cta_total(gnmr::warp_allreduce_sum(sum), sums);
     if (threadIdx.x == 0) {
-        for (int i = 1; i < kWarps; ++i)
-            sum += sums[i];
         const double norm = sqrt(sum);
         // a norm that is not finite compares as not above the limit, or as infinite
         scale_of_all = norm > max_norm && isfinite(norm) ? static_cast<float>(max_norm / norm) : 1.0f;
@@ -189,29 +231,31 @@ scale_kernel(const __grid_constant__ Plan p, const __grid_constant__ Places<kN> 
     }
     __syncthreads();
     const float scale = scale_of_all;
-    if (in_place && scale == 1.0f)
+    if (!kBoth && scale == 1.0f)
         return;
-    const int64_t w = int64_t(blockIdx.x) * kWarps + warp, all = int64_t(gridDim.x) * kWarps;
-    const int64_t c0 = p.chunk0 + p.chunks * w / all, c1 = p.chunk0 + p.chunks * (w + 1) / all;
-    int t = 0;
-    for (int64_t c = c0; c < c1; ++c) {
-        const Part part = part_of(p, c, t);
-        const int dtype = __ldg(p.dtypes + p.tensor0 + part.tensor);
-        const int64_t at = part.at * bytes_of(dtype);
-        const char *in = places.in[part.tensor] + at;
-        char *out = places.out[part.tensor] + at;
-        if (dtype == GNMR_DTYPE_F32)
-            scale_part(reinterpret_cast<const float *>(in), reinterpret_cast<float *>(out), part.n, scale, lane);
-        else if (dtype == GNMR_DTYPE_BF16)
-            scale_part(reinterpret_cast<const __nv_bfloat16 *>(in), reinterpret_cast<__nv_bfloat16 *>(out), part.n, scale, lane);
-        else
-            scale_part(reinterpret_cast<const __half *>(in), reinterpret_cast<__half *>(out), part.n, scale, lane);
+    for (;;) {
+        int64_t from, to;
+        part_of(e, share, from, to);
+        if (t < p.tensors && from < to) {
+            const int64_t at = from * (e.dtype == GNMR_DTYPE_F32 ? 4 : 2);
+            const char *const in = places.in[t] + at;
+            char *const out = kBoth ? outs.out[t] + at : const_cast<char *>(in);
+            if (e.dtype == GNMR_DTYPE_F32)
+                scale_part<float, kBatch>(reinterpret_cast<const float *>(in), reinterpret_cast<float *>(out), to - from, scale, lane);
+            else if (e.dtype == GNMR_DTYPE_BF16)
+                scale_part<__nv_bfloat16, kBatch>(reinterpret_cast<const __nv_bfloat16 *>(in), reinterpret_cast<__nv_bfloat16 *>(out), to - from, scale, lane);
+            else
+                scale_part<__half, kBatch>(reinterpret_cast<const __half *>(in), reinterpret_cast<__half *>(out), to - from, scale, lane);
+        }
+        if (t == 0 || e.first <= share.u0)
+            return;
+        e = p.entries[--t];
     }
 }
 
 // ---- host -----------------------------------------------------------------------
 
-constexpr int kMost = 1900;                            // tensors of one launch: places in 32,764 bytes of parameters
+constexpr int kMost = 2000;                            // tensors of one launch: places in 32,764 bytes of parameters
 
 gnmr_status fail(gnmr_status s, const char *why)
 {
@@ -219,45 +263,86 @@ gnmr_status fail(gnmr_status s, const char *why)
     return s;
 }
 
-int ctas_for(const gnmr_clip *c, int64_t chunks)
+cudaLaunchConfig_t config(int ctas, cudaStream_t st, cudaLaunchAttribute *attr)
 {
-    return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>((chunks + kWarps - 1) / kWarps, std::min(c->sms * kCtas, kMostCtas))));
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(ctas);
+    cfg.blockDim = dim3(kThreads);
+    cfg.stream = st;
+    attr->id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr->val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cfg;
 }
 
-template <int kN> Places<kN> places_of(int from, int count, const void *const *in, void *const *out)
+template <int kN> Places<kN> places_of(const Launch &l, const void *const *in)
 {
     Places<kN> p;
-    for (int i = 0; i < count; ++i) {
-        p.in[i] = static_cast<const char *>(in[from + i]);
-        p.out[i] = static_cast<char *>(out ? out[from + i] : const_cast<void *>(in[from + i]));
-    }
+    std::copy(in + l.from, in + l.from + l.tensors, reinterpret_cast<const void **>(p.in));
     return p;
 }
 
-int launches_of(const gnmr_clip *c) { return std::max(1, (c->tensors + kMost - 1) / kMost); }
+Plan plan_of(const gnmr_clip *c, const Launch &l, const Grid &g) { return {c->d_entries + l.from, c->d_start + g.start, l.tensors, l.unit0, l.units}; }
 
-// Calls f(plan, places) for every launch's tensors.
-template <typename F> cudaError_t by_launch(const gnmr_clip *c, const void *const *in, void *const *out, F f)
+template <int kN> cudaError_t launch_squares(const gnmr_clip *c, const Launch &l, const void *const *in, double *partial, cudaStream_t st)
 {
-    for (int from = 0; from < std::max(c->tensors, 1); from += kMost) {
-        const int count = std::min(kMost, c->tensors - from);
-        const Plan p{c->d_lengths, c->d_first, c->d_dtypes, c->chunk, from, count, c->first[from], c->first[from + count] - c->first[from]};
-        const cudaError_t e = count <= 64    ? f(p, places_of<64>(from, count, in, out))
-                              : count <= 400 ? f(p, places_of<400>(from, count, in, out))
-                                             : f(p, places_of<kMost>(from, count, in, out));
-        if (e != cudaSuccess)
-            return e;
-    }
-    return cudaSuccess;
+    cudaLaunchAttribute attr;
+    const cudaLaunchConfig_t cfg = config(l.squares.ctas, st, &attr);
+    return cudaLaunchKernelEx(&cfg, squares_kernel<kN>, plan_of(c, l, l.squares), places_of<kN>(l, in), partial);
 }
 
-template <int kN>
-cudaError_t launch_squares(const gnmr_clip *c, const Plan &p, const Places<kN> &places, double *partial, int *count, cudaStream_t st)
+template <int kN, bool kBoth>
+cudaError_t launch_scale(const gnmr_clip *c, const Launch &l, const void *const *in, void *const *out, const double *partial, int partials,
+                         double max_norm, float *norm, cudaStream_t st)
 {
-    const int ctas = ctas_for(c, p.chunks);
-    squares_kernel<kN><<<ctas, kThreads, 0, st>>>(p, places, partial + *count);
-    *count += ctas;
-    return cudaGetLastError();
+    Outs<kN, kBoth> outs;
+    if (kBoth)
+        std::copy(out + l.from, out + l.from + l.tensors, reinterpret_cast<void **>(outs.out));
+    const Grid &g = kBoth ? l.both : l.in_place;
+    cudaLaunchAttribute attr;
+    const cudaLaunchConfig_t cfg = config(g.ctas, st, &attr);
+    return cudaLaunchKernelEx(&cfg, scale_kernel<kN, kBoth>, plan_of(c, l, g), places_of<kN>(l, in), outs, partial, partials, max_norm, norm);
+}
+
+// Calls f with the capacity that a launch's parameters take, as a constant.
+template <typename F> cudaError_t by_capacity(const Launch &l, F f)
+{
+    if (l.tensors <= 64)
+        return f(std::integral_constant<int, 64>());
+    if (l.tensors <= 400)
+        return f(std::integral_constant<int, 400>());
+    return f(std::integral_constant<int, kMost>());
+}
+
+// The launches and each one's table of where its warps begin, for tensors laid end to end.
+std::vector<int32_t> cut(gnmr_clip *c, int sms)
+{
+    std::vector<int32_t> start;
+    const int all = static_cast<int>(c->entries.size()) - 1;
+    for (int from = 0; from < std::max(all, 1); from += kMost) {
+        Launch l = {};
+        l.from = from;
+        l.tensors = std::min(kMost, all - from);
+        l.unit0 = c->entries[from].first;
+        l.units = c->entries[from + l.tensors].first - l.unit0;
+        const int64_t most = std::max<int64_t>(1, l.units / (kLeastUnits * kWarps));
+        l.squares.ctas = static_cast<int>(std::min<int64_t>(most, std::min(sms * kSquaresCtas, kMostSquares)));
+        l.both.ctas = static_cast<int>(std::min<int64_t>(most, sms * kBothCtas));
+        l.in_place.ctas = static_cast<int>(std::min<int64_t>(most, sms * kInPlaceCtas));
+        for (Grid *g : {&l.squares, &l.both, &l.in_place}) {
+            const int64_t warps = int64_t(g->ctas) * kWarps;
+            g->start = start.size();
+            int t = 0;
+            for (int64_t w = 0; w <= warps; ++w) {
+                while (t < l.tensors && c->entries[from + t + 1].first <= l.unit0 + l.units * w / warps)
+                    ++t;
+                start.push_back(t);
+            }
+        }
+        c->launches.push_back(l);
+    }
+    return start;
 }
 
 }  // namespace
@@ -284,45 +369,39 @@ gnmr_status gnmr_clip_create(int32_t num_tensors, const int64_t *lengths, const 
         return fail(GNMR_ERR_CUDA, "clip: device not available");
     }
     gnmr_clip *c = nullptr;
-    int prev = 0;
+    int prev = 0, sms = 1;
     cudaGetDevice(&prev);
-    cudaError_t e = cudaSuccess;
+    cudaError_t e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
+    std::vector<int32_t> start;
     try {
         c = new gnmr_clip;
         c->device = device;
-        c->tensors = num_tensors;
-        c->lengths.assign(lengths, lengths + num_tensors);
-        c->dtypes.assign(dtypes, dtypes + num_tensors);
-        e = cudaDeviceGetAttribute(&c->sms, cudaDevAttrMultiProcessorCount, device);
-        // chunks of 4 KB that give every warp one, 64 KB at most
-        const int64_t warps = int64_t(c->sms) * kCtas * kWarps;
-        c->chunk = std::min<int64_t>(65536, std::max<int64_t>(1, (static_cast<int64_t>(bytes) / warps + 4095) / 4096) * 4096);
-        c->first.resize(num_tensors + 1);
-        for (int i = 0; i < num_tensors; ++i)
-            c->first[i + 1] = c->first[i] + (lengths[i] * int64_t(element_bytes(dtypes[i])) + c->chunk - 1) / c->chunk;
-        c->chunks = c->first[num_tensors];
+        c->entries.resize(num_tensors + 1);
+        int64_t units = 0;
+        for (int i = 0; i < num_tensors; ++i) {
+            c->entries[i] = Entry{lengths[i], units, dtypes[i]};
+            if (lengths[i])
+                units += kBegin + (lengths[i] * int64_t(element_bytes(dtypes[i])) + kUnit - 1) / kUnit;
+        }
+        c->entries[num_tensors] = Entry{0, units, 0};
+        start = cut(c, sms);
     } catch (const std::bad_alloc &) {
         delete c;
         return fail(GNMR_ERR_OOM, "clip: host allocation failed");
     }
-    const size_t wide = num_tensors * sizeof(int64_t), all = 2 * wide + sizeof(int64_t) + num_tensors * sizeof(int32_t);
+    const size_t wide = c->entries.size() * sizeof(Entry);
     cudaSetDevice(device);
     if (e == cudaSuccess)
-        e = cudaMalloc(&c->dmem, all);
+        e = cudaMalloc(&c->dmem, wide + start.size() * sizeof(int32_t));
     char *at = static_cast<char *>(c->dmem);
-    if (e == cudaSuccess) {
-        c->d_first = reinterpret_cast<const int64_t *>(at);
-        c->d_lengths = c->d_first + num_tensors + 1;
-        c->d_dtypes = reinterpret_cast<const int32_t *>(c->d_lengths + num_tensors);
-        e = cudaMemcpy(at, c->first.data(), wide + sizeof(int64_t), cudaMemcpyHostToDevice);
-    }
-    if (e == cudaSuccess && num_tensors) {
-        e = cudaMemcpy(at + wide + sizeof(int64_t), lengths, wide, cudaMemcpyHostToDevice);
-        if (e == cudaSuccess)
-            e = cudaMemcpy(at + 2 * wide + sizeof(int64_t), dtypes, num_tensors * sizeof(int32_t), cudaMemcpyHostToDevice);
-    }
+    if (e == cudaSuccess)
+        e = cudaMemcpy(at, c->entries.data(), wide, cudaMemcpyHostToDevice);
+    if (e == cudaSuccess)
+        e = cudaMemcpy(at + wide, start.data(), start.size() * sizeof(int32_t), cudaMemcpyHostToDevice);
     if (e == cudaSuccess)
         e = cudaStreamSynchronize(nullptr);            // the tables are in place whatever stream reads them
+    c->d_entries = reinterpret_cast<const Entry *>(at);
+    c->d_start = reinterpret_cast<const int32_t *>(at + wide);
     cudaSetDevice(prev);
     if (e != cudaSuccess) {
         cudaGetLastError();
@@ -337,14 +416,15 @@ gnmr_status gnmr_clip_scratch_bytes(const gnmr_clip *c, int64_t *bytes)
 {
     if (!c || !bytes)
         return fail(GNMR_ERR_INVALID_ARG, "clip: NULL argument");
-    *bytes = int64_t(launches_of(c)) * kMostCtas * sizeof(double);
+    *bytes = int64_t(c->launches.size()) * kMostSquares * sizeof(double);
     return GNMR_OK;
 }
 
 gnmr_status gnmr_clip_run(const gnmr_clip *c, const void *const *d_in, void *const *d_out, double max_norm, const double *d_unit_norms,
                           int64_t num_norms, float *d_norm, void *d_scratch, int64_t scratch_bytes, void *stream)
 {
-    if (!c || !d_norm || (c->tensors > 0 && !d_in) || num_norms < 0)
+    const int tensors = c ? static_cast<int>(c->entries.size()) - 1 : 0;
+    if (!c || !d_norm || (tensors > 0 && !d_in) || num_norms < 0)
         return fail(GNMR_ERR_INVALID_ARG, "clip: NULL argument, or a negative number of norms");
     if (!(max_norm >= 0))
         return fail(GNMR_ERR_INVALID_ARG, "clip: max_norm has to be 0 or more");
@@ -354,9 +434,9 @@ gnmr_status gnmr_clip_run(const gnmr_clip *c, const void *const *d_in, void *con
         return fail(GNMR_ERR_LAYOUT, "clip: scratch missing, too small or misaligned");
     if (misaligned(d_unit_norms, 8) || misaligned(d_norm, 4))
         return fail(GNMR_ERR_LAYOUT, "clip: a buffer not aligned to its element size");
-    for (int i = 0; i < c->tensors; ++i) {
-        const size_t eb = element_bytes(c->dtypes[i]);
-        if (c->lengths[i] > 0 && (!d_in[i] || (d_out && !d_out[i])))
+    for (int i = 0; i < tensors; ++i) {
+        const size_t eb = element_bytes(c->entries[i].dtype);
+        if (c->entries[i].length > 0 && (!d_in[i] || (d_out && !d_out[i])))
             return fail(GNMR_ERR_INVALID_ARG, "clip: NULL tensor");
         if (misaligned(d_in[i], eb) || (d_out && misaligned(d_out[i], eb)))
             return fail(GNMR_ERR_LAYOUT, "clip: a tensor not aligned to its element size");
@@ -366,25 +446,30 @@ gnmr_status gnmr_clip_run(const gnmr_clip *c, const void *const *d_in, void *con
     if (prev != c->device)
         cudaSetDevice(c->device);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    double *partial = static_cast<double *>(d_scratch);
+    double *const partial = static_cast<double *>(d_scratch);
     int partials = 0;
     cudaError_t e = cudaSuccess;
     if (d_unit_norms) {
-        partials = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>((num_norms + kThreads - 1) / kThreads, c->sms)));
-        norms_kernel<<<partials, kThreads, 0, st>>>(d_unit_norms, num_norms, partial);
-        e = cudaGetLastError();
+        partials = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>((num_norms + kThreads - 1) / kThreads, 128)));
+        cudaLaunchAttribute attr;
+        const cudaLaunchConfig_t cfg = config(partials, st, &attr);
+        e = cudaLaunchKernelEx(&cfg, norms_kernel, d_unit_norms, num_norms, partial);
     } else {
-        e = by_launch(c, d_in, d_out, [&](const Plan &p, const auto &places) {
-            return launch_squares(c, p, places, partial, &partials, st);
-        });
+        for (const Launch &l : c->launches)
+            if (e == cudaSuccess) {
+                e = by_capacity(l, [&](auto n) { return launch_squares<n.value>(c, l, d_in, partial + partials, st); });
+                partials += l.squares.ctas;
+            }
     }
     float *norm = d_norm;
-    if (e == cudaSuccess)
-        e = by_launch(c, d_in, d_out, [&](const Plan &p, const auto &places) {
-            scale_kernel<<<ctas_for(c, p.chunks), kThreads, 0, st>>>(p, places, partial, partials, max_norm, norm, !d_out);
+    for (const Launch &l : c->launches)
+        if (e == cudaSuccess) {
+            e = by_capacity(l, [&](auto n) {
+                return d_out ? launch_scale<n.value, true>(c, l, d_in, d_out, partial, partials, max_norm, norm, st)
+                             : launch_scale<n.value, false>(c, l, d_in, nullptr, partial, partials, max_norm, norm, st);
+            });
             norm = nullptr;
-            return cudaGetLastError();
-        });
+        }
     if (e != cudaSuccess)
         cudaGetLastError();
     if (prev != c->device)
