@@ -12,11 +12,33 @@ namespace gnmr_act {
 // nothing, which the 16-bit outputs do not see.
 __device__ __forceinline__ float sigmoid(float a) { return __fdividef(1.0f, 1.0f + __expf(-a)); }
 
+// The normal distribution function P(a) = erfc(-a / sqrt 2) / 2, and exp(-a^2 / 2).  Hastings' form (Abramowitz and
+// Stegun 7.1.26): P(-|a|) = exp(-a^2 / 2) t Q(t), t = 1 / (1 + 0.375 |a|), with a Q of degree 8 fitted to
+// 64-bit values: 2.2e-7 relative over the whole range, and with fp32's roundings less than half of (8 + 1.2 |a| + a^2) 2^-23.
+// (1 + erf would cancel below zero.  erfcf took the gradient of 49,152 x 1408 168 us, this 123.)
+__device__ __forceinline__ float normal(float a, float &bell)
+{
+    const float m = fabsf(a), t = __fdividef(1.0f, fmaf(0.375f, m, 1.0f));
+    bell = __expf(-0.5f * a * a);
+    float q = -0.03291367366909981f;
+    q = fmaf(q, t, 0.1368897706270218f);
+    q = fmaf(q, t, -0.18653617799282074f);
+    q = fmaf(q, t, 0.050644271075725555f);
+    q = fmaf(q, t, 0.015622680075466633f);
+    q = fmaf(q, t, 0.0886395052075386f);
+    q = fmaf(q, t, 0.12844553589820862f);
+    q = fmaf(q, t, 0.14960458874702454f);
+    q = fmaf(q, t, 0.14960338175296783f);
+    const float tail = bell * (t * q);
+    return a < 0.0f ? tail : 1.0f - tail;
+}
+
 template <int kAct> __device__ __forceinline__ float activated(float a)
 {
     if (kAct == GNMR_ACT_SILU)
         return a * sigmoid(a);
-    return a * (0.5f * erfcf(a * -0.70710678f));             // erfc: 1 + erf would cancel below zero
+    float bell;
+    return a * normal(a, bell);
 }
 
 // act(a), and its derivative.
@@ -27,8 +49,9 @@ template <int kAct> __device__ __forceinline__ float activated(float a, float &s
         slope = s * (1.0f + a * (1.0f - s));
         return a * s;
     }
-    const float p = 0.5f * erfcf(a * -0.70710678f);
-    slope = p + a * (0.39894228f * __expf(-0.5f * a * a));
+    float bell;
+    const float p = normal(a, bell);
+    slope = fmaf(a * 0.39894228f, bell, p);
     return a * p;
 }
 

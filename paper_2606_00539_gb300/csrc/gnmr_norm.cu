@@ -31,6 +31,7 @@ struct Norm {
     int parts;
     void *dw, *db;
     int add;
+    int aligned;                                       // the parameters start at multiples of 16 bytes
 };
 
 constexpr int kThreads = 256;
@@ -122,21 +123,32 @@ template <typename T, int kUnits, bool kVector> struct Held {
     }
 };
 
-// kN parameters from element `at` on, or `none` where there are none.
-template <typename P, int kN> __device__ __forceinline__ void params(const void *from, int64_t at, float none, float (&f)[kN])
+// kN parameters from element `at` on, or `none` where there are none.  aligned: whole 16 bytes may be read.
+template <typename P, int kN> __device__ __forceinline__ void params(const void *from, int64_t at, float none, bool aligned, float (&f)[kN])
 {
     const P *p = static_cast<const P *>(from) + at;
     if (!from) {
 #pragma unroll
         for (int j = 0; j < kN; ++j)
             f[j] = none;
-    } else if constexpr (kN == 1) {
-        f[0] = to_f32(*p);
-    } else {
-#pragma unroll
-        for (int j = 0; j < kN; ++j)
-            f[j] = to_f32(p[j]);
+        return;
     }
+    if constexpr (kN % kIn16<P> == 0) {
+        if (aligned) {
+#pragma unroll
+            for (int j = 0; j < kN; j += kIn16<P>) {
+                float part[kIn16<P>];
+                widen<P>(__ldg(reinterpret_cast<const uint4 *>(p + j)), part);
+#pragma unroll
+                for (int k = 0; k < kIn16<P>; ++k)
+                    f[j + k] = part[k];
+            }
+            return;
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < kN; ++j)
+        f[j] = to_f32(p[j]);
 }
 
 template <typename T, int kN> __device__ __forceinline__ void store_unit(T *to, const float (&f)[kN])
@@ -159,8 +171,8 @@ __global__ void __launch_bounds__(kThreads, kUnits > 12 ? 2 : kUnits > 6 ? 3 : 4
     const int units = n.cols / kN, lane = threadIdx.x & 31;
     for (int i = threadIdx.x; i < units; i += kThreads) {
         float w[kN], b[kN];
-        params<P, kN>(n.w, int64_t(i) * kN, 1.0f, w);
-        params<P, kN>(n.b, int64_t(i) * kN, 0.0f, b);
+        params<P, kN>(n.w, int64_t(i) * kN, 1.0f, n.aligned, w);
+        params<P, kN>(n.b, int64_t(i) * kN, 0.0f, n.aligned, b);
 #pragma unroll
         for (int q = 0; q < kQuads; ++q) {
             quads[q * units + i] = make_float4(w[4 * q], w[4 * q + 1], w[4 * q + 2], w[4 * q + 3]);
@@ -226,8 +238,8 @@ __global__ void __launch_bounds__(1024) norm_cta_kernel(const Norm n)
             if (at + u * step < units) {
                 const int64_t e = int64_t(at + u * step) * kN;
                 float f[kN], w[kN], b[kN];
-                params<P, kN>(n.w, e, 1.0f, w);
-                params<P, kN>(n.b, e, 0.0f, b);
+                params<P, kN>(n.w, e, 1.0f, n.aligned, w);
+                params<P, kN>(n.b, e, 0.0f, n.aligned, b);
                 x.get(u, f);
 #pragma unroll
                 for (int j = 0; j < kN; ++j)
@@ -330,7 +342,7 @@ template <typename S> __global__ void __launch_bounds__(S::kMost, 1) norm_grad_k
         for (int j = 0; j < kN; ++j)
             w[u][j] = dw[u][j] = db[u][j] = 0.0f;
         if (at + u * span < units)
-            params<P, kN>(n.w, int64_t(at + u * span) * kN, 1.0f, w[u]);
+            params<P, kN>(n.w, int64_t(at + u * span) * kN, 1.0f, n.aligned, w[u]);
     }
     float mean[kRows], rstd[kRows];                    // of the turn to come
     const auto statistics = [&](int64_t turn) {
@@ -622,6 +634,7 @@ Norm norm_of(const gnmr_norm *p)
     n.x = p->d_x;
     n.x_stride = p->x_stride;
     n.w = p->d_weight;
+    n.aligned = !misaligned(p->d_weight, 16) && !misaligned(p->d_bias, 16);
     return n;
 }
 

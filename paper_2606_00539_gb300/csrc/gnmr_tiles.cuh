@@ -399,36 +399,50 @@ template <int kPieces, int kType, int kAct>
 __device__ __forceinline__ void finish_gated(const Product &p, const Item &it, uint32_t (&acc)[kPieces][16], int lane, int col, int span)
 {
     const int odd = lane & 1, second = (lane >> 1) & 1, half = p.lanes >> 1;
-    const int at = lane >> 1, first = at & ~1;           // this lane's output, and the first of the two that it stores
-    const int64_t row = int64_t(it.row0) + it.col0 + col;
-    uint16_t *out = static_cast<uint16_t *>(p.out) + row * p.out_col + first;
-    uint16_t *keep = static_cast<uint16_t *>(p.keep) + row * p.keep_col + (odd ? half : 0) + first;
+    const int first = (lane >> 1) & ~1;                  // the first of the two outputs that this lane stores
+    const int64_t row = int64_t(it.row0) + it.col0 + col, out_step = p.out_col * 2, keep_step = p.keep_col * 2;
+    char *out = static_cast<char *>(p.out) + row * out_step + int64_t(first) * 2;
+    char *keep = static_cast<char *>(p.keep) + row * keep_step + int64_t((odd ? half : 0) + first) * 2;
     const int left = it.cols - col;
     const int there = min(half - first, 2);              // of the two outputs: 0 or less, 1, 2
     const unsigned which = second ? 0x3276 : 0x5410;
+    // both outputs of every lane there, stored as one, 16 columns' offsets within 32 bits
+    const bool whole = (lane | 31) < p.lanes && p.pairs_aligned && (!p.keep || p.keep_aligned) && (out_step | keep_step) < (int64_t(1) << 27);
+    const unsigned out_near = static_cast<unsigned>(out_step), keep_near = static_cast<unsigned>(keep_step);
+    const auto store = [&](char *to, unsigned two) {
+        if (there == 2 && (reinterpret_cast<uintptr_t>(to) & 3) == 0) {
+            *reinterpret_cast<unsigned *>(to) = two;
+        } else {
+            if (there > 0)
+                *reinterpret_cast<uint16_t *>(to) = static_cast<uint16_t>(two);
+            if (there > 1)
+                *reinterpret_cast<uint16_t *>(to + 2) = static_cast<uint16_t>(two >> 16);
+        }
+    };
 #pragma unroll
     for (int q = 0; q < kPieces; ++q) {
         const int n = min(span, left) - q * 16;          // columns of this piece that there are
         if (n <= 0)
             break;
         if (p.keep) {
+            unsigned two[8];                             // of columns 2 j + second
 #pragma unroll
-            for (int j = 0; j < 16; j += 2) {
-                const unsigned w = pack<kType>(__uint_as_float(acc[q][j]), __uint_as_float(acc[q][j + 1]));
-                const unsigned two = __byte_perm(w, __shfl_xor_sync(~0u, w, 2), which);
-                uint16_t *to = keep + (j + second) * p.keep_col;
-                if (j + second < n) {
-                    if (p.keep_aligned && there == 2) {
-                        *reinterpret_cast<unsigned *>(to) = two;
-                    } else {
-                        if (there > 0)
-                            to[0] = static_cast<uint16_t>(two);
-                        if (there > 1)
-                            to[1] = static_cast<uint16_t>(two >> 16);
-                    }
-                }
+            for (int j = 0; j < 8; ++j) {
+                const unsigned w = pack<kType>(__uint_as_float(acc[q][2 * j]), __uint_as_float(acc[q][2 * j + 1]));
+                two[j] = __byte_perm(w, __shfl_xor_sync(~0u, w, 2), which);
             }
-            keep += 16 * p.keep_col;
+            if (whole && n >= 16) {
+                char *const to = keep + second * keep_step;
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    *reinterpret_cast<unsigned *>(to + 2 * j * keep_near) = two[j];
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (2 * j + second < n)
+                        store(keep + (2 * j + second) * keep_step, two[j]);
+            }
+            keep += 16 * keep_step;
         }
         float h[8];                                      // of columns 2 i + odd
 #pragma unroll
@@ -437,24 +451,24 @@ __device__ __forceinline__ void finish_gated(const Product &p, const Item &it, u
             const float other = __shfl_xor_sync(~0u, __uint_as_float(odd ? acc[q][2 * i] : acc[q][2 * i + 1]), 1);
             h[i] = gnmr_act::activated<kAct>(odd ? other : mine) * (odd ? mine : other);
         }
+        unsigned two[4];                                 // of columns 4 i + 2 second + odd
 #pragma unroll
-        for (int i = 0; i < 8; i += 2) {
-            const unsigned w = pack<kType>(h[i], h[i + 1]);
-            const unsigned two = __byte_perm(w, __shfl_xor_sync(~0u, w, 2), which);
-            const int c = 2 * (i + second) + odd;
-            uint16_t *to = out + c * p.out_col;
-            if (c < n) {
-                if (p.pairs_aligned && there == 2) {
-                    *reinterpret_cast<unsigned *>(to) = two;
-                } else {
-                    if (there > 0)
-                        to[0] = static_cast<uint16_t>(two);
-                    if (there > 1)
-                        to[1] = static_cast<uint16_t>(two >> 16);
-                }
-            }
+        for (int i = 0; i < 4; ++i) {
+            const unsigned w = pack<kType>(h[2 * i], h[2 * i + 1]);
+            two[i] = __byte_perm(w, __shfl_xor_sync(~0u, w, 2), which);
         }
-        out += 16 * p.out_col;
+        if (whole && n >= 16) {
+            char *const to = out + (2 * second + odd) * out_step;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                *reinterpret_cast<unsigned *>(to + 4 * i * out_near) = two[i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (4 * i + 2 * second + odd < n)
+                    store(out + (4 * i + 2 * second + odd) * out_step, two[i]);
+        }
+        out += 16 * out_step;
     }
 }
 
