@@ -29,13 +29,13 @@ struct Norm {
     void *y;                                           // or dx
     float *part_w, *part_b;                            // [parts][cols] each
     int parts;
+    int strip;                                         // columns that a CTA of the backward kernel takes
     void *dw, *db;
     int add;
     int aligned;                                       // the parameters start at multiples of 16 bytes
 };
 
 constexpr int kThreads = 256;
-constexpr int kWarps = kThreads / 32;
 
 __device__ __forceinline__ float warp_sum(float v)
 {
@@ -159,17 +159,41 @@ template <typename T, int kN> __device__ __forceinline__ void store_unit(T *to, 
         store_once(to, narrow<T>(f));
 }
 
+__device__ __forceinline__ float sum_of(Pair p)
+{
+    const float2 v = apart(p);
+    return v.x + v.y;
+}
+
 __device__ __forceinline__ float rstd_of(float squares, const Norm &n) { return 1.0f / sqrtf(squares / n.cols + n.eps); }
 
-// A warp a row, which it holds in registers: no barrier, sums by shuffles.  The parameters are in shared
-// memory, as fp32, in groups of four of which a warp reads contiguous ones.
+// A warp a row, which it holds in registers: no barrier, sums by shuffles.  The next row is on its way to
+// shared memory meanwhile, where each lane copies its own bytes.  The parameters are there too, as fp32, in groups of
+// four of which a warp reads contiguous ones.
+template <int kUnits> struct Warps {
+    static constexpr int kEach = 8, kCtas = kUnits > 4 ? 2 : 4;    // of a CTA; an SM
+};
+
 template <typename T, typename P, int kUnits>
-__global__ void __launch_bounds__(kThreads, kUnits > 12 ? 2 : kUnits > 6 ? 3 : 4) norm_warp_kernel(const Norm n)
+__global__ void __launch_bounds__(32 * Warps<kUnits>::kEach, Warps<kUnits>::kCtas) norm_warp_kernel(const Norm n)
 {
-    constexpr int kN = kIn16<T>, kQuads = kN / 4;
-    extern __shared__ float4 quads[];                  // weight: [kQuads][units], then bias
+    constexpr int kN = kIn16<T>, kQuads = kN / 4, kPairs = kN / 2, kEach = Warps<kUnits>::kEach;
+    extern __shared__ float4 quads[];                  // weight: [kQuads][units], then bias; then [kEach][kUnits][32] of 16 bytes
     const int units = n.cols / kN, lane = threadIdx.x & 31;
-    for (int i = threadIdx.x; i < units; i += kThreads) {
+    const uint32_t mine = shared_address(quads + 2 * kQuads * units) + ((threadIdx.x >> 5) * kUnits * 32 + lane) * 16;
+    const auto fetch = [&](int64_t r) {
+        if (r < n.rows) {
+            const T *const x = static_cast<const T *>(n.x) + r * n.x_stride;
+#pragma unroll
+            for (int u = 0; u < kUnits; ++u)
+                if (lane + u * 32 < units)
+                    copy16(mine + u * 512, x + (lane + u * 32) * kN);
+        }
+        copies_begun();
+    };
+    int64_t r = int64_t(blockIdx.x) * kEach + (threadIdx.x >> 5);
+    fetch(r);
+    for (int i = threadIdx.x; i < units; i += 32 * kEach) {
         float w[kN], b[kN];
         params<P, kN>(n.w, int64_t(i) * kN, 1.0f, n.aligned, w);
         params<P, kN>(n.b, int64_t(i) * kN, 0.0f, n.aligned, b);
@@ -180,11 +204,38 @@ __global__ void __launch_bounds__(kThreads, kUnits > 12 ? 2 : kUnits > 6 ? 3 : 4
         }
     }
     __syncthreads();
-    for (int64_t r = int64_t(blockIdx.x) * kWarps + (threadIdx.x >> 5); r < n.rows; r += int64_t(gridDim.x) * kWarps) {
-        Held<T, kUnits, true> x;
-        x.load(static_cast<const T *>(n.x) + r * n.x_stride, lane, 32, units);
-        const float mean = warp_sum(x.sum(lane, 32, units)) / n.cols;
-        const float rstd = rstd_of(warp_sum(x.squares(lane, 32, units, mean)), n);
+    for (; r < n.rows; r += int64_t(gridDim.x) * kEach) {
+        copies_done<0>();
+        uint4 x[kUnits];
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u)
+            if (lane + u * 32 < units)
+                x[u] = load_shared(mine + u * 512);
+        fetch(r + int64_t(gridDim.x) * kEach);
+        Pair s = both(0.0f);
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u)
+            if (lane + u * 32 < units) {
+                Pair f[kPairs];
+                widen2<T>(x[u], f);
+                s = add2(s, kPairs == 4 ? add2(add2(f[0], f[1]), add2(f[2], f[kPairs - 1])) : add2(f[0], f[1]));
+            }
+        const float mean = warp_sum(sum_of(s)) / n.cols;
+        const Pair minus = both(-mean);
+        s = both(0.0f);
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u)
+            if (lane + u * 32 < units) {
+                Pair f[kPairs], q = both(0.0f);
+                widen2<T>(x[u], f);
+#pragma unroll
+                for (int j = 0; j < kPairs; ++j) {
+                    f[j] = add2(f[j], minus);
+                    q = fma2(f[j], f[j], q);
+                }
+                s = add2(s, q);
+            }
+        const float rstd = rstd_of(warp_sum(sum_of(s)), n);
         if (lane == 0) {
             if (n.mean)
                 n.mean[r] = mean;
@@ -192,24 +243,235 @@ __global__ void __launch_bounds__(kThreads, kUnits > 12 ? 2 : kUnits > 6 ? 3 : 4
                 n.rstd[r] = rstd;
         }
         T *const y = static_cast<T *>(n.y) + r * n.y_stride;
+        const Pair by = both(rstd);
 #pragma unroll
         for (int u = 0; u < kUnits; ++u) {
             const int at = lane + u * 32;
             if (at < units) {
-                float f[kN];
-                x.get(u, f);
+                Pair f[kPairs];
+                widen2<T>(x[u], f);
 #pragma unroll
                 for (int q = 0; q < kQuads; ++q) {
                     const float4 w = quads[q * units + at], b = quads[(kQuads + q) * units + at];
-                    f[4 * q] = fmaf((f[4 * q] - mean) * rstd, w.x, b.x);
-                    f[4 * q + 1] = fmaf((f[4 * q + 1] - mean) * rstd, w.y, b.y);
-                    f[4 * q + 2] = fmaf((f[4 * q + 2] - mean) * rstd, w.z, b.z);
-                    f[4 * q + 3] = fmaf((f[4 * q + 3] - mean) * rstd, w.w, b.w);
+                    f[2 * q] = fma2(mul2(add2(f[2 * q], minus), by), pair(w.x, w.y), pair(b.x, b.y));
+                    f[2 * q + 1] = fma2(mul2(add2(f[2 * q + 1], minus), by), pair(w.z, w.w), pair(b.z, b.w));
                 }
-                store_unit<T, kN>(y + int64_t(at) * kN, f);
+                store_once(y + at * kN, narrow2<T>(f));
             }
         }
     }
+    copies_done<0>();
+}
+
+// ---- rows by groups of warps --------------------------------------------------------
+
+// Wider rows: `each` warps of a CTA share one, kUnits times 16 bytes a lane, so that 32 warps are under way with 64
+// registers a thread; sums by shuffles, and between the group's warps through shared memory and a barrier of their
+// own.  The next row is on its way to shared memory meanwhile, where each lane copies its own bytes.  The
+// parameters are there too, as they are, since a CTA takes many rows.
+struct Group {
+    int each, base, at, step;                          // warps; this group's first; this thread's first unit, and from one to the next
+    __device__ __forceinline__ Group(int warps)
+        : each(warps), base((threadIdx.x >> 5) / warps * warps), at(threadIdx.x - base * 32), step(32 * warps)
+    {
+    }
+    // The sum of v over the group, the same bits in every thread.  shared: [32] floats that no other sum between two
+    // barriers uses.
+    __device__ __forceinline__ float sum(float v, float *shared) const
+    {
+        v = warp_sum(v);
+        if (each == 1)
+            return v;
+        if ((threadIdx.x & 31) == 0)
+            shared[threadIdx.x >> 5] = v;
+        asm volatile("bar.sync %0, %1;" ::"r"(base / each), "r"(step) : "memory");
+        v = shared[base];
+        for (int i = 1; i < each; ++i)
+            v += shared[base + i];
+        return v;
+    }
+};
+
+// The parameters in shared memory, filled by the CTA: those of unit u in place u, and, where they are wider than the
+// rows' elements, the second half of them `units` places behind, so that a warp reads contiguous places.
+template <typename T, typename P> __device__ __forceinline__ void fill_params(uint4 *to, const void *from, float none, const Norm &n)
+{
+    constexpr int kN = kIn16<P>, kEach = static_cast<int>(sizeof(P) / sizeof(T));
+    const int places = n.cols / kN, units = places / kEach;
+    for (int i = threadIdx.x; i < places; i += blockDim.x) {
+        float f[kN];
+        params<P, kN>(from, int64_t(i) * kN, none, n.aligned, f);
+        to[i / kEach + i % kEach * units] = narrow<P>(f);
+    }
+}
+
+template <typename T, typename P> __device__ __forceinline__ void params_of(const uint4 *from, int u, int units, Pair (&f)[kIn16<T> / 2])
+{
+    if constexpr (sizeof(T) == sizeof(P)) {
+        widen2<P>(from[u], f);
+    } else {
+        Pair half[2];
+        widen2<P>(from[u], half);
+        f[0] = half[0], f[1] = half[1];
+        widen2<P>(from[units + u], half);
+        f[2] = half[0], f[3] = half[1];
+    }
+}
+
+// Bytes of shared memory beside the rows.
+template <typename P> __host__ __device__ constexpr int params_bytes(int cols, int how_many) { return how_many * cols * static_cast<int>(sizeof(P)); }
+
+template <typename T, typename P, int kUnits, int kThreadsMost>
+__global__ void __launch_bounds__(kThreadsMost, 1) norm_group_kernel(const Norm n, int each)
+{
+    constexpr int kN = kIn16<T>, kPairs = kN / 2;
+    extern __shared__ uint4 held[];                    // the weight, the bias; the rows on their way: [warps][kUnits][32]
+    __shared__ float shared[2][2][32];                 // by turns: a row's sums are read while the next one's are formed
+    const int units = n.cols / kN, of_params = params_bytes<P>(n.cols, 1) / 16;
+    const Group g(each);
+    const uint4 *const weight = held, *const bias = held + of_params;
+    const uint32_t mine = shared_address(held + 2 * of_params) + ((threadIdx.x >> 5) * kUnits * 32 + (threadIdx.x & 31)) * 16;
+    const int rows = (blockDim.x >> 5) / each;         // at a time
+    const auto fetch = [&](int64_t r) {
+        if (r < n.rows) {
+            const T *const x = static_cast<const T *>(n.x) + r * n.x_stride;
+#pragma unroll
+            for (int u = 0; u < kUnits; ++u)
+                if (g.at + u * g.step < units)
+                    copy16(mine + u * 512, x + (g.at + u * g.step) * kN);
+        }
+        copies_begun();
+    };
+    int64_t r = int64_t(blockIdx.x) * rows + g.base / each;
+    fetch(r);
+    fill_params<T, P>(held, n.w, 1.0f, n);
+    fill_params<T, P>(held + of_params, n.b, 0.0f, n);
+    __syncthreads();
+    int turn = 0;
+    for (; r < n.rows; r += int64_t(gridDim.x) * rows, turn ^= 1) {
+        copies_done<0>();
+        uint4 x[kUnits];
+        Pair s = both(0.0f);
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u)
+            if (g.at + u * g.step < units) {
+                x[u] = load_shared(mine + u * 512);
+                Pair f[kPairs];
+                widen2<T>(x[u], f);
+                s = add2(s, kPairs == 4 ? add2(add2(f[0], f[1]), add2(f[2], f[kPairs - 1])) : add2(f[0], f[1]));
+            }
+        fetch(r + int64_t(gridDim.x) * rows);
+        const float mean = g.sum(sum_of(s), shared[turn][0]) * n.inverse;
+        const Pair minus = both(-mean);
+        s = both(0.0f);
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u)
+            if (g.at + u * g.step < units) {
+                Pair f[kPairs], q = both(0.0f);
+                widen2<T>(x[u], f);
+#pragma unroll
+                for (int j = 0; j < kPairs; ++j) {
+                    f[j] = add2(f[j], minus);
+                    q = fma2(f[j], f[j], q);
+                }
+                s = add2(s, q);
+            }
+        const float rstd = rstd_of(g.sum(sum_of(s), shared[turn][1]), n);
+        if (g.at == 0) {
+            if (n.mean)
+                n.mean[r] = mean;
+            if (n.rstd)
+                n.rstd[r] = rstd;
+        }
+        T *const y = static_cast<T *>(n.y) + r * n.y_stride;
+        const Pair by = both(rstd);
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u) {
+            const int at = g.at + u * g.step;
+            if (at < units) {
+                Pair f[kPairs], w[kPairs], b[kPairs];
+                widen2<T>(x[u], f);
+                params_of<T, P>(weight, at, units, w);
+                params_of<T, P>(bias, at, units, b);
+#pragma unroll
+                for (int j = 0; j < kPairs; ++j)
+                    f[j] = fma2(mul2(add2(f[j], minus), by), w[j], b[j]);
+                store_once(y + at * kN, narrow2<T>(f));
+            }
+        }
+    }
+    copies_done<0>();
+}
+
+// dx alone, likewise: rows too wide for one CTA to hold their columns' sums.
+template <typename T, typename P, int kUnits, int kThreadsMost>
+__global__ void __launch_bounds__(kThreadsMost, 1) norm_dx_kernel(const Norm n, int each)
+{
+    constexpr int kN = kIn16<T>, kPairs = kN / 2;
+    extern __shared__ uint4 held[];                    // the weight; the rows of x and dy: [warps][2][kUnits][32]
+    __shared__ float shared[2][2][32];
+    const int units = n.cols / kN, of_params = params_bytes<P>(n.cols, 1) / 16;
+    const Group g(each);
+    const uint32_t mine = shared_address(held + of_params) + ((threadIdx.x >> 5) * 2 * kUnits * 32 + (threadIdx.x & 31)) * 16;
+    const int rows = (blockDim.x >> 5) / each;
+    const auto fetch = [&](int64_t r) {
+        if (r < n.rows) {
+            const T *const x = static_cast<const T *>(n.x) + r * n.x_stride, *const dy = static_cast<const T *>(n.dy) + r * n.dy_stride;
+#pragma unroll
+            for (int u = 0; u < kUnits; ++u)
+                if (g.at + u * g.step < units) {
+                    copy16(mine + u * 512, x + (g.at + u * g.step) * kN);
+                    copy16(mine + (kUnits + u) * 512, dy + (g.at + u * g.step) * kN);
+                }
+        }
+        copies_begun();
+    };
+    int64_t r = int64_t(blockIdx.x) * rows + g.base / each;
+    fetch(r);
+    fill_params<T, P>(held, n.w, 1.0f, n);
+    __syncthreads();
+    int turn = 0;
+    for (; r < n.rows; r += int64_t(gridDim.x) * rows, turn ^= 1) {
+        const float mean = n.mean_in[r], by = n.rstd_in[r];
+        copies_done<0>();
+        const Pair minus = both(-mean), rstd = both(by);
+        uint4 x[kUnits], dy[kUnits];
+        Pair s = both(0.0f), q = both(0.0f);
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u)
+            if (g.at + u * g.step < units) {
+                x[u] = load_shared(mine + u * 512);
+                dy[u] = load_shared(mine + (kUnits + u) * 512);
+                Pair f[kPairs], d[kPairs], w[kPairs];
+                widen2<T>(x[u], f);
+                widen2<T>(dy[u], d);
+                params_of<T, P>(held, g.at + u * g.step, units, w);
+#pragma unroll
+                for (int j = 0; j < kPairs; ++j) {
+                    const Pair t = mul2(d[j], w[j]);
+                    s = add2(s, t);
+                    q = fma2(t, mul2(add2(f[j], minus), rstd), q);
+                }
+            }
+        fetch(r + int64_t(gridDim.x) * rows);
+        const Pair minus_m1 = both(-(g.sum(sum_of(s), shared[turn][0]) * n.inverse) * by), minus_m2 = both(-(g.sum(sum_of(q), shared[turn][1]) * n.inverse));
+        T *const dx = static_cast<T *>(n.y) + r * n.y_stride;
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u) {
+            const int at = g.at + u * g.step;
+            if (at < units) {
+                Pair f[kPairs], d[kPairs], w[kPairs];
+                widen2<T>(x[u], f);
+                widen2<T>(dy[u], d);
+                params_of<T, P>(held, at, units, w);
+#pragma unroll
+                for (int j = 0; j < kPairs; ++j)
+                    f[j] = fma2(fma2(mul2(add2(f[j], minus), rstd), minus_m2, mul2(d[j], w[j])), rstd, minus_m1);
+                store_once(dx + at * kN, narrow2<T>(f));
+            }
+        }
+    }
+    copies_done<0>();
 }
 
 // A CTA a row, which it holds in registers: few rows, wide ones, and those that do not start at multiples of 16 bytes.
@@ -251,164 +513,191 @@ __global__ void __launch_bounds__(1024) norm_cta_kernel(const Norm n)
 
 // ---- backward -------------------------------------------------------------------
 
-__device__ __forceinline__ void copy16(uint32_t to, const void *from)
-{
-    asm volatile("cp.async.cg.shared.global.L2::256B [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
-}
-
-__device__ __forceinline__ void copies_begun() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int kLeft> __device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory"); }
-
-__device__ __forceinline__ uint4 load_shared(uint32_t at)
-{
-    uint4 v;
-    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
-    return v;
-}
-
-// kV sums (2 or 4) over a warp at once: in the end lanes of 32 / kV have one each, lane l the (l kV / 32)-th.
+// kV sums (2, 4 or 8) over a warp at once: in the end lanes of 32 / kV have one each, lane l the (l kV / 32)-th.
 template <int kV> __device__ __forceinline__ float warp_sums(const float (&v)[kV])
 {
     const int lane = threadIdx.x & 31;
+    const bool high = lane & 16;
     float s;
-    if constexpr (kV == 4) {
-        const bool high = lane & 16;
-        const float a = (high ? v[2] : v[0]) + __shfl_xor_sync(~0u, high ? v[0] : v[2], 16);
-        const float b = (high ? v[3] : v[1]) + __shfl_xor_sync(~0u, high ? v[1] : v[3], 16);
-        const bool second = lane & 8;
-        s = (second ? b : a) + __shfl_xor_sync(~0u, second ? a : b, 8);
-    } else {
-        const bool high = lane & 16;
+    if constexpr (kV == 2) {
         s = (high ? v[1] : v[0]) + __shfl_xor_sync(~0u, high ? v[0] : v[1], 16);
-        s += __shfl_xor_sync(~0u, s, 8);
+#pragma unroll
+        for (int o = 8; o > 0; o >>= 1)
+            s += __shfl_xor_sync(~0u, s, o);
+        return s;
+    } else {
+        float half[kV / 2];
+#pragma unroll
+        for (int i = 0; i < kV / 2; ++i)
+            half[i] = (high ? v[kV / 2 + i] : v[i]) + __shfl_xor_sync(~0u, high ? v[i] : v[kV / 2 + i], 16);
+        const bool second = lane & 8;
+        if constexpr (kV == 4) {
+            s = (second ? half[1] : half[0]) + __shfl_xor_sync(~0u, second ? half[0] : half[1], 8);
+            s += __shfl_xor_sync(~0u, s, 4);
+        } else {
+            const float a = (second ? half[2] : half[0]) + __shfl_xor_sync(~0u, second ? half[0] : half[2], 8);
+            const float b = (second ? half[3] : half[1]) + __shfl_xor_sync(~0u, second ? half[1] : half[3], 8);
+            const bool third = lane & 4;
+            s = (third ? b : a) + __shfl_xor_sync(~0u, third ? a : b, 4);
+        }
     }
-    s += __shfl_xor_sync(~0u, s, 4);
     s += __shfl_xor_sync(~0u, s, 2);
     return s + __shfl_xor_sync(~0u, s, 1);
 }
 
 // How the backward kernel takes rows: a group of `span` threads has kRows of them a turn, as many groups as there are
-// threads for.  A thread has the same columns of every row, kUnits times 16 bytes (or single elements), so that the sums over the rows
-// stay in its registers; rows on their way are in shared memory, where each thread copies its own bytes (no barrier for
-// that), kTurns turns ahead.  One barrier a turn, for the row sums.
-template <typename T_, typename P_, int kUnits_, int kRows_, int kTurns_, int kMost_, bool kVector_> struct Shape {
+// threads for.  A thread has the same columns of every row, in kPairs pairs: kUnits times 16 bytes, or, where rows do not start at
+// multiples of 16 bytes, single elements `span` apart.  So the sums over the rows stay in its registers; rows on their way
+// are in shared memory, where each thread copies its own bytes (no barrier for that), kTurns turns ahead.  One barrier a
+// turn, for the row sums; across it a thread holds what it read as it was, and widens it twice: several rows a turn
+// share what a turn costs besides.
+template <typename T_, typename P_, int kColumns, int kRows_, int kTurns_, int kMost_, int kCtas_, bool kVector_> struct Shape {
     using T = T_;
     using P = P_;
-    static constexpr int kUnits = kUnits_, kRows = kRows_, kTurns = kTurns_, kMost = kMost_;
+    static constexpr int kRows = kRows_, kTurns = kTurns_, kMost = kMost_, kCtas = kCtas_;
     static constexpr bool kVector = kVector_;
-    static constexpr int kN = kVector ? kIn16<T> : 1;
+    static constexpr int kN = kVector ? kIn16<T> : 2;  // elements of a unit
+    static constexpr int kUnits = kColumns / kN, kPairs = kColumns / 2, kHalf = kN / 2;
     static constexpr int kV = 2 * kRows;               // row sums a turn
     static constexpr int kTurnBytes = kVector ? kRows * kUnits * 2 * 16 : 0;       // of a thread
-    static constexpr int kShared = kMost * kTurnBytes * kTurns;
+    using Raw = std::conditional_t<kVector, uint4, Pair>;
 };
 
-template <typename S> __global__ void __launch_bounds__(S::kMost, 1) norm_grad_kernel(const Norm n, int span)
+// The columns of pair k of a thread at `at` of `span`.
+template <typename S> __device__ __forceinline__ int column(int k, int second, int at, int span)
+{
+    if (S::kVector)
+        return (at + (2 * k / S::kN) * span) * S::kN + 2 * k % S::kN + second;
+    return at + (2 * k + second) * span;
+}
+
+template <typename S> __device__ __forceinline__ void pairs_of(const typename S::Raw &raw, Pair (&f)[S::kHalf])
+{
+    if constexpr (S::kVector)
+        widen2<typename S::T>(raw, f);
+    else
+        f[0] = raw;
+}
+
+template <typename S> __global__ void __launch_bounds__(S::kMost, S::kCtas) norm_grad_kernel(const Norm n, int span)
 {
     using T = typename S::T;
     using P = typename S::P;
-    constexpr int kN = S::kN, kUnits = S::kUnits, kRows = S::kRows, kV = S::kV, kMost = S::kMost;
+    constexpr int kN = S::kN, kUnits = S::kUnits, kPairs = S::kPairs, kHalf = S::kHalf, kRows = S::kRows, kV = S::kV, kMost = S::kMost;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     extern __shared__ __align__(16) uint8_t bytes[];
     __shared__ float sums[2][kMost / 32][kV];
-    const int units = n.cols / kN, groups = blockDim.x / span, group = threadIdx.x / span, at = threadIdx.x - group * span;
+    const int col0 = blockIdx.y * n.strip, cols = min(n.strip, n.cols - col0);
+    const int groups = blockDim.x / span, group = threadIdx.x / span, at = threadIdx.x - group * span;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = span >> 5, warp0 = group * warps;
-    const T *const x = static_cast<const T *>(n.x), *const dy = static_cast<const T *>(n.dy);
-    T *const dx = static_cast<T *>(n.y);
-    const int64_t turns = (n.rows + groups * kRows - 1) / (groups * kRows);
+    const int turns = static_cast<int>((n.rows + groups * kRows - 1) / (groups * kRows));
+    int turn = blockIdx.x;
+    // the first row of this group's next turn, of its next copies, and where these lie
+    int64_t row = (int64_t(turn) * groups + group) * kRows, ahead = row;
+    const int64_t step = int64_t(gridDim.x) * groups * kRows;
+    const T *x = static_cast<const T *>(n.x) + row * n.x_stride + col0 + (S::kVector ? at * kN : 0);
+    const T *dy = static_cast<const T *>(n.dy) + row * n.dy_stride + col0 + (S::kVector ? at * kN : 0);
+    T *dx = n.y ? static_cast<T *>(n.y) + row * n.y_stride + col0 + (S::kVector ? at * kN : 0) : nullptr;
     // 16-byte places of this thread: turn, row, unit, x or dy; those of a warp side by side
-    const uint32_t mine = static_cast<uint32_t>(__cvta_generic_to_shared(bytes)) + threadIdx.x * 16;
-    const auto place = [&](int slot, int row, int u, int which) {
-        return mine + (((slot * kRows + row) * kUnits + u) * 2 + which) * (blockDim.x * 16);
-    };
-    const auto row_of = [&](int64_t turn, int row) { return (turn * groups + group) * kRows + row; };
-    const auto fetch = [&](int64_t turn, int slot) {
-        if (S::kVector && turn < turns)
+    const uint32_t mine = shared_address(bytes) + threadIdx.x * 16, next = blockDim.x * 16;
+    const auto place = [&](int slot, int i, int u) { return mine + ((slot * kRows + i) * kUnits + u) * 2 * next; };
+    const auto fetch = [&](int slot) {
+        if (S::kVector) {
 #pragma unroll
-            for (int i = 0; i < kRows; ++i) {
-                const int64_t r = row_of(turn, i);
-                if (r < n.rows)
+            for (int i = 0; i < kRows; ++i)
+                if (ahead + i < n.rows)
 #pragma unroll
                     for (int u = 0; u < kUnits; ++u)
-                        if (at + u * span < units) {
-                            copy16(place(slot, i, u, 0), x + r * n.x_stride + int64_t(at + u * span) * kN);
-                            copy16(place(slot, i, u, 1), dy + r * n.dy_stride + int64_t(at + u * span) * kN);
+                        if ((at + u * span) * kN < cols) {
+                            copy16(place(slot, i, u), x + i * n.x_stride + u * span * kN);
+                            copy16(place(slot, i, u) + next, dy + i * n.dy_stride + u * span * kN);
                         }
-            }
+            ahead += step;
+            x += step * n.x_stride;
+            dy += step * n.dy_stride;
+        }
         copies_begun();
     };
-    float w[kUnits][kN], dw[kUnits][kN], db[kUnits][kN];
 #pragma unroll
-    for (int u = 0; u < kUnits; ++u) {
+    for (int s = 0; s < S::kTurns; ++s) {
+        if (S::kVector)                                // columns that there are not: zeros
 #pragma unroll
-        for (int j = 0; j < kN; ++j)
-            w[u][j] = dw[u][j] = db[u][j] = 0.0f;
-        if (at + u * span < units)
-            params<P, kN>(n.w, int64_t(at + u * span) * kN, 1.0f, n.aligned, w[u]);
-    }
-    float mean[kRows], rstd[kRows];                    // of the turn to come
-    const auto statistics = [&](int64_t turn) {
-#pragma unroll
-        for (int i = 0; i < kRows; ++i) {
-            const int64_t r = row_of(turn, i);
-            mean[i] = r < n.rows ? n.mean_in[r] : 0.0f;
-            rstd[i] = r < n.rows ? n.rstd_in[r] : 0.0f;
-        }
-    };
-    int64_t turn = blockIdx.x;
-#pragma unroll
-    for (int s = 0; s < S::kTurns; ++s)
-        fetch(turn + int64_t(s) * gridDim.x, s);
-    statistics(turn);
-    int slot = 0, parity = 0;
-    for (; turn < turns; turn += gridDim.x) {
-        copies_done<S::kTurns - 1>();
-        float xh[kRows][kUnits][kN], t[kRows][kUnits][kN], v[kV], scale[kRows];
-#pragma unroll
-        for (int i = 0; i < kRows; ++i) {
-            const int64_t r = row_of(turn, i);
-            const bool there = r < n.rows;
-            scale[i] = rstd[i];
-            v[2 * i] = v[2 * i + 1] = 0.0f;
-#pragma unroll
-            for (int u = 0; u < kUnits; ++u) {
-                float d[kN], q[kN];
-#pragma unroll
-                for (int j = 0; j < kN; ++j)
-                    xh[i][u][j] = t[i][u][j] = d[j] = q[j] = 0.0f;
-                if (there && at + u * span < units) {
-                    float f[kN];
-                    if constexpr (S::kVector) {
-                        widen<T>(load_shared(place(slot, i, u, 0)), f);
-                        widen<T>(load_shared(place(slot, i, u, 1)), d);
-                    } else {
-                        f[0] = to_f32(x[r * n.x_stride + at + u * span]);
-                        d[0] = to_f32(dy[r * n.dy_stride + at + u * span]);
+            for (int u = 0; u < kUnits; ++u)
+                if ((at + u * span) * kN >= cols)
+                    for (int i = 0; i < kRows; ++i) {
+                        store_shared(place(s, i, u), make_uint4(0, 0, 0, 0));
+                        store_shared(place(s, i, u) + next, make_uint4(0, 0, 0, 0));
                     }
+        fetch(s);
+    }
+    Pair w[kPairs], dw[kPairs], db[kPairs];
 #pragma unroll
-                    for (int j = 0; j < kN; ++j) {
-                        xh[i][u][j] = (f[j] - mean[i]) * rstd[i];
-                        t[i][u][j] = d[j] * w[u][j];
-                        q[j] = t[i][u][j] * xh[i][u][j];
-                        dw[u][j] = fmaf(d[j], xh[i][u][j], dw[u][j]);
-                        db[u][j] += d[j];
+    for (int k = 0; k < kPairs; ++k) {
+        const int c0 = column<S>(k, 0, at, span), c1 = column<S>(k, 1, at, span);
+        const P *const p = n.w ? static_cast<const P *>(n.w) + col0 : nullptr;
+        w[k] = pair(c0 < cols ? (p ? to_f32(p[c0]) : 1.0f) : 0.0f, c1 < cols ? (p ? to_f32(p[c1]) : 1.0f) : 0.0f);
+        dw[k] = db[k] = both(0.0f);
+    }
+    // lane l has the statistics of row l % kRows of the (l / kRows)-th turn from here, reloaded when they are used up
+    constexpr int kStored = 32 / kRows;
+    float minus_of = 0.0f, rstd_of = 0.0f;
+    int slot = 0, parity = 0, stored = 0;
+    for (; turn < turns; turn += gridDim.x, row += step, stored = (stored + 1) % kStored) {
+        if (stored == 0) {
+            const int64_t r = row + lane / kRows * step + lane % kRows;
+            if (r < n.rows)
+                minus_of = -n.mean_in[r], rstd_of = n.rstd_in[r];
+        }
+        Pair minus[kRows], rstd[kRows];
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) {
+            minus[i] = both(__shfl_sync(~0u, minus_of, stored * kRows + i));
+            rstd[i] = both(__shfl_sync(~0u, rstd_of, stored * kRows + i));
+        }
+        copies_done<S::kTurns - 1>();
+        typename S::Raw a[kRows][kUnits], d[kRows][kUnits];
+        float v[kV];
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) {
+            Pair s = both(0.0f), q = both(0.0f);
+            if (row + i < n.rows)
+#pragma unroll
+                for (int u = 0; u < kUnits; ++u) {
+                    if constexpr (S::kVector) {
+                        a[i][u] = load_shared(place(slot, i, u));
+                        d[i][u] = load_shared(place(slot, i, u) + next);
+                    } else {
+                        const int c0 = column<S>(u, 0, at, span), c1 = column<S>(u, 1, at, span);
+                        const auto get = [&](const T *from, int c) { return c < cols ? to_f32(from[c]) : 0.0f; };
+                        a[i][u] = pair(get(x + i * n.x_stride, c0), get(x + i * n.x_stride, c1));
+                        d[i][u] = pair(get(dy + i * n.dy_stride, c0), get(dy + i * n.dy_stride, c1));
+                    }
+                    Pair f[kHalf], g[kHalf];
+                    pairs_of<S>(a[i][u], f);
+                    pairs_of<S>(d[i][u], g);
+#pragma unroll
+                    for (int j = 0; j < kHalf; ++j) {
+                        const Pair t = mul2(g[j], w[u * kHalf + j]);
+                        s = add2(s, t);
+                        q = fma2(t, mul2(add2(f[j], minus[i]), rstd[i]), q);
                     }
                 }
-                v[2 * i] += tree_sum<kN>(t[i][u]);
-                v[2 * i + 1] += tree_sum<kN>(q);
-            }
+            v[2 * i] = sum_of(s);
+            v[2 * i + 1] = sum_of(q);
         }
-        fetch(turn + int64_t(S::kTurns) * gridDim.x, slot);
+        if (!S::kVector) {
+            x += step * n.x_stride;
+            dy += step * n.dy_stride;
+        }
+        fetch(slot);
         if (++slot == S::kTurns)
             slot = 0;
-        statistics(turn + gridDim.x);
-        if (!dx)
-            continue;
         // the sums of every warp, and then of the group's warps in their order
-        const float s = warp_sums<kV>(v);
         constexpr int kLanes = 32 / kV;
-        float of_group = s;
-        if (warps > 1) {
+        float of_group = warp_sums<kV>(v);
+        if (warps > 1 && dx) {
             if (lane % kLanes == 0)
-                sums[parity][warp][lane / kLanes] = s;
+                sums[parity][warp][lane / kLanes] = of_group;
             __syncthreads();
             of_group = 0.0f;
             for (int i = lane % kLanes; i < warps; i += kLanes)
@@ -418,58 +707,82 @@ template <typename S> __global__ void __launch_bounds__(S::kMost, 1) norm_grad_k
                 of_group += __shfl_xor_sync(~0u, of_group, o);
             parity ^= 1;
         }
+        of_group *= n.inverse;
 #pragma unroll
         for (int i = 0; i < kRows; ++i) {
-            const float m1 = __shfl_sync(~0u, of_group, 2 * i * kLanes) / n.cols, m2 = __shfl_sync(~0u, of_group, (2 * i + 1) * kLanes) / n.cols;
-            const int64_t r = row_of(turn, i);
-            if (r < n.rows)
+            const float m1 = __shfl_sync(~0u, of_group, 2 * i * kLanes), m2 = __shfl_sync(~0u, of_group, (2 * i + 1) * kLanes);
+            if (row + i >= n.rows)
+                continue;
+            const Pair minus_m2 = both(-m2), minus_m1 = mul2(both(-m1), rstd[i]);
 #pragma unroll
-                for (int u = 0; u < kUnits; ++u)
-                    if (at + u * span < units) {
-                        float f[kN];
+            for (int u = 0; u < kUnits; ++u) {
+                Pair f[kHalf], g[kHalf];
+                pairs_of<S>(a[i][u], f);
+                pairs_of<S>(d[i][u], g);
 #pragma unroll
-                        for (int j = 0; j < kN; ++j)
-                            f[j] = scale[i] * (t[i][u][j] - m1 - xh[i][u][j] * m2);
-                        store_unit<T, kN>(dx + r * n.y_stride + int64_t(at + u * span) * kN, f);
-                    }
+                for (int j = 0; j < kHalf; ++j) {
+                    const int k = u * kHalf + j;
+                    const Pair xh = mul2(add2(f[j], minus[i]), rstd[i]);
+                    dw[k] = fma2(g[j], xh, dw[k]);
+                    db[k] = add2(db[k], g[j]);
+                    f[j] = fma2(fma2(xh, minus_m2, mul2(g[j], w[k])), rstd[i], minus_m1);
+                }
+                if (!dx)
+                    continue;
+                if constexpr (S::kVector) {
+                    if ((at + u * span) * kN < cols)
+                        store_once(dx + i * n.y_stride + u * span * kN, narrow2<T>(f));
+                } else {
+                    const int c0 = column<S>(u, 0, at, span), c1 = column<S>(u, 1, at, span);
+                    const float2 two = apart(f[0]);
+                    if (c0 < cols)
+                        dx[i * n.y_stride + c0] = from_f32<T>(two.x);
+                    if (c1 < cols)
+                        dx[i * n.y_stride + c1] = from_f32<T>(two.y);
+                }
+            }
         }
+        if (dx)
+            dx += step * n.y_stride;
     }
+    copies_done<0>();
     if (!n.dw && !n.db)
         return;
     // the groups' sums over their rows, added up in their order
-    copies_done<0>();
-    float *const all = reinterpret_cast<float *>(bytes);           // [2][unit's element][thread]
     if (groups > 1) {
+        ulonglong2 *const all = reinterpret_cast<ulonglong2 *>(bytes);       // [pair][thread]
         __syncthreads();
 #pragma unroll
-        for (int u = 0; u < kUnits; ++u)
-#pragma unroll
-            for (int j = 0; j < kN; ++j) {
-                all[(u * kN + j) * blockDim.x + threadIdx.x] = dw[u][j];
-                all[((kUnits + u) * kN + j) * blockDim.x + threadIdx.x] = db[u][j];
-            }
+        for (int k = 0; k < kPairs; ++k)
+            all[k * blockDim.x + threadIdx.x] = make_ulonglong2(dw[k], db[k]);
         __syncthreads();
         if (group)
             return;
 #pragma unroll
-        for (int u = 0; u < kUnits; ++u)
-#pragma unroll
-            for (int j = 0; j < kN; ++j)
-                for (int g = 1; g < groups; ++g) {
-                    dw[u][j] += all[(u * kN + j) * blockDim.x + g * span + at];
-                    db[u][j] += all[((kUnits + u) * kN + j) * blockDim.x + g * span + at];
-                }
-    }
-#pragma unroll
-    for (int u = 0; u < kUnits; ++u)
-        if (at + u * span < units) {
-            const int64_t e = int64_t(blockIdx.x) * n.cols + int64_t(at + u * span) * kN;
-#pragma unroll
-            for (int j = 0; j < kN; ++j) {
-                n.part_w[e + j] = dw[u][j];
-                n.part_b[e + j] = db[u][j];
+        for (int k = 0; k < kPairs; ++k)
+            for (int g = 1; g < groups; ++g) {
+                const ulonglong2 o = all[k * blockDim.x + g * span + at];
+                dw[k] = add2(dw[k], o.x);
+                db[k] = add2(db[k], o.y);
             }
+    }
+    float *const part_w = n.part_w + int64_t(blockIdx.x) * n.cols + col0, *const part_b = n.part_b + int64_t(blockIdx.x) * n.cols + col0;
+#pragma unroll
+    for (int k = 0; k < kPairs; ++k) {
+        const int c0 = column<S>(k, 0, at, span), c1 = column<S>(k, 1, at, span);
+        if (S::kVector) {                              // pairs of neighbours, an even number of columns
+            if (c0 < cols) {
+                *reinterpret_cast<Pair *>(part_w + c0) = dw[k];
+                *reinterpret_cast<Pair *>(part_b + c0) = db[k];
+            }
+        } else {
+            const float2 of_w = apart(dw[k]), of_b = apart(db[k]);
+            if (c0 < cols)
+                part_w[c0] = of_w.x, part_b[c0] = of_b.x;
+            if (c1 < cols)
+                part_w[c1] = of_w.y, part_b[c1] = of_b.y;
         }
+    }
 }
 
 // Any width and alignment: a CTA a row, which it reads three times.
@@ -551,10 +864,13 @@ __global__ void __launch_bounds__(kThreads) columns_any_kernel(const Norm n)
 }
 
 // The parts' sums: 32 columns a CTA, its warps a share of the parts each, joined in their order.
+constexpr int kJoinWarps = 16;
+
 template <typename G>
-__global__ void __launch_bounds__(kThreads) join_kernel(const Norm n)
+__global__ void __launch_bounds__(32 * kJoinWarps) join_kernel(const Norm n)
 {
-    __shared__ float shared[kWarps][32];
+    __shared__ float shared[kJoinWarps][32];
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     G *const to = static_cast<G *>(blockIdx.y ? n.db : n.dw);
     if (!to)
         return;
@@ -562,16 +878,16 @@ __global__ void __launch_bounds__(kThreads) join_kernel(const Norm n)
     float s = 0.0f;
     if (i < n.cols) {
         const float *const part = (blockIdx.y ? n.part_b : n.part_w) + i;
-#pragma unroll 8
-        for (int p = warp; p < n.parts; p += kWarps)
-            s += part[int64_t(p) * n.cols];
+#pragma unroll 10
+        for (int p = warp; p < n.parts; p += kJoinWarps)
+            s += __ldcg(part + int64_t(p) * n.cols);
     }
     shared[warp][lane] = s;
     __syncthreads();
     if (warp || i >= n.cols)
         return;
 #pragma unroll
-    for (int k = 1; k < kWarps; ++k)
+    for (int k = 1; k < kJoinWarps; ++k)
         s += shared[k][lane];
     to[i] = from_f32<G>(n.add ? to_f32(to[i]) + s : s);
 }
@@ -646,15 +962,65 @@ gnmr_status said(cudaError_t e)
     return fail(GNMR_ERR_CUDA, cudaGetErrorString(e));
 }
 
+constexpr int kSharedMost = 226 << 10;
+
+// How many warps share a row of `units`, at most kMost units a lane: a power of two, or 0 where 16 do not hold it.
+int warps_for(int units, int most)
+{
+    int each = 1;
+    while (each <= 16 && (units + 32 * each - 1) / (32 * each) > most)
+        each *= 2;
+    return each <= 16 ? each : 0;
+}
+
 template <typename T, typename P, int kUnits> cudaError_t launch_warps(const Norm &n, int sms, cudaStream_t st)
 {
-    const int shared = 8 * n.cols, most = kUnits > 12 ? 2 : kUnits > 6 ? 3 : 4;
+    using W = Warps<kUnits>;
+    const int shared = 8 * n.cols + W::kEach * kUnits * 512;
     const cudaError_t e = cudaFuncSetAttribute(norm_warp_kernel<T, P, kUnits>, cudaFuncAttributeMaxDynamicSharedMemorySize, shared);
     if (e != cudaSuccess)
         return e;
-    const int64_t ctas = std::min<int64_t>((n.rows + kWarps - 1) / kWarps, int64_t(sms) * most);
-    norm_warp_kernel<T, P, kUnits><<<static_cast<unsigned>(ctas), kThreads, shared, st>>>(n);
+    const int64_t ctas = std::min<int64_t>((n.rows + W::kEach - 1) / W::kEach, int64_t(sms) * W::kCtas);
+    norm_warp_kernel<T, P, kUnits><<<static_cast<unsigned>(ctas), 32 * W::kEach, shared, st>>>(n);
     return cudaGetLastError();
+}
+
+// `kernel` in CTAs of up to `threads`, as many as have shared memory beside the parameters, and as few as give every SM rows.
+template <typename K>
+cudaError_t launch_groups(K kernel, const Norm &n, int each, int threads, int params, int held, int sms, cudaStream_t st)
+{
+    while (threads > 32 * each && (params + threads * held > kSharedMost || n.rows * 32 * each <= int64_t(threads) / 2 * sms))
+        threads /= 2;
+    const int shared = params + threads * held;
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, shared);
+    if (e != cudaSuccess)
+        return e;
+    const int rows = threads / (32 * each);
+    const int64_t ctas = std::min<int64_t>((n.rows + rows - 1) / rows, int64_t(sms));
+    kernel<<<static_cast<unsigned>(ctas), threads, shared, st>>>(n, each);
+    return cudaGetLastError();
+}
+
+constexpr int kMostUnits = 5;                          // 16-byte units a lane of the forward kernel
+
+template <typename T, typename P> cudaError_t launch_forward(const Norm &n, int units, int sms, cudaStream_t st)
+{
+    const int each = warps_for(units, kMostUnits), lane = (units + 32 * each - 1) / (32 * each);
+    const auto go = [&](auto k) {
+        constexpr int kUnits = decltype(k)::value;
+        return launch_groups(norm_group_kernel<T, P, kUnits, 1024>, n, each, 1024, params_bytes<P>(n.cols, 2), kUnits * 16, sms, st);
+    };
+    if (lane <= 3)
+        return go(std::integral_constant<int, 3>());
+    if (lane <= 4)
+        return go(std::integral_constant<int, 4>());
+    return go(std::integral_constant<int, 5>());
+}
+
+template <typename T, typename P> cudaError_t launch_dx(const Norm &n, int units, int sms, cudaStream_t st)
+{
+    const int each = warps_for(units, 8);
+    return launch_groups(norm_dx_kernel<T, P, 8, 512>, n, each, 512, params_bytes<P>(n.cols, 1), 2 * 8 * 16, sms, st);
 }
 
 template <typename T, typename P, int kUnits, bool kVector> cudaError_t launch_ctas(const Norm &n, int units, int sms, cudaStream_t st)
@@ -665,28 +1031,24 @@ template <typename T, typename P, int kUnits, bool kVector> cudaError_t launch_c
     return cudaGetLastError();
 }
 
-constexpr int64_t kFewRows = 600;
+constexpr int64_t kFewRows = 400;
 
 template <typename T, typename P> cudaError_t forward(const Norm &n, int sms, cudaStream_t st)
 {
     constexpr int kN = kIn16<T>;
     const bool vector = n.cols % kN == 0 && rows_of_16(n.x, n.rows, n.x_stride, sizeof(T)) && rows_of_16(n.y, n.rows, n.y_stride, sizeof(T));
     const int units = vector ? n.cols / kN : n.cols;
-    if (vector && units <= 24 * 32 && (n.rows > kFewRows || units <= 64)) {
+    if (vector && units <= 8 * 32 && (n.rows > kFewRows || units <= 64)) {
         if (units <= 2 * 32)
             return launch_warps<T, P, 2>(n, sms, st);
         if (units <= 4 * 32)
             return launch_warps<T, P, 4>(n, sms, st);
-        if (units <= 8 * 32)
-            return launch_warps<T, P, 8>(n, sms, st);
-        if (units <= 12 * 32)
-            return launch_warps<T, P, 12>(n, sms, st);
-        if (units <= 16 * 32)
-            return launch_warps<T, P, 16>(n, sms, st);
-        if (units <= 20 * 32)
-            return launch_warps<T, P, 20>(n, sms, st);
-        return launch_warps<T, P, 24>(n, sms, st);
+        return launch_warps<T, P, 8>(n, sms, st);
     }
+    const int each = vector ? warps_for(units, kMostUnits) : 0;
+    // a row's CTA of its own where there are few rows: no parameters to be laid down first
+    if (each && params_bytes<P>(n.cols, 2) + 32 * each * kMostUnits * 16 <= kSharedMost && n.rows > kFewRows)
+        return launch_forward<T, P>(n, units, sms, st);
     if (vector && units <= 8 * 1024) {
         if (units <= 1024)
             return launch_ctas<T, P, 1, true>(n, units, sms, st);
@@ -707,18 +1069,20 @@ template <typename T, typename P> cudaError_t forward(const Norm &n, int sms, cu
     return cudaGetLastError();
 }
 
-template <typename S> cudaError_t launch_grad(Norm &n, int units, int sms, cudaStream_t st)
+// strip: columns that a CTA takes, all of them unless n.y is NULL.
+template <typename S> cudaError_t launch_grad(Norm &n, int strip, int sms, cudaStream_t st)
 {
-    const int span = ((units + S::kUnits - 1) / S::kUnits + 31) / 32 * 32, groups = S::kMost / span;
+    const int units = (strip + S::kN - 1) / S::kN, span = ((units + S::kUnits - 1) / S::kUnits + 31) / 32 * 32, groups = S::kMost / span;
     // the groups' sums over the rows pass through the same memory
-    const int sums = groups > 1 ? S::kMost * S::kUnits * S::kN * 8 : 0;
-    const int shared = std::max(S::kShared / S::kMost * (groups * span), sums);
+    const int sums = groups > 1 ? groups * span * S::kPairs * 16 : 0;
+    const int shared = std::max(S::kTurnBytes * S::kTurns * groups * span, sums);
     const cudaError_t e = cudaFuncSetAttribute(norm_grad_kernel<S>, cudaFuncAttributeMaxDynamicSharedMemorySize, shared);
     if (e != cudaSuccess)
         return e;
     const int64_t turns = (n.rows + groups * S::kRows - 1) / (groups * S::kRows);
-    n.parts = static_cast<int>(std::min<int64_t>(turns, std::min(sms * (S::kVector ? 1 : 2), kMostParts)));
-    norm_grad_kernel<S><<<n.parts, groups * span, shared, st>>>(n, span);
+    n.parts = static_cast<int>(std::min<int64_t>(turns, std::min(sms * S::kCtas, kMostParts)));
+    n.strip = strip;
+    norm_grad_kernel<S><<<dim3(n.parts, (n.cols + strip - 1) / strip), groups * span, shared, st>>>(n, span);
     return cudaGetLastError();
 }
 
@@ -727,14 +1091,28 @@ template <typename T, typename P> cudaError_t backward(Norm &n, int sms, cudaStr
     constexpr int kN = kIn16<T>;
     const bool vector = n.cols % kN == 0 && rows_of_16(n.x, n.rows, n.x_stride, sizeof(T)) && rows_of_16(n.dy, n.rows, n.dy_stride, sizeof(T)) &&
                         (!n.y || rows_of_16(n.y, n.rows, n.y_stride, sizeof(T)));
-    if (vector && n.cols <= 640 * 8)
-        return launch_grad<Shape<T, P, 8 / kN, kN / 4, 4, 640, true>>(n, n.cols / kN, sms, st);
+    if (vector && n.cols <= 256)
+        return launch_grad<Shape<T, P, 8, kN / 4, 4, 640, 1, true>>(n, n.cols, sms, st);
+    if (vector && n.cols <= 320 * 16)
+        return launch_grad<Shape<T, P, 16, kN / 2, 2, 320, 1, true>>(n, n.cols, sms, st);
     if (vector && n.cols <= 512 * 16)
-        return launch_grad<Shape<T, P, 16 / kN, 1, kN == 8 ? 6 : 3, 512, true>>(n, n.cols / kN, sms, st);
+        return launch_grad<Shape<T, P, 16, kN / 4, 3, 512, 1, true>>(n, n.cols, sms, st);
     if (!vector && n.cols <= 256 * 8)
-        return launch_grad<Shape<T, P, 8, 1, 1, 256, false>>(n, n.cols, sms, st);
+        return launch_grad<Shape<T, P, 8, 1, 1, 256, 3, false>>(n, n.cols, sms, st);
     if (!vector && n.cols <= 512 * 16)
-        return launch_grad<Shape<T, P, 16, 1, 1, 512, false>>(n, n.cols, sms, st);
+        return launch_grad<Shape<T, P, 16, 1, 1, 512, 1, false>>(n, n.cols, sms, st);
+    const int units = n.cols / kN, each = vector ? warps_for(units, 8) : 0;
+    if (each && params_bytes<P>(n.cols, 1) + 32 * each * 2 * 8 * 16 <= kSharedMost) {
+        cudaError_t e = cudaSuccess;
+        void *const dx = n.y;
+        if (n.dw || n.db) {                            // strips of columns need no sums over rows
+            n.y = nullptr;
+            const int strips = (n.cols + 5119) / 5120;
+            e = launch_grad<Shape<T, P, 16, kN / 2, 2, 320, 1, true>>(n, (n.cols / kN + strips - 1) / strips * kN, sms, st);
+            n.y = dx;
+        }
+        return e == cudaSuccess && dx ? launch_dx<T, P>(n, units, sms, st) : e;      // last: it may write over dy
+    }
     if (n.dw || n.db) {
         n.parts = static_cast<int>(std::min<int64_t>(n.rows, std::min(kMostParts, 2 * sms)));
         columns_any_kernel<T><<<dim3((n.cols + kThreads - 1) / kThreads, n.parts), kThreads, 0, st>>>(n);
@@ -809,8 +1187,16 @@ gnmr_status gnmr_layer_norm_grad(const gnmr_norm *p, void *stream)
         e = by_type(p->dtype, [&](auto v) { return by_params<decltype(v)>(p, n, true, sms, st); });
     if (e == cudaSuccess && (n.dw || n.db) && (n.rows > 0 || !n.add))
         e = by_type(p->grad_dtype, [&](auto v) {
-            join_kernel<decltype(v)><<<dim3((n.cols + 31) / 32, 2), kThreads, 0, st>>>(n);
-            return cudaGetLastError();
+            cudaLaunchConfig_t cfg = {};
+            cfg.gridDim = dim3((n.cols + 31) / 32, 2);
+            cfg.blockDim = dim3(32 * kJoinWarps);
+            cfg.stream = st;
+            cudaLaunchAttribute attr;
+            attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+            attr.val.programmaticStreamSerializationAllowed = 1;
+            cfg.attrs = &attr;
+            cfg.numAttrs = 1;
+            return cudaLaunchKernelEx(&cfg, join_kernel<decltype(v)>, n);
         });
     return said(e);
 }

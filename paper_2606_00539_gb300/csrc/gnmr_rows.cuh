@@ -60,6 +60,90 @@ template <typename T> __device__ __forceinline__ uint4 narrow(const float (&f)[k
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
+// Two fp32 numbers in a pair of registers, and their operations in one instruction.
+using Pair = unsigned long long;
+
+__device__ __forceinline__ Pair pair(float lo, float hi)
+{
+    Pair p;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(p) : "f"(lo), "f"(hi));
+    return p;
+}
+
+__device__ __forceinline__ Pair both(float v) { return pair(v, v); }
+
+__device__ __forceinline__ float2 apart(Pair p)
+{
+    float2 v;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(v.x), "=f"(v.y) : "l"(p));
+    return v;
+}
+
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c)
+{
+    Pair r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+
+__device__ __forceinline__ Pair add2(Pair a, Pair b)
+{
+    Pair r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
+__device__ __forceinline__ Pair mul2(Pair a, Pair b)
+{
+    Pair r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
+// 16 bytes as pairs of neighbours, and back.
+template <typename T> __device__ __forceinline__ void widen2(const uint4 &v, Pair (&f)[kIn16<T> / 2])
+{
+    float e[kIn16<T>];
+    widen<T>(v, e);
+#pragma unroll
+    for (int i = 0; i < kIn16<T> / 2; ++i)
+        f[i] = pair(e[2 * i], e[2 * i + 1]);
+}
+
+template <typename T> __device__ __forceinline__ uint4 narrow2(const Pair (&f)[kIn16<T> / 2])
+{
+    float e[kIn16<T>];
+#pragma unroll
+    for (int i = 0; i < kIn16<T> / 2; ++i) {
+        const float2 v = apart(f[i]);
+        e[2 * i] = v.x, e[2 * i + 1] = v.y;
+    }
+    return narrow<T>(e);
+}
+
+// Copies of 16 bytes to shared memory that their thread waits for, by the groups that it begins.
+__device__ __forceinline__ void copy16(uint32_t to, const void *from)
+{
+    asm volatile("cp.async.cg.shared.global.L2::256B [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+
+__device__ __forceinline__ void copies_begun() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int kLeft> __device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory"); }
+
+__device__ __forceinline__ uint4 load_shared(uint32_t at)
+{
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(at) : "memory");
+    return v;
+}
+
+__device__ __forceinline__ void store_shared(uint32_t at, const uint4 &v)
+{
+    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
+}
+
+__device__ __forceinline__ uint32_t shared_address(const void *p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
+
 // Loads and stores of what is used once.  Volatile: none moves up over griddepcontrol.wait.
 __device__ __forceinline__ uint4 load_once(const void *p)
 {
