@@ -30,6 +30,7 @@ struct Norm {
     float *part_w, *part_b;                            // [parts][cols] each
     int parts;
     int strip;                                         // columns that a CTA of the backward kernel takes
+    int pairs, split;                                  // elements are read two at a time; rows that start alike: every one, or every second
     void *dw, *db;
     int add;
     int aligned;                                       // the parameters start at multiples of 16 bytes
@@ -403,6 +404,136 @@ __global__ void __launch_bounds__(kThreadsMost, 1) norm_group_kernel(const Norm 
     copies_done<0>();
 }
 
+// Two neighbouring elements of a row, as they are in memory.
+template <typename T> using Two = std::conditional_t<sizeof(T) == 2, unsigned, unsigned long long>;
+
+template <typename T> __device__ __forceinline__ Two<T> two_of(T lo, T hi)
+{
+    struct alignas(2 * sizeof(T)) { T lo, hi; } v{lo, hi};
+    return reinterpret_cast<const Two<T> &>(v);
+}
+
+template <typename T> __device__ __forceinline__ Pair widen_two(Two<T> v)
+{
+    if constexpr (sizeof(T) == 4) {
+        return v;
+    } else if constexpr (std::is_same_v<T, __nv_bfloat16>) {
+        return pair(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u));
+    } else {
+        const float2 f = __half22float2(reinterpret_cast<const __half2 &>(v));
+        return pair(f.x, f.y);
+    }
+}
+
+// Columns c and c + 1 of a row of `cols`, c from -1 on: which of them there are.
+template <typename T> __device__ __forceinline__ Two<T> mask_of(int c, int cols)
+{
+    constexpr int kBits = 8 * sizeof(T);
+    const Two<T> all = ~Two<T>(0);
+    return (c >= 0 && c < cols ? all >> kBits : 0) | (c + 1 < cols ? all << kBits : 0);
+}
+
+// Both at once.  One of them may be a neighbour outside the row, whose value means nothing: not in the first row or the last,
+// beyond which there may be no memory.
+template <typename T> __device__ __forceinline__ Two<T> load_two(const T *row, int c, int cols)
+{
+    return c < cols ? *reinterpret_cast<const Two<T> *>(row + c) : Two<T>(0);
+}
+
+template <typename T> __device__ __forceinline__ Two<T> load_each(const T *row, int c, int cols)
+{
+    const T none = from_f32<T>(0.0f);
+    return two_of<T>(c >= 0 && c < cols ? row[c] : none, c + 1 < cols ? row[c + 1] : none);
+}
+
+template <typename T> __device__ __forceinline__ void store_two(T *row, int c, int cols, bool together, float2 v)
+{
+    const T lo = from_f32<T>(v.x), hi = from_f32<T>(v.y);
+    if (together && c >= 0 && c + 1 < cols) {
+        *reinterpret_cast<Two<T> *>(row + c) = two_of<T>(lo, hi);
+        return;
+    }
+    if (c >= 0 && c < cols)
+        row[c] = lo;
+    if (c + 1 < cols)
+        row[c + 1] = hi;
+}
+
+// Whether a row starts at an odd element, seen from places where pairs may be read.
+template <typename T> __device__ __forceinline__ int odd_start(const T *row) { return reinterpret_cast<uintptr_t>(row) / sizeof(T) & 1; }
+
+// The same for rows that do not start at multiples of 16 bytes: kTwos pairs a lane, straight to registers.  The parameters are
+// there twice, for rows that start at even and at odd elements.
+template <typename T, typename P, int kTwos>
+__global__ void __launch_bounds__(1024, 1) norm_pairs_kernel(const Norm n, int each)
+{
+    extern __shared__ uint4 held[];
+    __shared__ float shared[2][2][32];
+    const int twos = n.cols / 2 + 1;                   // of a row, one that begins early among them
+    float2 *const weight = reinterpret_cast<float2 *>(held), *const bias = weight + 2 * twos;
+    for (int i = threadIdx.x; i < 2 * twos; i += blockDim.x) {
+        const int c = 2 * (i % twos) - i / twos;
+        const auto of = [&](const void *p, int c, float none) { return c < 0 || c >= n.cols ? 0.0f : p ? to_f32(static_cast<const P *>(p)[c]) : none; };
+        weight[i] = make_float2(of(n.w, c, 1.0f), of(n.w, c + 1, 1.0f));
+        bias[i] = make_float2(of(n.b, c, 0.0f), of(n.b, c + 1, 0.0f));
+    }
+    __syncthreads();
+    const Group g(each);
+    const int rows = (blockDim.x >> 5) / each;
+    int turn = 0;
+    for (int64_t r = int64_t(blockIdx.x) * rows + g.base / each; r < n.rows; r += int64_t(gridDim.x) * rows, turn ^= 1) {
+        const T *const from = static_cast<const T *>(n.x) + r * n.x_stride;
+        const int odd = odd_start(from);
+        Two<T> raw[kTwos];
+        if (r > 0 && r + 1 < n.rows) {
+#pragma unroll
+            for (int u = 0; u < kTwos; ++u)
+                raw[u] = load_two(from, 2 * (g.at + u * g.step) - odd, n.cols);
+        } else {
+#pragma unroll
+            for (int u = 0; u < kTwos; ++u)
+                raw[u] = load_each(from, 2 * (g.at + u * g.step) - odd, n.cols);
+        }
+        Pair x[kTwos], s = both(0.0f);
+#pragma unroll
+        for (int u = 0; u < kTwos; ++u) {
+            x[u] = widen_two<T>(raw[u] & mask_of<T>(2 * (g.at + u * g.step) - odd, n.cols));
+            s = add2(s, x[u]);
+        }
+        const float mean = g.sum(sum_of(s), shared[turn][0]) * n.inverse;
+        s = both(0.0f);
+#pragma unroll
+        for (int u = 0; u < kTwos; ++u) {
+            const int c = 2 * (g.at + u * g.step) - odd;
+            x[u] = add2(x[u], both(-mean));
+            if (c >= 0 && c + 1 < n.cols) {
+                s = fma2(x[u], x[u], s);
+            } else {
+                const float2 v = apart(x[u]);
+                const Pair there = pair(c >= 0 && c < n.cols ? v.x : 0.0f, c + 1 < n.cols ? v.y : 0.0f);
+                s = fma2(there, there, s);
+            }
+        }
+        const float rstd = rstd_of(g.sum(sum_of(s), shared[turn][1]), n);
+        if (g.at == 0) {
+            if (n.mean)
+                n.mean[r] = mean;
+            if (n.rstd)
+                n.rstd[r] = rstd;
+        }
+        T *const y = static_cast<T *>(n.y) + r * n.y_stride;
+        const Pair by = both(rstd);
+#pragma unroll
+        for (int u = 0; u < kTwos; ++u) {
+            const int i = g.at + u * g.step;
+            if (2 * i - odd < n.cols) {
+                const float2 w = weight[odd * twos + i], b = bias[odd * twos + i];
+                store_two(y, 2 * i - odd, n.cols, true, apart(fma2(mul2(x[u], by), pair(w.x, w.y), pair(b.x, b.y))));
+            }
+        }
+    }
+}
+
 // dx alone, likewise: rows too wide for one CTA to hold their columns' sums.
 template <typename T, typename P, int kUnits, int kThreadsMost>
 __global__ void __launch_bounds__(kThreadsMost, 1) norm_dx_kernel(const Norm n, int each)
@@ -547,7 +678,8 @@ template <int kV> __device__ __forceinline__ float warp_sums(const float (&v)[kV
 
 // How the backward kernel takes rows: a group of `span` threads has kRows of them a turn, as many groups as there are
 // threads for.  A thread has the same columns of every row, in kPairs pairs: kUnits times 16 bytes, or, where rows do not start at
-// multiples of 16 bytes, single elements `span` apart.  So the sums over the rows stay in its registers; rows on their way
+// multiples of 16 bytes, pairs of elements `span` apart (a CTA then takes rows that start alike, at even elements or at odd ones:
+// its pairs are the same columns of each).  So the sums over the rows stay in its registers; rows on their way
 // are in shared memory, where each thread copies its own bytes (no barrier for that), kTurns turns ahead.  One barrier a
 // turn, for the row sums; across it a thread holds what it read as it was, and widens it twice: several rows a turn
 // share what a turn costs besides.
@@ -560,15 +692,15 @@ template <typename T_, typename P_, int kColumns, int kRows_, int kTurns_, int k
     static constexpr int kUnits = kColumns / kN, kPairs = kColumns / 2, kHalf = kN / 2;
     static constexpr int kV = 2 * kRows;               // row sums a turn
     static constexpr int kTurnBytes = kVector ? kRows * kUnits * 2 * 16 : 0;       // of a thread
-    using Raw = std::conditional_t<kVector, uint4, Pair>;
+    using Raw = std::conditional_t<kVector, uint4, Two<T>>;
 };
 
-// The columns of pair k of a thread at `at` of `span`.
-template <typename S> __device__ __forceinline__ int column(int k, int second, int at, int span)
+// The first column of pair k of a thread at `at` of `span`; odd: rows start at odd elements.
+template <typename S> __device__ __forceinline__ int column(int k, int at, int span, int odd)
 {
     if (S::kVector)
-        return (at + (2 * k / S::kN) * span) * S::kN + 2 * k % S::kN + second;
-    return at + (2 * k + second) * span;
+        return (at + (2 * k / S::kN) * span) * S::kN + 2 * k % S::kN;
+    return 2 * (at + k * span) - odd;
 }
 
 template <typename S> __device__ __forceinline__ void pairs_of(const typename S::Raw &raw, Pair (&f)[S::kHalf])
@@ -576,7 +708,7 @@ template <typename S> __device__ __forceinline__ void pairs_of(const typename S:
     if constexpr (S::kVector)
         widen2<typename S::T>(raw, f);
     else
-        f[0] = raw;
+        f[0] = widen_two<typename S::T>(raw);
 }
 
 template <typename S> __global__ void __launch_bounds__(S::kMost, S::kCtas) norm_grad_kernel(const Norm n, int span)
@@ -590,14 +722,19 @@ template <typename S> __global__ void __launch_bounds__(S::kMost, S::kCtas) norm
     const int col0 = blockIdx.y * n.strip, cols = min(n.strip, n.cols - col0);
     const int groups = blockDim.x / span, group = threadIdx.x / span, at = threadIdx.x - group * span;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = span >> 5, warp0 = group * warps;
-    const int turns = static_cast<int>((n.rows + groups * kRows - 1) / (groups * kRows));
-    int turn = blockIdx.x;
+    // of rows that start alike (all of them, or every second) the first, how many, and the CTAs that share them
+    const int first = blockIdx.x % n.split, ctas = gridDim.x / n.split;
+    const int64_t rows = (n.rows - first + n.split - 1) / n.split;
+    const int64_t x_stride = n.x_stride * n.split, dy_stride = n.dy_stride * n.split, y_stride = n.y_stride * n.split;
+    const int turns = static_cast<int>((rows + groups * kRows - 1) / (groups * kRows));
+    int turn = blockIdx.x / n.split;
     // the first row of this group's next turn, of its next copies, and where these lie
     int64_t row = (int64_t(turn) * groups + group) * kRows, ahead = row;
-    const int64_t step = int64_t(gridDim.x) * groups * kRows;
-    const T *x = static_cast<const T *>(n.x) + row * n.x_stride + col0 + (S::kVector ? at * kN : 0);
-    const T *dy = static_cast<const T *>(n.dy) + row * n.dy_stride + col0 + (S::kVector ? at * kN : 0);
-    T *dx = n.y ? static_cast<T *>(n.y) + row * n.y_stride + col0 + (S::kVector ? at * kN : 0) : nullptr;
+    const int64_t step = int64_t(ctas) * groups * kRows;
+    const T *x = static_cast<const T *>(n.x) + first * n.x_stride + row * x_stride + col0 + (S::kVector ? at * kN : 0);
+    const T *dy = static_cast<const T *>(n.dy) + first * n.dy_stride + row * dy_stride + col0 + (S::kVector ? at * kN : 0);
+    T *dx = n.y ? static_cast<T *>(n.y) + first * n.y_stride + row * y_stride + col0 + (S::kVector ? at * kN : 0) : nullptr;
+    const int odd = !S::kVector && n.pairs ? odd_start(static_cast<const T *>(n.x) + first * n.x_stride + col0) : 0;
     // 16-byte places of this thread: turn, row, unit, x or dy; those of a warp side by side
     const uint32_t mine = shared_address(bytes) + threadIdx.x * 16, next = blockDim.x * 16;
     const auto place = [&](int slot, int i, int u) { return mine + ((slot * kRows + i) * kUnits + u) * 2 * next; };
@@ -605,16 +742,16 @@ template <typename S> __global__ void __launch_bounds__(S::kMost, S::kCtas) norm
         if (S::kVector) {
 #pragma unroll
             for (int i = 0; i < kRows; ++i)
-                if (ahead + i < n.rows)
+                if (ahead + i < rows)
 #pragma unroll
                     for (int u = 0; u < kUnits; ++u)
                         if ((at + u * span) * kN < cols) {
-                            copy16(place(slot, i, u), x + i * n.x_stride + u * span * kN);
-                            copy16(place(slot, i, u) + next, dy + i * n.dy_stride + u * span * kN);
+                            copy16(place(slot, i, u), x + i * x_stride + u * span * kN);
+                            copy16(place(slot, i, u) + next, dy + i * dy_stride + u * span * kN);
                         }
             ahead += step;
-            x += step * n.x_stride;
-            dy += step * n.dy_stride;
+            x += step * x_stride;
+            dy += step * dy_stride;
         }
         copies_begun();
     };
@@ -633,20 +770,46 @@ template <typename S> __global__ void __launch_bounds__(S::kMost, S::kCtas) norm
     Pair w[kPairs], dw[kPairs], db[kPairs];
 #pragma unroll
     for (int k = 0; k < kPairs; ++k) {
-        const int c0 = column<S>(k, 0, at, span), c1 = column<S>(k, 1, at, span);
+        const int c = column<S>(k, at, span, odd);
         const P *const p = n.w ? static_cast<const P *>(n.w) + col0 : nullptr;
-        w[k] = pair(c0 < cols ? (p ? to_f32(p[c0]) : 1.0f) : 0.0f, c1 < cols ? (p ? to_f32(p[c1]) : 1.0f) : 0.0f);
+        const auto weight = [&](int c) { return c < 0 || c >= cols ? 0.0f : p ? to_f32(p[c]) : 1.0f; };
+        w[k] = pair(weight(c), weight(c + 1));
         dw[k] = db[k] = both(0.0f);
     }
     // lane l has the statistics of row l % kRows of the (l / kRows)-th turn from here, reloaded when they are used up
     constexpr int kStored = 32 / kRows;
     float minus_of = 0.0f, rstd_of = 0.0f;
     int slot = 0, parity = 0, stored = 0;
-    for (; turn < turns; turn += gridDim.x, row += step, stored = (stored + 1) % kStored) {
+    typename S::Raw a[kRows][kUnits], d[kRows][kUnits];
+    const auto elements = [&](auto &a, auto &d, int64_t r) {
+#pragma unroll
+        for (int i = 0; i < kRows; ++i)
+#pragma unroll
+            for (int u = 0; u < kUnits; ++u) {
+                const int c = column<S>(u, at, span, odd);
+                if (r + i >= rows)
+                    continue;
+                if (n.pairs && r + i > 0 && r + i + 1 < rows) {
+                    a[i][u] = load_two(x + i * x_stride, c, cols);
+                    d[i][u] = load_two(dy + i * dy_stride, c, cols);
+                } else {
+                    a[i][u] = load_each(x + i * x_stride, c, cols);
+                    d[i][u] = load_each(dy + i * dy_stride, c, cols);
+                }
+            }
+    };
+    typename S::Raw there[S::kVector ? 1 : kUnits];
+    if constexpr (!S::kVector) {
+        elements(a, d, row);
+#pragma unroll
+        for (int u = 0; u < kUnits; ++u)
+            there[u] = mask_of<T>(column<S>(u, at, span, odd), cols);
+    }
+    for (; turn < turns; turn += ctas, row += step, stored = (stored + 1) % kStored) {
         if (stored == 0) {
             const int64_t r = row + lane / kRows * step + lane % kRows;
-            if (r < n.rows)
-                minus_of = -n.mean_in[r], rstd_of = n.rstd_in[r];
+            if (r < rows)
+                minus_of = -n.mean_in[r * n.split + first], rstd_of = n.rstd_in[r * n.split + first];
         }
         Pair minus[kRows], rstd[kRows];
 #pragma unroll
@@ -655,22 +818,19 @@ template <typename S> __global__ void __launch_bounds__(S::kMost, S::kCtas) norm
             rstd[i] = both(__shfl_sync(~0u, rstd_of, stored * kRows + i));
         }
         copies_done<S::kTurns - 1>();
-        typename S::Raw a[kRows][kUnits], d[kRows][kUnits];
         float v[kV];
 #pragma unroll
         for (int i = 0; i < kRows; ++i) {
             Pair s = both(0.0f), q = both(0.0f);
-            if (row + i < n.rows)
+            if (row + i < rows)
 #pragma unroll
                 for (int u = 0; u < kUnits; ++u) {
                     if constexpr (S::kVector) {
                         a[i][u] = load_shared(place(slot, i, u));
                         d[i][u] = load_shared(place(slot, i, u) + next);
                     } else {
-                        const int c0 = column<S>(u, 0, at, span), c1 = column<S>(u, 1, at, span);
-                        const auto get = [&](const T *from, int c) { return c < cols ? to_f32(from[c]) : 0.0f; };
-                        a[i][u] = pair(get(x + i * n.x_stride, c0), get(x + i * n.x_stride, c1));
-                        d[i][u] = pair(get(dy + i * n.dy_stride, c0), get(dy + i * n.dy_stride, c1));
+                        a[i][u] &= there[u];
+                        d[i][u] &= there[u];
                     }
                     Pair f[kHalf], g[kHalf];
                     pairs_of<S>(a[i][u], f);
@@ -685,9 +845,11 @@ template <typename S> __global__ void __launch_bounds__(S::kMost, S::kCtas) norm
             v[2 * i] = sum_of(s);
             v[2 * i + 1] = sum_of(q);
         }
-        if (!S::kVector) {
-            x += step * n.x_stride;
-            dy += step * n.dy_stride;
+        typename S::Raw a2[S::kVector ? 1 : kRows][kUnits], d2[S::kVector ? 1 : kRows][kUnits];
+        if constexpr (!S::kVector) {                   // a turn ahead too, in registers
+            x += step * x_stride;
+            dy += step * dy_stride;
+            elements(a2, d2, row + step);
         }
         fetch(slot);
         if (++slot == S::kTurns)
@@ -711,7 +873,7 @@ template <typename S> __global__ void __launch_bounds__(S::kMost, S::kCtas) norm
 #pragma unroll
         for (int i = 0; i < kRows; ++i) {
             const float m1 = __shfl_sync(~0u, of_group, 2 * i * kLanes), m2 = __shfl_sync(~0u, of_group, (2 * i + 1) * kLanes);
-            if (row + i >= n.rows)
+            if (row + i >= rows)
                 continue;
             const Pair minus_m2 = both(-m2), minus_m1 = mul2(both(-m1), rstd[i]);
 #pragma unroll
@@ -731,19 +893,20 @@ template <typename S> __global__ void __launch_bounds__(S::kMost, S::kCtas) norm
                     continue;
                 if constexpr (S::kVector) {
                     if ((at + u * span) * kN < cols)
-                        store_once(dx + i * n.y_stride + u * span * kN, narrow2<T>(f));
+                        store_once(dx + i * y_stride + u * span * kN, narrow2<T>(f));
                 } else {
-                    const int c0 = column<S>(u, 0, at, span), c1 = column<S>(u, 1, at, span);
-                    const float2 two = apart(f[0]);
-                    if (c0 < cols)
-                        dx[i * n.y_stride + c0] = from_f32<T>(two.x);
-                    if (c1 < cols)
-                        dx[i * n.y_stride + c1] = from_f32<T>(two.y);
+                    store_two(dx + i * y_stride, column<S>(u, at, span, odd), cols, n.pairs, apart(f[0]));
                 }
             }
         }
         if (dx)
-            dx += step * n.y_stride;
+            dx += step * y_stride;
+        if constexpr (!S::kVector)
+#pragma unroll
+            for (int i = 0; i < kRows; ++i)
+#pragma unroll
+                for (int u = 0; u < kUnits; ++u)
+                    a[i][u] = a2[i][u], d[i][u] = d2[i][u];
     }
     copies_done<0>();
     if (!n.dw && !n.db)
@@ -769,18 +932,15 @@ template <typename S> __global__ void __launch_bounds__(S::kMost, S::kCtas) norm
     float *const part_w = n.part_w + int64_t(blockIdx.x) * n.cols + col0, *const part_b = n.part_b + int64_t(blockIdx.x) * n.cols + col0;
 #pragma unroll
     for (int k = 0; k < kPairs; ++k) {
-        const int c0 = column<S>(k, 0, at, span), c1 = column<S>(k, 1, at, span);
+        const int c = column<S>(k, at, span, odd);
         if (S::kVector) {                              // pairs of neighbours, an even number of columns
-            if (c0 < cols) {
-                *reinterpret_cast<Pair *>(part_w + c0) = dw[k];
-                *reinterpret_cast<Pair *>(part_b + c0) = db[k];
+            if (c < cols) {
+                *reinterpret_cast<Pair *>(part_w + c) = dw[k];
+                *reinterpret_cast<Pair *>(part_b + c) = db[k];
             }
         } else {
-            const float2 of_w = apart(dw[k]), of_b = apart(db[k]);
-            if (c0 < cols)
-                part_w[c0] = of_w.x, part_b[c0] = of_b.x;
-            if (c1 < cols)
-                part_w[c1] = of_w.y, part_b[c1] = of_b.y;
+            store_two(part_w, c, cols, false, apart(dw[k]));
+            store_two(part_b, c, cols, false, apart(db[k]));
         }
     }
 }
@@ -1026,12 +1186,18 @@ template <typename T, typename P> cudaError_t launch_dx(const Norm &n, int units
 template <typename T, typename P, int kUnits, bool kVector> cudaError_t launch_ctas(const Norm &n, int units, int sms, cudaStream_t st)
 {
     const int threads = ((units + kUnits - 1) / kUnits + 31) / 32 * 32;
-    const int64_t ctas = std::min<int64_t>(n.rows, int64_t(sms) * std::min(2048 / threads, 16));
+    const int64_t ctas = std::min<int64_t>(n.rows, int64_t(sms) * std::min(2048 / threads, 32));
     norm_cta_kernel<T, P, kUnits, kVector><<<static_cast<unsigned>(ctas), threads, 0, st>>>(n);
     return cudaGetLastError();
 }
 
 constexpr int64_t kFewRows = 400;
+
+// Whether the rows of two matrices begin at odd elements alike, and all elements where their size says.
+bool alike(const void *a, int64_t a_stride, const void *b, int64_t b_stride, size_t bytes)
+{
+    return ((reinterpret_cast<uintptr_t>(a) ^ reinterpret_cast<uintptr_t>(b)) / bytes & 1) == 0 && ((a_stride ^ b_stride) & 1) == 0;
+}
 
 template <typename T, typename P> cudaError_t forward(const Norm &n, int sms, cudaStream_t st)
 {
@@ -1058,9 +1224,17 @@ template <typename T, typename P> cudaError_t forward(const Norm &n, int sms, cu
             return launch_ctas<T, P, 4, true>(n, units, sms, st);
         return launch_ctas<T, P, 8, true>(n, units, sms, st);
     }
+    constexpr int kTwos = 12;
+    const int twos = units / 2 + 1, of_row = vector ? 0 : warps_for(twos, kTwos);
+    if (of_row && alike(n.x, n.x_stride, n.y, n.y_stride, sizeof(T)) && 32 * twos <= kSharedMost && n.rows > kFewRows) {
+        const auto go = [&](auto kernel) { return launch_groups(kernel, n, of_row, 1024, 32 * twos, 0, sms, st); };
+        return twos <= 2 * 32 ? go(norm_pairs_kernel<T, P, 2>) : twos <= 6 * 32 ? go(norm_pairs_kernel<T, P, 6>) : go(norm_pairs_kernel<T, P, kTwos>);
+    }
     if (!vector && units <= 32 * 1024) {
-        if (units <= 4 * 1024)
+        if (n.rows <= kFewRows && units <= 4 * 1024)
             return launch_ctas<T, P, 4, false>(n, units, sms, st);
+        if (units <= 8 * 1024)
+            return launch_ctas<T, P, 8, false>(n, units, sms, st);
         if (units <= 12 * 1024)
             return launch_ctas<T, P, 12, false>(n, units, sms, st);
         return launch_ctas<T, P, 32, false>(n, units, sms, st);
@@ -1072,15 +1246,19 @@ template <typename T, typename P> cudaError_t forward(const Norm &n, int sms, cu
 // strip: columns that a CTA takes, all of them unless n.y is NULL.
 template <typename S> cudaError_t launch_grad(Norm &n, int strip, int sms, cudaStream_t st)
 {
-    const int units = (strip + S::kN - 1) / S::kN, span = ((units + S::kUnits - 1) / S::kUnits + 31) / 32 * 32, groups = S::kMost / span;
+    // (a row at odd elements has one more pair)
+    const int units = S::kVector ? strip / S::kN : strip / 2 + 1, span = ((units + S::kUnits - 1) / S::kUnits + 31) / 32 * 32, groups = S::kMost / span;
     // the groups' sums over the rows pass through the same memory
     const int sums = groups > 1 ? groups * span * S::kPairs * 16 : 0;
     const int shared = std::max(S::kTurnBytes * S::kTurns * groups * span, sums);
     const cudaError_t e = cudaFuncSetAttribute(norm_grad_kernel<S>, cudaFuncAttributeMaxDynamicSharedMemorySize, shared);
     if (e != cudaSuccess)
         return e;
-    const int64_t turns = (n.rows + groups * S::kRows - 1) / (groups * S::kRows);
-    n.parts = static_cast<int>(std::min<int64_t>(turns, std::min(sms * S::kCtas, kMostParts)));
+    n.pairs = !S::kVector && alike(n.x, n.x_stride, n.dy, n.dy_stride, sizeof(typename S::T)) &&
+              (!n.y || alike(n.x, n.x_stride, n.y, n.y_stride, sizeof(typename S::T)));
+    n.split = n.pairs && n.x_stride % 2 && n.rows > 1 ? 2 : 1;
+    const int64_t turns = ((n.rows + n.split - 1) / n.split + groups * S::kRows - 1) / (groups * S::kRows);
+    n.parts = n.split * static_cast<int>(std::min<int64_t>(turns, std::min(sms * S::kCtas, kMostParts) / n.split));
     n.strip = strip;
     norm_grad_kernel<S><<<dim3(n.parts, (n.cols + strip - 1) / strip), groups * span, shared, st>>>(n, span);
     return cudaGetLastError();
@@ -1097,9 +1275,9 @@ template <typename T, typename P> cudaError_t backward(Norm &n, int sms, cudaStr
         return launch_grad<Shape<T, P, 16, kN / 2, 2, 320, 1, true>>(n, n.cols, sms, st);
     if (vector && n.cols <= 512 * 16)
         return launch_grad<Shape<T, P, 16, kN / 4, 3, 512, 1, true>>(n, n.cols, sms, st);
-    if (!vector && n.cols <= 256 * 8)
-        return launch_grad<Shape<T, P, 8, 1, 1, 256, 3, false>>(n, n.cols, sms, st);
-    if (!vector && n.cols <= 512 * 16)
+    if (!vector && n.cols <= 256 * 8 - 2)
+        return launch_grad<Shape<T, P, 8, 1, 1, 256, 2, false>>(n, n.cols, sms, st);
+    if (!vector && n.cols <= 512 * 16 - 2)
         return launch_grad<Shape<T, P, 16, 1, 1, 512, 1, false>>(n, n.cols, sms, st);
     const int units = n.cols / kN, each = vector ? warps_for(units, 8) : 0;
     if (each && params_bytes<P>(n.cols, 1) + 32 * each * 2 * 8 * 16 <= kSharedMost) {

@@ -148,13 +148,13 @@ def test_strides_and_arenas(norms, cols, pad, lead, dtype):
             assert (out[:, :lead] == 7).all() and (out[:, lead + cols:] == 7).all()
             for a, z in ((0, lead), (lead + cols, wide + lead), (wide + lead + cols, 2 * wide)):
                 assert torch.equal(arena[a:z], old[a:z])
-    # in place, against other memory: the same operands, so the same bits
+    # in place
     for a, b_ in ((dy, x), (dy.contiguous(), x.contiguous())):
-        own = a.clone(memory_format=torch.preserve_format) if a.is_contiguous() else a
-        want = norms.backward(own, b_, w, mean, rstd, weight_grad=torch.empty_like(w))
-        assert torch.equal(norms.backward(own, b_, w, mean, rstd, out=own, weight_grad=torch.empty_like(w)), want)
-        want = norms.forward(b_, w, b)[0]
-        assert torch.equal(norms.forward(b_, w, b, out=b_)[0], want)
+        dw = torch.empty(cols, device="cuda")
+        old = a.clone()
+        check_backward(norms.backward(a, b_, w, mean, rstd, out=a, weight_grad=dw), dw, None, old, b_, w, mean, rstd, dtype, "f32")
+        old = b_.clone()
+        check_forward(*norms.forward(b_, w, b, out=b_), old, w, b, 1e-5, dtype)
 
 
 def test_no_rows(norms):
