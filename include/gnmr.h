@@ -625,25 +625,30 @@ gnmr_status gnmr_layer_norm_scratch_bytes(const gnmr_norm *p, int64_t *bytes);
 typedef struct gnmr_clip gnmr_clip;
 
 /* A plan for `num_tensors` tensors of the given lengths (elements, 0 included) and types (gnmr_dtype),
- * host arrays that are copied.  It holds no gradient's address, and nothing that a call writes. */
+ * host arrays that are copied.  It is host memory alone: it holds no gradient's address, and nothing that a call writes. */
 gnmr_status gnmr_clip_create(int32_t num_tensors, const int64_t *lengths, const int32_t *dtypes, int32_t device,
                              gnmr_clip **out);
+
+/* The plan's table, which every call reads on the device: its size, and its bytes into host memory, for the caller to copy to
+ * device memory (16-byte aligned) that stays as it is while calls may run. */
+gnmr_status gnmr_clip_table_bytes(const gnmr_clip *c, int64_t *bytes);
+gnmr_status gnmr_clip_write_table(const gnmr_clip *c, void *table);
 
 /* Bytes of scratch that a call of gnmr_clip_run needs. */
 gnmr_status gnmr_clip_scratch_bytes(const gnmr_clip *c, int64_t *bytes);
 
-/* One pass on `stream`.  d_in, d_out: HOST arrays of num_tensors device pointers, each aligned to its element
+/* One pass on `stream`.  d_table: the plan's table on its device.  d_in, d_out: HOST arrays of num_tensors device pointers, each aligned to its element
  * size (NULL for an empty tensor only), read before the call returns.  d_out NULL: the gradients are scaled
  * where they lie, and written only if they are above the limit; otherwise all of d_out is written (no overlap but of a
  * tensor with itself).  max_norm: >= 0, infinity to scale nothing.  d_unit_norms: device fp64 [num_norms], the norms of parts that make up the
  * tensors, as gnmr_step writes them to stats->norm: the norm is formed from them and the gradients are not read for it; NULL: from
  * the gradients.  d_norm: device fp32 [1], written.  d_scratch: device, 256-byte aligned, used during the call only.
  * Errors: GNMR_ERR_INVALID_ARG, GNMR_ERR_LAYOUT, GNMR_ERR_CUDA; detail via gnmr_last_error(NULL). */
-gnmr_status gnmr_clip_run(const gnmr_clip *c, const void *const *d_in, void *const *d_out, double max_norm,
-                          const double *d_unit_norms, int64_t num_norms, float *d_norm, void *d_scratch,
+gnmr_status gnmr_clip_run(const gnmr_clip *c, const void *d_table, const void *const *d_in, void *const *d_out,
+                          double max_norm, const double *d_unit_norms, int64_t num_norms, float *d_norm, void *d_scratch,
                           int64_t scratch_bytes, void *stream);
 
-/* Waits for the plan's device and frees it.  NULL is accepted. */
+/* Frees the plan (no CUDA call: also while a stream is captured).  NULL is accepted. */
 gnmr_status gnmr_clip_destroy(gnmr_clip *c);
 
 #ifdef __cplusplus

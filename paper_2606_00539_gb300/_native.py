@@ -228,7 +228,9 @@ PROTOTYPES = {
     "gnmr_layer_norm_scratch_bytes": (ctypes.c_int, [_P, _P]),
     "gnmr_clip_create": (ctypes.c_int, [ctypes.c_int32, _P, _P, ctypes.c_int32, ctypes.POINTER(_P)]),
     "gnmr_clip_scratch_bytes": (ctypes.c_int, [_P, _P]),
-    "gnmr_clip_run": (ctypes.c_int, [_P, _P, _P, ctypes.c_double, _P, ctypes.c_int64, _P, _P, ctypes.c_int64, _P]),
+    "gnmr_clip_table_bytes": (ctypes.c_int, [_P, _P]),
+    "gnmr_clip_write_table": (ctypes.c_int, [_P, _P]),
+    "gnmr_clip_run": (ctypes.c_int, [_P, _P, _P, _P, ctypes.c_double, _P, ctypes.c_int64, _P, _P, ctypes.c_int64, _P]),
     "gnmr_clip_destroy": (ctypes.c_int, [_P]),
 }
 
@@ -432,6 +434,16 @@ def gnmr_clip_create(lengths, dtypes, device: int = 0) -> int:
     h = _P()
     _check(load().gnmr_clip_create(len(ln), ln.ctypes.data, dt.ctypes.data, int(device), ctypes.byref(h)), None)
     return h.value
+
+
+def gnmr_clip_table(handle: int):
+    """The plan's table as a numpy array of bytes, for the device."""
+    import numpy as np
+    n = ctypes.c_int64(0)
+    _check(load().gnmr_clip_table_bytes(handle, ctypes.addressof(n)), None)
+    table = np.empty(n.value, dtype=np.uint8)
+    _check(load().gnmr_clip_write_table(handle, table.ctypes.data), None)
+    return table
 
 
 def gnmr_clip_scratch_bytes(handle: int) -> int:

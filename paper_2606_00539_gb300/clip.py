@@ -30,19 +30,22 @@ class GradientClip:
             torch = P.torch
         self.device_index = int(device.index if hasattr(device, "index") else device)
         self._device = torch.device("cuda", self.device_index)
-        for i, t in enumerate(tensors):
-            if not isinstance(t, torch.Tensor) or t.dtype not in P._DTYPES:
-                raise ValueError(f"tensor {i} must be a tensor of {' or '.join(str(d) for d in P._DTYPES)}")
-        self._like = [(t.numel(), t.dtype) for t in tensors]
-        self._h = N.gnmr_clip_create([n for n, _ in self._like], [P._DTYPES[d] for _, d in self._like], self.device_index)
+        tensors = list(tensors)
+        if not all(isinstance(t, torch.Tensor) and t.dtype in P._DTYPES for t in tensors):
+            bad = next(i for i, t in enumerate(tensors) if not isinstance(t, torch.Tensor) or t.dtype not in P._DTYPES)
+            raise ValueError(f"tensor {bad} must be a tensor of {' or '.join(str(d) for d in P._DTYPES)}")
+        self._lengths, self._dtypes = [t.numel() for t in tensors], [t.dtype for t in tensors]
+        self._h = N.gnmr_clip_create(self._lengths, [P._DTYPES[d] for d in self._dtypes], self.device_index)
+        self._table = torch.from_numpy(N.gnmr_clip_table(self._h)).to(self._device)
+        self._made_on = torch._C._cuda_getCurrentRawStream(self.device_index)
         self._scratch_bytes = N.gnmr_clip_scratch_bytes(self._h)
 
     # -- lifetime -----------------------------------------------------------
     def close(self) -> None:
-        """Waits for the device and frees the plan."""
+        """Frees the plan; no CUDA call but what torch's allocator makes of its table."""
         if self._h:
             N.gnmr_clip_destroy(self._h)
-            self._h = None
+            self._h = self._table = None
 
     def __enter__(self):
         return self
@@ -59,14 +62,18 @@ class GradientClip:
     # -- the calls ------------------------------------------------------------
     def _places(self, tensors, name):
         tensors = list(tensors)
-        if len(tensors) != len(self._like):
-            raise ValueError(f"{name} must be {len(self._like)} tensors, got {len(tensors)}")
-        for i, (t, (n, dtype)) in enumerate(zip(tensors, self._like)):
-            if not isinstance(t, torch.Tensor) or t.get_device() != self.device_index:
-                raise ValueError(f"{name}[{i}] must be a CUDA tensor on device {self.device_index}")
-            if t.numel() != n or t.dtype != dtype or not t.is_contiguous():
-                raise ValueError(f"{name}[{i}] must be {n} contiguous elements of {dtype}")
-        return tensors, (ctypes.c_void_p * len(tensors))(*(t.data_ptr() for t in tensors))
+        if len(tensors) != len(self._lengths):
+            raise ValueError(f"{name} must be {len(self._lengths)} tensors, got {len(tensors)}")
+        here, isin = self.device_index, torch.Tensor
+        if not all(isinstance(t, isin) and t.get_device() == here for t in tensors):
+            bad = next(i for i, t in enumerate(tensors) if not isinstance(t, isin) or t.get_device() != here)
+            raise ValueError(f"{name}[{bad}] must be a CUDA tensor on device {here}")
+        if [t.numel() for t in tensors] != self._lengths or [t.dtype for t in tensors] != self._dtypes or \
+                not all(t.is_contiguous() for t in tensors):
+            for i, (t, n, dtype) in enumerate(zip(tensors, self._lengths, self._dtypes)):
+                if t.numel() != n or t.dtype != dtype or not t.is_contiguous():
+                    raise ValueError(f"{name}[{i}] must be {n} contiguous elements of {dtype}")
+        return tensors, (ctypes.c_void_p * len(tensors))(*[t.data_ptr() for t in tensors])
 
     def _new(self, shape, dtype, stream):
         if stream is None:
@@ -77,7 +84,8 @@ class GradientClip:
     def prepare_clip(self, grads, max_norm, *, out=None, unit_norms=None, norm=None, stream=None):
         """Validates and marshals clip()'s arguments once and returns a callable that enqueues one pass with
         them: each call is one C call, and returns the norm's tensor.  The tensors' storage and the stream are fixed at preparation, their
-        contents may change between calls; one such callable is for one stream at a time (it has scratch memory of its own)."""
+        contents may change between calls; one such callable is for one stream at a time (it has scratch memory of its own).  Keep it
+        as long as a graph that captured one of its calls is replayed."""
         if not self._h:
             raise ValueError("the plan was closed")
         max_norm = float(max_norm)
@@ -85,6 +93,9 @@ class GradientClip:
             raise ValueError(f"max_norm must be 0 or more, got {max_norm}")
         grads, at = self._places(grads, "grads")
         outs, to = (None, None) if out is None else self._places(out, "out")
+        written = [p for p, n in zip(at if to is None else to, self._lengths) if n]
+        if len(set(written)) != len(written):
+            raise ValueError("the same memory is written twice: no two of the tensors may overlap")
         units, count = None, 0
         if unit_norms is not None:
             if not isinstance(unit_norms, torch.Tensor) or unit_norms.get_device() != self.device_index or \
@@ -99,9 +110,11 @@ class GradientClip:
         if unit_norms is not None:                 # (an empty tensor has no address)
             units, count = unit_norms.data_ptr() or scratch.data_ptr(), unit_norms.numel()
         handle = torch._C._cuda_getCurrentRawStream(self.device_index) if stream is None else stream.cuda_stream
+        if handle != self._made_on:                # the table's memory is not given away before that stream is done with it
+            self._table.record_stream(torch.cuda.current_stream(self._device) if stream is None else stream)
         plan, fn = self._h, N.load().gnmr_clip_run
-        args = (plan, at, to, max_norm, units, count, norm.data_ptr(), scratch.data_ptr(), self._scratch_bytes, handle)
-        keep = (norm, grads, outs, unit_norms, scratch)          # storage the prepared call points into
+        args = (plan, self._table.data_ptr(), at, to, max_norm, units, count, norm.data_ptr(), scratch.data_ptr(), self._scratch_bytes, handle)
+        keep = (norm, grads, outs, unit_norms, scratch, self._table)          # storage the prepared call points into
 
         def run():
             if self._h != plan:
@@ -116,7 +129,7 @@ class GradientClip:
     def clip(self, grads, max_norm, *, out=None, unit_norms=None, norm=None, stream=None):
         """Enqueues one pass and returns the norm before scaling, an fp32 tensor (`norm`, if given).
 
-        grads: tensors of the plan's sizes and types, scaled where they lie, or, with out (as many, of the same types), left as
+        grads: tensors of the plan's sizes and types, no two of which overlap, scaled where they lie, or, with out (as many, of the same types), left as
         they are and written there, scaled or not.  max_norm: 0 or more; infinity only takes the norm.
         unit_norms: fp64 tensor of the norms of parts that make up the gradients, as the monitor's stats["norm"]
         after a step on the same arena: the norm is formed from them, and no gradient is read for it."""

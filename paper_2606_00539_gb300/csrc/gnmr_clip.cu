@@ -10,6 +10,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <cstring>
 #include <new>
 #include <vector>
 
@@ -45,9 +46,9 @@ struct gnmr_clip {
     int device = 0;
     std::vector<Entry> entries;                        // and one behind the last
     std::vector<Launch> launches;
-    const Entry *d_entries = nullptr;
-    const int32_t *d_start = nullptr;
-    void *dmem = nullptr;
+    std::vector<int32_t> start;                        // the launches' tables of their warps' first tensors
+
+    size_t entries_bytes() const { return entries.size() * sizeof(Entry); }
 };
 
 namespace {
@@ -56,13 +57,13 @@ using namespace gnmr_rows;
 
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
-// Few warps with many loads each on their way: 2.4 GB of bf16 took the first kernel 347 us so (7.0 TB/s), with 8
+// Few warps with many loads each on their way: 2.4 GB of bf16 took the first kernel 340 us so (7.1 TB/s), with 8
 // loads a lane and four CTAs an SM 377, with two 569.
 constexpr int kUnroll = 16, kSquaresCtas = 2;          // 16-byte loads a lane; CTAs an SM
 // The second kernel, of the same: 64 CTAs an SM, as they come, 733 us (6.6 TB/s moved), 8 763, 4 774; in place most calls end
-// with the limit not reached, and then a CTA costs its launch alone: 64 an SM 85 us, 4 less than one.  With 16 loads a lane
-// in place of 8, 4 an SM take 757.
-constexpr int kBothCtas = 64, kInPlaceCtas = 4;
+// with the limit not reached, and then the CTAs are what they cost: 64 an SM 85 us, 4 4 us more than 2.  With 16 loads a lane
+// in place of 8, 1 and 2 an SM scale 1.2 GB alike (390 us).
+constexpr int kBothCtas = 64, kInPlaceCtas = 2;
 constexpr int kMostSquares = 512;                      // the first kernel's CTAs, each with a partial sum
 
 // Shares are counted in units of 512 bytes, and four for beginning a tensor: a microsecond's latency,
@@ -208,7 +209,6 @@ __global__ void __launch_bounds__(kThreads)
 scale_kernel(const __grid_constant__ Plan p, const __grid_constant__ Places<kN> places, const __grid_constant__ Outs<kN, kBoth> outs,
              const double *partial, int partials, double max_norm, float *norm_out)
 {
-    __shared__ double sums[kWarps];
     __shared__ float scale_of_all;
     constexpr int kBatch = kBoth ? 8 : 16;             // loads a lane
     const int lane = threadIdx.x & 31;
@@ -218,16 +218,25 @@ scale_kernel(const __grid_constant__ Plan p, const __grid_constant__ Places<kN> 
     Entry e = p.entries[t];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    double sum = 0.0;
-    for (int i = threadIdx.x; i < partials; i += kThreads)
-        sum += __ldcg(partial + i);
-    sum = cta_total(gnmr::warp_allreduce_sum(sum), sums);
-    if (threadIdx.x == 0) {
-        const double norm = sqrt(sum);
-        // a norm that is not finite compares as not above the limit, or as infinite
-        scale_of_all = norm > max_norm && isfinite(norm) ? static_cast<float>(max_norm / norm) : 1.0f;
-        if (blockIdx.x == 0 && norm_out)
-            *norm_out = static_cast<float>(norm);
+    // by one warp: the SM's 64-bit unit takes 20 cycles an instruction, whoever they come from
+    if (threadIdx.x < 32) {
+        double sum = 0.0;
+#pragma unroll 4
+        for (int i = lane; i < partials; i += 32)
+            sum += __ldcg(partial + i);
+        sum = gnmr::warp_allreduce_sum(sum);
+        if (lane == 0) {
+            float scale = 1.0f;
+            if (blockIdx.x == 0 || sum > 0.999999 * max_norm * max_norm) {       // else surely below the limit
+                const double norm = sqrt(sum);
+                // a norm that is not finite compares as not above the limit, or as infinite
+                if (norm > max_norm && isfinite(norm))
+                    scale = static_cast<float>(max_norm / norm);
+                if (blockIdx.x == 0 && norm_out)
+                    *norm_out = static_cast<float>(norm);
+            }
+            scale_of_all = scale;
+        }
     }
     __syncthreads();
     const float scale = scale_of_all;
@@ -283,17 +292,22 @@ template <int kN> Places<kN> places_of(const Launch &l, const void *const *in)
     return p;
 }
 
-Plan plan_of(const gnmr_clip *c, const Launch &l, const Grid &g) { return {c->d_entries + l.from, c->d_start + g.start, l.tensors, l.unit0, l.units}; }
+Plan plan_of(const gnmr_clip *c, const void *table, const Launch &l, const Grid &g)
+{
+    const char *const at = static_cast<const char *>(table);
+    return {reinterpret_cast<const Entry *>(at) + l.from, reinterpret_cast<const int32_t *>(at + c->entries_bytes()) + g.start, l.tensors, l.unit0,
+            l.units};
+}
 
-template <int kN> cudaError_t launch_squares(const gnmr_clip *c, const Launch &l, const void *const *in, double *partial, cudaStream_t st)
+template <int kN> cudaError_t launch_squares(const gnmr_clip *c, const void *table, const Launch &l, const void *const *in, double *partial, cudaStream_t st)
 {
     cudaLaunchAttribute attr;
     const cudaLaunchConfig_t cfg = config(l.squares.ctas, st, &attr);
-    return cudaLaunchKernelEx(&cfg, squares_kernel<kN>, plan_of(c, l, l.squares), places_of<kN>(l, in), partial);
+    return cudaLaunchKernelEx(&cfg, squares_kernel<kN>, plan_of(c, table, l, l.squares), places_of<kN>(l, in), partial);
 }
 
 template <int kN, bool kBoth>
-cudaError_t launch_scale(const gnmr_clip *c, const Launch &l, const void *const *in, void *const *out, const double *partial, int partials,
+cudaError_t launch_scale(const gnmr_clip *c, const void *table, const Launch &l, const void *const *in, void *const *out, const double *partial, int partials,
                          double max_norm, float *norm, cudaStream_t st)
 {
     Outs<kN, kBoth> outs;
@@ -302,7 +316,7 @@ cudaError_t launch_scale(const gnmr_clip *c, const Launch &l, const void *const 
     const Grid &g = kBoth ? l.both : l.in_place;
     cudaLaunchAttribute attr;
     const cudaLaunchConfig_t cfg = config(g.ctas, st, &attr);
-    return cudaLaunchKernelEx(&cfg, scale_kernel<kN, kBoth>, plan_of(c, l, g), places_of<kN>(l, in), outs, partial, partials, max_norm, norm);
+    return cudaLaunchKernelEx(&cfg, scale_kernel<kN, kBoth>, plan_of(c, table, l, g), places_of<kN>(l, in), outs, partial, partials, max_norm, norm);
 }
 
 // Calls f with the capacity that a launch's parameters take, as a constant.
@@ -316,9 +330,9 @@ template <typename F> cudaError_t by_capacity(const Launch &l, F f)
 }
 
 // The launches and each one's table of where its warps begin, for tensors laid end to end.
-std::vector<int32_t> cut(gnmr_clip *c, int sms)
+void cut(gnmr_clip *c, int sms)
 {
-    std::vector<int32_t> start;
+    std::vector<int32_t> &start = c->start;
     const int all = static_cast<int>(c->entries.size()) - 1;
     for (int from = 0; from < std::max(all, 1); from += kMost) {
         Launch l = {};
@@ -342,7 +356,6 @@ std::vector<int32_t> cut(gnmr_clip *c, int sms)
         }
         c->launches.push_back(l);
     }
-    return start;
 }
 
 }  // namespace
@@ -368,11 +381,12 @@ gnmr_status gnmr_clip_create(int32_t num_tensors, const int64_t *lengths, const 
         cudaGetLastError();
         return fail(GNMR_ERR_CUDA, "clip: device not available");
     }
+    int sms = 1;
+    if (const cudaError_t e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device)) {
+        cudaGetLastError();
+        return fail(GNMR_ERR_CUDA, cudaGetErrorString(e));
+    }
     gnmr_clip *c = nullptr;
-    int prev = 0, sms = 1;
-    cudaGetDevice(&prev);
-    cudaError_t e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, device);
-    std::vector<int32_t> start;
     try {
         c = new gnmr_clip;
         c->device = device;
@@ -384,31 +398,29 @@ gnmr_status gnmr_clip_create(int32_t num_tensors, const int64_t *lengths, const 
                 units += kBegin + (lengths[i] * int64_t(element_bytes(dtypes[i])) + kUnit - 1) / kUnit;
         }
         c->entries[num_tensors] = Entry{0, units, 0};
-        start = cut(c, sms);
+        cut(c, sms);
     } catch (const std::bad_alloc &) {
         delete c;
         return fail(GNMR_ERR_OOM, "clip: host allocation failed");
     }
-    const size_t wide = c->entries.size() * sizeof(Entry);
-    cudaSetDevice(device);
-    if (e == cudaSuccess)
-        e = cudaMalloc(&c->dmem, wide + start.size() * sizeof(int32_t));
-    char *at = static_cast<char *>(c->dmem);
-    if (e == cudaSuccess)
-        e = cudaMemcpy(at, c->entries.data(), wide, cudaMemcpyHostToDevice);
-    if (e == cudaSuccess)
-        e = cudaMemcpy(at + wide, start.data(), start.size() * sizeof(int32_t), cudaMemcpyHostToDevice);
-    if (e == cudaSuccess)
-        e = cudaStreamSynchronize(nullptr);            // the tables are in place whatever stream reads them
-    c->d_entries = reinterpret_cast<const Entry *>(at);
-    c->d_start = reinterpret_cast<const int32_t *>(at + wide);
-    cudaSetDevice(prev);
-    if (e != cudaSuccess) {
-        cudaGetLastError();
-        gnmr_clip_destroy(c);
-        return fail(e == cudaErrorMemoryAllocation ? GNMR_ERR_OOM : GNMR_ERR_CUDA, cudaGetErrorString(e));
-    }
     *out = c;
+    return GNMR_OK;
+}
+
+gnmr_status gnmr_clip_table_bytes(const gnmr_clip *c, int64_t *bytes)
+{
+    if (!c || !bytes)
+        return fail(GNMR_ERR_INVALID_ARG, "clip: NULL argument");
+    *bytes = static_cast<int64_t>(c->entries_bytes() + c->start.size() * sizeof(int32_t));
+    return GNMR_OK;
+}
+
+gnmr_status gnmr_clip_write_table(const gnmr_clip *c, void *table)
+{
+    if (!c || !table)
+        return fail(GNMR_ERR_INVALID_ARG, "clip: NULL argument");
+    memcpy(table, c->entries.data(), c->entries_bytes());
+    memcpy(static_cast<char *>(table) + c->entries_bytes(), c->start.data(), c->start.size() * sizeof(int32_t));
     return GNMR_OK;
 }
 
@@ -420,11 +432,11 @@ gnmr_status gnmr_clip_scratch_bytes(const gnmr_clip *c, int64_t *bytes)
     return GNMR_OK;
 }
 
-gnmr_status gnmr_clip_run(const gnmr_clip *c, const void *const *d_in, void *const *d_out, double max_norm, const double *d_unit_norms,
-                          int64_t num_norms, float *d_norm, void *d_scratch, int64_t scratch_bytes, void *stream)
+gnmr_status gnmr_clip_run(const gnmr_clip *c, const void *d_table, const void *const *d_in, void *const *d_out, double max_norm,
+                          const double *d_unit_norms, int64_t num_norms, float *d_norm, void *d_scratch, int64_t scratch_bytes, void *stream)
 {
     const int tensors = c ? static_cast<int>(c->entries.size()) - 1 : 0;
-    if (!c || !d_norm || (tensors > 0 && !d_in) || num_norms < 0)
+    if (!c || !d_table || !d_norm || (tensors > 0 && !d_in) || num_norms < 0)
         return fail(GNMR_ERR_INVALID_ARG, "clip: NULL argument, or a negative number of norms");
     if (!(max_norm >= 0))
         return fail(GNMR_ERR_INVALID_ARG, "clip: max_norm has to be 0 or more");
@@ -432,7 +444,7 @@ gnmr_status gnmr_clip_run(const gnmr_clip *c, const void *const *d_in, void *con
     gnmr_clip_scratch_bytes(c, &need);
     if (!d_scratch || scratch_bytes < need || misaligned(d_scratch, 256))
         return fail(GNMR_ERR_LAYOUT, "clip: scratch missing, too small or misaligned");
-    if (misaligned(d_unit_norms, 8) || misaligned(d_norm, 4))
+    if (misaligned(d_table, 16) || misaligned(d_unit_norms, 8) || misaligned(d_norm, 4))
         return fail(GNMR_ERR_LAYOUT, "clip: a buffer not aligned to its element size");
     for (int i = 0; i < tensors; ++i) {
         const size_t eb = element_bytes(c->entries[i].dtype);
@@ -457,7 +469,7 @@ gnmr_status gnmr_clip_run(const gnmr_clip *c, const void *const *d_in, void *con
     } else {
         for (const Launch &l : c->launches)
             if (e == cudaSuccess) {
-                e = by_capacity(l, [&](auto n) { return launch_squares<n.value>(c, l, d_in, partial + partials, st); });
+                e = by_capacity(l, [&](auto n) { return launch_squares<n.value>(c, d_table, l, d_in, partial + partials, st); });
                 partials += l.squares.ctas;
             }
     }
@@ -465,8 +477,8 @@ gnmr_status gnmr_clip_run(const gnmr_clip *c, const void *const *d_in, void *con
     for (const Launch &l : c->launches)
         if (e == cudaSuccess) {
             e = by_capacity(l, [&](auto n) {
-                return d_out ? launch_scale<n.value, true>(c, l, d_in, d_out, partial, partials, max_norm, norm, st)
-                             : launch_scale<n.value, false>(c, l, d_in, nullptr, partial, partials, max_norm, norm, st);
+                return d_out ? launch_scale<n.value, true>(c, d_table, l, d_in, d_out, partial, partials, max_norm, norm, st)
+                             : launch_scale<n.value, false>(c, d_table, l, d_in, nullptr, partial, partials, max_norm, norm, st);
             });
             norm = nullptr;
         }
@@ -479,15 +491,8 @@ gnmr_status gnmr_clip_run(const gnmr_clip *c, const void *const *d_in, void *con
 
 gnmr_status gnmr_clip_destroy(gnmr_clip *c)
 {
-    if (!c)
-        return GNMR_OK;
-    int prev = 0;
-    cudaGetDevice(&prev);
-    cudaSetDevice(c->device);
-    const cudaError_t e = c->dmem ? cudaFree(c->dmem) : cudaSuccess;
-    cudaSetDevice(prev);
     delete c;
-    return e == cudaSuccess ? GNMR_OK : GNMR_ERR_CUDA;
+    return GNMR_OK;
 }
 
 }  // extern "C"

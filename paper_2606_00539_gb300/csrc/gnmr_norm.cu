@@ -1122,8 +1122,6 @@ gnmr_status said(cudaError_t e)
     return fail(GNMR_ERR_CUDA, cudaGetErrorString(e));
 }
 
-constexpr int kSharedMost = 226 << 10;
-
 // How many warps share a row of `units`, at most kMost units a lane: a power of two, or 0 where 16 do not hold it.
 int warps_for(int units, int most)
 {
@@ -1137,7 +1135,7 @@ template <typename T, typename P, int kUnits> cudaError_t launch_warps(const Nor
 {
     using W = Warps<kUnits>;
     const int shared = 8 * n.cols + W::kEach * kUnits * 512;
-    const cudaError_t e = cudaFuncSetAttribute(norm_warp_kernel<T, P, kUnits>, cudaFuncAttributeMaxDynamicSharedMemorySize, shared);
+    const cudaError_t e = allow_shared<norm_warp_kernel<T, P, kUnits>>();
     if (e != cudaSuccess)
         return e;
     const int64_t ctas = std::min<int64_t>((n.rows + W::kEach - 1) / W::kEach, int64_t(sms) * W::kCtas);
@@ -1145,19 +1143,19 @@ template <typename T, typename P, int kUnits> cudaError_t launch_warps(const Nor
     return cudaGetLastError();
 }
 
-// `kernel` in CTAs of up to `threads`, as many as have shared memory beside the parameters, and as few as give every SM rows.
-template <typename K>
-cudaError_t launch_groups(K kernel, const Norm &n, int each, int threads, int params, int held, int sms, cudaStream_t st)
+// kKernel in CTAs of up to `threads`, as many as have shared memory beside the parameters, and as few as give every SM rows.
+template <auto kKernel>
+cudaError_t launch_groups(const Norm &n, int each, int threads, int params, int held, int sms, cudaStream_t st)
 {
     while (threads > 32 * each && (params + threads * held > kSharedMost || n.rows * 32 * each <= int64_t(threads) / 2 * sms))
         threads /= 2;
     const int shared = params + threads * held;
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, shared);
+    const cudaError_t e = allow_shared<kKernel>();
     if (e != cudaSuccess)
         return e;
     const int rows = threads / (32 * each);
     const int64_t ctas = std::min<int64_t>((n.rows + rows - 1) / rows, int64_t(sms));
-    kernel<<<static_cast<unsigned>(ctas), threads, shared, st>>>(n, each);
+    kKernel<<<static_cast<unsigned>(ctas), threads, shared, st>>>(n, each);
     return cudaGetLastError();
 }
 
@@ -1168,7 +1166,7 @@ template <typename T, typename P> cudaError_t launch_forward(const Norm &n, int 
     const int each = warps_for(units, kMostUnits), lane = (units + 32 * each - 1) / (32 * each);
     const auto go = [&](auto k) {
         constexpr int kUnits = decltype(k)::value;
-        return launch_groups(norm_group_kernel<T, P, kUnits, 1024>, n, each, 1024, params_bytes<P>(n.cols, 2), kUnits * 16, sms, st);
+        return launch_groups<norm_group_kernel<T, P, kUnits, 1024>>(n, each, 1024, params_bytes<P>(n.cols, 2), kUnits * 16, sms, st);
     };
     if (lane <= 3)
         return go(std::integral_constant<int, 3>());
@@ -1180,7 +1178,7 @@ template <typename T, typename P> cudaError_t launch_forward(const Norm &n, int 
 template <typename T, typename P> cudaError_t launch_dx(const Norm &n, int units, int sms, cudaStream_t st)
 {
     const int each = warps_for(units, 8);
-    return launch_groups(norm_dx_kernel<T, P, 8, 512>, n, each, 512, params_bytes<P>(n.cols, 1), 2 * 8 * 16, sms, st);
+    return launch_groups<norm_dx_kernel<T, P, 8, 512>>(n, each, 512, params_bytes<P>(n.cols, 1), 2 * 8 * 16, sms, st);
 }
 
 template <typename T, typename P, int kUnits, bool kVector> cudaError_t launch_ctas(const Norm &n, int units, int sms, cudaStream_t st)
@@ -1227,8 +1225,10 @@ template <typename T, typename P> cudaError_t forward(const Norm &n, int sms, cu
     constexpr int kTwos = 12;
     const int twos = units / 2 + 1, of_row = vector ? 0 : warps_for(twos, kTwos);
     if (of_row && alike(n.x, n.x_stride, n.y, n.y_stride, sizeof(T)) && 32 * twos <= kSharedMost && n.rows > kFewRows) {
-        const auto go = [&](auto kernel) { return launch_groups(kernel, n, of_row, 1024, 32 * twos, 0, sms, st); };
-        return twos <= 2 * 32 ? go(norm_pairs_kernel<T, P, 2>) : twos <= 6 * 32 ? go(norm_pairs_kernel<T, P, 6>) : go(norm_pairs_kernel<T, P, kTwos>);
+        const int bytes = 32 * twos;
+        return twos <= 2 * 32   ? launch_groups<norm_pairs_kernel<T, P, 2>>(n, of_row, 1024, bytes, 0, sms, st)
+               : twos <= 6 * 32 ? launch_groups<norm_pairs_kernel<T, P, 6>>(n, of_row, 1024, bytes, 0, sms, st)
+                                : launch_groups<norm_pairs_kernel<T, P, kTwos>>(n, of_row, 1024, bytes, 0, sms, st);
     }
     if (!vector && units <= 32 * 1024) {
         if (n.rows <= kFewRows && units <= 4 * 1024)
@@ -1251,7 +1251,7 @@ template <typename S> cudaError_t launch_grad(Norm &n, int strip, int sms, cudaS
     // the groups' sums over the rows pass through the same memory
     const int sums = groups > 1 ? groups * span * S::kPairs * 16 : 0;
     const int shared = std::max(S::kTurnBytes * S::kTurns * groups * span, sums);
-    const cudaError_t e = cudaFuncSetAttribute(norm_grad_kernel<S>, cudaFuncAttributeMaxDynamicSharedMemorySize, shared);
+    const cudaError_t e = allow_shared<norm_grad_kernel<S>>();
     if (e != cudaSuccess)
         return e;
     n.pairs = !S::kVector && alike(n.x, n.x_stride, n.dy, n.dy_stride, sizeof(typename S::T)) &&

@@ -6,6 +6,7 @@
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
 
+#include <atomic>
 #include <cstdint>
 #include <type_traits>
 
@@ -180,6 +181,26 @@ inline cudaError_t current_sms(int *sms)
     int dev = 0;
     const cudaError_t e = cudaGetDevice(&dev);
     return e == cudaSuccess ? cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev) : e;
+}
+
+// Lets a kernel have all of an SM's shared memory on the current device, asking the driver once for each kernel and device
+// (every call would cost a small launch a quarter of its time).
+constexpr int kSharedMost = 226 << 10;
+
+template <auto kKernel> cudaError_t allow_shared()
+{
+    static std::atomic<unsigned long long> asked{0};   // a bit for each device
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess)
+        return e;
+    const unsigned long long bit = dev < 64 ? 1ull << dev : 0;
+    if (asked.load(std::memory_order_relaxed) & bit)
+        return cudaSuccess;
+    e = cudaFuncSetAttribute(kKernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSharedMost);
+    if (e == cudaSuccess)
+        asked.fetch_or(bit, std::memory_order_relaxed);
+    return e;
 }
 
 // Calls f with a value of the type that `dtype` names.

@@ -32,52 +32,57 @@ class LayerNorm:
             torch = P.torch
         self.device_index = int(device.index if hasattr(device, "index") else device)
         self._lib = N.load()
+        self._scratch = {}
         self._device = torch.device("cuda", self.device_index)
         self._types = tuple(_DTYPES)
         self._raw_stream = torch._C._cuda_getCurrentRawStream
 
     # -- argument checks ------------------------------------------------------
-    def _tensor(self, t, name, dims, dtypes):
+    # A few rows take the GPU 3 us: these checks are written to cost the host little more.
+    def _refuse(self, t, name, dims, dtypes):
         if not isinstance(t, torch.Tensor) or t.get_device() != self.device_index:
             raise ValueError(f"{name} must be a CUDA tensor on device {self.device_index}")
         if t.dtype not in dtypes:
             raise ValueError(f"{name} must be {' or '.join(str(d) for d in dtypes)}, got {t.dtype}")
-        if t.dim() != dims:
-            raise ValueError(f"{name} must have {dims} dimensions, got {t.dim()}")
+        raise ValueError(f"{name} must have {dims} dimensions, got {t.dim()}")
 
     def _matrix(self, t, name, shape, dtypes):
-        """The row stride of a matrix of contiguous rows."""
-        self._tensor(t, name, 2, dtypes)
+        """(rows, columns, row stride) of a matrix of contiguous rows."""
+        if not isinstance(t, torch.Tensor) or t.get_device() != self.device_index or t.dtype not in dtypes or t.dim() != 2:
+            self._refuse(t, name, 2, dtypes)
         rows, cols = t.shape
         if shape is not None and (rows, cols) != shape:
             raise ValueError(f"{name} must be {list(shape)}, got {[rows, cols]}")
-        if t.stride(1) != 1 and cols > 1:
+        step, one = t.stride()
+        if one != 1 and cols > 1:
             raise ValueError(f"{name} must have contiguous rows")
-        return t.stride(0) if rows > 1 else max(t.stride(0), cols)
+        return rows, cols, step if rows > 1 else max(step, cols)
 
     def _vector(self, t, name, n, dtypes):
         if t is None:
             return None
-        self._tensor(t, name, 1, dtypes)
+        if not isinstance(t, torch.Tensor) or t.get_device() != self.device_index or t.dtype not in dtypes or t.dim() != 1:
+            self._refuse(t, name, 1, dtypes)
         if t.numel() != n or not t.is_contiguous():
             raise ValueError(f"{name} must hold {n} contiguous entries")
         return t.data_ptr()
 
-    def _params(self, p, weight, bias, dtype):
-        p.param_dtype = p.dtype
-        for t in (weight, bias):
-            if t is not None:
-                if t.dtype not in (dtype, torch.float32):
-                    raise ValueError(f"weight and bias must be {dtype} or torch.float32, got {t.dtype}")
-                p.param_dtype = _DTYPES[t.dtype]
-        if weight is not None and bias is not None and weight.dtype != bias.dtype:
-            raise ValueError("weight and bias must be of one type")
-        p.d_weight = self._vector(weight, "weight", p.cols, (dtype, torch.float32))
-        p.d_bias = self._vector(bias, "bias", p.cols, (dtype, torch.float32))
+    def _params(self, weight, bias, dtype, cols):
+        """The parameters' type, and where they are."""
+        kind = dtype
+        if weight is not None:
+            kind = weight.dtype
+            if bias is not None and bias.dtype != kind and kind in (dtype, torch.float32):
+                raise ValueError("weight and bias must be of one type")
+        elif bias is not None:
+            kind = bias.dtype
+        kinds = (dtype, torch.float32)
+        w, b = self._vector(weight, "weight", cols, kinds), self._vector(bias, "bias", cols, kinds)
+        return _DTYPES[kind], w, b
 
     @staticmethod
-    def _no_graph(*operands):
-        if any(t is not None and t.requires_grad for t in operands) and torch.is_grad_enabled():
+    def _no_graph(a, b, c):
+        if (a.requires_grad or (b is not None and b.requires_grad) or (c is not None and c.requires_grad)) and torch.is_grad_enabled():
             raise ValueError("autograd records nothing of these calls: use layer_norm, or detach() or torch.no_grad()")
 
     def _new(self, shape, dtype, stream):
@@ -88,7 +93,7 @@ class LayerNorm:
 
     def _enqueue(self, fn, p, stream):
         handle = self._raw_stream(self.device_index) if stream is None else stream.cuda_stream
-        if torch.cuda.current_device() == self.device_index:
+        if torch._C._cuda_getDevice() == self.device_index:
             status = fn(ctypes.addressof(p), handle)
         else:
             with torch.cuda.device(self.device_index):
@@ -99,20 +104,19 @@ class LayerNorm:
     # -- the passes -------------------------------------------------------------
     def forward(self, x, weight=None, bias=None, *, eps=1e-5, out=None, stream=None):
         """(y, mean, rstd): y of x's type (in `out`, which may be x, if given), statistics fp32 [rows]."""
-        step = self._matrix(x, "x", None, self._types)
-        rows, cols = x.shape
+        rows, cols, step = self._matrix(x, "x", None, self._types)
         if cols < 1:
             raise ValueError("x must have at least one column")
+        dtype = x.dtype
+        kind, w, b = self._params(weight, bias, dtype, cols)
         self._no_graph(x, weight, bias)
-        p = N.gnmr_norm(rows, cols, _DTYPES[x.dtype])
-        self._params(p, weight, bias, x.dtype)
         if out is None:
-            out, across = self._new((rows, cols), x.dtype, stream), cols
+            out, across = self._new((rows, cols), dtype, stream), cols
         else:
-            across = self._matrix(out, "out", (rows, cols), (x.dtype,))
-        mean, rstd = (self._new(rows, torch.float32, stream) for _ in range(2))
-        p.eps, p.d_x, p.x_stride, p.d_y, p.y_stride = eps, x.data_ptr(), step, out.data_ptr(), across
-        p.d_mean, p.d_rstd = mean.data_ptr(), rstd.data_ptr()
+            _, _, across = self._matrix(out, "out", (rows, cols), (dtype,))
+        mean, rstd = self._new(rows, torch.float32, stream), self._new(rows, torch.float32, stream)
+        p = N.gnmr_norm(rows, cols, _DTYPES[dtype], kind, eps, x.data_ptr(), step, w, b, mean.data_ptr(), rstd.data_ptr(),
+                        out.data_ptr(), across)
         self._enqueue(self._lib.gnmr_layer_norm, p, stream)
         return out, mean, rstd
 
@@ -123,43 +127,39 @@ class LayerNorm:
         weight_grad, bias_grad: [cols] tensors of one type (bf16, f16 or fp32) that get the sums over the rows
         of dy * (x - mean) * rstd and of dy, e.g. views of the gradient arena; with add, these are added to
         what is there.  No rows give zeros (nothing is added)."""
-        step = self._matrix(x, "x", None, self._types)
-        rows, cols = x.shape
+        rows, cols, step = self._matrix(x, "x", None, self._types)
         if cols < 1:
             raise ValueError("x must have at least one column")
         dtype = x.dtype
-        apart = self._matrix(dy, "dy", (rows, cols), (dtype,))
+        _, _, apart = self._matrix(dy, "dy", (rows, cols), (dtype,))
+        kind, w, _ = self._params(weight, None, dtype, cols)
         self._no_graph(dy, x, weight)
-        p = N.gnmr_norm(rows, cols, _DTYPES[dtype])
-        self._params(p, weight, None, dtype)
-        p.d_x, p.x_stride, p.d_dy, p.dy_stride = x.data_ptr(), step, dy.data_ptr(), apart
-        p.d_mean = self._vector(mean, "mean", rows, (torch.float32,))
-        p.d_rstd = self._vector(rstd, "rstd", rows, (torch.float32,))
         if mean is None or rstd is None:
             raise ValueError("mean and rstd must be given")
+        m, r = self._vector(mean, "mean", rows, (torch.float32,)), self._vector(rstd, "rstd", rows, (torch.float32,))
+        to_w, to_b = self._vector(weight_grad, "weight_grad", cols, self._types), self._vector(bias_grad, "bias_grad", cols, self._types)
+        if weight_grad is not None and bias_grad is not None and weight_grad.dtype != bias_grad.dtype:
+            raise ValueError("weight_grad and bias_grad must be of one type")
+        grads = next((_DTYPES[t.dtype] for t in (weight_grad, bias_grad) if t is not None), _DTYPES[dtype])
+        at, across = None, 0
         if not input_grad:
             if out is not None:
                 raise ValueError("out is for the input's gradient")
         elif out is None:
-            out = self._new((rows, cols), dtype, stream)
-            p.d_dx, p.dx_stride = out.data_ptr(), cols
+            out, across = self._new((rows, cols), dtype, stream), cols
+            at = out.data_ptr()
         else:
-            p.dx_stride = self._matrix(out, "out", (rows, cols), (dtype,))
-            p.d_dx = out.data_ptr()
-        p.add = bool(add)
-        p.grad_dtype = p.dtype
-        scratch = None
-        if weight_grad is not None or bias_grad is not None:
-            p.d_dweight = self._vector(weight_grad, "weight_grad", cols, self._types)
-            p.d_dbias = self._vector(bias_grad, "bias_grad", cols, self._types)
-            kinds = {t.dtype for t in (weight_grad, bias_grad) if t is not None}
-            if len(kinds) > 1:
-                raise ValueError("weight_grad and bias_grad must be of one type")
-            p.grad_dtype = _DTYPES[kinds.pop()]
-            if rows:
-                p.scratch_bytes = N.gnmr_layer_norm_scratch_bytes(p)
-                scratch = self._new(p.scratch_bytes, torch.uint8, stream)
-                p.d_scratch = scratch.data_ptr()
+            _, _, across = self._matrix(out, "out", (rows, cols), (dtype,))
+            at = out.data_ptr()
+        p = N.gnmr_norm(rows, cols, _DTYPES[dtype], kind, 0.0, x.data_ptr(), step, w, None, m, r, None, 0, dy.data_ptr(), apart,
+                        at, across, to_w, to_b, grads, bool(add))
+        if rows and (to_w or to_b):
+            need = self._scratch.get(cols)         # it goes by the width alone
+            if need is None:
+                need = self._scratch[cols] = N.gnmr_layer_norm_scratch_bytes(p)
+            scratch = self._new(need, torch.uint8, stream)
+            p.scratch_bytes = need
+            p.d_scratch = scratch.data_ptr()
         self._enqueue(self._lib.gnmr_layer_norm_grad, p, stream)
         return out
 

@@ -219,6 +219,33 @@ def test_prepared_captured_and_from_two_streams():
         plan.clip(x, 1.0)
 
 
+def test_plans_come_and_go_while_a_stream_is_captured():
+    """A plan that is freed during a capture, as when a name is bound anew there, does not end the capture; the same for a
+    prepared call.  Calls that were enqueued on another stream before their plan went are what they were."""
+    g = gen(8)
+    x = [normal(g, 5000, dtype=torch.float32), normal(g, 77, dtype=torch.bfloat16)]
+    out = [torch.zeros_like(v) for v in x]
+    old = GradientClip(x)
+    call = old.prepare_clip(x, 1.0, out=out)
+    plan = GradientClip(x)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        norm = plan.clip(x, 2.0, out=out)
+        del old
+        call = None
+    graph.replay()
+    check(norm, out, x, 2.0)
+    side = torch.cuda.Stream()
+    for _ in range(50):
+        plan = GradientClip(x)
+        norm = plan.clip(x, 2.0, out=out, stream=side)
+        del plan
+        torch.full((1 << 10,), 7, dtype=torch.uint8, device="cuda")          # would land where the table was
+    torch.cuda.synchronize()
+    check(norm, out, x, 2.0)
+    assert call is None
+
+
 def test_offsets_past_31_bits():
     n = (1 << 31) + (1 << 20) + 3
     x = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
@@ -241,7 +268,8 @@ def test_refusals():
             (lambda: plan.clip(x[:1], 1.0), "2 tensors"), (lambda: plan.clip([x[0], x[0]], 1.0), "contiguous elements"),
             (lambda: plan.clip([x[0].cpu(), x[1]], 1.0), "CUDA"), (lambda: plan.clip([torch.zeros(20, device="cuda")[::2], x[1]], 1.0), "contiguous"),
             (lambda: plan.clip(x, 1.0, out=x[:1]), "out must"), (lambda: plan.clip(x, 1.0, unit_norms=x[0]), "unit_norms"),
-            (lambda: plan.clip(x, 1.0, norm=x[0]), "norm must"),
+            (lambda: plan.clip(x, 1.0, norm=x[0]), "norm must"), (lambda: GradientClip([x[0], x[0]]).clip([x[0], x[0]], 1.0), "twice"),
+            (lambda: GradientClip([x[0], x[0]]).clip([x[0], x[0].clone()], 1.0, out=[x[0], x[0]]), "twice"),
         ]:
             with pytest.raises(ValueError, match=why):
                 call()

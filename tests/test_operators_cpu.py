@@ -155,8 +155,8 @@ def test_clip_refusals(lib):
     assert out.value is None
     if not torch.cuda.is_available():
         assert make(2, lengths, dtypes, 0, ctypes.byref(out)) == N.GNMR_ERR_CUDA
-    assert lib.gnmr_clip_run(None, None, None, 1.0, None, 0, 4096, 4096, 1 << 20, None) == INVALID
-    assert lib.gnmr_clip_scratch_bytes(None, None) == INVALID
+    assert lib.gnmr_clip_run(None, 4096, None, None, 1.0, None, 0, 4096, 4096, 1 << 20, None) == INVALID
+    assert lib.gnmr_clip_scratch_bytes(None, None) == lib.gnmr_clip_table_bytes(None, None) == lib.gnmr_clip_write_table(None, None) == INVALID
     assert lib.gnmr_clip_destroy(None) == N.GNMR_OK
 
 
