@@ -191,6 +191,47 @@ def test_hard_rows(norms, cols):
     assert dx[6].isnan().all() and dx[7].isnan().all() and dx[rest].isfinite().all() and dw.isnan().all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("cols,pad", [(33, 0), (1371, 0), (99, 2), (1000, 1), (64, 0), (2056, 0), (5120, 0), (8192, 0), (20480, 0)])
+def test_rows_do_not_meet(norms, cols, pad, dtype):
+    """Neighbours of a row, read with it where rows start at odd places, mean nothing: every other row, and the gaps, are NaN."""
+    g, t, rows = gen(cols), TYPES[dtype], 1501
+    x, dy = (torch.full((rows, cols + pad), float("nan"), dtype=t, device="cuda") for _ in range(2))
+    x[::2, :cols], dy[::2, :cols] = normal(g, 751, cols, dtype=t), normal(g, 751, cols, dtype=t)
+    x, dy = x[:, :cols], dy[:, :cols]
+    y, mean, rstd = norms.forward(x, out=torch.empty_like(x) if pad == 0 else torch.empty(rows, cols + pad, dtype=t, device="cuda")[:, :cols])
+    check_forward(y[::2], mean[::2], rstd[::2], x[::2], None, None, 1e-5, dtype)
+    assert y[1::2].isnan().all() and mean[1::2].isnan().all()
+    dx = norms.backward(dy, x, None, mean, rstd)
+    check_backward(dx[::2], None, None, dy[::2], x[::2], None, mean[::2], rstd[::2], dtype, "f32")
+    assert dx[1::2].isnan().all()
+
+
+@pytest.mark.parametrize("rows,cols,dtype", [(3000, 512, "bf16"), (2000, 1371, "bf16"), (2000, 5120, "bf16"), (900, 8192, "f32"),
+                                             (800, 16384, "bf16"), (41, 777, "f32")])
+def test_statistics_are_optional_and_results_repeat(norms, rows, cols, dtype):
+    """The same bits each time, and with the statistics left out (the C call allows either)."""
+    import ctypes
+
+    from paper_2606_00539_gb300 import _native as N
+    g, t = gen(rows), TYPES[dtype]
+    x, w, b = normal(g, rows, cols, dtype=t), normal(g, cols, dtype=t), normal(g, cols, dtype=t)
+    y, mean, rstd = norms.forward(x, w, b)
+    for _ in range(3):
+        assert all(torch.equal(a, z) for a, z in zip(norms.forward(x, w, b), (y, mean, rstd)))
+    out = torch.empty_like(y)
+    p = N.gnmr_norm(rows, cols, N.GNMR_DTYPE_F32 if dtype == "f32" else N.GNMR_DTYPE_BF16, N.GNMR_DTYPE_F32 if dtype == "f32" else N.GNMR_DTYPE_BF16,
+                    1e-5, x.data_ptr(), cols, w.data_ptr(), b.data_ptr(), None, None, out.data_ptr(), cols)
+    assert N.load().gnmr_layer_norm(ctypes.addressof(p), torch.cuda.current_stream().cuda_stream) == N.GNMR_OK
+    assert torch.equal(out, y)
+    dw, db = torch.empty(2, cols, device="cuda").unbind()
+    dx = norms.backward(x, x, w, mean, rstd, weight_grad=dw, bias_grad=db)
+    first = dx.clone(), dw.clone(), db.clone()
+    for _ in range(3):
+        dx = norms.backward(x, x, w, mean, rstd, weight_grad=dw, bias_grad=db)
+        assert all(torch.equal(a, z) for a, z in zip((dx, dw, db), first))
+
+
 def test_offsets_past_31_bits_of_elements(norms):
     R, cols = (1 << 21) + 3, 1032
     x = torch.zeros(R, cols, dtype=torch.bfloat16, device="cuda")
