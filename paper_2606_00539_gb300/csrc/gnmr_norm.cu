@@ -1258,9 +1258,10 @@ template <typename S> cudaError_t launch_grad(Norm &n, int strip, int sms, cudaS
               (!n.y || alike(n.x, n.x_stride, n.y, n.y_stride, sizeof(typename S::T)));
     n.split = n.pairs && n.x_stride % 2 && n.rows > 1 ? 2 : 1;
     const int64_t turns = ((n.rows + n.split - 1) / n.split + groups * S::kRows - 1) / (groups * S::kRows);
-    n.parts = n.split * static_cast<int>(std::min<int64_t>(turns, std::min(sms * S::kCtas, kMostParts) / n.split));
+    const int strips = (n.cols + strip - 1) / strip;
+    n.parts = n.split * static_cast<int>(std::min<int64_t>(turns, std::max(std::min(sms * S::kCtas / strips, kMostParts) / n.split, 1)));
     n.strip = strip;
-    norm_grad_kernel<S><<<dim3(n.parts, (n.cols + strip - 1) / strip), groups * span, shared, st>>>(n, span);
+    norm_grad_kernel<S><<<dim3(n.parts, strips), groups * span, shared, st>>>(n, span);
     return cudaGetLastError();
 }
 
