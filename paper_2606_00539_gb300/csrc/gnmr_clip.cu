@@ -27,7 +27,8 @@ struct alignas(16) Entry {
     int32_t dtype;
 };
 
-// A kernel's CTAs, and where the table of its warps' first tensors begins ([warps + 1] of them).
+// A kernel's CTAs, and where the table of its warps' first tensors begins (of its CTAs', where outputs are in other memory: many
+// with little each), one more than there are.
 struct Grid {
     int ctas;
     size_t start;
@@ -60,10 +61,11 @@ constexpr int kWarps = kThreads / 32;
 // Few warps with many loads each on their way: 2.4 GB of bf16 took the first kernel 340 us so (7.1 TB/s), with 8
 // loads a lane and four CTAs an SM 377, with two 569.
 constexpr int kUnroll = 16, kSquaresCtas = 2;          // 16-byte loads a lane; CTAs an SM
-// The second kernel, of the same: 64 CTAs an SM, as they come, 733 us (6.6 TB/s moved), 8 763, 4 774; in place most calls end
-// with the limit not reached, and then the CTAs are what they cost: 64 an SM 85 us, 4 4 us more than 2.  With 16 loads a lane
-// in place of 8, 1 and 2 an SM scale 1.2 GB alike (390 us).
-constexpr int kBothCtas = 64, kInPlaceCtas = 2;
+// The second kernel, into other memory: CTAs of 64 KB, as they come, with 8 loads a lane: 2.4 GB 720 us (7.0 TB/s moved), 8 CTAs an
+// SM that stay 763; 256 MB 83.  In place most calls end with the limit not reached, and then the CTAs are what they cost: 64 an
+// SM 85 us, 4 4 us more than 2.
+constexpr int kBothCtas = 256, kBothLeast = 4, kInPlaceCtas = 2;
+constexpr int64_t kBothUnits = 128;                    // of a CTA, beyond kBothLeast an SM
 constexpr int kMostSquares = 512;                      // the first kernel's CTAs, each with a partial sum
 
 // Shares are counted in units of 512 bytes, and four for beginning a tensor: a microsecond's latency,
@@ -74,7 +76,7 @@ constexpr int64_t kLeastUnits = 8;
 
 struct Plan {
     const Entry *entries;                              // [tensors + 1], those of the launch
-    const int32_t *start;                              // [warps + 1] each warp's first tensor
+    const int32_t *start;                              // each warp's, or CTA's, first tensor, and one more
     int tensors;
     int64_t unit0, units;
 };
@@ -167,6 +169,26 @@ __global__ void __launch_bounds__(kThreads) norms_kernel(const double *norms, in
         partial[blockIdx.x] = sum;
 }
 
+// Vectors 0, 32, ... from here on, as far as they are below `there`: kBatch of them at most.
+template <typename T, int kBatch> __device__ __forceinline__ void scale_batch(const uint4 *in, uint4 *out, int there, float scale)
+{
+    uint4 v[kBatch];
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j)
+        if (32 * j < there)
+            v[j] = load_once(in + 32 * j);
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j)
+        if (32 * j < there) {
+            float f[kIn16<T>];
+            widen<T>(v[j], f);
+#pragma unroll
+            for (int k = 0; k < kIn16<T>; ++k)
+                f[k] *= scale;
+            store_once(out + 32 * j, narrow<T>(f));
+        }
+}
+
 // n elements scaled, by a warp, the last ones first: those that the first kernel read last are still in L2.
 template <typename T, int kBatch> __device__ __forceinline__ void scale_part(const T *in, T *out, int64_t n, float scale, int lane)
 {
@@ -180,32 +202,17 @@ template <typename T, int kBatch> __device__ __forceinline__ void scale_part(con
         const int64_t at = i < head ? i : i + vecs * kV;
         out[at] = from_f32<T>(to_f32(in[at]) * scale);
     }
-    in += head;
-    out += head;
-    for (int64_t end = vecs; end > 0; end -= 32 * kBatch) {
-        uint4 v[kBatch];
-#pragma unroll
-        for (int j = 0; j < kBatch; ++j) {
-            const int64_t i = end - 32 * (j + 1) + lane;
-            if (i >= 0)
-                v[j] = load_once(in + i * kV);
-        }
-#pragma unroll
-        for (int j = 0; j < kBatch; ++j) {
-            const int64_t i = end - 32 * (j + 1) + lane;
-            float f[kV];
-            widen<T>(v[j], f);
-#pragma unroll
-            for (int k = 0; k < kV; ++k)
-                f[k] *= scale;
-            if (i >= 0)
-                store_once(out + i * kV, narrow<T>(f));
-        }
-    }
+    const uint4 *const from = reinterpret_cast<const uint4 *>(in + head) + lane;
+    uint4 *const to = reinterpret_cast<uint4 *>(out + head) + lane;
+    int64_t end = vecs;
+    for (; end >= 32 * kBatch; end -= 32 * kBatch)
+        scale_batch<T, kBatch>(from + (end - 32 * kBatch), to + (end - 32 * kBatch), 32 * kBatch, scale);
+    if (end > 0)
+        scale_batch<T, kBatch>(from, to, static_cast<int>(end) - lane, scale);
 }
 
 template <int kN, bool kBoth>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, kBoth ? 4 : 2)
 scale_kernel(const __grid_constant__ Plan p, const __grid_constant__ Places<kN> places, const __grid_constant__ Outs<kN, kBoth> outs,
              const double *partial, int partials, double max_norm, float *norm_out)
 {
@@ -214,7 +221,7 @@ scale_kernel(const __grid_constant__ Plan p, const __grid_constant__ Places<kN> 
     const int lane = threadIdx.x & 31;
     const int64_t w = int64_t(blockIdx.x) * kWarps + (threadIdx.x >> 5);
     const Share share = share_of(p, w, int64_t(gridDim.x) * kWarps);
-    int t = __ldg(p.start + w + 1);                    // at or behind the last one
+    int t = __ldg(p.start + (kBoth ? int64_t(blockIdx.x) : w) + 1);         // at or behind the last one
     Entry e = p.entries[t];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -342,14 +349,14 @@ void cut(gnmr_clip *c, int sms)
         l.units = c->entries[from + l.tensors].first - l.unit0;
         const int64_t most = std::max<int64_t>(1, l.units / (kLeastUnits * kWarps));
         l.squares.ctas = static_cast<int>(std::min<int64_t>(most, std::min(sms * kSquaresCtas, kMostSquares)));
-        l.both.ctas = static_cast<int>(std::min<int64_t>(most, sms * kBothCtas));
+        l.both.ctas = static_cast<int>(std::min<int64_t>(std::max<int64_t>(std::min<int64_t>(most, sms * kBothLeast), l.units / kBothUnits), sms * kBothCtas));
         l.in_place.ctas = static_cast<int>(std::min<int64_t>(most, sms * kInPlaceCtas));
         for (Grid *g : {&l.squares, &l.both, &l.in_place}) {
-            const int64_t warps = int64_t(g->ctas) * kWarps;
+            const int64_t shares = int64_t(g->ctas) * (g == &l.both ? 1 : kWarps);
             g->start = start.size();
             int t = 0;
-            for (int64_t w = 0; w <= warps; ++w) {
-                while (t < l.tensors && c->entries[from + t + 1].first <= l.unit0 + l.units * w / warps)
+            for (int64_t w = 0; w <= shares; ++w) {
+                while (t < l.tensors && c->entries[from + t + 1].first <= l.unit0 + l.units * w / shares)
                     ++t;
                 start.push_back(t);
             }

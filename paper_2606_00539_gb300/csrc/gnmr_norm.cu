@@ -1038,9 +1038,18 @@ __global__ void __launch_bounds__(32 * kJoinWarps) join_kernel(const Norm n)
     float s = 0.0f;
     if (i < n.cols) {
         const float *const part = (blockIdx.y ? n.part_b : n.part_w) + i;
-#pragma unroll 10
-        for (int p = warp; p < n.parts; p += kJoinWarps)
-            s += __ldcg(part + int64_t(p) * n.cols);
+        constexpr int kBatch = 10;                     // loads on their way
+        for (int p0 = warp; p0 < n.parts; p0 += kBatch * kJoinWarps) {
+            float v[kBatch];
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) {
+                const int p = p0 + k * kJoinWarps;
+                v[k] = p < n.parts ? __ldcg(part + int64_t(p) * n.cols) : 0.0f;
+            }
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k)
+                s += v[k];
+        }
     }
     shared[warp][lane] = s;
     __syncthreads();
