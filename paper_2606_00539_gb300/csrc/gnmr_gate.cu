@@ -1,6 +1,7 @@
 // The gated blocks' element-wise halves: h = act(a) b where the projections come from the
 // 8-bit product, and the gradient of [a, b] from that of h.  Bound by memory: 6 and 10 bytes
-// an element of h, each read or written once.
+// an element of h, each read or written once.  49,152 x 1408 bf16: 59.7 us and 98.5, 7.0 TB/s, 1.03 of a plain copy's rate
+// (gelu's gradient 105); rows at odd starts, by elements, 5,003 x 1003: 15 and 16 us, 2.0 and 3.2 TB/s.
 #include <algorithm>
 #include <cstdint>
 #include <type_traits>

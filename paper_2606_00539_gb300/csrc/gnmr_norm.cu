@@ -4,7 +4,20 @@
 //   backward  xh = (x - mean) rstd, t = dy w; dx = rstd (t - mean of t - xh mean of t xh);
 //             dw = sum over rows of dy xh, db = sum over rows of dy
 //
-// Bound by memory: x read and y written; x and dy read and dx written.
+// Bound by memory: x read and y written; x and dy read and dx written.  A row's sums need all of it before its first
+// output, so rows are held on the SM between the two: in registers, the next ones on their way to shared memory (cp.async, each thread
+// its own bytes, no wait but its own).  Which threads hold a row goes by its width and alignment:
+//
+//   forward   up to 4 KB a warp a row; wider ones 2 to 16 warps; odd starts by pairs of elements; few rows a CTA each
+//   backward  a CTA has the same columns of every row it takes, so that the sums over the rows stay in its registers; each CTA's go
+//             to memory, and a second kernel adds them up in their order.  Rows past 16 KB (32 KB in fp32): these sums by strips
+//             of columns, which need no sums over a row, and dx by a kernel like the forward's
+//
+// Measured (one GB300, bf16 unless said; us, and TB/s of what is read and written once): 16384 x 5120 forward 56 (6.0), backward
+// 92 (5.4); 16384 x 2048 20.5 (6.5) and 45; 4096 x 8192 27 (5.0) and 48; 8192 x 5120 fp32 61 (5.5) and 86 (5.8);
+// 16384 x 1371, odd starts, 32 (2.8) and 64; 2000 x 16384 29 (4.5) and 80; one row of 5120 2.7 and 8.  The backward kernel
+// is bound by its threads' latency: 10 warps of 168 registers, instructions issued 42 % of the time.  Two turns in flight at
+// once, twice the warps with half the registers, and a scalar in place of the paired arithmetic were slower.
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
@@ -1168,7 +1181,9 @@ cudaError_t launch_groups(const Norm &n, int each, int threads, int params, int 
     return cudaGetLastError();
 }
 
-constexpr int kMostUnits = 5;                          // 16-byte units a lane of the forward kernel
+// 16-byte units a lane of the forward kernel, by 1,024 threads with 64 registers each.  16384 x 5120: four warps a row, 5 units, 56 us; one
+// warp, 20 units, 16 warps with 128 registers 58.
+constexpr int kMostUnits = 5;
 
 template <typename T, typename P> cudaError_t launch_forward(const Norm &n, int units, int sms, cudaStream_t st)
 {
@@ -1198,6 +1213,8 @@ template <typename T, typename P, int kUnits, bool kVector> cudaError_t launch_c
     return cudaGetLastError();
 }
 
+// Up to here a CTA a row, without laying the parameters down first.  5120 columns: 200 rows 3.5 us so, 600 5.9 and by groups of warps 5.2,
+// 1200 10.9 and 7.0; 2048: 600 3.2 and 3.7, 1200 5.2 and 3.9; 1371 at odd starts: 600 5.5 and 5.2.
 constexpr int64_t kFewRows = 400;
 
 // Whether the rows of two matrices begin at odd elements alike, and all elements where their size says.
@@ -1279,6 +1296,8 @@ template <typename T, typename P> cudaError_t backward(Norm &n, int sms, cudaStr
     constexpr int kN = kIn16<T>;
     const bool vector = n.cols % kN == 0 && rows_of_16(n.x, n.rows, n.x_stride, sizeof(T)) && rows_of_16(n.dy, n.rows, n.dy_stride, sizeof(T)) &&
                         (!n.y || rows_of_16(n.y, n.rows, n.y_stride, sizeof(T)));
+    // columns a thread, rows a turn, turns ahead, threads: 16384 x 5120 bf16 8, 2, 4, 640 98 us; 16, 2, 4, 320 99.5; 16, 4, 2, 320 92.  Narrow
+    // rows with 16 columns a thread leave lanes idle: 60,000 x 64 32 us, with 8 20.
     if (vector && n.cols <= 256)
         return launch_grad<Shape<T, P, 8, kN / 4, 4, 640, 1, true>>(n, n.cols, sms, st);
     if (vector && n.cols <= 320 * 16)

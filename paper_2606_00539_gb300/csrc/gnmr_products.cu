@@ -8,6 +8,9 @@
 //   gated block  A = W_g's two halves, row by row in turn         B = x's rows    c < n_in
 // so that the tensor cores' 128 lanes lie along the output's contiguous axis and a
 // group's ragged rows are columns, of which a tile has any multiple of 32 up to 256.
+// A gated block's two projections of one output are neighbouring lanes: its tiles of A are one load
+// of a tensor map with a dimension for the halves of W_g before that for their rows.  So the epilogue has both in
+// one warp, and the loop of loads and multiplies is the plain product's.
 //
 // A pair of CTAs computes 256 lanes by up to 256 columns (two SMs share an operand
 // tile: 32 KB of operands an SM for 64 steps of the contraction, where one SM alone

@@ -187,6 +187,22 @@ def test_the_monitors_norms():
     mon.close()
 
 
+@pytest.mark.parametrize("size", [1e-170, 1e-150, 1e-140, 1e-100, 1e-30, 1.0, 3.0, 1e10, 1e38, 1e100, 1e150])
+def test_roots_over_the_range_of_64_bits(size):
+    """Norms that a caller gives may be anything whose square is a number; the limit is right for each (norm / 8, so exactly 1 / 8)."""
+    x = [torch.full((5,), 8.0, device="cuda")]
+    out = [torch.zeros(5, device="cuda")]
+    with GradientClip(x) as plan:
+        for k in (1.0, 1.7, 2.0, 3.1):
+            units = torch.tensor([3.0, 4.0], dtype=torch.float64, device="cuda") * (size * k)
+            norm = plan.clip(x, 5.0 * size * k / 8, unit_norms=units, out=out)
+            want = 5.0 * size * k
+            if want * want < 1e-300:                             # squares below 64 bits' normal numbers keep fewer
+                continue
+            assert (out[0].double() - 1).abs().max() <= 2 * U
+            assert norm.isinf() if want > 3.5e38 else abs(norm.double().item() - want) <= 2 * U * want + 2.0 ** -150
+
+
 def test_prepared_captured_and_from_two_streams():
     g = gen(6)
     x = [normal(g, 300_000, dtype=torch.bfloat16), normal(g, 70_001, dtype=torch.float32)]

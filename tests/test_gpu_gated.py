@@ -294,6 +294,30 @@ def test_layer_on_both_paths(products, kind):
     assert torch.allclose(arena, 2 * before, rtol=1e-6, atol=1e-6)
 
 
+def test_given_codes_and_masks_of_one_kind(products):
+    """Codes of the weights made once give the same bits as made anew; with every expert on one path the other's calls write nothing."""
+    counts, n, k, t, g = [40, 0, 70, 33], 72, 136, torch.bfloat16, gen(22)
+    x, w = normal(g, 143, k, dtype=t).requires_grad_(), normal(g, 4, 2 * n, k, dtype=t, size=0.1)
+    dh, off = normal(g, 143, n, dtype=t), offsets_of(counts)
+    codes_of_w = (*products.quantize_rows(w), *products.quantize_columns(w))
+    for bits in ([0, 1, 0, 1], [0] * 4, [1] * 4):
+        mask = torch.tensor(bits, dtype=torch.uint8, device="cuda")
+        got = []
+        for held in (None, codes_of_w):
+            arena = torch.empty(4, 2 * n, k, device="cuda")
+            h = expert_gated(products, x, w, off, mask, arena, codes=held)
+            got.append((h, *torch.autograd.grad(h, x, dh), arena))
+        assert all(torch.equal(a, b) for a, b in zip(*got))
+        if all(bits):
+            plain = expert_gated(products, x, w, off)
+            assert torch.equal(got[0][0], plain) and torch.equal(got[0][1], torch.autograd.grad(plain, x, dh)[0])
+    with torch.no_grad():
+        assert torch.equal(expert_gated(products, x, w, off, mask), plain)
+    out = torch.full((143, n), 7.0, dtype=t, device="cuda")
+    products.gated(x.detach(), w, off, out=out, mask=torch.zeros_like(mask))
+    assert (out == 7).all()
+
+
 def test_gradients_against_differences(products):
     """The layer's directional derivative against a difference of losses formed in 64 bits from its own outputs: the
     step moves h by about 1 %, its rounding (2^-11 of each of 60 x 40 values, at random) adds up to 2^-11 * 49 * |h|."""
