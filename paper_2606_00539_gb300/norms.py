@@ -69,15 +69,11 @@ class LayerNorm:
 
     def _params(self, weight, bias, dtype, cols):
         """The parameters' type, and where they are."""
-        kind = dtype
-        if weight is not None:
-            kind = weight.dtype
-            if bias is not None and bias.dtype != kind and kind in (dtype, torch.float32):
-                raise ValueError("weight and bias must be of one type")
-        elif bias is not None:
-            kind = bias.dtype
         kinds = (dtype, torch.float32)
         w, b = self._vector(weight, "weight", cols, kinds), self._vector(bias, "bias", cols, kinds)
+        kind = dtype if weight is None and bias is None else bias.dtype if weight is None else weight.dtype
+        if weight is not None and bias is not None and bias.dtype != kind:
+            raise ValueError("weight and bias must be of one type")
         return _DTYPES[kind], w, b
 
     @staticmethod
