@@ -62,10 +62,14 @@ constexpr int kBlock = 64 * 128;                       // bytes of a tile of 64 
 // The epilogue's warps and the registers that the warpgroups share out between them, out of what the
 // block is launched with.  A weight gradient's contraction is short, so that it is bound by its
 // epilogue: 16 warps of 64 columns each (12288 rows, 64 fp32 gradients of 1408 x 2048: 8 warps 156 us,
-// 16 141); the others 8 of 128, with which 16 made no difference.  The 16 warps' 104 registers do not hold
-// the 64 sums beside what addresses them: about 300 bytes a thread are spilled.
+// 16 141).  So is a gated block of a short contraction, whose warps read two sums, take an exponential
+// and store three numbers for each output (49152 rows, 64 x 1408 features, the projections kept: of 256 steps
+// 189 us with 8 warps and 152 with 16, of 1024 235 and 217, of 2048, at the power limit, 355 to 413 and 356 to
+// 403; 12000 rows, 24 x 1003, of 2048 steps 107 and 89; 3000 rows, 8 x 2048, of 4096 72 and 73.5).  The others have
+// 8 warps of 128, with which 16 made no difference.  The 16 warps' 104 registers do not hold the 64 sums beside
+// what addresses them: about 300 bytes a thread of a weight gradient are spilled, about 110 of a gated block.
 template <int kOp> struct Roles {
-    static constexpr int kSides = kOp == GNMR_PRODUCT_WEIGHT_GRAD ? 4 : 2;
+    static constexpr int kSides = kOp == GNMR_PRODUCT_WEIGHT_GRAD || kOp == kGated ? 4 : 2;
     static constexpr int kThreads = 32 * (kFirstEpilogueWarp + 4 * kSides);
     static constexpr int kLaunchRegisters = kSides == 4 ? 96 : 168;
     static constexpr int kControlRegisters = kSides == 4 ? 64 : 72, kEpilogueRegisters = kSides == 4 ? 104 : 216;

@@ -397,8 +397,8 @@ __device__ __forceinline__ void finish(const Product &p, const Item &it, uint32_
 // two outputs of one column.  A warp's outputs of a column are 32 contiguous bytes: whole sectors, which L2 puts together.
 // h costs an exchange and an activation (two special-function operations) for each of 128 sums a thread, hidden
 // behind the next tile's multiplies: 49,152 rows of 64 x 1408 x 2048 take 330 us (1.7 PFLOP/s) where the plain product of
-// both projections takes 345 to 385; the projections kept as well, 277 MB more, 372 to 413.  With a predicate at every store
-// they took 438; with 16 epilogue warps of half the columns 387.
+// both projections takes 345 to 385; the projections kept as well, 277 MB more, 356 to 413.  With a predicate at every store
+// they took 438.
 template <int kPieces, int kType, int kAct>
 __device__ __forceinline__ void finish_gated(const Product &p, const Item &it, uint32_t (&acc)[kPieces][16], int lane, int col, int span)
 {
