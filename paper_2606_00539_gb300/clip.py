@@ -96,6 +96,10 @@ class GradientClip:
         written = [p for p, n in zip(at if to is None else to, self._lengths) if n]
         if len(set(written)) != len(written):
             raise ValueError("the same memory is written twice: no two of the tensors may overlap")
+        if to is not None and not set(written).isdisjoint(at):   # a gradient may be written where it lies, not where another one does
+            own = {p: q for p, q, n in zip(to, at, self._lengths) if n}
+            if any(own.get(p, p) != p for p, n in zip(at, self._lengths) if n):
+                raise ValueError("out must not be where another gradient lies")
         units, count = None, 0
         if unit_norms is not None:
             if not isinstance(unit_norms, torch.Tensor) or unit_norms.get_device() != self.device_index or \
@@ -130,7 +134,7 @@ class GradientClip:
         """Enqueues one pass and returns the norm before scaling, an fp32 tensor (`norm`, if given).
 
         grads: tensors of the plan's sizes and types, no two of which overlap, scaled where they lie, or, with out (as many, of the same types), left as
-        they are and written there, scaled or not.  max_norm: 0 or more; infinity only takes the norm.
+        they are and written there, scaled or not (out[i] may be grads[i], and overlaps no other).  max_norm: 0 or more; infinity only takes the norm.
         unit_norms: fp64 tensor of the norms of parts that make up the gradients, as the monitor's stats["norm"]
         after a step on the same arena: the norm is formed from them, and no gradient is read for it."""
         return self.prepare_clip(grads, max_norm, out=out, unit_norms=unit_norms, norm=norm, stream=stream)()

@@ -272,6 +272,23 @@ def test_offsets_past_31_bits():
     assert norm.item() == 7.0 and (x[-3:] == 2.0).all() and x[0] == 0.5 and x[n // 2] == 0
 
 
+def test_outputs_where_gradients_lie():
+    """out[i] may be grads[i]; where it is another gradient, which is still to be read, the call is refused."""
+    g = torch.Generator(device="cuda").manual_seed(5)
+    x = [torch.randn(5000, device="cuda", generator=g) for _ in range(3)]
+    was = [t.clone() for t in x]
+    with GradientClip(x) as plan:
+        other = torch.empty_like(x[0])
+        for out in ([x[1], x[0], x[2]], [x[0], x[2], other], [other, x[1], x[0]]):
+            with pytest.raises(ValueError, match="another gradient"):
+                plan.clip(x, 1.0, out=out)
+        assert all(torch.equal(a, b) for a, b in zip(x, was))
+        norm = plan.clip(x, 1.0, out=[x[0], other, x[2]])
+        coef = torch.tensor(1.0, device="cuda") / norm           # half steps: the norm, the division and the product here, the last two there
+        assert all(torch.allclose(a, b * coef, rtol=6 * 2.0 ** -24, atol=0) for a, b in zip((x[0], other, x[2]), was))
+        assert torch.equal(x[1], was[1])
+
+
 def test_refusals():
     x = [torch.zeros(10, device="cuda"), torch.zeros(4, dtype=torch.bfloat16, device="cuda")]
     for tensors in ([x[0].double()], [3], [x[0].int()]):
