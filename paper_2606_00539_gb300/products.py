@@ -280,9 +280,13 @@ class ExpertProducts:
         _, rows, both, step, _ = self._matrix(ab, "ab", (2,), self._sixteen)
         if both % 2:
             raise ValueError(f"ab must have the columns of two projections, got {both}")
-        if offsets is None and mask is not None and mask.numel() != 1:
-            raise ValueError("offsets may be None for one group only")
-        groups = 1 if offsets is None else offsets.numel() - 1
+        if offsets is None:
+            if isinstance(mask, torch.Tensor) and mask.numel() != 1:
+                raise ValueError("offsets may be None for one group only")
+            groups = 1
+        else:
+            self._tensor(offsets, "offsets", (1,), (torch.int64,))
+            groups = offsets.numel() - 1
         at, bits, each = self._grouping(groups, offsets, mask)
         self._no_graph(ab)
         out, across = self._out(out, rows, both // 2, (ab.dtype,), stream)

@@ -371,3 +371,13 @@ def test_refusals(products):
     ]:
         with pytest.raises(ValueError, match=why):
             call()
+
+
+def test_gate_refuses_what_is_no_tensor(products):
+    ab = torch.zeros(6, 8, dtype=torch.bfloat16, device="cuda")
+    for call, why in [
+        (lambda: products.gate(ab, mask=[0]), "mask must"), (lambda: products.gate(ab, [0, 6]), "offsets must"),
+        (lambda: products.gate(ab, torch.tensor([0, 6])), "offsets must"), (lambda: products.gate(ab, torch.tensor([0., 6.]).cuda()), "offsets must"),
+    ]:
+        with pytest.raises(ValueError, match=why):
+            call()
