@@ -10,6 +10,33 @@ from . import products as P
 torch = None                                       # loaded with the first GradientClip
 
 
+def _refuse_overlaps(at, to, norm, sizes):
+    """A call's warps go in no order: memory that is written twice, or written where another tensor is still to be read, would
+    get values that go by timing.  at, to: where the gradients and the outputs begin (to None: scaled where they lie); norm: where a
+    given norm is, or None; sizes: bytes."""
+    import numpy as np
+    size = np.array(sizes, dtype=np.int64)
+    there = size > 0
+    size = size[there]
+    reads = np.frombuffer(at, dtype=np.int64)[there] if sizes else size
+    first = reads if to is None else np.frombuffer(to, dtype=np.int64)[there] if sizes else size
+    end = first + size
+    if norm is not None:
+        first, end = np.append(first, norm), np.append(end, norm + 4)
+    order = np.argsort(first)
+    first, end = first[order], end[order]
+    if (first[1:] < end[:-1]).any():
+        raise ValueError("the same memory is written twice: no two of the tensors may overlap")
+    if to is not None and len(reads):
+        # the first written range that ends behind a gradient's beginning: its own output there and nothing else
+        k = np.searchsorted(end, reads, side="right")
+        met = k < len(first)
+        k[~met] = 0
+        met &= first[k] < reads + size
+        if (met & ((order[k] != np.arange(len(reads))) | (first[k] != reads))).any():
+            raise ValueError("out must not be where another gradient lies")
+
+
 class GradientClip:
     """The norm over many gradients, and the gradients scaled down to a limit:
     norm = sqrt(sum of x^2 over all of them), and where norm > max_norm every element times max_norm / norm.
@@ -35,6 +62,7 @@ class GradientClip:
             bad = next(i for i, t in enumerate(tensors) if not isinstance(t, torch.Tensor) or t.dtype not in P._DTYPES)
             raise ValueError(f"tensor {bad} must be a tensor of {' or '.join(str(d) for d in P._DTYPES)}")
         self._lengths, self._dtypes = [t.numel() for t in tensors], [t.dtype for t in tensors]
+        self._bytes = [t.numel() * t.element_size() for t in tensors]
         self._h = N.gnmr_clip_create(self._lengths, [P._DTYPES[d] for d in self._dtypes], self.device_index)
         self._table = torch.from_numpy(N.gnmr_clip_table(self._h)).to(self._device)
         self._made_on = torch._C._cuda_getCurrentRawStream(self.device_index)
@@ -93,23 +121,21 @@ class GradientClip:
             raise ValueError(f"max_norm must be 0 or more, got {max_norm}")
         grads, at = self._places(grads, "grads")
         outs, to = (None, None) if out is None else self._places(out, "out")
-        written = [p for p, n in zip(at if to is None else to, self._lengths) if n]
-        if len(set(written)) != len(written):
-            raise ValueError("the same memory is written twice: no two of the tensors may overlap")
-        if to is not None and not set(written).isdisjoint(at):   # a gradient may be written where it lies, not where another one does
-            own = {p: q for p, q, n in zip(to, at, self._lengths) if n}
-            if any(own.get(p, p) != p for p, n in zip(at, self._lengths) if n):
-                raise ValueError("out must not be where another gradient lies")
         units, count = None, 0
         if unit_norms is not None:
             if not isinstance(unit_norms, torch.Tensor) or unit_norms.get_device() != self.device_index or \
                     unit_norms.dtype != torch.float64 or not unit_norms.is_contiguous():
                 raise ValueError(f"unit_norms must be a contiguous fp64 tensor on device {self.device_index}")
+        given = None
         if norm is None:
             norm = self._new((), torch.float32, stream)
         elif not isinstance(norm, torch.Tensor) or norm.get_device() != self.device_index or norm.dtype != torch.float32 or \
                 norm.numel() != 1:
             raise ValueError(f"norm must be one fp32 element on device {self.device_index}")
+        else:
+            given = norm.data_ptr()
+        if given or to is not None or len(grads) > 1:
+            _refuse_overlaps(at, to, given, self._bytes)
         scratch = self._new(self._scratch_bytes, torch.uint8, stream)
         if unit_norms is not None:                 # (an empty tensor has no address)
             units, count = unit_norms.data_ptr() or scratch.data_ptr(), unit_norms.numel()
@@ -134,7 +160,8 @@ class GradientClip:
         """Enqueues one pass and returns the norm before scaling, an fp32 tensor (`norm`, if given).
 
         grads: tensors of the plan's sizes and types, no two of which overlap, scaled where they lie, or, with out (as many, of the same types), left as
-        they are and written there, scaled or not (out[i] may be grads[i], and overlaps no other).  max_norm: 0 or more; infinity only takes the norm.
+        they are and written there, scaled or not (out[i] may be grads[i], and overlaps no other).  Tensors that
+        overlap otherwise, or a `norm` among them, are refused.  max_norm: 0 or more; infinity only takes the norm.
         unit_norms: fp64 tensor of the norms of parts that make up the gradients, as the monitor's stats["norm"]
         after a step on the same arena: the norm is formed from them, and no gradient is read for it."""
         return self.prepare_clip(grads, max_norm, out=out, unit_norms=unit_norms, norm=norm, stream=stream)()

@@ -306,3 +306,18 @@ def test_refusals():
         ]:
             with pytest.raises(ValueError, match=why):
                 call()
+
+
+def test_tensors_that_overlap_are_refused_and_left_as_they_are():
+    flat, to = torch.ones(64, device="cuda"), torch.ones(64, device="cuda")
+    with GradientClip([flat[:10], flat[:10]]) as plan:
+        for grads, out, why in (([flat[0:10], flat[5:15]], None, "twice"), ([flat[0:10], flat[20:30]], [to[0:10], to[9:19]], "twice"),
+                                ([flat[0:10], flat[20:30]], [flat[40:50], flat[9:19]], "another gradient")):
+            with pytest.raises(ValueError, match=why):
+                plan.clip(grads, 1.0, out=out)
+        with pytest.raises(ValueError, match="twice"):
+            plan.clip([flat[0:10], flat[10:20]], 1.0, norm=flat[19])
+        assert (flat == 1).all() and (to == 1).all()
+        norm = plan.clip([flat[10:20], flat[0:10]], 1.0, norm=flat[20])                # neighbours
+        assert norm.item() == flat[20].item() and abs(norm.item() - 20 ** 0.5) <= 18 * U * 20 ** 0.5
+        assert (flat[21:] == 1).all() and ((flat[:20].double() - 20 ** -0.5).abs() <= 20 * U).all()
