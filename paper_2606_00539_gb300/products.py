@@ -186,8 +186,8 @@ class ExpertProducts:
 
     # -- 16-bit products ------------------------------------------------------
     @staticmethod
-    def _no_graph(*operands):
-        if any(t.requires_grad for t in operands) and torch.is_grad_enabled():
+    def _no_graph(a, b=None):
+        if (a.requires_grad or (b is not None and b.requires_grad)) and torch.is_grad_enabled():
             raise ValueError("autograd records nothing of a product: use expert_linear or expert_gated, or detach() or torch.no_grad()")
 
     def forward(self, x, w, offsets=None, *, out=None, mask=None, stream=None):
