@@ -613,7 +613,8 @@ typedef struct gnmr_norm {
 gnmr_status gnmr_layer_norm(const gnmr_norm *p, void *stream);
 gnmr_status gnmr_layer_norm_grad(const gnmr_norm *p, void *stream);
 
-/* Scratch that gnmr_layer_norm_grad needs for *p on any device.  Makes no CUDA call. */
+/* Scratch that gnmr_layer_norm_grad needs for *p on any device: up to 8 bytes for each column and each of rows + 1, of which
+ * it counts 512 at most; more rows of a width need no less.  Makes no CUDA call. */
 gnmr_status gnmr_layer_norm_scratch_bytes(const gnmr_norm *p, int64_t *bytes);
 
 /* ---- The norm over many gradients, and clipping --------------------------------

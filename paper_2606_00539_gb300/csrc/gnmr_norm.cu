@@ -1084,9 +1084,13 @@ gnmr_status fail(gnmr_status s, const char *why)
     return s;
 }
 
+// The parts that any kernel makes of so many rows: a row each at most, and where every second row starts alike the odd and the
+// even ones' parts are as many, one more than the rows where these are odd.
+int64_t most_parts(int64_t rows) { return rows ? std::min<int64_t>(rows + 1, kMostParts) : 0; }
+
 int64_t parts_bytes(const gnmr_norm *p)
 {
-    return p->d_dweight || p->d_dbias ? (2 * int64_t(kMostParts) * p->cols * 4 + 255) / 256 * 256 : 0;
+    return p->d_dweight || p->d_dbias ? (2 * most_parts(p->rows) * p->cols * 4 + 255) / 256 * 256 : 0;
 }
 
 gnmr_status check(const gnmr_norm *p, bool grad)
@@ -1363,8 +1367,8 @@ gnmr_status gnmr_layer_norm_scratch_bytes(const gnmr_norm *p, int64_t *bytes)
     if (!bytes || !p)
         return fail(GNMR_ERR_INVALID_ARG, "layer norm: NULL argument");
     *bytes = 0;
-    if (p->cols < 1 || p->cols > int64_t(1) << 30)
-        return fail(GNMR_ERR_INVALID_ARG, "layer norm: cols out of range");
+    if (p->rows < 0 || p->rows > INT32_MAX || p->cols < 1 || p->cols > int64_t(1) << 30)
+        return fail(GNMR_ERR_INVALID_ARG, "layer norm: rows or cols out of range");
     *bytes = parts_bytes(p);
     return GNMR_OK;
 }
@@ -1388,7 +1392,7 @@ gnmr_status gnmr_layer_norm_grad(const gnmr_norm *p, void *stream)
     n.db = p->d_dbias;
     n.add = p->add;
     n.part_w = static_cast<float *>(p->d_scratch);
-    n.part_b = n.part_w + int64_t(kMostParts) * n.cols;
+    n.part_b = n.part_w + most_parts(n.rows) * n.cols;
     cudaError_t e = cudaSuccess;
     if (n.rows > 0)
         e = by_type(p->dtype, [&](auto v) { return by_params<decltype(v)>(p, n, true, sms, st); });

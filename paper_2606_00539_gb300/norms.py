@@ -150,9 +150,10 @@ class LayerNorm:
         p = N.gnmr_norm(rows, cols, _DTYPES[dtype], kind, 0.0, x.data_ptr(), step, w, None, m, r, None, 0, dy.data_ptr(), apart,
                         at, across, to_w, to_b, grads, bool(add))
         if rows and (to_w or to_b):
-            need = self._scratch.get(cols)         # it goes by the width alone
-            if need is None:
-                need = self._scratch[cols] = N.gnmr_layer_norm_scratch_bytes(p)
+            of, need = self._scratch.get(cols, (0, 0))           # of the rows that this width was last called with
+            if of != rows:
+                need = N.gnmr_layer_norm_scratch_bytes(p)
+                self._scratch[cols] = rows, need
             scratch = self._new(need, torch.uint8, stream)
             p.scratch_bytes = need
             p.d_scratch = scratch.data_ptr()

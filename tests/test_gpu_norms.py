@@ -338,3 +338,40 @@ def test_refusals(norms):
     for eps in (-1.0, float("nan"), float("inf")):
         with pytest.raises(GnmrError, match="eps"):
             norms.forward(x.detach(), eps=eps)
+
+
+@pytest.mark.parametrize("rows", [1, 2, 3, 4, 5, 7])
+@pytest.mark.parametrize("cols", [777, 1371, 5120, 9001, 16384, 40001])
+def test_scratch_of_few_rows(norms, rows, cols):
+    """Scratch for so many rows' parts: it is enough, and nothing behind it is written."""
+    import ctypes
+
+    from paper_2606_00539_gb300 import _native as N
+    g = gen(rows + cols)
+    x, dy = (normal(g, rows, cols, dtype=torch.bfloat16) for _ in range(2))
+    _, mean, rstd = norms.forward(x)
+    dw, db = torch.empty(2, cols, device="cuda").unbind()
+    dx = torch.empty_like(x)
+    p = N.gnmr_norm(rows, cols, N.GNMR_DTYPE_BF16, N.GNMR_DTYPE_F32, 0.0, x.data_ptr(), cols, None, None, mean.data_ptr(), rstd.data_ptr(), None, 0,
+                    dy.data_ptr(), cols, dx.data_ptr(), cols, dw.data_ptr(), db.data_ptr(), N.GNMR_DTYPE_F32, 0)
+    need = N.gnmr_layer_norm_scratch_bytes(p)
+    scratch = torch.full((need + (1 << 20),), 77, dtype=torch.uint8, device="cuda")
+    p.d_scratch, p.scratch_bytes = scratch.data_ptr(), need
+    assert N.load().gnmr_layer_norm_grad(ctypes.addressof(p), torch.cuda.current_stream().cuda_stream) == N.GNMR_OK
+    check_backward(dx, dw, db, dy, x, None, mean, rstd, "bf16", "f32")
+    assert (scratch[need:] == 77).all()
+
+
+def test_a_row_of_millions_of_columns(norms):
+    """The backward pass of a few very wide rows takes memory by the rows: 4 KB a column would be 69 GB here."""
+    rows, cols = 3, 1 << 24
+    g = gen(11)
+    x, dy = (normal(g, rows, cols, dtype=torch.bfloat16) for _ in range(2))
+    xd = x.double()
+    mean, rstd = xd.mean(1).float(), (xd.var(1, unbiased=False) + 1e-5).rsqrt().float()
+    dw, db = torch.empty(2, cols, device="cuda").unbind()
+    torch.cuda.reset_peak_memory_stats()
+    before = torch.cuda.memory_allocated()
+    dx = norms.backward(dy, x, None, mean, rstd, weight_grad=dw, bias_grad=db)
+    assert torch.cuda.max_memory_allocated() - before <= rows * cols * 2 + 2 * (rows + 1) * cols * 4 + (4 << 20)
+    check_backward(dx, dw, db, dy, x, None, mean, rstd, "bf16", "f32")
