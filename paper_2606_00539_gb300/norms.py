@@ -56,7 +56,7 @@ class LayerNorm:
         step, one = t.stride()
         if one != 1 and cols > 1:
             raise ValueError(f"{name} must have contiguous rows")
-        return rows, cols, step if rows > 1 else max(step, cols)
+        return rows, cols, step if rows > 1 else cols    # a single row has no stride, and torch may give it any
 
     def _vector(self, t, name, n, dtypes):
         if t is None:
