@@ -201,7 +201,8 @@ template <bool kGrad> gnmr_status run(const Gate &g, int32_t dtype, int32_t act,
     if (g.gu_stride < wide || g.out_stride < (kGrad ? wide : g.n) || (kGrad && g.dh_stride < g.n) ||
         (g.mask && g.groups > 1 && g.mask_stride < 1))
         return fail(GNMR_ERR_LAYOUT, "gate: a stride below what it strides over");
-    if (g.gu_stride > far || g.out_stride > far || g.dh_stride > far)
+    // (a single row has no stride)
+    if (g.rows > 1 && (g.gu_stride > far || g.out_stride > far || g.dh_stride > far))
         return fail(GNMR_ERR_LAYOUT, "gate: a stride above 2^31 elements");
     if (g.rows == 0)
         return GNMR_OK;
@@ -209,7 +210,7 @@ template <bool kGrad> gnmr_status run(const Gate &g, int32_t dtype, int32_t act,
         return fail(GNMR_ERR_INVALID_ARG, "gate: NULL pointer");
     if (misaligned(g.gu, 2) || misaligned(g.out, 2) || misaligned(g.dh, 2) || misaligned(g.offsets, 8))
         return fail(GNMR_ERR_LAYOUT, "gate: a buffer not aligned to its element size");
-    if (kGrad && g.out == g.gu && g.out_stride != g.gu_stride)
+    if (kGrad && g.rows > 1 && g.out == g.gu && g.out_stride != g.gu_stride)
         return fail(GNMR_ERR_LAYOUT, "gate: in place with another stride");
     int sms = 0;
     if (current_sms(&sms) != cudaSuccess) {

@@ -381,3 +381,39 @@ def test_gate_refuses_what_is_no_tensor(products):
     ]:
         with pytest.raises(ValueError, match=why):
             call()
+
+
+@pytest.mark.parametrize("kind", ["silu", "gelu"])
+def test_one_row_of_any_stride_in_place(products, kind):
+    g, n = gen(12), 136
+    ab, dh = normal(g, 4, 2 * n, dtype=torch.bfloat16), normal(g, 4, n, dtype=torch.bfloat16)
+    old, want = ab.clone(), products.gate_grad(dh, ab, activation=kind)
+    products.gate_grad(dh[::3][:1], ab[::2][:1], out=ab[:1], activation=kind)
+    assert torch.equal(ab[:1], want[:1]) and torch.equal(ab[1:], old[1:])
+
+
+@pytest.mark.parametrize("n", [24, 5])
+@pytest.mark.parametrize("groups", [31, 32, 33, 64, 70, 257, 2048])
+def test_gate_of_many_groups(products, groups, n):
+    """Groups' first rows are found 32 at a time: groups of none to four rows, ahead of the first and behind the last group rows of none,
+    every other group on the other path; offsets that fall are as in the products."""
+    rng, g = np.random.default_rng(groups), gen(groups)
+    counts, first = rng.integers(0, 5, groups).tolist(), 3
+    counts[groups // 2] = 0
+    R = sum(counts) + first + 4
+    ab = normal(g, R, 2 * n, dtype=torch.bfloat16)
+    mask = torch.from_numpy(rng.integers(0, 2, groups).astype(np.uint8)).cuda()
+    every = products.gate(ab)
+    off = offsets_of(counts, first)
+    out = torch.full((R, n), 7.0, device="cuda", dtype=torch.bfloat16)
+    products.gate(ab, off, out=out, mask=mask)
+    wanted = torch.zeros(R, dtype=torch.bool)
+    for e, at in spans(counts, first):
+        wanted[at] = not mask[e].item()
+    wanted = wanted.cuda()
+    assert torch.equal(out[wanted], every[wanted]) and (out[~wanted] == 7).all()
+    # one that falls in the middle is taken as the largest before it: its group is empty, and the next one begins there
+    off[groups // 2] = 0
+    out.fill_(7.0)
+    products.gate(ab, off, out=out)
+    assert torch.equal(out[first:R - 4], every[first:R - 4]) and (out[:first] == 7).all() and (out[R - 4:] == 7).all()
