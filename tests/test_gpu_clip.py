@@ -321,3 +321,27 @@ def test_tensors_that_overlap_are_refused_and_left_as_they_are():
         norm = plan.clip([flat[10:20], flat[0:10]], 1.0, norm=flat[20])                # neighbours
         assert norm.item() == flat[20].item() and abs(norm.item() - 20 ** 0.5) <= 18 * U * 20 ** 0.5
         assert (flat[21:] == 1).all() and ((flat[:20].double() - 20 ** -0.5).abs() <= 20 * U).all()
+
+
+@pytest.mark.parametrize("gap", [0, 1, 8])
+@pytest.mark.parametrize("case", range(len(LAYOUTS)))
+def test_in_place_and_into_other_memory_give_the_same_bits(case, gap):
+    """The same norm, the same scale and one product for each element, whichever kernel's shares it falls in; and what lies between stays."""
+    lengths, kinds = LAYOUTS[case]
+    g = gen(case + 100 * gap + 7)
+    grads, flat = views(g, lengths, kinds, gap)
+    outs, _ = views(g, lengths, kinds, gap)
+    total = exact(grads)
+    was = {k: f.clone() for k, f in flat.items()}
+    with GradientClip(grads) as plan:
+        for limit in (0.25, 0.9, 1.5):
+            norm = plan.clip(grads, limit * total, out=outs)
+            at = plan.clip(grads, limit * total)
+            assert torch.equal(norm, at) and all(torch.equal(a, b) for a, b in zip(grads, outs))
+            for k, f in flat.items():
+                between = torch.ones(len(f), dtype=torch.bool, device="cuda")
+                for v in grads:
+                    if NAMES[v.dtype] == k:
+                        between[v.storage_offset():v.storage_offset() + len(v)] = False
+                assert torch.equal(f[between], was[k][between])
+                f.copy_(was[k])
