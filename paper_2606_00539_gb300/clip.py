@@ -3,6 +3,8 @@ libgnmr's kernels form the norm and scale the gradients."""
 from __future__ import annotations
 
 import ctypes
+from bisect import bisect_right
+from operator import add, gt
 
 from . import _native as N
 from . import products as P
@@ -14,26 +16,23 @@ def _refuse_overlaps(at, to, norm, sizes):
     """A call's warps go in no order: memory that is written twice, or written where another tensor is still to be read, would
     get values that go by timing.  at, to: where the gradients and the outputs begin (to None: scaled where they lie); norm: where a
     given norm is, or None; sizes: bytes."""
-    import numpy as np
-    size = np.array(sizes, dtype=np.int64)
-    there = size > 0
-    size = size[there]
-    reads = np.frombuffer(at, dtype=np.int64)[there] if sizes else size
-    first = reads if to is None else np.frombuffer(to, dtype=np.int64)[there] if sizes else size
-    end = first + size
+    if 0 in sizes:
+        at, to, sizes = ([v for v, n in zip(of, sizes) if n] if of is not None else None for of in (at, to, sizes))
+    first = at if to is None else to
+    end = list(map(add, first, sizes))
     if norm is not None:
-        first, end = np.append(first, norm), np.append(end, norm + 4)
-    order = np.argsort(first)
-    first, end = first[order], end[order]
-    if (first[1:] < end[:-1]).any():
-        raise ValueError("the same memory is written twice: no two of the tensors may overlap")
-    if to is not None and len(reads):
-        # the first written range that ends behind a gradient's beginning: its own output there and nothing else
-        k = np.searchsorted(end, reads, side="right")
-        met = k < len(first)
-        k[~met] = 0
-        met &= first[k] < reads + size
-        if (met & ((order[k] != np.arange(len(reads))) | (first[k] != reads))).any():
+        first, end = [*first, norm], [*end, norm + 4]
+    order = range(len(first))
+    if any(map(gt, end, first[1:])):               # not in order, or worse
+        order = sorted(order, key=first.__getitem__)
+        first, end = [first[i] for i in order], [end[i] for i in order]
+        if any(map(gt, end, first[1:])):
+            raise ValueError("the same memory is written twice: no two of the tensors may overlap")
+    if to is None or not at or end[-1] <= min(at) or max(map(add, at, sizes)) <= first[0]:
+        return
+    for i, (p, n) in enumerate(zip(at, sizes)):
+        k = bisect_right(end, p)                   # the first written range that ends behind p: this gradient's own, or beyond it
+        if k < len(end) and first[k] < p + n and (first[k] != p or order[k] != i):
             raise ValueError("out must not be where another gradient lies")
 
 
@@ -101,7 +100,7 @@ class GradientClip:
             for i, (t, n, dtype) in enumerate(zip(tensors, self._lengths, self._dtypes)):
                 if t.numel() != n or t.dtype != dtype or not t.is_contiguous():
                     raise ValueError(f"{name}[{i}] must be {n} contiguous elements of {dtype}")
-        return tensors, (ctypes.c_void_p * len(tensors))(*[t.data_ptr() for t in tensors])
+        return tensors, [t.data_ptr() for t in tensors]
 
     def _new(self, shape, dtype, stream):
         if stream is None:
@@ -134,8 +133,7 @@ class GradientClip:
             raise ValueError(f"norm must be one fp32 element on device {self.device_index}")
         else:
             given = norm.data_ptr()
-        if given or to is not None or len(grads) > 1:
-            _refuse_overlaps(at, to, given, self._bytes)
+        _refuse_overlaps(at, to, given, self._bytes)
         scratch = self._new(self._scratch_bytes, torch.uint8, stream)
         if unit_norms is not None:                 # (an empty tensor has no address)
             units, count = unit_norms.data_ptr() or scratch.data_ptr(), unit_norms.numel()
@@ -143,7 +141,8 @@ class GradientClip:
         if handle != self._made_on:                # the table's memory is not given away before that stream is done with it
             self._table.record_stream(torch.cuda.current_stream(self._device) if stream is None else stream)
         plan, fn = self._h, N.load().gnmr_clip_run
-        args = (plan, self._table.data_ptr(), at, to, max_norm, units, count, norm.data_ptr(), scratch.data_ptr(), self._scratch_bytes, handle)
+        places = ctypes.c_void_p * len(at)
+        args = (plan, self._table.data_ptr(), places(*at), None if to is None else places(*to), max_norm, units, count, norm.data_ptr(), scratch.data_ptr(), self._scratch_bytes, handle)
         keep = (norm, grads, outs, unit_norms, scratch, self._table)          # storage the prepared call points into
 
         def run():
