@@ -61,9 +61,10 @@ constexpr int kWarps = kThreads / 32;
 // Few warps with many loads each on their way: 2.4 GB of bf16 took the first kernel 340 us so (7.1 TB/s), with 8
 // loads a lane and four CTAs an SM 377, with two 569.
 constexpr int kUnroll = 16, kSquaresCtas = 2;          // 16-byte loads a lane; CTAs an SM
-// The second kernel, into other memory: CTAs of 64 KB, as they come, with 8 loads a lane: 2.4 GB 720 us (7.0 TB/s moved), 8 CTAs an
+// The second kernel, into other memory: CTAs of 64 KB, as they come, with 8 loads a lane: 2.4 GB 720 us (6.7 TB/s moved), 8 CTAs an
 // SM that stay 763; 256 MB 83.  In place most calls end with the limit not reached, and then the CTAs are what they cost: 64 an
-// SM 85 us, 4 4 us more than 2.
+// SM 85 us, 4 4 us more than 2.  Calls that do scale in place pay for so few: 2.4 GB 1025 us by given norms (4.7 TB/s moved), 1381 with
+// the norm's reading; 268 MB 107 and 137.  Three types' loops in one kernel spill: 384 bytes a thread stored into other memory, 508 in place.
 constexpr int kBothCtas = 256, kBothLeast = 4, kInPlaceCtas = 2;
 constexpr int64_t kBothUnits = 128;                    // of a CTA, beyond kBothLeast an SM
 constexpr int kMostSquares = 512;                      // the first kernel's CTAs, each with a partial sum
@@ -189,7 +190,9 @@ template <typename T, int kBatch> __device__ __forceinline__ void scale_batch(co
         }
 }
 
-// n elements scaled, by a warp, the last ones first: those that the first kernel read last are still in L2.
+// n elements scaled, by a warp, the last ones first: those that the first kernel read last are still in L2.  An output that starts otherwise
+// than its gradient, seen from multiples of 16 bytes, is written by elements, one a lane: 2.4 GB 3.8 ms with the norm, where alike starts
+// take 1.06; 268 MB 0.43 and 0.13.
 template <typename T, int kBatch> __device__ __forceinline__ void scale_part(const T *in, T *out, int64_t n, float scale, int lane)
 {
     constexpr int kV = kIn16<T>;

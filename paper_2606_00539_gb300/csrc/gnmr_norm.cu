@@ -11,11 +11,16 @@
 //   forward   up to 4 KB a warp a row; wider ones 2 to 16 warps; odd starts by pairs of elements; few rows a CTA each
 //   backward  a CTA has the same columns of every row it takes, so that the sums over the rows stay in its registers; each CTA's go
 //             to memory, and a second kernel adds them up in their order.  Rows past 16 KB (32 KB in fp32): these sums by strips
-//             of columns, which need no sums over a row, and dx by a kernel like the forward's
+//             of columns, which need no sums over a row, and dx by a kernel like the forward's, up to 64 KB (16-bit rows with
+//             an fp32 weight, which lies in shared memory too: 25,088 columns)
+//
+// What is beyond is read three times, and from memory or L2: backward, wider rows and odd starts past 8,190 columns; forward, rows past 128 KB
+// and odd starts past 32,768 columns.  Forward, odd starts past 12,286 columns are read once, by single elements.
 //
 // Measured (one GB300, bf16 unless said; us, and TB/s of what is read and written once): 16384 x 5120 forward 56 (6.0), backward
 // 92 (5.4); 16384 x 2048 20.5 (6.5) and 45; 4096 x 8192 27 (5.0) and 48; 8192 x 5120 fp32 61 (5.5) and 86 (5.8);
-// 16384 x 1371, odd starts, 32 (2.8) and 64; 2000 x 16384 29 (4.5) and 80; one row of 5120 2.7 and 8.  The backward kernel
+// 16384 x 1371, odd starts, 32 (2.8) and 64; 2000 x 16384 29 (4.5) and 80; one row of 5120 2.7 and 8; 2000 x 20001, odd starts, 230 and
+// 191; 2048 x 32768, an fp32 weight, 96 and 383.  The backward kernel
 // is bound by its threads' latency: 10 warps of 168 registers, instructions issued 42 % of the time.  Two turns in flight at
 // once, twice the warps with half the registers, and a scalar in place of the paired arithmetic were slower.
 #include <algorithm>

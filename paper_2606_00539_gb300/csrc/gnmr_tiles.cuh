@@ -395,10 +395,10 @@ __device__ __forceinline__ void finish(const Product &p, const Item &it, uint32_
 // columns of a lane pair are exchanged, so that the even lane forms the first column's h and the odd
 // lane the second's; then two lane pairs exchange h's of four columns, so that each thread stores
 // two outputs of one column.  A warp's outputs of a column are 32 contiguous bytes: whole sectors, which L2 puts together.
-// h costs an exchange and an activation (two special-function operations) for each of 128 sums a thread, hidden
-// behind the next tile's multiplies: 49,152 rows of 64 x 1408 x 2048 take 330 us (1.7 PFLOP/s) where the plain product of
-// both projections takes 345 to 385; the projections kept as well, 277 MB more, 356 to 413.  With a predicate at every store
-// they took 438.
+// h costs an exchange and an activation (two special-function operations) for each of 64 sums a thread, hidden
+// behind the next tile's multiplies: 49,152 rows of 64 x 1408 x 2048 take 347 us in a burst of 20 (1.6 PFLOP/s) where the plain product of
+// both projections takes 345 to 385, and 393 over seconds, at the power limit; the projections kept as well, 277 MB more, 366 and
+// 416.  With a predicate at every store they took 438.
 template <int kPieces, int kType, int kAct>
 __device__ __forceinline__ void finish_gated(const Product &p, const Item &it, uint32_t (&acc)[kPieces][16], int lane, int col, int span)
 {
